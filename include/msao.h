@@ -466,6 +466,162 @@ typedef struct {
 msao_status msao_draft_entropy(msao_ctx* ctx, const void* logits, int64_t rows, int64_t vocab, int64_t row_stride,
                                int dtype, float theta, const msao_entropy_out* out, void* stream);
 
+/* ---- Sec. 4.2: the paged cache that drafts are verified over ----------------- */
+
+/* The keys and values that a model's attention layer keeps of `n_seqs`
+ * sequences, in pages of page_size tokens. Token j of sequence s lies in page
+ * pages[s * table_stride + j / page_size] at slot j % page_size; the row of kv
+ * head h there starts at element page * stride[0] + h * stride[1] + slot *
+ * stride[2] of k (k_stride) and v (v_stride), head_dim values. length[s] counts
+ * the sequence's tokens, those of the running step among them (see msao_chunk).
+ * weight, if not NULL, holds the attention weight that each cached token has
+ * received: of token j, sequence s and kv head h at (s * kv_heads + h) *
+ * weight_stride + j.
+ *
+ * dtype MSAO_F32 or MSAO_BF16; head_dim a multiple of 8, at most
+ * MSAO_MAX_HEAD_DIM; page_size a power of two, 16 .. 65536; the capacity
+ * pages_per_seq * page_size at most 2^29; k, v and every stride multiples of 16
+ * bytes, a token's stride at least head_dim elements and below 2^26 bytes;
+ * weight_stride at least the capacity.
+ *
+ * pages, length and the pages' contents are read when the kernels run, so a
+ * captured graph follows them from replay to replay. A length outside [0,
+ * capacity] counts as the nearer end. A page outside [0, n_pages) is no page:
+ * nothing is stored there, what lies there is no token for attention, and
+ * eviction takes zeros from it. Sequences may share pages that are only read; a
+ * page that a call stores to belongs to one sequence. Memory past a sequence's
+ * length may hold anything, infinities and NaN included. */
+#define MSAO_MAX_HEAD_DIM 256
+typedef struct {
+    void* k;
+    void* v;
+    int64_t k_stride[3];       /* elements between pages, kv heads, tokens */
+    int64_t v_stride[3];
+    int32_t dtype;
+    int32_t head_dim;
+    int32_t kv_heads;
+    int32_t page_size;
+    int32_t n_pages;
+    int32_t n_seqs;
+    int32_t pages_per_seq;
+    int64_t table_stride;      /* elements between the rows of `pages`, >= pages_per_seq */
+    const int32_t* pages;      /* device [n_seqs][table_stride] */
+    int32_t* length;           /* device [n_seqs] */
+    float* weight;             /* device [n_seqs][kv_heads][weight_stride] or NULL */
+    int64_t weight_stride;
+} msao_kv_cache;
+
+/* The new tokens of one step: rows start[s] .. start[s+1]-1 of the step's
+ * arrays are the last tokens of sequence s, whose length counts them already
+ * (row start[s] + i is its token length[s] - n + i with n = start[s+1] -
+ * start[s]). start is device memory, ascending; entries are taken into [0,
+ * n_rows], a sequence whose end lies before its start has no rows. Rows of no
+ * sequence are left as they are. max_new: host's bound on n; of a sequence with
+ * more rows msao_cache_attention leaves those from max_new on as they are. */
+typedef struct {
+    const int32_t* start;      /* device [n_seqs + 1] */
+    int32_t n_rows;            /* rows of the step's arrays */
+    int32_t max_new;
+} msao_chunk;
+
+/* Check a cache and a chunk (NULL: none) without touching any device. */
+msao_status msao_cache_validate(const msao_kv_cache* cache, const msao_chunk* chunk);
+
+/* Neighbouring values (2i, 2i+1) are a pair of the rotation; without the flag
+ * (i, i + rot_dim/2). */
+#define MSAO_APPEND_NEIGHBOURS 1u
+#define MSAO_MAX_AXES 4
+
+/* What msao_cache_append takes besides the cache. Rows are of the cache's dtype;
+ * the heads of a row follow one another (head h at h * head_dim), strides are in
+ * elements between rows. Pointers and strides are multiples of 16 bytes.
+ *   q -> q_out [n_rows][heads * head_dim]: may be the same memory; NULL with heads 0.
+ *   k, v [n_rows][kv_heads * head_dim].
+ *   q_norm, k_norm [head_dim] or NULL: a head x becomes x / sqrt(mean(x^2) + eps) * norm.
+ *   Then the first rot_dim values (a multiple of 16, at most head_dim; 0: none) turn
+ *   by pairs: (a, b) -> (a cos t - b sin t, a sin t + b cos t), where pair i has the
+ *   angle t = position * inv_freq[i] (inv_freq: device [rot_dim/2] float), taken in 64
+ *   bits. The position is positions[a * position_stride + row] (device) for the axis a
+ *   to which sections (pairs per axis, summing to rot_dim/2) assign pair i, or with
+ *   positions NULL the token's place in the cache (n_axes 1).
+ * Norm and rotation are computed in 32 bits and rounded once. */
+typedef struct {
+    const void* q;
+    void* q_out;
+    const void* k;
+    const void* v;
+    int64_t q_stride, q_out_stride, k_stride, v_stride;
+    const void* q_norm;
+    const void* k_norm;
+    float eps;                 /* finite, >= 0 */
+    int32_t heads;
+    int32_t rot_dim;
+    const float* inv_freq;
+    const int32_t* positions;
+    int64_t position_stride;   /* >= n_rows */
+    int32_t n_axes;            /* 1 .. MSAO_MAX_AXES */
+    int32_t sections[MSAO_MAX_AXES];
+    uint32_t flags;            /* MSAO_APPEND_* */
+} msao_append;
+
+/* The chunk's queries and keys normed and rotated, its keys and values stored in
+ * the cache, their weight (if the cache has it) set to 0. q_out is written for
+ * every row of a sequence, also where its key has no page. */
+msao_status msao_cache_append(msao_ctx* ctx, const msao_kv_cache* cache, const msao_chunk* chunk,
+                              const msao_append* in, void* stream);
+
+#define MSAO_ATTEND_CAUSAL 1u  /* row i of n sees tokens 0 .. length - n + i; without it every token */
+#define MSAO_ATTEND_WEIGHT 2u  /* add to the cache's weight what each token receives */
+
+/* Attention of the chunk's queries over their sequences' caches: the drafts of a
+ * speculative round (n up to 1 + N_draft), single generated tokens, chunks of
+ * prompts, or (not causal) any queries over an encoder's states.
+ *     s_ij = scale q_i . k_j,  lse_i = ln sum_j exp(s_ij),  p_ij = exp(s_ij - lse_i),  out_i = sum_j p_ij v_j
+ * over the tokens j that row i sees. Query head h reads kv head h / (heads /
+ * kv_heads). q, out [n_rows][heads * head_dim] of the cache's dtype, 16-byte
+ * aligned with strides (elements between rows) of 16-byte multiples; out must not
+ * overlap q. lse: device [n_rows][heads] or NULL. A row that sees no token, or
+ * only scores of -inf, gets out 0 and lse -inf and adds no weight; what a row does
+ * not see has no effect on it, whatever it holds. With MSAO_ATTEND_WEIGHT, weight
+ * of (s, kv head, j) grows by the sum of p_ij over the chunk's rows and the query
+ * heads of the kv head; the order of every sum is fixed: the same call gives the
+ * same bits. For bf16, the p_ij that multiply v are rounded to bf16; sums, lse and
+ * weight are not. Workspace from msao_cache_attention_workspace, used only while
+ * the call runs on the GPU. */
+msao_status msao_cache_attention(msao_ctx* ctx, const msao_kv_cache* cache, const msao_chunk* chunk, const void* q,
+                                 int64_t q_stride, int heads, float scale, uint32_t flags, void* out,
+                                 int64_t out_stride, float* lse, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+msao_status msao_cache_attention_workspace(const msao_kv_cache* cache, const msao_chunk* chunk, int heads,
+                                           uint32_t flags, size_t* bytes);
+
+/* Eviction by the accumulated weight: of each sequence s the k = min(length[s],
+ * max(budget[s], 0), capacity of `to`) tokens that stay are, for each kv head on
+ * its own, the first min(n_first, k), the last min(n_recent, the rest of k), and
+ * of those between them the ones of largest weight (ties: the lower index; NaN
+ * and what is not above 0 counts as 0). They move to tokens 0 .. k-1 of `to` in
+ * their order: keys, values and, if `to` has it, weight; to->length[s] becomes k.
+ * to NULL: the same cache in place. Otherwise `to` has the same dtype, head_dim,
+ * kv_heads and n_seqs, its pages and arrays share no memory with those of `from`, and
+ * `from` stays as it is. kept_idx (device [n_seqs][kv_heads][idx_stride], idx_stride
+ * at least the capacity of `from`): the tokens that stay, ascending, then -1 up to
+ * the capacity. budget: device [n_seqs]. Workspace from msao_cache_evict_workspace. */
+msao_status msao_cache_evict(msao_ctx* ctx, const msao_kv_cache* from, const msao_kv_cache* to,
+                             const int32_t* budget, int n_first, int n_recent, int32_t* kept_idx,
+                             int64_t idx_stride, void* workspace, size_t workspace_bytes, void* stream);
+msao_status msao_cache_evict_workspace(const msao_kv_cache* from, size_t* bytes);
+
+/* Mean milliseconds per launch of the cache's kernels since the previous query,
+ * as msao_kernel_times gives them for the others. */
+#define MSAO_CACHE_KERNEL_APPEND 0
+#define MSAO_CACHE_KERNEL_ATTEND 1
+#define MSAO_CACHE_KERNEL_COMBINE 2   /* parts of split rows joined */
+#define MSAO_CACHE_KERNEL_WEIGHT 3
+#define MSAO_CACHE_KERNEL_SELECT 4    /* eviction: the tokens that stay */
+#define MSAO_CACHE_KERNEL_MOVE 5      /* eviction: their keys and values */
+#define MSAO_NUM_CACHE_KERNELS 6
+msao_status msao_cache_kernel_times(msao_ctx* ctx, float* ms);
+
 /* ---- Sec. 4.2.2: Algorithm 1 on the host ----------------------------------- */
 
 /* Parameters of Algorithm 1 (defaults from Sec. 5.1: P_target 0.8, N_max 5,

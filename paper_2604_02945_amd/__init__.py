@@ -15,4 +15,5 @@ from .binding import (  # noqa: F401
     expected_spec_tokens, msao_draft_entropy, p_conf, retention_floor, sched_default_params,
     msao_mas_score_learned, msao_temporal_simhash, msao_run_simhash, FLAG_SELECT_PER_FRAME,
     msao_run_noalloc, msao_stream_read, msao_run_learned,
+    KvCache, cache_attention_workspace, msao_cache_append, msao_cache_attention, msao_cache_evict,
 )

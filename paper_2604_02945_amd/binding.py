@@ -7,6 +7,7 @@ module never falls back to anything else.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import dataclasses
 import os
@@ -26,6 +27,11 @@ FLAG_SELECT_PER_FRAME = 2
  KERNEL_CLIP, KERNEL_READ, NUM_KERNELS) = 0, 1, 2, 3, 4, 5, 6, 7, 8, 9
 MODAL_DESC = 8
 DECIDE_HOLD, DECIDE_SEND, DECIDE_OFFLOAD = 0, 1, 2
+MAX_AXES = 4
+APPEND_NEIGHBOURS = 1
+ATTEND_CAUSAL, ATTEND_WEIGHT = 1, 2
+(CACHE_KERNEL_APPEND, CACHE_KERNEL_ATTEND, CACHE_KERNEL_COMBINE, CACHE_KERNEL_WEIGHT, CACHE_KERNEL_SELECT,
+ CACHE_KERNEL_MOVE, NUM_CACHE_KERNELS) = 0, 1, 2, 3, 4, 5, 6
 
 STATUS = {0: "MSAO_OK", 1: "MSAO_ERR_INVALID_ARG", 2: "MSAO_ERR_ALIGNMENT", 3: "MSAO_ERR_WORKSPACE",
           4: "MSAO_ERR_UNSUPPORTED", 5: "MSAO_ERR_HIP"}
@@ -97,6 +103,26 @@ class MsaoLatencyModel(ctypes.Structure):
                 ("t_draft", ctypes.c_double), ("t_verify", ctypes.c_double), ("t_offload", ctypes.c_double)]
 
 
+class MsaoKvCache(ctypes.Structure):
+    _fields_ = [("k", _P), ("v", _P), ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3),
+                ("dtype", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("n_seqs", ctypes.c_int32),
+                ("pages_per_seq", ctypes.c_int32), ("table_stride", ctypes.c_int64), ("pages", _P), ("length", _P),
+                ("weight", _P), ("weight_stride", ctypes.c_int64)]
+
+
+class MsaoChunk(ctypes.Structure):
+    _fields_ = [("start", _P), ("n_rows", ctypes.c_int32), ("max_new", ctypes.c_int32)]
+
+
+class MsaoAppend(ctypes.Structure):
+    _fields_ = [("q", _P), ("q_out", _P), ("k", _P), ("v", _P), ("q_stride", ctypes.c_int64),
+                ("q_out_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("q_norm", _P), ("k_norm", _P), ("eps", ctypes.c_float), ("heads", ctypes.c_int32),
+                ("rot_dim", ctypes.c_int32), ("inv_freq", _P), ("positions", _P), ("position_stride", ctypes.c_int64),
+                ("n_axes", ctypes.c_int32), ("sections", ctypes.c_int32 * MAX_AXES), ("flags", ctypes.c_uint32)]
+
+
 class MsaoError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"{STATUS.get(status, status)}: {message}")
@@ -145,6 +171,15 @@ SIGNATURES = [
                                         ctypes.c_int64, _P, ctypes.c_size_t, _P]),
     ("msao_draft_entropy", ctypes.c_int, [_P, _P, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int,
                                           ctypes.c_float, _P, _P]),
+    ("msao_cache_validate", ctypes.c_int, [_P, _P]),
+    ("msao_cache_append", ctypes.c_int, [_P, _P, _P, _P, _P]),
+    ("msao_cache_attention", ctypes.c_int, [_P, _P, _P, _P, ctypes.c_int64, ctypes.c_int, ctypes.c_float,
+                                            ctypes.c_uint32, _P, ctypes.c_int64, _P, _P, ctypes.c_size_t, _P]),
+    ("msao_cache_attention_workspace", ctypes.c_int, [_P, _P, ctypes.c_int, ctypes.c_uint32, _P]),
+    ("msao_cache_evict", ctypes.c_int, [_P, _P, _P, _P, ctypes.c_int, ctypes.c_int, _P, ctypes.c_int64, _P,
+                                        ctypes.c_size_t, _P]),
+    ("msao_cache_evict_workspace", ctypes.c_int, [_P, _P]),
+    ("msao_cache_kernel_times", ctypes.c_int, [_P, _P]),
     ("msao_stream_read", ctypes.c_int, [_P, _P, ctypes.c_int64, ctypes.c_int, _P, ctypes.c_int64, _P]),
     ("msao_sched_default_params", MsaoSchedParams, []),
     ("msao_sched_init", ctypes.c_int, [_P, ctypes.c_int64, _P, _P]),
@@ -274,6 +309,11 @@ class Context:
     def kernel_times(self) -> List[float]:
         ms = (ctypes.c_float * NUM_KERNELS)()
         _check(lib().msao_kernel_times(self.handle, ms), self)
+        return list(ms)
+
+    def cache_kernel_times(self) -> List[float]:
+        ms = (ctypes.c_float * NUM_CACHE_KERNELS)()
+        _check(lib().msao_cache_kernel_times(self.handle, ms), self)
         return list(ms)
 
 
@@ -696,6 +736,253 @@ def msao_stream_read(data: torch.Tensor, chunk_kib: int = 8, ctx: Optional[Conte
     _check(lib().msao_stream_read(ctx.handle, _ptr(data), nbytes, int(chunk_kib), _ptr(sink), sink.numel(),
                                   st), ctx)
     return sink
+
+
+# ---- Sec. 4.2: the paged cache that drafts are verified over -------------------
+
+def _same_device(device: torch.device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} is on {t.device}, the cache on {device}")
+
+
+def _int32(name: str, t: torch.Tensor, dim: int):
+    if t.dtype != torch.int32 or t.dim() != dim:
+        raise ValueError(f"{name} must be a {dim}-D int32 tensor")
+    if t.numel() and t.stride(-1) != 1:
+        raise ValueError(f"{name} must be contiguous in its last dimension")
+
+
+def _head_rows(name: str, t: torch.Tensor, dtype: torch.dtype, heads: Optional[int], dim: int) -> int:
+    """Elements between the rows of a [rows, heads, dim] tensor whose heads follow one another."""
+    if t.dim() != 3 or t.shape[2] != dim or (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{name} must be [rows, {'heads' if heads is None else heads}, {dim}]")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be of the cache's dtype")
+    if t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != dim)):
+        raise ValueError(f"the heads of {name} must follow one another")
+    return int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1]) * dim
+
+
+class KvCache:
+    """A paged cache (msao_kv_cache) over the caller's tensors: k and v [n_pages,
+    kv_heads, page_size, head_dim] (float32 or bfloat16; pages, heads and tokens at
+    any strides of 16-byte multiples, so a pool that interleaves them is a
+    permuted view), pages int32 [n_seqs, pages_per_seq], length int32 [n_seqs],
+    weight float32 [n_seqs, kv_heads, >= capacity] or None. The tensors are used in
+    place and kept alive; what they hold is read when the kernels run."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, pages: torch.Tensor, length: torch.Tensor,
+                 weight: Optional[torch.Tensor] = None):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype:
+            raise ValueError("k and v must be [n_pages, kv_heads, page_size, head_dim] of one dtype")
+        if k.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("k and v must be float32 or bfloat16")
+        if k.numel() and (k.stride(3) != 1 or v.stride(3) != 1):
+            raise ValueError("the head_dim values of a token must be contiguous")
+        _int32("pages", pages, 2)
+        _int32("length", length, 1)
+        _same_device(k.device, v=v, pages=pages, length=length, weight=weight)
+        n_seqs = int(length.shape[0])
+        if pages.shape[0] != n_seqs:
+            raise ValueError("pages and length differ in n_seqs")
+        self.k, self.v, self.pages, self.length, self.weight = k, v, pages, length, weight
+        self.device, self.dtype, self.n_seqs = k.device, k.dtype, n_seqs  # (a tensor's cuda device has an index)
+        self.n_pages, self.kv_heads, self.page_size, self.head_dim = (int(x) for x in k.shape)
+        self.pages_per_seq = int(pages.shape[1])
+        self.capacity = self.pages_per_seq * self.page_size
+        c = self.struct = MsaoKvCache()
+        c.k, c.v = (k.data_ptr(), v.data_ptr()) if k.numel() else (None, None)
+        for i in range(3):
+            c.k_stride[i], c.v_stride[i] = k.stride(i), v.stride(i)
+        c.dtype = F32 if k.dtype == torch.float32 else BF16
+        c.head_dim, c.kv_heads, c.page_size, c.n_pages = self.head_dim, self.kv_heads, self.page_size, self.n_pages
+        c.n_seqs, c.pages_per_seq = n_seqs, self.pages_per_seq
+        c.table_stride = pages.stride(0) if n_seqs > 1 else self.pages_per_seq
+        c.pages, c.length = pages.data_ptr(), length.data_ptr()
+        if weight is not None:
+            if weight.dtype != torch.float32 or weight.dim() != 3 or tuple(weight.shape[:2]) != (n_seqs, self.kv_heads):
+                raise ValueError("weight must be float32 [n_seqs, kv_heads, capacity]")
+            if weight.shape[2] < self.capacity or not weight.is_contiguous():
+                raise ValueError("weight must be contiguous and as long as the capacity")
+            c.weight, c.weight_stride = weight.data_ptr(), weight.shape[2]
+        self.addr = _addr(c)
+        _check(lib().msao_cache_validate(self.addr, None))
+
+
+def _cache_ctx(cache: KvCache, ctx: Optional[Context], stream) -> Context:
+    if cache.device.type != "cuda":
+        raise ValueError(f"the cache is on {cache.device}, not on a GPU")
+    index = cache.device.index
+    if ctx is None:
+        ctx = default_context(index)
+    elif ctx.device != index:
+        raise ValueError(f"the context is of device {ctx.device}, the cache on {cache.device}")
+    if stream is not None and stream.device != cache.device:
+        raise ValueError(f"the stream is of {stream.device}, the cache on {cache.device}")
+    return ctx
+
+
+def _chunk(cache: KvCache, start: torch.Tensor, n_rows: int, max_new: int) -> MsaoChunk:
+    _int32("start", start, 1)
+    if start.shape[0] != cache.n_seqs + 1:
+        raise ValueError("start must have n_seqs + 1 entries")
+    _same_device(cache.device, start=start)
+    return MsaoChunk(start.data_ptr(), n_rows, int(max_new))
+
+
+def _on(stream):
+    """Memory allocated inside is `stream`'s, where the call will use it (None: the current stream's)."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def msao_cache_append(cache: KvCache, start: torch.Tensor, max_new: int, k: torch.Tensor, v: torch.Tensor,
+                      q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                      q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                      positions: Optional[torch.Tensor] = None, inv_freq: Optional[torch.Tensor] = None,
+                      sections: Optional[Sequence[int]] = None, interleaved: bool = False,
+                      ctx: Optional[Context] = None, stream=None) -> Optional[torch.Tensor]:
+    """The step's keys and values into the cache, queries and keys normed and
+    rotated: rows start[s] .. start[s+1]-1 of q [rows, heads, head_dim] and k, v
+    [rows, kv_heads, head_dim] are the last tokens of sequence s, counted by
+    cache.length already. q_norm and k_norm [head_dim] or None; inv_freq
+    float32 [pairs] (None: no rotation) turns the first 2 * pairs values by
+    positions int32 [rows] or [axes, rows] (None: the places in the cache),
+    sections naming the pairs of each axis; interleaved pairs neighbours. Returns
+    q_out (q's own memory may be passed)."""
+    ctx = _cache_ctx(cache, ctx, stream)
+    rows = int(k.shape[0]) if k.dim() else -1
+    a = MsaoAppend()
+    a.k_stride = _head_rows("k", k, cache.dtype, cache.kv_heads, cache.head_dim)
+    a.v_stride = _head_rows("v", v, cache.dtype, cache.kv_heads, cache.head_dim)
+    if v.shape[0] != rows or (q is not None and q.shape[0] != rows):
+        raise ValueError("q, k and v differ in rows")
+    a.k, a.v, a.eps = _ptr(k), _ptr(v), float(eps)
+    if q is not None:
+        a.q_stride = _head_rows("q", q, cache.dtype, None, cache.head_dim)
+        if q_out is None:
+            with _on(stream):
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if q_out.shape != q.shape:
+            raise ValueError("q_out must have q's shape")
+        a.q_out_stride = _head_rows("q_out", q_out, cache.dtype, None, cache.head_dim)
+        a.q, a.q_out, a.heads = _ptr(q), _ptr(q_out), int(q.shape[1])
+    elif q_out is not None or q_norm is not None:
+        raise ValueError("q_out and q_norm need q")
+    for name, w in (("q_norm", q_norm), ("k_norm", k_norm)):
+        if w is not None:
+            if w.dtype != cache.dtype or tuple(w.shape) != (cache.head_dim,) or not w.is_contiguous():
+                raise ValueError(f"{name} must be [head_dim] of the cache's dtype")
+            setattr(a, name, w.data_ptr())
+    if inv_freq is not None and inv_freq.numel():
+        if inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+            raise ValueError("inv_freq must be a contiguous 1-D float32 tensor")
+        a.rot_dim, a.inv_freq, a.n_axes = 2 * int(inv_freq.shape[0]), inv_freq.data_ptr(), 1
+        if positions is not None:
+            if positions.dim() == 1:
+                positions = positions[None]
+            _int32("positions", positions, 2)
+            if positions.shape[1] != rows:
+                raise ValueError("positions must be [rows] or [axes, rows]")
+            a.n_axes = int(positions.shape[0])
+            a.positions = positions.data_ptr()
+            a.position_stride = int(positions.stride(0)) if a.n_axes > 1 else rows
+        sec = list(sections) if sections is not None else [int(inv_freq.shape[0])]
+        if len(sec) != a.n_axes or a.n_axes > MAX_AXES:
+            raise ValueError("sections must name the pairs of each axis of positions (at most 4)")
+        for i, n in enumerate(sec):
+            a.sections[i] = int(n)
+    elif positions is not None or sections is not None:
+        raise ValueError("positions and sections need inv_freq")
+    _same_device(cache.device, k=k, v=v, q=q, q_out=q_out, q_norm=q_norm, k_norm=k_norm, positions=positions,
+                 inv_freq=inv_freq)
+    a.flags = APPEND_NEIGHBOURS if interleaved else 0
+    ch = _chunk(cache, start, rows, max_new)
+    st = _stream_ptr(stream, cache.device)
+    _check(lib().msao_cache_append(ctx.handle, cache.addr, _addr(ch), _addr(a), st), ctx)
+    return q_out
+
+
+def cache_attention_workspace(cache: KvCache, start: torch.Tensor, n_rows: int, max_new: int, heads: int,
+                              causal: bool = True, accumulate: bool = False) -> int:
+    """Bytes of workspace that msao_cache_attention needs for such a call."""
+    ch, n = _chunk(cache, start, n_rows, max_new), ctypes.c_size_t()
+    flags = (ATTEND_CAUSAL if causal else 0) | (ATTEND_WEIGHT if accumulate else 0)
+    _check(lib().msao_cache_attention_workspace(cache.addr, _addr(ch), heads, flags, ctypes.byref(n)))
+    return n.value
+
+
+def msao_cache_attention(cache: KvCache, start: torch.Tensor, max_new: int, q: torch.Tensor,
+                         scale: Optional[float] = None, causal: bool = True, out: Optional[torch.Tensor] = None,
+                         lse: Optional[torch.Tensor] = None, accumulate: bool = False,
+                         workspace: Optional[torch.Tensor] = None, ctx: Optional[Context] = None,
+                         stream=None) -> torch.Tensor:
+    """Attention of q [rows, heads, head_dim] (rows of sequences as for
+    msao_cache_append) over the cache; scale 1/sqrt(head_dim) when None. lse
+    float32 [rows, heads] is filled if given; accumulate adds to cache.weight what
+    each token receives. workspace: uint8, 256-byte aligned, of
+    cache_attention_workspace bytes (allocated when None). Returns out; rows of
+    no sequence keep what `out` held (0 in one allocated here)."""
+    ctx = _cache_ctx(cache, ctx, stream)
+    q_stride = _head_rows("q", q, cache.dtype, None, cache.head_dim)
+    rows, heads = int(q.shape[0]), int(q.shape[1])
+    if out is None:
+        with _on(stream):
+            out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+    if out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    out_stride = _head_rows("out", out, cache.dtype, None, cache.head_dim)
+    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (rows, heads) or not lse.is_contiguous()):
+        raise ValueError("lse must be contiguous float32 [rows, heads]")
+    _same_device(cache.device, q=q, out=out, lse=lse, workspace=workspace)
+    ch = _chunk(cache, start, rows, max_new)
+    flags = (ATTEND_CAUSAL if causal else 0) | (ATTEND_WEIGHT if accumulate else 0)
+    need = ctypes.c_size_t()
+    _check(lib().msao_cache_attention_workspace(cache.addr, _addr(ch), heads, flags, ctypes.byref(need)))
+    if workspace is None:
+        with _on(stream):
+            workspace = _workspace(need.value, cache.device)
+    st = _stream_ptr(stream, cache.device)
+    _check(lib().msao_cache_attention(ctx.handle, cache.addr, _addr(ch), _ptr(q), q_stride, heads,
+                                      cache.head_dim ** -0.5 if scale is None else float(scale), flags, _ptr(out),
+                                      out_stride, _ptr(lse), _ptr(workspace),
+                                      ctypes.c_size_t(workspace.numel() * workspace.element_size()), st), ctx)
+    return out
+
+
+def msao_cache_evict(cache: KvCache, budget: torch.Tensor, n_first: int = 0, n_recent: int = 0,
+                     to: Optional[KvCache] = None, kept_idx: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None, ctx: Optional[Context] = None,
+                     stream=None) -> Dict[str, torch.Tensor]:
+    """Each sequence cut to its budget (int32 [n_seqs]) by the accumulated weight,
+    per kv head, with the first n_first and the last n_recent tokens kept; into
+    `to` or, when None, in place. Lengths (and weight) of the target are updated on
+    the device. Returns kept_idx, int32 [n_seqs, kv_heads, capacity]: the kept
+    tokens ascending, then -1; and kept_count, the target's lengths."""
+    ctx = _cache_ctx(cache, ctx, stream)
+    _int32("budget", budget, 1)
+    if budget.shape[0] != cache.n_seqs:
+        raise ValueError("budget must have n_seqs entries")
+    if to is not None and to.device != cache.device:
+        raise ValueError("the caches are on different devices")
+    if kept_idx is None:
+        with _on(stream):
+            kept_idx = torch.empty(cache.n_seqs, cache.kv_heads, cache.capacity, dtype=torch.int32,
+                                   device=cache.device)
+    if (kept_idx.dtype != torch.int32 or kept_idx.dim() != 3 or not kept_idx.is_contiguous()
+            or tuple(kept_idx.shape[:2]) != (cache.n_seqs, cache.kv_heads) or kept_idx.shape[2] < cache.capacity):
+        raise ValueError("kept_idx must be contiguous int32 [n_seqs, kv_heads, capacity]")
+    _same_device(cache.device, budget=budget, kept_idx=kept_idx, workspace=workspace)
+    need = ctypes.c_size_t()
+    _check(lib().msao_cache_evict_workspace(cache.addr, ctypes.byref(need)))
+    if workspace is None:
+        with _on(stream):
+            workspace = _workspace(need.value, cache.device)
+    st = _stream_ptr(stream, cache.device)
+    _check(lib().msao_cache_evict(ctx.handle, cache.addr, to.addr if to is not None else None, _ptr(budget),
+                                  int(n_first), int(n_recent), _ptr(kept_idx), kept_idx.shape[2], _ptr(workspace),
+                                  ctypes.c_size_t(workspace.numel() * workspace.element_size()), st), ctx)
+    return {"kept_idx": kept_idx, "kept_count": (to or cache).length}
 
 
 def sched_default_params() -> MsaoSchedParams:

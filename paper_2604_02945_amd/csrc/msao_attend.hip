@@ -1,0 +1,709 @@
+// msao_attend.hip -- gfx950 (CDNA4) kernels for attention of a chunk of new tokens
+// over a paged cache, and for the attention weight that each cached token receives.
+//
+// Rows of a (sequence, kv head) are its n new tokens times the `group` query heads
+// that share the kv head: all of them read the same keys and values, so they fill the
+// columns of the matrix instructions, and K and V are read once for up to 64 rows.
+//
+// k_attend: a wavefront takes 32 tokens at a time, K and V straight from memory into
+// registers in whole rows, and nothing through LDS:
+//   S^T = K Q^T    A operand: lane (c, i) holds 16 bytes of token i's row
+//   O^T = V^T P^T  S^T leaves lane (c, q) with tokens 4c..4c+3 of each 16, which is a
+//                  B operand as it stands once the instruction's k index is read as
+//                  those tokens; its A operand wants, of the same tokens, one channel a
+//                  lane: lane (c, i) loads channels [i*E, i*E+E) (E = padded dim / 16)
+//                  of tokens 4c..4c+3 and turns the block round with byte permutes.
+// The wavefronts of a workgroup take tiles in turn and join at the end through LDS;
+// workgroups that share a row's tokens leave parts in the workspace, which k_combine
+// joins. The running maximum is a reference that moves only when a score passes it by
+// more than 2^kSlack, so most tiles need no reduction across lanes and no rescaling.
+#include <hip/hip_ext.h>
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "msao_cache.h"
+#include "msao_device.h"
+#include "msao_internal.h"
+
+namespace msao {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
+
+constexpr int kWave = 64;
+constexpr int kBlock = 256;
+constexpr int kWaves = kBlock / kWave;
+constexpr float kSlack = 8.0f;     // log2 units a score may pass the reference by
+constexpr int kFar = 0x7FFFFF00;   // an offset past every buffer: the load gives zeros
+constexpr float kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ rsrc_t rsrc(const void* base, int bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, bytes, 0x00020000);
+}
+
+__device__ __forceinline__ const uint8_t* uniform(const uint8_t* p)
+{
+    const uint64_t v = (uint64_t)p;
+    return (const uint8_t*)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
+}
+
+template <int DT> struct Type;
+template <> struct Type<kBF16> { static constexpr int kSize = 2; };
+template <> struct Type<kF32> { static constexpr int kSize = 4; };
+
+// 32-bit words that hold E values, loaded in pieces of 16 or 8 bytes.
+template <int W>
+__device__ __forceinline__ void load_words(uint32_t (&w)[W], rsrc_t r, int off)
+{
+    static_assert(W == 2 || W % 4 == 0, "");
+    if constexpr (W == 2) {
+        const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
+        w[0] = v.x;
+        w[1] = v.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < W / 4; ++i) {
+            const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(r, off + 16 * i, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[4 * i + e] = v[e];
+        }
+    }
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
+{
+    const f32x2 v = {a, b};
+    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf2));
+}
+
+// Whether a 32-bit word of values holds an infinity or a NaN; and the word without them.
+template <int DT>
+__device__ __forceinline__ bool strange(uint32_t w)
+{
+    if constexpr (DT == kF32) return (w & 0x7F800000u) == 0x7F800000u;
+    return (w & 0x7F800000u) == 0x7F800000u || (w & 0x7F80u) == 0x7F80u;
+}
+template <int DT>
+__device__ __forceinline__ uint32_t without_strange(uint32_t w)
+{
+    if constexpr (DT == kF32) return strange<DT>(w) ? 0u : w;
+    return ((w & 0x7F800000u) == 0x7F800000u ? 0u : w & 0xFFFF0000u) | ((w & 0x7F80u) == 0x7F80u ? 0u : w & 0xFFFFu);
+}
+
+// Which (sequence, kv head, ...) a block of the flattened grid has.
+struct Place {
+    int seq, head, n_new, begin, length;
+};
+__device__ __forceinline__ Place place_of(const AttendArgs& a, int sh)
+{
+    Place p;
+    p.seq = sh / a.c.kv_heads;
+    p.head = sh - p.seq * a.c.kv_heads;
+    const Rows r = seq_rows(a.ch, p.seq);
+    p.begin = r.begin;
+    p.n_new = r.n;
+    p.length = seq_length(a.c, p.seq);
+    return p;
+}
+
+// Rows of the sequence that the call computes (max_new bounds the grid).
+__device__ __forceinline__ int call_rows(const AttendArgs& a, const Place& p) { return min(p.n_new, a.ch.max_new) * a.group; }
+
+// Pages of 64 half tiles (16 tokens) of a wavefront, one a lane: lane i has half i % NH of
+// tile first + i / NH of those the wavefront takes (every kWaves-th of NH halves).
+template <int NH>
+__device__ __forceinline__ int lane_pages(const CacheDev& c, int seq, int lo, int hi, int wave, int first)
+{
+    const int lane = threadIdx.x & (kWave - 1);
+    const int64_t tok = (int64_t)lo + 16 * NH * (wave + kWaves * ((int64_t)first + lane / NH)) + 16 * (lane % NH);
+    return tok < hi ? page_at(c, seq, (int)(tok >> c.page_shift)) : -1;
+}
+
+// A 16-token half tile: its buffers and how many of its tokens there are.
+struct Half {
+    rsrc_t r;
+    int n;
+};
+__device__ __forceinline__ Half half_of(const uint8_t* base, int64_t page_bytes, int64_t tok_bytes, int row_bytes, int page,
+                                        int tok, int hi, int mask)
+{
+    Half h;
+    h.n = page < 0 ? 0 : clamp_int(hi - tok, 0, 16);
+    h.n = uniform(h.n);
+    const int64_t off = page < 0 ? 0 : (int64_t)page * page_bytes + (int64_t)(tok & mask) * tok_bytes;
+    h.r = rsrc(uniform(base + off), uniform(h.n > 0 ? (h.n - 1) * (int)tok_bytes + row_bytes : 0));
+    return h;
+}
+
+// The queries of 16 rows as B operands: lane (c, i) row i, 16 bytes from channel
+// (16 bytes) * (4 s + c) for step s. Rows past the last are zeros.
+template <int DT, int DP>
+struct Query {
+    static constexpr int kSteps = DP * Type<DT>::kSize / 64;
+    u32x4 v[kSteps];
+    __device__ __forceinline__ void load(const AttendArgs& a, const Place& p, int row, int n_rows)
+    {
+        const int c = (threadIdx.x & (kWave - 1)) >> 4;
+        const int tok = row / a.group, head = p.head * a.group + (row - tok * a.group);
+        const uint8_t* src = a.q + (int64_t)(p.begin + tok) * a.q_stride + (int64_t)head * a.c.dim * Type<DT>::kSize;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const int off = 64 * s + 16 * c;
+            v[s] = row < n_rows && off < a.c.dim * Type<DT>::kSize ? *(const u32x4*)(src + off) : u32x4{0, 0, 0, 0};
+        }
+    }
+};
+
+// Scores of 16 tokens (rows of the result: lane (c, q) tokens 4c + r) and 16 queries.
+template <int DT, int DP>
+__device__ __forceinline__ f32x4 scores(const u32x4 (&k)[DP * Type<DT>::kSize / 64], const Query<DT, DP>& q)
+{
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < DP * Type<DT>::kSize / 64; ++i) {
+        if constexpr (DT == kBF16) {
+            s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[i]), __builtin_bit_cast(bf16x8, q.v[i]),
+                                                        s, 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                s = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[i][e]), __uint_as_float(q.v[i][e]), s, 0, 0, 0);
+        }
+    }
+    return s;
+}
+
+// Offsets of a lane's pieces of a row of K; channels past the head read as zeros.
+template <int DT, int DP>
+struct KeyOffsets {
+    int off[DP * Type<DT>::kSize / 64];
+    __device__ __forceinline__ KeyOffsets(int64_t tok_bytes, int row_bytes)
+    {
+        const int lane = threadIdx.x & (kWave - 1), i = lane & 15, c = lane >> 4;
+#pragma unroll
+        for (int s = 0; s < DP * Type<DT>::kSize / 64; ++s) {
+            const int at = 64 * s + 16 * c;
+            off[s] = at < row_bytes ? i * (int)tok_bytes + at : kFar;
+        }
+    }
+};
+
+template <int DT, int DP, int MT>
+__global__ __launch_bounds__(kBlock) void k_attend(AttendArgs a)
+{
+    constexpr int ES = Type<DT>::kSize;
+    constexpr int KS = DP * ES / 64;   // pieces of a row of K a lane holds
+    constexpr int E = DP / 16;         // channels of V a lane holds of a token
+    constexpr int VW = E * ES / 4;     // as 32-bit words
+    // halves of a tile; float32 heads of 256 keep one of K and V in registers
+    constexpr int NH = DT == kF32 && DP == 256 ? 1 : 2, TT = 16 * NH;
+    constexpr int LDP = DP + 4;        // floats between rows in LDS: spreads the banks
+    __shared__ __align__(16) float lds_o[kWaves][16][LDP];
+    __shared__ float lds_m[kWaves][MT * 16], lds_l[kWaves][MT * 16];
+
+    const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
+    const int i16 = lane & 15, c = lane >> 4;
+    int id = blockIdx.x;
+    const int split = id % a.splits;
+    id /= a.splits;
+    const int tile = id % a.row_tiles;
+    const Place p = place_of(a, id / a.row_tiles);
+    const int n_rows = call_rows(a, p), r0 = tile * MT * 16;
+    if (r0 >= n_rows) return;
+    const int r_end = min(r0 + MT * 16, n_rows);
+    const int seen = group_sees(p.length, p.n_new, a.group, r_end - 1, a.causal);
+    const Cut cut = cut_tokens(seen, a.splits);
+    if (split >= max(cut.n, 1)) return;
+    const int lo = split * cut.per, hi = min(seen, lo + cut.per);
+
+    const int row_bytes = a.c.dim * ES, mask = (1 << a.c.page_shift) - 1;
+    const uint8_t* kb = a.c.k + (int64_t)p.head * a.c.k_head;
+    const uint8_t* vb = a.c.v + (int64_t)p.head * a.c.v_head;
+    const KeyOffsets<DT, DP> ko(a.c.k_tok, row_bytes);
+    int vo[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) vo[r] = i16 * E * ES < row_bytes ? (4 * c + r) * (int)a.c.v_tok + i16 * E * ES : kFar;
+
+    Query<DT, DP> q[MT];
+    int last[MT];  // the last token that the lane's row sees
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const int row = r0 + 16 * m + i16;
+        q[m].load(a, p, row, n_rows);
+        last[m] = a.causal ? p.length - p.n_new + row / a.group : p.length - 1;
+    }
+    const int least = a.causal ? p.length - p.n_new + r0 / a.group : p.length - 1;  // of all rows
+
+    f32x4 o[MT][E];
+    float ref[MT], sum[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        ref[m] = -INFINITY;
+        sum[m] = 0.0f;
+#pragma unroll
+        for (int t = 0; t < E; ++t) o[m][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    const int tiles = (hi - lo + TT - 1) / TT;
+    const int mine = tiles > wave ? (tiles - wave + kWaves - 1) / kWaves : 0;
+    u32x4 kf[NH][KS];
+    uint32_t vf[NH][4][VW];
+    int pages = lane_pages<NH>(a.c, p.seq, lo, hi, wave, 0);
+    int kn[NH], next_n[NH];
+    auto load_k = [&](int it) {
+        const int tok = lo + TT * (wave + kWaves * it);
+#pragma unroll
+        for (int h = 0; h < NH; ++h) {
+            const int page = __builtin_amdgcn_readlane(pages, (NH * it + h) & 63);
+            const Half f = half_of(kb, a.c.k_page, a.c.k_tok, row_bytes, page, tok + 16 * h, hi, mask);
+            next_n[h] = f.n;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) kf[h][s] = __builtin_amdgcn_raw_buffer_load_b128(f.r, ko.off[s], 0, 0);
+        }
+    };
+    auto load_v = [&](int it) {
+        const int tok = lo + TT * (wave + kWaves * it);
+#pragma unroll
+        for (int h = 0; h < NH; ++h) {
+            const int page = __builtin_amdgcn_readlane(pages, (NH * it + h) & 63);
+            const Half f = half_of(vb, a.c.v_page, a.c.v_tok, row_bytes, page, tok + 16 * h, hi, mask);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) load_words<VW>(vf[h][r], f.r, vo[r]);
+        }
+    };
+    if (mine > 0) {
+        load_k(0);
+        load_v(0);
+    }
+    bool left_out = false;
+    for (int it = 0; it < mine; ++it) {
+        const int tok = lo + TT * (wave + kWaves * it);
+        const bool seen_whole = tok + TT <= hi && tok + TT - 1 <= least;  // all of it, by every row
+        bool whole = seen_whole;
+#pragma unroll
+        for (int h = 0; h < NH; ++h) {
+            kn[h] = next_n[h];
+            whole = whole && kn[h] == 16;
+        }
+        float x[MT][4 * NH];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int h = 0; h < NH; ++h) {
+                const f32x4 s = scores<DT, DP>(kf[h], q[m]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[m][4 * h + r] = s[r] * a.scale;
+            }
+        // (V of this tile is on its way: the lanes' pages may be the next ones)
+        if (it + 1 < mine) {
+            if (((it + 1) & (64 / NH - 1)) == 0) pages = lane_pages<NH>(a.c, p.seq, lo, hi, wave, it + 1);
+            load_k(it + 1);
+        }
+        if (!whole) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int h = 0; h < NH; ++h)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int j = 4 * c + r;
+                        if (j >= kn[h] || tok + 16 * h + j > last[m]) x[m][4 * h + r] = -INFINITY;
+                    }
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            float most = x[m][0];
+#pragma unroll
+            for (int e = 1; e < 4 * NH; ++e) most = fmaxf(most, x[m][e]);
+            if (__ballot(most > ref[m] + kSlack) != 0) {
+                most = fmaxf(most, __shfl_xor(most, 16));
+                most = fmaxf(most, __shfl_xor(most, 32));
+                const float up = fmaxf(most, ref[m]);
+                // (ref -inf: the sums are 0 and stay 0)
+                const float sc = ref[m] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref[m] - up);
+                ref[m] = up;
+                sum[m] *= sc;
+#pragma unroll
+                for (int t = 0; t < E; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[m][t][r] *= sc;
+            }
+            const float base = ref[m] == -INFINITY ? 0.0f : ref[m];
+#pragma unroll
+            for (int e = 0; e < 4 * NH; ++e) {
+                x[m][e] = __builtin_amdgcn_exp2f(x[m][e] - base);
+                sum[m] += x[m][e];
+            }
+        }
+        if (!seen_whole && a.causal) {
+            // a value that some rows must not see is 0 times its weight there, and that is NaN
+            // for one that is not finite: such values stay out of the product (see below)
+            bool any = false;
+#pragma unroll
+            for (int h = 0; h < NH; ++h)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int w = 0; w < VW; ++w) any = any || strange<DT>(vf[h][r][w]);
+            if (__ballot(any) != 0) {
+                left_out = true;
+#pragma unroll
+                for (int h = 0; h < NH; ++h)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+#pragma unroll
+                        for (int w = 0; w < VW; ++w) vf[h][r][w] = without_strange<DT>(vf[h][r][w]);
+            }
+        }
+        if constexpr (DT == kBF16) {
+            u32x4 pb[MT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) pb[m][e] = pack_bf16(x[m][2 * e], x[m][2 * e + 1]);
+#pragma unroll
+            for (int t = 0; t < E; ++t) {
+                const uint32_t sel = t & 1 ? 0x07060302u : 0x05040100u;
+                u32x4 vt;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    vt[e] = __builtin_amdgcn_perm(vf[e / 2][2 * (e & 1) + 1][t / 2], vf[e / 2][2 * (e & 1)][t / 2], sel);
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+                    o[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vt),
+                                                                      __builtin_bit_cast(bf16x8, pb[m]), o[m][t], 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int h = 0; h < NH; ++h)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int t = 0; t < E; ++t)
+#pragma unroll
+                        for (int m = 0; m < MT; ++m)
+                            o[m][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[h][r][t]), x[m][4 * h + r],
+                                                                           o[m][t], 0, 0, 0);
+        }
+        if (it + 1 < mine) load_v(it + 1);
+    }
+
+    if (left_out) {
+        // the values left out, to the rows that see them: whatever the weight, it is above 0, and
+        // the sum is infinite or NaN. From the first tile that some row does not see all of
+#pragma unroll 1
+        for (int it = max(0, (least + 1 - lo) / TT - wave) / kWaves; it < mine; ++it) {
+            const int tok = lo + TT * (wave + kWaves * it);
+            if (tok + TT <= hi && tok + TT - 1 <= least) continue;
+#pragma unroll 1
+            for (int t = tok; t < min(tok + TT, hi); ++t) {
+                const int page = page_at(a.c, p.seq, t >> a.c.page_shift);
+                if (page < 0) continue;
+                const uint8_t* src = vb + (int64_t)page * a.c.v_page + (int64_t)(t & mask) * a.c.v_tok;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int w = 0; w < VW; ++w) {
+                        const int at = (4 * c + r) * E * ES + 4 * w;
+                        const uint32_t v = at < row_bytes ? *(const uint32_t*)(src + at) : 0u;
+                        const uint32_t bad = v ^ without_strange<DT>(v);
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) {
+                            if (t > last[m]) continue;
+                            if constexpr (DT == kF32) {
+                                o[m][w][r] += __uint_as_float(bad);
+                            } else {
+                                o[m][2 * w][r] += __uint_as_float(bad << 16);
+                                o[m][2 * w + 1][r] += __uint_as_float(bad & 0xFFFF0000u);
+                            }
+                        }
+                    }
+            }
+        }
+    }
+
+    // join the wavefronts: references and sums, then the outputs 16 rows at a time
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        sum[m] += __shfl_xor(sum[m], 16);
+        sum[m] += __shfl_xor(sum[m], 32);
+        if (c == 0) {
+            lds_m[wave][16 * m + i16] = ref[m];
+            lds_l[wave][16 * m + i16] = sum[m];
+        }
+    }
+    const int orow = threadIdx.x >> 4, od = (threadIdx.x & 15) * E;  // row and first channel that this thread writes
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        __syncthreads();
+        if (r0 + 16 * m >= n_rows) break;
+        float most = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) most = fmaxf(most, lds_m[w][16 * m + i16]);
+        const float sc = ref[m] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref[m] - most);
+        // lane (c, q): channel (4c + r) E + t of tile t
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int t = 0; t < E; ++t) lds_o[wave][i16][(4 * c + r) * E + t] = o[m][t][r] * sc;
+        __syncthreads();
+        const int row = r0 + 16 * m + orow;
+        if (row < n_rows && od < a.c.dim) {
+            float mm = -INFINITY, l = 0.0f, acc[E];
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, lds_m[w][16 * m + orow]);
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float mw = lds_m[w][16 * m + orow];
+                l += mw == -INFINITY ? 0.0f : lds_l[w][16 * m + orow] * __builtin_amdgcn_exp2f(mw - mm);
+            }
+#pragma unroll
+            for (int t = 0; t < E; ++t) {
+                acc[t] = lds_o[0][orow][od + t];
+#pragma unroll
+                for (int w = 1; w < kWaves; ++w) acc[t] += lds_o[w][orow][od + t];
+            }
+            const int tok = row / a.group, head = p.head * a.group + (row - tok * a.group);
+            const int64_t at = (int64_t)(p.begin + tok) * a.heads + head;
+            if (cut.n <= 1) {
+                const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+                uint8_t* dst = a.out + (int64_t)(p.begin + tok) * a.out_stride + ((int64_t)head * a.c.dim + od) * ES;
+                // (the head's last channels may be half of what the thread has)
+#pragma unroll
+                for (int t = 0; t < E; t += 4) {
+                    if (od + t >= a.c.dim) break;
+                    if constexpr (DT == kBF16)
+                        *(u32x2*)(dst + 2 * t) =
+                            u32x2{pack_bf16(acc[t] * inv, acc[t + 1] * inv), pack_bf16(acc[t + 2] * inv, acc[t + 3] * inv)};
+                    else
+                        *(f32x4*)(dst + 4 * t) = f32x4{acc[t] * inv, acc[t + 1] * inv, acc[t + 2] * inv, acc[t + 3] * inv};
+                }
+                if (od == 0) {
+                    const float z = l == 0.0f ? -INFINITY : mm + __builtin_amdgcn_logf(l);
+                    if (a.lse) a.lse[at] = z * kLn2;
+                    if (a.lse2) a.lse2[at] = z;
+                }
+            } else {
+                const int64_t all = (int64_t)a.ch.n_rows * a.heads;
+                float* po = a.part_o + (split * all + at) * a.c.dim + od;
+#pragma unroll
+                for (int t = 0; t < E; t += 4)
+                    if (od + t < a.c.dim) *(f32x4*)(po + t) = f32x4{acc[t], acc[t + 1], acc[t + 2], acc[t + 3]};
+                if (od == 0) *(f32x2*)(a.part_ml + 2 * (split * all + at)) = f32x2{mm, l};
+            }
+        }
+    }
+}
+
+// Parts of split rows joined: a wavefront a row.
+template <int DT>
+__global__ __launch_bounds__(kBlock) void k_combine(AttendArgs a, int blocks_per)
+{
+    constexpr int ES = Type<DT>::kSize;
+    const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
+    const int sh = blockIdx.x / blocks_per;
+    const Place p = place_of(a, sh);
+    const int n_rows = call_rows(a, p), row = (blockIdx.x - sh * blocks_per) * kWaves + wave;
+    if (row >= n_rows) return;
+    const int r_end = min(row / a.tile_rows * a.tile_rows + a.tile_rows, n_rows);
+    const int seen = group_sees(p.length, p.n_new, a.group, r_end - 1, a.causal);
+    const Cut cut = cut_tokens(seen, a.splits);
+    if (cut.n <= 1) return;  // written by k_attend
+    const int tok = row / a.group, head = p.head * a.group + (row - tok * a.group);
+    const int64_t all = (int64_t)a.ch.n_rows * a.heads, at = (int64_t)(p.begin + tok) * a.heads + head;
+    float most = -INFINITY;
+    for (int i = lane; i < cut.n; i += kWave) most = fmaxf(most, a.part_ml[2 * (i * all + at)]);
+#pragma unroll
+    for (int s = 1; s < kWave; s <<= 1) most = fmaxf(most, __shfl_xor(most, s));
+    const float base = most == -INFINITY ? 0.0f : most;
+    float l = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // channels lane, lane + 64, ...
+    for (int i = 0; i < cut.n; ++i) {
+        const f32x2 ml = *(const f32x2*)(a.part_ml + 2 * (i * all + at));
+        const float sc = __builtin_amdgcn_exp2f(ml.x - base);
+        l = fmaf(ml.y, sc, l);
+        const float* po = a.part_o + (i * all + at) * a.c.dim;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (lane + kWave * e < a.c.dim) acc[e] = fmaf(po[lane + kWave * e], sc, acc[e]);
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    uint8_t* dst = a.out + (int64_t)(p.begin + tok) * a.out_stride + (int64_t)head * a.c.dim * ES;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int d = lane + kWave * e;
+        if (d >= a.c.dim) break;
+        if constexpr (DT == kBF16) ((uint16_t*)dst)[d] = (uint16_t)pack_bf16(acc[e] * inv, 0.0f);
+        else ((float*)dst)[d] = acc[e] * inv;
+    }
+    if (lane == 0) {
+        const float z = l == 0.0f ? -INFINITY : most + __builtin_amdgcn_logf(l);
+        if (a.lse) a.lse[at] = z * kLn2;
+        if (a.lse2) a.lse2[at] = z;
+    }
+}
+
+// The weight that each token receives: a wavefront holds the keys of 32 tokens and
+// goes over the rows, 16 at a time, whose sums (lse2) are known by now:
+//   weight_j += sum_i 2^(x_ij - lse2_i).
+// Lane (c, q) sums tokens 4c + r over its rows; the 16 lanes are added at the end. Every
+// token has one wavefront, so no atomics, and the order of the sum is fixed.
+template <int DT, int DP>
+__global__ __launch_bounds__(kBlock) void k_weight(AttendArgs a)
+{
+    constexpr int ES = Type<DT>::kSize;
+    constexpr int KS = DP * ES / 64;
+    const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
+    const int i16 = lane & 15, c = lane >> 4;
+    const int sh = blockIdx.x / a.weight_blocks, block = blockIdx.x - sh * a.weight_blocks;
+    const Place p = place_of(a, sh);
+    const int n_rows = call_rows(a, p);
+    if (n_rows == 0) return;
+    const int seen = group_sees(p.length, p.n_new, a.group, n_rows - 1, a.causal);
+    const int row_bytes = a.c.dim * ES, mask = (1 << a.c.page_shift) - 1;
+    const uint8_t* kb = a.c.k + (int64_t)p.head * a.c.k_head;
+    const KeyOffsets<DT, DP> ko(a.c.k_tok, row_bytes);
+    float* weight = a.c.weight + (int64_t)sh * a.c.weight_stride;
+    for (int64_t t = (int64_t)block * kWaves + wave; t * kTile < seen; t += (int64_t)a.weight_blocks * kWaves) {
+        const int tok = (int)t * kTile;
+        u32x4 kf[2][KS];
+        int kn[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int page = tok + 16 * h < seen ? page_at(a.c, p.seq, (tok + 16 * h) >> a.c.page_shift) : -1;
+            const Half f = half_of(kb, a.c.k_page, a.c.k_tok, row_bytes, uniform(page), tok + 16 * h, seen, mask);
+            kn[h] = f.n;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) kf[h][s] = __builtin_amdgcn_raw_buffer_load_b128(f.r, ko.off[s], 0, 0);
+        }
+        float w[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        // the first row that sees the tile's first token
+        const int from = a.causal ? max(0, tok - (p.length - p.n_new)) * a.group & ~15 : 0;
+        for (int r0 = from; r0 < n_rows; r0 += 16) {
+            const int row = r0 + i16;
+            Query<DT, DP> q;
+            q.load(a, p, row, n_rows);
+            const int qt = row / a.group, head = p.head * a.group + (row - qt * a.group);
+            const float z = row < n_rows ? a.lse2[(int64_t)(p.begin + qt) * a.heads + head] : -INFINITY;
+            const int last = a.causal ? p.length - p.n_new + qt : p.length - 1;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const f32x4 s = scores<DT, DP>(kf[h], q);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int j = 4 * c + r;
+                    const bool sees = z != -INFINITY && j < kn[h] && tok + 16 * h + j <= last;
+                    w[4 * h + r] += sees ? __builtin_amdgcn_exp2f(fmaf(s[r], a.scale, -z)) : 0.0f;
+                }
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int s = 1; s < 16; s <<= 1) w[e] += __shfl_xor(w[e], s);
+        if (i16 == 0) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (4 * c + r < kn[h]) weight[tok + 16 * h + 4 * c + r] += w[4 * h + r];
+        }
+    }
+}
+
+template <typename K, typename... A>
+int enqueue(K kernel, int64_t blocks, void* stream, void* ev0, void* ev1, A... args)
+{
+    if (blocks <= 0) return kNoLaunch;
+    if (ev0 && ev1)
+        hipExtLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kBlock), 0, (hipStream_t)stream, (hipEvent_t)ev0,
+                              (hipEvent_t)ev1, 0, args...);
+    else
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kBlock), 0, (hipStream_t)stream, args...);
+    return (int)hipGetLastError();
+}
+
+int padded_dim(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
+
+int64_t pairs(const AttendArgs& a) { return (int64_t)a.c.n_seqs * a.c.kv_heads; }
+
+template <int DT, int DP>
+int attend_rows(const AttendArgs& a, void* st, void* e0, void* e1)
+{
+    const int64_t blocks = pairs(a) * a.row_tiles * a.splits;
+    if (a.tile_rows == 16) return enqueue(k_attend<DT, DP, 1>, blocks, st, e0, e1, a);
+    if constexpr (DP <= 128)
+        if (a.tile_rows == 32) return enqueue(k_attend<DT, DP, 2>, blocks, st, e0, e1, a);
+    if constexpr (DT == kBF16 && DP <= 128)
+        if (a.tile_rows == 64) return enqueue(k_attend<DT, DP, 4>, blocks, st, e0, e1, a);
+    return (int)hipErrorInvalidValue;
+}
+
+}  // namespace
+
+void attend_shape(AttendArgs& a)
+{
+    const int64_t rows = (int64_t)a.ch.max_new * a.group;
+    const int dp = padded_dim(a.c.dim);
+    const int most = dp == 256 ? 16 : a.dtype == kBF16 ? 64 : 32;  // rows that registers hold
+    a.tile_rows = rows <= 16 || most == 16 ? 16 : rows <= 32 || most == 32 ? 32 : 64;
+    a.row_tiles = (int)((rows + a.tile_rows - 1) / a.tile_rows);
+    const int64_t groups = std::max<int64_t>(pairs(a) * a.row_tiles, 1), cap = capacity(a.c);
+    const int64_t fill = (1024 + groups - 1) / groups, longest = (cap + 2047) / 2048, blocks = (cap + kPartTokens - 1) / kPartTokens;
+    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::max(fill, longest), blocks));
+    if (rows > 512) a.splits = (int)std::min<int64_t>(a.splits, fill);
+    const int64_t wtiles = (cap + kTile * kWaves - 1) / (kTile * kWaves);
+    a.weight_blocks = (int)std::max<int64_t>(1, std::min<int64_t>(wtiles, std::max<int64_t>(4096 / std::max<int64_t>(pairs(a), 1), 1)));
+}
+
+AttendBytes attend_bytes(const AttendArgs& a)
+{
+    const size_t rows = (size_t)a.ch.n_rows * (size_t)a.heads;
+    AttendBytes b{0, 0, 0};
+    if (a.splits > 1) {
+        b.part_o = rows * (size_t)a.splits * (size_t)a.c.dim * 4;
+        b.part_ml = rows * (size_t)a.splits * 8;
+    }
+    if (a.add_weight) b.lse2 = rows * 4;
+    return b;
+}
+
+int launch_attend(const AttendArgs& a, void* st, void* e0, void* e1)
+{
+    const int dp = padded_dim(a.c.dim);
+    if (a.dtype == kBF16)
+        return dp == 64 ? attend_rows<kBF16, 64>(a, st, e0, e1) : dp == 128 ? attend_rows<kBF16, 128>(a, st, e0, e1)
+                                                                            : attend_rows<kBF16, 256>(a, st, e0, e1);
+    return dp == 64 ? attend_rows<kF32, 64>(a, st, e0, e1) : dp == 128 ? attend_rows<kF32, 128>(a, st, e0, e1)
+                                                                       : attend_rows<kF32, 256>(a, st, e0, e1);
+}
+
+int launch_combine(const AttendArgs& a, void* st, void* e0, void* e1)
+{
+    if (a.splits <= 1) return kNoLaunch;
+    const int per = (int)(((int64_t)a.ch.max_new * a.group + kWaves - 1) / kWaves);
+    return a.dtype == kBF16 ? enqueue(k_combine<kBF16>, pairs(a) * per, st, e0, e1, a, per)
+                            : enqueue(k_combine<kF32>, pairs(a) * per, st, e0, e1, a, per);
+}
+
+int launch_weight(const AttendArgs& a, void* st, void* e0, void* e1)
+{
+    if (!a.add_weight) return kNoLaunch;
+    const int dp = padded_dim(a.c.dim);
+    const int64_t blocks = pairs(a) * a.weight_blocks;
+    if (a.dtype == kBF16)
+        return dp == 64 ? enqueue(k_weight<kBF16, 64>, blocks, st, e0, e1, a) : dp == 128
+                   ? enqueue(k_weight<kBF16, 128>, blocks, st, e0, e1, a) : enqueue(k_weight<kBF16, 256>, blocks, st, e0, e1, a);
+    return dp == 64 ? enqueue(k_weight<kF32, 64>, blocks, st, e0, e1, a) : dp == 128
+               ? enqueue(k_weight<kF32, 128>, blocks, st, e0, e1, a) : enqueue(k_weight<kF32, 256>, blocks, st, e0, e1, a);
+}
+
+}  // namespace msao

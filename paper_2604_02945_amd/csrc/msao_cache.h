@@ -1,0 +1,161 @@
+// msao_cache.h -- the paged cache's kernels' arguments, and the indexing that
+// kernels and host share: which rows a sequence has, where its tokens lie, how
+// a row's tokens are cut into parts. Compiles for the host alone, so that the
+// indexing is tested on the CPU (tests/c/cache_check.cpp). Not part of the ABI.
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+#if defined(__HIPCC__)
+#include <hip/hip_runtime.h>
+#define MSAO_HD __host__ __device__ __forceinline__
+#else
+#define MSAO_HD inline
+#endif
+
+namespace msao {
+
+// msao_kv_cache as the kernels take it: strides in bytes, the page size as a shift.
+struct CacheDev {
+    uint8_t* k;
+    uint8_t* v;
+    int64_t k_page, k_head, k_tok;
+    int64_t v_page, v_head, v_tok;
+    int32_t dim, kv_heads, page_shift, n_pages, n_seqs, per_seq;
+    int64_t table_stride;
+    const int32_t* pages;
+    int32_t* length;
+    float* weight;
+    int64_t weight_stride;
+};
+
+struct ChunkDev {
+    const int32_t* start;
+    int32_t n_rows, max_new;
+};
+
+MSAO_HD int clamp_int(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
+
+MSAO_HD int capacity(const CacheDev& c) { return c.per_seq << c.page_shift; }
+
+// Tokens of sequence s, whatever the caller's array says.
+MSAO_HD int seq_length(const CacheDev& c, int s) { return clamp_int(c.length[s], 0, capacity(c)); }
+
+// Rows of sequence s of the chunk: the first, and how many (all of them in [0, n_rows)).
+struct Rows {
+    int begin, n;
+};
+MSAO_HD Rows seq_rows(const ChunkDev& ch, int s)
+{
+    const int b = clamp_int(ch.start[s], 0, ch.n_rows), e = clamp_int(ch.start[s + 1], b, ch.n_rows);
+    return Rows{b, e - b};
+}
+
+// The page that column `col` of the sequence's table names, -1 if it names none.
+MSAO_HD int page_or_none(int page, int n_pages) { return page >= 0 && page < n_pages ? page : -1; }
+MSAO_HD int page_at(const CacheDev& c, int s, int col)
+{
+    return page_or_none(c.pages[(int64_t)s * c.table_stride + col], c.n_pages);
+}
+
+// How the `seen` tokens of a group of rows are cut into at most `most` parts of
+// whole 32-token tiles, none of fewer than kPartTokens tokens but the last: parts 0 ..
+// n-1, part i from token i * per. No part for no token.
+constexpr int kTile = 32;
+constexpr int kPartTokens = 256;
+struct Cut {
+    int n, per;
+};
+MSAO_HD Cut cut_tokens(int seen, int most)
+{
+    if (seen <= 0) return Cut{0, kTile};
+    const int blocks = (seen + kPartTokens - 1) / kPartTokens, want = most < blocks ? most : blocks;
+    const int per = ((seen + want - 1) / want + kTile - 1) / kTile * kTile;
+    return Cut{(seen + per - 1) / per, per};
+}
+
+// Tokens that rows [r0, r0 + rows) of a (sequence, kv head) see at most: row r is
+// query head r % group of token r / group. Without `causal` all of them.
+MSAO_HD int group_sees(int length, int n_new, int group, int last_row, bool causal)
+{
+    return causal ? clamp_int(length - n_new + last_row / group + 1, 0, length) : length;
+}
+
+// ---- append -------------------------------------------------------------------
+struct AppendArgs {
+    CacheDev c;
+    ChunkDev ch;
+    const uint8_t* q;
+    uint8_t* q_out;
+    const uint8_t* k;
+    const uint8_t* v;
+    int64_t q_stride, q_out_stride, k_stride, v_stride;  // bytes
+    const uint8_t* q_norm;
+    const uint8_t* k_norm;
+    float eps;
+    int32_t heads, rot, neighbours;
+    const float* inv_freq;
+    const int32_t* positions;
+    int64_t position_stride;
+    int32_t axis_end[4];  // first pair past each axis
+    int32_t dtype;
+    int32_t lanes;        // lanes of a head
+    int32_t parts;        // wavefronts of a token
+};
+
+// ---- attention ------------------------------------------------------------------
+struct AttendArgs {
+    CacheDev c;
+    ChunkDev ch;
+    const uint8_t* q;
+    uint8_t* out;
+    int64_t q_stride, out_stride;  // bytes
+    float* lse;
+    int32_t heads, group, dtype;
+    int32_t causal, add_weight;
+    float scale;                   // scale * log2(e)
+    int32_t splits, row_tiles;     // most parts of a group of rows; groups of a (sequence, kv head)
+    int32_t tile_rows;             // rows of a group
+    int32_t weight_blocks;         // blocks of the weight pass for each (sequence, kv head)
+    // workspace
+    float* part_o;                 // [splits][n_rows * heads][dim], a part's sum of 2^(x - m) v
+    float* part_ml;                // [splits][n_rows * heads][2], its m and sum of 2^(x - m)
+    float* lse2;                   // [n_rows * heads] log2 of the sums, for the weight pass
+};
+
+// ---- eviction -------------------------------------------------------------------
+struct EvictInfo {
+    int32_t kept, first_moved;     // tokens that stay; the first of them whose place changes
+};
+struct EvictArgs {
+    CacheDev from, to;
+    const int32_t* budget;
+    int32_t n_first, n_recent;
+    int32_t* kept_idx;
+    int64_t idx_stride;
+    EvictInfo* info;               // workspace [n_seqs * kv_heads]
+    int32_t in_place, dtype;
+    int32_t blocks;                // of the move, for each (sequence, kv head, k or v, column part)
+    int32_t col_parts;             // parts that a row is cut into
+};
+
+int launch_append(const AppendArgs& a, void* stream, void* ev0, void* ev1);
+int launch_attend(const AttendArgs& a, void* stream, void* ev0, void* ev1);
+int launch_combine(const AttendArgs& a, void* stream, void* ev0, void* ev1);
+int launch_weight(const AttendArgs& a, void* stream, void* ev0, void* ev1);
+int launch_select(const EvictArgs& a, void* stream, void* ev0, void* ev1);
+int launch_move(const EvictArgs& a, void* stream, void* ev0, void* ev1);
+
+// Launch shapes: lanes and parts of an append; blocks and col_parts of an eviction's move.
+void append_shape(AppendArgs& a);
+void evict_shape(EvictArgs& a);
+// Launch shape of an attention call: fills splits, row_tiles, tile_rows and weight_blocks.
+void attend_shape(AttendArgs& a);
+// Bytes of each of its workspace arrays.
+struct AttendBytes {
+    size_t part_o, part_ml, lse2;
+};
+AttendBytes attend_bytes(const AttendArgs& a);
+
+}  // namespace msao

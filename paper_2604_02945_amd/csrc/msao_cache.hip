@@ -1,0 +1,465 @@
+// msao_cache.hip -- gfx950 (CDNA4) kernels that store to a paged cache: append (norm of
+// the queries' and keys' heads, position rotation, and the keys and values into their
+// pages, in one pass) and eviction by accumulated attention weight.
+#include <hip/hip_ext.h>
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "msao_cache.h"
+#include "msao_device.h"
+#include "msao_internal.h"
+
+namespace msao {
+namespace {
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kWave = 64;
+constexpr int kBlock = 256;
+constexpr int kWaves = kBlock / kWave;
+constexpr int kMaxPairs = 128;  // of a rotation: half the largest head
+
+// Eight neighbouring values of a row in 32 bits.
+template <int DT>
+struct Eight {
+    u32x4 w[DT == kBF16 ? 1 : 2];
+    __device__ __forceinline__ void load(const uint8_t* p)
+    {
+        w[0] = ((const u32x4*)p)[0];
+        if constexpr (DT == kF32) w[1] = ((const u32x4*)p)[1];
+    }
+    __device__ __forceinline__ void store(uint8_t* p) const
+    {
+        ((u32x4*)p)[0] = w[0];
+        if constexpr (DT == kF32) ((u32x4*)p)[1] = w[1];
+    }
+    __device__ __forceinline__ void zero()
+    {
+        w[0] = u32x4{0, 0, 0, 0};
+        if constexpr (DT == kF32) w[1] = w[0];
+    }
+    __device__ __forceinline__ void widen(float (&x)[8]) const
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (DT == kBF16) {
+                x[2 * e] = __uint_as_float(w[0][e] << 16);
+                x[2 * e + 1] = __uint_as_float(w[0][e] & 0xFFFF0000u);
+            } else {
+                x[e] = __uint_as_float(w[0][e]);
+                x[4 + e] = __uint_as_float(w[1][e]);
+            }
+        }
+    }
+    __device__ __forceinline__ void narrow(const float (&x)[8])
+    {
+        typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (DT == kBF16) {
+                const f32x2 v = {x[2 * e], x[2 * e + 1]};
+                w[0][e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf2));
+            } else {
+                w[0][e] = __float_as_uint(x[e]);
+                w[1][e] = __float_as_uint(x[4 + e]);
+            }
+        }
+    }
+};
+
+// The sequence of a row of the chunk (-1: none): of the starts that are not past the
+// row, the last one's.
+__device__ __forceinline__ int seq_of_row(const AppendArgs& a, int row)
+{
+    const int lane = threadIdx.x & (kWave - 1);
+    int n = 0;
+    for (int i0 = 0; i0 <= a.c.n_seqs; i0 += kWave) {
+        const int i = i0 + lane;
+        n += __popcll(__ballot(i <= a.c.n_seqs && clamp_int(a.ch.start[min(i, a.c.n_seqs)], 0, a.ch.n_rows) <= row));
+    }
+    const int s = n - 1;
+    if (s < 0 || s >= a.c.n_seqs) return -1;
+    const Rows r = seq_rows(a.ch, s);
+    return row >= r.begin && row < r.begin + r.n ? s : -1;
+}
+
+// One pass over a row's heads: queries, keys, then values. A head takes `lanes` lanes of
+// a wavefront (a power of two), each with two eights of it that hold whole pairs of the
+// rotation: (8u, rot/2 + 8u) below rot (or 16u, 16u + 8 for neighbouring pairs), two
+// neighbours above. The norm is a sum over those lanes; the angles are the same for
+// every head, so a wavefront computes each once, into LDS, and a lane keeps the eight
+// that it turns. HBM bound: each value is read and written once, four heads in flight.
+// The angle is taken in turns in 64 bits (position * inv_freq / 2 pi less its whole
+// part), which keeps far positions as exact as near ones.
+template <int DT>
+__global__ __launch_bounds__(kBlock) void k_append(AppendArgs a)
+{
+    constexpr int ES = DT == kBF16 ? 2 : 4;
+    constexpr int U = 4;  // rounds of heads in flight
+    __shared__ f32x2 turn[kWaves][kMaxPairs];
+    const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
+    const int64_t item = (int64_t)blockIdx.x * kWaves + wave;
+    const int row = (int)(item / a.parts), part = (int)(item - (int64_t)row * a.parts);
+    if (row >= a.ch.n_rows) return;
+    const int s = uniform(seq_of_row(a, row));
+    if (s < 0) return;
+    const Rows rows = seq_rows(a.ch, s);
+    const int64_t place = (int64_t)seq_length(a.c, s) - rows.n + (row - rows.begin);  // in the cache
+    const int mask = (1 << a.c.page_shift) - 1;
+    const int page = place >= 0 ? page_at(a.c, s, (int)place >> a.c.page_shift) : -1;
+    const int slot = (int)place & mask;
+
+    const int half = a.rot / 2;
+    for (int i = lane; i < half; i += kWave) {
+        int axis = 0;
+#pragma unroll
+        for (int x = 0; x < 3; ++x) axis += i >= a.axis_end[x];
+        const int at = a.positions ? a.positions[axis * a.position_stride + row] : (int)place;
+        double t = (double)at * (double)a.inv_freq[i] * 0.15915494309189533577;
+        t -= floor(t);
+        float sn, cs;
+        sincospif(2.0f * (float)t, &sn, &cs);
+        turn[wave][i] = f32x2{cs, sn};
+    }
+    // the wavefront's own stores, read by its other lanes
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+
+    const int u = lane & (a.lanes - 1), per = kWave / a.lanes;  // the lane's pair of eights; heads of a round
+    const int turned = a.rot / 16;
+    const bool turns = u < turned;
+    int d0, d1;
+    if (turns && !a.neighbours) {
+        d0 = 8 * u;
+        d1 = half + 8 * u;
+    } else {
+        d0 = 16 * u;
+        d1 = d0 + 8;
+    }
+    const bool has0 = d0 < a.c.dim, has1 = d1 < a.c.dim;
+    float cs[8], sn[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const f32x2 v = turns ? turn[wave][8 * u + e] : f32x2{1.0f, 0.0f};
+        cs[e] = v.x;
+        sn[e] = v.y;
+    }
+
+    const int heads = a.heads + 2 * a.c.kv_heads;
+    const int rounds = (heads + per - 1) / per;
+    if (a.c.weight && part == 0 && place >= 0)
+        for (int h = lane; h < a.c.kv_heads; h += kWave)
+            a.c.weight[((int64_t)s * a.c.kv_heads + h) * a.c.weight_stride + place] = 0.0f;
+    for (int r0 = part * U; r0 < rounds; r0 += a.parts * U) {
+        Eight<DT> x0[U], x1[U];
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const int h = (r0 + j) * per + lane / a.lanes;
+            x0[j].zero();
+            x1[j].zero();
+            if (h >= heads) continue;
+            const uint8_t* src;
+            if (h < a.heads) src = a.q + row * a.q_stride + (int64_t)h * a.c.dim * ES;
+            else if (h < a.heads + a.c.kv_heads) src = a.k + row * a.k_stride + (int64_t)(h - a.heads) * a.c.dim * ES;
+            else src = a.v + row * a.v_stride + (int64_t)(h - a.heads - a.c.kv_heads) * a.c.dim * ES;
+            if (has0) x0[j].load(src + d0 * ES);
+            if (has1) x1[j].load(src + d1 * ES);
+        }
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const int h = (r0 + j) * per + lane / a.lanes;
+            const bool is_q = h < a.heads, is_v = h >= a.heads + a.c.kv_heads;
+            float y0[8], y1[8];
+            x0[j].widen(y0);
+            x1[j].widen(y1);
+            float sq = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sq = fmaf(y0[e], y0[e], fmaf(y1[e], y1[e], sq));
+            for (int o = 1; o < a.lanes; o <<= 1) sq += __shfl_xor(sq, o);
+            const uint8_t* norm = is_q ? a.q_norm : a.k_norm;
+            if (!is_v) {
+                if (norm) {
+                    const float f = 1.0f / sqrtf(sq / (float)a.c.dim + a.eps);
+                    Eight<DT> n0, n1;
+                    n0.zero();
+                    n1.zero();
+                    if (has0) n0.load(norm + d0 * ES);
+                    if (has1) n1.load(norm + d1 * ES);
+                    float w0[8], w1[8];
+                    n0.widen(w0);
+                    n1.widen(w1);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        y0[e] *= f * w0[e];
+                        y1[e] *= f * w1[e];
+                    }
+                }
+                if (turns) {
+                    if (a.neighbours) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float p = y0[2 * e], q = y0[2 * e + 1], r = y1[2 * e], t = y1[2 * e + 1];
+                            y0[2 * e] = p * cs[e] - q * sn[e];
+                            y0[2 * e + 1] = p * sn[e] + q * cs[e];
+                            y1[2 * e] = r * cs[4 + e] - t * sn[4 + e];
+                            y1[2 * e + 1] = r * sn[4 + e] + t * cs[4 + e];
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float p = y0[e], q = y1[e];
+                            y0[e] = p * cs[e] - q * sn[e];
+                            y1[e] = p * sn[e] + q * cs[e];
+                        }
+                    }
+                }
+                x0[j].narrow(y0);
+                x1[j].narrow(y1);
+            }
+            if (h >= heads) continue;
+            uint8_t* dst;
+            if (is_q) {
+                dst = a.q_out + row * a.q_out_stride + (int64_t)h * a.c.dim * ES;
+            } else {
+                if (page < 0) continue;
+                const int kh = is_v ? h - a.heads - a.c.kv_heads : h - a.heads;
+                dst = is_v ? a.c.v + page * a.c.v_page + kh * a.c.v_head + slot * a.c.v_tok
+                           : a.c.k + page * a.c.k_page + kh * a.c.k_head + slot * a.c.k_tok;
+            }
+            if (has0) x0[j].store(dst + d0 * ES);
+            if (has1) x1[j].store(dst + d1 * ES);
+        }
+    }
+}
+
+// ---- eviction -------------------------------------------------------------------
+
+constexpr int kSelBlock = 1024;
+constexpr int kSelWaves = kSelBlock / kWave;
+constexpr int kBins = 2048;
+
+// Order of a weight: larger is kept; NaN and what is not above 0 counts as 0.
+__device__ __forceinline__ uint32_t weight_key(float w) { return w > 0.0f ? __float_as_uint(w) : 0u; }
+
+// Exclusive sum over the block of a per-thread value, and the total.
+__device__ __forceinline__ uint64_t block_scan(uint64_t v, uint64_t* lds, uint64_t* total)
+{
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
+    uint64_t x = v;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        const uint64_t y = (uint64_t)__shfl_up((unsigned long long)x, o);
+        if (lane >= o) x += y;
+    }
+    __syncthreads();  // (an earlier call's sums have been read)
+    if (lane == kWave - 1) lds[wave] = x;
+    __syncthreads();
+    uint64_t before = 0, all = 0;
+    for (int w = 0; w < kSelWaves; ++w) {
+        const uint64_t t = lds[w];
+        before += w < wave ? t : 0;
+        all += t;
+    }
+    *total = all;
+    return before + x - v;
+}
+
+// The tokens that stay of one (sequence, kv head), by one workgroup: the k-th largest
+// key by digits of 11, 10 and 10 bits, counted in LDS, then one ascending pass that
+// writes the kept indices and weights. In place, a pass's weights are all in registers
+// before any is written, and go to places not past those already read.
+__global__ __launch_bounds__(kSelBlock) void k_select(EvictArgs a)
+{
+    __shared__ uint32_t bins[kBins];
+    __shared__ uint64_t sums[kSelWaves];
+    __shared__ uint32_t found[2];
+    __shared__ int first_moved;
+    const int sh = blockIdx.x, s = sh / a.from.kv_heads, tid = threadIdx.x;
+    const int L = seq_length(a.from, s), cap = capacity(a.from);
+    const int k = min(min(L, max(a.budget[s], 0)), capacity(a.to));
+    const int first = min(a.n_first, k), recent = min(a.n_recent, k - first);
+    const int lo = first, hi = L - recent;              // those between are ranked
+    const int take = k - first - recent;                // and so many of them stay
+    const float* w = a.from.weight + (int64_t)sh * a.from.weight_stride;
+    uint32_t least = 0;       // the smallest key that stays
+    uint32_t ties = 0;        // how many of that key
+    if (take > 0 && take < hi - lo) {
+        uint32_t want = (uint32_t)take;
+        const int shift[3] = {20, 10, 0}, width[3] = {11, 10, 10};
+        for (int d = 0; d < 3; ++d) {
+            for (int b = tid; b < kBins; b += kSelBlock) bins[b] = 0;
+            __syncthreads();
+            for (int j = lo + tid; j < hi; j += kSelBlock) {
+                const uint32_t key = weight_key(w[j]);
+                if (d == 0 || key >> (shift[d] + width[d]) == least >> (shift[d] + width[d]))
+                    atomicAdd(&bins[key >> shift[d] & ((1u << width[d]) - 1)], 1u);
+            }
+            __syncthreads();
+            // from the largest digit down: thread t has bins 2047 - 2t and the one below
+            const uint32_t b0 = bins[kBins - 1 - 2 * tid], b1 = bins[kBins - 2 - 2 * tid];
+            uint64_t total;
+            const uint32_t before = (uint32_t)block_scan(b0 + b1, sums, &total);
+            if (before < want && want <= before + b0 + b1) {
+                const bool second = want > before + b0;
+                found[0] = (uint32_t)(kBins - 1 - 2 * tid - (second ? 1 : 0));
+                found[1] = want - before - (second ? b0 : 0);
+            }
+            __syncthreads();
+            least |= found[0] << shift[d];
+            want = found[1];
+            __syncthreads();
+        }
+        ties = want;
+    }
+    const bool all = take >= hi - lo, none = take <= 0;
+    if (tid == 0) first_moved = k;
+    int32_t* idx = a.kept_idx + (int64_t)sh * a.idx_stride;
+    float* tw = a.to.weight ? a.to.weight + (int64_t)sh * a.to.weight_stride : nullptr;
+    uint32_t kept = 0, tied = 0;  // before this pass: kept beside the ties, and of the tied key
+    for (int j0 = 0; j0 < L; j0 += 4 * kSelBlock) {
+        float v[4];
+        bool above[4], equal[4];
+        uint32_t n = 0, e = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int j = j0 + 4 * tid + i;
+            v[i] = j < L ? w[j] : 0.0f;
+            const uint32_t key = weight_key(v[i]);
+            const bool fixed = j < lo || j >= hi;
+            above[i] = j < L && (fixed || all || (!none && key > least));
+            equal[i] = j < L && !fixed && !all && !none && key == least;
+            n += above[i];
+            e += equal[i];
+        }
+        uint64_t total;
+        const uint64_t at = block_scan((uint64_t)n << 32 | e, sums, &total);
+        uint32_t n_at = kept + (uint32_t)(at >> 32), e_at = tied + (uint32_t)at;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int j = j0 + 4 * tid + i;
+            const bool stays = above[i] || (equal[i] && e_at < ties);
+            if (stays) {
+                const int to = (int)(n_at + min(e_at, ties));
+                idx[to] = j;
+                if (tw) tw[to] = v[i];
+                if (to != j) atomicMin(&first_moved, to);
+            }
+            n_at += above[i];
+            e_at += equal[i];
+        }
+        kept += (uint32_t)(total >> 32);
+        tied += (uint32_t)total;
+    }
+    for (int j = k + tid; j < cap; j += kSelBlock) idx[j] = -1;
+    __syncthreads();
+    if (tid == 0) a.info[sh] = EvictInfo{k, a.in_place ? first_moved : 0};
+}
+
+// The kept tokens' keys and values to their places. A block takes chunks of `kMoveRows`
+// places in turn; in place there is one block for each (sequence, kv head, K or V,
+// column part), whose loads of a chunk are done before its stores begin: a kept token
+// only ever moves down, so a later chunk reads nothing that an earlier one wrote.
+constexpr int kMoveUnits = 4;  // 16-byte pieces of a thread in flight
+__global__ __launch_bounds__(kBlock) void k_move(EvictArgs a)
+{
+    int id = blockIdx.x;
+    const int block = id % a.blocks;
+    id /= a.blocks;
+    const int col = id % a.col_parts;
+    id /= a.col_parts;
+    const bool is_v = id & 1;
+    const int sh = id >> 1, s = sh / a.from.kv_heads, h = sh - s * a.from.kv_heads;
+    const EvictInfo info = a.info[sh];
+    if (block == 0 && col == 0 && !is_v && h == 0 && threadIdx.x == 0) a.to.length[s] = info.kept;
+    const int units = a.from.dim * (a.dtype == kBF16 ? 2 : 4) / 16 / a.col_parts;  // 16-byte pieces of a row's part
+    const uint8_t* src = (is_v ? a.from.v + h * a.from.v_head : a.from.k + h * a.from.k_head) + (int64_t)col * units * 16;
+    uint8_t* dst = (is_v ? a.to.v + h * a.to.v_head : a.to.k + h * a.to.k_head) + (int64_t)col * units * 16;
+    const int64_t sp = is_v ? a.from.v_page : a.from.k_page, st = is_v ? a.from.v_tok : a.from.k_tok;
+    const int64_t dp = is_v ? a.to.v_page : a.to.k_page, dt = is_v ? a.to.v_tok : a.to.k_tok;
+    const int smask = (1 << a.from.page_shift) - 1, dmask = (1 << a.to.page_shift) - 1;
+    const int32_t* idx = a.kept_idx + (int64_t)sh * a.idx_stride;
+    const int64_t end = (int64_t)info.kept * units, step = (int64_t)kBlock * kMoveUnits;
+    for (int64_t p0 = (int64_t)info.first_moved * units + block * step; p0 < end; p0 += a.blocks * step) {
+        u32x4 x[kMoveUnits];
+#pragma unroll
+        for (int i = 0; i < kMoveUnits; ++i) {
+            const int64_t p = p0 + i * kBlock + threadIdx.x;
+            x[i] = u32x4{0, 0, 0, 0};
+            if (p < end) {
+                const int to = (int)(p / units), j = idx[to];
+                const int page = page_at(a.from, s, j >> a.from.page_shift);
+                if (page >= 0) x[i] = *(const u32x4*)(src + page * sp + (j & smask) * st + (p - (int64_t)to * units) * 16);
+            }
+        }
+        if (a.in_place) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kMoveUnits; ++i) {
+            const int64_t p = p0 + i * kBlock + threadIdx.x;
+            if (p < end) {
+                const int to = (int)(p / units);
+                const int page = page_at(a.to, s, to >> a.to.page_shift);
+                if (page >= 0) *(u32x4*)(dst + page * dp + (to & dmask) * dt + (p - (int64_t)to * units) * 16) = x[i];
+            }
+        }
+    }
+}
+
+template <typename K, typename A>
+int enqueue(K kernel, int64_t blocks, int threads, void* stream, void* ev0, void* ev1, const A& a)
+{
+    if (blocks <= 0) return kNoLaunch;
+    if (ev0 && ev1)
+        hipExtLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), 0, (hipStream_t)stream, (hipEvent_t)ev0,
+                              (hipEvent_t)ev1, 0, a);
+    else
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), 0, (hipStream_t)stream, a);
+    return (int)hipGetLastError();
+}
+
+}  // namespace
+
+void append_shape(AppendArgs& a)
+{
+    a.lanes = 1;
+    while (a.lanes * 16 < a.c.dim) a.lanes *= 2;
+    const int per = kWave / a.lanes, rounds = (a.heads + 2 * a.c.kv_heads + per - 1) / per;
+    // few rows: a row's heads over several wavefronts
+    const int most = (rounds + 3) / 4;
+    a.parts = (int)std::max<int64_t>(1, std::min<int64_t>(most, 2048 / std::max(a.ch.n_rows, 1)));
+}
+
+void evict_shape(EvictArgs& a)
+{
+    const int units = a.from.dim * (a.dtype == kBF16 ? 2 : 4) / 16;
+    const int64_t rows = std::min(capacity(a.from), capacity(a.to));
+    a.col_parts = 1;
+    a.blocks = 1;
+    if (!a.in_place) {
+        a.blocks = (int)std::max<int64_t>(1, (rows * units + kBlock * kMoveUnits - 1) / (kBlock * kMoveUnits));
+        a.blocks = std::min(a.blocks, 64);
+    } else {
+        while (a.col_parts < 4 && units % (2 * a.col_parts) == 0) a.col_parts *= 2;
+    }
+}
+
+int launch_append(const AppendArgs& a, void* st, void* e0, void* e1)
+{
+    const int64_t blocks = ((int64_t)a.ch.n_rows * a.parts + kWaves - 1) / kWaves;
+    return a.dtype == kBF16 ? enqueue(k_append<kBF16>, blocks, kBlock, st, e0, e1, a)
+                            : enqueue(k_append<kF32>, blocks, kBlock, st, e0, e1, a);
+}
+
+int launch_select(const EvictArgs& a, void* st, void* e0, void* e1)
+{
+    return enqueue(k_select, (int64_t)a.from.n_seqs * a.from.kv_heads, kSelBlock, st, e0, e1, a);
+}
+
+int launch_move(const EvictArgs& a, void* st, void* e0, void* e1)
+{
+    return enqueue(k_move, (int64_t)a.from.n_seqs * a.from.kv_heads * 2 * a.col_parts * a.blocks, kBlock, st, e0, e1, a);
+}
+
+}  // namespace msao

@@ -15,68 +15,17 @@
 #include <vector>
 
 #include "../../include/msao.h"
+#include "msao_ctx.h"
 #include "msao_internal.h"
 #include "msao_wait.h"
 
 using namespace msao;
 
-// Slots of pinned staging: so many uploads may be waiting on the GPU before
-// the host waits for the oldest.
-constexpr int kStageSlots = 4;
-
-struct msao_ctx {
-    int device = 0;
-    std::string err;
-    // pinned staging slots, used in turn. The upload kernel's block b sets
-    // stage_done[slot * kUploadMaxBlocks + b] to stage_ticket[slot] once it
-    // has read the slot; until its stage_blocks[slot] blocks have, the slot
-    // is not written again.
-    void* stage[kStageSlots] = {};
-    size_t stage_cap[kStageSlots] = {};
-    uint32_t* stage_done = nullptr;   // pinned
-    uint32_t stage_ticket[kStageSlots] = {};
-    int stage_blocks[kStageSlots] = {};
-    hipStream_t stage_stream[kStageSlots] = {};
-    int next_slot = 0;
-    // slots in which the workgroups of a split row of logits meet. A call takes
-    // one whose last user has set ent_done[slot] to ent_ticket[slot]
-    EntSlot* ent_slot[kEntSlots] = {};
-    uint32_t* ent_done = nullptr;     // pinned, behind stage_done
-    uint32_t ent_ticket[kEntSlots] = {};
-    hipStream_t ent_stream[kEntSlots] = {};
-    int n_ent = 0, next_ent = 0;
-    // profiling: an event pair around every launch, averaged per kernel on query
-    bool profiling = false;
-    std::vector<hipEvent_t> pool;                       // free events
-    std::vector<std::pair<hipEvent_t, hipEvent_t>> rec[MSAO_NUM_KERNELS];
-    // tuning
-    int row_item_bytes = 8192;
-    int chain_frames = 0;       // frames per temporal work item; 0 = automatic
-    int xcd_order = -1;         // scoring block order: -1 automatic, 0 dispatch order, 1 one range per XCD
-    int clip_fuse = 1;          // the SimHash run scores and hashes its clips in one pass (k_clip)
-    int pair_path = 1;          // clips with rows of at most 4 KiB are scored by k_pair
-    int post_big_segment = kPostBigSegment;  // selections this large take 1024-thread blocks
-};
-
 namespace {
-
-thread_local std::string g_err;
-
-constexpr size_t kWsAlign = 256;
-
-size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
-
-int elt_size(int dtype) { return dtype == MSAO_F32 ? 4 : 2; }
 
 bool is_temporal(const msao_segment& s)
 {
     return s.modality == MSAO_VIDEO && s.n_frames >= 2 && s.tokens_per_frame > 0;
-}
-
-msao_status fail(std::string* err, msao_status st, const std::string& msg)
-{
-    if (err) *err = msg;
-    return st;
 }
 
 // Keep count: k = min(N, ceil(kappa * N)) in double.
@@ -661,31 +610,6 @@ void build_plan(const msao_ctx* ctx, const msao_segment* segs, int n, int R, con
     }
 }
 
-#define MSAO_TRY(x)                                                                                                   \
-    do {                                                                                                              \
-        msao_status st_ = (x);                                                                                        \
-        if (st_ != MSAO_OK) return st_;                                                                               \
-    } while (0)
-
-msao_status hip_fail(msao_ctx* ctx, hipError_t e, const char* what)
-{
-    ctx->err = std::string(what) + ": " + hipGetErrorString(e);
-    return MSAO_ERR_HIP;
-}
-
-struct DeviceGuard {
-    int prev = -1;
-    bool changed = false;
-    explicit DeviceGuard(int dev)
-    {
-        if (hipGetDevice(&prev) == hipSuccess && prev != dev) changed = hipSetDevice(dev) == hipSuccess;
-    }
-    ~DeviceGuard()
-    {
-        if (changed) (void)hipSetDevice(prev);
-    }
-};
-
 // Pinned staging slot `slot` of at least `bytes` (grown when smaller).
 msao_status reserve_stage(msao_ctx* ctx, int slot, size_t bytes)
 {
@@ -891,49 +815,6 @@ msao_status check_ws(msao_ctx* ctx, const Plan& pl, void* ws, size_t ws_bytes)
         std::snprintf(buf, sizeof buf, "workspace too small: %zu bytes given, %zu needed", ws_bytes, pl.total_bytes);
         return fail(&ctx->err, MSAO_ERR_WORKSPACE, buf);
     }
-    return MSAO_OK;
-}
-
-bool aligned(const void* p, size_t a) { return ((uintptr_t)p) % a == 0; }
-
-// Output arrays of 4 or 8 bytes must be naturally aligned.
-msao_status check_out_alignment(msao_ctx* ctx, std::initializer_list<std::pair<const void*, size_t>> ptrs)
-{
-    for (const auto& pr : ptrs)
-        if (pr.first && !aligned(pr.first, pr.second))
-            return fail(&ctx->err, MSAO_ERR_ALIGNMENT, "an output array is not naturally aligned");
-    return MSAO_OK;
-}
-
-hipEvent_t pooled_event(msao_ctx* ctx)
-{
-    if (!ctx->pool.empty()) {
-        hipEvent_t e = ctx->pool.back();
-        ctx->pool.pop_back();
-        return e;
-    }
-    hipEvent_t e = nullptr;
-    return hipEventCreate(&e) == hipSuccess ? e : nullptr;
-}
-
-// Launch, with profiling events recorded at the kernel's start and end.
-msao_status launched(msao_ctx* ctx, int kernel, hipStream_t stream, int (*fn)(const void*, void*, void*, void*),
-                     const void* args)
-{
-    hipEvent_t e0 = nullptr, e1 = nullptr;
-    if (ctx->profiling) {
-        e0 = pooled_event(ctx);
-        e1 = pooled_event(ctx);
-        if (!e0 || !e1) return fail(&ctx->err, MSAO_ERR_HIP, "hipEventCreate failed");
-    }
-    const int rc = fn(args, stream, e0, e1);
-    if (rc == kNoLaunch) {  // nothing to launch: the events were not recorded
-        if (e0) ctx->pool.push_back(e0);
-        if (e1) ctx->pool.push_back(e1);
-        return MSAO_OK;
-    }
-    if (rc != 0) return hip_fail(ctx, (hipError_t)rc, "kernel launch");
-    if (ctx->profiling) ctx->rec[kernel].push_back({e0, e1});
     return MSAO_OK;
 }
 
@@ -1185,12 +1066,16 @@ void msao_destroy(msao_ctx* ctx)
         }
     ent_slots_give(ctx->device, ctx->n_ent, ctx->ent_slot);
     if (all && ctx->stage_done) (void)hipHostFree(ctx->stage_done);
-    for (int k = 0; k < MSAO_NUM_KERNELS; ++k)
-        for (auto& pr : ctx->rec[k]) {
-            (void)hipEventSynchronize(pr.second);
-            ctx->pool.push_back(pr.first);
-            ctx->pool.push_back(pr.second);
-        }
+    auto reclaim = [&](std::vector<std::pair<hipEvent_t, hipEvent_t>>* rec, int n) {
+        for (int k = 0; k < n; ++k)
+            for (auto& pr : rec[k]) {
+                (void)hipEventSynchronize(pr.second);
+                ctx->pool.push_back(pr.first);
+                ctx->pool.push_back(pr.second);
+            }
+    };
+    reclaim(ctx->rec, MSAO_NUM_KERNELS);
+    reclaim(ctx->cache_rec, MSAO_NUM_CACHE_KERNELS);
     for (hipEvent_t e : ctx->pool) (void)hipEventDestroy(e);
     delete ctx;
 }
@@ -1207,23 +1092,7 @@ msao_status msao_set_profiling(msao_ctx* ctx, int enable)
 msao_status msao_kernel_times(msao_ctx* ctx, float* ms)
 {
     if (!ctx || !ms) return MSAO_ERR_INVALID_ARG;
-    DeviceGuard guard(ctx->device);
-    msao_status st = MSAO_OK;
-    for (int k = 0; k < MSAO_NUM_KERNELS; ++k) {
-        double sum = 0.0;
-        for (auto& pr : ctx->rec[k]) {
-            float t = 0.0f;
-            hipError_t e = hipEventSynchronize(pr.second);
-            if (e == hipSuccess) e = hipEventElapsedTime(&t, pr.first, pr.second);
-            if (e != hipSuccess && st == MSAO_OK) st = hip_fail(ctx, e, "msao_kernel_times");
-            sum += t;
-            ctx->pool.push_back(pr.first);
-            ctx->pool.push_back(pr.second);
-        }
-        ms[k] = ctx->rec[k].empty() ? 0.0f : (float)(sum / (double)ctx->rec[k].size());
-        ctx->rec[k].clear();
-    }
-    return st;
+    return mean_times(ctx, ctx->rec, MSAO_NUM_KERNELS, ms);
 }
 
 msao_status msao_mas_score(msao_ctx* ctx, const msao_segment* segs, int n, int R, const msao_params* params,

@@ -1,0 +1,126 @@
+"""Eviction from a paged cache on the GPU against its definition."""
+import numpy as np
+import pytest
+import torch
+
+from cache_ref import Case, evicted
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def target(case, cap_pages, order="head", weight=True, page=None):
+    import paper_2604_02945_amd as msao
+    page = page or case.page
+    n = case.B * cap_pages + 2
+    k = torch.full((n, case.kv_heads, page, case.dim), 5.0, dtype=case.dtype, device=DEV)
+    v = k.clone()
+    if order == "token":
+        k, v = (x.transpose(1, 2).contiguous().transpose(1, 2) for x in (k, v))
+    pages = torch.randperm(n, generator=case.g)[:case.B * cap_pages].view(case.B, cap_pages).to(torch.int32)
+    return msao.KvCache(k, v, pages.to(DEV), torch.full((case.B,), -3, dtype=torch.int32, device=DEV),
+                        torch.full((case.B, case.kv_heads, cap_pages * page), 5.0, device=DEV) if weight else None)
+
+
+def check(case, budget, n_first=0, n_recent=0, to=None):
+    import paper_2604_02945_amd as msao
+    cache, _ = case.device(DEV)
+    into = to if to is not None else cache
+    old_k, old_v, old_w = (x.clone() for x in (into.k, into.v, into.weight if into.weight is not None else into.length))
+    src_k, src_v = cache.k.cpu(), cache.v.cpu()
+    r = msao.msao_cache_evict(cache, torch.tensor(budget, dtype=torch.int32, device=DEV), n_first, n_recent, to=to)
+    torch.cuda.synchronize()
+    idx = r["kept_idx"].cpu().numpy()
+    bits = torch.int32 if case.dtype == F32 else torch.int16
+    pages = into.pages.cpu().numpy()
+    want_k, want_v, want_w = old_k.cpu(), old_v.cpu(), old_w.cpu()
+    for b in range(case.B):
+        for h in range(case.kv_heads):
+            kept = evicted(case.weight[b, h].numpy(), case.lengths[b], budget[b], into.capacity, n_first, n_recent)
+            assert np.array_equal(idx[b, h, :len(kept)], kept), (b, h)
+            assert (idx[b, h, len(kept):case.cap] == -1).all()
+            assert int(into.length[b]) == len(kept)
+            for to_j, j in enumerate(kept):
+                sp, dp = case.pages[b, j // case.page], pages[b, to_j // into.page_size]
+                if into.weight is not None:
+                    want_w[b, h, to_j] = case.weight[b, h, j]
+                if not 0 <= dp < into.n_pages:
+                    continue
+                there = 0 <= sp < case.n_pages
+                want_k[dp, h, to_j % into.page_size] = src_k[sp, h, j % case.page] if there else 0
+                want_v[dp, h, to_j % into.page_size] = src_v[sp, h, j % case.page] if there else 0
+    same = lambda a, b: torch.equal(a.cpu().contiguous().view(bits), b.contiguous().view(bits))  # noqa: E731
+    assert same(into.k, want_k) and same(into.v, want_v)
+    if into.weight is not None:
+        assert torch.equal(into.weight.cpu().view(torch.int32), want_w.view(torch.int32))
+    if to is not None:  # the source as it was
+        assert same(cache.k, case.k) and same(cache.v, case.v)
+        assert torch.equal(cache.weight.cpu().view(torch.int32), case.weight.view(torch.int32))
+        assert cache.length.tolist() == case.lengths
+
+
+LENGTHS = [0, 1, 15, 16, 17, 100, 257, 600]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("first,recent", [(0, 0), (4, 16), (1000, 1000), (0, 7), (3, 0)])
+@pytest.mark.parametrize("place", ["in place", "other pages"])
+def test_budgets(dtype, first, recent, place):
+    case = Case(31, LENGTHS, [0] * len(LENGTHS), 2, 2, 64, 16, dtype)
+    budget = [5, 0, 15, 8, 1, 60, 100, 599]
+    check(case, budget, first, recent, None if place == "in place" else target(case, 40))
+
+
+@pytest.mark.parametrize("dim,dtype", [(8, BF16), (40, F32), (72, BF16), (128, BF16), (256, F32), (96, BF16)])
+def test_dims_layouts_and_page_sizes(dim, dtype):
+    for order in ("head", "token", "mixed"):
+        case = Case(32, [100, 333, 64], [0] * 3, 3, 3, dim, 32, dtype, order=order)
+        check(case, [50, 200, 63], 2, 8)
+        check(case, [50, 200, 63], 2, 8, target(case, 4, "token", page=64))
+
+
+def test_more_than_a_block_of_tokens_at_once():
+    case = Case(33, [9000, 4097, 12345], [0] * 3, 1, 1, 64, 64, BF16)
+    check(case, [4500, 4096, 1], 4, 100)
+    check(case, [8000, 100, 12000], 4, 100, target(case, 200))
+
+
+@pytest.mark.parametrize("kind", ["ties", "zeros", "strange", "two values", "near"])
+def test_ties_go_to_the_lower_index(kind):
+    case = Case(34, [700, 333], [0, 0], 2, 2, 64, 16, BF16)
+    w = case.weight
+    if kind == "ties":
+        w.copy_((w * 4).floor())
+    elif kind == "zeros":
+        w.zero_()
+    elif kind == "strange":
+        odd = torch.tensor([float("nan"), float("inf"), -1.0, -0.0, 0.0, 1e-45, 3e38, float("-inf"), 1.0])
+        w.copy_(odd[torch.randint(0, len(odd), w.shape, generator=case.g)])
+    elif kind == "two values":
+        w.copy_((w > 0.5).float() * 2 ** -20 + 1)
+    else:
+        w.copy_(torch.randint(0, 5, w.shape, generator=case.g).int().add(0x3F800000).view(torch.float32))
+    check(case, [350, 100], 1, 3)
+    check(case, [350, 100], 1, 3, target(case, 40))
+
+
+def test_a_target_smaller_than_the_budget_bounds_it():
+    case = Case(35, [100, 200], [0, 0], 2, 2, 64, 16, BF16)
+    check(case, [90, 150], 2, 5, target(case, 2))
+
+
+def test_a_target_without_weight():
+    case = Case(36, [100, 200], [0, 0], 2, 2, 64, 16, BF16)
+    check(case, [40, 60], 2, 5, target(case, 8, weight=False))
+
+
+@pytest.mark.parametrize("bad", [-1, 10 ** 6])
+def test_pages_of_none(bad):
+    """Tokens taken from no page are zeros; what would go to no page is dropped."""
+    case = Case(37, [100, 64], [0, 0], 2, 2, 64, 16, BF16, bad_page=(0, 3, bad))
+    check(case, [70, 40], 2, 5, target(case, 8))
+    check(Case(37, [100, 64], [0, 0], 2, 2, 64, 16, BF16, bad_page=(0, 3, bad)), [70, 40], 2, 5)
+    to = target(case, 8)
+    to.pages[0, 1] = bad
+    check(case, [70, 40], 2, 5, to)
