@@ -617,9 +617,10 @@ msao_status msao_cache_evict_workspace(const msao_kv_cache* from, size_t* bytes)
 #define MSAO_CACHE_KERNEL_ATTEND 1
 #define MSAO_CACHE_KERNEL_COMBINE 2   /* parts of split rows joined */
 #define MSAO_CACHE_KERNEL_WEIGHT 3
-#define MSAO_CACHE_KERNEL_SELECT 4    /* eviction: the tokens that stay */
-#define MSAO_CACHE_KERNEL_MOVE 5      /* eviction: their keys and values */
-#define MSAO_NUM_CACHE_KERNELS 6
+#define MSAO_CACHE_KERNEL_WEIGHT_JOIN 4 /* its sums over parts of many rows */
+#define MSAO_CACHE_KERNEL_SELECT 5    /* eviction: the tokens that stay */
+#define MSAO_CACHE_KERNEL_MOVE 6      /* eviction: their keys and values */
+#define MSAO_NUM_CACHE_KERNELS 7
 msao_status msao_cache_kernel_times(msao_ctx* ctx, float* ms);
 
 /* ---- Sec. 4.2.2: Algorithm 1 on the host ----------------------------------- */

@@ -30,8 +30,8 @@ DECIDE_HOLD, DECIDE_SEND, DECIDE_OFFLOAD = 0, 1, 2
 MAX_AXES = 4
 APPEND_NEIGHBOURS = 1
 ATTEND_CAUSAL, ATTEND_WEIGHT = 1, 2
-(CACHE_KERNEL_APPEND, CACHE_KERNEL_ATTEND, CACHE_KERNEL_COMBINE, CACHE_KERNEL_WEIGHT, CACHE_KERNEL_SELECT,
- CACHE_KERNEL_MOVE, NUM_CACHE_KERNELS) = 0, 1, 2, 3, 4, 5, 6
+(CACHE_KERNEL_APPEND, CACHE_KERNEL_ATTEND, CACHE_KERNEL_COMBINE, CACHE_KERNEL_WEIGHT,
+ CACHE_KERNEL_WEIGHT_JOIN, CACHE_KERNEL_SELECT, CACHE_KERNEL_MOVE, NUM_CACHE_KERNELS) = 0, 1, 2, 3, 4, 5, 6, 7
 
 STATUS = {0: "MSAO_OK", 1: "MSAO_ERR_INVALID_ARG", 2: "MSAO_ERR_ALIGNMENT", 3: "MSAO_ERR_WORKSPACE",
           4: "MSAO_ERR_UNSUPPORTED", 5: "MSAO_ERR_HIP"}

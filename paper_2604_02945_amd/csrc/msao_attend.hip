@@ -13,10 +13,15 @@
 //                  those tokens; its A operand wants, of the same tokens, one channel a
 //                  lane: lane (c, i) loads channels [i*E, i*E+E) (E = padded dim / 16)
 //                  of tokens 4c..4c+3 and turns the block round with byte permutes.
-// The wavefronts of a workgroup take tiles in turn and join at the end through LDS;
-// workgroups that share a row's tokens leave parts in the workspace, which k_combine
-// joins. The running maximum is a reference that moves only when a score passes it by
-// more than 2^kSlack, so most tiles need no reduction across lanes and no rescaling.
+// The queries lie in LDS, from where each wavefront takes them tile by tile: what the
+// registers hold besides (K and V on their way, the output, the scores) then leaves two
+// wavefronts on a SIMD, so that loads, exponents and products of different ones overlap.
+// The wavefronts of a workgroup take tiles in turn (for more than 32 rows two of them
+// take the same tile, each for its half of the rows; the second reads it from a cache) and
+// join at the end through LDS; workgroups that share a row's tokens leave parts in the
+// workspace, which k_combine joins. The running maximum is a reference that moves only
+// when a score passes it by more than 2^kSlack, so most tiles need no reduction across
+// lanes and no rescaling.
 #include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -54,6 +59,9 @@ __device__ __forceinline__ const uint8_t* uniform(const uint8_t* p)
     const uint64_t v = (uint64_t)p;
     return (const uint8_t*)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
 }
+
+// Wavefronts on a SIMD that the registers are divided among: heads of 256 take more than half.
+constexpr int waves_per_simd(int dp) { return dp == 256 ? 1 : 2; }
 
 template <int DT> struct Type;
 template <> struct Type<kBF16> { static constexpr int kSize = 2; };
@@ -99,6 +107,16 @@ __device__ __forceinline__ uint32_t without_strange(uint32_t w)
     return ((w & 0x7F800000u) == 0x7F800000u ? 0u : w & 0xFFFF0000u) | ((w & 0x7F80u) == 0x7F80u ? 0u : w & 0xFFFFu);
 }
 
+// Sum over the 16 lanes of a row, in each of them.
+__device__ __forceinline__ float row_sum(float v)
+{
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xF, 0xF, false));  // turned by 8
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x124, 0xF, 0xF, false));
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x122, 0xF, 0xF, false));
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x121, 0xF, 0xF, false));
+    return v;
+}
+
 // Which (sequence, kv head, ...) a block of the flattened grid has.
 struct Place {
     int seq, head, n_new, begin, length;
@@ -119,12 +137,12 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a, int sh)
 __device__ __forceinline__ int call_rows(const AttendArgs& a, const Place& p) { return min(p.n_new, a.ch.max_new) * a.group; }
 
 // Pages of 64 half tiles (16 tokens) of a wavefront, one a lane: lane i has half i % NH of
-// tile first + i / NH of those the wavefront takes (every kWaves-th of NH halves).
+// tile first + i / NH of those that turn `turn` of `step` takes (every step-th of NH halves).
 template <int NH>
-__device__ __forceinline__ int lane_pages(const CacheDev& c, int seq, int lo, int hi, int wave, int first)
+__device__ __forceinline__ int lane_pages(const CacheDev& c, int seq, int lo, int hi, int turn, int step, int first)
 {
     const int lane = threadIdx.x & (kWave - 1);
-    const int64_t tok = (int64_t)lo + 16 * NH * (wave + kWaves * ((int64_t)first + lane / NH)) + 16 * (lane % NH);
+    const int64_t tok = (int64_t)lo + 16 * NH * (turn + step * ((int64_t)first + lane / NH)) + 16 * (lane % NH);
     return tok < hi ? page_at(c, seq, (int)(tok >> c.page_shift)) : -1;
 }
 
@@ -144,28 +162,42 @@ __device__ __forceinline__ Half half_of(const uint8_t* base, int64_t page_bytes,
     return h;
 }
 
-// The queries of 16 rows as B operands: lane (c, i) row i, 16 bytes from channel
-// (16 bytes) * (4 s + c) for step s. Rows past the last are zeros.
+// Rows of queries in LDS, a row a line of DP values and 16 bytes that spread the banks.
+// As a B operand lane (c, i) takes row i, 16 bytes from (16 bytes) * (4 s + c) for step s.
 template <int DT, int DP>
-struct Query {
-    static constexpr int kSteps = DP * Type<DT>::kSize / 64;
-    u32x4 v[kSteps];
-    __device__ __forceinline__ void load(const AttendArgs& a, const Place& p, int row, int n_rows)
+struct Queries {
+    static constexpr int kLine = DP * Type<DT>::kSize + 16;
+    static constexpr int kPieces = DP * Type<DT>::kSize / 16;  // of a row
+    // Piece `piece` of the row: zeros past the last row and past the head's channels.
+    __device__ static __forceinline__ u32x4 fetch(const AttendArgs& a, const Place& p, int row, int n_rows, int piece)
     {
-        const int c = (threadIdx.x & (kWave - 1)) >> 4;
         const int tok = row / a.group, head = p.head * a.group + (row - tok * a.group);
-        const uint8_t* src = a.q + (int64_t)(p.begin + tok) * a.q_stride + (int64_t)head * a.c.dim * Type<DT>::kSize;
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const int off = 64 * s + 16 * c;
-            v[s] = row < n_rows && off < a.c.dim * Type<DT>::kSize ? *(const u32x4*)(src + off) : u32x4{0, 0, 0, 0};
+        const int off = 16 * piece;
+        if (row >= n_rows || off >= a.c.dim * Type<DT>::kSize) return u32x4{0, 0, 0, 0};
+        return *(const u32x4*)(a.q + (int64_t)(p.begin + tok) * a.q_stride + (int64_t)head * a.c.dim * Type<DT>::kSize + off);
+    }
+    // `rows` rows from r0 by the whole workgroup; the caller waits for it.
+    __device__ static __forceinline__ void fill(uint8_t* lds, const AttendArgs& a, const Place& p, int r0, int rows, int n_rows)
+    {
+        for (int i = threadIdx.x; i < rows * kPieces; i += kBlock) {
+            const int row = i / kPieces, piece = i - row * kPieces;
+            *(u32x4*)(lds + row * kLine + 16 * piece) = fetch(a, p, r0 + row, n_rows, piece);
         }
+    }
+    // Operands of 16 rows from line `row`.
+    u32x4 v[kPieces / 4];
+    __device__ __forceinline__ void take(const uint8_t* lds, int row)
+    {
+        const int lane = threadIdx.x & (kWave - 1);
+        const uint8_t* src = lds + (row + (lane & 15)) * kLine + 16 * (lane >> 4);
+#pragma unroll
+        for (int s = 0; s < kPieces / 4; ++s) v[s] = *(const u32x4*)(src + 64 * s);
     }
 };
 
 // Scores of 16 tokens (rows of the result: lane (c, q) tokens 4c + r) and 16 queries.
 template <int DT, int DP>
-__device__ __forceinline__ f32x4 scores(const u32x4 (&k)[DP * Type<DT>::kSize / 64], const Query<DT, DP>& q)
+__device__ __forceinline__ f32x4 scores(const u32x4 (&k)[DP * Type<DT>::kSize / 64], const Queries<DT, DP>& q)
 {
     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -197,29 +229,32 @@ struct KeyOffsets {
     }
 };
 
-template <int DT, int DP, int MT>
-__global__ __launch_bounds__(kBlock) void k_attend(AttendArgs a)
+template <int DT, int DP, int MT, int RW>
+__global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArgs a)
 {
     constexpr int ES = Type<DT>::kSize;
     constexpr int KS = DP * ES / 64;   // pieces of a row of K a lane holds
     constexpr int E = DP / 16;         // channels of V a lane holds of a token
     constexpr int VW = E * ES / 4;     // as 32-bit words
-    // halves of a tile; float32 heads of 256 keep one of K and V in registers
-    constexpr int NH = DT == kF32 && DP == 256 ? 1 : 2, TT = 16 * NH;
+    // halves of a tile; of float32 heads of 128 and more the registers hold one
+    constexpr int NH = DT == kF32 && DP >= 128 ? 1 : 2, TT = 16 * NH;
     constexpr int LDP = DP + 4;        // floats between rows in LDS: spreads the banks
-    __shared__ __align__(16) float lds_o[kWaves][16][LDP];
+    constexpr int TW = kWaves / RW;    // wavefronts that take different tiles
+    constexpr int kQBytes = RW * MT * 16 * Queries<DT, DP>::kLine, kOBytes = kWaves * 16 * LDP * 4;
+    __shared__ __align__(16) uint8_t lds[kQBytes > kOBytes ? kQBytes : kOBytes];
     __shared__ float lds_m[kWaves][MT * 16], lds_l[kWaves][MT * 16];
+    float (*lds_o)[16][LDP] = (float (*)[16][LDP])lds;  // once the queries are used up
 
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
-    const int i16 = lane & 15, c = lane >> 4;
+    const int i16 = lane & 15, c = lane >> 4, rw = wave % RW, tw = wave / RW;
     int id = blockIdx.x;
     const int split = id % a.splits;
     id /= a.splits;
     const int tile = id % a.row_tiles;
     const Place p = place_of(a, id / a.row_tiles);
-    const int n_rows = call_rows(a, p), r0 = tile * MT * 16;
+    const int n_rows = call_rows(a, p), r0 = tile * RW * MT * 16;
     if (r0 >= n_rows) return;
-    const int r_end = min(r0 + MT * 16, n_rows);
+    const int r_end = min(r0 + RW * MT * 16, n_rows);
     const int seen = group_sees(p.length, p.n_new, a.group, r_end - 1, a.causal);
     const Cut cut = cut_tokens(seen, a.splits);
     if (split >= max(cut.n, 1)) return;
@@ -233,12 +268,13 @@ __global__ __launch_bounds__(kBlock) void k_attend(AttendArgs a)
 #pragma unroll
     for (int r = 0; r < 4; ++r) vo[r] = i16 * E * ES < row_bytes ? (4 * c + r) * (int)a.c.v_tok + i16 * E * ES : kFar;
 
-    Query<DT, DP> q[MT];
+    Queries<DT, DP>::fill(lds, a, p, r0, RW * MT * 16, n_rows);
+    const int line0 = rw * MT * 16;                                       // the wavefront's rows
+    const int used = clamp_int((n_rows - r0 - line0 + 15) / 16, 0, MT);   // and how many sixteens of them there are
     int last[MT];  // the last token that the lane's row sees
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-        const int row = r0 + 16 * m + i16;
-        q[m].load(a, p, row, n_rows);
+        const int row = r0 + line0 + 16 * m + i16;
         last[m] = a.causal ? p.length - p.n_new + row / a.group : p.length - 1;
     }
     const int least = a.causal ? p.length - p.n_new + r0 / a.group : p.length - 1;  // of all rows
@@ -254,13 +290,13 @@ __global__ __launch_bounds__(kBlock) void k_attend(AttendArgs a)
     }
 
     const int tiles = (hi - lo + TT - 1) / TT;
-    const int mine = tiles > wave ? (tiles - wave + kWaves - 1) / kWaves : 0;
+    const int mine = used > 0 && tiles > tw ? (tiles - tw + TW - 1) / TW : 0;
     u32x4 kf[NH][KS];
     uint32_t vf[NH][4][VW];
-    int pages = lane_pages<NH>(a.c, p.seq, lo, hi, wave, 0);
+    int pages = lane_pages<NH>(a.c, p.seq, lo, hi, tw, TW, 0);
     int kn[NH], next_n[NH];
     auto load_k = [&](int it) {
-        const int tok = lo + TT * (wave + kWaves * it);
+        const int tok = lo + TT * (tw + TW * it);
 #pragma unroll
         for (int h = 0; h < NH; ++h) {
             const int page = __builtin_amdgcn_readlane(pages, (NH * it + h) & 63);
@@ -271,7 +307,7 @@ __global__ __launch_bounds__(kBlock) void k_attend(AttendArgs a)
         }
     };
     auto load_v = [&](int it) {
-        const int tok = lo + TT * (wave + kWaves * it);
+        const int tok = lo + TT * (tw + TW * it);
 #pragma unroll
         for (int h = 0; h < NH; ++h) {
             const int page = __builtin_amdgcn_readlane(pages, (NH * it + h) & 63);
@@ -284,9 +320,10 @@ __global__ __launch_bounds__(kBlock) void k_attend(AttendArgs a)
         load_k(0);
         load_v(0);
     }
+    __syncthreads();
     bool left_out = false;
     for (int it = 0; it < mine; ++it) {
-        const int tok = lo + TT * (wave + kWaves * it);
+        const int tok = lo + TT * (tw + TW * it);
         const bool seen_whole = tok + TT <= hi && tok + TT - 1 <= least;  // all of it, by every row
         bool whole = seen_whole;
 #pragma unroll
@@ -296,16 +333,20 @@ __global__ __launch_bounds__(kBlock) void k_attend(AttendArgs a)
         }
         float x[MT][4 * NH];
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int m = 0; m < MT; ++m) {
+            if (m >= used) break;
+            Queries<DT, DP> q;
+            q.take(lds, line0 + 16 * m);
 #pragma unroll
             for (int h = 0; h < NH; ++h) {
-                const f32x4 s = scores<DT, DP>(kf[h], q[m]);
+                const f32x4 s = scores<DT, DP>(kf[h], q);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) x[m][4 * h + r] = s[r] * a.scale;
             }
+        }
         // (V of this tile is on its way: the lanes' pages may be the next ones)
         if (it + 1 < mine) {
-            if (((it + 1) & (64 / NH - 1)) == 0) pages = lane_pages<NH>(a.c, p.seq, lo, hi, wave, it + 1);
+            if (((it + 1) & (64 / NH - 1)) == 0) pages = lane_pages<NH>(a.c, p.seq, lo, hi, tw, TW, it + 1);
             load_k(it + 1);
         }
         if (!whole) {
@@ -321,15 +362,17 @@ __global__ __launch_bounds__(kBlock) void k_attend(AttendArgs a)
         }
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
+            if (m >= used) break;
             float most = x[m][0];
 #pragma unroll
             for (int e = 1; e < 4 * NH; ++e) most = fmaxf(most, x[m][e]);
             if (__ballot(most > ref[m] + kSlack) != 0) {
                 most = fmaxf(most, __shfl_xor(most, 16));
                 most = fmaxf(most, __shfl_xor(most, 32));
-                const float up = fmaxf(most, ref[m]);
+                // (a row that its own scores do not move stays as it is, bit for bit)
+                const float up = most > ref[m] + kSlack ? most : ref[m];
                 // (ref -inf: the sums are 0 and stay 0)
-                const float sc = ref[m] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref[m] - up);
+                const float sc = ref[m] == up ? 1.0f : ref[m] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref[m] - up);
                 ref[m] = up;
                 sum[m] *= sc;
 #pragma unroll
@@ -379,8 +422,9 @@ __global__ __launch_bounds__(kBlock) void k_attend(AttendArgs a)
                     vt[e] = __builtin_amdgcn_perm(vf[e / 2][2 * (e & 1) + 1][t / 2], vf[e / 2][2 * (e & 1)][t / 2], sel);
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
-                    o[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vt),
-                                                                      __builtin_bit_cast(bf16x8, pb[m]), o[m][t], 0, 0, 0);
+                    if (m < used)
+                        o[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vt),
+                                                                          __builtin_bit_cast(bf16x8, pb[m]), o[m][t], 0, 0, 0);
             }
         } else {
 #pragma unroll
@@ -391,8 +435,9 @@ __global__ __launch_bounds__(kBlock) void k_attend(AttendArgs a)
                     for (int t = 0; t < E; ++t)
 #pragma unroll
                         for (int m = 0; m < MT; ++m)
-                            o[m][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[h][r][t]), x[m][4 * h + r],
-                                                                           o[m][t], 0, 0, 0);
+                            if (m < used)
+                                o[m][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[h][r][t]), x[m][4 * h + r],
+                                                                               o[m][t], 0, 0, 0);
         }
         if (it + 1 < mine) load_v(it + 1);
     }
@@ -401,8 +446,8 @@ __global__ __launch_bounds__(kBlock) void k_attend(AttendArgs a)
         // the values left out, to the rows that see them: whatever the weight, it is above 0, and
         // the sum is infinite or NaN. From the first tile that some row does not see all of
 #pragma unroll 1
-        for (int it = max(0, (least + 1 - lo) / TT - wave) / kWaves; it < mine; ++it) {
-            const int tok = lo + TT * (wave + kWaves * it);
+        for (int it = max(0, (least + 1 - lo) / TT - tw) / TW; it < mine; ++it) {
+            const int tok = lo + TT * (tw + TW * it);
             if (tok + TT <= hi && tok + TT - 1 <= least) continue;
 #pragma unroll 1
             for (int t = tok; t < min(tok + TT, hi); ++t) {
@@ -448,7 +493,7 @@ __global__ __launch_bounds__(kBlock) void k_attend(AttendArgs a)
         if (r0 + 16 * m >= n_rows) break;
         float most = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) most = fmaxf(most, lds_m[w][16 * m + i16]);
+        for (int w = 0; w < TW; ++w) most = fmaxf(most, lds_m[w * RW + rw][16 * m + i16]);
         const float sc = ref[m] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref[m] - most);
         // lane (c, q): channel (4c + r) E + t of tile t
 #pragma unroll
@@ -456,21 +501,23 @@ __global__ __launch_bounds__(kBlock) void k_attend(AttendArgs a)
 #pragma unroll
             for (int t = 0; t < E; ++t) lds_o[wave][i16][(4 * c + r) * E + t] = o[m][t][r] * sc;
         __syncthreads();
-        const int row = r0 + 16 * m + orow;
-        if (row < n_rows && od < a.c.dim) {
+#pragma unroll
+        for (int g = 0; g < RW; ++g) {
+            const int line = 16 * m + orow, row = r0 + g * MT * 16 + line;
+            if (row >= n_rows || od >= a.c.dim) continue;
             float mm = -INFINITY, l = 0.0f, acc[E];
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, lds_m[w][16 * m + orow]);
+            for (int w = 0; w < TW; ++w) mm = fmaxf(mm, lds_m[w * RW + g][line]);
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                const float mw = lds_m[w][16 * m + orow];
-                l += mw == -INFINITY ? 0.0f : lds_l[w][16 * m + orow] * __builtin_amdgcn_exp2f(mw - mm);
+            for (int w = 0; w < TW; ++w) {
+                const float mw = lds_m[w * RW + g][line];
+                l += mw == -INFINITY ? 0.0f : lds_l[w * RW + g][line] * __builtin_amdgcn_exp2f(mw - mm);
             }
 #pragma unroll
             for (int t = 0; t < E; ++t) {
-                acc[t] = lds_o[0][orow][od + t];
+                acc[t] = lds_o[g][orow][od + t];
 #pragma unroll
-                for (int w = 1; w < kWaves; ++w) acc[t] += lds_o[w][orow][od + t];
+                for (int w = 1; w < TW; ++w) acc[t] += lds_o[w * RW + g][orow][od + t];
             }
             const int tok = row / a.group, head = p.head * a.group + (row - tok * a.group);
             const int64_t at = (int64_t)(p.begin + tok) * a.heads + head;
@@ -504,119 +551,316 @@ __global__ __launch_bounds__(kBlock) void k_attend(AttendArgs a)
     }
 }
 
-// Parts of split rows joined: a wavefront a row.
-template <int DT>
+// Parts of split rows joined: W wavefronts a row. DP / 4 lanes hold four channels each of a
+// part; the lanes' groups take parts in turn, four in flight, and join at the end.
+template <int DT, int DP, int W>
 __global__ __launch_bounds__(kBlock) void k_combine(AttendArgs a, int blocks_per)
 {
     constexpr int ES = Type<DT>::kSize;
+    constexpr int LP = DP / 4, kGroups = W * kWave / LP, kFly = 4;
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
     const int sh = blockIdx.x / blocks_per;
     const Place p = place_of(a, sh);
-    const int n_rows = call_rows(a, p), row = (blockIdx.x - sh * blocks_per) * kWaves + wave;
-    if (row >= n_rows) return;
+    const int n_rows = call_rows(a, p), row = (blockIdx.x - sh * blocks_per) * (kWaves / W) + wave / W;
+    if (row >= n_rows) return;  // (W = kWaves: the whole block)
     const int r_end = min(row / a.tile_rows * a.tile_rows + a.tile_rows, n_rows);
     const int seen = group_sees(p.length, p.n_new, a.group, r_end - 1, a.causal);
     const Cut cut = cut_tokens(seen, a.splits);
     if (cut.n <= 1) return;  // written by k_attend
     const int tok = row / a.group, head = p.head * a.group + (row - tok * a.group);
     const int64_t all = (int64_t)a.ch.n_rows * a.heads, at = (int64_t)(p.begin + tok) * a.heads + head;
-    float most = -INFINITY;
-    for (int i = lane; i < cut.n; i += kWave) most = fmaxf(most, a.part_ml[2 * (i * all + at)]);
+    const int t = wave % W * kWave + lane, group = t / LP, ch = (t & (LP - 1)) * 4;
+    const bool has = ch < a.c.dim;
+    float most = -INFINITY, l = 0.0f;
+    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    auto join = [&](float m2, float l2, const f32x4& o2) {
+        const float up = fmaxf(most, m2), base = up == -INFINITY ? 0.0f : up;
+        const float s1 = __builtin_amdgcn_exp2f(most - base), s2 = __builtin_amdgcn_exp2f(m2 - base);
+        most = up;
+        l = l * s1 + l2 * s2;
 #pragma unroll
-    for (int s = 1; s < kWave; s <<= 1) most = fmaxf(most, __shfl_xor(most, s));
-    const float base = most == -INFINITY ? 0.0f : most;
-    float l = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // channels lane, lane + 64, ...
-    for (int i = 0; i < cut.n; ++i) {
-        const f32x2 ml = *(const f32x2*)(a.part_ml + 2 * (i * all + at));
-        const float sc = __builtin_amdgcn_exp2f(ml.x - base);
-        l = fmaf(ml.y, sc, l);
-        const float* po = a.part_o + (i * all + at) * a.c.dim;
+        for (int e = 0; e < 4; ++e) acc[e] = acc[e] * s1 + o2[e] * s2;
+    };
+    for (int i0 = group; i0 < cut.n; i0 += kGroups * kFly) {
+        f32x2 ml[kFly];
+        f32x4 o[kFly];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (lane + kWave * e < a.c.dim) acc[e] = fmaf(po[lane + kWave * e], sc, acc[e]);
+        for (int f = 0; f < kFly; ++f) {
+            const int i = i0 + f * kGroups;
+            ml[f] = f32x2{-INFINITY, 0.0f};
+            o[f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (i < cut.n) {
+                ml[f] = *(const f32x2*)(a.part_ml + 2 * (i * all + at));
+                if (has) o[f] = *(const f32x4*)(a.part_o + (i * all + at) * a.c.dim + ch);
+            }
+        }
+#pragma unroll
+        for (int f = 0; f < kFly; ++f) join(ml[f].x, ml[f].y, o[f]);
     }
+#pragma unroll
+    for (int s = LP; s < kWave; s <<= 1) {
+        f32x4 o2;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o2[e] = __shfl_xor(acc[e], s);
+        join(__shfl_xor(most, s), __shfl_xor(l, s), o2);
+    }
+    if constexpr (W > 1) {
+        __shared__ float lds[W][LP][6];
+        if (lane < LP) {
+            float* d = lds[wave][lane];
+            d[0] = most;
+            d[1] = l;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) d[2 + e] = acc[e];
+        }
+        __syncthreads();
+        if (threadIdx.x >= LP) return;
+#pragma unroll
+        for (int w = 1; w < W; ++w) {
+            const float* d = lds[w][lane];
+            join(d[0], d[1], f32x4{d[2], d[3], d[4], d[5]});
+        }
+    } else if (lane >= LP) return;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    uint8_t* dst = a.out + (int64_t)(p.begin + tok) * a.out_stride + (int64_t)head * a.c.dim * ES;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int d = lane + kWave * e;
-        if (d >= a.c.dim) break;
-        if constexpr (DT == kBF16) ((uint16_t*)dst)[d] = (uint16_t)pack_bf16(acc[e] * inv, 0.0f);
-        else ((float*)dst)[d] = acc[e] * inv;
+    uint8_t* dst = a.out + (int64_t)(p.begin + tok) * a.out_stride + ((int64_t)head * a.c.dim + ch) * ES;
+    if (has) {
+        if constexpr (DT == kBF16) *(u32x2*)dst = u32x2{pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)};
+        else *(f32x4*)dst = f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
     }
-    if (lane == 0) {
+    if (ch == 0) {
         const float z = l == 0.0f ? -INFINITY : most + __builtin_amdgcn_logf(l);
         if (a.lse) a.lse[at] = z * kLn2;
         if (a.lse2) a.lse2[at] = z;
     }
 }
 
-// The weight that each token receives: a wavefront holds the keys of 32 tokens and
-// goes over the rows, 16 at a time, whose sums (lse2) are known by now:
+// The weight that each token receives, once the rows' sums (lse2) are known:
 //   weight_j += sum_i 2^(x_ij - lse2_i).
-// Lane (c, q) sums tokens 4c + r over its rows; the 16 lanes are added at the end. Every
+// Lane (c, q) sums tokens 4c + r over its rows, and 16 lanes are added at the end. Every
 // token has one wavefront, so no atomics, and the order of the sum is fixed.
-template <int DT, int DP>
-__global__ __launch_bounds__(kBlock) void k_weight(AttendArgs a)
+//
+// Few rows (k_weight): K streams by as in k_attend, past the queries in LDS.
+template <int DT, int DP, int MT>
+__global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight(AttendArgs a)
 {
     constexpr int ES = Type<DT>::kSize;
     constexpr int KS = DP * ES / 64;
+    __shared__ __align__(16) uint8_t lds[MT * 16 * Queries<DT, DP>::kLine];
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
     const int i16 = lane & 15, c = lane >> 4;
-    const int sh = blockIdx.x / a.weight_blocks, block = blockIdx.x - sh * a.weight_blocks;
+    const int sh = blockIdx.x / a.weight_parts, part = blockIdx.x - sh * a.weight_parts;
     const Place p = place_of(a, sh);
     const int n_rows = call_rows(a, p);
     if (n_rows == 0) return;
     const int seen = group_sees(p.length, p.n_new, a.group, n_rows - 1, a.causal);
+    const Cut cut = cut_tokens(seen, a.weight_parts);
+    if (part >= cut.n) return;
+    const int lo = part * cut.per, hi = min(seen, lo + cut.per);
     const int row_bytes = a.c.dim * ES, mask = (1 << a.c.page_shift) - 1;
     const uint8_t* kb = a.c.k + (int64_t)p.head * a.c.k_head;
     const KeyOffsets<DT, DP> ko(a.c.k_tok, row_bytes);
     float* weight = a.c.weight + (int64_t)sh * a.c.weight_stride;
-    for (int64_t t = (int64_t)block * kWaves + wave; t * kTile < seen; t += (int64_t)a.weight_blocks * kWaves) {
-        const int tok = (int)t * kTile;
-        u32x4 kf[2][KS];
-        int kn[2];
+    Queries<DT, DP>::fill(lds, a, p, 0, MT * 16, n_rows);
+    const int used = min((n_rows + 15) / 16, MT);
+    float z[MT];   // the row's sum (rows of no weight: +inf, which gives 0)
+    int last[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const int row = 16 * m + i16, tok = row / a.group, head = p.head * a.group + (row - tok * a.group);
+        z[m] = row < n_rows ? a.lse2[(int64_t)(p.begin + tok) * a.heads + head] : INFINITY;
+        if (z[m] == -INFINITY) z[m] = INFINITY;
+        last[m] = a.causal ? p.length - p.n_new + tok : p.length - 1;
+    }
+    const int least = a.causal ? p.length - p.n_new : p.length - 1;
+    const int tiles = (hi - lo + kTile - 1) / kTile, mine = tiles > wave ? (tiles - wave + kWaves - 1) / kWaves : 0;
+    u32x4 kf[2][KS];
+    float old[8];
+    int kn[2], next_n[2];
+    int pages = lane_pages<2>(a.c, p.seq, lo, hi, wave, kWaves, 0);
+    auto load_k = [&](int it) {
+        const int tok = lo + kTile * (wave + kWaves * it);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int page = tok + 16 * h < seen ? page_at(a.c, p.seq, (tok + 16 * h) >> a.c.page_shift) : -1;
-            const Half f = half_of(kb, a.c.k_page, a.c.k_tok, row_bytes, uniform(page), tok + 16 * h, seen, mask);
-            kn[h] = f.n;
+            const int page = __builtin_amdgcn_readlane(pages, (2 * it + h) & 63);
+            const Half f = half_of(kb, a.c.k_page, a.c.k_tok, row_bytes, page, tok + 16 * h, hi, mask);
+            next_n[h] = f.n;
 #pragma unroll
             for (int s = 0; s < KS; ++s) kf[h][s] = __builtin_amdgcn_raw_buffer_load_b128(f.r, ko.off[s], 0, 0);
         }
+    };
+    if (mine > 0) load_k(0);
+    __syncthreads();
+    for (int it = 0; it < mine; ++it) {
+        const int tok = lo + kTile * (wave + kWaves * it);
+        bool whole = tok + kTile - 1 <= least;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            kn[h] = next_n[h];
+            whole = whole && kn[h] == 16;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                old[4 * h + r] = i16 == 0 && 4 * c + r < kn[h] ? weight[tok + 16 * h + 4 * c + r] : 0.0f;
+        }
         float w[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-        // the first row that sees the tile's first token
-        const int from = a.causal ? max(0, tok - (p.length - p.n_new)) * a.group & ~15 : 0;
-        for (int r0 = from; r0 < n_rows; r0 += 16) {
-            const int row = r0 + i16;
-            Query<DT, DP> q;
-            q.load(a, p, row, n_rows);
-            const int qt = row / a.group, head = p.head * a.group + (row - qt * a.group);
-            const float z = row < n_rows ? a.lse2[(int64_t)(p.begin + qt) * a.heads + head] : -INFINITY;
-            const int last = a.causal ? p.length - p.n_new + qt : p.length - 1;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            if (m >= used) break;
+            Queries<DT, DP> q;
+            q.take(lds, 16 * m);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const f32x4 s = scores<DT, DP>(kf[h], q);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int j = 4 * c + r;
-                    const bool sees = z != -INFINITY && j < kn[h] && tok + 16 * h + j <= last;
-                    w[4 * h + r] += sees ? __builtin_amdgcn_exp2f(fmaf(s[r], a.scale, -z)) : 0.0f;
+                    const float x = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale, -z[m]));
+                    w[4 * h + r] += whole || (j < kn[h] && tok + 16 * h + j <= last[m]) ? x : 0.0f;
                 }
             }
         }
+        if (it + 1 < mine) {
+            if (((it + 1) & 31) == 0) pages = lane_pages<2>(a.c, p.seq, lo, hi, wave, kWaves, it + 1);
+            load_k(it + 1);
+        }
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-#pragma unroll
-            for (int s = 1; s < 16; s <<= 1) w[e] += __shfl_xor(w[e], s);
+        for (int e = 0; e < 8; ++e) w[e] = row_sum(w[e]);
         if (i16 == 0) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    if (4 * c + r < kn[h]) weight[tok + 16 * h + 4 * c + r] += w[4 * h + r];
+                    if (4 * c + r < kn[h]) weight[tok + 16 * h + 4 * c + r] = old[4 * h + r] + w[4 * h + r];
         }
     }
+}
+
+// Many rows (k_weight_rows): a wavefront keeps the keys of 32 tokens, and the rows stream
+// by through LDS, 64 at a time, the next ones on their way meanwhile. The rows that see a
+// block's tokens are cut into row_parts parts, so that a few short prompts fill the
+// device too; k_weight_join adds the parts' sums in order.
+constexpr int kRowStep = 64;
+template <int DT, int DP>
+__global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight_rows(AttendArgs a)
+{
+    constexpr int ES = Type<DT>::kSize;
+    constexpr int KS = DP * ES / 64;
+    using Q = Queries<DT, DP>;
+    constexpr int kPer = kRowStep * Q::kPieces / kBlock;  // pieces of a thread
+    __shared__ __align__(16) uint8_t lds[kRowStep * Q::kLine];
+    __shared__ float lds_z[kRowStep];
+    __shared__ int lds_last[kRowStep];
+    const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
+    const int i16 = lane & 15, c = lane >> 4;
+    int id = blockIdx.x;
+    const int part = id % a.row_parts;
+    id /= a.row_parts;
+    const int sh = id / a.weight_parts, block = id - sh * a.weight_parts;
+    const Place p = place_of(a, sh);
+    const int n_rows = call_rows(a, p);
+    const int seen = n_rows > 0 ? group_sees(p.length, p.n_new, a.group, n_rows - 1, a.causal) : 0;
+    const int b0 = block * kTile * kWaves;
+    if (b0 >= seen) return;
+    const int tok = b0 + kTile * wave;
+    const int row_bytes = a.c.dim * ES, mask = (1 << a.c.page_shift) - 1;
+    const uint8_t* kb = a.c.k + (int64_t)p.head * a.c.k_head;
+    const KeyOffsets<DT, DP> ko(a.c.k_tok, row_bytes);
+    u32x4 kf[2][KS];
+    int kn[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int t = tok + 16 * h, page = t < seen ? page_at(a.c, p.seq, t >> a.c.page_shift) : -1;
+        const Half f = half_of(kb, a.c.k_page, a.c.k_tok, row_bytes, uniform(page), t, seen, mask);
+        kn[h] = f.n;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) kf[h][s] = __builtin_amdgcn_raw_buffer_load_b128(f.r, ko.off[s], 0, 0);
+    }
+    // rows from the first that sees the block's first token, this part's share of them
+    const int from = a.causal ? max(0, b0 - (p.length - p.n_new)) * a.group : 0;
+    const int steps = (n_rows - from + kRowStep - 1) / kRowStep, per = (steps + a.row_parts - 1) / a.row_parts;
+    const int s_end = min(steps, (part + 1) * per);
+    float w[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    u32x4 next[kPer];
+    float next_z = INFINITY;
+    int next_last = -1;
+    auto fetch = [&](int step) {
+        const int r0 = from + step * kRowStep;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int at = i * kBlock + threadIdx.x, row = at / Q::kPieces;
+            next[i] = Q::fetch(a, p, r0 + row, n_rows, at - row * Q::kPieces);
+        }
+        if (threadIdx.x < kRowStep) {
+            const int row = r0 + threadIdx.x, t = row / a.group, head = p.head * a.group + (row - t * a.group);
+            next_z = row < n_rows ? a.lse2[(int64_t)(p.begin + t) * a.heads + head] : INFINITY;
+            if (next_z == -INFINITY) next_z = INFINITY;
+            next_last = a.causal ? p.length - p.n_new + t : p.length - 1;
+        }
+    };
+    if (part * per < s_end) fetch(part * per);
+    for (int step = part * per; step < s_end; ++step) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int at = i * kBlock + threadIdx.x, row = at / Q::kPieces;
+            *(u32x4*)(lds + row * Q::kLine + 16 * (at - row * Q::kPieces)) = next[i];
+        }
+        if (threadIdx.x < kRowStep) {
+            lds_z[threadIdx.x] = next_z;
+            lds_last[threadIdx.x] = next_last;
+        }
+        __syncthreads();
+        if (step + 1 < s_end) fetch(step + 1);
+        const int r0 = from + step * kRowStep;
+        const int least = a.causal ? p.length - p.n_new + r0 / a.group : p.length - 1;
+        const bool whole = kn[0] == 16 && kn[1] == 16 && tok + kTile - 1 <= least;
+#pragma unroll
+        for (int m = 0; m < kRowStep / 16; ++m) {
+            Q q;
+            q.take(lds, 16 * m);
+            const float z = lds_z[16 * m + i16];
+            const int last = lds_last[16 * m + i16];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const f32x4 s = scores<DT, DP>(kf[h], q);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int j = 4 * c + r;
+                    const float x = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale, -z));
+                    w[4 * h + r] += whole || (j < kn[h] && tok + 16 * h + j <= last) ? x : 0.0f;
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = row_sum(w[e]);
+    if (i16 != 0) return;
+    float* weight = a.c.weight + (int64_t)sh * a.c.weight_stride;
+    float* mine = a.part_w + ((int64_t)part * a.c.n_seqs * a.c.kv_heads + sh) * capacity(a.c);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int t = tok + 16 * h + 4 * c + r;
+            if (4 * c + r >= kn[h]) continue;
+            if (a.row_parts == 1) weight[t] += w[4 * h + r];
+            else mine[t] = w[4 * h + r];
+        }
+}
+
+__global__ __launch_bounds__(kBlock) void k_weight_join(AttendArgs a, int blocks_per)
+{
+    const int sh = blockIdx.x / blocks_per;
+    const Place p = place_of(a, sh);
+    const int n_rows = call_rows(a, p);
+    const int seen = n_rows > 0 ? group_sees(p.length, p.n_new, a.group, n_rows - 1, a.causal) : 0;
+    const int t = (blockIdx.x - sh * blocks_per) * kBlock + threadIdx.x;
+    // (a token of no page got nothing)
+    if (t >= seen || page_at(a.c, p.seq, t >> a.c.page_shift) < 0) return;
+    const int64_t step = (int64_t)a.c.n_seqs * a.c.kv_heads * capacity(a.c);
+    const float* src = a.part_w + (int64_t)sh * capacity(a.c) + t;
+    float w = 0.0f;
+    for (int i = 0; i < a.row_parts; ++i) w += src[i * step];
+    a.c.weight[(int64_t)sh * a.c.weight_stride + t] += w;
 }
 
 template <typename K, typename... A>
@@ -635,75 +879,112 @@ int padded_dim(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 
 int64_t pairs(const AttendArgs& a) { return (int64_t)a.c.n_seqs * a.c.kv_heads; }
 
+// Rows of a workgroup: what the registers of its wavefronts hold.
 template <int DT, int DP>
 int attend_rows(const AttendArgs& a, void* st, void* e0, void* e1)
 {
     const int64_t blocks = pairs(a) * a.row_tiles * a.splits;
-    if (a.tile_rows == 16) return enqueue(k_attend<DT, DP, 1>, blocks, st, e0, e1, a);
-    if constexpr (DP <= 128)
-        if (a.tile_rows == 32) return enqueue(k_attend<DT, DP, 2>, blocks, st, e0, e1, a);
-    if constexpr (DT == kBF16 && DP <= 128)
-        if (a.tile_rows == 64) return enqueue(k_attend<DT, DP, 4>, blocks, st, e0, e1, a);
+    if (a.tile_rows == 16) return enqueue(k_attend<DT, DP, 1, 1>, blocks, st, e0, e1, a);
+    if constexpr (DP == 256) {
+        if (a.tile_rows == 32) return enqueue(k_attend<DT, DP, 1, 2>, blocks, st, e0, e1, a);
+    } else {
+        if (a.tile_rows == 32) return enqueue(k_attend<DT, DP, 2, 1>, blocks, st, e0, e1, a);
+        if (a.tile_rows == 64) return enqueue(k_attend<DT, DP, 2, 2>, blocks, st, e0, e1, a);
+    }
     return (int)hipErrorInvalidValue;
 }
+
+template <int DT, int DP>
+int combine_rows(const AttendArgs& a, void* st, void* e0, void* e1)
+{
+    const int rows = a.ch.max_new * a.group;
+    // many parts: the whole block on one row
+    if (a.splits > 16) return enqueue(k_combine<DT, DP, kWaves>, pairs(a) * rows, st, e0, e1, a, rows);
+    const int per = (rows + kWaves - 1) / kWaves;
+    return enqueue(k_combine<DT, DP, 1>, pairs(a) * per, st, e0, e1, a, per);
+}
+
+template <int DT, int DP>
+int weight_rows(const AttendArgs& a, void* st, void* e0, void* e1)
+{
+    const int64_t blocks = pairs(a) * a.weight_parts * a.row_parts;
+    const int64_t rows = (int64_t)a.ch.max_new * a.group;
+    if (rows > kRowStep) return enqueue(k_weight_rows<DT, DP>, blocks, st, e0, e1, a);
+    return rows <= 16 ? enqueue(k_weight<DT, DP, 1>, blocks, st, e0, e1, a) : enqueue(k_weight<DT, DP, 4>, blocks, st, e0, e1, a);
+}
+
+template <template <int, int> class F>
+int by_type(const AttendArgs& a, void* st, void* e0, void* e1)
+{
+    const int dp = padded_dim(a.c.dim);
+    if (a.dtype == kBF16)
+        return dp == 64 ? F<kBF16, 64>::go(a, st, e0, e1) : dp == 128 ? F<kBF16, 128>::go(a, st, e0, e1)
+                                                                      : F<kBF16, 256>::go(a, st, e0, e1);
+    return dp == 64 ? F<kF32, 64>::go(a, st, e0, e1) : dp == 128 ? F<kF32, 128>::go(a, st, e0, e1)
+                                                                 : F<kF32, 256>::go(a, st, e0, e1);
+}
+template <int DT, int DP> struct Attend {
+    static int go(const AttendArgs& a, void* st, void* e0, void* e1) { return attend_rows<DT, DP>(a, st, e0, e1); }
+};
+template <int DT, int DP> struct Combine {
+    static int go(const AttendArgs& a, void* st, void* e0, void* e1) { return combine_rows<DT, DP>(a, st, e0, e1); }
+};
+template <int DT, int DP> struct Weight {
+    static int go(const AttendArgs& a, void* st, void* e0, void* e1) { return weight_rows<DT, DP>(a, st, e0, e1); }
+};
 
 }  // namespace
 
 void attend_shape(AttendArgs& a)
 {
     const int64_t rows = (int64_t)a.ch.max_new * a.group;
-    const int dp = padded_dim(a.c.dim);
-    const int most = dp == 256 ? 16 : a.dtype == kBF16 ? 64 : 32;  // rows that registers hold
-    a.tile_rows = rows <= 16 || most == 16 ? 16 : rows <= 32 || most == 32 ? 32 : 64;
+    const int most = padded_dim(a.c.dim) == 256 ? 32 : 64;  // rows of a workgroup at most
+    a.tile_rows = rows <= 16 ? 16 : rows <= 32 || most == 32 ? 32 : 64;
     a.row_tiles = (int)((rows + a.tile_rows - 1) / a.tile_rows);
-    const int64_t groups = std::max<int64_t>(pairs(a) * a.row_tiles, 1), cap = capacity(a.c);
-    const int64_t fill = (1024 + groups - 1) / groups, longest = (cap + 2047) / 2048, blocks = (cap + kPartTokens - 1) / kPartTokens;
-    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::max(fill, longest), blocks));
-    if (rows > 512) a.splits = (int)std::min<int64_t>(a.splits, fill);
-    const int64_t wtiles = (cap + kTile * kWaves - 1) / (kTile * kWaves);
-    a.weight_blocks = (int)std::max<int64_t>(1, std::min<int64_t>(wtiles, std::max<int64_t>(4096 / std::max<int64_t>(pairs(a), 1), 1)));
+    const int64_t np = std::max<int64_t>(pairs(a), 1), groups = std::max<int64_t>(np * a.row_tiles, 1), cap = capacity(a.c);
+    const int64_t blocks = std::max<int64_t>((cap + kPartTokens - 1) / kPartTokens, 1);
+    const int64_t fill = (1024 + groups - 1) / groups, longest = rows > 512 ? 1 : (cap + 2047) / 2048;
+    a.splits = (int)std::min<int64_t>(std::max(fill, longest), blocks);
+    a.row_parts = 1;
+    if (rows > kRowStep) {
+        a.weight_parts = (int)std::max<int64_t>((cap + kTile * kWaves - 1) / (kTile * kWaves), 1);
+        const int64_t steps = (rows + kRowStep - 1) / kRowStep;
+        a.row_parts = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(steps, 16), 2048 / (np * a.weight_parts)));
+    } else {
+        a.weight_parts = (int)std::min<int64_t>(blocks, std::max((2048 + np - 1) / np, (cap + 2047) / 2048));
+    }
 }
 
 AttendBytes attend_bytes(const AttendArgs& a)
 {
     const size_t rows = (size_t)a.ch.n_rows * (size_t)a.heads;
-    AttendBytes b{0, 0, 0};
+    AttendBytes b{0, 0, 0, 0};
     if (a.splits > 1) {
         b.part_o = rows * (size_t)a.splits * (size_t)a.c.dim * 4;
         b.part_ml = rows * (size_t)a.splits * 8;
     }
     if (a.add_weight) b.lse2 = rows * 4;
+    if (a.add_weight && a.row_parts > 1) b.part_w = (size_t)a.row_parts * (size_t)pairs(a) * (size_t)capacity(a.c) * 4;
     return b;
 }
 
-int launch_attend(const AttendArgs& a, void* st, void* e0, void* e1)
-{
-    const int dp = padded_dim(a.c.dim);
-    if (a.dtype == kBF16)
-        return dp == 64 ? attend_rows<kBF16, 64>(a, st, e0, e1) : dp == 128 ? attend_rows<kBF16, 128>(a, st, e0, e1)
-                                                                            : attend_rows<kBF16, 256>(a, st, e0, e1);
-    return dp == 64 ? attend_rows<kF32, 64>(a, st, e0, e1) : dp == 128 ? attend_rows<kF32, 128>(a, st, e0, e1)
-                                                                       : attend_rows<kF32, 256>(a, st, e0, e1);
-}
+int launch_attend(const AttendArgs& a, void* st, void* e0, void* e1) { return by_type<Attend>(a, st, e0, e1); }
 
 int launch_combine(const AttendArgs& a, void* st, void* e0, void* e1)
 {
-    if (a.splits <= 1) return kNoLaunch;
-    const int per = (int)(((int64_t)a.ch.max_new * a.group + kWaves - 1) / kWaves);
-    return a.dtype == kBF16 ? enqueue(k_combine<kBF16>, pairs(a) * per, st, e0, e1, a, per)
-                            : enqueue(k_combine<kF32>, pairs(a) * per, st, e0, e1, a, per);
+    return a.splits <= 1 ? kNoLaunch : by_type<Combine>(a, st, e0, e1);
 }
 
 int launch_weight(const AttendArgs& a, void* st, void* e0, void* e1)
 {
-    if (!a.add_weight) return kNoLaunch;
-    const int dp = padded_dim(a.c.dim);
-    const int64_t blocks = pairs(a) * a.weight_blocks;
-    if (a.dtype == kBF16)
-        return dp == 64 ? enqueue(k_weight<kBF16, 64>, blocks, st, e0, e1, a) : dp == 128
-                   ? enqueue(k_weight<kBF16, 128>, blocks, st, e0, e1, a) : enqueue(k_weight<kBF16, 256>, blocks, st, e0, e1, a);
-    return dp == 64 ? enqueue(k_weight<kF32, 64>, blocks, st, e0, e1, a) : dp == 128
-               ? enqueue(k_weight<kF32, 128>, blocks, st, e0, e1, a) : enqueue(k_weight<kF32, 256>, blocks, st, e0, e1, a);
+    return !a.add_weight ? kNoLaunch : by_type<Weight>(a, st, e0, e1);
+}
+
+int launch_weight_join(const AttendArgs& a, void* st, void* e0, void* e1)
+{
+    if (!a.add_weight || a.row_parts <= 1) return kNoLaunch;
+    const int per = (capacity(a.c) + kBlock - 1) / kBlock;
+    return enqueue(k_weight_join, pairs(a) * per, st, e0, e1, a, per);
 }
 
 }  // namespace msao

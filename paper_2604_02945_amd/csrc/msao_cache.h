@@ -117,11 +117,13 @@ struct AttendArgs {
     float scale;                   // scale * log2(e)
     int32_t splits, row_tiles;     // most parts of a group of rows; groups of a (sequence, kv head)
     int32_t tile_rows;             // rows of a group
-    int32_t weight_blocks;         // blocks of the weight pass for each (sequence, kv head)
+    int32_t weight_parts;          // parts of the tokens in the weight pass, for each (sequence, kv head)
+    int32_t row_parts;             // and of the rows
     // workspace
     float* part_o;                 // [splits][n_rows * heads][dim], a part's sum of 2^(x - m) v
     float* part_ml;                // [splits][n_rows * heads][2], its m and sum of 2^(x - m)
     float* lse2;                   // [n_rows * heads] log2 of the sums, for the weight pass
+    float* part_w;                 // [row_parts][n_seqs * kv_heads][capacity]
 };
 
 // ---- eviction -------------------------------------------------------------------
@@ -144,17 +146,18 @@ int launch_append(const AppendArgs& a, void* stream, void* ev0, void* ev1);
 int launch_attend(const AttendArgs& a, void* stream, void* ev0, void* ev1);
 int launch_combine(const AttendArgs& a, void* stream, void* ev0, void* ev1);
 int launch_weight(const AttendArgs& a, void* stream, void* ev0, void* ev1);
+int launch_weight_join(const AttendArgs& a, void* stream, void* ev0, void* ev1);
 int launch_select(const EvictArgs& a, void* stream, void* ev0, void* ev1);
 int launch_move(const EvictArgs& a, void* stream, void* ev0, void* ev1);
 
 // Launch shapes: lanes and parts of an append; blocks and col_parts of an eviction's move.
 void append_shape(AppendArgs& a);
 void evict_shape(EvictArgs& a);
-// Launch shape of an attention call: fills splits, row_tiles, tile_rows and weight_blocks.
+// Launch shape of an attention call: fills splits, row_tiles, tile_rows, weight_parts and row_parts.
 void attend_shape(AttendArgs& a);
 // Bytes of each of its workspace arrays.
 struct AttendBytes {
-    size_t part_o, part_ml, lse2;
+    size_t part_o, part_ml, lse2, part_w;
 };
 AttendBytes attend_bytes(const AttendArgs& a);
 

@@ -175,7 +175,7 @@ ChunkDev chunk_dev(const msao_chunk& ch) { return ChunkDev{ch.start, ch.n_rows, 
 // The launch shape and the workspace of an attention call.
 struct AttendPlan {
     AttendArgs a;
-    size_t part_o, part_ml, lse2, total;
+    size_t part_o, part_ml, lse2, part_w, total;
 };
 msao_status attend_plan(const msao_kv_cache* cache, const msao_chunk* chunk, int heads, uint32_t flags, AttendPlan& pl,
                         std::string* err)
@@ -196,13 +196,15 @@ msao_status attend_plan(const msao_kv_cache* cache, const msao_chunk* chunk, int
     a.add_weight = flags & MSAO_ATTEND_WEIGHT ? 1 : 0;
     attend_shape(a);
     const int64_t groups = (int64_t)a.c.n_seqs * a.c.kv_heads;
-    const int64_t most = std::max<int64_t>((int64_t)a.row_tiles * a.splits, std::max<int64_t>((int64_t)chunk->max_new * a.group, a.weight_blocks));
+    const int64_t most = std::max<int64_t>(std::max<int64_t>((int64_t)a.row_tiles * a.splits, (int64_t)chunk->max_new * a.group),
+                                           std::max<int64_t>((int64_t)a.weight_parts * a.row_parts, a.c.per_seq * (int64_t)cache->page_size / 256 + 1));
     if (groups > 0 && most > kMaxBlocks / groups) return fail(err, MSAO_ERR_UNSUPPORTED, "more workgroups than one launch takes");
     const AttendBytes b = attend_bytes(a);
     pl.part_o = 0;
     pl.part_ml = align_up(b.part_o, kWsAlign);
     pl.lse2 = pl.part_ml + align_up(b.part_ml, kWsAlign);
-    pl.total = pl.lse2 + align_up(b.lse2, kWsAlign);
+    pl.part_w = pl.lse2 + align_up(b.lse2, kWsAlign);
+    pl.total = pl.part_w + align_up(b.part_w, kWsAlign);
     return MSAO_OK;
 }
 
@@ -220,6 +222,7 @@ int run_append(const void* a, void* s, void* e0, void* e1) { return launch_appen
 int run_attend(const void* a, void* s, void* e0, void* e1) { return launch_attend(*(const AttendArgs*)a, s, e0, e1); }
 int run_combine(const void* a, void* s, void* e0, void* e1) { return launch_combine(*(const AttendArgs*)a, s, e0, e1); }
 int run_weight(const void* a, void* s, void* e0, void* e1) { return launch_weight(*(const AttendArgs*)a, s, e0, e1); }
+int run_weight_join(const void* a, void* s, void* e0, void* e1) { return launch_weight_join(*(const AttendArgs*)a, s, e0, e1); }
 int run_select(const void* a, void* s, void* e0, void* e1) { return launch_select(*(const EvictArgs*)a, s, e0, e1); }
 int run_move(const void* a, void* s, void* e0, void* e1) { return launch_move(*(const EvictArgs*)a, s, e0, e1); }
 
@@ -326,11 +329,15 @@ msao_status msao_cache_attention(msao_ctx* ctx, const msao_kv_cache* cache, cons
             a.part_o = (float*)(ws + pl.part_o);
             a.part_ml = (float*)(ws + pl.part_ml);
         }
-        if (a.add_weight) a.lse2 = (float*)(ws + pl.lse2);
+        if (a.add_weight) {
+            a.lse2 = (float*)(ws + pl.lse2);
+            a.part_w = (float*)(ws + pl.part_w);
+        }
         DeviceGuard guard(ctx->device);
         MSAO_TRY(cache_launch(ctx, MSAO_CACHE_KERNEL_ATTEND, stream, run_attend, &a));
         MSAO_TRY(cache_launch(ctx, MSAO_CACHE_KERNEL_COMBINE, stream, run_combine, &a));
-        return cache_launch(ctx, MSAO_CACHE_KERNEL_WEIGHT, stream, run_weight, &a);
+        MSAO_TRY(cache_launch(ctx, MSAO_CACHE_KERNEL_WEIGHT, stream, run_weight, &a));
+        return cache_launch(ctx, MSAO_CACHE_KERNEL_WEIGHT_JOIN, stream, run_weight_join, &a);
     });
 }
 
