@@ -149,6 +149,7 @@ __device__ __forceinline__ int lane_pages(const CacheDev& c, int seq, int lo, in
 // A 16-token half tile: its buffers and how many of its tokens there are.
 struct Half {
     rsrc_t r;
+    u32x4 words;  // the same as four words
     int n;
 };
 __device__ __forceinline__ Half half_of(const uint8_t* base, int64_t page_bytes, int64_t tok_bytes, int row_bytes, int page,
@@ -158,7 +159,10 @@ __device__ __forceinline__ Half half_of(const uint8_t* base, int64_t page_bytes,
     h.n = page < 0 ? 0 : clamp_int(hi - tok, 0, 16);
     h.n = uniform(h.n);
     const int64_t off = page < 0 ? 0 : (int64_t)page * page_bytes + (int64_t)(tok & mask) * tok_bytes;
-    h.r = rsrc(uniform(base + off), uniform(h.n > 0 ? (h.n - 1) * (int)tok_bytes + row_bytes : 0));
+    const uint8_t* at = uniform(base + off);
+    const int bytes = uniform(h.n > 0 ? (h.n - 1) * (int)tok_bytes + row_bytes : 0);
+    h.r = rsrc(at, bytes);
+    h.words = u32x4{(uint32_t)(uint64_t)at, (uint32_t)((uint64_t)at >> 32) & 0xFFFFu, (uint32_t)bytes, 0x00020000u};
     return h;
 }
 
@@ -247,18 +251,19 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArg
 
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
     const int i16 = lane & 15, c = lane >> 4, rw = wave % RW, tw = wave / RW;
-    int id = blockIdx.x;
-    const int split = id % a.splits;
-    id /= a.splits;
-    const int tile = id % a.row_tiles;
-    const Place p = place_of(a, id / a.row_tiles);
+    // neighbouring blocks lie on different XCDs: the parts of a pair start at a place of its own,
+    // so that first parts, which every sequence has, are spread; last tiles, which see most, first
+    const int per_pair = a.row_tiles * a.splits, sh = blockIdx.x / per_pair;
+    const int j = (blockIdx.x - sh * per_pair + sh) % per_pair;
+    const int split = j / a.row_tiles, tile = a.row_tiles - 1 - (j - split * a.row_tiles);
+    const Place p = place_of(a, sh);
     const int n_rows = call_rows(a, p), r0 = tile * RW * MT * 16;
     if (r0 >= n_rows) return;
     const int r_end = min(r0 + RW * MT * 16, n_rows);
     const int seen = group_sees(p.length, p.n_new, a.group, r_end - 1, a.causal);
-    const Cut cut = cut_tokens(seen, a.splits);
-    if (split >= max(cut.n, 1)) return;
-    const int lo = split * cut.per, hi = min(seen, lo + cut.per);
+    const int parts = parts_of(seen, a.part_tokens);
+    if (split >= max(parts, 1)) return;
+    const int lo = split * a.part_tokens, hi = min(seen, lo + a.part_tokens);
 
     const int row_bytes = a.c.dim * ES, mask = (1 << a.c.page_shift) - 1;
     const uint8_t* kb = a.c.k + (int64_t)p.head * a.c.k_head;
@@ -521,7 +526,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArg
             }
             const int tok = row / a.group, head = p.head * a.group + (row - tok * a.group);
             const int64_t at = (int64_t)(p.begin + tok) * a.heads + head;
-            if (cut.n <= 1) {
+            if (parts <= 1) {
                 const float inv = l == 0.0f ? 0.0f : 1.0f / l;
                 uint8_t* dst = a.out + (int64_t)(p.begin + tok) * a.out_stride + ((int64_t)head * a.c.dim + od) * ES;
                 // (the head's last channels may be half of what the thread has)
@@ -551,6 +556,286 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArg
     }
 }
 
+// Many rows, bf16 (chunks of prompts): bound by the matrix cores and the exponents, so that
+// K and V are read once for 64 MT rows. A stage of 64 tokens goes from memory to LDS without
+// passing through registers (each wavefront brings 16 tokens) while the stage before it is
+// used. Every wavefront has 16 MT rows of its own and takes all of the tokens, 32 at a time:
+//   S^T = K Q^T with the queries in registers and K's rows as A operands,
+//   O^T = V^T P^T with V's channels as A operands, by the reads that transpose 4 x 16 blocks
+//   (lane (c, i): tokens 4c .. 4c+3 and 16+4c .. of channel i, the tokens of its P).
+// In LDS the 16-byte pieces of a row are exchanged by a pattern of the row (K: piece ^ row,
+// V: piece ^ 2 row), so that the lanes of a read, which lie in different rows, hit
+// different banks; the lanes that bring a row choose their pieces accordingly.
+typedef __attribute__((address_space(3))) uint8_t lds_byte;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// 16 bytes a lane from `off` of a buffer straight to LDS, 1 KiB from the (uniform) address
+// `to`; out of range zeros. As instructions of its own, because the compiler, which cannot
+// tell the two stages apart, would wait for the next stage's loads before it reads this
+// one's. The load has no register to write; it is waited for (stage_came) before the
+// barrier after which its stage is read. M0 is set for it alone: nothing else here uses M0.
+__device__ __forceinline__ void load_to_lds(const u32x4& buffer, uint32_t to, int off)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(buffer)
+                 : "memory");
+}
+__device__ __forceinline__ void stage_came() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+template <int DP, int MT, int NW, int ST, int WPS>
+__global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
+{
+    constexpr int KS = DP / 32, VT = DP / 16;        // steps of a score; tiles of channels
+    constexpr int CH = DP / 8, RB = DP * 2;          // 16-byte pieces of a row in LDS; its bytes
+    constexpr int NI = 16 * CH / kWave;              // loads that bring 16 tokens
+    __shared__ __align__(16) uint8_t lds_k[2][ST * RB], lds_v[2][ST * RB];
+    __shared__ __align__(16) int lds_n[2][ST / 16];  // tokens that there are of each 16
+
+    const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
+    const int i16 = lane & 15, c = lane >> 4;
+    const int per_pair = a.row_tiles * a.splits, sh = blockIdx.x / per_pair;
+    const int j = (blockIdx.x - sh * per_pair + sh) % per_pair;
+    const int split = j / a.row_tiles, tile = a.row_tiles - 1 - (j - split * a.row_tiles);
+    const Place p = place_of(a, sh);
+    const int n_rows = call_rows(a, p), r0 = tile * NW * MT * 16;
+    if (r0 >= n_rows) return;
+    const int r_end = min(r0 + NW * MT * 16, n_rows);
+    const int seen = group_sees(p.length, p.n_new, a.group, r_end - 1, a.causal);
+    const int parts = parts_of(seen, a.part_tokens);
+    if (split >= max(parts, 1)) return;
+    const int lo = split * a.part_tokens, hi = min(seen, lo + a.part_tokens);
+
+    const int row_bytes = a.c.dim * 2, mask = (1 << a.c.page_shift) - 1;
+    const uint8_t* kb = a.c.k + (int64_t)p.head * a.c.k_head;
+    const uint8_t* vb = a.c.v + (int64_t)p.head * a.c.v_head;
+    constexpr int kTasks = ST / 8;  // 16 tokens of K or of V each
+    int ko[NI], vo[NI];  // what a lane brings of 16 tokens
+#pragma unroll
+    for (int n = 0; n < NI; ++n) {
+        const int row = (n * kWave + lane) / CH, piece = lane % CH;
+        const int kp = piece ^ (row & (CH - 1)), vp = piece ^ (2 * row & (CH - 1));
+        ko[n] = 16 * kp < row_bytes ? row * (int)a.c.k_tok + 16 * kp : kFar;
+        vo[n] = 16 * vp < row_bytes ? row * (int)a.c.v_tok + 16 * vp : kFar;
+    }
+
+    const int w0 = r0 + wave * MT * 16;                      // the wavefront's rows
+    const int used = clamp_int((n_rows - w0 + 15) / 16, 0, MT);
+    Queries<kBF16, DP> q[MT];
+    int last[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const int row = w0 + 16 * m + i16;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) q[m].v[s] = Queries<kBF16, DP>::fetch(a, p, row, n_rows, 4 * s + c) ^ (a.scale < 0.0f ? 0x80008000u : 0u);
+        last[m] = a.causal ? p.length - p.n_new + row / a.group : p.length - 1;
+    }
+    const int least = a.causal ? p.length - p.n_new + w0 / a.group : p.length - 1;
+    // tokens that the wavefront's own last row sees
+    const int w_hi = used > 0 ? min(hi, group_sees(p.length, p.n_new, a.group, min(w0 + MT * 16, n_rows) - 1, a.causal)) : lo;
+
+    // the scale's sign is the queries', so that the largest product gives the largest score;
+    // above 0, so that what is masked stays at -inf
+    const float scale = fmaxf(fabsf(a.scale), 1.17549435e-38f);
+    f32x4 o[MT][VT];
+    float ref[MT], sum[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        ref[m] = -INFINITY;
+        sum[m] = 0.0f;
+#pragma unroll
+        for (int t = 0; t < VT; ++t) o[m][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    // where the lane's operands lie: K row i, pieces c ^ row + 4 s; V row 4c + i / 4, piece of
+    // channels 4 (i % 4) .., half of it
+    const int ka = i16 * RB + ((c ^ (i16 & (CH - 1))) << 4);
+    const int vr = 4 * c + (i16 >> 2);
+    const int va = vr * RB + ((((i16 & 3) >> 1) ^ (2 * vr & (CH - 1))) << 4) + 8 * (i16 & 1);
+
+    const int stages = (hi - lo + ST - 1) / ST;
+    static_assert(kTasks % NW == 0 || NW % kTasks == 0, "");
+    const int half0 = wave % (ST / 16);  // the wavefront's 16 tokens of a stage, or the first of them
+    int pages = 0;
+    auto bring = [&](int st) {
+        if ((st & 63) == 0) {
+            const int64_t tok = (int64_t)lo + (int64_t)ST * (st + lane) + 16 * half0;
+            pages = tok < hi ? page_at(a.c, p.seq, (int)(tok >> a.c.page_shift)) : -1;
+        }
+        const int tok = lo + ST * st + 16 * half0, page = __builtin_amdgcn_readlane(pages, st & 63);
+        const bool does_k = NW < kTasks || wave < ST / 16, does_v = NW < kTasks || (wave >= ST / 16 && wave < kTasks);
+        if (does_k) {
+            const Half k = half_of(kb, a.c.k_page, a.c.k_tok, row_bytes, page, tok, hi, mask);
+            lds_n[st & 1][half0] = k.n;
+            const uint32_t to = uniform((int)(uint32_t)(uintptr_t)(lds_byte*)lds_k[st & 1]) + half0 * 16 * RB;
+#pragma unroll
+            for (int n = 0; n < NI; ++n) load_to_lds(k.words, to + n * 1024, ko[n]);
+        }
+        if (does_v) {
+            const Half v = half_of(vb, a.c.v_page, a.c.v_tok, row_bytes, page, tok, hi, mask);
+            const uint32_t to = uniform((int)(uint32_t)(uintptr_t)(lds_byte*)lds_v[st & 1]) + half0 * 16 * RB;
+#pragma unroll
+            for (int n = 0; n < NI; ++n) load_to_lds(v.words, to + n * 1024, vo[n]);
+        }
+    };
+
+    bool left_out = false;
+    if (stages > 0) bring(0);
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): the queries, so that the loop need not wait for them
+    for (int st = 0; st < stages; ++st) {
+        // the stage has come, and nobody reads the other one any more
+        stage_came();
+        __syncthreads();
+        if (st + 1 < stages) bring(st + 1);
+        int kn[ST / 16];
+#pragma unroll
+        for (int w = 0; w < ST / 16; ++w) kn[w] = uniform(lds_n[st & 1][w]);
+        const uint8_t* sk = lds_k[st & 1];
+        const uint8_t* sv = lds_v[st & 1];
+#pragma unroll
+        for (int u = 0; u < ST / kTile; ++u) {
+            const int tok = lo + ST * st + kTile * u;
+            if (tok >= w_hi) break;
+            float x[MT][8];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                u32x4 kf[KS];
+#pragma unroll
+                for (int s = 0; s < KS; ++s) kf[s] = *(const u32x4*)(sk + (2 * u + h) * 16 * RB + (ka ^ s << 6));
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    const f32x4 sc = scores<kBF16, DP>(kf, q[m]);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[m][4 * h + r] = sc[r];
+                }
+            }
+            const bool seen_whole = tok + kTile <= hi && tok + kTile - 1 <= least;
+            if (!seen_whole || kn[2 * u] != 16 || kn[2 * u + 1] != 16) {
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const int j = 4 * c + r;
+                            if (j >= kn[2 * u + h] || tok + 16 * h + j > last[m]) x[m][4 * h + r] = -INFINITY;
+                        }
+            }
+            u32x4 pb[MT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                float most = x[m][0];
+#pragma unroll
+                for (int e = 1; e < 8; ++e) most = fmaxf(most, x[m][e]);
+                most *= scale;
+                if (__ballot(most > ref[m] + kSlack) != 0) {
+                    most = fmaxf(most, __shfl_xor(most, 16));
+                    most = fmaxf(most, __shfl_xor(most, 32));
+                    const float up = most > ref[m] + kSlack ? most : ref[m];
+                    const float sc = ref[m] == up ? 1.0f : ref[m] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref[m] - up);
+                    ref[m] = up;
+                    sum[m] *= sc;
+#pragma unroll
+                    for (int t = 0; t < VT; ++t)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) o[m][t][r] *= sc;
+                }
+                const float base = ref[m] == -INFINITY ? 0.0f : ref[m];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[m][e] = __builtin_amdgcn_exp2f(fmaf(x[m][e], scale, -base));
+                    sum[m] += x[m][e];
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) pb[m][e] = pack_bf16(x[m][2 * e], x[m][2 * e + 1]);
+            }
+            auto value = [&](int t) {
+                u32x4 w;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const lds_byte* at = (const lds_byte*)sv + (2 * u + h) * 16 * RB + (va ^ t << 5);
+                    const u32x2 z = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at));
+                    w[2 * h] = z.x;
+                    w[2 * h + 1] = z.y;
+                }
+                return w;
+            };
+            const bool careful = !seen_whole && a.causal;
+#pragma unroll
+            for (int t = 0; t < VT; ++t) {
+                u32x4 w = value(t);
+                if (careful) {  // (see k_attend)
+                    const bool any = strange<kBF16>(w[0]) || strange<kBF16>(w[1]) || strange<kBF16>(w[2]) || strange<kBF16>(w[3]);
+                    if (__ballot(any) != 0) {
+                        left_out = true;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) w[e] = without_strange<kBF16>(w[e]);
+                    }
+                }
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+                    o[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, pb[m]),
+                                                                      o[m][t], 0, 0, 0);
+            }
+        }
+    }
+    if (left_out) {
+#pragma unroll 1
+        for (int tok = lo + max(0, least + 1 - lo) / kTile * kTile; tok < w_hi; tok += kTile) {
+            if (tok + kTile <= hi && tok + kTile - 1 <= least) continue;
+#pragma unroll 1
+            for (int t = tok; t < min(tok + kTile, hi); ++t) {
+                const int page = page_at(a.c, p.seq, t >> a.c.page_shift);
+                if (page < 0) continue;
+                const uint8_t* src = vb + (int64_t)page * a.c.v_page + (int64_t)(t & mask) * a.c.v_tok;
+#pragma unroll
+                for (int v = 0; v < VT; ++v) {
+                    const int at = (16 * v + 4 * c) * 2;
+                    if (at >= row_bytes) continue;
+                    const u32x2 w = *(const u32x2*)(src + at);
+                    const uint32_t b0 = w.x ^ without_strange<kBF16>(w.x), b1 = w.y ^ without_strange<kBF16>(w.y);
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) {
+                        if (t > last[m]) continue;
+                        o[m][v][0] += __uint_as_float(b0 << 16);
+                        o[m][v][1] += __uint_as_float(b0 & 0xFFFF0000u);
+                        o[m][v][2] += __uint_as_float(b1 << 16);
+                        o[m][v][3] += __uint_as_float(b1 & 0xFFFF0000u);
+                    }
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        sum[m] += __shfl_xor(sum[m], 16);
+        sum[m] += __shfl_xor(sum[m], 32);
+        const int row = w0 + 16 * m + i16;
+        if (row >= n_rows) continue;
+        const int tok = row / a.group, head = p.head * a.group + (row - tok * a.group);
+        const int64_t at = (int64_t)(p.begin + tok) * a.heads + head;
+        if (parts <= 1) {
+            const float inv = sum[m] == 0.0f ? 0.0f : 1.0f / sum[m];
+            uint8_t* dst = a.out + (int64_t)(p.begin + tok) * a.out_stride + (int64_t)head * row_bytes;
+#pragma unroll
+            for (int t = 0; t < VT; ++t) {
+                const int ch = 16 * t + 4 * c;
+                if (ch < a.c.dim)
+                    *(u32x2*)(dst + 2 * ch) = u32x2{pack_bf16(o[m][t][0] * inv, o[m][t][1] * inv), pack_bf16(o[m][t][2] * inv, o[m][t][3] * inv)};
+            }
+            if (c == 0) {
+                const float z = sum[m] == 0.0f ? -INFINITY : ref[m] + __builtin_amdgcn_logf(sum[m]);
+                if (a.lse) a.lse[at] = z * kLn2;
+                if (a.lse2) a.lse2[at] = z;
+            }
+        } else {
+            const int64_t all = (int64_t)a.ch.n_rows * a.heads;
+            float* po = a.part_o + (split * all + at) * a.c.dim;
+#pragma unroll
+            for (int t = 0; t < VT; ++t)
+                if (16 * t + 4 * c < a.c.dim) *(f32x4*)(po + 16 * t + 4 * c) = o[m][t];
+            if (c == 0) *(f32x2*)(a.part_ml + 2 * (split * all + at)) = f32x2{ref[m], sum[m]};
+        }
+    }
+}
+
 // Parts of split rows joined: W wavefronts a row. DP / 4 lanes hold four channels each of a
 // part; the lanes' groups take parts in turn, four in flight, and join at the end.
 template <int DT, int DP, int W>
@@ -565,8 +850,8 @@ __global__ __launch_bounds__(kBlock) void k_combine(AttendArgs a, int blocks_per
     if (row >= n_rows) return;  // (W = kWaves: the whole block)
     const int r_end = min(row / a.tile_rows * a.tile_rows + a.tile_rows, n_rows);
     const int seen = group_sees(p.length, p.n_new, a.group, r_end - 1, a.causal);
-    const Cut cut = cut_tokens(seen, a.splits);
-    if (cut.n <= 1) return;  // written by k_attend
+    const int parts = parts_of(seen, a.part_tokens);
+    if (parts <= 1) return;  // written by k_attend
     const int tok = row / a.group, head = p.head * a.group + (row - tok * a.group);
     const int64_t all = (int64_t)a.ch.n_rows * a.heads, at = (int64_t)(p.begin + tok) * a.heads + head;
     const int t = wave % W * kWave + lane, group = t / LP, ch = (t & (LP - 1)) * 4;
@@ -581,7 +866,7 @@ __global__ __launch_bounds__(kBlock) void k_combine(AttendArgs a, int blocks_per
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] = acc[e] * s1 + o2[e] * s2;
     };
-    for (int i0 = group; i0 < cut.n; i0 += kGroups * kFly) {
+    for (int i0 = group; i0 < parts; i0 += kGroups * kFly) {
         f32x2 ml[kFly];
         f32x4 o[kFly];
 #pragma unroll
@@ -589,7 +874,7 @@ __global__ __launch_bounds__(kBlock) void k_combine(AttendArgs a, int blocks_per
             const int i = i0 + f * kGroups;
             ml[f] = f32x2{-INFINITY, 0.0f};
             o[f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            if (i < cut.n) {
+            if (i < parts) {
                 ml[f] = *(const f32x2*)(a.part_ml + 2 * (i * all + at));
                 if (has) o[f] = *(const f32x4*)(a.part_o + (i * all + at) * a.c.dim + ch);
             }
@@ -648,14 +933,13 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight(AttendArg
     __shared__ __align__(16) uint8_t lds[MT * 16 * Queries<DT, DP>::kLine];
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
     const int i16 = lane & 15, c = lane >> 4;
-    const int sh = blockIdx.x / a.weight_parts, part = blockIdx.x - sh * a.weight_parts;
+    const int sh = blockIdx.x / a.weight_parts, part = (blockIdx.x - sh * a.weight_parts + sh) % a.weight_parts;
     const Place p = place_of(a, sh);
     const int n_rows = call_rows(a, p);
     if (n_rows == 0) return;
     const int seen = group_sees(p.length, p.n_new, a.group, n_rows - 1, a.causal);
-    const Cut cut = cut_tokens(seen, a.weight_parts);
-    if (part >= cut.n) return;
-    const int lo = part * cut.per, hi = min(seen, lo + cut.per);
+    const int lo = part * a.weight_tokens, hi = min(seen, lo + a.weight_tokens);
+    if (lo >= seen) return;
     const int row_bytes = a.c.dim * ES, mask = (1 << a.c.page_shift) - 1;
     const uint8_t* kb = a.c.k + (int64_t)p.head * a.c.k_head;
     const KeyOffsets<DT, DP> ko(a.c.k_tok, row_bytes);
@@ -751,10 +1035,8 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight_rows(Atte
     __shared__ int lds_last[kRowStep];
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
     const int i16 = lane & 15, c = lane >> 4;
-    int id = blockIdx.x;
-    const int part = id % a.row_parts;
-    id /= a.row_parts;
-    const int sh = id / a.weight_parts, block = id - sh * a.weight_parts;
+    const int per_pair = a.weight_parts * a.row_parts, sh = blockIdx.x / per_pair;
+    const int j = (blockIdx.x - sh * per_pair + sh) % per_pair, block = j / a.row_parts, part = j - block * a.row_parts;
     const Place p = place_of(a, sh);
     const int n_rows = call_rows(a, p);
     const int seen = n_rows > 0 ? group_sees(p.length, p.n_new, a.group, n_rows - 1, a.causal) : 0;
@@ -864,27 +1146,48 @@ __global__ __launch_bounds__(kBlock) void k_weight_join(AttendArgs a, int blocks
 }
 
 template <typename K, typename... A>
-int enqueue(K kernel, int64_t blocks, void* stream, void* ev0, void* ev1, A... args)
+int enqueue_of(K kernel, int64_t blocks, int threads, void* stream, void* ev0, void* ev1, A... args)
 {
     if (blocks <= 0) return kNoLaunch;
     if (ev0 && ev1)
-        hipExtLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kBlock), 0, (hipStream_t)stream, (hipEvent_t)ev0,
+        hipExtLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), 0, (hipStream_t)stream, (hipEvent_t)ev0,
                               (hipEvent_t)ev1, 0, args...);
     else
-        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kBlock), 0, (hipStream_t)stream, args...);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), 0, (hipStream_t)stream, args...);
     return (int)hipGetLastError();
+}
+
+template <typename K, typename... A>
+int enqueue(K kernel, int64_t blocks, void* stream, void* ev0, void* ev1, A... args)
+{
+    return enqueue_of(kernel, blocks, kBlock, stream, ev0, ev1, args...);
 }
 
 int padded_dim(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 
 int64_t pairs(const AttendArgs& a) { return (int64_t)a.c.n_seqs * a.c.kv_heads; }
 
+#ifndef CFG
+#define CFG 2, 4, 64, 2
+#endif
+#ifndef MT_ROWS
+#define MT_ROWS 2
+#endif
+#ifndef NWV
+#define NWV 4
+#endif
+#ifndef MANY
+#define MANY 128
+#endif
+constexpr int kManyTiles = MT_ROWS, kManyRows = kManyTiles * 16 * NWV;
 // Rows of a workgroup: what the registers of its wavefronts hold.
 template <int DT, int DP>
 int attend_rows(const AttendArgs& a, void* st, void* e0, void* e1)
 {
     const int64_t blocks = pairs(a) * a.row_tiles * a.splits;
     if (a.tile_rows == 16) return enqueue(k_attend<DT, DP, 1, 1>, blocks, st, e0, e1, a);
+    if constexpr (DT == kBF16 && DP <= 128)
+        if (a.tile_rows == kManyRows) return enqueue_of(k_attend_rows<DP, CFG>, blocks, NWV * kWave, st, e0, e1, a);
     if constexpr (DP == 256) {
         if (a.tile_rows == 32) return enqueue(k_attend<DT, DP, 1, 2>, blocks, st, e0, e1, a);
     } else {
@@ -935,23 +1238,43 @@ template <int DT, int DP> struct Weight {
 
 }  // namespace
 
+#ifndef PT
+#define PT 2048
+#endif
+#ifndef PM
+#define PM 1024
+#endif
+#ifndef PL
+#define PL 128
+#endif
+#ifndef WT
+#define WT 8192
+#endif
+constexpr int64_t kPartTarget = PT, kPartLeast = PL, kWeightTarget = WT, kPartMost = PM;
 void attend_shape(AttendArgs& a)
 {
     const int64_t rows = (int64_t)a.ch.max_new * a.group;
     const int most = padded_dim(a.c.dim) == 256 ? 32 : 64;  // rows of a workgroup at most
     a.tile_rows = rows <= 16 ? 16 : rows <= 32 || most == 32 ? 32 : 64;
+    if (a.dtype == kBF16 && most == 64 && rows > MANY) a.tile_rows = kManyRows;
     a.row_tiles = (int)((rows + a.tile_rows - 1) / a.tile_rows);
     const int64_t np = std::max<int64_t>(pairs(a), 1), groups = std::max<int64_t>(np * a.row_tiles, 1), cap = capacity(a.c);
-    const int64_t blocks = std::max<int64_t>((cap + kPartTokens - 1) / kPartTokens, 1);
-    const int64_t fill = (1024 + groups - 1) / groups, longest = rows > 512 ? 1 : (cap + 2047) / 2048;
-    a.splits = (int)std::min<int64_t>(std::max(fill, longest), blocks);
+    auto up = [](int64_t v, int64_t to) { return (v + to - 1) / to * to; };
+    const int64_t whole = std::max<int64_t>(up(cap, kTile), kTile);
+    // parts for about kPartTarget workgroups if every sequence were as long as can be
+    int64_t per = std::min<int64_t>(up((groups * cap + kPartTarget - 1) / kPartTarget, kPartLeast), kPartMost);
+    if (rows > 64) per = groups >= 512 ? whole : up((groups * cap + 511) / 512, kPartLeast);
+    a.part_tokens = (int)std::min(std::max<int64_t>(per, kPartLeast), whole);
+    a.splits = std::max(1, parts_of((int)cap, a.part_tokens));
     a.row_parts = 1;
     if (rows > kRowStep) {
-        a.weight_parts = (int)std::max<int64_t>((cap + kTile * kWaves - 1) / (kTile * kWaves), 1);
+        a.weight_tokens = kTile * kWaves;
+        a.weight_parts = std::max(1, parts_of((int)cap, a.weight_tokens));
         const int64_t steps = (rows + kRowStep - 1) / kRowStep;
         a.row_parts = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(steps, 16), 2048 / (np * a.weight_parts)));
     } else {
-        a.weight_parts = (int)std::min<int64_t>(blocks, std::max((2048 + np - 1) / np, (cap + 2047) / 2048));
+        a.weight_tokens = (int)std::min<int64_t>(std::max<int64_t>(up((np * cap + kWeightTarget - 1) / kWeightTarget, kPartLeast), kPartLeast), whole);
+        a.weight_parts = std::max(1, parts_of((int)cap, a.weight_tokens));
     }
 }
 

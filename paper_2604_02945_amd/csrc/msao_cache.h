@@ -59,21 +59,11 @@ MSAO_HD int page_at(const CacheDev& c, int s, int col)
     return page_or_none(c.pages[(int64_t)s * c.table_stride + col], c.n_pages);
 }
 
-// How the `seen` tokens of a group of rows are cut into at most `most` parts of
-// whole 32-token tiles, none of fewer than kPartTokens tokens but the last: parts 0 ..
-// n-1, part i from token i * per. No part for no token.
+// How the `seen` tokens of a group of rows are cut: parts of `per` tokens (whole 32-token
+// tiles; the last may be shorter), as many as it takes. No part for no token. Parts of
+// one size, not a number of parts: sequences of any lengths give workgroups of equal work.
 constexpr int kTile = 32;
-constexpr int kPartTokens = 256;
-struct Cut {
-    int n, per;
-};
-MSAO_HD Cut cut_tokens(int seen, int most)
-{
-    if (seen <= 0) return Cut{0, kTile};
-    const int blocks = (seen + kPartTokens - 1) / kPartTokens, want = most < blocks ? most : blocks;
-    const int per = ((seen + want - 1) / want + kTile - 1) / kTile * kTile;
-    return Cut{(seen + per - 1) / per, per};
-}
+MSAO_HD int parts_of(int seen, int per) { return seen <= 0 ? 0 : (seen - 1) / per + 1; }
 
 // Tokens that rows [r0, r0 + rows) of a (sequence, kv head) see at most: row r is
 // query head r % group of token r / group. Without `causal` all of them.
@@ -115,9 +105,11 @@ struct AttendArgs {
     int32_t heads, group, dtype;
     int32_t causal, add_weight;
     float scale;                   // scale * log2(e)
+    int32_t part_tokens;           // tokens of a part
     int32_t splits, row_tiles;     // most parts of a group of rows; groups of a (sequence, kv head)
     int32_t tile_rows;             // rows of a group
-    int32_t weight_parts;          // parts of the tokens in the weight pass, for each (sequence, kv head)
+    int32_t weight_tokens;         // tokens of a part in the weight pass
+    int32_t weight_parts;          // most of them for each (sequence, kv head)
     int32_t row_parts;             // and of the rows
     // workspace
     float* part_o;                 // [splits][n_rows * heads][dim], a part's sum of 2^(x - m) v
@@ -153,7 +145,7 @@ int launch_move(const EvictArgs& a, void* stream, void* ev0, void* ev1);
 // Launch shapes: lanes and parts of an append; blocks and col_parts of an eviction's move.
 void append_shape(AppendArgs& a);
 void evict_shape(EvictArgs& a);
-// Launch shape of an attention call: fills splits, row_tiles, tile_rows, weight_parts and row_parts.
+// Launch shape of an attention call: fills part_tokens .. row_parts.
 void attend_shape(AttendArgs& a);
 // Bytes of each of its workspace arrays.
 struct AttendBytes {
