@@ -67,19 +67,20 @@ template <int DT> struct Type;
 template <> struct Type<kBF16> { static constexpr int kSize = 2; };
 template <> struct Type<kF32> { static constexpr int kSize = 4; };
 
-// 32-bit words that hold E values, loaded in pieces of 16 or 8 bytes.
-template <int W>
+// 32-bit words that hold E values, loaded in pieces of 16 or 8 bytes; AUX: cache policy.
+constexpr int kOnce = 2;  // nontemporal: read once
+template <int W, int AUX>
 __device__ __forceinline__ void load_words(uint32_t (&w)[W], rsrc_t r, int off)
 {
     static_assert(W == 2 || W % 4 == 0, "");
     if constexpr (W == 2) {
-        const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
+        const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, AUX);
         w[0] = v.x;
         w[1] = v.y;
     } else {
 #pragma unroll
         for (int i = 0; i < W / 4; ++i) {
-            const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(r, off + 16 * i, 0, 0);
+            const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(r, off + 16 * i, 0, AUX);
 #pragma unroll
             for (int e = 0; e < 4; ++e) w[4 * i + e] = v[e];
         }
@@ -244,6 +245,9 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArg
     constexpr int NH = DT == kF32 && DP >= 128 ? 1 : 2, TT = 16 * NH;
     constexpr int LDP = DP + 4;        // floats between rows in LDS: spreads the banks
     constexpr int TW = kWaves / RW;    // wavefronts that take different tiles
+    // values that no other wavefront reads need no cache (long rows of one token: 176 -> 165 us);
+    // keys stay for the weight pass (read once too, its call takes 295 us instead of 267)
+    constexpr int kValuesOnce = RW == 1 ? kOnce : 0;
     constexpr int kQBytes = RW * MT * 16 * Queries<DT, DP>::kLine, kOBytes = kWaves * 16 * LDP * 4;
     __shared__ __align__(16) uint8_t lds[kQBytes > kOBytes ? kQBytes : kOBytes];
     __shared__ float lds_m[kWaves][MT * 16], lds_l[kWaves][MT * 16];
@@ -318,7 +322,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArg
             const int page = __builtin_amdgcn_readlane(pages, (NH * it + h) & 63);
             const Half f = half_of(vb, a.c.v_page, a.c.v_tok, row_bytes, page, tok + 16 * h, hi, mask);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) load_words<VW>(vf[h][r], f.r, vo[r]);
+            for (int r = 0; r < 4; ++r) load_words<VW, kValuesOnce>(vf[h][r], f.r, vo[r]);
         }
     };
     if (mine > 0) {
@@ -969,7 +973,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight(AttendArg
             const Half f = half_of(kb, a.c.k_page, a.c.k_tok, row_bytes, page, tok + 16 * h, hi, mask);
             next_n[h] = f.n;
 #pragma unroll
-            for (int s = 0; s < KS; ++s) kf[h][s] = __builtin_amdgcn_raw_buffer_load_b128(f.r, ko.off[s], 0, 0);
+            for (int s = 0; s < KS; ++s) kf[h][s] = __builtin_amdgcn_raw_buffer_load_b128(f.r, ko.off[s], 0, kOnce);
         }
     };
     if (mine > 0) load_k(0);
