@@ -740,28 +740,33 @@ def msao_stream_read(data: torch.Tensor, chunk_kib: int = 8, ctx: Optional[Conte
 
 # ---- Sec. 4.2: the paged cache that drafts are verified over -------------------
 
-def _same_device(device: torch.device, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError(f"{name} is on {t.device}, the cache on {device}")
+# (These run before every launch of a serving step, so they ask each tensor once.)
+
+def _same_device(index: int, what: str, *tensors):
+    """All on the cache's device (None is no tensor; -1 is host memory)."""
+    for t in tensors:
+        if t is not None and t.get_device() != index:
+            raise ValueError(f"{what} must be on the cache's device")
 
 
 def _int32(name: str, t: torch.Tensor, dim: int):
-    if t.dtype != torch.int32 or t.dim() != dim:
+    if t.dtype is not torch.int32 or t.dim() != dim:
         raise ValueError(f"{name} must be a {dim}-D int32 tensor")
-    if t.numel() and t.stride(-1) != 1:
+    if t.stride(-1) != 1 and t.numel():
         raise ValueError(f"{name} must be contiguous in its last dimension")
 
 
 def _head_rows(name: str, t: torch.Tensor, dtype: torch.dtype, heads: Optional[int], dim: int) -> int:
     """Elements between the rows of a [rows, heads, dim] tensor whose heads follow one another."""
-    if t.dim() != 3 or t.shape[2] != dim or (heads is not None and t.shape[1] != heads):
+    shape = t.shape
+    if len(shape) != 3 or shape[2] != dim or (heads is not None and shape[1] != heads):
         raise ValueError(f"{name} must be [rows, {'heads' if heads is None else heads}, {dim}]")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{name} must be of the cache's dtype")
-    if t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != dim)):
+    row, head, value = t.stride()
+    if (value != 1 or (head != dim and shape[1] > 1)) and t.numel():
         raise ValueError(f"the heads of {name} must follow one another")
-    return int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1]) * dim
+    return row if shape[0] > 1 else shape[1] * dim
 
 
 class KvCache:
@@ -782,7 +787,8 @@ class KvCache:
             raise ValueError("the head_dim values of a token must be contiguous")
         _int32("pages", pages, 2)
         _int32("length", length, 1)
-        _same_device(k.device, v=v, pages=pages, length=length, weight=weight)
+        self.index = k.get_device()
+        _same_device(self.index, "v, pages, length and weight", v, pages, length, weight)
         n_seqs = int(length.shape[0])
         if pages.shape[0] != n_seqs:
             raise ValueError("pages and length differ in n_seqs")
@@ -811,24 +817,34 @@ class KvCache:
 
 
 def _cache_ctx(cache: KvCache, ctx: Optional[Context], stream) -> Context:
-    if cache.device.type != "cuda":
+    if cache.index < 0:
         raise ValueError(f"the cache is on {cache.device}, not on a GPU")
-    index = cache.device.index
     if ctx is None:
-        ctx = default_context(index)
-    elif ctx.device != index:
+        ctx = default_context(cache.index)
+    elif ctx.device != cache.index:
         raise ValueError(f"the context is of device {ctx.device}, the cache on {cache.device}")
     if stream is not None and stream.device != cache.device:
         raise ValueError(f"the stream is of {stream.device}, the cache on {cache.device}")
     return ctx
 
 
+def _stream_of(cache: KvCache, stream) -> int:
+    """The handle of `stream`, or of the current stream of the cache's device."""
+    return torch._C._cuda_getCurrentRawStream(cache.index) if stream is None else stream.cuda_stream
+
+
 def _chunk(cache: KvCache, start: torch.Tensor, n_rows: int, max_new: int) -> MsaoChunk:
     _int32("start", start, 1)
     if start.shape[0] != cache.n_seqs + 1:
         raise ValueError("start must have n_seqs + 1 entries")
-    _same_device(cache.device, start=start)
+    _same_device(cache.index, "start", start)
     return MsaoChunk(start.data_ptr(), n_rows, int(max_new))
+
+
+def _scratch(cache: KvCache, nbytes: int, stream) -> torch.Tensor:
+    with _on(stream):
+        buf = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=cache.device)
+        return buf if buf.data_ptr() % 256 == 0 else _workspace(nbytes, cache.device)
 
 
 def _on(stream):
@@ -851,55 +867,56 @@ def msao_cache_append(cache: KvCache, start: torch.Tensor, max_new: int, k: torc
     sections naming the pairs of each axis; interleaved pairs neighbours. Returns
     q_out (q's own memory may be passed)."""
     ctx = _cache_ctx(cache, ctx, stream)
-    rows = int(k.shape[0]) if k.dim() else -1
+    dim, dtype = cache.head_dim, cache.dtype
     a = MsaoAppend()
-    a.k_stride = _head_rows("k", k, cache.dtype, cache.kv_heads, cache.head_dim)
-    a.v_stride = _head_rows("v", v, cache.dtype, cache.kv_heads, cache.head_dim)
+    a.k_stride = _head_rows("k", k, dtype, cache.kv_heads, dim)
+    a.v_stride = _head_rows("v", v, dtype, cache.kv_heads, dim)
+    rows = k.shape[0]
     if v.shape[0] != rows or (q is not None and q.shape[0] != rows):
         raise ValueError("q, k and v differ in rows")
-    a.k, a.v, a.eps = _ptr(k), _ptr(v), float(eps)
+    a.k, a.v, a.eps = k.data_ptr(), v.data_ptr(), eps
     if q is not None:
-        a.q_stride = _head_rows("q", q, cache.dtype, None, cache.head_dim)
+        a.q_stride = _head_rows("q", q, dtype, None, dim)
         if q_out is None:
             with _on(stream):
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+                q_out = torch.empty(q.shape, dtype=dtype, device=q.device)
         if q_out.shape != q.shape:
             raise ValueError("q_out must have q's shape")
-        a.q_out_stride = _head_rows("q_out", q_out, cache.dtype, None, cache.head_dim)
-        a.q, a.q_out, a.heads = _ptr(q), _ptr(q_out), int(q.shape[1])
+        a.q_out_stride = _head_rows("q_out", q_out, dtype, None, dim)
+        a.q, a.q_out, a.heads = q.data_ptr(), q_out.data_ptr(), q.shape[1]
     elif q_out is not None or q_norm is not None:
         raise ValueError("q_out and q_norm need q")
     for name, w in (("q_norm", q_norm), ("k_norm", k_norm)):
         if w is not None:
-            if w.dtype != cache.dtype or tuple(w.shape) != (cache.head_dim,) or not w.is_contiguous():
+            if w.dtype is not dtype or w.shape != (dim,) or not w.is_contiguous():
                 raise ValueError(f"{name} must be [head_dim] of the cache's dtype")
             setattr(a, name, w.data_ptr())
     if inv_freq is not None and inv_freq.numel():
-        if inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+        if inv_freq.dtype is not torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
             raise ValueError("inv_freq must be a contiguous 1-D float32 tensor")
-        a.rot_dim, a.inv_freq, a.n_axes = 2 * int(inv_freq.shape[0]), inv_freq.data_ptr(), 1
+        pairs = inv_freq.shape[0]
+        a.rot_dim, a.inv_freq, a.n_axes = 2 * pairs, inv_freq.data_ptr(), 1
         if positions is not None:
-            if positions.dim() == 1:
-                positions = positions[None]
-            _int32("positions", positions, 2)
-            if positions.shape[1] != rows:
+            dims = positions.dim()
+            _int32("positions", positions, 1 if dims == 1 else 2)
+            if positions.shape[-1] != rows:
                 raise ValueError("positions must be [rows] or [axes, rows]")
-            a.n_axes = int(positions.shape[0])
+            a.n_axes = 1 if dims == 1 else positions.shape[0]
             a.positions = positions.data_ptr()
-            a.position_stride = int(positions.stride(0)) if a.n_axes > 1 else rows
-        sec = list(sections) if sections is not None else [int(inv_freq.shape[0])]
-        if len(sec) != a.n_axes or a.n_axes > MAX_AXES:
+            a.position_stride = positions.stride(0) if dims == 2 and a.n_axes > 1 else rows
+        if sections is None:
+            sections = (pairs,)
+        if len(sections) != a.n_axes or len(sections) > MAX_AXES:
             raise ValueError("sections must name the pairs of each axis of positions (at most 4)")
-        for i, n in enumerate(sec):
-            a.sections[i] = int(n)
+        a.sections = tuple(sections)
     elif positions is not None or sections is not None:
         raise ValueError("positions and sections need inv_freq")
-    _same_device(cache.device, k=k, v=v, q=q, q_out=q_out, q_norm=q_norm, k_norm=k_norm, positions=positions,
-                 inv_freq=inv_freq)
-    a.flags = APPEND_NEIGHBOURS if interleaved else 0
+    _same_device(cache.index, "every tensor of the step", k, v, q, q_out, q_norm, k_norm, positions, inv_freq)
+    if interleaved:
+        a.flags = APPEND_NEIGHBOURS
     ch = _chunk(cache, start, rows, max_new)
-    st = _stream_ptr(stream, cache.device)
-    _check(lib().msao_cache_append(ctx.handle, cache.addr, _addr(ch), _addr(a), st), ctx)
+    _check(lib().msao_cache_append(ctx.handle, cache.addr, ctypes.byref(ch), ctypes.byref(a), _stream_of(cache, stream)),
+           ctx)
     return q_out
 
 
@@ -925,28 +942,26 @@ def msao_cache_attention(cache: KvCache, start: torch.Tensor, max_new: int, q: t
     no sequence keep what `out` held (0 in one allocated here)."""
     ctx = _cache_ctx(cache, ctx, stream)
     q_stride = _head_rows("q", q, cache.dtype, None, cache.head_dim)
-    rows, heads = int(q.shape[0]), int(q.shape[1])
+    rows, heads = q.shape[0], q.shape[1]
     if out is None:
         with _on(stream):
             out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
-    if out.shape != q.shape:
+    elif out.shape != q.shape:
         raise ValueError("out must have q's shape")
     out_stride = _head_rows("out", out, cache.dtype, None, cache.head_dim)
-    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (rows, heads) or not lse.is_contiguous()):
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (rows, heads) or not lse.is_contiguous()):
         raise ValueError("lse must be contiguous float32 [rows, heads]")
-    _same_device(cache.device, q=q, out=out, lse=lse, workspace=workspace)
+    _same_device(cache.index, "q, out, lse and workspace", q, out, lse, workspace)
     ch = _chunk(cache, start, rows, max_new)
     flags = (ATTEND_CAUSAL if causal else 0) | (ATTEND_WEIGHT if accumulate else 0)
-    need = ctypes.c_size_t()
-    _check(lib().msao_cache_attention_workspace(cache.addr, _addr(ch), heads, flags, ctypes.byref(need)))
     if workspace is None:
-        with _on(stream):
-            workspace = _workspace(need.value, cache.device)
-    st = _stream_ptr(stream, cache.device)
-    _check(lib().msao_cache_attention(ctx.handle, cache.addr, _addr(ch), _ptr(q), q_stride, heads,
-                                      cache.head_dim ** -0.5 if scale is None else float(scale), flags, _ptr(out),
-                                      out_stride, _ptr(lse), _ptr(workspace),
-                                      ctypes.c_size_t(workspace.numel() * workspace.element_size()), st), ctx)
+        need = ctypes.c_size_t()
+        _check(lib().msao_cache_attention_workspace(cache.addr, ctypes.byref(ch), heads, flags, ctypes.byref(need)))
+        workspace = _scratch(cache, need.value, stream)
+    _check(lib().msao_cache_attention(ctx.handle, cache.addr, ctypes.byref(ch), q.data_ptr(), q_stride, heads,
+                                      cache.head_dim ** -0.5 if scale is None else scale, flags, out.data_ptr(),
+                                      out_stride, None if lse is None else lse.data_ptr(), workspace.data_ptr(),
+                                      workspace.numel() * workspace.element_size(), _stream_of(cache, stream)), ctx)
     return out
 
 
@@ -963,25 +978,24 @@ def msao_cache_evict(cache: KvCache, budget: torch.Tensor, n_first: int = 0, n_r
     _int32("budget", budget, 1)
     if budget.shape[0] != cache.n_seqs:
         raise ValueError("budget must have n_seqs entries")
-    if to is not None and to.device != cache.device:
+    if to is not None and to.index != cache.index:
         raise ValueError("the caches are on different devices")
     if kept_idx is None:
         with _on(stream):
-            kept_idx = torch.empty(cache.n_seqs, cache.kv_heads, cache.capacity, dtype=torch.int32,
+            kept_idx = torch.empty((cache.n_seqs, cache.kv_heads, cache.capacity), dtype=torch.int32,
                                    device=cache.device)
-    if (kept_idx.dtype != torch.int32 or kept_idx.dim() != 3 or not kept_idx.is_contiguous()
-            or tuple(kept_idx.shape[:2]) != (cache.n_seqs, cache.kv_heads) or kept_idx.shape[2] < cache.capacity):
+    elif (kept_idx.dtype is not torch.int32 or kept_idx.dim() != 3 or not kept_idx.is_contiguous()
+          or kept_idx.shape[:2] != (cache.n_seqs, cache.kv_heads) or kept_idx.shape[2] < cache.capacity):
         raise ValueError("kept_idx must be contiguous int32 [n_seqs, kv_heads, capacity]")
-    _same_device(cache.device, budget=budget, kept_idx=kept_idx, workspace=workspace)
-    need = ctypes.c_size_t()
-    _check(lib().msao_cache_evict_workspace(cache.addr, ctypes.byref(need)))
+    _same_device(cache.index, "budget, kept_idx and workspace", budget, kept_idx, workspace)
     if workspace is None:
-        with _on(stream):
-            workspace = _workspace(need.value, cache.device)
-    st = _stream_ptr(stream, cache.device)
-    _check(lib().msao_cache_evict(ctx.handle, cache.addr, to.addr if to is not None else None, _ptr(budget),
-                                  int(n_first), int(n_recent), _ptr(kept_idx), kept_idx.shape[2], _ptr(workspace),
-                                  ctypes.c_size_t(workspace.numel() * workspace.element_size()), st), ctx)
+        need = ctypes.c_size_t()
+        _check(lib().msao_cache_evict_workspace(cache.addr, ctypes.byref(need)))
+        workspace = _scratch(cache, need.value, stream)
+    _check(lib().msao_cache_evict(ctx.handle, cache.addr, to.addr if to is not None else None, budget.data_ptr(),
+                                  int(n_first), int(n_recent), kept_idx.data_ptr(), kept_idx.shape[2],
+                                  workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                  _stream_of(cache, stream)), ctx)
     return {"kept_idx": kept_idx, "kept_count": (to or cache).length}
 
 

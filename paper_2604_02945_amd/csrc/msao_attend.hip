@@ -1133,57 +1133,53 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight_rows(Atte
         }
 }
 
+// Four tokens a thread (they share a page), eight parts in flight.
 __global__ __launch_bounds__(kBlock) void k_weight_join(AttendArgs a, int blocks_per)
 {
     const int sh = blockIdx.x / blocks_per;
     const Place p = place_of(a, sh);
     const int n_rows = call_rows(a, p);
     const int seen = n_rows > 0 ? group_sees(p.length, p.n_new, a.group, n_rows - 1, a.causal) : 0;
-    const int t = (blockIdx.x - sh * blocks_per) * kBlock + threadIdx.x;
+    const int t = ((blockIdx.x - sh * blocks_per) * kBlock + threadIdx.x) * 4;
     // (a token of no page got nothing)
     if (t >= seen || page_at(a.c, p.seq, t >> a.c.page_shift) < 0) return;
     const int64_t step = (int64_t)a.c.n_seqs * a.c.kv_heads * capacity(a.c);
     const float* src = a.part_w + (int64_t)sh * capacity(a.c) + t;
-    float w = 0.0f;
-    for (int i = 0; i < a.row_parts; ++i) w += src[i * step];
-    a.c.weight[(int64_t)sh * a.c.weight_stride + t] += w;
-}
-
-template <typename K, typename... A>
-int enqueue_of(K kernel, int64_t blocks, int threads, void* stream, void* ev0, void* ev1, A... args)
-{
-    if (blocks <= 0) return kNoLaunch;
-    if (ev0 && ev1)
-        hipExtLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), 0, (hipStream_t)stream, (hipEvent_t)ev0,
-                              (hipEvent_t)ev1, 0, args...);
-    else
-        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), 0, (hipStream_t)stream, args...);
-    return (int)hipGetLastError();
+    f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i = 0; i < a.row_parts; i += 8) {
+        f32x4 v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = i + e < a.row_parts ? *(const f32x4*)(src + (i + e) * step) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w += v[e];
+    }
+    float* dst = a.c.weight + (int64_t)sh * a.c.weight_stride + t;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (t + e < seen) dst[e] += w[e];
 }
 
 template <typename K, typename... A>
 int enqueue(K kernel, int64_t blocks, void* stream, void* ev0, void* ev1, A... args)
 {
-    return enqueue_of(kernel, blocks, kBlock, stream, ev0, ev1, args...);
+    if (blocks <= 0) return kNoLaunch;
+    if (ev0 && ev1)
+        hipExtLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kBlock), 0, (hipStream_t)stream, (hipEvent_t)ev0,
+                              (hipEvent_t)ev1, 0, args...);
+    else
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kBlock), 0, (hipStream_t)stream, args...);
+    return (int)hipGetLastError();
 }
 
 int padded_dim(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 
 int64_t pairs(const AttendArgs& a) { return (int64_t)a.c.n_seqs * a.c.kv_heads; }
 
-#ifndef CFG
-#define CFG 2, 4, 64, 2
-#endif
-#ifndef MT_ROWS
-#define MT_ROWS 2
-#endif
-#ifndef NWV
-#define NWV 4
-#endif
-#ifndef MANY
-#define MANY 128
-#endif
-constexpr int kManyTiles = MT_ROWS, kManyRows = kManyTiles * 16 * NWV;
+// k_attend_rows: 32 rows a wavefront, four wavefronts, stages of 64 tokens. Chunks of 2,048
+// over 12,288 tokens: 730 us; 48 rows a wavefront 884 (246 registers, as fast a SIMD but fewer
+// workgroups), 64 spill; 16 rows and eight wavefronts 770; stages of 32 tokens 852. With fewer
+// than kManyRows rows its wavefronts would be idle or its tokens not spread: k_attend.
+constexpr int kRowTiles = 2, kStageTokens = 64, kManyRows = kRowTiles * 16 * kWaves;
 // Rows of a workgroup: what the registers of its wavefronts hold.
 template <int DT, int DP>
 int attend_rows(const AttendArgs& a, void* st, void* e0, void* e1)
@@ -1191,7 +1187,7 @@ int attend_rows(const AttendArgs& a, void* st, void* e0, void* e1)
     const int64_t blocks = pairs(a) * a.row_tiles * a.splits;
     if (a.tile_rows == 16) return enqueue(k_attend<DT, DP, 1, 1>, blocks, st, e0, e1, a);
     if constexpr (DT == kBF16 && DP <= 128)
-        if (a.tile_rows == kManyRows) return enqueue_of(k_attend_rows<DP, CFG>, blocks, NWV * kWave, st, e0, e1, a);
+        if (a.tile_rows == kManyRows) return enqueue(k_attend_rows<DP, kRowTiles, kWaves, kStageTokens, 2>, blocks, st, e0, e1, a);
     if constexpr (DP == 256) {
         if (a.tile_rows == 32) return enqueue(k_attend<DT, DP, 1, 2>, blocks, st, e0, e1, a);
     } else {
@@ -1242,32 +1238,33 @@ template <int DT, int DP> struct Weight {
 
 }  // namespace
 
-#ifndef PT
-#define PT 2048
-#endif
-#ifndef PM
-#define PM 1024
-#endif
-#ifndef PL
-#define PL 128
-#endif
-#ifndef WT
-#define WT 8192
-#endif
-constexpr int64_t kPartTarget = PT, kPartLeast = PL, kWeightTarget = WT, kPartMost = PM;
+// Parts of a row's tokens. Few rows: parts for kPartTarget workgroups if every sequence were
+// as long as can be, of 128 .. 1,024 tokens (a tile a wavefront at least; 64 requests of up to
+// 16,000 tokens: 166 us with 1,024, 178 with 512, 188 with 2,048; two of 131,072: 188, 198,
+// 186). Many rows, whose parts cost a store and a load of 4 bytes a channel: none from 512
+// workgroups on (8 prompts of up to 1,500 tokens 79 us, 107 with parts of 256), below that
+// parts for kManyTarget, or as many as for few rows with float32, whose products take eight
+// times as long (text over encoder states 70 us, 103 with parts for 512).
+constexpr int64_t kPartTarget = 2048, kPartLeast = 128, kPartMost = 1024, kManyTarget = 1024, kManyTargetF32 = 4096;
+// Parts of the tokens in the weight pass of few rows (attend_round's 98 us; 112 with 4,096,
+// 105 with 16,384), and of the rows in that of many: up to 32 (25 us, 33 with 10).
+constexpr int64_t kWeightTarget = 8192, kWeightRowTarget = 8192, kMostRowParts = 32;
 void attend_shape(AttendArgs& a)
 {
     const int64_t rows = (int64_t)a.ch.max_new * a.group;
     const int most = padded_dim(a.c.dim) == 256 ? 32 : 64;  // rows of a workgroup at most
     a.tile_rows = rows <= 16 ? 16 : rows <= 32 || most == 32 ? 32 : 64;
-    if (a.dtype == kBF16 && most == 64 && rows > MANY) a.tile_rows = kManyRows;
+    if (a.dtype == kBF16 && most == 64 && rows >= kManyRows) a.tile_rows = kManyRows;
     a.row_tiles = (int)((rows + a.tile_rows - 1) / a.tile_rows);
     const int64_t np = std::max<int64_t>(pairs(a), 1), groups = std::max<int64_t>(np * a.row_tiles, 1), cap = capacity(a.c);
     auto up = [](int64_t v, int64_t to) { return (v + to - 1) / to * to; };
     const int64_t whole = std::max<int64_t>(up(cap, kTile), kTile);
     // parts for about kPartTarget workgroups if every sequence were as long as can be
     int64_t per = std::min<int64_t>(up((groups * cap + kPartTarget - 1) / kPartTarget, kPartLeast), kPartMost);
-    if (rows > 64) per = groups >= 512 ? whole : up((groups * cap + 511) / 512, kPartLeast);
+    if (rows > 64) {
+        const int64_t target = a.dtype == kBF16 ? kManyTarget : kManyTargetF32;
+        per = groups >= target / 2 ? whole : up((groups * cap + target - 1) / target, kPartLeast);
+    }
     a.part_tokens = (int)std::min(std::max<int64_t>(per, kPartLeast), whole);
     a.splits = std::max(1, parts_of((int)cap, a.part_tokens));
     a.row_parts = 1;
@@ -1275,7 +1272,7 @@ void attend_shape(AttendArgs& a)
         a.weight_tokens = kTile * kWaves;
         a.weight_parts = std::max(1, parts_of((int)cap, a.weight_tokens));
         const int64_t steps = (rows + kRowStep - 1) / kRowStep;
-        a.row_parts = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(steps, 16), 2048 / (np * a.weight_parts)));
+        a.row_parts = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(steps, kMostRowParts), kWeightRowTarget / (np * a.weight_parts)));
     } else {
         a.weight_tokens = (int)std::min<int64_t>(std::max<int64_t>(up((np * cap + kWeightTarget - 1) / kWeightTarget, kPartLeast), kPartLeast), whole);
         a.weight_parts = std::max(1, parts_of((int)cap, a.weight_tokens));
@@ -1310,7 +1307,7 @@ int launch_weight(const AttendArgs& a, void* st, void* e0, void* e1)
 int launch_weight_join(const AttendArgs& a, void* st, void* e0, void* e1)
 {
     if (!a.add_weight || a.row_parts <= 1) return kNoLaunch;
-    const int per = (capacity(a.c) + kBlock - 1) / kBlock;
+    const int per = (capacity(a.c) + 4 * kBlock - 1) / (4 * kBlock);
     return enqueue(k_weight_join, pairs(a) * per, st, e0, e1, a, per);
 }
 

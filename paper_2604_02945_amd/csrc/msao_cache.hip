@@ -104,6 +104,47 @@ __global__ __launch_bounds__(kBlock) void k_append(AppendArgs a)
     const int64_t item = (int64_t)blockIdx.x * kWaves + wave;
     const int row = (int)(item / a.parts), part = (int)(item - (int64_t)row * a.parts);
     if (row >= a.ch.n_rows) return;
+    const int u = lane & (a.lanes - 1), per = kWave / a.lanes;  // the lane's pair of eights; heads of a round
+    const int half = a.rot / 2, turned = a.rot / 16;
+    const bool turns = u < turned;
+    int d0, d1;
+    if (turns && !a.neighbours) {
+        d0 = 8 * u;
+        d1 = half + 8 * u;
+    } else {
+        d0 = 16 * u;
+        d1 = d0 + 8;
+    }
+    const bool has0 = d0 < a.c.dim, has1 = d1 < a.c.dim;
+    const int heads = a.heads + 2 * a.c.kv_heads;
+    const int rounds = (heads + per - 1) / per;
+    Eight<DT> x0[U], x1[U];
+    auto load = [&](int r0) {
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const int h = (r0 + j) * per + lane / a.lanes;
+            x0[j].zero();
+            x1[j].zero();
+            if (h >= heads) continue;
+            const uint8_t* src;
+            if (h < a.heads) src = a.q + row * a.q_stride + (int64_t)h * a.c.dim * ES;
+            else if (h < a.heads + a.c.kv_heads) src = a.k + row * a.k_stride + (int64_t)(h - a.heads) * a.c.dim * ES;
+            else src = a.v + row * a.v_stride + (int64_t)(h - a.heads - a.c.kv_heads) * a.c.dim * ES;
+            if (has0) x0[j].load(src + d0 * ES);
+            if (has1) x1[j].load(src + d1 * ES);
+        }
+    };
+    // the row's values and the norms' come while its sequence, place and page are found
+    load(part * U);
+    Eight<DT> nq0, nq1, nk0, nk1;
+    nq0.zero();
+    nq1.zero();
+    nk0.zero();
+    nk1.zero();
+    if (a.q_norm && has0) nq0.load(a.q_norm + d0 * ES);
+    if (a.q_norm && has1) nq1.load(a.q_norm + d1 * ES);
+    if (a.k_norm && has0) nk0.load(a.k_norm + d0 * ES);
+    if (a.k_norm && has1) nk1.load(a.k_norm + d1 * ES);
     const int s = uniform(seq_of_row(a, row));
     if (s < 0) return;
     const Rows rows = seq_rows(a.ch, s);
@@ -112,7 +153,6 @@ __global__ __launch_bounds__(kBlock) void k_append(AppendArgs a)
     const int page = place >= 0 ? page_at(a.c, s, (int)place >> a.c.page_shift) : -1;
     const int slot = (int)place & mask;
 
-    const int half = a.rot / 2;
     for (int i = lane; i < half; i += kWave) {
         int axis = 0;
 #pragma unroll
@@ -127,19 +167,6 @@ __global__ __launch_bounds__(kBlock) void k_append(AppendArgs a)
     // the wavefront's own stores, read by its other lanes
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-
-    const int u = lane & (a.lanes - 1), per = kWave / a.lanes;  // the lane's pair of eights; heads of a round
-    const int turned = a.rot / 16;
-    const bool turns = u < turned;
-    int d0, d1;
-    if (turns && !a.neighbours) {
-        d0 = 8 * u;
-        d1 = half + 8 * u;
-    } else {
-        d0 = 16 * u;
-        d1 = d0 + 8;
-    }
-    const bool has0 = d0 < a.c.dim, has1 = d1 < a.c.dim;
     float cs[8], sn[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -148,26 +175,11 @@ __global__ __launch_bounds__(kBlock) void k_append(AppendArgs a)
         sn[e] = v.y;
     }
 
-    const int heads = a.heads + 2 * a.c.kv_heads;
-    const int rounds = (heads + per - 1) / per;
     if (a.c.weight && part == 0 && place >= 0)
         for (int h = lane; h < a.c.kv_heads; h += kWave)
             a.c.weight[((int64_t)s * a.c.kv_heads + h) * a.c.weight_stride + place] = 0.0f;
     for (int r0 = part * U; r0 < rounds; r0 += a.parts * U) {
-        Eight<DT> x0[U], x1[U];
-#pragma unroll
-        for (int j = 0; j < U; ++j) {
-            const int h = (r0 + j) * per + lane / a.lanes;
-            x0[j].zero();
-            x1[j].zero();
-            if (h >= heads) continue;
-            const uint8_t* src;
-            if (h < a.heads) src = a.q + row * a.q_stride + (int64_t)h * a.c.dim * ES;
-            else if (h < a.heads + a.c.kv_heads) src = a.k + row * a.k_stride + (int64_t)(h - a.heads) * a.c.dim * ES;
-            else src = a.v + row * a.v_stride + (int64_t)(h - a.heads - a.c.kv_heads) * a.c.dim * ES;
-            if (has0) x0[j].load(src + d0 * ES);
-            if (has1) x1[j].load(src + d1 * ES);
-        }
+        if (r0 != part * U) load(r0);
 #pragma unroll
         for (int j = 0; j < U; ++j) {
             const int h = (r0 + j) * per + lane / a.lanes;
@@ -183,12 +195,12 @@ __global__ __launch_bounds__(kBlock) void k_append(AppendArgs a)
             if (!is_v) {
                 if (norm) {
                     const float f = 1.0f / sqrtf(sq / (float)a.c.dim + a.eps);
-                    Eight<DT> n0, n1;
-                    n0.zero();
-                    n1.zero();
-                    if (has0) n0.load(norm + d0 * ES);
-                    if (has1) n1.load(norm + d1 * ES);
                     float w0[8], w1[8];
+                    Eight<DT> n0 = nk0, n1 = nk1;
+                    if (is_q) {
+                        n0 = nq0;
+                        n1 = nq1;
+                    }
                     n0.widen(w0);
                     n1.widen(w1);
 #pragma unroll

@@ -17,17 +17,14 @@ int main()
 {
     std::mt19937_64 rng(1);
     // parts
-    for (int most : {1, 2, 3, 7, 64, 513})
-        for (int seen : {-5, 0, 1, 31, 32, 33, 255, 256, 257, 300, 511, 512, 513, 4097, 131072, 1 << 29}) {
-            const Cut c = cut_tokens(seen, most);
-            CHECK(c.per % kTile == 0 && c.per > 0);
+    for (int per : {32, 128, 256, 1024, 1 << 29})
+        for (int seen : {-5, 0, 1, 31, 32, 33, 127, 128, 129, 300, 4097, 131072, 1 << 29}) {
+            const int n = parts_of(seen, per);
             if (seen <= 0) {
-                CHECK(c.n == 0);
+                CHECK(n == 0);
                 continue;
             }
-            CHECK(c.n >= 1 && c.n <= most);
-            CHECK((int64_t)c.n * c.per >= seen && (int64_t)(c.n - 1) * c.per < seen);
-            if (c.n > 1) CHECK(c.per >= kPartTokens / 2);
+            CHECK((int64_t)n * per >= seen && (int64_t)(n - 1) * per < seen);
         }
     // what the last row of a group sees
     for (int i = 0; i < 100000; ++i) {

@@ -159,7 +159,7 @@ def test_attention_workspace():
     a, b = size(chunk()), size(chunk(), flags=3)
     assert a % 256 == 0 and b >= a + 10 * 32 * 4
     assert size(chunk(n_rows=0, max_new=0)) == 0
-    one = cache(pages_per_seq=4, table_stride=4)  # 256 tokens: one part
+    one = cache(pages_per_seq=2, table_stride=2)  # 128 tokens: one part
     assert size(chunk(), c=one) == 0
     assert B.lib().msao_cache_attention_workspace(B._addr(c), B._addr(chunk()), 32, 1, None) == INVALID
 
