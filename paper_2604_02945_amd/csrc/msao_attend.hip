@@ -1027,16 +1027,17 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight(AttendArg
 // block's tokens are cut into row_parts parts, so that a few short prompts fill the
 // device too; k_weight_join adds the parts' sums in order.
 constexpr int kRowStep = 64;
+constexpr int row_step(int dt, int dp) { return dt == kF32 && dp == 256 ? 32 : kRowStep; }  // registers
 template <int DT, int DP>
 __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight_rows(AttendArgs a)
 {
     constexpr int ES = Type<DT>::kSize;
-    constexpr int KS = DP * ES / 64;
+    constexpr int KS = DP * ES / 64, kStep = row_step(DT, DP);
     using Q = Queries<DT, DP>;
-    constexpr int kPer = kRowStep * Q::kPieces / kBlock;  // pieces of a thread
-    __shared__ __align__(16) uint8_t lds[kRowStep * Q::kLine];
-    __shared__ float lds_z[kRowStep];
-    __shared__ int lds_last[kRowStep];
+    constexpr int kPer = kStep * Q::kPieces / kBlock;  // pieces of a thread
+    __shared__ __align__(16) uint8_t lds[kStep * Q::kLine];
+    __shared__ float lds_z[kStep];
+    __shared__ int lds_last[kStep];
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
     const int i16 = lane & 15, c = lane >> 4;
     const int per_pair = a.weight_parts * a.row_parts, sh = blockIdx.x / per_pair;
@@ -1062,20 +1063,20 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight_rows(Atte
     }
     // rows from the first that sees the block's first token, this part's share of them
     const int from = a.causal ? max(0, b0 - (p.length - p.n_new)) * a.group : 0;
-    const int steps = (n_rows - from + kRowStep - 1) / kRowStep, per = (steps + a.row_parts - 1) / a.row_parts;
+    const int steps = (n_rows - from + kStep - 1) / kStep, per = (steps + a.row_parts - 1) / a.row_parts;
     const int s_end = min(steps, (part + 1) * per);
     float w[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     u32x4 next[kPer];
     float next_z = INFINITY;
     int next_last = -1;
     auto fetch = [&](int step) {
-        const int r0 = from + step * kRowStep;
+        const int r0 = from + step * kStep;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int at = i * kBlock + threadIdx.x, row = at / Q::kPieces;
             next[i] = Q::fetch(a, p, r0 + row, n_rows, at - row * Q::kPieces);
         }
-        if (threadIdx.x < kRowStep) {
+        if (threadIdx.x < kStep) {
             const int row = r0 + threadIdx.x, t = row / a.group, head = p.head * a.group + (row - t * a.group);
             next_z = row < n_rows ? a.lse2[(int64_t)(p.begin + t) * a.heads + head] : INFINITY;
             if (next_z == -INFINITY) next_z = INFINITY;
@@ -1090,17 +1091,17 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight_rows(Atte
             const int at = i * kBlock + threadIdx.x, row = at / Q::kPieces;
             *(u32x4*)(lds + row * Q::kLine + 16 * (at - row * Q::kPieces)) = next[i];
         }
-        if (threadIdx.x < kRowStep) {
+        if (threadIdx.x < kStep) {
             lds_z[threadIdx.x] = next_z;
             lds_last[threadIdx.x] = next_last;
         }
         __syncthreads();
         if (step + 1 < s_end) fetch(step + 1);
-        const int r0 = from + step * kRowStep;
+        const int r0 = from + step * kStep;
         const int least = a.causal ? p.length - p.n_new + r0 / a.group : p.length - 1;
         const bool whole = kn[0] == 16 && kn[1] == 16 && tok + kTile - 1 <= least;
 #pragma unroll
-        for (int m = 0; m < kRowStep / 16; ++m) {
+        for (int m = 0; m < kStep / 16; ++m) {
             Q q;
             q.take(lds, 16 * m);
             const float z = lds_z[16 * m + i16];

@@ -35,12 +35,24 @@ struct ChunkDev {
     int32_t n_rows, max_new;
 };
 
+// An entry of a table that no kernel writes while it reads it: where the index is the same
+// for a wavefront it comes through the scalar cache, and its wait is no wait for the vector
+// loads before it.
+MSAO_HD int entry(const int32_t* table, int64_t i)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    return ((const __attribute__((address_space(4))) int32_t*)(uintptr_t)table)[i];
+#else
+    return table[i];
+#endif
+}
+
 MSAO_HD int clamp_int(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
 
 MSAO_HD int capacity(const CacheDev& c) { return c.per_seq << c.page_shift; }
 
 // Tokens of sequence s, whatever the caller's array says.
-MSAO_HD int seq_length(const CacheDev& c, int s) { return clamp_int(c.length[s], 0, capacity(c)); }
+MSAO_HD int seq_length(const CacheDev& c, int s) { return clamp_int(entry(c.length, s), 0, capacity(c)); }
 
 // Rows of sequence s of the chunk: the first, and how many (all of them in [0, n_rows)).
 struct Rows {
@@ -48,7 +60,7 @@ struct Rows {
 };
 MSAO_HD Rows seq_rows(const ChunkDev& ch, int s)
 {
-    const int b = clamp_int(ch.start[s], 0, ch.n_rows), e = clamp_int(ch.start[s + 1], b, ch.n_rows);
+    const int b = clamp_int(entry(ch.start, s), 0, ch.n_rows), e = clamp_int(entry(ch.start, s + 1), b, ch.n_rows);
     return Rows{b, e - b};
 }
 
@@ -56,7 +68,7 @@ MSAO_HD Rows seq_rows(const ChunkDev& ch, int s)
 MSAO_HD int page_or_none(int page, int n_pages) { return page >= 0 && page < n_pages ? page : -1; }
 MSAO_HD int page_at(const CacheDev& c, int s, int col)
 {
-    return page_or_none(c.pages[(int64_t)s * c.table_stride + col], c.n_pages);
+    return page_or_none(entry(c.pages, (int64_t)s * c.table_stride + col), c.n_pages);
 }
 
 // How the `seen` tokens of a group of rows are cut: parts of `per` tokens (whole 32-token

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "msao_cache.h"
 #include "msao_device.h"
@@ -71,14 +72,14 @@ struct Eight {
 };
 
 // The sequence of a row of the chunk (-1: none): of the starts that are not past the
-// row, the last one's.
-__device__ __forceinline__ int seq_of_row(const AppendArgs& a, int row)
+// row, the last one's. `first`: the lane's of the first 64 starts.
+__device__ __forceinline__ int seq_of_row(const AppendArgs& a, int row, int first)
 {
     const int lane = threadIdx.x & (kWave - 1);
     int n = 0;
     for (int i0 = 0; i0 <= a.c.n_seqs; i0 += kWave) {
-        const int i = i0 + lane;
-        n += __popcll(__ballot(i <= a.c.n_seqs && clamp_int(a.ch.start[min(i, a.c.n_seqs)], 0, a.ch.n_rows) <= row));
+        const int i = i0 + lane, start = i0 == 0 ? first : a.ch.start[min(i, a.c.n_seqs)];
+        n += __popcll(__ballot(i <= a.c.n_seqs && clamp_int(start, 0, a.ch.n_rows) <= row));
     }
     const int s = n - 1;
     if (s < 0 || s >= a.c.n_seqs) return -1;
@@ -134,7 +135,20 @@ __global__ __launch_bounds__(kBlock) void k_append(AppendArgs a)
             if (has1) x1[j].load(src + d1 * ES);
         }
     };
-    // the row's values and the norms' come while its sequence, place and page are found
+    // what needs no sequence is on its way while the row's sequence, place and page are found
+    const int first = a.ch.start[min(lane, a.c.n_seqs)];
+    int at[2] = {0, 0};
+    float freq[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int i = lane + kWave * e;
+        if (i >= half) continue;
+        int axis = 0;
+#pragma unroll
+        for (int x = 0; x < 3; ++x) axis += i >= a.axis_end[x];
+        if (a.positions) at[e] = a.positions[axis * a.position_stride + row];
+        freq[e] = a.inv_freq[i];
+    }
     load(part * U);
     Eight<DT> nq0, nq1, nk0, nk1;
     nq0.zero();
@@ -145,7 +159,7 @@ __global__ __launch_bounds__(kBlock) void k_append(AppendArgs a)
     if (a.q_norm && has1) nq1.load(a.q_norm + d1 * ES);
     if (a.k_norm && has0) nk0.load(a.k_norm + d0 * ES);
     if (a.k_norm && has1) nk1.load(a.k_norm + d1 * ES);
-    const int s = uniform(seq_of_row(a, row));
+    const int s = uniform(seq_of_row(a, row, first));
     if (s < 0) return;
     const Rows rows = seq_rows(a.ch, s);
     const int64_t place = (int64_t)seq_length(a.c, s) - rows.n + (row - rows.begin);  // in the cache
@@ -153,16 +167,14 @@ __global__ __launch_bounds__(kBlock) void k_append(AppendArgs a)
     const int page = place >= 0 ? page_at(a.c, s, (int)place >> a.c.page_shift) : -1;
     const int slot = (int)place & mask;
 
-    for (int i = lane; i < half; i += kWave) {
-        int axis = 0;
 #pragma unroll
-        for (int x = 0; x < 3; ++x) axis += i >= a.axis_end[x];
-        const int at = a.positions ? a.positions[axis * a.position_stride + row] : (int)place;
-        double t = (double)at * (double)a.inv_freq[i] * 0.15915494309189533577;
+    for (int e = 0; e < 2; ++e) {
+        if (kWave * e >= half) break;
+        double t = (double)(a.positions ? at[e] : (int)place) * (double)freq[e] * 0.15915494309189533577;
         t -= floor(t);
         float sn, cs;
         sincospif(2.0f * (float)t, &sn, &cs);
-        turn[wave][i] = f32x2{cs, sn};
+        if (lane + kWave * e < half) turn[wave][lane + kWave * e] = f32x2{cs, sn};
     }
     // the wavefront's own stores, read by its other lanes
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -249,14 +261,97 @@ __global__ __launch_bounds__(kBlock) void k_append(AppendArgs a)
 
 // ---- eviction -------------------------------------------------------------------
 
-constexpr int kSelBlock = 1024;
-constexpr int kSelWaves = kSelBlock / kWave;
-constexpr int kBins = 2048;
+// The tokens that stay of one (sequence, kv head), by one workgroup: the key of the last
+// ranked one by digits of 11, 10 and 10 bits (the sign is 0), counted in LDS, then the kept
+// indices and weights in one ascending pass. k_select holds the weights in registers, 16
+// neighbours a thread, and so has one block-wide sum and four other barriers in all; beyond
+// kSelTokens tokens k_select_long goes over memory again for each digit.
+constexpr int kSelItems = 16;
+constexpr int kSelLong = 1024;                    // threads of k_select_long
+constexpr int kSelTokens = kSelItems * 1024;
+constexpr int kDigits = 3;
+__device__ constexpr int kShift[kDigits] = {20, 10, 0}, kWidth[kDigits] = {11, 10, 10};
+constexpr int kBins = 2048 + 1024 + 1024;
+__device__ __forceinline__ constexpr int first_bin(int d) { return d == 0 ? 0 : 1024 + 1024 * d; }
 
 // Order of a weight: larger is kept; NaN and what is not above 0 counts as 0.
 __device__ __forceinline__ uint32_t weight_key(float w) { return w > 0.0f ? __float_as_uint(w) : 0u; }
 
+// Which tokens stay: the first `lo`, those from `hi` on, and `take` of those between.
+struct Kept {
+    int L, k, lo, hi, take;
+    __device__ __forceinline__ Kept(const EvictArgs& a, int s)
+    {
+        L = seq_length(a.from, s);
+        k = min(min(L, max(entry(a.budget, s), 0)), capacity(a.to));
+        lo = min(a.n_first, k);
+        const int recent = min(a.n_recent, k - lo);
+        hi = L - recent;
+        take = k - lo - recent;
+    }
+    __device__ __forceinline__ bool all() const { return take >= hi - lo; }
+};
+
+// The least key that stays and how many of that key do; `whole`: all of them from `least` on.
+struct Border {
+    uint32_t least, ties;
+    bool whole;
+    __device__ __forceinline__ bool above(uint32_t key) const { return whole ? key >= least : key > least; }
+    __device__ __forceinline__ bool equal(uint32_t key) const { return !whole && key == least; }
+};
+
+// The bin, from the largest down, in which the `want`-th key lies, the rank within it, and
+// its count; every wavefront finds it for itself.
+struct Found {
+    uint32_t bin, rank, count;
+};
+template <int BINS>
+__device__ __forceinline__ Found find_bin(const uint32_t* bins, uint32_t want)
+{
+    constexpr int N = BINS / kWave;  // a lane's bins, those of lane 0 the largest
+    const int lane = threadIdx.x & (kWave - 1);
+    const uint32_t* mine = bins + BINS - (lane + 1) * N;
+    uint32_t sum = 0;
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        const u32x4 v = *(const u32x4*)(mine + i);
+        sum += v[0] + v[1] + v[2] + v[3];
+    }
+    uint32_t upto = sum;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        const uint32_t y = (uint32_t)__shfl_up((int)upto, o);
+        if (lane >= o) upto += y;
+    }
+    const int at = __builtin_ctzll(__ballot(upto >= want) | 1ull << (kWave - 1));
+    const uint32_t before = (uint32_t)__builtin_amdgcn_readlane((int)(upto - sum), at);
+    // the N bins of lane `at`, one a lane
+    const int top = BINS - 1 - at * N;
+    uint32_t c = lane < N ? bins[top - lane] : 0u, run = c;
+#pragma unroll
+    for (int o = 1; o < N; o <<= 1) {
+        const uint32_t y = (uint32_t)__shfl_up((int)run, o);
+        if (lane >= o) run += y;
+    }
+    const int l = __builtin_ctzll(__ballot(lane < N && before + run >= want) | 1ull << (N - 1));
+    const uint32_t count = (uint32_t)__builtin_amdgcn_readlane((int)c, l);
+    return Found{(uint32_t)(top - l), want - before - ((uint32_t)__builtin_amdgcn_readlane((int)run, l) - count), count};
+}
+
+// One digit of the border: its bins are counted; false once the border is known.
+template <int D>
+__device__ __forceinline__ bool next_digit(Border& b, uint32_t& want, const uint32_t* bins)
+{
+    const Found f = find_bin<1 << kWidth[D]>(bins + first_bin(D), want);
+    b.least |= f.bin << kShift[D];
+    want = f.rank;
+    b.ties = want;
+    b.whole = f.rank == f.count;  // all of the bin stay, whatever the lower digits
+    return !b.whole;
+}
+
 // Exclusive sum over the block of a per-thread value, and the total.
+template <int WAVES>
 __device__ __forceinline__ uint64_t block_scan(uint64_t v, uint64_t* lds, uint64_t* total)
 {
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
@@ -270,7 +365,8 @@ __device__ __forceinline__ uint64_t block_scan(uint64_t v, uint64_t* lds, uint64
     if (lane == kWave - 1) lds[wave] = x;
     __syncthreads();
     uint64_t before = 0, all = 0;
-    for (int w = 0; w < kSelWaves; ++w) {
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
         const uint64_t t = lds[w];
         before += w < wave ? t : 0;
         all += t;
@@ -279,95 +375,149 @@ __device__ __forceinline__ uint64_t block_scan(uint64_t v, uint64_t* lds, uint64
     return before + x - v;
 }
 
-// The tokens that stay of one (sequence, kv head), by one workgroup: the k-th largest
-// key by digits of 11, 10 and 10 bits, counted in LDS, then one ascending pass that
-// writes the kept indices and weights. In place, a pass's weights are all in registers
-// before any is written, and go to places not past those already read.
-__global__ __launch_bounds__(kSelBlock) void k_select(EvictArgs a)
+// N neighbouring tokens of a thread, from j0: the kept ones' indices and weights to their
+// places (`above` << 32 | `equal` tokens lie before them); the least place that changes.
+template <int N>
+__device__ __forceinline__ int put_kept(const EvictArgs& a, const Kept& q, const Border& b, int sh, int j0, const float (&v)[N],
+                                        uint64_t before)
 {
-    __shared__ uint32_t bins[kBins];
-    __shared__ uint64_t sums[kSelWaves];
-    __shared__ uint32_t found[2];
-    __shared__ int first_moved;
-    const int sh = blockIdx.x, s = sh / a.from.kv_heads, tid = threadIdx.x;
-    const int L = seq_length(a.from, s), cap = capacity(a.from);
-    const int k = min(min(L, max(a.budget[s], 0)), capacity(a.to));
-    const int first = min(a.n_first, k), recent = min(a.n_recent, k - first);
-    const int lo = first, hi = L - recent;              // those between are ranked
-    const int take = k - first - recent;                // and so many of them stay
-    const float* w = a.from.weight + (int64_t)sh * a.from.weight_stride;
-    uint32_t least = 0;       // the smallest key that stays
-    uint32_t ties = 0;        // how many of that key
-    if (take > 0 && take < hi - lo) {
-        uint32_t want = (uint32_t)take;
-        const int shift[3] = {20, 10, 0}, width[3] = {11, 10, 10};
-        for (int d = 0; d < 3; ++d) {
-            for (int b = tid; b < kBins; b += kSelBlock) bins[b] = 0;
-            __syncthreads();
-            for (int j = lo + tid; j < hi; j += kSelBlock) {
-                const uint32_t key = weight_key(w[j]);
-                if (d == 0 || key >> (shift[d] + width[d]) == least >> (shift[d] + width[d]))
-                    atomicAdd(&bins[key >> shift[d] & ((1u << width[d]) - 1)], 1u);
-            }
-            __syncthreads();
-            // from the largest digit down: thread t has bins 2047 - 2t and the one below
-            const uint32_t b0 = bins[kBins - 1 - 2 * tid], b1 = bins[kBins - 2 - 2 * tid];
-            uint64_t total;
-            const uint32_t before = (uint32_t)block_scan(b0 + b1, sums, &total);
-            if (before < want && want <= before + b0 + b1) {
-                const bool second = want > before + b0;
-                found[0] = (uint32_t)(kBins - 1 - 2 * tid - (second ? 1 : 0));
-                found[1] = want - before - (second ? b0 : 0);
-            }
-            __syncthreads();
-            least |= found[0] << shift[d];
-            want = found[1];
-            __syncthreads();
-        }
-        ties = want;
-    }
-    const bool all = take >= hi - lo, none = take <= 0;
-    if (tid == 0) first_moved = k;
     int32_t* idx = a.kept_idx + (int64_t)sh * a.idx_stride;
     float* tw = a.to.weight ? a.to.weight + (int64_t)sh * a.to.weight_stride : nullptr;
-    uint32_t kept = 0, tied = 0;  // before this pass: kept beside the ties, and of the tied key
-    for (int j0 = 0; j0 < L; j0 += 4 * kSelBlock) {
-        float v[4];
-        bool above[4], equal[4];
-        uint32_t n = 0, e = 0;
+    uint32_t n = (uint32_t)(before >> 32), e = (uint32_t)before;
+    int moved = INT32_MAX;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int j = j0 + 4 * tid + i;
-            v[i] = j < L ? w[j] : 0.0f;
-            const uint32_t key = weight_key(v[i]);
-            const bool fixed = j < lo || j >= hi;
-            above[i] = j < L && (fixed || all || (!none && key > least));
-            equal[i] = j < L && !fixed && !all && !none && key == least;
-            n += above[i];
-            e += equal[i];
+    for (int i = 0; i < N; ++i) {
+        const int j = j0 + i;
+        if (j >= q.L) break;
+        const uint32_t key = weight_key(v[i]);
+        const bool fixed = j < q.lo || j >= q.hi, above = fixed || b.above(key), equal = !fixed && b.equal(key);
+        if (above || (equal && e < b.ties)) {
+            const int to = (int)(n + min(e, b.ties));
+            idx[to] = j;
+            if (tw) tw[to] = v[i];
+            if (to != j) moved = min(moved, to);
         }
-        uint64_t total;
-        const uint64_t at = block_scan((uint64_t)n << 32 | e, sums, &total);
-        uint32_t n_at = kept + (uint32_t)(at >> 32), e_at = tied + (uint32_t)at;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int j = j0 + 4 * tid + i;
-            const bool stays = above[i] || (equal[i] && e_at < ties);
-            if (stays) {
-                const int to = (int)(n_at + min(e_at, ties));
-                idx[to] = j;
-                if (tw) tw[to] = v[i];
-                if (to != j) atomicMin(&first_moved, to);
-            }
-            n_at += above[i];
-            e_at += equal[i];
-        }
-        kept += (uint32_t)(total >> 32);
-        tied += (uint32_t)total;
+        n += above;
+        e += equal;
     }
-    for (int j = k + tid; j < cap; j += kSelBlock) idx[j] = -1;
+    return moved;
+}
+template <int N>
+__device__ __forceinline__ uint64_t count_kept(const Kept& q, const Border& b, int j0, const float (&v)[N])
+{
+    uint32_t n = 0, e = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int j = j0 + i;
+        const uint32_t key = weight_key(v[i]);
+        const bool fixed = j < q.lo || j >= q.hi;
+        n += j < q.L && (fixed || b.above(key));
+        e += j < q.L && !fixed && b.equal(key);
+    }
+    return (uint64_t)n << 32 | e;
+}
+
+template <int T>
+__device__ __forceinline__ void finish(const EvictArgs& a, const Kept& q, int sh, int moved, int* first_moved)
+{
+    if (moved < INT32_MAX) atomicMin(first_moved, moved);
+    int32_t* idx = a.kept_idx + (int64_t)sh * a.idx_stride;
+    const int cap = capacity(a.from);
+    for (int j = q.k + (int)threadIdx.x; j < cap; j += T) idx[j] = -1;
     __syncthreads();
-    if (tid == 0) a.info[sh] = EvictInfo{k, a.in_place ? first_moved : 0};
+    if (threadIdx.x == 0) a.info[sh] = EvictInfo{q.k, a.in_place ? *first_moved : 0};
+}
+
+template <int T>
+__global__ __launch_bounds__(T) void k_select(EvictArgs a)
+{
+    __shared__ __align__(16) uint32_t bins[kBins];
+    __shared__ uint64_t sums[T / kWave];
+    __shared__ int first_moved;
+    const int sh = blockIdx.x, tid = threadIdx.x, j0 = kSelItems * tid;
+    const Kept q(a, sh / a.from.kv_heads);
+    const float* w = a.from.weight + (int64_t)sh * a.from.weight_stride;
+    float v[kSelItems];
+#pragma unroll
+    for (int i = 0; i < kSelItems; ++i) v[i] = j0 + i < q.L ? w[j0 + i] : 0.0f;
+    for (int b = tid; b < kBins; b += T) bins[b] = 0;
+    if (tid == 0) first_moved = q.k;
+    Border border{0, 0, true};  // all stay
+    if (!q.all()) {
+        border = Border{q.take > 0 ? 0u : ~0u, 0, false};
+        uint32_t want = (uint32_t)max(q.take, 0);
+        auto count = [&](auto digit) {
+            constexpr int D = decltype(digit)::value;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kSelItems; ++i) {
+                const int j = j0 + i;
+                const uint32_t key = weight_key(v[i]);
+                if (j >= q.lo && j < q.hi && (D == 0 || key >> (kShift[D] + kWidth[D]) == border.least >> (kShift[D] + kWidth[D])))
+                    atomicAdd(&bins[first_bin(D) + (key >> kShift[D] & ((1u << kWidth[D]) - 1))], 1u);
+            }
+            __syncthreads();
+            return next_digit<D>(border, want, bins);
+        };
+        if (want > 0 && count(std::integral_constant<int, 0>()) && count(std::integral_constant<int, 1>()))
+            count(std::integral_constant<int, 2>());
+    }
+    uint64_t total;
+    const uint64_t before = block_scan<T / kWave>(count_kept(q, border, j0, v), sums, &total);
+    finish<T>(a, q, sh, put_kept(a, q, border, sh, j0, v, before), &first_moved);
+}
+
+// In place, a pass's weights are all in registers before any is written, and go to places
+// not past those already read.
+__global__ __launch_bounds__(kSelLong) void k_select_long(EvictArgs a)
+{
+    __shared__ __align__(16) uint32_t bins[kBins];
+    __shared__ uint64_t sums[kSelLong / kWave];
+    __shared__ int first_moved;
+    const int sh = blockIdx.x, tid = threadIdx.x;
+    const Kept q(a, sh / a.from.kv_heads);
+    const float* w = a.from.weight + (int64_t)sh * a.from.weight_stride;
+    for (int b = tid; b < kBins; b += kSelLong) bins[b] = 0;
+    if (tid == 0) first_moved = q.k;
+    Border border{0, 0, true};
+    if (!q.all()) {
+        border = Border{q.take > 0 ? 0u : ~0u, 0, false};
+        uint32_t want = (uint32_t)max(q.take, 0);
+        auto count = [&](auto digit) {
+            constexpr int D = decltype(digit)::value;
+            constexpr int U = 8;  // loads in flight
+            __syncthreads();
+            for (int i0 = q.lo + tid; i0 < q.hi; i0 += U * kSelLong) {
+                float v[U];
+#pragma unroll
+                for (int i = 0; i < U; ++i) v[i] = i0 + i * kSelLong < q.hi ? w[i0 + i * kSelLong] : 0.0f;
+#pragma unroll
+                for (int i = 0; i < U; ++i) {
+                    const uint32_t key = weight_key(v[i]);
+                    if (i0 + i * kSelLong < q.hi &&
+                        (D == 0 || key >> (kShift[D] + kWidth[D]) == border.least >> (kShift[D] + kWidth[D])))
+                        atomicAdd(&bins[first_bin(D) + (key >> kShift[D] & ((1u << kWidth[D]) - 1))], 1u);
+                }
+            }
+            __syncthreads();
+            return next_digit<D>(border, want, bins);
+        };
+        if (want > 0 && count(std::integral_constant<int, 0>()) && count(std::integral_constant<int, 1>()))
+            count(std::integral_constant<int, 2>());
+    }
+    uint64_t done = 0;  // of the passes before
+    int moved = INT32_MAX;
+    for (int p0 = 0; p0 < q.L; p0 += kSelItems * kSelLong) {
+        const int j0 = p0 + kSelItems * tid;
+        float v[kSelItems];
+#pragma unroll
+        for (int i = 0; i < kSelItems; ++i) v[i] = j0 + i < q.L ? w[j0 + i] : 0.0f;
+        uint64_t total;
+        const uint64_t before = block_scan<kSelLong / kWave>(count_kept(q, border, j0, v), sums, &total);
+        moved = min(moved, put_kept(a, q, border, sh, j0, v, done + before));
+        done += total;
+    }
+    finish<kSelLong>(a, q, sh, moved, &first_moved);
 }
 
 // The kept tokens' keys and values to their places. A block takes chunks of `kMoveRows`
@@ -466,7 +616,11 @@ int launch_append(const AppendArgs& a, void* st, void* e0, void* e1)
 
 int launch_select(const EvictArgs& a, void* st, void* e0, void* e1)
 {
-    return enqueue(k_select, (int64_t)a.from.n_seqs * a.from.kv_heads, kSelBlock, st, e0, e1, a);
+    const int64_t blocks = (int64_t)a.from.n_seqs * a.from.kv_heads, cap = capacity(a.from);
+    if (cap <= kSelItems * 256) return enqueue(k_select<256>, blocks, 256, st, e0, e1, a);
+    if (cap <= kSelItems * 512) return enqueue(k_select<512>, blocks, 512, st, e0, e1, a);
+    if (cap <= kSelTokens) return enqueue(k_select<1024>, blocks, 1024, st, e0, e1, a);
+    return enqueue(k_select_long, blocks, kSelLong, st, e0, e1, a);
 }
 
 int launch_move(const EvictArgs& a, void* st, void* e0, void* e1)
