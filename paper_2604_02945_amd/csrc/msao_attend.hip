@@ -593,6 +593,7 @@ __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
     constexpr int NI = 16 * CH / kWave;              // loads that bring 16 tokens
     __shared__ __align__(16) uint8_t lds_k[2][ST * RB], lds_v[2][ST * RB];
     __shared__ __align__(16) int lds_n[2][ST / 16];  // tokens that there are of each 16
+    __shared__ int lds_left_out;
 
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
     const int i16 = lane & 15, c = lane >> 4;
@@ -633,6 +634,8 @@ __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
         last[m] = a.causal ? p.length - p.n_new + row / a.group : p.length - 1;
     }
     const int least = a.causal ? p.length - p.n_new + w0 / a.group : p.length - 1;
+    const int least_of_all = a.causal ? p.length - p.n_new + r0 / a.group : p.length - 1;
+    if (threadIdx.x == 0) lds_left_out = 0;
     // tokens that the wavefront's own last row sees
     const int w_hi = used > 0 ? min(hi, group_sees(p.length, p.n_new, a.group, min(w0 + MT * 16, n_rows) - 1, a.causal)) : lo;
 
@@ -688,6 +691,28 @@ __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
         stage_came();
         __syncthreads();
         if (st + 1 < stages) bring(st + 1);
+        if (a.causal && !(lo + ST * st + ST <= hi && lo + ST * st + ST - 1 <= least_of_all)) {
+            // some row does not see all of the stage: what is not finite of its values stays out of
+            // the products (see k_attend). Each wavefront looks at the 16 tokens it brought
+            if (NW < kTasks || (wave >= ST / 16 && wave < kTasks)) {
+                uint8_t* mine = lds_v[st & 1] + half0 * 16 * RB + 16 * lane;
+                bool any = false;
+#pragma unroll
+                for (int n = 0; n < NI; ++n) {
+                    u32x4 w = *(const u32x4*)(mine + n * 1024);
+                    const bool bad = strange<kBF16>(w[0]) || strange<kBF16>(w[1]) || strange<kBF16>(w[2]) || strange<kBF16>(w[3]);
+                    any = any || bad;
+                    if (bad) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) w[e] = without_strange<kBF16>(w[e]);
+                        *(u32x4*)(mine + n * 1024) = w;
+                    }
+                }
+                if (any) lds_left_out = 1;
+            }
+            __syncthreads();
+            left_out = uniform(lds_left_out) != 0;
+        }
         int kn[ST / 16];
 #pragma unroll
         for (int w = 0; w < ST / 16; ++w) kn[w] = uniform(lds_n[st & 1][w]);
@@ -761,31 +786,22 @@ __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
                 }
                 return w;
             };
-            const bool careful = !seen_whole && a.causal;
-#pragma unroll
-            for (int t = 0; t < VT; ++t) {
-                u32x4 w = value(t);
-                if (careful) {  // (see k_attend)
-                    const bool any = strange<kBF16>(w[0]) || strange<kBF16>(w[1]) || strange<kBF16>(w[2]) || strange<kBF16>(w[3]);
-                    if (__ballot(any) != 0) {
-                        left_out = true;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) w[e] = without_strange<kBF16>(w[e]);
-                    }
-                }
+            auto add = [&](int t, const u32x4& w) {
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
                     o[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, pb[m]),
                                                                       o[m][t], 0, 0, 0);
-            }
+            };
+#pragma unroll
+            for (int t = 0; t < VT; ++t) add(t, value(t));
         }
     }
     if (left_out) {
 #pragma unroll 1
-        for (int tok = lo + max(0, least + 1 - lo) / kTile * kTile; tok < w_hi; tok += kTile) {
-            if (tok + kTile <= hi && tok + kTile - 1 <= least) continue;
+        for (int tok = lo + max(0, least_of_all + 1 - lo) / ST * ST; tok < w_hi; tok += ST) {
+            if (tok + ST <= hi && tok + ST - 1 <= least_of_all) continue;
 #pragma unroll 1
-            for (int t = tok; t < min(tok + kTile, hi); ++t) {
+            for (int t = tok; t < min(tok + ST, hi); ++t) {
                 const int page = page_at(a.c, p.seq, t >> a.c.page_shift);
                 if (page < 0) continue;
                 const uint8_t* src = vb + (int64_t)page * a.c.v_page + (int64_t)(t & mask) * a.c.v_tok;
