@@ -37,6 +37,7 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x3 __attribute__((ext_vector_type(3)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -67,16 +68,23 @@ template <int DT> struct Type;
 template <> struct Type<kBF16> { static constexpr int kSize = 2; };
 template <> struct Type<kF32> { static constexpr int kSize = 4; };
 
-// 32-bit words that hold E values, loaded in pieces of 16 or 8 bytes; AUX: cache policy.
+// 32-bit words that hold E values, loaded in pieces of 16, 12 or 8 bytes; AUX: cache policy.
 constexpr int kOnce = 2;  // nontemporal: read once
 template <int W, int AUX>
 __device__ __forceinline__ void load_words(uint32_t (&w)[W], rsrc_t r, int off)
 {
-    static_assert(W == 2 || W % 4 == 0, "");
-    if constexpr (W == 2) {
-        const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, AUX);
-        w[0] = v.x;
-        w[1] = v.y;
+    static_assert(W == 2 || W == 3 || W == 6 || W % 4 == 0, "");
+    if constexpr (W == 3) {
+        const u32x3 v = __builtin_amdgcn_raw_buffer_load_b96(r, off, 0, AUX);
+#pragma unroll
+        for (int e = 0; e < 3; ++e) w[e] = v[e];
+    } else if constexpr (W == 2 || W == 6) {
+#pragma unroll
+        for (int i = 0; i < W / 2; ++i) {
+            const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(r, off + 8 * i, 0, AUX);
+            w[2 * i] = v.x;
+            w[2 * i + 1] = v.y;
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < W / 4; ++i) {
@@ -92,6 +100,19 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
     const f32x2 v = {a, b};
     typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf2));
+}
+
+// N values to 8- or 16-byte aligned memory (4 bytes for two of bf16).
+template <int DT, int N>
+__device__ __forceinline__ void store_values(uint8_t* dst, const float* v)
+{
+    if constexpr (DT == kBF16) {
+        if constexpr (N == 4) *(u32x2*)dst = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        else *(uint32_t*)dst = pack_bf16(v[0], v[1]);
+    } else {
+        if constexpr (N == 4) *(f32x4*)dst = f32x4{v[0], v[1], v[2], v[3]};
+        else *(f32x2*)dst = f32x2{v[0], v[1]};
+    }
 }
 
 // Whether a 32-bit word of values holds an infinity or a NaN; and the word without them.
@@ -241,8 +262,9 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArg
     constexpr int KS = DP * ES / 64;   // pieces of a row of K a lane holds
     constexpr int E = DP / 16;         // channels of V a lane holds of a token
     constexpr int VW = E * ES / 4;     // as 32-bit words
-    // halves of a tile; of float32 heads of 128 and more the registers hold one
-    constexpr int NH = DT == kF32 && DP >= 128 ? 1 : 2, TT = 16 * NH;
+    constexpr int S = E % 4 == 0 ? 4 : 2;  // channels of a store
+    // halves of a tile; of float32 heads of 96 and more the registers hold one
+    constexpr int NH = DT == kF32 && DP >= 96 ? 1 : 2, TT = 16 * NH;
     constexpr int LDP = DP + 4;        // floats between rows in LDS: spreads the banks
     constexpr int TW = kWaves / RW;    // wavefronts that take different tiles
     // values that no other wavefront reads need no cache (long rows of one token: 176 -> 165 us);
@@ -533,15 +555,13 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArg
             if (parts <= 1) {
                 const float inv = l == 0.0f ? 0.0f : 1.0f / l;
                 uint8_t* dst = a.out + (int64_t)(p.begin + tok) * a.out_stride + ((int64_t)head * a.c.dim + od) * ES;
-                // (the head's last channels may be half of what the thread has)
+                // (the head's last channels may be part of what the thread has)
 #pragma unroll
-                for (int t = 0; t < E; t += 4) {
+                for (int t = 0; t < E; t += S) {
                     if (od + t >= a.c.dim) break;
-                    if constexpr (DT == kBF16)
-                        *(u32x2*)(dst + 2 * t) =
-                            u32x2{pack_bf16(acc[t] * inv, acc[t + 1] * inv), pack_bf16(acc[t + 2] * inv, acc[t + 3] * inv)};
-                    else
-                        *(f32x4*)(dst + 4 * t) = f32x4{acc[t] * inv, acc[t + 1] * inv, acc[t + 2] * inv, acc[t + 3] * inv};
+#pragma unroll
+                    for (int e = 0; e < S; ++e) acc[t + e] *= inv;
+                    store_values<DT, S>(dst + ES * t, &acc[t]);
                 }
                 if (od == 0) {
                     const float z = l == 0.0f ? -INFINITY : mm + __builtin_amdgcn_logf(l);
@@ -552,8 +572,8 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArg
                 const int64_t all = (int64_t)a.ch.n_rows * a.heads;
                 float* po = a.part_o + (split * all + at) * a.c.dim + od;
 #pragma unroll
-                for (int t = 0; t < E; t += 4)
-                    if (od + t < a.c.dim) *(f32x4*)(po + t) = f32x4{acc[t], acc[t + 1], acc[t + 2], acc[t + 3]};
+                for (int t = 0; t < E; t += S)
+                    if (od + t < a.c.dim) store_values<kF32, S>((uint8_t*)(po + t), &acc[t]);
                 if (od == 0) *(f32x2*)(a.part_ml + 2 * (split * all + at)) = f32x2{mm, l};
             }
         }
@@ -589,7 +609,7 @@ template <int DP, int MT, int NW, int ST, int WPS>
 __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
 {
     constexpr int KS = DP / 32, VT = DP / 16;        // steps of a score; tiles of channels
-    constexpr int CH = DP / 8, RB = DP * 2;          // 16-byte pieces of a row in LDS; its bytes
+    constexpr int CH = DP == 64 ? 8 : 16, RB = 16 * CH;  // 16-byte pieces of a row in LDS; its bytes
     constexpr int NI = 16 * CH / kWave;              // loads that bring 16 tokens
     __shared__ __align__(16) uint8_t lds_k[2][ST * RB], lds_v[2][ST * RB];
     __shared__ __align__(16) int lds_n[2][ST / 16];  // tokens that there are of each 16
@@ -862,7 +882,7 @@ template <int DT, int DP, int W>
 __global__ __launch_bounds__(kBlock) void k_combine(AttendArgs a, int blocks_per)
 {
     constexpr int ES = Type<DT>::kSize;
-    constexpr int LP = DP / 4, kGroups = W * kWave / LP, kFly = 4;
+    constexpr int LP = DP == 96 ? 32 : DP / 4, kGroups = W * kWave / LP, kFly = 4;
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
     const int sh = blockIdx.x / blocks_per;
     const Place p = place_of(a, sh);
@@ -1188,7 +1208,7 @@ int enqueue(K kernel, int64_t blocks, void* stream, void* ev0, void* ev1, A... a
     return (int)hipGetLastError();
 }
 
-int padded_dim(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
+int padded_dim(int dim) { return dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 128 : 256; }
 
 int64_t pairs(const AttendArgs& a) { return (int64_t)a.c.n_seqs * a.c.kv_heads; }
 
@@ -1238,10 +1258,10 @@ int by_type(const AttendArgs& a, void* st, void* e0, void* e1)
 {
     const int dp = padded_dim(a.c.dim);
     if (a.dtype == kBF16)
-        return dp == 64 ? F<kBF16, 64>::go(a, st, e0, e1) : dp == 128 ? F<kBF16, 128>::go(a, st, e0, e1)
-                                                                      : F<kBF16, 256>::go(a, st, e0, e1);
-    return dp == 64 ? F<kF32, 64>::go(a, st, e0, e1) : dp == 128 ? F<kF32, 128>::go(a, st, e0, e1)
-                                                                 : F<kF32, 256>::go(a, st, e0, e1);
+        return dp == 64 ? F<kBF16, 64>::go(a, st, e0, e1) : dp == 96 ? F<kBF16, 96>::go(a, st, e0, e1)
+             : dp == 128 ? F<kBF16, 128>::go(a, st, e0, e1) : F<kBF16, 256>::go(a, st, e0, e1);
+    return dp == 64 ? F<kF32, 64>::go(a, st, e0, e1) : dp == 96 ? F<kF32, 96>::go(a, st, e0, e1)
+         : dp == 128 ? F<kF32, 128>::go(a, st, e0, e1) : F<kF32, 256>::go(a, st, e0, e1);
 }
 template <int DT, int DP> struct Attend {
     static int go(const AttendArgs& a, void* st, void* e0, void* e1) { return attend_rows<DT, DP>(a, st, e0, e1); }

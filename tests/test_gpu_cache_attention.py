@@ -73,6 +73,13 @@ def test_long_rows_are_split_and_joined(dtype):
     check(Case(5, [9000, 3, 4097, 2048], [2, 1, 5, 1], 4, 1, 128, 64, dtype))
 
 
+@pytest.mark.parametrize("dim", [16, 24, 40, 56, 80, 88, 104, 120, 168, 248])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_dims_between_the_padded_ones(dtype, dim):
+    """The last channels of the last token end inside a lane's piece of a row."""
+    check(Case(13, [48, 17, 150], [2, 1, 40], 6, 2, dim, 16, dtype, spare_pages=0))
+
+
 @pytest.mark.parametrize("order", ["token", "mixed"])
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
 def test_pool_layouts(order, dtype):
