@@ -73,6 +73,9 @@ msao_status check_cache(const msao_kv_cache* cache, std::string* err)
     return MSAO_OK;
 }
 
+// Whether the cache can hold a token at all (an array of none may be NULL).
+bool has_tokens(const msao_kv_cache& c) { return c.n_seqs > 0 && c.pages_per_seq > 0; }
+
 msao_status check_chunk(const msao_chunk* ch, const msao_kv_cache& c, std::string* err)
 {
     if (!ch) return bad(err, "chunk is NULL");
@@ -184,7 +187,7 @@ msao_status attend_plan(const msao_kv_cache* cache, const msao_chunk* chunk, int
     MSAO_TRY(check_chunk(chunk, *cache, err));
     MSAO_TRY(check_heads(heads, *cache, *chunk, err));
     if (flags & ~(MSAO_ATTEND_CAUSAL | MSAO_ATTEND_WEIGHT)) return bad(err, "unknown flag bits");
-    if ((flags & MSAO_ATTEND_WEIGHT) && !cache->weight) return bad(err, "the cache has no weight to add to");
+    if ((flags & MSAO_ATTEND_WEIGHT) && !cache->weight && has_tokens(*cache)) return bad(err, "the cache has no weight to add to");
     AttendArgs& a = pl.a;
     std::memset(&a, 0, sizeof a);
     a.c = cache_dev(*cache);
@@ -358,7 +361,7 @@ msao_status msao_cache_evict(msao_ctx* ctx, const msao_kv_cache* from, const msa
     return guarded([&]() -> msao_status {
         std::string* err = ctx ? &ctx->err : &g_err;
         MSAO_TRY(check_cache(from, err));
-        if (!from->weight) return bad(err, "the cache has no weight to evict by");
+        if (!from->weight && has_tokens(*from)) return bad(err, "the cache has no weight to evict by");
         const msao_kv_cache& dst = to ? *to : *from;
         if (to) {
             MSAO_TRY(check_cache(to, err));
