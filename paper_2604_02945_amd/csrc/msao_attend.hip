@@ -964,7 +964,10 @@ __global__ __launch_bounds__(kBlock) void k_combine(AttendArgs a, int blocks_per
 // Lane (c, q) sums tokens 4c + r over its rows, and 16 lanes are added at the end. Every
 // token has one wavefront, so no atomics, and the order of the sum is fixed.
 //
-// Few rows (k_weight): K streams by as in k_attend, past the queries in LDS.
+// Few rows (k_weight): K streams by, 16 tokens a wavefront, past the queries in LDS. HBM
+// bound; 60 registers leave eight wavefronts on a SIMD, which is what hides the loads (32
+// tokens in 94 registers: 100 us for attend_round's 383 MB against 91; two sets of registers
+// in turn 112).
 template <int DT, int DP, int MT>
 __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight(AttendArgs a)
 {
@@ -996,64 +999,48 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight(AttendArg
         last[m] = a.causal ? p.length - p.n_new + tok : p.length - 1;
     }
     const int least = a.causal ? p.length - p.n_new : p.length - 1;
-    const int tiles = (hi - lo + kTile - 1) / kTile, mine = tiles > wave ? (tiles - wave + kWaves - 1) / kWaves : 0;
-    u32x4 kf[2][KS];
-    float old[8];
-    int kn[2], next_n[2];
-    int pages = lane_pages<2>(a.c, p.seq, lo, hi, wave, kWaves, 0);
+    const int tiles = (hi - lo + 15) / 16, mine = tiles > wave ? (tiles - wave + kWaves - 1) / kWaves : 0;
+    u32x4 kf[KS];
+    int n = 0, next_n = 0;
+    int pages = lane_pages<1>(a.c, p.seq, lo, hi, wave, kWaves, 0);
     auto load_k = [&](int it) {
-        const int tok = lo + kTile * (wave + kWaves * it);
+        const int page = __builtin_amdgcn_readlane(pages, it & 63);
+        const Half f = half_of(kb, a.c.k_page, a.c.k_tok, row_bytes, page, lo + 16 * (wave + kWaves * it), hi, mask);
+        next_n = f.n;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int page = __builtin_amdgcn_readlane(pages, (2 * it + h) & 63);
-            const Half f = half_of(kb, a.c.k_page, a.c.k_tok, row_bytes, page, tok + 16 * h, hi, mask);
-            next_n[h] = f.n;
-#pragma unroll
-            for (int s = 0; s < KS; ++s) kf[h][s] = __builtin_amdgcn_raw_buffer_load_b128(f.r, ko.off[s], 0, kOnce);
-        }
+        for (int s = 0; s < KS; ++s) kf[s] = __builtin_amdgcn_raw_buffer_load_b128(f.r, ko.off[s], 0, kOnce);
     };
     if (mine > 0) load_k(0);
     __syncthreads();
     for (int it = 0; it < mine; ++it) {
-        const int tok = lo + kTile * (wave + kWaves * it);
-        bool whole = tok + kTile - 1 <= least;
+        const int tok = lo + 16 * (wave + kWaves * it) + 4 * c;  // the lane's first token
+        n = next_n;
+        const bool whole = n == 16 && tok - 4 * c + 15 <= least;
+        float old[4], w[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            kn[h] = next_n[h];
-            whole = whole && kn[h] == 16;
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                old[4 * h + r] = i16 == 0 && 4 * c + r < kn[h] ? weight[tok + 16 * h + 4 * c + r] : 0.0f;
-        }
-        float w[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        for (int r = 0; r < 4; ++r) old[r] = i16 == 0 && 4 * c + r < n ? weight[tok + r] : 0.0f;
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             if (m >= used) break;
             Queries<DT, DP> q;
             q.take(lds, 16 * m);
+            const f32x4 s = scores<DT, DP>(kf, q);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const f32x4 s = scores<DT, DP>(kf[h], q);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int j = 4 * c + r;
-                    const float x = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale, -z[m]));
-                    w[4 * h + r] += whole || (j < kn[h] && tok + 16 * h + j <= last[m]) ? x : 0.0f;
-                }
+            for (int r = 0; r < 4; ++r) {
+                const float x = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale, -z[m]));
+                w[r] += whole || (4 * c + r < n && tok + r <= last[m]) ? x : 0.0f;
             }
         }
         if (it + 1 < mine) {
-            if (((it + 1) & 31) == 0) pages = lane_pages<2>(a.c, p.seq, lo, hi, wave, kWaves, it + 1);
+            if (((it + 1) & 63) == 0) pages = lane_pages<1>(a.c, p.seq, lo, hi, wave, kWaves, it + 1);
             load_k(it + 1);
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = row_sum(w[e]);
+        for (int r = 0; r < 4; ++r) w[r] = row_sum(w[r]);
         if (i16 == 0) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (4 * c + r < kn[h]) weight[tok + 16 * h + 4 * c + r] = old[4 * h + r] + w[4 * h + r];
+            for (int r = 0; r < 4; ++r)
+                if (4 * c + r < n) weight[tok + r] = old[r] + w[r];
         }
     }
 }
@@ -1283,9 +1270,9 @@ template <int DT, int DP> struct Weight {
 // parts for kManyTarget, or as many as for few rows with float32, whose products take eight
 // times as long (text over encoder states 70 us, 103 with parts for 512).
 constexpr int64_t kPartTarget = 2048, kPartLeast = 128, kPartMost = 1024, kManyTarget = 1024, kManyTargetF32 = 4096;
-// Parts of the tokens in the weight pass of few rows (attend_round's 98 us; 112 with 4,096,
-// 105 with 16,384), and of the rows in that of many: up to 32 (25 us, 33 with 10).
-constexpr int64_t kWeightTarget = 8192, kWeightRowTarget = 8192, kMostRowParts = 32;
+// Parts of the tokens in the weight pass of few rows (attend_round 91 us; 93 with 8,192), and
+// of the rows in that of many: up to 32 (25 us, 33 with 10).
+constexpr int64_t kWeightTarget = 16384, kWeightRowTarget = 8192, kMostRowParts = 32;
 void attend_shape(AttendArgs& a)
 {
     const int64_t rows = (int64_t)a.ch.max_new * a.group;
