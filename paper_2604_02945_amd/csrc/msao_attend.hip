@@ -27,6 +27,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "msao_cache.h"
 #include "msao_device.h"
@@ -1019,18 +1020,23 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight(AttendArg
         float old[4], w[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int r = 0; r < 4; ++r) old[r] = i16 == 0 && 4 * c + r < n ? weight[tok + r] : 0.0f;
+        auto add = [&](auto all_seen) {
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            if (m >= used) break;
-            Queries<DT, DP> q;
-            q.take(lds, 16 * m);
-            const f32x4 s = scores<DT, DP>(kf, q);
+            for (int m = 0; m < MT; ++m) {
+                if (m >= used) break;
+                Queries<DT, DP> q;
+                q.take(lds, 16 * m);
+                const f32x4 s = scores<DT, DP>(kf, q);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float x = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale, -z[m]));
-                w[r] += whole || (4 * c + r < n && tok + r <= last[m]) ? x : 0.0f;
+                for (int r = 0; r < 4; ++r) {
+                    const float x = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale, -z[m]));
+                    if (decltype(all_seen)::value) w[r] += x;
+                    else w[r] += 4 * c + r < n && tok + r <= last[m] ? x : 0.0f;
+                }
             }
-        }
+        };
+        if (whole) add(std::true_type());
+        else add(std::false_type());
         if (it + 1 < mine) {
             if (((it + 1) & 63) == 0) pages = lane_pages<1>(a.c, p.seq, lo, hi, wave, kWaves, it + 1);
             load_k(it + 1);
@@ -1050,7 +1056,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight(AttendArg
 // block's tokens are cut into row_parts parts, so that a few short prompts fill the
 // device too; k_weight_join adds the parts' sums in order.
 constexpr int kRowStep = 64;
-constexpr int row_step(int dt, int dp) { return dt == kF32 && dp == 256 ? 32 : kRowStep; }  // registers
+constexpr int row_step(int dt, int dp) { return dt == kF32 && dp == 256 ? 16 : kRowStep; }  // registers
 template <int DT, int DP>
 __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight_rows(AttendArgs a)
 {
@@ -1123,23 +1129,28 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight_rows(Atte
         const int r0 = from + step * kStep;
         const int least = a.causal ? p.length - p.n_new + r0 / a.group : p.length - 1;
         const bool whole = kn[0] == 16 && kn[1] == 16 && tok + kTile - 1 <= least;
+        auto add = [&](auto all_seen) {
 #pragma unroll
-        for (int m = 0; m < kStep / 16; ++m) {
-            Q q;
-            q.take(lds, 16 * m);
-            const float z = lds_z[16 * m + i16];
-            const int last = lds_last[16 * m + i16];
+            for (int m = 0; m < kStep / 16; ++m) {
+                Q q;
+                q.take(lds, 16 * m);
+                const float z = lds_z[16 * m + i16];
+                const int last = lds_last[16 * m + i16];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const f32x4 s = scores<DT, DP>(kf[h], q);
+                for (int h = 0; h < 2; ++h) {
+                    const f32x4 s = scores<DT, DP>(kf[h], q);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int j = 4 * c + r;
-                    const float x = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale, -z));
-                    w[4 * h + r] += whole || (j < kn[h] && tok + 16 * h + j <= last) ? x : 0.0f;
+                    for (int r = 0; r < 4; ++r) {
+                        const int j = 4 * c + r;
+                        const float x = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale, -z));
+                        if (decltype(all_seen)::value) w[4 * h + r] += x;
+                        else w[4 * h + r] += j < kn[h] && tok + 16 * h + j <= last ? x : 0.0f;
+                    }
                 }
             }
-        }
+        };
+        if (whole) add(std::true_type());
+        else add(std::false_type());
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) w[e] = row_sum(w[e]);
@@ -1211,7 +1222,7 @@ int attend_rows(const AttendArgs& a, void* st, void* e0, void* e1)
     const int64_t blocks = pairs(a) * a.row_tiles * a.splits;
     if (a.tile_rows == 16) return enqueue(k_attend<DT, DP, 1, 1>, blocks, st, e0, e1, a);
     if constexpr (DT == kBF16 && DP <= 128)
-        if (a.tile_rows == kManyRows) return enqueue(k_attend_rows<DP, kRowTiles, kWaves, kStageTokens, 2>, blocks, st, e0, e1, a);
+        if (a.tile_rows == kManyRows) return enqueue(k_attend_rows<DP, kRowTiles, kWaves, kStageTokens, DP == 64 ? 3 : 2>, blocks, st, e0, e1, a);
     if constexpr (DP == 256) {
         if (a.tile_rows == 32) return enqueue(k_attend<DT, DP, 1, 2>, blocks, st, e0, e1, a);
     } else {
