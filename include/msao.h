@@ -516,8 +516,9 @@ typedef struct {
  * (row start[s] + i is its token length[s] - n + i with n = start[s+1] -
  * start[s]). start is device memory, ascending; entries are taken into [0,
  * n_rows], a sequence whose end lies before its start has no rows. Rows of no
- * sequence are left as they are. max_new: host's bound on n; of a sequence with
- * more rows msao_cache_attention leaves those from max_new on as they are. */
+ * sequence are left as they are. max_new: the host's bound on n (more than n_rows
+ * counts as n_rows); of a sequence with more rows msao_cache_attention leaves
+ * those from max_new on as they are. */
 typedef struct {
     const int32_t* start;      /* device [n_seqs + 1] */
     int32_t n_rows;            /* rows of the step's arrays */
@@ -535,7 +536,8 @@ msao_status msao_cache_validate(const msao_kv_cache* cache, const msao_chunk* ch
 /* What msao_cache_append takes besides the cache. Rows are of the cache's dtype;
  * the heads of a row follow one another (head h at h * head_dim), strides are in
  * elements between rows. Pointers and strides are multiples of 16 bytes.
- *   q -> q_out [n_rows][heads * head_dim]: may be the same memory; NULL with heads 0.
+ *   q -> q_out [n_rows][heads * head_dim]: the same pointer and stride, or memory apart;
+ *     NULL with heads 0.
  *   k, v [n_rows][kv_heads * head_dim].
  *   q_norm, k_norm [head_dim] or NULL: a head x becomes x / sqrt(mean(x^2) + eps) * norm.
  *   Then the first rot_dim values (a multiple of 16, at most head_dim; 0: none) turn

@@ -800,7 +800,8 @@ class KvCache:
         c = self.struct = MsaoKvCache()
         c.k, c.v = (k.data_ptr(), v.data_ptr()) if k.numel() else (None, None)
         for i in range(3):
-            c.k_stride[i], c.v_stride[i] = k.stride(i), v.stride(i)
+            # (the only page or head is at no distance, whatever torch says)
+            c.k_stride[i], c.v_stride[i] = (k.stride(i), v.stride(i)) if k.shape[i] > 1 else (0, 0)
         c.dtype = F32 if k.dtype == torch.float32 else BF16
         c.head_dim, c.kv_heads, c.page_size, c.n_pages = self.head_dim, self.kv_heads, self.page_size, self.n_pages
         c.n_seqs, c.pages_per_seq = n_seqs, self.pages_per_seq

@@ -610,7 +610,7 @@ template <int DP, int MT, int NW, int ST, int WPS>
 __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
 {
     constexpr int KS = DP / 32, VT = DP / 16;        // steps of a score; tiles of channels
-    constexpr int CH = DP == 64 ? 8 : 16, RB = 16 * CH;  // 16-byte pieces of a row in LDS; its bytes
+    constexpr int CH = DP == 64 ? 8 : DP == 256 ? 32 : 16, RB = 16 * CH;  // 16-byte pieces of a row in LDS; its bytes
     constexpr int NI = 16 * CH / kWave;              // loads that bring 16 tokens
     __shared__ __align__(16) uint8_t lds_k[2][ST * RB], lds_v[2][ST * RB];
     __shared__ __align__(16) int lds_n[2][ST / 16];  // tokens that there are of each 16
@@ -1214,15 +1214,20 @@ int64_t pairs(const AttendArgs& a) { return (int64_t)a.c.n_seqs * a.c.kv_heads; 
 // over 12,288 tokens: 730 us; 48 rows a wavefront 884 (246 registers, as fast a SIMD but fewer
 // workgroups), 64 spill; 16 rows and eight wavefronts 770; stages of 32 tokens 852. With fewer
 // than kManyRows rows its wavefronts would be idle or its tokens not spread: k_attend.
-constexpr int kRowTiles = 2, kStageTokens = 64, kManyRows = kRowTiles * 16 * kWaves;
+// Heads of 256: 16 rows a wavefront and stages of 32, for the same registers and LDS (the
+// same chunks 1.70 ms, 6.26 through k_attend).
+constexpr int kManyRows = 128;
+constexpr int row_tiles_of(int dp) { return dp == 256 ? 1 : 2; }
+constexpr int stage_of(int dp) { return dp == 256 ? 32 : 64; }
+constexpr int many_rows(int dp) { return row_tiles_of(dp) * 16 * kWaves; }
 // Rows of a workgroup: what the registers of its wavefronts hold.
 template <int DT, int DP>
 int attend_rows(const AttendArgs& a, void* st, void* e0, void* e1)
 {
     const int64_t blocks = pairs(a) * a.row_tiles * a.splits;
     if (a.tile_rows == 16) return enqueue(k_attend<DT, DP, 1, 1>, blocks, st, e0, e1, a);
-    if constexpr (DT == kBF16 && DP <= 128)
-        if (a.tile_rows == kManyRows) return enqueue(k_attend_rows<DP, kRowTiles, kWaves, kStageTokens, DP == 64 ? 3 : 2>, blocks, st, e0, e1, a);
+    if constexpr (DT == kBF16)
+        if (a.many) return enqueue(k_attend_rows<DP, row_tiles_of(DP), kWaves, stage_of(DP), DP == 64 ? 3 : 2>, blocks, st, e0, e1, a);
     if constexpr (DP == 256) {
         if (a.tile_rows == 32) return enqueue(k_attend<DT, DP, 1, 2>, blocks, st, e0, e1, a);
     } else {
@@ -1287,9 +1292,10 @@ constexpr int64_t kWeightTarget = 16384, kWeightRowTarget = 8192, kMostRowParts 
 void attend_shape(AttendArgs& a)
 {
     const int64_t rows = (int64_t)a.ch.max_new * a.group;
-    const int most = padded_dim(a.c.dim) == 256 ? 32 : 64;  // rows of a workgroup at most
+    const int most = padded_dim(a.c.dim) == 256 ? 32 : 64;  // rows of a workgroup of k_attend at most
     a.tile_rows = rows <= 16 ? 16 : rows <= 32 || most == 32 ? 32 : 64;
-    if (a.dtype == kBF16 && most == 64 && rows >= kManyRows) a.tile_rows = kManyRows;
+    a.many = a.dtype == kBF16 && rows >= kManyRows;
+    if (a.many) a.tile_rows = many_rows(padded_dim(a.c.dim));
     a.row_tiles = (int)((rows + a.tile_rows - 1) / a.tile_rows);
     const int64_t np = std::max<int64_t>(pairs(a), 1), groups = std::max<int64_t>(np * a.row_tiles, 1), cap = capacity(a.c);
     auto up = [](int64_t v, int64_t to) { return (v + to - 1) / to * to; };

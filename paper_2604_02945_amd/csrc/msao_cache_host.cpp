@@ -18,7 +18,7 @@ namespace {
 
 constexpr int64_t kMaxCapacity = (int64_t)1 << 29;
 constexpr int64_t kMaxTokBytes = (int64_t)1 << 26;  // 16 tokens are one buffer
-constexpr int64_t kMaxBlocks = INT32_MAX;
+constexpr int64_t kMaxBlocks = (1 << 24) - 1;        // of 256 threads: a launch has fewer than 2^32
 constexpr int64_t kMaxStride = (int64_t)1 << 40;    // elements; products with 31-bit counts stay in 63 bits with 2^10 pages to spare
 
 // A call that the C ABI must not leave by an exception.
@@ -80,7 +80,7 @@ msao_status check_chunk(const msao_chunk* ch, const msao_kv_cache& c, std::strin
 {
     if (!ch) return bad(err, "chunk is NULL");
     if (ch->n_rows < 0) return bad(err, "n_rows is negative");
-    if (ch->max_new < 0 || ch->max_new > ch->n_rows) return bad(err, "max_new must be in 0 .. n_rows");
+    if (ch->max_new < 0) return bad(err, "max_new is negative");
     if (c.n_seqs > 0 && !ch->start) return bad(err, "start is NULL");
     if (!aligned(ch->start, 4)) return fail(err, MSAO_ERR_ALIGNMENT, "start is not 4-byte aligned");
     return MSAO_OK;
@@ -173,7 +173,7 @@ CacheDev cache_dev(const msao_kv_cache& c)
     return d;
 }
 
-ChunkDev chunk_dev(const msao_chunk& ch) { return ChunkDev{ch.start, ch.n_rows, ch.max_new}; }
+ChunkDev chunk_dev(const msao_chunk& ch) { return ChunkDev{ch.start, ch.n_rows, std::min(ch.max_new, ch.n_rows)}; }
 
 // The launch shape and the workspace of an attention call.
 struct AttendPlan {
@@ -199,7 +199,7 @@ msao_status attend_plan(const msao_kv_cache* cache, const msao_chunk* chunk, int
     a.add_weight = flags & MSAO_ATTEND_WEIGHT ? 1 : 0;
     attend_shape(a);
     const int64_t groups = (int64_t)a.c.n_seqs * a.c.kv_heads;
-    const int64_t most = std::max<int64_t>(std::max<int64_t>((int64_t)a.row_tiles * a.splits, (int64_t)chunk->max_new * a.group),
+    const int64_t most = std::max<int64_t>(std::max<int64_t>((int64_t)a.row_tiles * a.splits, (int64_t)a.ch.max_new * a.group),
                                            std::max<int64_t>((int64_t)a.weight_parts * a.row_parts, a.c.per_seq * (int64_t)cache->page_size / 256 + 1));
     if (groups > 0 && most > kMaxBlocks / groups) return fail(err, MSAO_ERR_UNSUPPORTED, "more workgroups than one launch takes");
     const AttendBytes b = attend_bytes(a);
@@ -285,6 +285,7 @@ msao_status msao_cache_append(msao_ctx* ctx, const msao_kv_cache* cache, const m
         }
         a.dtype = cache->dtype;
         append_shape(a);
+        if ((int64_t)a.ch.n_rows * a.parts > 4 * kMaxBlocks) return fail(err, MSAO_ERR_UNSUPPORTED, "more workgroups than one launch takes");
         DeviceGuard guard(ctx->device);
         return cache_launch(ctx, MSAO_CACHE_KERNEL_APPEND, stream, run_append, &a);
     });
@@ -393,7 +394,8 @@ msao_status msao_cache_evict(msao_ctx* ctx, const msao_kv_cache* from, const msa
         a.dtype = from->dtype;
         evict_shape(a);
         const int64_t groups = (int64_t)from->n_seqs * from->kv_heads * 2 * a.col_parts;
-        if (groups > kMaxBlocks / std::max(a.blocks, 1)) return fail(err, MSAO_ERR_UNSUPPORTED, "more workgroups than one launch takes");
+        // (the selection's workgroups have up to four times as many threads)
+        if (groups > kMaxBlocks / std::max(a.blocks, 4)) return fail(err, MSAO_ERR_UNSUPPORTED, "more workgroups than one launch takes");
         size_t need = 0;
         MSAO_TRY(msao_cache_evict_workspace(from, &need));
         MSAO_TRY(check_workspace(workspace, workspace_bytes, need, err));

@@ -56,6 +56,15 @@ def test_heads_dims_and_pages(dtype, causal, heads, kv_heads, dim, page):
     check(Case(2, [130, 7, 0, 33, 1, 500], [3, 7, 0, 1, 1, 6], heads, kv_heads, dim, page, dtype, extra_rows=3), causal)
 
 
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "all"])
+@pytest.mark.parametrize("heads,kv_heads,dim,page", [(6, 1, 64, 16), (4, 2, 88, 32), (3, 1, 128, 64), (2, 1, 256, 16), (4, 2, 176, 32)])
+def test_many_rows_with_holes_and_tails(heads, kv_heads, dim, page, causal):
+    """128 rows and more, in one workgroup and over several; a page that is none; odd lengths."""
+    check(Case(14, [333, 150, 64, 130, 40], [101, 150, 64, 3, 40], heads, kv_heads, dim, page, BF16, bad_page=(0, 1, -1),
+               extra_rows=2), causal)
+    check(Case(15, [700, 30], [70, 9], heads, kv_heads, dim, page, BF16, bad_page=(0, 2, 10 ** 6)), causal, scale=-0.2)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("new,length", [(1, 1), (2, 2), (17, 17), (40, 300), (70, 70), (130, 150), (257, 700)])
 def test_chunks_of_prompts(dtype, new, length):
@@ -146,7 +155,7 @@ def test_queries_beside_keys_and_values_in_one_projection():
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")], ids=str)
-@pytest.mark.parametrize("dim,heads", [(128, 4), (64, 14), (256, 2)])
+@pytest.mark.parametrize("dim,heads", [(128, 4), (64, 14), (256, 2), (96, 34), (128, 36), (256, 32)])
 @pytest.mark.parametrize("at", ["k", "v", "both"])
 def test_what_a_row_does_not_see_has_no_effect(dtype, value, dim, heads, at):
     """Token L - n + bad holds no finite value: rows before it are as without it, rows from it on

@@ -124,3 +124,44 @@ def test_pages_of_none(bad):
     to = target(case, 8)
     to.pages[0, 1] = bad
     check(case, [70, 40], 2, 5, to)
+
+
+def test_other_pages_of_the_same_pool():
+    """Pages of one pool, free ones as the target: the caches share k and v, not a page."""
+    import paper_2604_02945_amd as msao
+    case = Case(38, [300, 77], [0, 0], 2, 2, 64, 16, BF16, spare_pages=40)
+    cache, _ = case.device(DEV)
+    free = torch.tensor(sorted(set(range(case.n_pages)) - set(case.pages[case.pages >= 0].tolist())), dtype=torch.int32)
+    to = msao.KvCache(cache.k, cache.v, free[:20].view(2, 10).to(DEV), torch.zeros(2, dtype=torch.int32, device=DEV),
+                      torch.zeros(2, 2, 160, device=DEV))
+    want = []
+    src_k, src_v = cache.k.clone(), cache.v.clone()
+    r = msao.msao_cache_evict(cache, torch.tensor([150, 40], dtype=torch.int32, device=DEV), 1, 4, to=to)
+    torch.cuda.synchronize()
+    for b in range(2):
+        for h in range(2):
+            kept = evicted(case.weight[b, h].numpy(), case.lengths[b], [150, 40][b], 160, 1, 4)
+            assert np.array_equal(r["kept_idx"][b, h, :len(kept)].cpu().numpy(), kept)
+            for j, t in enumerate(kept):
+                a, p = int(free[10 * b + j // 16]), case.pages[b, t // 16]
+                want.append((a, h, j % 16))
+                assert torch.equal(cache.k[a, h, j % 16], src_k[p, h, t % 16])
+                assert torch.equal(cache.v[a, h, j % 16], src_v[p, h, t % 16])
+    mask = torch.ones(cache.k.shape[:3], dtype=torch.bool)
+    for a, h, j in want:
+        mask[a, h, j] = False
+    bits = lambda x: x.view(torch.int16)[mask.to(DEV)]  # noqa: E731
+    assert torch.equal(bits(cache.k), bits(src_k)) and torch.equal(bits(cache.v), bits(src_v))
+
+
+def test_the_only_head_and_page_at_odd_strides():
+    """Dimensions of one element have any stride; they are at no distance."""
+    import paper_2604_02945_amd as msao
+    base = torch.randn(16 * 64 + 64, device=DEV).to(BF16)
+    k = torch.as_strided(base, (1, 1, 16, 64), (3, 5, 64, 1))
+    cache = msao.KvCache(k, k.clone().contiguous(), torch.zeros(1, 1, dtype=torch.int32, device=DEV),
+                         torch.tensor([16], dtype=torch.int32, device=DEV), torch.rand(1, 1, 16, device=DEV))
+    before = k.clone()
+    r = msao.msao_cache_evict(cache, torch.tensor([5], dtype=torch.int32, device=DEV))
+    idx = r["kept_idx"][0, 0, :5].long()
+    assert torch.equal(k[0, 0, :5], before[0, 0, idx])
