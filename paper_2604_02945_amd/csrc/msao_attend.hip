@@ -1288,7 +1288,7 @@ template <int DT, int DP> struct Weight {
 constexpr int64_t kPartTarget = 2048, kPartLeast = 128, kPartMost = 1024, kManyTarget = 1024, kManyTargetF32 = 4096;
 // Parts of the tokens in the weight pass of few rows (attend_round 91 us; 93 with 8,192), and
 // of the rows in that of many: up to 32 (25 us, 33 with 10).
-constexpr int64_t kWeightTarget = 16384, kWeightRowTarget = 8192, kMostRowParts = 32;
+constexpr int64_t kWeightTarget = 16384, kWeightLeast = 256, kWeightRowTarget = 8192, kMostRowParts = 32;
 void attend_shape(AttendArgs& a)
 {
     const int64_t rows = (int64_t)a.ch.max_new * a.group;
@@ -1315,7 +1315,7 @@ void attend_shape(AttendArgs& a)
         const int64_t steps = (rows + kRowStep - 1) / kRowStep;
         a.row_parts = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(steps, kMostRowParts), kWeightRowTarget / (np * a.weight_parts)));
     } else {
-        a.weight_tokens = (int)std::min<int64_t>(std::max<int64_t>(up((np * cap + kWeightTarget - 1) / kWeightTarget, kPartLeast), kPartLeast), whole);
+        a.weight_tokens = (int)std::min<int64_t>(std::max<int64_t>(up((np * cap + kWeightTarget - 1) / kWeightTarget, kWeightLeast), kWeightLeast), whole);
         a.weight_parts = std::max(1, parts_of((int)cap, a.weight_tokens));
     }
 }

@@ -263,12 +263,15 @@ __global__ __launch_bounds__(kBlock) void k_append(AppendArgs a)
 
 // The tokens that stay of one (sequence, kv head), by one workgroup: the key of the last
 // ranked one by digits of 11, 10 and 10 bits (the sign is 0), counted in LDS, then the kept
-// indices and weights in one ascending pass. k_select holds the weights in registers, 16
-// neighbours a thread, and so has one block-wide sum and four other barriers in all; beyond
-// kSelTokens tokens k_select_long goes over memory again for each digit.
-constexpr int kSelItems = 16;
+// indices and weights in one ascending pass. k_select holds the weights in registers, item i
+// of thread t token i T + t, so that loads and stores are of neighbours; in the ascending
+// pass each wavefront's counts of each item meet in LDS once, and ballots order the rest.
+// Beyond kSelTokens tokens k_select_long goes over memory again for each digit. Bound by
+// latency: one pass over the weights and a dozen barriers (8 x 2,944 tokens 12 us, 256 x 8,000
+// 19; 12 x 81,000, past the registers, 92).
 constexpr int kSelLong = 1024;                    // threads of k_select_long
-constexpr int kSelTokens = kSelItems * 1024;
+constexpr int kSelItems = 32;                     // tokens of a thread, at most (64 spill)
+constexpr int kSelTokens = kSelItems * kSelLong;
 constexpr int kDigits = 3;
 __device__ constexpr int kShift[kDigits] = {20, 10, 0}, kWidth[kDigits] = {11, 10, 10};
 constexpr int kBins = 2048 + 1024 + 1024;
@@ -375,46 +378,51 @@ __device__ __forceinline__ uint64_t block_scan(uint64_t v, uint64_t* lds, uint64
     return before + x - v;
 }
 
-// N neighbouring tokens of a thread, from j0: the kept ones' indices and weights to their
-// places (`above` << 32 | `equal` tokens lie before them); the least place that changes.
-template <int N>
-__device__ __forceinline__ int put_kept(const EvictArgs& a, const Kept& q, const Border& b, int sh, int j0, const float (&v)[N],
-                                        uint64_t before)
+// The kept ones of T N tokens from j0 on (v: item i of thread t is token j0 + i T + t; a
+// barrier stands between their loads and here): indices and weights to their places.
+// `done` (tokens kept beside the ties << 32 | tokens of the border's key before) moves on.
+template <int T, int N>
+__device__ __forceinline__ void put_kept(const EvictArgs& a, const Kept& q, const Border& b, int sh, int j0, const float (&v)[N],
+                                         uint64_t* counts, uint64_t* sums, uint64_t* done, int* moved)
 {
+    constexpr int W = T / kWave;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = uniform(tid >> 6);
     int32_t* idx = a.kept_idx + (int64_t)sh * a.idx_stride;
     float* tw = a.to.weight ? a.to.weight + (int64_t)sh * a.to.weight_stride : nullptr;
-    uint32_t n = (uint32_t)(before >> 32), e = (uint32_t)before;
-    int moved = INT32_MAX;
+    auto look = [&](int i, uint64_t* above, uint64_t* equal) {
+        const int j = j0 + i * T + tid;
+        const uint32_t key = weight_key(v[i]);
+        const bool there = j < q.L, fixed = j < q.lo || j >= q.hi;
+        *above = __ballot(there && (fixed || b.above(key)));
+        *equal = __ballot(there && !fixed && b.equal(key));
+    };
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const int j = j0 + i;
-        if (j >= q.L) break;
-        const uint32_t key = weight_key(v[i]);
-        const bool fixed = j < q.lo || j >= q.hi, above = fixed || b.above(key), equal = !fixed && b.equal(key);
-        if (above || (equal && e < b.ties)) {
-            const int to = (int)(n + min(e, b.ties));
+        uint64_t n, e;
+        look(i, &n, &e);
+        if (lane == 0) counts[i * W + wave] = (uint64_t)__popcll(n) << 32 | (uint32_t)__popcll(e);
+    }
+    __syncthreads();
+    const uint64_t mine = tid < N * W ? counts[tid] : 0;
+    uint64_t total;
+    const uint64_t before = block_scan<W>(mine, sums, &total);
+    if (tid < N * W) counts[tid] = *done + before;
+    __syncthreads();
+    const uint64_t below = (1ull << lane) - 1;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        uint64_t n, e;
+        look(i, &n, &e);
+        const uint64_t base = counts[i * W + wave];
+        const uint32_t n_at = (uint32_t)(base >> 32) + __popcll(n & below), e_at = (uint32_t)base + __popcll(e & below);
+        if ((n >> lane & 1) || ((e >> lane & 1) && e_at < b.ties)) {
+            const int j = j0 + i * T + tid, to = (int)(n_at + min(e_at, b.ties));
             idx[to] = j;
             if (tw) tw[to] = v[i];
-            if (to != j) moved = min(moved, to);
+            if (to != j) *moved = min(*moved, to);
         }
-        n += above;
-        e += equal;
     }
-    return moved;
-}
-template <int N>
-__device__ __forceinline__ uint64_t count_kept(const Kept& q, const Border& b, int j0, const float (&v)[N])
-{
-    uint32_t n = 0, e = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int j = j0 + i;
-        const uint32_t key = weight_key(v[i]);
-        const bool fixed = j < q.lo || j >= q.hi;
-        n += j < q.L && (fixed || b.above(key));
-        e += j < q.L && !fixed && b.equal(key);
-    }
-    return (uint64_t)n << 32 | e;
+    *done += total;
 }
 
 template <int T>
@@ -428,96 +436,88 @@ __device__ __forceinline__ void finish(const EvictArgs& a, const Kept& q, int sh
     if (threadIdx.x == 0) a.info[sh] = EvictInfo{q.k, a.in_place ? *first_moved : 0};
 }
 
-template <int T>
+// The border over the tokens that `each` hands to a function one by one (the same ones each time).
+template <typename Each>
+__device__ __forceinline__ Border find_border(const Kept& q, uint32_t* bins, Each each)
+{
+    Border border{0, 0, true};  // all stay
+    if (q.all()) return border;
+    border = Border{q.take > 0 ? 0u : ~0u, 0, false};
+    uint32_t want = (uint32_t)max(q.take, 0);
+    auto count = [&](auto digit) {
+        constexpr int D = decltype(digit)::value;
+        __syncthreads();
+        each([&](int j, float w) {
+            const uint32_t key = weight_key(w);
+            if (j >= q.lo && j < q.hi && (D == 0 || key >> (kShift[D] + kWidth[D]) == border.least >> (kShift[D] + kWidth[D])))
+                atomicAdd(&bins[first_bin(D) + (key >> kShift[D] & ((1u << kWidth[D]) - 1))], 1u);
+        });
+        __syncthreads();
+        return next_digit<D>(border, want, bins);
+    };
+    if (want > 0 && count(std::integral_constant<int, 0>()) && count(std::integral_constant<int, 1>()))
+        count(std::integral_constant<int, 2>());
+    return border;
+}
+
+template <int T, int N>
 __global__ __launch_bounds__(T) void k_select(EvictArgs a)
 {
     __shared__ __align__(16) uint32_t bins[kBins];
-    __shared__ uint64_t sums[T / kWave];
+    __shared__ uint64_t counts[N * (T / kWave)], sums[T / kWave];
     __shared__ int first_moved;
-    const int sh = blockIdx.x, tid = threadIdx.x, j0 = kSelItems * tid;
+    const int sh = blockIdx.x, tid = threadIdx.x;
     const Kept q(a, sh / a.from.kv_heads);
     const float* w = a.from.weight + (int64_t)sh * a.from.weight_stride;
-    float v[kSelItems];
+    float v[N];
 #pragma unroll
-    for (int i = 0; i < kSelItems; ++i) v[i] = j0 + i < q.L ? w[j0 + i] : 0.0f;
+    for (int i = 0; i < N; ++i) v[i] = i * T + tid < q.L ? w[i * T + tid] : 0.0f;
     for (int b = tid; b < kBins; b += T) bins[b] = 0;
     if (tid == 0) first_moved = q.k;
-    Border border{0, 0, true};  // all stay
-    if (!q.all()) {
-        border = Border{q.take > 0 ? 0u : ~0u, 0, false};
-        uint32_t want = (uint32_t)max(q.take, 0);
-        auto count = [&](auto digit) {
-            constexpr int D = decltype(digit)::value;
-            __syncthreads();
+    const Border border = find_border(q, bins, [&](auto&& f) {
 #pragma unroll
-            for (int i = 0; i < kSelItems; ++i) {
-                const int j = j0 + i;
-                const uint32_t key = weight_key(v[i]);
-                if (j >= q.lo && j < q.hi && (D == 0 || key >> (kShift[D] + kWidth[D]) == border.least >> (kShift[D] + kWidth[D])))
-                    atomicAdd(&bins[first_bin(D) + (key >> kShift[D] & ((1u << kWidth[D]) - 1))], 1u);
-            }
-            __syncthreads();
-            return next_digit<D>(border, want, bins);
-        };
-        if (want > 0 && count(std::integral_constant<int, 0>()) && count(std::integral_constant<int, 1>()))
-            count(std::integral_constant<int, 2>());
-    }
-    uint64_t total;
-    const uint64_t before = block_scan<T / kWave>(count_kept(q, border, j0, v), sums, &total);
-    finish<T>(a, q, sh, put_kept(a, q, border, sh, j0, v, before), &first_moved);
+        for (int i = 0; i < N; ++i) f(i * T + tid, v[i]);
+    });
+    __syncthreads();  // (every weight is in registers: in place, they may be overwritten)
+    uint64_t done = 0;
+    int moved = INT32_MAX;
+    put_kept<T>(a, q, border, sh, 0, v, counts, sums, &done, &moved);
+    finish<T>(a, q, sh, moved, &first_moved);
 }
 
 // In place, a pass's weights are all in registers before any is written, and go to places
 // not past those already read.
 __global__ __launch_bounds__(kSelLong) void k_select_long(EvictArgs a)
 {
+    constexpr int T = kSelLong, N = 16;
     __shared__ __align__(16) uint32_t bins[kBins];
-    __shared__ uint64_t sums[kSelLong / kWave];
+    __shared__ uint64_t counts[N * (T / kWave)], sums[T / kWave];
     __shared__ int first_moved;
     const int sh = blockIdx.x, tid = threadIdx.x;
     const Kept q(a, sh / a.from.kv_heads);
     const float* w = a.from.weight + (int64_t)sh * a.from.weight_stride;
-    for (int b = tid; b < kBins; b += kSelLong) bins[b] = 0;
+    for (int b = tid; b < kBins; b += T) bins[b] = 0;
     if (tid == 0) first_moved = q.k;
-    Border border{0, 0, true};
-    if (!q.all()) {
-        border = Border{q.take > 0 ? 0u : ~0u, 0, false};
-        uint32_t want = (uint32_t)max(q.take, 0);
-        auto count = [&](auto digit) {
-            constexpr int D = decltype(digit)::value;
-            constexpr int U = 8;  // loads in flight
-            __syncthreads();
-            for (int i0 = q.lo + tid; i0 < q.hi; i0 += U * kSelLong) {
-                float v[U];
+    const Border border = find_border(q, bins, [&](auto&& f) {
+        constexpr int U = 16;  // loads in flight
+        for (int j0 = 0; j0 < q.L; j0 += U * T) {
+            float v[U];
 #pragma unroll
-                for (int i = 0; i < U; ++i) v[i] = i0 + i * kSelLong < q.hi ? w[i0 + i * kSelLong] : 0.0f;
+            for (int i = 0; i < U; ++i) v[i] = j0 + i * T + tid < q.L ? w[j0 + i * T + tid] : 0.0f;
 #pragma unroll
-                for (int i = 0; i < U; ++i) {
-                    const uint32_t key = weight_key(v[i]);
-                    if (i0 + i * kSelLong < q.hi &&
-                        (D == 0 || key >> (kShift[D] + kWidth[D]) == border.least >> (kShift[D] + kWidth[D])))
-                        atomicAdd(&bins[first_bin(D) + (key >> kShift[D] & ((1u << kWidth[D]) - 1))], 1u);
-                }
-            }
-            __syncthreads();
-            return next_digit<D>(border, want, bins);
-        };
-        if (want > 0 && count(std::integral_constant<int, 0>()) && count(std::integral_constant<int, 1>()))
-            count(std::integral_constant<int, 2>());
-    }
-    uint64_t done = 0;  // of the passes before
+            for (int i = 0; i < U; ++i) f(j0 + i * T + tid, v[i]);
+        }
+    });
+    uint64_t done = 0;
     int moved = INT32_MAX;
-    for (int p0 = 0; p0 < q.L; p0 += kSelItems * kSelLong) {
-        const int j0 = p0 + kSelItems * tid;
-        float v[kSelItems];
+    for (int j0 = 0; j0 < q.L; j0 += N * T) {
+        float v[N];
 #pragma unroll
-        for (int i = 0; i < kSelItems; ++i) v[i] = j0 + i < q.L ? w[j0 + i] : 0.0f;
-        uint64_t total;
-        const uint64_t before = block_scan<kSelLong / kWave>(count_kept(q, border, j0, v), sums, &total);
-        moved = min(moved, put_kept(a, q, border, sh, j0, v, done + before));
-        done += total;
+        for (int i = 0; i < N; ++i) v[i] = j0 + i * T + tid < q.L ? w[j0 + i * T + tid] : 0.0f;
+        __syncthreads();
+        put_kept<T>(a, q, border, sh, j0, v, counts, sums, &done, &moved);
     }
-    finish<kSelLong>(a, q, sh, moved, &first_moved);
+    finish<T>(a, q, sh, moved, &first_moved);
 }
 
 // The kept tokens' keys and values to their places. A block takes chunks of `kMoveRows`
@@ -617,9 +617,10 @@ int launch_append(const AppendArgs& a, void* st, void* e0, void* e1)
 int launch_select(const EvictArgs& a, void* st, void* e0, void* e1)
 {
     const int64_t blocks = (int64_t)a.from.n_seqs * a.from.kv_heads, cap = capacity(a.from);
-    if (cap <= kSelItems * 256) return enqueue(k_select<256>, blocks, 256, st, e0, e1, a);
-    if (cap <= kSelItems * 512) return enqueue(k_select<512>, blocks, 512, st, e0, e1, a);
-    if (cap <= kSelTokens) return enqueue(k_select<1024>, blocks, 1024, st, e0, e1, a);
+    if (cap <= 16 * 256) return enqueue(k_select<256, 16>, blocks, 256, st, e0, e1, a);
+    if (cap <= 16 * 512) return enqueue(k_select<512, 16>, blocks, 512, st, e0, e1, a);
+    if (cap <= 16 * 1024) return enqueue(k_select<1024, 16>, blocks, 1024, st, e0, e1, a);
+    if (cap <= kSelTokens) return enqueue(k_select<1024, kSelItems>, blocks, 1024, st, e0, e1, a);
     return enqueue(k_select_long, blocks, kSelLong, st, e0, e1, a);
 }
 

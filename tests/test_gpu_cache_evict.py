@@ -165,3 +165,28 @@ def test_the_only_head_and_page_at_odd_strides():
     r = msao.msao_cache_evict(cache, torch.tensor([5], dtype=torch.int32, device=DEV))
     idx = r["kept_idx"][0, 0, :5].long()
     assert torch.equal(k[0, 0, :5], before[0, 0, idx])
+
+
+@pytest.mark.parametrize("length", [8193, 16385, 20000, 32769, 50000])
+@pytest.mark.parametrize("place", ["in place", "other pages"])
+def test_long_caches(length, place):
+    """Past what each form of the selection holds; ties across its passes."""
+    import paper_2604_02945_amd as msao
+    case = Case(39, [length, 100], [0, 0], 1, 1, 8, 256, BF16)
+    case.weight[0, 0, :length] = torch.where(torch.rand(length, generator=case.g) < 0.3, torch.tensor(0.5), case.weight[0, 0, :length])
+    cache, _ = case.device(DEV)
+    to = target(case, case.per) if place == "other pages" else None
+    budget = [int((case.weight[0, 0, :length] > 0.5).sum()) + 1000, 60]  # the border is a tie
+    src = cache.k.clone()
+    r = msao.msao_cache_evict(cache, torch.tensor(budget, dtype=torch.int32, device=DEV), 3, 50, to=to)
+    torch.cuda.synchronize()
+    into = to or cache
+    for b in range(2):
+        kept = evicted(case.weight[b, 0].numpy(), case.lengths[b], budget[b], into.capacity, 3, 50)
+        assert np.array_equal(r["kept_idx"][b, 0, :len(kept)].cpu().numpy(), kept)
+        assert (r["kept_idx"][b, 0, len(kept):case.cap] == -1).all() and int(into.length[b]) == len(kept)
+        assert torch.equal(into.weight[b, 0, :len(kept)].cpu(), case.weight[b, 0, kept])
+        n = torch.arange(len(kept))
+        old = torch.from_numpy(case.pages[b])[kept // 256].long().to(DEV)
+        new = into.pages[b].long()[(n // 256).to(DEV)]
+        assert torch.equal(into.k[new, 0, (n % 256).to(DEV)], src[old, 0, torch.from_numpy(kept % 256).to(DEV)])
