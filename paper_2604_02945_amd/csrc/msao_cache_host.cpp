@@ -371,7 +371,8 @@ msao_status msao_cache_evict(msao_ctx* ctx, const msao_kv_cache* from, const msa
                 return bad(err, "the caches differ in dtype, head_dim, kv_heads or n_seqs");
             // pages of one pool are told apart by their tables, on the device; arrays of
             // the same address are the same cache, whose moves need the order of `to` NULL
-            if (to->pages == from->pages || to->length == from->length || (to->weight && to->weight == from->weight))
+            if ((to->pages && to->pages == from->pages) || (to->length && to->length == from->length) ||
+                (to->weight && to->weight == from->weight))
                 return bad(err, "the caches share an array: pass NULL for eviction in place");
         }
         if (n_first < 0 || n_recent < 0) return bad(err, "n_first or n_recent is negative");

@@ -191,6 +191,14 @@ def test_evict_refusals(kw, code):
         assert rc == code and message() != "ctx is NULL", message()
 
 
+@pytest.mark.parametrize("kw", [dict(n_seqs=0, pages=None, length=None, weight=None),
+                                dict(pages_per_seq=0, table_stride=0, weight_stride=0, pages=None, weight=None)])
+def test_evict_of_nothing_shares_no_array(kw):
+    """Arrays of no element may be NULL in both caches."""
+    to = dict(OTHER, **kw)
+    assert evict(c=cache(**kw), to=cache(**to)) == INVALID and message() == "ctx is NULL"
+
+
 def test_evict_needs_weight():
     assert evict(c=cache(weight=None)) == INVALID and "weight" in message()
 
