@@ -213,10 +213,11 @@ struct Queries {
     }
     // Operands of 16 rows from line `row`.
     u32x4 v[kPieces / 4];
-    __device__ __forceinline__ void take(const uint8_t* lds, int row)
+    __device__ __forceinline__ void take(const uint8_t* lds, int row) { take_line(lds, row + (int)(threadIdx.x & 15)); }
+    __device__ __forceinline__ void take_line(const uint8_t* lds, int line)
     {
         const int lane = threadIdx.x & (kWave - 1);
-        const uint8_t* src = lds + (row + (lane & 15)) * kLine + 16 * (lane >> 4);
+        const uint8_t* src = lds + line * kLine + 16 * (lane >> 4);
 #pragma unroll
         for (int s = 0; s < kPieces / 4; ++s) v[s] = *(const u32x4*)(src + 64 * s);
     }
@@ -990,12 +991,14 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight(AttendArg
     float* weight = a.c.weight + (int64_t)sh * a.c.weight_stride;
     Queries<DT, DP>::fill(lds, a, p, 0, MT * 16, n_rows);
     const int used = min((n_rows + 15) / 16, MT);
-    float z[MT];   // the row's sum (rows of no weight: +inf, which gives 0)
+    // Columns behind the last row are that row again, with a sum of +inf, which gives 0 as for
+    // rows of no weight: zeros for them would be NaN at an infinite key whose weight is 0
+    float z[MT];
     int last[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-        const int row = 16 * m + i16, tok = row / a.group, head = p.head * a.group + (row - tok * a.group);
-        z[m] = row < n_rows ? a.lse2[(int64_t)(p.begin + tok) * a.heads + head] : INFINITY;
+        const int row = min(16 * m + i16, n_rows - 1), tok = row / a.group, head = p.head * a.group + (row - tok * a.group);
+        z[m] = 16 * m + i16 < n_rows ? a.lse2[(int64_t)(p.begin + tok) * a.heads + head] : INFINITY;
         if (z[m] == -INFINITY) z[m] = INFINITY;
         last[m] = a.causal ? p.length - p.n_new + tok : p.length - 1;
     }
@@ -1025,7 +1028,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight(AttendArg
             for (int m = 0; m < MT; ++m) {
                 if (m >= used) break;
                 Queries<DT, DP> q;
-                q.take(lds, 16 * m);
+                q.take_line(lds, min(16 * m + i16, n_rows - 1));
                 const f32x4 s = scores<DT, DP>(kf, q);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
@@ -1109,7 +1112,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight_rows(Atte
             const int row = r0 + threadIdx.x, t = row / a.group, head = p.head * a.group + (row - t * a.group);
             next_z = row < n_rows ? a.lse2[(int64_t)(p.begin + t) * a.heads + head] : INFINITY;
             if (next_z == -INFINITY) next_z = INFINITY;
-            next_last = a.causal ? p.length - p.n_new + t : p.length - 1;
+            next_last = row >= n_rows ? -1 : a.causal ? p.length - p.n_new + t : p.length - 1;
         }
     };
     if (part * per < s_end) fetch(part * per);
@@ -1128,7 +1131,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight_rows(Atte
         if (step + 1 < s_end) fetch(step + 1);
         const int r0 = from + step * kStep;
         const int least = a.causal ? p.length - p.n_new + r0 / a.group : p.length - 1;
-        const bool whole = kn[0] == 16 && kn[1] == 16 && tok + kTile - 1 <= least;
+        const bool whole = kn[0] == 16 && kn[1] == 16 && tok + kTile - 1 <= least && r0 + kStep <= n_rows;
         auto add = [&](auto all_seen) {
 #pragma unroll
             for (int m = 0; m < kStep / 16; ++m) {

@@ -193,3 +193,23 @@ def test_what_a_row_does_not_see_has_no_effect(dtype, value, dim, heads, at):
         assert torch.equal(got[bad:n, :G], want[bad:n, :G])
     elif value != value:
         assert torch.isnan(got[bad:n]).all() and torch.isnan(lse[bad:n]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 3, 9, 40])
+@pytest.mark.parametrize("dim,heads", [(128, 14), (256, 2)])
+def test_a_key_at_minus_infinity_gives_nothing(dtype, n, dim, heads):
+    """Every row that sees token 20 has the score -inf there: all is as with a score of -1e30."""
+    import paper_2604_02945_amd as msao
+    case = Case(16, [70, 50], [n, 1], heads, 2, dim, 16, dtype)
+    case.q[..., 0] = case.q[..., 0].abs() + 1
+    out = []
+    for value in (-1e30, float("-inf")):
+        case.k[int(case.pages[0, 1]), :, 4, 0] = value
+        cache, start = case.device(DEV)
+        lse = torch.zeros(n + 1, heads, device=DEV)
+        o = msao.msao_cache_attention(cache, start, n, case.q.to(DEV), lse=lse, accumulate=True)
+        out.append((o, lse, cache.weight))
+    torch.cuda.synchronize()
+    for a, b in zip(*out):
+        assert torch.isfinite(a).all() and torch.equal(a, b)
