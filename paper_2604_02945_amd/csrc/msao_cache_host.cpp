@@ -313,7 +313,9 @@ msao_status msao_cache_attention(msao_ctx* ctx, const msao_kv_cache* cache, cons
         MSAO_TRY(attend_plan(cache, chunk, heads, flags, pl, err));
         AttendArgs& a = pl.a;
         const int64_t es = elt_size(cache->dtype), values = (int64_t)heads * cache->head_dim;
-        if (std::isnan(scale) || std::isinf(scale)) return bad(err, "scale is not finite");
+        // (in base 2, as the kernels take it, too)
+        const float scale2 = (float)((double)scale * 1.44269504088896340736);
+        if (!std::isfinite(scale2)) return bad(err, "scale is not finite");
         if (chunk->n_rows > 0) {
             MSAO_TRY(check_rows(q, q_stride, values, es, "q", err));
             MSAO_TRY(check_rows(out, out_stride, values, es, "out", err));
@@ -327,7 +329,7 @@ msao_status msao_cache_attention(msao_ctx* ctx, const msao_kv_cache* cache, cons
         a.q_stride = q_stride * es;
         a.out_stride = out_stride * es;
         a.lse = lse;
-        a.scale = (float)((double)scale * 1.44269504088896340736);
+        a.scale = scale2;
         uint8_t* ws = (uint8_t*)workspace;
         if (a.splits > 1) {
             a.part_o = (float*)(ws + pl.part_o);
