@@ -607,6 +607,7 @@ __device__ __forceinline__ void load_to_lds(const u32x4& buffer, uint32_t to, in
 }
 __device__ __forceinline__ void stage_came() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
+constexpr int kRowLevel = 32;
 template <int DP, int MT, int NW, int ST, int WPS>
 __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
 {
@@ -619,8 +620,14 @@ __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
 
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
     const int i16 = lane & 15, c = lane >> 4;
-    const int per_pair = a.row_tiles * a.splits, sh = blockIdx.x / per_pair;
-    const int j = (blockIdx.x - sh * per_pair + sh) % per_pair;
+    // the last tiles, which see most, of all pairs before the ones before them, so that no long
+    // one is left to the end; a pair's kRowLevel tiles of a level side by side, which share keys
+    // and values in the caches. 8 prompts of 1,500 tokens 71 us (83 pair by pair, 65 tile by tile),
+    // one of 8,000 574 us (665, 543), chunks of 2,048 over 12,288 717 us (746, 780)
+    const int per_pair = a.row_tiles * a.splits, pairs = a.c.n_seqs * a.c.kv_heads;
+    const int level = min((int)blockIdx.x / (kRowLevel * pairs), per_pair / kRowLevel), in_level = blockIdx.x - level * kRowLevel * pairs;
+    const int width = min(kRowLevel, per_pair - level * kRowLevel), sh = in_level / width;
+    const int j = level * kRowLevel + (in_level - sh * width + sh) % width;
     const int split = j / a.row_tiles, tile = a.row_tiles - 1 - (j - split * a.row_tiles);
     const Place p = place_of(a, sh);
     const int n_rows = call_rows(a, p), r0 = tile * NW * MT * 16;
