@@ -157,7 +157,7 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a, int sh)
 }
 
 // Rows of the sequence that the call computes (max_new bounds the grid).
-__device__ __forceinline__ int call_rows(const AttendArgs& a, const Place& p) { return min(p.n_new, a.ch.max_new) * a.group; }
+__device__ __forceinline__ int call_rows(const AttendArgs& a, const Place& p) { return min(p.n_new, a.ch.max_new) * a.group.n; }
 
 // Pages of 64 half tiles (16 tokens) of a wavefront, one a lane: lane i has half i % NH of
 // tile first + i / NH of those that turn `turn` of `step` takes (every step-th of NH halves).
@@ -198,7 +198,7 @@ struct Queries {
     // Piece `piece` of the row: zeros past the last row and past the head's channels.
     __device__ static __forceinline__ u32x4 fetch(const AttendArgs& a, const Place& p, int row, int n_rows, int piece)
     {
-        const int tok = row / a.group, head = p.head * a.group + (row - tok * a.group);
+        const int tok = a.group.of(row), head = p.head * a.group.n + (row - tok * a.group.n);
         const int off = 16 * piece;
         if (row >= n_rows || off >= a.c.dim * Type<DT>::kSize) return u32x4{0, 0, 0, 0};
         return *(const u32x4*)(a.q + (int64_t)(p.begin + tok) * a.q_stride + (int64_t)head * a.c.dim * Type<DT>::kSize + off);
@@ -308,9 +308,9 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArg
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
         const int row = r0 + line0 + 16 * m + i16;
-        last[m] = a.causal ? p.length - p.n_new + row / a.group : p.length - 1;
+        last[m] = a.causal ? p.length - p.n_new + a.group.of(row) : p.length - 1;
     }
-    const int least = a.causal ? p.length - p.n_new + r0 / a.group : p.length - 1;  // of all rows
+    const int least = a.causal ? p.length - p.n_new + a.group.of(r0) : p.length - 1;  // of all rows
 
     f32x4 o[MT][E];
     float ref[MT], sum[MT];
@@ -552,7 +552,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArg
 #pragma unroll
                 for (int w = 1; w < TW; ++w) acc[t] += lds_o[w * RW + g][orow][od + t];
             }
-            const int tok = row / a.group, head = p.head * a.group + (row - tok * a.group);
+            const int tok = a.group.of(row), head = p.head * a.group.n + (row - tok * a.group.n);
             const int64_t at = (int64_t)(p.begin + tok) * a.heads + head;
             if (parts <= 1) {
                 const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -660,10 +660,10 @@ __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
         const int row = w0 + 16 * m + i16;
 #pragma unroll
         for (int s = 0; s < KS; ++s) q[m].v[s] = Queries<kBF16, DP>::fetch(a, p, row, n_rows, 4 * s + c) ^ (a.scale < 0.0f ? 0x80008000u : 0u);
-        last[m] = a.causal ? p.length - p.n_new + row / a.group : p.length - 1;
+        last[m] = a.causal ? p.length - p.n_new + a.group.of(row) : p.length - 1;
     }
-    const int least = a.causal ? p.length - p.n_new + w0 / a.group : p.length - 1;
-    const int least_of_all = a.causal ? p.length - p.n_new + r0 / a.group : p.length - 1;
+    const int least = a.causal ? p.length - p.n_new + a.group.of(w0) : p.length - 1;
+    const int least_of_all = a.causal ? p.length - p.n_new + a.group.of(r0) : p.length - 1;
     if (threadIdx.x == 0) lds_left_out = 0;
     // tokens that the wavefront's own last row sees
     const int w_hi = used > 0 ? min(hi, group_sees(p.length, p.n_new, a.group, min(w0 + MT * 16, n_rows) - 1, a.causal)) : lo;
@@ -858,7 +858,7 @@ __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
         sum[m] += __shfl_xor(sum[m], 32);
         const int row = w0 + 16 * m + i16;
         if (row >= n_rows) continue;
-        const int tok = row / a.group, head = p.head * a.group + (row - tok * a.group);
+        const int tok = a.group.of(row), head = p.head * a.group.n + (row - tok * a.group.n);
         const int64_t at = (int64_t)(p.begin + tok) * a.heads + head;
         if (parts <= 1) {
             const float inv = sum[m] == 0.0f ? 0.0f : 1.0f / sum[m];
@@ -901,7 +901,7 @@ __global__ __launch_bounds__(kBlock) void k_combine(AttendArgs a, int blocks_per
     const int seen = group_sees(p.length, p.n_new, a.group, r_end - 1, a.causal);
     const int parts = parts_of(seen, a.part_tokens);
     if (parts <= 1) return;  // written by k_attend
-    const int tok = row / a.group, head = p.head * a.group + (row - tok * a.group);
+    const int tok = a.group.of(row), head = p.head * a.group.n + (row - tok * a.group.n);
     const int64_t all = (int64_t)a.ch.n_rows * a.heads, at = (int64_t)(p.begin + tok) * a.heads + head;
     const int t = wave % W * kWave + lane, group = t / LP, ch = (t & (LP - 1)) * 4;
     const bool has = ch < a.c.dim;
@@ -1004,7 +1004,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight(AttendArg
     int last[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-        const int row = min(16 * m + i16, n_rows - 1), tok = row / a.group, head = p.head * a.group + (row - tok * a.group);
+        const int row = min(16 * m + i16, n_rows - 1), tok = a.group.of(row), head = p.head * a.group.n + (row - tok * a.group.n);
         z[m] = 16 * m + i16 < n_rows ? a.lse2[(int64_t)(p.begin + tok) * a.heads + head] : INFINITY;
         if (z[m] == -INFINITY) z[m] = INFINITY;
         last[m] = a.causal ? p.length - p.n_new + tok : p.length - 1;
@@ -1101,7 +1101,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight_rows(Atte
         for (int s = 0; s < KS; ++s) kf[h][s] = __builtin_amdgcn_raw_buffer_load_b128(f.r, ko.off[s], 0, 0);
     }
     // rows from the first that sees the block's first token, this part's share of them
-    const int from = a.causal ? max(0, b0 - (p.length - p.n_new)) * a.group : 0;
+    const int from = a.causal ? max(0, b0 - (p.length - p.n_new)) * a.group.n : 0;
     const int steps = (n_rows - from + kStep - 1) / kStep, per = (steps + a.row_parts - 1) / a.row_parts;
     const int s_end = min(steps, (part + 1) * per);
     float w[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
@@ -1116,7 +1116,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight_rows(Atte
             next[i] = Q::fetch(a, p, r0 + row, n_rows, at - row * Q::kPieces);
         }
         if (threadIdx.x < kStep) {
-            const int row = r0 + threadIdx.x, t = row / a.group, head = p.head * a.group + (row - t * a.group);
+            const int row = r0 + threadIdx.x, t = a.group.of(row), head = p.head * a.group.n + (row - t * a.group.n);
             next_z = row < n_rows ? a.lse2[(int64_t)(p.begin + t) * a.heads + head] : INFINITY;
             if (next_z == -INFINITY) next_z = INFINITY;
             next_last = row >= n_rows ? -1 : a.causal ? p.length - p.n_new + t : p.length - 1;
@@ -1137,7 +1137,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight_rows(Atte
         __syncthreads();
         if (step + 1 < s_end) fetch(step + 1);
         const int r0 = from + step * kStep;
-        const int least = a.causal ? p.length - p.n_new + r0 / a.group : p.length - 1;
+        const int least = a.causal ? p.length - p.n_new + a.group.of(r0) : p.length - 1;
         const bool whole = kn[0] == 16 && kn[1] == 16 && tok + kTile - 1 <= least && r0 + kStep <= n_rows;
         auto add = [&](auto all_seen) {
 #pragma unroll
@@ -1250,7 +1250,7 @@ int attend_rows(const AttendArgs& a, void* st, void* e0, void* e1)
 template <int DT, int DP>
 int combine_rows(const AttendArgs& a, void* st, void* e0, void* e1)
 {
-    const int rows = a.ch.max_new * a.group;
+    const int rows = a.ch.max_new * a.group.n;
     // many parts: the whole block on one row
     if (a.splits > 16) return enqueue(k_combine<DT, DP, kWaves>, pairs(a) * rows, st, e0, e1, a, rows);
     const int per = (rows + kWaves - 1) / kWaves;
@@ -1261,7 +1261,7 @@ template <int DT, int DP>
 int weight_rows(const AttendArgs& a, void* st, void* e0, void* e1)
 {
     const int64_t blocks = pairs(a) * a.weight_parts * a.row_parts;
-    const int64_t rows = (int64_t)a.ch.max_new * a.group;
+    const int64_t rows = (int64_t)a.ch.max_new * a.group.n;
     if (rows > kRowStep) return enqueue(k_weight_rows<DT, DP>, blocks, st, e0, e1, a);
     return rows <= 16 ? enqueue(k_weight<DT, DP, 1>, blocks, st, e0, e1, a) : enqueue(k_weight<DT, DP, 4>, blocks, st, e0, e1, a);
 }
@@ -1301,7 +1301,7 @@ constexpr int64_t kPartTarget = 2048, kPartLeast = 128, kPartMost = 1024, kManyT
 constexpr int64_t kWeightTarget = 16384, kWeightLeast = 256, kWeightRowTarget = 8192, kMostRowParts = 32;
 void attend_shape(AttendArgs& a)
 {
-    const int64_t rows = (int64_t)a.ch.max_new * a.group;
+    const int64_t rows = (int64_t)a.ch.max_new * a.group.n;
     const int most = padded_dim(a.c.dim) == 256 ? 32 : 64;  // rows of a workgroup of k_attend at most
     a.tile_rows = rows <= 16 ? 16 : rows <= 32 || most == 32 ? 32 : 64;
     a.many = a.dtype == kBF16 && rows >= kManyRows;

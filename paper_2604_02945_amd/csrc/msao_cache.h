@@ -77,11 +77,34 @@ MSAO_HD int page_at(const CacheDev& c, int s, int col)
 constexpr int kTile = 32;
 MSAO_HD int parts_of(int seen, int per) { return seen <= 0 ? 0 : (seen - 1) / per + 1; }
 
-// Tokens that rows [r0, r0 + rows) of a (sequence, kv head) see at most: row r is
-// query head r % group of token r / group. Without `causal` all of them.
-MSAO_HD int group_sees(int length, int n_new, int group, int last_row, bool causal)
+// Query heads that share a kv head: row r of a (sequence, kv head) is query head r % n of token
+// r / n. The quotient of a row in [0, 2^31) as the upper half of a product: with l the least of
+// n <= 2^l and mul = floor(2^(31 + l) / n) + 1, r mul is r 2^(31 + l) / n and less than
+// 2^(31 + l) / n more. (A division of integers is some 20 instructions, and there is one for each
+// 16 bytes of queries: one prompt of 8,000 tokens, weight pass 412 us with it, 361 without.)
+struct Group {
+    int32_t n;
+    uint32_t mul;
+    int32_t shift;
+    MSAO_HD int of(int row) const
+    {
+        return (int)((uint32_t)(((uint64_t)(2 * (uint32_t)row) * mul) >> 32) >> shift);
+    }
+};
+MSAO_HD Group make_group(int n)
 {
-    return causal ? clamp_int(length - n_new + last_row / group + 1, 0, length) : length;
+    Group g{n, 0, 0};
+    while (g.shift < 31 && (int64_t)1 << g.shift < n) ++g.shift;
+    const uint64_t mul = ((uint64_t)1 << (31 + g.shift)) / (uint32_t)n + 1;
+    g.mul = (uint32_t)mul;
+    return g;
+}
+
+// Tokens that rows [r0, r0 + rows) of a (sequence, kv head) see at most: row r is
+// query head r % group.n of token r / group.n. Without `causal` all of them.
+MSAO_HD int group_sees(int length, int n_new, const Group& group, int last_row, bool causal)
+{
+    return causal ? clamp_int(length - n_new + group.of(last_row) + 1, 0, length) : length;
 }
 
 // ---- append -------------------------------------------------------------------
@@ -114,7 +137,8 @@ struct AttendArgs {
     uint8_t* out;
     int64_t q_stride, out_stride;  // bytes
     float* lse;
-    int32_t heads, group, dtype;
+    int32_t heads, dtype;
+    Group group;
     int32_t causal, add_weight;
     float scale;                   // scale * log2(e)
     int32_t part_tokens;           // tokens of a part

@@ -193,13 +193,13 @@ msao_status attend_plan(const msao_kv_cache* cache, const msao_chunk* chunk, int
     a.c = cache_dev(*cache);
     a.ch = chunk_dev(*chunk);
     a.heads = heads;
-    a.group = heads / cache->kv_heads;
+    a.group = make_group(heads / cache->kv_heads);
     a.dtype = cache->dtype;
     a.causal = flags & MSAO_ATTEND_CAUSAL ? 1 : 0;
     a.add_weight = flags & MSAO_ATTEND_WEIGHT ? 1 : 0;
     attend_shape(a);
     const int64_t groups = (int64_t)a.c.n_seqs * a.c.kv_heads;
-    const int64_t most = std::max<int64_t>(std::max<int64_t>((int64_t)a.row_tiles * a.splits, (int64_t)a.ch.max_new * a.group),
+    const int64_t most = std::max<int64_t>(std::max<int64_t>((int64_t)a.row_tiles * a.splits, (int64_t)a.ch.max_new * a.group.n),
                                            std::max<int64_t>((int64_t)a.weight_parts * a.row_parts, a.c.per_seq * (int64_t)cache->page_size / 256 + 1));
     if (groups > 0 && most > kMaxBlocks / groups) return fail(err, MSAO_ERR_UNSUPPORTED, "more workgroups than one launch takes");
     const AttendBytes b = attend_bytes(a);

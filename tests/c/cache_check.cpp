@@ -26,17 +26,24 @@ int main()
             }
             CHECK((int64_t)n * per >= seen && (int64_t)(n - 1) * per < seen);
         }
+    // quotients by multiplication
+    for (int n : {1, 2, 3, 5, 6, 7, 8, 12, 14, 28, 48, 71, 255, 256, 257, 65535, 65537, (1 << 30) - 1, (1 << 30) + 1, INT_MAX - 1, INT_MAX}) {
+        const Group g = make_group(n);
+        for (int64_t k = 0; k < 3000; ++k)
+            for (int64_t r : {k, INT_MAX - k, k * n, k * n - 1, INT_MAX / n * (int64_t)n - k, (int64_t)(rng() & INT_MAX)})
+                if (r >= 0 && r <= INT_MAX) CHECK(g.of((int)r) == (int)r / n);
+    }
     // what the last row of a group sees
     for (int i = 0; i < 100000; ++i) {
         const int length = (int)(rng() % 300), n = (int)(rng() % 300), group = 1 + (int)(rng() % 8);
         if (n == 0) continue;
         const int row = (int)(rng() % (uint64_t)(n * group));
-        const int s = group_sees(length, n, group, row, true);
+        const int s = group_sees(length, n, make_group(group), row, true);
         CHECK(s >= 0 && s <= length);
         int count = 0;
         for (int j = 0; j < length; ++j) count += j <= length - n + row / group;
         CHECK(s == count);
-        CHECK(group_sees(length, n, group, row, false) == length);
+        CHECK(group_sees(length, n, make_group(group), row, false) == length);
     }
     // arrays of anything
     const int strange[] = {INT_MIN, INT_MIN + 1, -17, -1, 0, 1, 5, 31, 32, 33, 1000, INT_MAX - 1, INT_MAX};
