@@ -1108,12 +1108,27 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight_rows(Atte
     u32x4 next[kPer];
     float next_z = INFINITY;
     int next_last = -1;
-    auto fetch = [&](int step) {
-        const int r0 = from + step * kStep;
+    // Where a thread's pieces lie from the step's first token on. A group that divides the step
+    // has each step start with a token's first head, and the offsets of all steps are one's
+    uint32_t off[kPer];
+    auto offsets = [&](int first_head) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const int at = i * kBlock + threadIdx.x, row = at / Q::kPieces;
-            next[i] = Q::fetch(a, p, r0 + row, n_rows, at - row * Q::kPieces);
+            const int at = i * kBlock + threadIdx.x, line = at / Q::kPieces, row = first_head + line, t = a.group.of(row);
+            off[i] = (uint32_t)t * (uint32_t)a.q_stride + (uint32_t)((row - t * a.group.n) * row_bytes + 16 * (at - line * Q::kPieces));
+        }
+    };
+    const bool even = kStep % a.group.n == 0;
+    if (even) offsets(0);
+    auto fetch = [&](int step) {
+        const int r0 = from + step * kStep, t0 = a.group.of(r0);
+        const uint8_t* src = a.q + (int64_t)(p.begin + t0) * a.q_stride + (int64_t)p.head * a.group.n * row_bytes;
+        if (!even) offsets(r0 - t0 * a.group.n);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int at = i * kBlock + threadIdx.x, line = at / Q::kPieces;
+            next[i] = u32x4{0, 0, 0, 0};
+            if (r0 + line < n_rows && 16 * (at - line * Q::kPieces) < row_bytes) next[i] = *(const u32x4*)(src + off[i]);
         }
         if (threadIdx.x < kStep) {
             const int row = r0 + threadIdx.x, t = a.group.of(row), head = p.head * a.group.n + (row - t * a.group.n);

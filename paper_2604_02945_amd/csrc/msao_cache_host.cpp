@@ -18,6 +18,7 @@ namespace {
 
 constexpr int64_t kMaxCapacity = (int64_t)1 << 29;
 constexpr int64_t kMaxTokBytes = (int64_t)1 << 26;  // 16 tokens are one buffer
+constexpr int64_t kMaxRowBytes = (int64_t)1 << 25;  // 64 rows' offsets stay in 31 bits
 constexpr int64_t kMaxBlocks = (1 << 24) - 1;        // of 256 threads: a launch has fewer than 2^32
 constexpr int64_t kMaxStride = (int64_t)1 << 40;    // elements; products with 31-bit counts stay in 63 bits with 2^10 pages to spare
 
@@ -318,6 +319,7 @@ msao_status msao_cache_attention(msao_ctx* ctx, const msao_kv_cache* cache, cons
         if (!std::isfinite(scale2)) return bad(err, "scale is not finite");
         if (chunk->n_rows > 0) {
             MSAO_TRY(check_rows(q, q_stride, values, es, "q", err));
+            if (q_stride * es >= kMaxRowBytes) return fail(err, MSAO_ERR_UNSUPPORTED, "a stride of q of 32 MiB or more");
             MSAO_TRY(check_rows(out, out_stride, values, es, "out", err));
         }
         if (!aligned(lse, 4)) return fail(err, MSAO_ERR_ALIGNMENT, "lse is not 4-byte aligned");

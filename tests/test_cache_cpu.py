@@ -128,6 +128,7 @@ def attention(c=None, ch=None, q=FAKE, q_stride=32 * 128, heads=32, scale=0.1, f
     ({}, OK), ({"flags": 3}, OK), ({"flags": 0}, OK), ({"lse": None}, OK), ({"scale": 0.0}, OK), ({"scale": -1.0}, OK),
     ({"heads": 0}, INVALID), ({"heads": 30}, INVALID), ({"scale": float("nan")}, INVALID), ({"scale": float("inf")}, INVALID), ({"scale": 3e38}, INVALID),
     ({"flags": 4}, INVALID), ({"q": None}, INVALID), ({"out": None}, INVALID), ({"q": FAKE + 4}, ALIGN),
+    ({"q_stride": 1 << 24}, UNSUP), ({"q_stride": (1 << 24) - 8, "out_stride": 1 << 30}, OK),
     ({"out_stride": 32 * 128 + 2}, ALIGN), ({"out_stride": 31 * 128}, INVALID), ({"lse": FAKE + 2}, ALIGN),
     ({"ws": None}, WS), ({"ws": FAKE + 16}, WS), ({"ws_bytes": 0}, WS)])
 def test_attention_refusals(kw, code):
