@@ -1236,7 +1236,7 @@ int padded_dim(int dim) { return dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 
 int64_t pairs(const AttendArgs& a) { return (int64_t)a.c.n_seqs * a.c.kv_heads; }
 
 // k_attend_rows: 32 rows a wavefront, four wavefronts, stages of 64 tokens. Chunks of 2,048
-// over 12,288 tokens: 730 us; 48 rows a wavefront 884 (246 registers, as fast a SIMD but fewer
+// over 12,288 tokens: 717 us (730 on the card of the others); 48 rows a wavefront 884 (246 registers, as fast a SIMD but fewer
 // workgroups), 64 spill; 16 rows and eight wavefronts 770; stages of 32 tokens 852. With fewer
 // than kManyRows rows its wavefronts would be idle or its tokens not spread: k_attend.
 // Heads of 256: 16 rows a wavefront and stages of 32, for the same registers and LDS (the

@@ -169,6 +169,7 @@ struct EvictArgs {
     int32_t in_place, dtype;
     int32_t blocks;                // of the move, for each (sequence, kv head, k or v, column part)
     int32_t col_parts;             // parts that a row is cut into
+    Group units;                   // 16-byte pieces of a row's part
 };
 
 int launch_append(const AppendArgs& a, void* stream, void* ev0, void* ev1);

@@ -102,8 +102,8 @@ __global__ __launch_bounds__(kBlock) void k_append(AppendArgs a)
     constexpr int U = 4;  // rounds of heads in flight
     __shared__ f32x2 turn[kWaves][kMaxPairs];
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
-    const int64_t item = (int64_t)blockIdx.x * kWaves + wave;
-    const int row = (int)(item / a.parts), part = (int)(item - (int64_t)row * a.parts);
+    const uint32_t item = blockIdx.x * kWaves + wave;  // below 2^27
+    const int row = item / (uint32_t)a.parts, part = item - row * a.parts;
     if (row >= a.ch.n_rows) return;
     const int u = lane & (a.lanes - 1), per = kWave / a.lanes;  // the lane's pair of eights; heads of a round
     const int half = a.rot / 2, turned = a.rot / 16;
@@ -267,8 +267,8 @@ __global__ __launch_bounds__(kBlock) void k_append(AppendArgs a)
 // of thread t token i T + t, so that loads and stores are of neighbours; in the ascending
 // pass each wavefront's counts of each item meet in LDS once, and ballots order the rest.
 // Beyond kSelTokens tokens k_select_long goes over memory again for each digit. Bound by
-// latency: one pass over the weights and a dozen barriers (8 x 2,944 tokens 12 us, 256 x 8,000
-// 19; 12 x 81,000, past the registers, 92).
+// latency: one pass over the weights and a dozen barriers (8 x 2,944 tokens 12-13 us, 256 x 8,000
+// 16; 12 x 81,000, past the registers, 73).
 constexpr int kSelLong = 1024;                    // threads of k_select_long
 constexpr int kSelItems = 32;                     // tokens of a thread, at most (64 spill)
 constexpr int kSelTokens = kSelItems * kSelLong;
@@ -520,10 +520,13 @@ __global__ __launch_bounds__(kSelLong) void k_select_long(EvictArgs a)
     finish<T>(a, q, sh, moved, &first_moved);
 }
 
-// The kept tokens' keys and values to their places. A block takes chunks of `kMoveRows`
-// places in turn; in place there is one block for each (sequence, kv head, K or V,
-// column part), whose loads of a chunk are done before its stores begin: a kept token
-// only ever moves down, so a later chunk reads nothing that an earlier one wrote.
+// The kept tokens' keys and values to their places. A block takes chunks of whole places,
+// up to kMoveUnits 16-byte pieces a thread, in turn; in place there is one block for each
+// (sequence, kv head, K or V, column part), whose loads of a chunk are done before its stores
+// begin: a kept token only ever moves down, so a later chunk reads nothing that an earlier
+// one wrote. HBM bound: 256 heads of 2,048 tokens of 8,000, in place, 102-107 us for 546 MB,
+// the rate of a large copy (one block a head and K or V, without the column parts, leaves half
+// of the device idle).
 constexpr int kMoveUnits = 4;  // 16-byte pieces of a thread in flight
 __global__ __launch_bounds__(kBlock) void k_move(EvictArgs a)
 {
@@ -536,34 +539,35 @@ __global__ __launch_bounds__(kBlock) void k_move(EvictArgs a)
     const int sh = id >> 1, s = sh / a.from.kv_heads, h = sh - s * a.from.kv_heads;
     const EvictInfo info = a.info[sh];
     if (block == 0 && col == 0 && !is_v && h == 0 && threadIdx.x == 0) a.to.length[s] = info.kept;
-    const int units = a.from.dim * (a.dtype == kBF16 ? 2 : 4) / 16 / a.col_parts;  // 16-byte pieces of a row's part
+    const int units = a.units.n;
     const uint8_t* src = (is_v ? a.from.v + h * a.from.v_head : a.from.k + h * a.from.k_head) + (int64_t)col * units * 16;
     uint8_t* dst = (is_v ? a.to.v + h * a.to.v_head : a.to.k + h * a.to.k_head) + (int64_t)col * units * 16;
     const int64_t sp = is_v ? a.from.v_page : a.from.k_page, st = is_v ? a.from.v_tok : a.from.k_tok;
     const int64_t dp = is_v ? a.to.v_page : a.to.k_page, dt = is_v ? a.to.v_tok : a.to.k_tok;
     const int smask = (1 << a.from.page_shift) - 1, dmask = (1 << a.to.page_shift) - 1;
     const int32_t* idx = a.kept_idx + (int64_t)sh * a.idx_stride;
-    const int64_t end = (int64_t)info.kept * units, step = (int64_t)kBlock * kMoveUnits;
-    for (int64_t p0 = (int64_t)info.first_moved * units + block * step; p0 < end; p0 += a.blocks * step) {
+    const Group& per = a.units;
+    const int rows = kBlock * kMoveUnits / units;  // of a chunk
+    for (int64_t r0 = info.first_moved + (int64_t)block * rows; r0 < info.kept; r0 += (int64_t)a.blocks * rows) {
+        const int end = min(rows, info.kept - (int)r0) * units;
         u32x4 x[kMoveUnits];
 #pragma unroll
         for (int i = 0; i < kMoveUnits; ++i) {
-            const int64_t p = p0 + i * kBlock + threadIdx.x;
+            const int p = i * kBlock + threadIdx.x, row = per.of(p), to = (int)r0 + row;
             x[i] = u32x4{0, 0, 0, 0};
             if (p < end) {
-                const int to = (int)(p / units), j = idx[to];
+                const int j = idx[to];
                 const int page = page_at(a.from, s, j >> a.from.page_shift);
-                if (page >= 0) x[i] = *(const u32x4*)(src + page * sp + (j & smask) * st + (p - (int64_t)to * units) * 16);
+                if (page >= 0) x[i] = *(const u32x4*)(src + page * sp + (j & smask) * st + (p - row * units) * 16);
             }
         }
         if (a.in_place) __syncthreads();
 #pragma unroll
         for (int i = 0; i < kMoveUnits; ++i) {
-            const int64_t p = p0 + i * kBlock + threadIdx.x;
+            const int p = i * kBlock + threadIdx.x, row = per.of(p), to = (int)r0 + row;
             if (p < end) {
-                const int to = (int)(p / units);
                 const int page = page_at(a.to, s, to >> a.to.page_shift);
-                if (page >= 0) *(u32x4*)(dst + page * dp + (to & dmask) * dt + (p - (int64_t)to * units) * 16) = x[i];
+                if (page >= 0) *(u32x4*)(dst + page * dp + (to & dmask) * dt + (p - row * units) * 16) = x[i];
             }
         }
     }
@@ -605,6 +609,7 @@ void evict_shape(EvictArgs& a)
     } else {
         while (a.col_parts < 4 && units % (2 * a.col_parts) == 0) a.col_parts *= 2;
     }
+    a.units = make_group(units / a.col_parts);
 }
 
 int launch_append(const AppendArgs& a, void* st, void* e0, void* e1)
