@@ -1236,11 +1236,11 @@ int padded_dim(int dim) { return dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 
 int64_t pairs(const AttendArgs& a) { return (int64_t)a.c.n_seqs * a.c.kv_heads; }
 
 // k_attend_rows: 32 rows a wavefront, four wavefronts, stages of 64 tokens. Chunks of 2,048
-// over 12,288 tokens: 717 us (730 on the card of the others); 48 rows a wavefront 884 (246 registers, as fast a SIMD but fewer
-// workgroups), 64 spill; 16 rows and eight wavefronts 770; stages of 32 tokens 852. With fewer
-// than kManyRows rows its wavefronts would be idle or its tokens not spread: k_attend.
-// Heads of 256: 16 rows a wavefront and stages of 32, for the same registers and LDS (the
-// same chunks 1.70 ms, 6.26 through k_attend).
+// over 12,288 tokens: 730 us, with 48 rows a wavefront 884 (246 registers, as fast a SIMD but
+// fewer workgroups; 64 spill), 16 rows and eight wavefronts 770, stages of 32 tokens 852 (each
+// pair by pair; in levels 700-717). With fewer than kManyRows rows its wavefronts would be idle
+// or its tokens not spread: k_attend. Heads of 256: 16 rows a wavefront and stages of 32, for
+// the same registers and LDS (the same chunks 1.70 ms, 6.26 through k_attend).
 constexpr int kManyRows = 128;
 constexpr int row_tiles_of(int dp) { return dp == 256 ? 1 : 2; }
 constexpr int stage_of(int dp) { return dp == 256 ? 32 : 64; }

@@ -525,8 +525,7 @@ __global__ __launch_bounds__(kSelLong) void k_select_long(EvictArgs a)
 // (sequence, kv head, K or V, column part), whose loads of a chunk are done before its stores
 // begin: a kept token only ever moves down, so a later chunk reads nothing that an earlier
 // one wrote. HBM bound: 256 heads of 2,048 tokens of 8,000, in place, 102-107 us for 546 MB,
-// the rate of a large copy (one block a head and K or V, without the column parts, leaves half
-// of the device idle).
+// the rate of a large copy.
 constexpr int kMoveUnits = 4;  // 16-byte pieces of a thread in flight
 __global__ __launch_bounds__(kBlock) void k_move(EvictArgs a)
 {
