@@ -1,7 +1,9 @@
 """MI355X (gfx950) implementation of MSAO's fine-grained sparsity analysis
 (Sec. 4.1, with the MAS-guided selection and compaction it drives) and of the
 decoding-side pieces of its speculative offloading (Sec. 4.2): the draft
-model's confidence on the GPU and Algorithm 1's threshold logic on the host.
+model's confidence on the GPU, Algorithm 1's threshold logic on the host, and
+for the model that verifies the drafts its paged key-value cache: append,
+attention, eviction (`KvCache`, `msao_cache_*`).
 
 The HIP kernels and the C ABI live in libmsao.so (sources in csrc/, ABI in
 include/msao.h at the repository root); `binding` is a thin ctypes layer over
