@@ -582,8 +582,8 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArg
     }
 }
 
-// Many rows, bf16 (chunks of prompts): bound by the matrix cores and the exponents, so that
-// K and V are read once for 64 MT rows. A stage of 64 tokens goes from memory to LDS without
+// Many rows, bf16 (wide drafts, chunks of prompts): K and V are read once for 64 MT rows; from some
+// 100 rows on bound by the matrix cores and the exponents. A stage of 64 tokens goes from memory to LDS without
 // passing through registers (each wavefront brings 16 tokens) while the stage before it is
 // used. Every wavefront has 16 MT rows of its own and takes all of the tokens, 32 at a time:
 //   S^T = K Q^T with the queries in registers and K's rows as A operands,
@@ -600,10 +600,18 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 // tell the two stages apart, would wait for the next stage's loads before it reads this
 // one's. The load has no register to write; it is waited for (stage_came) before the
 // barrier after which its stage is read. M0 is set for it alone: nothing else here uses M0.
+// ONCE: the values of a call with one tile of rows need no cache, which keeps the keys for the
+// weight pass (64 requests of 14 to 42 rows over up to 16,000 tokens: 146 us and 83 for the weight,
+// 153 and 90 without; 8 such requests of 42 to 63 rows 29.8, 27.5 without).
+template <bool ONCE>
 __device__ __forceinline__ void load_to_lds(const u32x4& buffer, uint32_t to, int off)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(buffer)
-                 : "memory");
+    if constexpr (ONCE)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(to), "v"(off), "s"(buffer)
+                     : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(buffer)
+                     : "memory");
 }
 __device__ __forceinline__ void stage_came() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
@@ -702,13 +710,13 @@ __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
             lds_n[st & 1][half0] = k.n;
             const uint32_t to = uniform((int)(uint32_t)(uintptr_t)(lds_byte*)lds_k[st & 1]) + half0 * 16 * RB;
 #pragma unroll
-            for (int n = 0; n < NI; ++n) load_to_lds(k.words, to + n * 1024, ko[n]);
+            for (int n = 0; n < NI; ++n) load_to_lds<false>(k.words, to + n * 1024, ko[n]);
         }
         if (does_v) {
             const Half v = half_of(vb, a.c.v_page, a.c.v_tok, row_bytes, page, tok, hi, mask);
             const uint32_t to = uniform((int)(uint32_t)(uintptr_t)(lds_byte*)lds_v[st & 1]) + half0 * 16 * RB;
 #pragma unroll
-            for (int n = 0; n < NI; ++n) load_to_lds(v.words, to + n * 1024, vo[n]);
+            for (int n = 0; n < NI; ++n) load_to_lds<MT == 1 && DP != 256>(v.words, to + n * 1024, vo[n]);
         }
     };
 
@@ -1235,16 +1243,17 @@ int padded_dim(int dim) { return dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 
 
 int64_t pairs(const AttendArgs& a) { return (int64_t)a.c.n_seqs * a.c.kv_heads; }
 
-// k_attend_rows: 32 rows a wavefront, four wavefronts, stages of 64 tokens. Chunks of 2,048
+// k_attend_rows from 33 rows on: stages of 64 tokens serve all four wavefronts, where k_attend reads
+// a tile once for each 32 rows (64 requests over up to 16,000 tokens: 42 to 63 rows 153 us, 205
+// through k_attend; 70 to 126 rows 272, 461; one of 100,000 tokens with 126 rows 61, 91; 14 to 28
+// rows 150, 146 through k_attend). Up to 64 rows 16 a wavefront (162 us, with 32 and two
+// wavefronts idle 168), beyond 32 a wavefront. Chunks of 2,048
 // over 12,288 tokens: 730 us, with 48 rows a wavefront 884 (246 registers, as fast a SIMD but
 // fewer workgroups; 64 spill), 16 rows and eight wavefronts 770, stages of 32 tokens 852 (each
-// pair by pair; in levels 700-717). With fewer than kManyRows rows its wavefronts would be idle
-// or its tokens not spread: k_attend. Heads of 256: 16 rows a wavefront and stages of 32, for
+// pair by pair; in levels 700-717). Heads of 256: 16 rows a wavefront and stages of 32, for
 // the same registers and LDS (the same chunks 1.70 ms, 6.26 through k_attend).
-constexpr int kManyRows = 128;
-constexpr int row_tiles_of(int dp) { return dp == 256 ? 1 : 2; }
+constexpr int kManyRows = 33;
 constexpr int stage_of(int dp) { return dp == 256 ? 32 : 64; }
-constexpr int many_rows(int dp) { return row_tiles_of(dp) * 16 * kWaves; }
 // Rows of a workgroup: what the registers of its wavefronts hold.
 template <int DT, int DP>
 int attend_rows(const AttendArgs& a, void* st, void* e0, void* e1)
@@ -1252,12 +1261,17 @@ int attend_rows(const AttendArgs& a, void* st, void* e0, void* e1)
     const int64_t blocks = pairs(a) * a.row_tiles * a.splits;
     if (a.tile_rows == 16) return enqueue(k_attend<DT, DP, 1, 1>, blocks, st, e0, e1, a);
     if constexpr (DT == kBF16)
-        if (a.many) return enqueue(k_attend_rows<DP, row_tiles_of(DP), kWaves, stage_of(DP), DP == 64 ? 3 : 2>, blocks, st, e0, e1, a);
+        if (a.many) {
+            if (a.tile_rows == 64) return enqueue(k_attend_rows<DP, 1, kWaves, stage_of(DP), DP == 64 ? 3 : 2>, blocks, st, e0, e1, a);
+            if constexpr (DP != 256)
+                return enqueue(k_attend_rows<DP, 2, kWaves, stage_of(DP), DP == 64 ? 3 : 2>, blocks, st, e0, e1, a);
+        }
     if constexpr (DP == 256) {
         if (a.tile_rows == 32) return enqueue(k_attend<DT, DP, 1, 2>, blocks, st, e0, e1, a);
     } else {
         if (a.tile_rows == 32) return enqueue(k_attend<DT, DP, 2, 1>, blocks, st, e0, e1, a);
-        if (a.tile_rows == 64) return enqueue(k_attend<DT, DP, 2, 2>, blocks, st, e0, e1, a);
+        if constexpr (DT == kF32)
+            if (a.tile_rows == 64) return enqueue(k_attend<DT, DP, 2, 2>, blocks, st, e0, e1, a);
     }
     return (int)hipErrorInvalidValue;
 }
@@ -1320,7 +1334,7 @@ void attend_shape(AttendArgs& a)
     const int most = padded_dim(a.c.dim) == 256 ? 32 : 64;  // rows of a workgroup of k_attend at most
     a.tile_rows = rows <= 16 ? 16 : rows <= 32 || most == 32 ? 32 : 64;
     a.many = a.dtype == kBF16 && rows >= kManyRows;
-    if (a.many) a.tile_rows = many_rows(padded_dim(a.c.dim));
+    if (a.many) a.tile_rows = rows <= 64 || padded_dim(a.c.dim) == 256 ? 64 : 128;
     a.row_tiles = (int)((rows + a.tile_rows - 1) / a.tile_rows);
     const int64_t np = std::max<int64_t>(pairs(a), 1), groups = std::max<int64_t>(np * a.row_tiles, 1), cap = capacity(a.c);
     auto up = [](int64_t v, int64_t to) { return (v + to - 1) / to * to; };

@@ -213,3 +213,34 @@ def test_a_key_at_minus_infinity_gives_nothing(dtype, n, dim, heads):
     torch.cuda.synchronize()
     for a, b in zip(*out):
         assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "all"])
+@pytest.mark.parametrize("heads,kv_heads,dim,page", [(33, 1, 64, 16), (10, 2, 88, 32), (7, 1, 96, 16), (14, 2, 120, 64), (7, 1, 128, 16),
+                                                     (8, 1, 256, 32), (14, 2, 176, 16)])
+def test_rows_of_one_tile(heads, kv_heads, dim, page, causal):
+    """33 to 64 rows: a single token of many heads, drafts; holes, tails, sequences of none; split and not."""
+    n = 64 * kv_heads // heads
+    new = [n, max(1, n - 1), 0, 1, n]
+    check(Case(17, [333, 150, 0, 31, 64], new, heads, kv_heads, dim, page, BF16, bad_page=(0, 1, -1), extra_rows=2), causal)
+    check(Case(18, [3000, n], [n, n], heads, kv_heads, dim, page, BF16, bad_page=(0, 2, 10 ** 6)), causal, scale=-0.2)
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")], ids=str)
+@pytest.mark.parametrize("dim,heads", [(128, 14), (96, 14), (64, 10), (256, 14)])
+def test_values_not_seen_by_rows_of_one_tile(value, dim, heads):
+    """Only the rows that see the token get its value."""
+    import paper_2604_02945_amd as msao
+    L, n, bad = 150, 9, 4
+    case = Case(19, [L, 33], [n, 2], heads, 2, dim, 16, BF16)
+    j = L - n + bad
+    clean, start = case.device(DEV)
+    want = msao.msao_cache_attention(clean, start, n, case.q.to(DEV))
+    case.v[int(case.pages[0, j // 16]), 1, j % 16, 5] = value
+    cache, _ = case.device(DEV)
+    got = msao.msao_cache_attention(cache, start, n, case.q.to(DEV))
+    torch.cuda.synchronize()
+    hit = torch.zeros(n + 2, heads, dim, dtype=torch.bool)
+    hit[bad:n, heads // 2:, 5] = True
+    assert torch.equal(got.cpu()[~hit], want.cpu()[~hit])
+    assert (torch.isnan(got.cpu()[hit]) if value != value else got.cpu()[hit] == value).all()
