@@ -3,10 +3,10 @@
 //
 // Rows of a (sequence, kv head) are its n new tokens times the `group` query heads
 // that share the kv head: all of them read the same keys and values, so they fill the
-// columns of the matrix instructions, and K and V are read once for up to 64 rows.
+// columns of the matrix instructions, and K and V are read once for up to 128 rows.
 //
-// k_attend: a wavefront takes 32 tokens at a time, K and V straight from memory into
-// registers in whole rows, and nothing through LDS:
+// k_attend (up to 16 rows of bf16; float32): a wavefront takes 32 tokens at a time, K and V
+// straight from memory into registers in whole rows, and nothing through LDS:
 //   S^T = K Q^T    A operand: lane (c, i) holds 16 bytes of token i's row
 //   O^T = V^T P^T  S^T leaves lane (c, q) with tokens 4c..4c+3 of each 16, which is a
 //                  B operand as it stands once the instruction's k index is read as
@@ -16,7 +16,7 @@
 // The queries lie in LDS, from where each wavefront takes them tile by tile: what the
 // registers hold besides (K and V on their way, the output, the scores) then leaves two
 // wavefronts on a SIMD, so that loads, exponents and products of different ones overlap.
-// The wavefronts of a workgroup take tiles in turn (for more than 32 rows two of them
+// The wavefronts of a workgroup take tiles in turn (for more rows than one holds two of them
 // take the same tile, each for its half of the rows; the second reads it from a cache) and
 // join at the end through LDS; workgroups that share a row's tokens leave parts in the
 // workspace, which k_combine joins. The running maximum is a reference that moves only
@@ -270,7 +270,8 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArg
     constexpr int LDP = DP + 4;        // floats between rows in LDS: spreads the banks
     constexpr int TW = kWaves / RW;    // wavefronts that take different tiles
     // values that no other wavefront reads need no cache (long rows of one token: 176 -> 165 us);
-    // keys stay for the weight pass (read once too, its call takes 295 us instead of 267)
+    // keys stay for the weight pass (a call with it over 383 MB of keys: 295 us with keys read once
+    // too, 267 without)
     constexpr int kValuesOnce = RW == 1 ? kOnce : 0;
     constexpr int kQBytes = RW * MT * 16 * Queries<DT, DP>::kLine, kOBytes = kWaves * 16 * LDP * 4;
     __shared__ __align__(16) uint8_t lds[kQBytes > kOBytes ? kQBytes : kOBytes];
@@ -1243,35 +1244,41 @@ int padded_dim(int dim) { return dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 
 
 int64_t pairs(const AttendArgs& a) { return (int64_t)a.c.n_seqs * a.c.kv_heads; }
 
-// k_attend_rows from 33 rows on: stages of 64 tokens serve all four wavefronts, where k_attend reads
-// a tile once for each 32 rows (64 requests over up to 16,000 tokens: 42 to 63 rows 153 us, 205
-// through k_attend; 70 to 126 rows 272, 461; one of 100,000 tokens with 126 rows 61, 91; 14 to 28
-// rows 150, 146 through k_attend). Up to 64 rows 16 a wavefront (162 us, with 32 and two
-// wavefronts idle 168), beyond 32 a wavefront. Chunks of 2,048
-// over 12,288 tokens: 730 us, with 48 rows a wavefront 884 (246 registers, as fast a SIMD but
-// fewer workgroups; 64 spill), 16 rows and eight wavefronts 770, stages of 32 tokens 852 (each
-// pair by pair; in levels 700-717). Heads of 256: 16 rows a wavefront and stages of 32, for
-// the same registers and LDS (the same chunks 1.70 ms, 6.26 through k_attend).
-constexpr int kManyRows = 33;
+// bf16 rows go through k_attend_rows from 17 on: stages of 64 tokens serve all four wavefronts,
+// where k_attend reads a tile once for each 32 rows (64 requests of up to 16,000 tokens: with 21
+// to 28 rows 144 us, 151 through k_attend; 42 to 63 rows 153, 205; 70 to 126 rows 272, 461; one of
+// 100,000 tokens with 126 rows 61, 91). Up to 16 rows k_attend (7 rows of 64 requests 134 us,
+// 136 through the other; of 256 requests 185, 191; one row of two long ones 162, 164), but for
+// heads of 256, of which its registers hold one wavefront a SIMD (two rows 135 us, 108 through
+// the other). Up to 64 rows 16 rows a wavefront (42 to 63 rows: 162 us, with 32 and two
+// wavefronts idle 168), beyond 32 a wavefront. Chunks of 2,048 over 12,288 tokens: 730 us, with
+// 48 rows a wavefront 884 (246 registers, as fast a SIMD but fewer workgroups; 64 spill), 16
+// rows and eight wavefronts 770, stages of 32 tokens 852 (each pair by pair; in levels 700-720).
+// Heads of 256: 16 rows a wavefront and stages of 32, for the same registers and LDS (the
+// same chunks 1.70 ms, 6.26 through k_attend). float32 stays with k_attend: its products, not
+// its loads, are the bound.
+constexpr int kFewRows = 16;
 constexpr int stage_of(int dp) { return dp == 256 ? 32 : 64; }
 // Rows of a workgroup: what the registers of its wavefronts hold.
 template <int DT, int DP>
 int attend_rows(const AttendArgs& a, void* st, void* e0, void* e1)
 {
     const int64_t blocks = pairs(a) * a.row_tiles * a.splits;
-    if (a.tile_rows == 16) return enqueue(k_attend<DT, DP, 1, 1>, blocks, st, e0, e1, a);
-    if constexpr (DT == kBF16)
-        if (a.many) {
-            if (a.tile_rows == 64) return enqueue(k_attend_rows<DP, 1, kWaves, stage_of(DP), DP == 64 ? 3 : 2>, blocks, st, e0, e1, a);
-            if constexpr (DP != 256)
-                return enqueue(k_attend_rows<DP, 2, kWaves, stage_of(DP), DP == 64 ? 3 : 2>, blocks, st, e0, e1, a);
+    if constexpr (DT == kBF16) {
+        constexpr int kPerSimd = DP == 64 ? 3 : 2;
+        if (a.tile_rows == 64) return enqueue(k_attend_rows<DP, 1, kWaves, stage_of(DP), kPerSimd>, blocks, st, e0, e1, a);
+        if constexpr (DP != 256) {
+            if (a.tile_rows == 128) return enqueue(k_attend_rows<DP, 2, kWaves, stage_of(DP), kPerSimd>, blocks, st, e0, e1, a);
+            if (a.tile_rows == 16) return enqueue(k_attend<DT, DP, 1, 1>, blocks, st, e0, e1, a);
         }
-    if constexpr (DP == 256) {
-        if (a.tile_rows == 32) return enqueue(k_attend<DT, DP, 1, 2>, blocks, st, e0, e1, a);
     } else {
-        if (a.tile_rows == 32) return enqueue(k_attend<DT, DP, 2, 1>, blocks, st, e0, e1, a);
-        if constexpr (DT == kF32)
+        if (a.tile_rows == 16) return enqueue(k_attend<DT, DP, 1, 1>, blocks, st, e0, e1, a);
+        if constexpr (DP == 256) {
+            if (a.tile_rows == 32) return enqueue(k_attend<DT, DP, 1, 2>, blocks, st, e0, e1, a);
+        } else {
+            if (a.tile_rows == 32) return enqueue(k_attend<DT, DP, 2, 1>, blocks, st, e0, e1, a);
             if (a.tile_rows == 64) return enqueue(k_attend<DT, DP, 2, 2>, blocks, st, e0, e1, a);
+        }
     }
     return (int)hipErrorInvalidValue;
 }
@@ -1319,11 +1326,15 @@ template <int DT, int DP> struct Weight {
 
 // Parts of a row's tokens. Few rows: parts for kPartTarget workgroups if every sequence were
 // as long as can be, of 128 .. 1,024 tokens (a tile a wavefront at least; 64 requests of up to
-// 16,000 tokens: 166 us with 1,024, 178 with 512, 188 with 2,048; two of 131,072: 188, 198,
-// 186). Many rows, whose parts cost a store and a load of 4 bytes a channel: none from 512
-// workgroups on (8 prompts of up to 1,500 tokens 79 us, 107 with parts of 256), below that
-// parts for kManyTarget, or as many as for few rows with float32, whose products take eight
-// times as long (text over encoder states 70 us, 103 with parts for 512).
+// 16,000 tokens with 14 to 42 rows: 153 us with the join for 1,024, 173 with 512, 161 with 2,048;
+// two of 131,072 with one: 188 through a kernel of 166, 198, 186). More than 64 rows, whose
+// parts cost a store and a load of 4 bytes a channel: none from 512 workgroups on (8 prompts of
+// up to 1,500 tokens 79 us, 107 with parts of 256; 200 requests of up to 3,000 with 70 to 126 rows
+// 240, 260 with parts of 1,024), below that parts for kManyTarget (8 requests of up to 16,000 with
+// as many rows: 80 us), of at most 1,024 tokens where all rows are one workgroup's (64 requests: 346 us, 423
+// with 4,000). float32, whose
+// products take eight times as long, as many as for few rows (text over encoder states 70 us,
+// 103 with parts for 512).
 constexpr int64_t kPartTarget = 2048, kPartLeast = 128, kPartMost = 1024, kManyTarget = 1024, kManyTargetF32 = 4096;
 // Parts of the tokens in the weight pass of few rows (attend_round 91 us; 93 with 8,192), and
 // of the rows in that of many: up to 32 (25 us, 33 with 10).
@@ -1331,10 +1342,9 @@ constexpr int64_t kWeightTarget = 16384, kWeightLeast = 256, kWeightRowTarget = 
 void attend_shape(AttendArgs& a)
 {
     const int64_t rows = (int64_t)a.ch.max_new * a.group.n;
-    const int most = padded_dim(a.c.dim) == 256 ? 32 : 64;  // rows of a workgroup of k_attend at most
-    a.tile_rows = rows <= 16 ? 16 : rows <= 32 || most == 32 ? 32 : 64;
-    a.many = a.dtype == kBF16 && rows >= kManyRows;
-    if (a.many) a.tile_rows = rows <= 64 || padded_dim(a.c.dim) == 256 ? 64 : 128;
+    const bool wide = padded_dim(a.c.dim) == 256;
+    if (a.dtype == kBF16) a.tile_rows = rows <= kFewRows && !wide ? 16 : rows <= 64 || wide ? 64 : 128;
+    else a.tile_rows = rows <= 16 ? 16 : rows <= 32 || wide ? 32 : 64;
     a.row_tiles = (int)((rows + a.tile_rows - 1) / a.tile_rows);
     const int64_t np = std::max<int64_t>(pairs(a), 1), groups = std::max<int64_t>(np * a.row_tiles, 1), cap = capacity(a.c);
     auto up = [](int64_t v, int64_t to) { return (v + to - 1) / to * to; };
@@ -1343,7 +1353,9 @@ void attend_shape(AttendArgs& a)
     int64_t per = std::min<int64_t>(up((groups * cap + kPartTarget - 1) / kPartTarget, kPartLeast), kPartMost);
     if (rows > 64) {
         const int64_t target = a.dtype == kBF16 ? kManyTarget : kManyTargetF32;
-        per = groups >= target / 2 ? whole : up((groups * cap + target - 1) / target, kPartLeast);
+        per = up((groups * cap + target - 1) / target, kPartLeast);
+        if (a.row_tiles == 1) per = std::min(per, kPartMost);
+        if (groups >= target / 2) per = whole;
     }
     a.part_tokens = (int)std::min(std::max<int64_t>(per, kPartLeast), whole);
     a.splits = std::max(1, parts_of((int)cap, a.part_tokens));

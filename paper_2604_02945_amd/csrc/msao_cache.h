@@ -144,7 +144,6 @@ struct AttendArgs {
     int32_t part_tokens;           // tokens of a part
     int32_t splits, row_tiles;     // most parts of a group of rows; groups of a (sequence, kv head)
     int32_t tile_rows;             // rows of a group
-    int32_t many;                  // they go through k_attend_rows
     int32_t weight_tokens;         // tokens of a part in the weight pass
     int32_t weight_parts;          // most of them for each (sequence, kv head)
     int32_t row_parts;             // and of the rows
