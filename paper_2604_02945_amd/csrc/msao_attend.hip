@@ -544,8 +544,9 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArg
             for (int w = 0; w < TW; ++w) mm = fmaxf(mm, lds_m[w * RW + g][line]);
 #pragma unroll
             for (int w = 0; w < TW; ++w) {
-                const float mw = lds_m[w * RW + g][line];
-                l += mw == -INFINITY ? 0.0f : lds_l[w * RW + g][line] * __builtin_amdgcn_exp2f(mw - mm);
+                // (a reference that never moved: the sum is 0, or NaN where a score was NaN, which moves none)
+                const float mw = lds_m[w * RW + g][line], lw = lds_l[w * RW + g][line];
+                l += mw == -INFINITY ? lw : lw * __builtin_amdgcn_exp2f(mw - mm);
             }
 #pragma unroll
             for (int t = 0; t < E; ++t) {
