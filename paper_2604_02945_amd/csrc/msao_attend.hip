@@ -103,6 +103,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf2));
 }
 
+// A channel's sum by the weights' sum l (inv = 1 / l). A row of no token, or of scores of -inf
+// alone, has l 0 (the largest score's term is near 1 otherwise) and is 0, whatever its sum of
+// values times 0 is: NaN where a value is not finite.
+__device__ __forceinline__ float normed(float acc, float inv, float l) { return l == 0.0f ? 0.0f : acc * inv; }
+
 // N values to 8- or 16-byte aligned memory (4 bytes for two of bf16).
 template <int DT, int N>
 __device__ __forceinline__ void store_values(uint8_t* dst, const float* v)
@@ -557,14 +562,14 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArg
             const int tok = a.group.of(row), head = p.head * a.group.n + (row - tok * a.group.n);
             const int64_t at = (int64_t)(p.begin + tok) * a.heads + head;
             if (parts <= 1) {
-                const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+                const float inv = 1.0f / l;
                 uint8_t* dst = a.out + (int64_t)(p.begin + tok) * a.out_stride + ((int64_t)head * a.c.dim + od) * ES;
                 // (the head's last channels may be part of what the thread has)
 #pragma unroll
                 for (int t = 0; t < E; t += S) {
                     if (od + t >= a.c.dim) break;
 #pragma unroll
-                    for (int e = 0; e < S; ++e) acc[t + e] *= inv;
+                    for (int e = 0; e < S; ++e) acc[t + e] = normed(acc[t + e], inv, l);
                     store_values<DT, S>(dst + ES * t, &acc[t]);
                 }
                 if (od == 0) {
@@ -871,13 +876,14 @@ __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
         const int tok = a.group.of(row), head = p.head * a.group.n + (row - tok * a.group.n);
         const int64_t at = (int64_t)(p.begin + tok) * a.heads + head;
         if (parts <= 1) {
-            const float inv = sum[m] == 0.0f ? 0.0f : 1.0f / sum[m];
+            const float inv = 1.0f / sum[m];
+            auto of = [&](int t, int r) { return normed(o[m][t][r], inv, sum[m]); };
             uint8_t* dst = a.out + (int64_t)(p.begin + tok) * a.out_stride + (int64_t)head * row_bytes;
 #pragma unroll
             for (int t = 0; t < VT; ++t) {
                 const int ch = 16 * t + 4 * c;
                 if (ch < a.c.dim)
-                    *(u32x2*)(dst + 2 * ch) = u32x2{pack_bf16(o[m][t][0] * inv, o[m][t][1] * inv), pack_bf16(o[m][t][2] * inv, o[m][t][3] * inv)};
+                    *(u32x2*)(dst + 2 * ch) = u32x2{pack_bf16(of(t, 0), of(t, 1)), pack_bf16(of(t, 2), of(t, 3))};
             }
             if (c == 0) {
                 const float z = sum[m] == 0.0f ? -INFINITY : ref[m] + __builtin_amdgcn_logf(sum[m]);
@@ -965,11 +971,13 @@ __global__ __launch_bounds__(kBlock) void k_combine(AttendArgs a, int blocks_per
             join(d[0], d[1], f32x4{d[2], d[3], d[4], d[5]});
         }
     } else if (lane >= LP) return;
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const float inv = 1.0f / l;
     uint8_t* dst = a.out + (int64_t)(p.begin + tok) * a.out_stride + ((int64_t)head * a.c.dim + ch) * ES;
     if (has) {
-        if constexpr (DT == kBF16) *(u32x2*)dst = u32x2{pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)};
-        else *(f32x4*)dst = f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = normed(acc[e], inv, l);
+        if constexpr (DT == kBF16) *(u32x2*)dst = u32x2{pack_bf16(acc[0], acc[1]), pack_bf16(acc[2], acc[3])};
+        else *(f32x4*)dst = acc;
     }
     if (ch == 0) {
         const float z = l == 0.0f ? -INFINITY : most + __builtin_amdgcn_logf(l);

@@ -71,3 +71,25 @@ def test_a_nan_key_alone_in_its_tile(dtype, n, heads, dim, length):
     seen = torch.zeros(w.shape, dtype=torch.bool)
     seen[0, 1, :length] = True
     same_but(w, w0, seen)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 8, 20, 40])
+@pytest.mark.parametrize("heads,dim", [(4, 64), (2, 96), (4, 128), (2, 256)])
+@pytest.mark.parametrize("length", [70, 1300], ids=["whole", "split"])
+@pytest.mark.parametrize("value", [float("inf"), float("nan")], ids=str)
+def test_only_scores_of_minus_infinity(dtype, n, heads, dim, length, value):
+    """Rows without a score above -inf are empty, whatever the values hold: out 0, lse -inf, no weight."""
+    case = Case(73, [length, 40], [n, 2], heads, 2, dim, 16, dtype)
+    out0, lse0, w0 = attend(case)
+    case.q[:n, :, 0] = case.q[:n, :, 0].abs() + 1
+    for j in range(length):
+        case.k[int(case.pages[0, j // 16]), 1, j % 16, 0] = float("-inf")
+    for j in (0, length // 2, length - n, length - 1):  # tiles that every row sees, and those of the chunk
+        case.v[int(case.pages[0, j // 16]), 1, j % 16, 2] = value
+    out, lse, w = attend(case)
+    G = heads // 2
+    assert (out[:n, G:] == 0).all() and (lse[:n, G:] == -np.inf).all()
+    assert torch.equal(w[0, 1], case.weight[0, 1])
+    assert torch.equal(out[n:], out0[n:]) and torch.equal(lse[n:], lse0[n:]) and torch.equal(w[1], w0[1])
+    assert torch.isfinite(out[:n, :G]).all() and torch.isfinite(lse[:n, :G]).all() and torch.isfinite(w[0, 0]).all()
