@@ -591,7 +591,9 @@ msao_status msao_cache_append(msao_ctx* ctx, const msao_kv_cache* cache, const m
  * heads of the kv head; the order of every sum is fixed: the same call gives the
  * same bits. For bf16, the p_ij that multiply v are rounded to bf16; sums, lse and
  * weight are not. Workspace from msao_cache_attention_workspace, used only while
- * the call runs on the GPU. */
+ * the call runs on the GPU. A call of 2^24 workgroups or more gives MSAO_ERR_UNSUPPORTED: one takes
+ * 16 to 128 rows of a (sequence, kv head) and 128 tokens or more, the weight of more than 64 rows
+ * 128 tokens, with the capacity and max_new for every sequence. */
 msao_status msao_cache_attention(msao_ctx* ctx, const msao_kv_cache* cache, const msao_chunk* chunk, const void* q,
                                  int64_t q_stride, int heads, float scale, uint32_t flags, void* out,
                                  int64_t out_stride, float* lse, void* workspace, size_t workspace_bytes,

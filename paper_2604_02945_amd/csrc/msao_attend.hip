@@ -1253,6 +1253,9 @@ int padded_dim(int dim) { return dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 
 
 int64_t pairs(const AttendArgs& a) { return (int64_t)a.c.n_seqs * a.c.kv_heads; }
 
+// Of rows with many parts k_combine has the whole block on one row.
+bool block_a_row(const AttendArgs& a) { return a.splits > 16; }
+
 // bf16 rows go through k_attend_rows from 17 on: stages of 64 tokens serve all four wavefronts,
 // where k_attend reads a tile once for each 32 rows (64 requests of up to 16,000 tokens: with 21
 // to 28 rows 144 us, 151 through k_attend; 42 to 63 rows 153, 205; 70 to 126 rows 272, 461; one of
@@ -1272,7 +1275,7 @@ constexpr int stage_of(int dp) { return dp == 256 ? 32 : 64; }
 template <int DT, int DP>
 int attend_rows(const AttendArgs& a, void* st, void* e0, void* e1)
 {
-    const int64_t blocks = pairs(a) * a.row_tiles * a.splits;
+    const int64_t blocks = pairs(a) * attend_blocks(a).attend;
     if constexpr (DT == kBF16) {
         constexpr int kPerSimd = DP == 64 ? 3 : 2;
         if (a.tile_rows == 64) return enqueue(k_attend_rows<DP, 1, kWaves, stage_of(DP), kPerSimd>, blocks, st, e0, e1, a);
@@ -1295,17 +1298,15 @@ int attend_rows(const AttendArgs& a, void* st, void* e0, void* e1)
 template <int DT, int DP>
 int combine_rows(const AttendArgs& a, void* st, void* e0, void* e1)
 {
-    const int rows = a.ch.max_new * a.group.n;
-    // many parts: the whole block on one row
-    if (a.splits > 16) return enqueue(k_combine<DT, DP, kWaves>, pairs(a) * rows, st, e0, e1, a, rows);
-    const int per = (rows + kWaves - 1) / kWaves;
-    return enqueue(k_combine<DT, DP, 1>, pairs(a) * per, st, e0, e1, a, per);
+    const int per = (int)attend_blocks(a).combine;
+    return block_a_row(a) ? enqueue(k_combine<DT, DP, kWaves>, pairs(a) * per, st, e0, e1, a, per)
+                          : enqueue(k_combine<DT, DP, 1>, pairs(a) * per, st, e0, e1, a, per);
 }
 
 template <int DT, int DP>
 int weight_rows(const AttendArgs& a, void* st, void* e0, void* e1)
 {
-    const int64_t blocks = pairs(a) * a.weight_parts * a.row_parts;
+    const int64_t blocks = pairs(a) * attend_blocks(a).weight;
     const int64_t rows = (int64_t)a.ch.max_new * a.group.n;
     if (rows > kRowStep) return enqueue(k_weight_rows<DT, DP>, blocks, st, e0, e1, a);
     return rows <= 16 ? enqueue(k_weight<DT, DP, 1>, blocks, st, e0, e1, a) : enqueue(k_weight<DT, DP, 4>, blocks, st, e0, e1, a);
@@ -1380,6 +1381,16 @@ void attend_shape(AttendArgs& a)
     }
 }
 
+AttendBlocks attend_blocks(const AttendArgs& a)
+{
+    const int64_t rows = (int64_t)a.ch.max_new * a.group.n;
+    AttendBlocks b{(int64_t)a.row_tiles * a.splits, 0, 0, 0};
+    if (a.splits > 1) b.combine = block_a_row(a) ? rows : (rows + kWaves - 1) / kWaves;
+    if (a.add_weight) b.weight = (int64_t)a.weight_parts * a.row_parts;
+    if (a.add_weight && a.row_parts > 1) b.join = ((int64_t)capacity(a.c) + 4 * kBlock - 1) / (4 * kBlock);
+    return b;
+}
+
 AttendBytes attend_bytes(const AttendArgs& a)
 {
     const size_t rows = (size_t)a.ch.n_rows * (size_t)a.heads;
@@ -1408,7 +1419,7 @@ int launch_weight(const AttendArgs& a, void* st, void* e0, void* e1)
 int launch_weight_join(const AttendArgs& a, void* st, void* e0, void* e1)
 {
     if (!a.add_weight || a.row_parts <= 1) return kNoLaunch;
-    const int per = (capacity(a.c) + 4 * kBlock - 1) / (4 * kBlock);
+    const int per = (int)attend_blocks(a).join;
     return enqueue(k_weight_join, pairs(a) * per, st, e0, e1, a, per);
 }
 

@@ -184,6 +184,11 @@ void append_shape(AppendArgs& a);
 void evict_shape(EvictArgs& a);
 // Launch shape of an attention call: fills part_tokens .. row_parts.
 void attend_shape(AttendArgs& a);
+// Workgroups that its kernels launch for each (sequence, kv head); 0: no such launch.
+struct AttendBlocks {
+    int64_t attend, combine, weight, join;
+};
+AttendBlocks attend_blocks(const AttendArgs& a);
 // Bytes of each of its workspace arrays.
 struct AttendBytes {
     size_t part_o, part_ml, lse2, part_w;

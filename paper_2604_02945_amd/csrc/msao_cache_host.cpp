@@ -200,8 +200,8 @@ msao_status attend_plan(const msao_kv_cache* cache, const msao_chunk* chunk, int
     a.add_weight = flags & MSAO_ATTEND_WEIGHT ? 1 : 0;
     attend_shape(a);
     const int64_t groups = (int64_t)a.c.n_seqs * a.c.kv_heads;
-    const int64_t most = std::max<int64_t>(std::max<int64_t>((int64_t)a.row_tiles * a.splits, (int64_t)a.ch.max_new * a.group.n),
-                                           std::max<int64_t>((int64_t)a.weight_parts * a.row_parts, a.c.per_seq * (int64_t)cache->page_size / 256 + 1));
+    const AttendBlocks n = attend_blocks(a);
+    const int64_t most = std::max(std::max(n.attend, n.combine), std::max(n.weight, n.join));
     if (groups > 0 && most > kMaxBlocks / groups) return fail(err, MSAO_ERR_UNSUPPORTED, "more workgroups than one launch takes");
     const AttendBytes b = attend_bytes(a);
     pl.part_o = 0;

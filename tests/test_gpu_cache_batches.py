@@ -1,0 +1,80 @@
+"""Attention of large batches over a paged cache against its definition in 64 bits (on
+the GPU: products of many sequences)."""
+import numpy as np
+import pytest
+import torch
+
+from cache_ref import Case, tolerances
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def attention64(case, scale, causal):
+    """Case.attention, a kv head's rows at a time."""
+    out, mag = (torch.zeros(case.rows, case.heads, case.dim, dtype=torch.float64, device=DEV) for _ in range(2))
+    lse = torch.zeros(case.rows, case.heads, dtype=torch.float64, device=DEV)
+    weight = case.weight.double().to(DEV)
+    span = torch.zeros((), dtype=torch.float64, device=DEV)
+    G, K = case.heads // case.kv_heads, case.kv_heads
+    for b in range(case.B):
+        n, m, at = case.lengths[b], case.new[b], int(case.start[b])
+        if n == 0 or m == 0:
+            continue
+        k, v, _ = case.tokens(b)
+        k, v = torch.from_numpy(k).to(DEV), torch.from_numpy(v).to(DEV)
+        q = case.q[at:at + m].double().to(DEV).view(m, K, G, case.dim).permute(1, 0, 2, 3).reshape(K, m * G, case.dim)
+        kt = k.transpose(1, 2).contiguous()
+        s = scale * torch.bmm(q.contiguous(), kt)
+        span = torch.maximum(span, scale * torch.bmm(q.abs(), kt.abs()).max())
+        if causal:
+            tok = torch.arange(m, device=DEV).repeat_interleave(G)[:, None]
+            s.masked_fill_(torch.arange(n, device=DEV)[None] > n - m + tok, -np.inf)
+        z = torch.logsumexp(s, -1, keepdim=True)
+        p = torch.exp(s - z)
+        weight[b, :, :n] += p.sum(1)
+        back = lambda x: x.view(K, m, G, -1).permute(1, 0, 2, 3).reshape(m, case.heads, -1)  # noqa: E731
+        out[at:at + m], mag[at:at + m] = back(torch.bmm(p, v)), back(torch.bmm(p, v.abs()))
+        lse[at:at + m] = back(z)[..., 0]
+    return out.cpu().numpy(), lse.cpu().numpy(), weight.cpu().numpy(), mag.cpu().numpy(), float(span)
+
+
+def check(case, accumulate=True, per=None, causal=True):
+    """`per`: columns of a page table wider than the sequences need. Returns the workspace's bytes."""
+    import paper_2604_02945_amd as msao
+    if per is not None:
+        wide = np.full((case.B, per), -3, np.int32)
+        wide[:, :case.per] = case.pages
+        case.pages = wide
+        if accumulate:
+            old = case.weight
+            case.weight = torch.zeros(case.B, case.kv_heads, per * case.page)
+            case.weight[..., :old.shape[2]] = old
+    cache, start = case.device(DEV, with_weight=accumulate)
+    scale = case.dim ** -0.5
+    out = torch.full((case.rows, case.heads, case.dim), 7.0, dtype=case.dtype, device=DEV)
+    lse = torch.full((case.rows, case.heads), 7.0, device=DEV)
+    msao.msao_cache_attention(cache, start, case.max_new, case.q.to(DEV), causal=causal, out=out, lse=lse, accumulate=accumulate)
+    torch.cuda.synchronize()
+    want, z, weight, mag, span = attention64(case, scale, causal)
+    tol_z, tol = tolerances(case, mag, span, want)
+    assert np.abs(lse.double().cpu().numpy() - z).max() <= tol_z
+    assert (np.abs(out.double().cpu().numpy() - want) <= tol).all()
+    if accumulate:
+        rows = case.max_new * case.heads // case.kv_heads
+        tol_w = (2 * tol_z + (rows + 4) * 2.0 ** -24) * (weight + 1)
+        assert (np.abs(cache.weight.double().cpu().numpy() - weight) <= tol_w).all()
+    return msao.cache_attention_workspace(cache, start, case.rows, case.max_new, case.heads, causal, accumulate)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("accumulate", [False, True], ids=["out", "weight"])
+def test_one_prompts_chunk_beside_generating_requests(dtype, accumulate):
+    """256 requests of 32 heads, one with 2,048 new tokens."""
+    rng = np.random.RandomState(0)
+    lengths = rng.randint(1, 120, 256).tolist()
+    lengths[77] = 2100
+    new = [1] * 256
+    new[77] = 2048
+    check(Case(91, lengths, new, 32, 8, 64, 64, dtype), accumulate)
