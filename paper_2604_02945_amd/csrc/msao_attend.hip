@@ -1351,12 +1351,13 @@ constexpr int64_t kPartTarget = 2048, kPartLeast = 128, kPartMost = 1024, kManyT
 constexpr int64_t kWeightTarget = 16384, kWeightLeast = 256, kWeightRowTarget = 8192, kMostRowParts = 32;
 void attend_shape(AttendArgs& a)
 {
+    constexpr int64_t kMostGroups = (int64_t)1 << 30;  // more than a launch has; times a capacity below 2^60
     const int64_t rows = (int64_t)a.ch.max_new * a.group.n;
     const bool wide = padded_dim(a.c.dim) == 256;
     if (a.dtype == kBF16) a.tile_rows = rows <= kFewRows && !wide ? 16 : rows <= 64 || wide ? 64 : 128;
     else a.tile_rows = rows <= 16 ? 16 : rows <= 32 || wide ? 32 : 64;
     a.row_tiles = (int)((rows + a.tile_rows - 1) / a.tile_rows);
-    const int64_t np = std::max<int64_t>(pairs(a), 1), groups = std::max<int64_t>(np * a.row_tiles, 1), cap = capacity(a.c);
+    const int64_t np = std::max<int64_t>(pairs(a), 1), groups = std::min(std::max<int64_t>(np * a.row_tiles, 1), kMostGroups), cap = capacity(a.c);
     auto up = [](int64_t v, int64_t to) { return (v + to - 1) / to * to; };
     const int64_t whole = std::max<int64_t>(up(cap, kTile), kTile);
     // parts for about kPartTarget workgroups if every sequence were as long as can be

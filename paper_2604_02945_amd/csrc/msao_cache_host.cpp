@@ -198,8 +198,10 @@ msao_status attend_plan(const msao_kv_cache* cache, const msao_chunk* chunk, int
     a.dtype = cache->dtype;
     a.causal = flags & MSAO_ATTEND_CAUSAL ? 1 : 0;
     a.add_weight = flags & MSAO_ATTEND_WEIGHT ? 1 : 0;
-    attend_shape(a);
     const int64_t groups = (int64_t)a.c.n_seqs * a.c.kv_heads;
+    // (before the shape, whose products of counts would pass 63 bits)
+    if (groups > kMaxBlocks) return fail(err, MSAO_ERR_UNSUPPORTED, "more workgroups than one launch takes");
+    attend_shape(a);
     const AttendBlocks n = attend_blocks(a);
     const int64_t most = std::max(std::max(n.attend, n.combine), std::max(n.weight, n.join));
     if (groups > 0 && most > kMaxBlocks / groups) return fail(err, MSAO_ERR_UNSUPPORTED, "more workgroups than one launch takes");

@@ -31,3 +31,11 @@ def test_ordinary_batches_are_taken(n_seqs, capacity, n_rows, max_new, flags):
 def test_more_workgroups_than_a_launch_takes(flags):
     assert attention_workspace(1 << 14, 4096, 1 << 20, 1 << 14, flags=flags)[0] == UNSUP
     assert attention_workspace(1 << 22, 64, 1 << 22, 1, flags=flags)[0] == UNSUP
+
+
+@pytest.mark.parametrize("flags", [1, 3], ids=["causal", "weight"])
+@pytest.mark.parametrize("n_seqs,kv_heads,n_rows,max_new", [(1 << 27, 1 << 15, 1000, 1000), (2 ** 31 - 1, 65535, 100, 100),
+                                                            (1 << 26, 1 << 15, 10, 1), (511, 1 << 15, 60000, 60000)])
+def test_counts_whose_products_pass_64_bits_are_refused(n_seqs, kv_heads, n_rows, max_new, flags):
+    got = attention_workspace(n_seqs, 1 << 29, n_rows, max_new, heads=kv_heads, kv_heads=kv_heads, flags=flags, page=65536)
+    assert got[0] == UNSUP, message()
