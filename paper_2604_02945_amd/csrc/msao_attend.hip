@@ -1344,8 +1344,13 @@ template <int DT, int DP> struct Weight {
 // as many rows: 80 us), of at most 1,024 tokens where all rows are one workgroup's (64 requests: 346 us, 423
 // with 4,000). float32, whose
 // products take eight times as long, as many as for few rows (text over encoder states 70 us,
-// 103 with parts for 512).
-constexpr int64_t kPartTarget = 2048, kPartLeast = 128, kPartMost = 1024, kManyTarget = 1024, kManyTargetF32 = 4096;
+// 103 with parts for 512). Never parts for more than kMostParts workgroups: the workspace holds
+// a part's output for each row of every sequence as if it were as long as the table allows, 3 to
+// 50 GiB for 256 requests in tables of 2^17 to 2^20 tokens by parts of 1,024. (In a table of
+// 2^17, against parts of 1,024: 256 requests of up to 3,000 tokens with 24 rows 457 us, 581; one of
+// 100,000 among them 508, 628; 64 of up to 16,000 with 4 rows 224, 216, and with one of 120,000
+// 296, 290; with 24 rows 313, 376.)
+constexpr int64_t kPartTarget = 2048, kPartLeast = 128, kPartMost = 1024, kManyTarget = 1024, kManyTargetF32 = 4096, kMostParts = 16384;
 // Parts of the tokens in the weight pass of few rows (attend_round 91 us; 93 with 8,192), and
 // of the rows in that of many: up to 32 (25 us, 33 with 10).
 constexpr int64_t kWeightTarget = 16384, kWeightLeast = 256, kWeightRowTarget = 8192, kMostRowParts = 32;
@@ -1368,6 +1373,7 @@ void attend_shape(AttendArgs& a)
         if (a.row_tiles == 1) per = std::min(per, kPartMost);
         if (groups >= target / 2) per = whole;
     }
+    per = std::max(per, up((groups * cap + kMostParts - 1) / kMostParts, kPartLeast));  // (a multiple of a stage)
     a.part_tokens = (int)std::min(std::max<int64_t>(per, kPartLeast), whole);
     a.splits = std::max(1, parts_of((int)cap, a.part_tokens));
     a.row_parts = 1;

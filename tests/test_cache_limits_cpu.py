@@ -39,3 +39,22 @@ def test_more_workgroups_than_a_launch_takes(flags):
 def test_counts_whose_products_pass_64_bits_are_refused(n_seqs, kv_heads, n_rows, max_new, flags):
     got = attention_workspace(n_seqs, 1 << 29, n_rows, max_new, heads=kv_heads, kv_heads=kv_heads, flags=flags, page=65536)
     assert got[0] == UNSUP, message()
+
+
+MIB = 1 << 20
+
+
+@pytest.mark.parametrize("dtype", [B.BF16, B.F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("n_seqs,heads,kv_heads,new", [(256, 32, 8, 6), (256, 64, 8, 6), (64, 64, 8, 1), (48, 128, 8, 8), (1024, 32, 8, 1)])
+@pytest.mark.parametrize("capacity", [1 << 17, 1 << 20])
+def test_the_workspace_of_wide_tables_is_bounded(n_seqs, heads, kv_heads, new, capacity, dtype):
+    """Parts of at least pairs * capacity / 16,384 tokens: at most 16,384 / pairs and one for the
+    rounding, with 128 channels and two sums in 32 bits for each row."""
+    rc, n = attention_workspace(n_seqs, capacity, n_seqs * new, new, heads, kv_heads, dtype=dtype)
+    assert rc == OK, message()
+    assert n <= (16384 / (n_seqs * kv_heads) + 1) * n_seqs * new * heads * 130 * 4 + 512 and n < 1200 * MIB
+
+
+def test_a_wider_table_needs_no_more_once_every_workgroup_has_its_part():
+    sizes = [attention_workspace(256, 1 << e, 256 * 6, 6)[1] for e in range(10, 21)]
+    assert sizes[0] < sizes[3] and max(sizes) == max(sizes[:5]) and sizes[-1] < 512 * MIB

@@ -78,3 +78,17 @@ def test_one_prompts_chunk_beside_generating_requests(dtype, accumulate):
     new = [1] * 256
     new[77] = 2048
     check(Case(91, lengths, new, 32, 8, 64, 64, dtype), accumulate)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("heads,new", [(8, 3), (32, 3), (32, 16)], ids=["few", "rows", "tile"])
+def test_wide_tables(dtype, heads, new):
+    """Short requests and a few longer ones in a table of 131,072 tokens: parts longer than most of them."""
+    rng = np.random.RandomState(1)
+    lengths = rng.randint(new, 200, 64).tolist()
+    lengths[5], lengths[40], lengths[63] = 9000, 4096, 4097
+    case = Case(92, lengths, [new if i % 3 else 1 for i in range(64)], heads, 8, 64, 64, dtype)
+    tight = check(case, accumulate=False)
+    wide = check(case, accumulate=False, per=2048)
+    # parts of 64 * 8 * 131,072 / 16,384 = 4,096 tokens: 32, each with 64 channels and two sums a row
+    assert 0 < tight and wide <= 32 * case.rows * heads * 66 * 4 + 512
