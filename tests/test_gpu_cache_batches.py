@@ -92,3 +92,18 @@ def test_wide_tables(dtype, heads, new):
     wide = check(case, accumulate=False, per=2048)
     # parts of 64 * 8 * 131,072 / 16,384 = 4,096 tokens: 32, each with 64 channels and two sums a row
     assert 0 < tight and wide <= 32 * case.rows * heads * 66 * 4 + 512
+
+
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "all"])
+@pytest.mark.parametrize("dtype,dim", [(BF16, 64), (BF16, 128), (BF16, 256), (F32, 64), (F32, 96)])
+def test_many_prompts_with_weight_that_no_parts_are_made_for(dtype, dim, causal):
+    """128 prompts of 8 kv heads and up to 80 rows: rows and tokens whole, the weight added without a join."""
+    rng = np.random.RandomState(2)
+    new = rng.randint(1, 41, 128).tolist()
+    new[17] = 40
+    lengths = [n + int(rng.randint(0, 300)) for n in new]
+    lengths[3], lengths[17], lengths[90] = 0, 700, new[90]
+    new[3] = 0
+    case = Case(93, lengths, new, 16, 8, dim, 16, dtype)
+    # no parts of rows or tokens: the workspace is the sums of the rows
+    assert check(case, causal=causal) == (case.rows * 16 * 4 + 255) // 256 * 256
