@@ -518,7 +518,8 @@ typedef struct {
  * (row start[s] + i is its token length[s] - n + i with n = start[s+1] -
  * start[s]). start is device memory, ascending; entries are taken into [0,
  * n_rows], a sequence whose end lies before its start has no rows. Rows of no
- * sequence are left as they are. max_new: the host's bound on n (more than n_rows
+ * sequence are left as they are; what is written for rows that such an array gives to
+ * several sequences is not specified. max_new: the host's bound on n (more than n_rows
  * counts as n_rows); of a sequence with more rows msao_cache_attention leaves
  * those from max_new on as they are. */
 typedef struct {

@@ -71,20 +71,27 @@ struct Eight {
     }
 };
 
-// The sequence of a row of the chunk (-1: none): of the starts that are not past the
-// row, the last one's. `first`: the lane's of the first 64 starts.
-__device__ __forceinline__ int seq_of_row(const AppendArgs& a, int row, int first)
+// The sequence of a row of the chunk (-1: none), and its rows: the first sequence whose rows
+// (seq_rows) the row is one of, 64 sequences at a time. `first`, `last`: the lane's starts and
+// ends of the first 64.
+__device__ __forceinline__ int seq_of_row(const AppendArgs& a, int row, int first, int last, Rows* rows)
 {
     const int lane = threadIdx.x & (kWave - 1);
-    int n = 0;
-    for (int i0 = 0; i0 <= a.c.n_seqs; i0 += kWave) {
-        const int i = i0 + lane, start = i0 == 0 ? first : a.ch.start[min(i, a.c.n_seqs)];
-        n += __popcll(__ballot(i <= a.c.n_seqs && clamp_int(start, 0, a.ch.n_rows) <= row));
+    for (int s0 = 0; s0 < a.c.n_seqs; s0 += kWave) {
+        const int s = s0 + lane;
+        if (s0 > 0) {
+            first = a.ch.start[min(s, a.c.n_seqs)];
+            last = a.ch.start[min(s + 1, a.c.n_seqs)];
+        }
+        const int b = clamp_int(first, 0, a.ch.n_rows), e = clamp_int(last, b, a.ch.n_rows);
+        const uint64_t mine = __ballot(s < a.c.n_seqs && row >= b && row < e);
+        if (mine == 0) continue;
+        const int at = __builtin_ctzll(mine);
+        rows->begin = __builtin_amdgcn_readlane(b, at);
+        rows->n = __builtin_amdgcn_readlane(e, at) - rows->begin;
+        return s0 + at;
     }
-    const int s = n - 1;
-    if (s < 0 || s >= a.c.n_seqs) return -1;
-    const Rows r = seq_rows(a.ch, s);
-    return row >= r.begin && row < r.begin + r.n ? s : -1;
+    return -1;
 }
 
 // One pass over a row's heads: queries, keys, then values. A head takes `lanes` lanes of
@@ -136,7 +143,7 @@ __global__ __launch_bounds__(kBlock) void k_append(AppendArgs a)
         }
     };
     // what needs no sequence is on its way while the row's sequence, place and page are found
-    const int first = a.ch.start[min(lane, a.c.n_seqs)];
+    const int first = a.ch.start[min(lane, a.c.n_seqs)], last = a.ch.start[min(lane + 1, a.c.n_seqs)];
     int at[2] = {0, 0};
     float freq[2] = {0.0f, 0.0f};
 #pragma unroll
@@ -159,9 +166,9 @@ __global__ __launch_bounds__(kBlock) void k_append(AppendArgs a)
     if (a.q_norm && has1) nq1.load(a.q_norm + d1 * ES);
     if (a.k_norm && has0) nk0.load(a.k_norm + d0 * ES);
     if (a.k_norm && has1) nk1.load(a.k_norm + d1 * ES);
-    const int s = uniform(seq_of_row(a, row, first));
+    Rows rows;
+    const int s = uniform(seq_of_row(a, row, first, last, &rows));
     if (s < 0) return;
-    const Rows rows = seq_rows(a.ch, s);
     const int64_t place = (int64_t)seq_length(a.c, s) - rows.n + (row - rows.begin);  // in the cache
     const int mask = (1 << a.c.page_shift) - 1;
     const int page = place >= 0 ? page_at(a.c, s, (int)place >> a.c.page_shift) : -1;
