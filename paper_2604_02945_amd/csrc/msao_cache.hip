@@ -100,8 +100,9 @@ __device__ __forceinline__ int seq_of_row(const AppendArgs& a, int row, int firs
 // neighbours above. The norm is a sum over those lanes; the angles are the same for
 // every head, so a wavefront computes each once, into LDS, and a lane keeps the eight
 // that it turns. HBM bound: each value is read and written once, four heads in flight.
-// The angle is taken in turns in 64 bits (position * inv_freq / 2 pi less its whole
-// part), which keeps far positions as exact as near ones.
+// The angle is taken in turns in 64 bits (position * inv_freq / 2 pi), less its quarter
+// turns, which keeps far positions as exact as near ones and rounds at most an eighth of a
+// turn to 32 bits: 2^-28 of a turn, where a whole turn's 2^-25 is three times a sine's own rounding.
 template <int DT>
 __global__ __launch_bounds__(kBlock) void k_append(AppendArgs a)
 {
@@ -178,10 +179,14 @@ __global__ __launch_bounds__(kBlock) void k_append(AppendArgs a)
     for (int e = 0; e < 2; ++e) {
         if (kWave * e >= half) break;
         double t = (double)(a.positions ? at[e] : (int)place) * (double)freq[e] * 0.15915494309189533577;
-        t -= floor(t);
+        const double quarters = rint(4.0 * t);
+        t -= 0.25 * quarters;  // exact, in [-1/8, 1/8]
         float sn, cs;
         sincospif(2.0f * (float)t, &sn, &cs);
-        if (lane + kWave * e < half) turn[wave][lane + kWave * e] = f32x2{cs, sn};
+        const int quarter = (int)(quarters - 4.0 * floor(0.25 * quarters));  // 0 .. 3, of any number of them
+        const float x = quarter & 1 ? sn : cs, y = quarter & 1 ? cs : sn;
+        const bool minus_x = quarter == 1 || quarter == 2, minus_y = quarter >= 2;
+        if (lane + kWave * e < half) turn[wave][lane + kWave * e] = f32x2{minus_x ? -x : x, minus_y ? -y : y};
     }
     // the wavefront's own stores, read by its other lanes
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
