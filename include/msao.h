@@ -585,7 +585,7 @@ msao_status msao_cache_append(msao_ctx* ctx, const msao_kv_cache* cache, const m
  * over the tokens j that row i sees. Query head h reads kv head h / (heads /
  * kv_heads). q, out [n_rows][heads * head_dim] of the cache's dtype, 16-byte
  * aligned with strides (elements between rows) of 16-byte multiples, q's below
- * 2^25 bytes; out must not overlap q. lse: device [n_rows][heads] or NULL. A row that sees no token, or
+ * 2^25 bytes; out must not overlap q (refused where the host can tell). lse: device [n_rows][heads] or NULL. A row that sees no token, or
  * only scores of -inf, gets out 0 and lse -inf and adds no weight; what a row does
  * not see has no effect on it, whatever it holds. With MSAO_ATTEND_WEIGHT, weight
  * of (s, kv head, j) grows by the sum of p_ij over the chunk's rows and the query

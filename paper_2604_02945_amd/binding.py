@@ -939,8 +939,9 @@ def msao_cache_attention(cache: KvCache, start: torch.Tensor, max_new: int, q: t
     msao_cache_append) over the cache; scale 1/sqrt(head_dim) when None. lse
     float32 [rows, heads] is filled if given; accumulate adds to cache.weight what
     each token receives. workspace: uint8, 256-byte aligned, of
-    cache_attention_workspace bytes (allocated when None). Returns out; rows of
-    no sequence keep what `out` held (0 in one allocated here)."""
+    cache_attention_workspace bytes (allocated when None). Returns out, which must
+    share no memory with q; rows of no sequence, and those from max_new on of a longer
+    one, keep what `out` held (0 in one allocated here)."""
     ctx = _cache_ctx(cache, ctx, stream)
     q_stride = _head_rows("q", q, cache.dtype, None, cache.head_dim)
     rows, heads = q.shape[0], q.shape[1]

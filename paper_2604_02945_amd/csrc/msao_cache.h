@@ -107,6 +107,19 @@ MSAO_HD int group_sees(int length, int n_new, const Group& group, int last_row, 
     return causal ? clamp_int(length - n_new + group.of(last_row) + 1, 0, length) : length;
 }
 
+// Whether n rows of `bytes` bytes from a, every `sa` bytes, and from b, every `sb` (both at
+// least `bytes`), certainly share memory: exact for rows at one distance, which may lie between
+// one another as the parts of one projection do; at different ones the first rows are compared.
+MSAO_HD bool rows_meet(const void* a, int64_t sa, const void* b, int64_t sb, int64_t bytes, int64_t n)
+{
+    if (n <= 0) return false;
+    const int64_t d = (int64_t)((uintptr_t)b - (uintptr_t)a);
+    if (d > -bytes && d < bytes) return true;
+    if (sa != sb) return false;
+    const int64_t k = d / sa - (d % sa < 0 ? 1 : 0), r = d - k * sa;  // b's first row is r past the k-th of a, and sa - r before the next
+    return (r < bytes && k > -n && k < n) || (sa - r < bytes && k + 1 > -n && k + 1 < n);
+}
+
 // ---- append -------------------------------------------------------------------
 struct AppendArgs {
     CacheDev c;

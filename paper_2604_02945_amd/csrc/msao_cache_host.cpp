@@ -327,6 +327,7 @@ msao_status msao_cache_attention(msao_ctx* ctx, const msao_kv_cache* cache, cons
         if (!aligned(lse, 4)) return fail(err, MSAO_ERR_ALIGNMENT, "lse is not 4-byte aligned");
         MSAO_TRY(check_workspace(workspace, workspace_bytes, pl.total, err));
         if (!ctx) return bad(err, "ctx is NULL");
+        if (rows_meet(q, q_stride * es, out, out_stride * es, values * es, chunk->n_rows)) return bad(err, "out overlaps q");
         if (chunk->max_new == 0 || cache->n_seqs == 0) return MSAO_OK;
         a.q = (const uint8_t*)q;
         a.out = (uint8_t*)out;

@@ -1,11 +1,13 @@
 """What the paged cache's calls take and refuse at large sizes, on the CPU: launches,
 workspaces, integers."""
 import ctypes
+import os
+import subprocess
 
 import pytest
 
 from paper_2604_02945_amd import binding as B
-from test_cache_cpu import OK, UNSUP, cache, chunk, message
+from test_cache_cpu import INVALID, OK, ROOT, UNSUP, append, cache, chunk, message
 
 
 def attention_workspace(n_seqs, capacity, n_rows, max_new, heads=32, kv_heads=8, flags=1, dim=128, page=64, dtype=B.BF16):
@@ -58,3 +60,12 @@ def test_the_workspace_of_wide_tables_is_bounded(n_seqs, heads, kv_heads, new, c
 def test_a_wider_table_needs_no_more_once_every_workgroup_has_its_part():
     sizes = [attention_workspace(256, 1 << e, 256 * 6, 6)[1] for e in range(10, 21)]
     assert sizes[0] < sizes[3] and max(sizes) == max(sizes[:5]) and sizes[-1] < 512 * MIB
+
+
+def test_rows_that_share_memory(tmp_path):
+    exe = str(tmp_path / "rows_check")
+    subprocess.check_call(["g++", "-std=c++17", "-O2", "-Wall", "-Wextra", "-Werror", "-fsanitize=address,undefined",
+                           "-fno-sanitize-recover=all", "-I", os.path.join(ROOT, "paper_2604_02945_amd", "csrc"),
+                           os.path.join(ROOT, "tests", "c", "cache_rows_check.cpp"), "-o", exe])
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, r.stdout + r.stderr
