@@ -539,7 +539,8 @@ msao_status msao_cache_validate(const msao_kv_cache* cache, const msao_chunk* ch
 /* What msao_cache_append takes besides the cache. Rows are of the cache's dtype;
  * the heads of a row follow one another (head h at h * head_dim), strides are in
  * elements between rows. Pointers and strides are multiples of 16 bytes.
- *   q -> q_out [n_rows][heads * head_dim]: the same pointer and stride, or memory apart;
+ *   q -> q_out [n_rows][heads * head_dim]: the same pointer and stride, or memory apart (refused where
+ *     the host can tell);
  *     NULL with heads 0.
  *   k, v [n_rows][kv_heads * head_dim].
  *   q_norm, k_norm [head_dim] or NULL: a head x becomes x / sqrt(mean(x^2) + eps) * norm.

@@ -866,7 +866,7 @@ def msao_cache_append(cache: KvCache, start: torch.Tensor, max_new: int, k: torc
     float32 [pairs] (None: no rotation) turns the first 2 * pairs values by
     positions int32 [rows] or [axes, rows] (None: the places in the cache),
     sections naming the pairs of each axis; interleaved pairs neighbours. Returns
-    q_out (q's own memory may be passed)."""
+    q_out (q itself may be passed, or memory that shares none with it)."""
     ctx = _cache_ctx(cache, ctx, stream)
     dim, dtype = cache.head_dim, cache.dtype
     a = MsaoAppend()

@@ -114,6 +114,9 @@ msao_status check_append(const msao_kv_cache& c, const msao_chunk& ch, const msa
         if (in->heads > 0) {
             MSAO_TRY(check_rows(in->q, in->q_stride, in->heads * dim, es, "q", err));
             MSAO_TRY(check_rows(in->q_out, in->q_out_stride, in->heads * dim, es, "q_out", err));
+            const bool in_place = in->q == in->q_out && (in->q_stride == in->q_out_stride || ch.n_rows == 1);
+            if (!in_place && rows_meet(in->q, in->q_stride * es, in->q_out, in->q_out_stride * es, in->heads * dim * es, ch.n_rows))
+                return bad(err, "q_out overlaps q and is not q");
         }
         MSAO_TRY(check_rows(in->k, in->k_stride, c.kv_heads * dim, es, "k", err));
         MSAO_TRY(check_rows(in->v, in->v_stride, c.kv_heads * dim, es, "v", err));

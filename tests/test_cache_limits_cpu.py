@@ -69,3 +69,26 @@ def test_rows_that_share_memory(tmp_path):
                            os.path.join(ROOT, "tests", "c", "cache_rows_check.cpp"), "-o", exe])
     r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0, r.stdout + r.stderr
+
+
+ROW = 32 * 128
+
+
+@pytest.mark.parametrize("q_out,stride,rows,code", [
+    (0, ROW, 10, OK), (0, ROW + 64, 1, OK), (10 * ROW, ROW, 10, OK), (-10 * ROW, ROW, 10, OK), (10 * ROW, 3 * ROW, 10, OK),
+    (0, ROW + 64, 10, INVALID), (0, 2 * ROW, 2, INVALID), (ROW, ROW, 10, INVALID), (-ROW, ROW, 10, INVALID), (9 * ROW, ROW, 10, INVALID),
+    (8, ROW, 10, INVALID), (-8, ROW, 1, INVALID), (ROW - 8, 5 * ROW, 10, INVALID)])
+def test_append_into_part_of_the_queries(q_out, stride, rows, code):
+    """(q_out and strides in bf16 elements from q; the header's forms: q itself, or memory apart)"""
+    base = 1 << 30
+    a = append(q=base, q_out=base + 2 * q_out, q_stride=ROW, q_out_stride=stride)
+    ch = chunk(n_rows=rows, max_new=min(rows, 4))
+    rc = B.lib().msao_cache_append(None, B._addr(cache()), B._addr(ch), B._addr(a), None)
+    assert rc == INVALID and ("overlaps" in message()) == (code == INVALID), message()
+
+
+def test_queries_and_outputs_as_parts_of_one_array():
+    base = 1 << 30
+    a = append(q=base, q_out=base + 2 * ROW, q_stride=2 * ROW, q_out_stride=2 * ROW)
+    assert B.lib().msao_cache_append(None, B._addr(cache()), B._addr(chunk()), B._addr(a), None) == INVALID
+    assert message() == "ctx is NULL"  # the arguments pass
