@@ -82,13 +82,14 @@ def test_append_into_part_of_the_queries(q_out, stride, rows, code):
     """(q_out and strides in bf16 elements from q; the header's forms: q itself, or memory apart)"""
     base = 1 << 30
     a = append(q=base, q_out=base + 2 * q_out, q_stride=ROW, q_out_stride=stride)
-    ch = chunk(n_rows=rows, max_new=min(rows, 4))
-    rc = B.lib().msao_cache_append(None, B._addr(cache()), B._addr(ch), B._addr(a), None)
+    c, ch = cache(), chunk(n_rows=rows, max_new=min(rows, 4))  # (held: the call has their addresses)
+    rc = B.lib().msao_cache_append(None, B._addr(c), B._addr(ch), B._addr(a), None)
     assert rc == INVALID and ("overlaps" in message()) == (code == INVALID), message()
 
 
 def test_queries_and_outputs_as_parts_of_one_array():
     base = 1 << 30
     a = append(q=base, q_out=base + 2 * ROW, q_stride=2 * ROW, q_out_stride=2 * ROW)
-    assert B.lib().msao_cache_append(None, B._addr(cache()), B._addr(chunk()), B._addr(a), None) == INVALID
+    c, ch = cache(), chunk()
+    assert B.lib().msao_cache_append(None, B._addr(c), B._addr(ch), B._addr(a), None) == INVALID
     assert message() == "ctx is NULL"  # the arguments pass
