@@ -606,7 +606,10 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 // `to`; out of range zeros. As instructions of its own, because the compiler, which cannot
 // tell the two stages apart, would wait for the next stage's loads before it reads this
 // one's. The load has no register to write; it is waited for (stage_came) before the
-// barrier after which its stage is read. M0 is set for it alone: nothing else here uses M0.
+// barrier after which its stage is read. The descriptor may have come from a vector instruction
+// (readfirstlane), after which the hardware wants five wait states before a load reads it, and
+// M0 one; the compiler counts none for text, so the text has six (attend_chunk 758 us, 753 with
+// two). M0 is set for it alone: nothing else in the kernel uses M0.
 // ONCE: the values of a call with one tile of rows need no cache, which keeps the keys for the
 // weight pass (64 requests of 14 to 42 rows over up to 16,000 tokens: 146 us and 83 for the weight,
 // 153 and 90 without; 8 such requests of 42 to 63 rows 29.8, 27.5 without).
@@ -614,10 +617,10 @@ template <bool ONCE>
 __device__ __forceinline__ void load_to_lds(const u32x4& buffer, uint32_t to, int off)
 {
     if constexpr (ONCE)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(to), "v"(off), "s"(buffer)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(to), "v"(off), "s"(buffer)
                      : "memory");
     else
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(buffer)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(buffer)
                      : "memory");
 }
 __device__ __forceinline__ void stage_came() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
