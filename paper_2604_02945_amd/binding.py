@@ -834,12 +834,22 @@ def _stream_of(cache: KvCache, stream) -> int:
     return torch._C._cuda_getCurrentRawStream(cache.index) if stream is None else stream.cuda_stream
 
 
+INT_MAX = 2 ** 31 - 1
+
+
+def _fits(name: str, value: int) -> int:
+    """(ctypes would take the low bits of an integer that its field cannot hold)"""
+    if not -INT_MAX <= value <= INT_MAX:
+        raise ValueError(f"{name} is out of range")
+    return int(value)
+
+
 def _chunk(cache: KvCache, start: torch.Tensor, n_rows: int, max_new: int) -> MsaoChunk:
     _int32("start", start, 1)
     if start.shape[0] != cache.n_seqs + 1:
         raise ValueError("start must have n_seqs + 1 entries")
     _same_device(cache.index, "start", start)
-    return MsaoChunk(start.data_ptr(), n_rows, int(max_new))
+    return MsaoChunk(start.data_ptr(), _fits("n_rows", n_rows), _fits("max_new", min(max_new, max(n_rows, 0))))
 
 
 def _scratch(cache: KvCache, nbytes: int, stream) -> torch.Tensor:
@@ -926,7 +936,7 @@ def cache_attention_workspace(cache: KvCache, start: torch.Tensor, n_rows: int, 
     """Bytes of workspace that msao_cache_attention needs for such a call."""
     ch, n = _chunk(cache, start, n_rows, max_new), ctypes.c_size_t()
     flags = (ATTEND_CAUSAL if causal else 0) | (ATTEND_WEIGHT if accumulate else 0)
-    _check(lib().msao_cache_attention_workspace(cache.addr, _addr(ch), heads, flags, ctypes.byref(n)))
+    _check(lib().msao_cache_attention_workspace(cache.addr, _addr(ch), _fits("heads", heads), flags, ctypes.byref(n)))
     return n.value
 
 
@@ -995,7 +1005,7 @@ def msao_cache_evict(cache: KvCache, budget: torch.Tensor, n_first: int = 0, n_r
         _check(lib().msao_cache_evict_workspace(cache.addr, ctypes.byref(need)))
         workspace = _scratch(cache, need.value, stream)
     _check(lib().msao_cache_evict(ctx.handle, cache.addr, to.addr if to is not None else None, budget.data_ptr(),
-                                  int(n_first), int(n_recent), kept_idx.data_ptr(), kept_idx.shape[2],
+                                  _fits("n_first", min(n_first, INT_MAX)), _fits("n_recent", min(n_recent, INT_MAX)), kept_idx.data_ptr(), kept_idx.shape[2],
                                   workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                                   _stream_of(cache, stream)), ctx)
     return {"kept_idx": kept_idx, "kept_count": (to or cache).length}

@@ -5,6 +5,7 @@ import os
 import subprocess
 
 import pytest
+import torch
 
 from paper_2604_02945_amd import binding as B
 from test_cache_cpu import INVALID, OK, ROOT, UNSUP, append, cache, chunk, message
@@ -93,3 +94,26 @@ def test_queries_and_outputs_as_parts_of_one_array():
     c, ch = cache(), chunk()
     assert B.lib().msao_cache_append(None, B._addr(c), B._addr(ch), B._addr(a), None) == INVALID
     assert message() == "ctx is NULL"  # the arguments pass
+
+
+def host_cache(n_seqs=3, per=2, **kw):
+    k = torch.zeros(6, 2, 16, 64)
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    return B.KvCache(k, k.clone(), kw.get("pages", i32(n_seqs, per)), kw.get("length", i32(n_seqs)))
+
+
+@pytest.mark.parametrize("max_new", [11, 2 ** 31, 2 ** 32, 2 ** 32 + 1, 2 ** 63, 2 ** 70])
+def test_a_bound_past_an_integer_is_the_number_of_rows(max_new):
+    """max_new beyond n_rows counts as n_rows, whatever its low bits are."""
+    c, start = host_cache(per=200), torch.zeros(4, dtype=torch.int32)
+    ch = B._chunk(c, start, 10, max_new)
+    assert (ch.n_rows, ch.max_new) == (10, 10)
+    assert B.cache_attention_workspace(c, start, 10, max_new, 4) == B.cache_attention_workspace(c, start, 10, 10, 4) > 0
+
+
+@pytest.mark.parametrize("n_rows,max_new,heads", [(2 ** 31, 1, 4), (2 ** 32 + 10, 4, 4), (10, -2 ** 32, 4), (-2 ** 32, 1, 4),
+                                                  (10, 4, 2 ** 32 + 4), (-1, 1, 4), (10, -1, 4), (10, 4, 0), (10, 4, -4)])
+def test_counts_past_an_integer_are_refused(n_rows, max_new, heads):
+    small = all(abs(x) < 2 ** 31 for x in (n_rows, max_new, heads))
+    with pytest.raises(B.MsaoError if small else ValueError, match="negative|positive" if small else "out of range"):
+        B.cache_attention_workspace(host_cache(), torch.zeros(4, dtype=torch.int32), n_rows, max_new, heads)

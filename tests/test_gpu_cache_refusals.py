@@ -31,3 +31,27 @@ def test_out_in_the_queries_memory(dtype, accumulate):
     want = msao.msao_cache_attention(cache, start, 7, case.q.to(DEV))
     assert torch.equal(msao.msao_cache_attention(cache, start, 7, q, out=both[:, 1]), want)
     assert torch.equal(msao.msao_cache_attention(cache, start, 7, flat[:9], out=flat[9:18]), want)
+
+
+def test_numbers_past_an_integer():
+    """Counts that only bound others: more than there are counts as all; below 0 they are refused."""
+    import paper_2604_02945_amd as msao
+    case = Case(96, [40, 70], [2, 7], 8, 2, 64, 16, BF16)
+    cache, start = case.device(DEV)
+    q = case.q.to(DEV)
+    want = msao.msao_cache_attention(cache, start, 7, q)
+    for many in (2 ** 31, 2 ** 32, 2 ** 32 + 1, 2 ** 64):
+        assert torch.equal(msao.msao_cache_attention(cache, start, many, q), want)
+    budget = torch.tensor([20, 30], dtype=torch.int32, device=DEV)
+    for many in (70, 2 ** 31, 2 ** 32, 2 ** 64 + 3):
+        for first, recent, ids in ((0, many, [range(20, 40), range(40, 70)]), (many, 0, [range(20), range(30)])):
+            c, _ = case.device(DEV)
+            r = msao.msao_cache_evict(c, budget, first, recent)
+            for b in range(2):
+                for h in range(2):
+                    assert r["kept_idx"][b, h, :len(ids[b])].tolist() == list(ids[b])
+    for first, recent, error in ((-1, 0, msao.MsaoError), (0, -1, msao.MsaoError), (-2 ** 32, 0, ValueError), (0, -2 ** 33, ValueError)):
+        with pytest.raises(error, match="negative|out of range"):
+            msao.msao_cache_evict(cache, budget, first, recent)
+    with pytest.raises(ValueError, match="out of range"):
+        msao.msao_cache_attention(cache, start, -2 ** 32, q)
