@@ -858,6 +858,12 @@ def _scratch(cache: KvCache, nbytes: int, stream) -> torch.Tensor:
         return buf if buf.data_ptr() % 256 == 0 else _workspace(nbytes, cache.device)
 
 
+def _bytes_of(workspace: torch.Tensor) -> int:
+    if not workspace.is_contiguous():  # (its elements may be fewer bytes apart than they have, or none)
+        raise ValueError("workspace must be contiguous")
+    return workspace.numel() * workspace.element_size()
+
+
 def _on(stream):
     """Memory allocated inside is `stream`'s, where the call will use it (None: the current stream's)."""
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
@@ -973,7 +979,7 @@ def msao_cache_attention(cache: KvCache, start: torch.Tensor, max_new: int, q: t
     _check(lib().msao_cache_attention(ctx.handle, cache.addr, ctypes.byref(ch), q.data_ptr(), q_stride, heads,
                                       cache.head_dim ** -0.5 if scale is None else scale, flags, out.data_ptr(),
                                       out_stride, None if lse is None else lse.data_ptr(), workspace.data_ptr(),
-                                      workspace.numel() * workspace.element_size(), _stream_of(cache, stream)), ctx)
+                                      _bytes_of(workspace), _stream_of(cache, stream)), ctx)
     return out
 
 
@@ -1006,8 +1012,7 @@ def msao_cache_evict(cache: KvCache, budget: torch.Tensor, n_first: int = 0, n_r
         workspace = _scratch(cache, need.value, stream)
     _check(lib().msao_cache_evict(ctx.handle, cache.addr, to.addr if to is not None else None, budget.data_ptr(),
                                   _fits("n_first", min(n_first, INT_MAX)), _fits("n_recent", min(n_recent, INT_MAX)), kept_idx.data_ptr(), kept_idx.shape[2],
-                                  workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                                  _stream_of(cache, stream)), ctx)
+                                  workspace.data_ptr(), _bytes_of(workspace), _stream_of(cache, stream)), ctx)
     return {"kept_idx": kept_idx, "kept_count": (to or cache).length}
 
 

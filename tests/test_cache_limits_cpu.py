@@ -117,3 +117,12 @@ def test_counts_past_an_integer_are_refused(n_rows, max_new, heads):
     small = all(abs(x) < 2 ** 31 for x in (n_rows, max_new, heads))
     with pytest.raises(B.MsaoError if small else ValueError, match="negative|positive" if small else "out of range"):
         B.cache_attention_workspace(host_cache(), torch.zeros(4, dtype=torch.int32), n_rows, max_new, heads)
+
+
+def test_a_workspace_has_the_bytes_it_says():
+    ws = torch.zeros(1024, dtype=torch.uint8)
+    assert B._bytes_of(ws) == B._bytes_of(ws.view(torch.float32)) == 1024 and B._bytes_of(ws[512:]) == 512
+    assert B._bytes_of(ws[:0]) == 0
+    for bad in (ws[:1].expand(1 << 30), ws[::2], ws.view(32, 32).t(), torch.as_strided(ws, (64, 64), (4, 1))):
+        with pytest.raises(ValueError, match="contiguous"):
+            B._bytes_of(bad)

@@ -55,3 +55,18 @@ def test_numbers_past_an_integer():
             msao.msao_cache_evict(cache, budget, first, recent)
     with pytest.raises(ValueError, match="out of range"):
         msao.msao_cache_attention(cache, start, -2 ** 32, q)
+
+
+def test_a_workspace_of_one_byte_expanded():
+    import paper_2604_02945_amd as msao
+    case = Case(97, [2000, 70], [2, 7], 8, 2, 64, 16, BF16)
+    cache, start = case.device(DEV)
+    q = case.q.to(DEV)
+    ws = torch.zeros(256, dtype=torch.uint8, device=DEV)
+    for bad in (ws[:1].expand(1 << 28), torch.as_strided(ws, (1 << 20, 16), (0, 1))):
+        with pytest.raises(ValueError, match="workspace must be contiguous"):
+            msao.msao_cache_attention(cache, start, 7, q, workspace=bad)
+        with pytest.raises(ValueError, match="workspace must be contiguous"):
+            msao.msao_cache_evict(cache, torch.tensor([20, 30], dtype=torch.int32, device=DEV), workspace=bad)
+    with pytest.raises(msao.MsaoError, match="workspace too small"):
+        msao.msao_cache_attention(cache, start, 7, q, workspace=ws)
