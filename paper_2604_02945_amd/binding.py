@@ -752,7 +752,7 @@ def _same_device(index: int, what: str, *tensors):
 def _int32(name: str, t: torch.Tensor, dim: int):
     if t.dtype is not torch.int32 or t.dim() != dim:
         raise ValueError(f"{name} must be a {dim}-D int32 tensor")
-    if t.stride(-1) != 1 and t.numel():
+    if t.stride(-1) != 1 and t.shape[-1] > 1 and t.numel():  # (a single entry is at no distance)
         raise ValueError(f"{name} must be contiguous in its last dimension")
 
 

@@ -126,3 +126,15 @@ def test_a_workspace_has_the_bytes_it_says():
     for bad in (ws[:1].expand(1 << 30), ws[::2], ws.view(32, 32).t(), torch.as_strided(ws, (64, 64), (4, 1))):
         with pytest.raises(ValueError, match="contiguous"):
             B._bytes_of(bad)
+
+
+def test_single_entries_at_any_distance():
+    """One sequence of a table whose columns hold what others need: torch says any stride of one entry."""
+    table = torch.zeros(4, 7, dtype=torch.int32)
+    c = host_cache(n_seqs=1, pages=table[:1, :3], length=table[:1, 5])
+    assert c.n_seqs == 1 and c.struct.length == table.data_ptr() + 20
+    c = host_cache(n_seqs=4, pages=torch.zeros(1, 4, dtype=torch.int32).t(), length=table.view(-1)[:4])
+    assert (c.pages_per_seq, c.struct.table_stride) == (1, 1)
+    for bad in (dict(n_seqs=4, length=table[:, 0]), dict(n_seqs=4, pages=table.t()[:4, :3])):
+        with pytest.raises(ValueError, match="contiguous"):
+            host_cache(**bad)

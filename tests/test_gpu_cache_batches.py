@@ -107,3 +107,23 @@ def test_many_prompts_with_weight_that_no_parts_are_made_for(dtype, dim, causal)
     case = Case(93, lengths, new, 16, 8, dim, 16, dtype)
     # no parts of rows or tokens: the workspace is the sums of the rows
     assert check(case, causal=causal) == (case.rows * 16 * 4 + 255) // 256 * 256
+
+
+def test_one_sequence_of_a_strided_table():
+    """Lengths, pages, starts and positions of one entry, at the strides that a slice leaves them."""
+    import paper_2604_02945_amd as msao
+    case = Case(94, [90], [1], 4, 2, 64, 16, BF16)
+    cache, start = case.device(DEV)
+    q, kv = case.q.to(DEV), torch.randn(1, 2, 64, device=DEV).to(BF16)
+    inv = torch.rand(32, device=DEV)
+    table = torch.zeros(1, 9, dtype=torch.int32, device=DEV)
+    table[0, 3:3 + case.per] = torch.from_numpy(case.pages[0]).to(DEV)
+    table[0, 1] = 90
+    odd = msao.KvCache(cache.k.clone(), cache.v.clone(), table[:, 3:3 + case.per], table[:, 1], cache.weight.clone())
+    at = torch.tensor([[5, 6, 7], [1, 2, 3]], dtype=torch.int32, device=DEV)
+    got = []
+    for c, pos in ((cache, at[:, :1].contiguous()), (odd, at.t().contiguous().t()[:, :1])):
+        x = msao.msao_cache_append(c, start, 1, kv, kv, q=q, inv_freq=inv, positions=pos, sections=(20, 12))
+        got.append((msao.msao_cache_attention(c, start, 1, x, accumulate=True), c.weight, x))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
