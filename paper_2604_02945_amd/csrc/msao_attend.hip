@@ -3,7 +3,11 @@
 //
 // Rows of a (sequence, kv head) are its n new tokens times the `group` query heads
 // that share the kv head: all of them read the same keys and values, so they fill the
-// columns of the matrix instructions, and K and V are read once for up to 128 rows.
+// columns of the matrix instructions, and K and V are read once for up to 128 rows (64 of
+// float32; half as many of heads above 128 channels). For bf16 each p is rounded to bf16 for the
+// second product, by 2^-8 of it at most: float32 products take eight times as long, and two bf16 pieces of
+// p twice. Errors of whole rows against 64 bits are 0.0017-0.0023 then, of which the result's
+// own rounding is 0.0016-0.0017. Scores, sums, lse and weight are not rounded.
 //
 // k_attend (up to 16 rows of bf16; float32): a wavefront takes 32 tokens at a time, K and V
 // straight from memory into registers in whole rows, and nothing through LDS:
@@ -590,7 +594,9 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArg
 }
 
 // Many rows, bf16 (wide drafts, chunks of prompts): K and V are read once for 64 MT rows; from some
-// 100 rows on bound by the matrix cores and the exponents. A stage of 64 tokens goes from memory to LDS without
+// 100 rows on bound by the matrix cores, the reads of LDS and the exponents together: for heads of 128
+// a workgroup reads 64 KB of LDS for 32 tokens, 512 clocks at 128 bytes, and its products take 515;
+// for heads of 256, whose K and V serve 16 rows of a wavefront, 1,024 against 515. A stage of 64 tokens goes from memory to LDS without
 // passing through registers (each wavefront brings 16 tokens) while the stage before it is
 // used. Every wavefront has 16 MT rows of its own and takes all of the tokens, 32 at a time:
 //   S^T = K Q^T with the queries in registers and K's rows as A operands,
@@ -1270,8 +1276,9 @@ bool block_a_row(const AttendArgs& a) { return a.splits > 16; }
 // 48 rows a wavefront 884 (246 registers, as fast a SIMD but fewer workgroups; 64 spill), 16
 // rows and eight wavefronts 770, stages of 32 tokens 852 (each pair by pair; in levels 700-720).
 // Heads of 256: 16 rows a wavefront and stages of 32, for the same registers and LDS (the
-// same chunks 1.70 ms, 6.26 through k_attend). float32 stays with k_attend: its products, not
-// its loads, are the bound.
+// same chunks 1.70 ms, 6.26 through k_attend). float32 stays with k_attend: the same chunks take
+// 6.0 ms, 114 TFLOP/s of the 153 that a large product reaches (short ragged queries, which leave
+// workgroups uneven and loads exposed, 39).
 constexpr int kFewRows = 16;
 constexpr int stage_of(int dp) { return dp == 256 ? 32 : 64; }
 // Rows of a workgroup: what the registers of its wavefronts hold.

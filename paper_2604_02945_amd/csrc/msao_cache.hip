@@ -102,7 +102,7 @@ __device__ __forceinline__ int seq_of_row(const AppendArgs& a, int row, int firs
 // that it turns. HBM bound: each value is read and written once, four heads in flight.
 // The angle is taken in turns in 64 bits (position * inv_freq / 2 pi), less its quarter
 // turns, which keeps far positions as exact as near ones and rounds at most an eighth of a
-// turn to 32 bits: 2^-28 of a turn, where a whole turn's 2^-25 is three times a sine's own rounding.
+// turn to 32 bits: 2^-28 of a turn, 2.3e-8 rad, where a whole turn's 2^-25 is three steps of a sine below 1.
 template <int DT>
 __global__ __launch_bounds__(kBlock) void k_append(AppendArgs a)
 {
