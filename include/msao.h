@@ -490,8 +490,8 @@ msao_status msao_draft_entropy(msao_ctx* ctx, const void* logits, int64_t rows, 
  * captured graph follows them from replay to replay. A length outside [0,
  * capacity] counts as the nearer end. A page outside [0, n_pages) is no page:
  * nothing is stored there, what lies there is no token for attention, and
- * eviction takes zeros from it. Sequences may share pages that are only read; a
- * page that a call stores to belongs to one sequence. Memory past a sequence's
+ * eviction takes zeros from it. Sequences may share pages that are only read, and
+ * name one twice; a page that a call stores to is named once, by one sequence. Memory past a sequence's
  * length may hold anything, infinities and NaN included. */
 #define MSAO_MAX_HEAD_DIM 256
 typedef struct {
