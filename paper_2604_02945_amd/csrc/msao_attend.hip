@@ -647,7 +647,8 @@ __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
     // the last tiles, which see most, of all pairs before the ones before them, so that no long
     // one is left to the end; a pair's kRowLevel tiles of a level side by side, which share keys
     // and values in the caches. 8 prompts of 1,500 tokens 71 us (83 pair by pair, 65 tile by tile),
-    // one of 8,000 574 us (665, 543), chunks of 2,048 over 12,288 717 us (746, 780)
+    // one of 8,000 574 us (665, 543), chunks of 2,048 over 12,288 717 us (746, 780; the
+    // clock takes 30 passes to rise, whose first take up to 1,020)
     const int per_pair = a.row_tiles * a.splits, pairs = a.c.n_seqs * a.c.kv_heads;
     const int level = min((int)blockIdx.x / (kRowLevel * pairs), per_pair / kRowLevel), in_level = blockIdx.x - level * kRowLevel * pairs;
     const int width = min(kRowLevel, per_pair - level * kRowLevel), sh = in_level / width;
@@ -1002,7 +1003,7 @@ __global__ __launch_bounds__(kBlock) void k_combine(AttendArgs a, int blocks_per
 //
 // Few rows (k_weight): K streams by, 16 tokens a wavefront, past the queries in LDS. HBM
 // bound; 60 registers leave eight wavefronts on a SIMD, which is what hides the loads (32
-// tokens in 94 registers: 100 us for attend_round's 383 MB against 91; two sets of registers
+// tokens in 94 registers: 100 us for attend_round's 383 MB against 91, which attention's nontemporal values made 83-89; two sets of registers
 // in turn 112).
 template <int DT, int DP, int MT>
 __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight(AttendArgs a)
@@ -1361,7 +1362,8 @@ template <int DT, int DP> struct Weight {
 // 100,000 among them 508, 628; 64 of up to 16,000 with 4 rows 224, 216, and with one of 120,000
 // 296, 290; with 24 rows 313, 376.)
 constexpr int64_t kPartTarget = 2048, kPartLeast = 128, kPartMost = 1024, kManyTarget = 1024, kManyTargetF32 = 4096, kMostParts = 16384;
-// Parts of the tokens in the weight pass of few rows (attend_round 91 us; 93 with 8,192), and
+// Parts of the tokens in the weight pass of few rows (attend_round 91 us, 93 with 8,192, before
+// attention's values were nontemporal), and
 // of the rows in that of many: up to 32 (25 us, 33 with 10).
 constexpr int64_t kWeightTarget = 16384, kWeightLeast = 256, kWeightRowTarget = 8192, kMostRowParts = 32;
 void attend_shape(AttendArgs& a)

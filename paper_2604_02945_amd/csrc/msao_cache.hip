@@ -280,7 +280,7 @@ __global__ __launch_bounds__(kBlock) void k_append(AppendArgs a)
 // pass each wavefront's counts of each item meet in LDS once, and ballots order the rest.
 // Beyond kSelTokens tokens k_select_long goes over memory again for each digit. Bound by
 // latency: one pass over the weights and a dozen barriers (8 x 2,944 tokens 12-13 us, 256 x 8,000
-// 16; 12 x 81,000, past the registers, 73).
+// 17-18; 12 x 81,000, past the registers, 73-82).
 constexpr int kSelLong = 1024;                    // threads of k_select_long
 constexpr int kSelItems = 32;                     // tokens of a thread, at most (64 spill)
 constexpr int kSelTokens = kSelItems * kSelLong;
@@ -536,8 +536,8 @@ __global__ __launch_bounds__(kSelLong) void k_select_long(EvictArgs a)
 // up to kMoveUnits 16-byte pieces a thread, in turn; in place there is one block for each
 // (sequence, kv head, K or V, column part), whose loads of a chunk are done before its stores
 // begin: a kept token only ever moves down, so a later chunk reads nothing that an earlier
-// one wrote. HBM bound: 256 heads of 2,048 tokens of 8,000, in place, 102-107 us for 546 MB,
-// the rate of a large copy.
+// one wrote. HBM bound into other pages: 256 heads of 2,048 tokens of up to 8,000 115-117 us for
+// 546 MB, the rate of a large copy; in place, a chain of loads and stores in each block, 154.
 constexpr int kMoveUnits = 4;  // 16-byte pieces of a thread in flight
 __global__ __launch_bounds__(kBlock) void k_move(EvictArgs a)
 {
