@@ -1003,8 +1003,8 @@ __global__ __launch_bounds__(kBlock) void k_combine(AttendArgs a, int blocks_per
 //
 // Few rows (k_weight): K streams by, 16 tokens a wavefront, past the queries in LDS. HBM
 // bound; 60 registers leave eight wavefronts on a SIMD, which is what hides the loads (32
-// tokens in 94 registers: 100 us for attend_round's 383 MB against 91, which attention's nontemporal values made 83-89; two sets of registers
-// in turn 112).
+// tokens in 94 registers: 100 us for attend_round's 383 MB against 91, which attention's nontemporal
+// values made 83-89; two sets of registers in turn 112).
 template <int DT, int DP, int MT>
 __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight(AttendArgs a)
 {
