@@ -586,16 +586,18 @@ msao_status msao_cache_append(msao_ctx* ctx, const msao_kv_cache* cache, const m
  * over the tokens j that row i sees. Query head h reads kv head h / (heads /
  * kv_heads). q, out [n_rows][heads * head_dim] of the cache's dtype, 16-byte
  * aligned with strides (elements between rows) of 16-byte multiples, q's below
- * 2^25 bytes; out must not overlap q (refused where the host can tell). lse: device [n_rows][heads] or NULL. A row that sees no token, or
- * only scores of -inf, gets out 0 and lse -inf and adds no weight; what a row does
- * not see has no effect on it, whatever it holds. With MSAO_ATTEND_WEIGHT, weight
- * of (s, kv head, j) grows by the sum of p_ij over the chunk's rows and the query
- * heads of the kv head; the order of every sum is fixed: the same call gives the
- * same bits. For bf16, the p_ij that multiply v are rounded to bf16; sums, lse and
- * weight are not. Workspace from msao_cache_attention_workspace, used only while
- * the call runs on the GPU. A call of 2^24 workgroups or more gives MSAO_ERR_UNSUPPORTED: one takes
- * 16 to 128 rows of a (sequence, kv head) and 128 tokens or more, the weight of more than 64 rows
- * 128 tokens, with the capacity and max_new for every sequence. */
+ * 2^25 bytes; out must not overlap q (refused where the host can tell). lse: device
+ * [n_rows][heads] or NULL. A row that sees no token, or only scores of -inf, gets out
+ * 0 and lse -inf and adds no weight; what a row does not see has no effect on it,
+ * whatever it holds, and a value that is not finite makes its channel infinite or NaN
+ * in the other rows that see it, whatever their p. With MSAO_ATTEND_WEIGHT, weight of
+ * (s, kv head, j) grows by the sum of p_ij over the chunk's rows and the query heads
+ * of the kv head; the order of every sum is fixed: the same call gives the same bits.
+ * For bf16, the p_ij that multiply v are rounded to bf16; sums, lse and weight are
+ * not. Workspace from msao_cache_attention_workspace, used only while the call runs on
+ * the GPU. A call of 2^24 workgroups or more gives MSAO_ERR_UNSUPPORTED: one takes 16
+ * to 128 rows of a (sequence, kv head) and 128 tokens or more, the weight of more than
+ * 64 rows 128 tokens, with the capacity and max_new for every sequence. */
 msao_status msao_cache_attention(msao_ctx* ctx, const msao_kv_cache* cache, const msao_chunk* chunk, const void* q,
                                  int64_t q_stride, int heads, float scale, uint32_t flags, void* out,
                                  int64_t out_stride, float* lse, void* workspace, size_t workspace_bytes,

@@ -93,3 +93,26 @@ def test_only_scores_of_minus_infinity(dtype, n, heads, dim, length, value):
     assert torch.equal(w[0, 1], case.weight[0, 1])
     assert torch.equal(out[n:], out0[n:]) and torch.equal(lse[n:], lse0[n:]) and torch.equal(w[1], w0[1])
     assert torch.isfinite(out[:n, :G]).all() and torch.isfinite(lse[:n, :G]).all() and torch.isfinite(w[0, 0]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("n", [3, 20, 40])
+@pytest.mark.parametrize("heads,dim", [(4, 64), (2, 96), (4, 128), (2, 256)])
+@pytest.mark.parametrize("score", ["-inf", "far below"])
+@pytest.mark.parametrize("value", [float("inf"), float("nan")], ids=str)
+def test_values_of_no_weight_that_are_not_finite(dtype, n, heads, dim, score, value):
+    """A token whose p is 0: its value still reaches the rows that see it, in a tile that all see and in the chunk's."""
+    L = 170
+    for j, first in ((5, 0), (L - 2, n - 2)):  # the token, and the first row that sees it
+        case = Case(74, [L, 40], [n, 2], heads, 2, dim, 16, dtype)
+        case.q[:n, :, 0] = case.q[:n, :, 0].abs() + 1
+        p, slot = int(case.pages[0, j // 16]), j % 16
+        case.k[p, 1, slot, 0] = float("-inf") if score == "-inf" else -1e6
+        out0, lse0, w0 = attend(case)
+        case.v[p, 1, slot, 7] = value
+        out, lse, w = attend(case)
+        hit = torch.zeros(out.shape, dtype=torch.bool)
+        hit[first:n, heads // 2:, 7] = True
+        assert not torch.isfinite(out[hit]).any()
+        assert torch.isfinite(out0).all() and torch.equal(out[~hit], out0[~hit])
+        assert torch.equal(lse, lse0) and torch.equal(w, w0)
