@@ -633,6 +633,80 @@ msao_status msao_cache_evict_workspace(const msao_kv_cache* from, size_t* bytes)
 #define MSAO_NUM_CACHE_KERNELS 7
 msao_status msao_cache_kernel_times(msao_ctx* ctx, float* ms);
 
+/* ---- Sec. 4.2: drawing tokens, and verifying drafts --------------------------- */
+
+/* How a row's distribution is made from its logits x_v, each array device [rows] or NULL
+ * (the value in brackets for every row). With m the largest logit and z_v = (x_v - m) /
+ * temperature, w_v = exp(z_v) is a token's weight. Tokens are in order by logit, the largest
+ * first, equal ones by index. Of this order stay
+ *   the first top_k (<= 0, or vocab and more: all) [all],
+ *   of these the fewest whose weight is at least top_p of theirs, one at least (1 or more,
+ *     or NaN: all) [all],
+ *   of these the ones with w_v >= min_p (0 or less, or NaN: all; more than 1 counts as 1) [all].
+ * A temperature of 0 or less, or NaN, leaves the first alone [1]. p_v = w_v / W, W the sum of
+ * those that stay. A token of logit -inf never stays. A row with a NaN or +inf logit, or with
+ * no finite one, has no distribution. Weights and their sums are 64-bit, whatever the logits. */
+typedef struct {
+    const float* temperature;
+    const int32_t* top_k;
+    const float* top_p;
+    const float* min_p;
+} msao_sampling;
+
+/* Outputs of msao_sample, each device [rows] or NULL (not written). token: the drawn one, -1
+ * of a row without a distribution. logprob: ln p of it (NaN). kept: how many tokens stay (0). */
+typedef struct {
+    int32_t* token;
+    float* logprob;
+    int32_t* kept;
+} msao_sample_out;
+
+/* A token of each of `rows` rows of logits: the first whose running sum of weights, in the order of
+ * the indices, passes u W. u: device [rows], given random numbers in [0, 1); below 0 and NaN
+ * count as 0, from 1 on the last token of weight above 0 is drawn. logits: device, row r starts at
+ * element r * row_stride, dtype MSAO_F32 or MSAO_BF16; 16-byte aligned, row_stride * element size a
+ * multiple of 16, row_stride >= vocab, 1 <= vocab <= 2^20 (MSAO_ERR_UNSUPPORTED beyond), rows <
+ * 2^24. set NULL: every default. The same call gives the same bits. Workspace from
+ * msao_sample_workspace, used only while the call runs on the GPU. */
+msao_status msao_sample(msao_ctx* ctx, const void* logits, int64_t rows, int64_t vocab, int64_t row_stride, int dtype,
+                        const msao_sampling* set, const float* u, const msao_sample_out* out, void* workspace,
+                        size_t workspace_bytes, void* stream);
+msao_status msao_sample_workspace(int64_t rows, int64_t vocab, int dtype, size_t* bytes);
+
+/* Outputs of msao_verify, each device memory or NULL (not written).
+ *   accepted [n_seqs]: how many of a sequence's drafts stand.
+ *   next [n_rows]: the token that follows a row: its draft where that stands, in the row behind
+ *     the last such one a drawn token, and -1 in the rows after it (their inputs were wrong).
+ *   logprob [n_rows]: ln p of that token in the row's distribution, NaN where there is none.
+ *   length [n_seqs]: length[s] - n + 1 + accepted, the tokens whose keys and values stay. */
+typedef struct {
+    int32_t* accepted;
+    int32_t* next;
+    float* logprob;
+    int32_t* length;
+} msao_verify_out;
+
+/* Verification of a speculative round over the rows of a chunk (see msao_chunk): tokens (device [n_rows])
+ * are the ones that the model was given, of each sequence first one that is certain and then its
+ * drafts; row i's logits, and its distribution p, are of the token that follows it, so the draft in
+ * row i + 1 is verified by row i. A draft d stands if the ones before it do and u_accept q(d) <
+ * p(d). q is the distribution that the draft was drawn from: of draft_logits, laid out like logits
+ * (row i's for the draft in row i + 1), by the same settings; without draft_logits (NULL), or where
+ * their row has no distribution, q(d) is 1. In the first row whose draft does not stand a token is
+ * drawn from what p has more than q, max(p - q, 0), in the last row of a sequence one from p: as
+ * msao_sample draws it, by u. (Where p has nothing more than q, from p.) So the tokens are
+ * distributed as if each had been drawn from p. A draft outside [0, vocab) does not stand. A row
+ * without a distribution ends its sequence with the token -1. u_accept, u: device [n_rows],
+ * given random numbers as in msao_sample. Of a sequence with more than max_new rows the first max_new are
+ * looked at. Rows of no sequence are left as they are. length (device [n_seqs]) is needed for
+ * out->length. n_seqs * max_new below 2^24; settings arrays have n_rows entries; out's arrays share no
+ * memory with the inputs, but out->length may be length. Workspace from msao_verify_workspace. */
+msao_status msao_verify(msao_ctx* ctx, const msao_chunk* chunk, int32_t n_seqs, const int32_t* tokens, const void* logits,
+                        const void* draft_logits, int64_t vocab, int64_t row_stride, int64_t draft_stride, int dtype,
+                        const msao_sampling* set, const float* u_accept, const float* u, const int32_t* length,
+                        const msao_verify_out* out, void* workspace, size_t workspace_bytes, void* stream);
+msao_status msao_verify_workspace(const msao_chunk* chunk, int32_t n_seqs, int64_t vocab, int dtype, size_t* bytes);
+
 /* ---- Sec. 4.2.2: Algorithm 1 on the host ----------------------------------- */
 
 /* Parameters of Algorithm 1 (defaults from Sec. 5.1: P_target 0.8, N_max 5,
@@ -718,6 +792,18 @@ double msao_expected_e2e_latency(const msao_latency_model* m);
 #define MSAO_KERNEL_CLIP 7    /* the SimHash run's clips: statistics and signatures in one pass */
 #define MSAO_KERNEL_READ 8    /* msao_stream_read: the plain streaming read */
 #define MSAO_NUM_KERNELS 9
+
+/* And of the kernels of a speculative round, for msao_round_kernel_times. */
+#define MSAO_ROUND_KERNEL_SAMPLE 0
+#define MSAO_ROUND_KERNEL_VERIFY 1        /* each row's draft and token */
+#define MSAO_ROUND_KERNEL_VERIFY_JOIN 2   /* up to the first draft that does not stand */
+#define MSAO_ROUND_KERNEL_RESIZE 3
+#define MSAO_ROUND_KERNEL_RESIZE_FILL 4   /* its tables and slots where they are many */
+#define MSAO_ROUND_KERNEL_SHARED 5        /* attention over the shared prefixes */
+#define MSAO_ROUND_KERNEL_OWN 6           /* and over each sequence's own tokens */
+#define MSAO_ROUND_KERNEL_SHARED_JOIN 7
+#define MSAO_NUM_ROUND_KERNELS 8
+msao_status msao_round_kernel_times(msao_ctx* ctx, float* ms);
 
 /* When enabled, every launch is bracketed by a pair of HIP events recorded on
  * the caller's stream. */

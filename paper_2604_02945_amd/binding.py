@@ -32,6 +32,8 @@ APPEND_NEIGHBOURS = 1
 ATTEND_CAUSAL, ATTEND_WEIGHT = 1, 2
 (CACHE_KERNEL_APPEND, CACHE_KERNEL_ATTEND, CACHE_KERNEL_COMBINE, CACHE_KERNEL_WEIGHT,
  CACHE_KERNEL_WEIGHT_JOIN, CACHE_KERNEL_SELECT, CACHE_KERNEL_MOVE, NUM_CACHE_KERNELS) = 0, 1, 2, 3, 4, 5, 6, 7
+(ROUND_KERNEL_SAMPLE, ROUND_KERNEL_VERIFY, ROUND_KERNEL_VERIFY_JOIN, ROUND_KERNEL_RESIZE, ROUND_KERNEL_RESIZE_FILL,
+ ROUND_KERNEL_SHARED, ROUND_KERNEL_OWN, ROUND_KERNEL_SHARED_JOIN, NUM_ROUND_KERNELS) = 0, 1, 2, 3, 4, 5, 6, 7, 8
 
 STATUS = {0: "MSAO_OK", 1: "MSAO_ERR_INVALID_ARG", 2: "MSAO_ERR_ALIGNMENT", 3: "MSAO_ERR_WORKSPACE",
           4: "MSAO_ERR_UNSUPPORTED", 5: "MSAO_ERR_HIP"}
@@ -123,6 +125,18 @@ class MsaoAppend(ctypes.Structure):
                 ("n_axes", ctypes.c_int32), ("sections", ctypes.c_int32 * MAX_AXES), ("flags", ctypes.c_uint32)]
 
 
+class MsaoSampling(ctypes.Structure):
+    _fields_ = [(n, _P) for n in ("temperature", "top_k", "top_p", "min_p")]
+
+
+class MsaoSampleOut(ctypes.Structure):
+    _fields_ = [(n, _P) for n in ("token", "logprob", "kept")]
+
+
+class MsaoVerifyOut(ctypes.Structure):
+    _fields_ = [(n, _P) for n in ("accepted", "next", "logprob", "length")]
+
+
 class MsaoError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"{STATUS.get(status, status)}: {message}")
@@ -180,6 +194,13 @@ SIGNATURES = [
                                         ctypes.c_size_t, _P]),
     ("msao_cache_evict_workspace", ctypes.c_int, [_P, _P]),
     ("msao_cache_kernel_times", ctypes.c_int, [_P, _P]),
+    ("msao_sample", ctypes.c_int, [_P, _P, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int, _P, _P, _P, _P,
+                                   ctypes.c_size_t, _P]),
+    ("msao_sample_workspace", ctypes.c_int, [ctypes.c_int64, ctypes.c_int64, ctypes.c_int, _P]),
+    ("msao_verify", ctypes.c_int, [_P, _P, ctypes.c_int32, _P, _P, _P, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64,
+                                   ctypes.c_int, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
+    ("msao_verify_workspace", ctypes.c_int, [_P, ctypes.c_int32, ctypes.c_int64, ctypes.c_int, _P]),
+    ("msao_round_kernel_times", ctypes.c_int, [_P, _P]),
     ("msao_stream_read", ctypes.c_int, [_P, _P, ctypes.c_int64, ctypes.c_int, _P, ctypes.c_int64, _P]),
     ("msao_sched_default_params", MsaoSchedParams, []),
     ("msao_sched_init", ctypes.c_int, [_P, ctypes.c_int64, _P, _P]),
@@ -314,6 +335,11 @@ class Context:
     def cache_kernel_times(self) -> List[float]:
         ms = (ctypes.c_float * NUM_CACHE_KERNELS)()
         _check(lib().msao_cache_kernel_times(self.handle, ms), self)
+        return list(ms)
+
+    def round_kernel_times(self) -> List[float]:
+        ms = (ctypes.c_float * NUM_ROUND_KERNELS)()
+        _check(lib().msao_round_kernel_times(self.handle, ms), self)
         return list(ms)
 
 
@@ -1014,6 +1040,180 @@ def msao_cache_evict(cache: KvCache, budget: torch.Tensor, n_first: int = 0, n_r
                                   _fits("n_first", min(n_first, INT_MAX)), _fits("n_recent", min(n_recent, INT_MAX)), kept_idx.data_ptr(), kept_idx.shape[2],
                                   workspace.data_ptr(), _bytes_of(workspace), _stream_of(cache, stream)), ctx)
     return {"kept_idx": kept_idx, "kept_count": (to or cache).length}
+
+
+# ---- Sec. 4.2: drawing tokens, and verifying drafts ------------------------------
+
+def _vector(name: str, t: torch.Tensor, n: int, dtype: torch.dtype, index: int):
+    """A contiguous [n] tensor of the dtype on the device of that index."""
+    if t.dtype is not dtype or t.dim() != 1 or t.shape[0] != n:
+        raise ValueError(f"{name} must be {str(dtype)[6:]} [{n}]")
+    if n > 1 and t.stride(0) != 1:
+        raise ValueError(f"{name} must be contiguous")
+    if t.get_device() != index:
+        raise ValueError(f"{name} must be on the device of the logits")
+    return t.data_ptr()
+
+
+def _logit_rows(name: str, logits: torch.Tensor, vocab: Optional[int]):
+    """Rows, vocabulary, elements between rows, and dtype of a [rows, row_stride] tensor of logits."""
+    if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"{name} must be a 2-D float32 or bfloat16 tensor")
+    rows, width = (int(x) for x in logits.shape)
+    V = width if vocab is None else int(vocab)
+    if not 1 <= V <= width:
+        raise ValueError(f"vocab must be 1 .. {width}, the columns of {name}")
+    if logits.numel() and logits.stride(1) != 1 and width > 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    es = logits.element_size()
+    # (the only row is at no distance, whatever torch says)
+    stride = int(logits.stride(0)) if rows > 1 else -(-width * es // 16) * 16 // es
+    return rows, V, stride, F32 if logits.dtype == torch.float32 else BF16
+
+
+def _round_ctx(device: torch.device, index: int, ctx: Optional[Context], stream) -> Context:
+    if index < 0:
+        raise ValueError(f"the logits are on {device}, not on a GPU")
+    if ctx is None:
+        ctx = default_context(index)
+    elif ctx.device != index:
+        raise ValueError(f"the context is of device {ctx.device}, the logits on {device}")
+    if stream is not None and stream.device != device:
+        raise ValueError(f"the stream is of {stream.device}, the logits on {device}")
+    return ctx
+
+
+def _settings(rows: int, index: int, temperature, top_k, top_p, min_p) -> MsaoSampling:
+    s = MsaoSampling()
+    for name, t, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                           ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+        if t is not None:
+            setattr(s, name, _vector(name, t, rows, dtype, index))
+    return s
+
+
+def _outputs(struct, outputs, shapes, device, index: int, stream):
+    """The struct over `outputs` (None: all of `shapes` allocated)."""
+    if outputs is None:
+        with _on(stream):
+            outputs = {k: torch.empty(n, dtype=dtype, device=device) for k, (n, dtype) in shapes.items()}
+    for k, t in outputs.items():
+        if k not in shapes:
+            raise ValueError(f"unknown output {k}: there are {', '.join(shapes)}")
+        if t is not None:
+            setattr(struct, k, _vector(k, t, *shapes[k], index))
+    return outputs
+
+
+def _workspace_for(workspace: Optional[torch.Tensor], need: int, device, index: int, stream):
+    """Address and bytes of the caller's workspace, or of one allocated for the call (kept by the third)."""
+    if workspace is None:
+        if need == 0:
+            return None, 0, None
+        with _on(stream):
+            buf = torch.empty(need, dtype=torch.uint8, device=device)
+            buf = buf if buf.data_ptr() % 256 == 0 else _workspace(need, device)
+        return buf.data_ptr(), need, buf
+    if workspace.get_device() != index:
+        raise ValueError("workspace must be on the call's device")
+    return workspace.data_ptr(), _bytes_of(workspace), workspace
+
+
+def sample_workspace(rows: int, vocab: int, dtype: torch.dtype) -> int:
+    """Bytes of workspace that msao_sample needs for such a call."""
+    n = ctypes.c_size_t()
+    _check(lib().msao_sample_workspace(rows, vocab, F32 if dtype == torch.float32 else BF16, ctypes.byref(n)))
+    return n.value
+
+
+def msao_sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Tensor] = None,
+                top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+                min_p: Optional[torch.Tensor] = None, vocab: Optional[int] = None,
+                outputs: Optional[Dict[str, torch.Tensor]] = None, workspace: Optional[torch.Tensor] = None,
+                ctx: Optional[Context] = None, stream=None) -> Dict[str, torch.Tensor]:
+    """A token of each row of a [rows, row_stride] float32/bfloat16 device tensor (the first `vocab`
+    columns are the logits; rows at multiples of 16 bytes), drawn by the numbers u float32 [rows] in
+    [0, 1). temperature, top_p, min_p float32 [rows] and top_k int32 [rows], each None for no such
+    setting; 0 as a temperature takes the largest logit. Returns device tensors token (int32; -1 of a
+    row with a NaN or +inf, or without a finite logit), logprob and kept (int32, tokens that could have
+    been drawn); `outputs` may name some of them to fill."""
+    rows, V, stride, dt = _logit_rows("logits", logits, vocab)
+    index, dev = logits.get_device(), logits.device
+    ctx = _round_ctx(dev, index, ctx, stream)
+    s = _settings(rows, index, temperature, top_k, top_p, min_p)
+    out = MsaoSampleOut()
+    o = _outputs(out, outputs, {"token": (rows, torch.int32), "logprob": (rows, torch.float32), "kept": (rows, torch.int32)},
+                 dev, index, stream)
+    at = _vector("u", u, rows, torch.float32, index)
+    need = ctypes.c_size_t()
+    if workspace is None:
+        _check(lib().msao_sample_workspace(rows, V, dt, ctypes.byref(need)))
+    ws, given, _keep = _workspace_for(workspace, need.value, dev, index, stream)
+    _check(lib().msao_sample(ctx.handle, logits.data_ptr() if rows else None, rows, V, stride, dt, ctypes.byref(s), at,
+                             ctypes.byref(out), ws, given,
+                             torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream), ctx)
+    return o
+
+
+def _round_chunk(start: torch.Tensor, n_rows: int, max_new: int, index: int) -> MsaoChunk:
+    _int32("start", start, 1)
+    if start.shape[0] < 1:
+        raise ValueError("start must have n_seqs + 1 entries")
+    if start.get_device() != index:
+        raise ValueError("start must be on the device of the logits")
+    return MsaoChunk(start.data_ptr(), _fits("n_rows", n_rows), _fits("max_new", min(max_new, max(n_rows, 0))))
+
+
+def verify_workspace(start: torch.Tensor, max_new: int, rows: int, vocab: int, dtype: torch.dtype) -> int:
+    """Bytes of workspace that msao_verify needs for such a call."""
+    ch, n = _round_chunk(start, rows, max_new, start.get_device()), ctypes.c_size_t()
+    _check(lib().msao_verify_workspace(ctypes.byref(ch), start.shape[0] - 1, vocab, F32 if dtype == torch.float32 else BF16,
+                                       ctypes.byref(n)))
+    return n.value
+
+
+def msao_verify(start: torch.Tensor, max_new: int, tokens: torch.Tensor, logits: torch.Tensor, u_accept: torch.Tensor,
+                u: torch.Tensor, temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+                top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None, vocab: Optional[int] = None,
+                draft_logits: Optional[torch.Tensor] = None, length: Optional[torch.Tensor] = None,
+                outputs: Optional[Dict[str, torch.Tensor]] = None, workspace: Optional[torch.Tensor] = None,
+                ctx: Optional[Context] = None, stream=None) -> Dict[str, torch.Tensor]:
+    """Verification of drafts: rows start[s] .. start[s+1]-1 of tokens int32 [rows] are a token of sequence s that
+    is certain and its drafts, those of logits [rows, row_stride] what the model gives behind each. A draft
+    stands by u_accept float32 [rows], and where one does not (or behind the last) a token is drawn by u, so that
+    tokens are distributed as ones drawn by msao_sample with the same settings, float32 or int32 [rows].
+    draft_logits: what the drafts were drawn from by the same settings, row i's for the draft in row i + 1
+    (None: each draft was certain, as a greedy one is). Returns device tensors accepted int32 [n_seqs], next
+    int32 [rows] (the token behind each row, -1 behind the last that stands), logprob [rows], and
+    with `length` int32 [n_seqs] (that counts the rows) length: the tokens whose keys and values stay."""
+    rows, V, stride, dt = _logit_rows("logits", logits, vocab)
+    index, dev = logits.get_device(), logits.device
+    ctx = _round_ctx(dev, index, ctx, stream)
+    ch = _round_chunk(start, rows, max_new, index)
+    n_seqs = start.shape[0] - 1
+    s = _settings(rows, index, temperature, top_k, top_p, min_p)
+    draft, draft_stride = None, 0
+    if draft_logits is not None:
+        r2, v2, draft_stride, dt2 = _logit_rows("draft_logits", draft_logits, V)
+        if r2 != rows or dt2 != dt or draft_logits.get_device() != index:
+            raise ValueError("draft_logits must have the rows, dtype and device of logits")
+        draft = draft_logits.data_ptr() if rows else None
+    shapes = {"accepted": (n_seqs, torch.int32), "next": (rows, torch.int32), "logprob": (rows, torch.float32)}
+    if length is not None:
+        shapes["length"] = (n_seqs, torch.int32)
+    out = MsaoVerifyOut()
+    o = _outputs(out, outputs, shapes, dev, index, stream)
+    need = ctypes.c_size_t()
+    if workspace is None:
+        _check(lib().msao_verify_workspace(ctypes.byref(ch), n_seqs, V, dt, ctypes.byref(need)))
+    ws, given, _keep = _workspace_for(workspace, need.value, dev, index, stream)
+    _check(lib().msao_verify(ctx.handle, ctypes.byref(ch), n_seqs, _vector("tokens", tokens, rows, torch.int32, index),
+                             logits.data_ptr() if rows else None, draft, V, stride, draft_stride, dt, ctypes.byref(s),
+                             _vector("u_accept", u_accept, rows, torch.float32, index), _vector("u", u, rows, torch.float32, index),
+                             None if length is None else _vector("length", length, n_seqs, torch.int32, index),
+                             ctypes.byref(out), ws, given,
+                             torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream), ctx)
+    return o
 
 
 def sched_default_params() -> MsaoSchedParams:

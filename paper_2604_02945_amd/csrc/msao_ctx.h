@@ -47,6 +47,7 @@ struct msao_ctx {
     std::vector<hipEvent_t> pool;                       // free events
     std::vector<std::pair<hipEvent_t, hipEvent_t>> rec[MSAO_NUM_KERNELS];
     std::vector<std::pair<hipEvent_t, hipEvent_t>> cache_rec[MSAO_NUM_CACHE_KERNELS];
+    std::vector<std::pair<hipEvent_t, hipEvent_t>> round_rec[MSAO_NUM_ROUND_KERNELS];
     // tuning
     int row_item_bytes = 8192;
     int chain_frames = 0;       // frames per temporal work item; 0 = automatic

@@ -1076,6 +1076,7 @@ void msao_destroy(msao_ctx* ctx)
     };
     reclaim(ctx->rec, MSAO_NUM_KERNELS);
     reclaim(ctx->cache_rec, MSAO_NUM_CACHE_KERNELS);
+    reclaim(ctx->round_rec, MSAO_NUM_ROUND_KERNELS);
     for (hipEvent_t e : ctx->pool) (void)hipEventDestroy(e);
     delete ctx;
 }

@@ -1,0 +1,61 @@
+// msao_sample.h -- arguments of the kernels that draw tokens from rows of logits and
+// verify drafts against them. Not part of the ABI.
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "msao_cache.h"
+
+namespace msao {
+
+// Rows of logits: row r starts at base + r * row_bytes.
+struct LogitRows {
+    const uint8_t* base;
+    int64_t row_bytes;
+};
+
+// msao_sampling: per row, each may be NULL.
+struct SamplingDev {
+    const float* temperature;
+    const int32_t* top_k;
+    const float* top_p;
+    const float* min_p;
+};
+
+constexpr int64_t kMaxVocab = (int64_t)1 << 20;
+
+struct SampleArgs {
+    LogitRows logits;
+    SamplingDev set;
+    const float* u;
+    int32_t rows, vocab, dtype;
+    int32_t* token;
+    float* logprob;
+    int32_t* kept;
+};
+
+struct VerifyArgs {
+    LogitRows logits, draft;   // draft.base NULL: drafts are certain
+    SamplingDev set;
+    ChunkDev ch;
+    int32_t n_seqs, vocab, dtype;
+    const int32_t* tokens;
+    const float* u_accept;
+    const float* u;
+    const int32_t* length;
+    int32_t* accepted;
+    int32_t* next;
+    float* logprob;
+    int32_t* length_out;
+    // workspace [n_rows]
+    int32_t* row_token;        // the token that follows the row
+    float* row_logprob;
+    int32_t* row_yes;          // whether it is the row's draft
+};
+
+int launch_sample(const SampleArgs& a, void* stream, void* ev0, void* ev1);
+int launch_verify(const VerifyArgs& a, void* stream, void* ev0, void* ev1);
+int launch_verify_join(const VerifyArgs& a, void* stream, void* ev0, void* ev1);
+
+}  // namespace msao
