@@ -621,6 +621,51 @@ msao_status msao_cache_evict(msao_ctx* ctx, const msao_kv_cache* from, const msa
                              int64_t idx_stride, void* workspace, size_t workspace_bytes, void* stream);
 msao_status msao_cache_evict_workspace(const msao_kv_cache* from, size_t* bytes);
 
+/* The pages that no sequence has: free[0 .. count - 1] (device [cache->n_pages] and [1]), the
+ * last of them the next to be taken. A count outside [0, n_pages] counts as the nearer end. */
+typedef struct {
+    int32_t* free;
+    int32_t* count;
+} msao_page_pool;
+
+/* What msao_cache_resize takes and fills besides the cache and the pool; device memory, each but
+ * want may be NULL.
+ *   want [n_seqs]: tokens that each sequence is to have, taken into [0, capacity].
+ *   held [n_seqs], taken into [0, pages_per_seq]: the first columns of a sequence's table that are
+ *     not its own (a shared prefix's): never given back, and none are taken for them.
+ *   columns [n_seqs]: how many columns of its table name pages, the held ones among them; read and
+ *     updated. NULL: as many as length and held take.
+ *   start [n_seqs + 1]: the chunk that the growth is: sequence s grows by rows start[s] ..
+ *     start[s+1] - 1 (one that does not grow has none).
+ *   slots, positions [n_rows]: of each such row below n_rows its place in the pool, page *
+ *     page_size + slot (-1 where the table names no page), and its place in the sequence; rows from
+ *     start[n_seqs] on are left as they are.
+ *   granted [n_seqs]: 1, or 0 of a sequence that wants more pages than there are. */
+typedef struct {
+    const int32_t* want;
+    const int32_t* held;
+    int32_t* columns;
+    int32_t* start;
+    int64_t* slots;
+    int32_t* positions;
+    int32_t n_rows;
+    uint8_t* granted;
+} msao_resize;
+
+/* Each sequence given the pages that want[s] tokens take, max(ceil(want / page_size), held) columns, its
+ * length set to want[s]: for the rows of the next step, for what a verification left (msao_verify's length),
+ * for requests that begin (from length 0) or end (want 0). Columns that are added take pages from the
+ * pool, in the order of sequences and columns from its last on; columns that are no longer needed go
+ * back to it, so that the j-th of them, in the same order, is the j-th from its new end, and
+ * become -1. Pages given back by a call are free from the next call on. A sequence that needs
+ * more pages, where those that it and the ones before it need are more than the pool has, stays
+ * as it is in length, columns and pages. The table's columns below `columns` should name
+ * different pages of the pool; what they name is moved as it is. The order of everything is
+ * fixed. Workspace from msao_cache_resize_workspace. */
+msao_status msao_cache_resize(msao_ctx* ctx, const msao_kv_cache* cache, const msao_page_pool* pool, const msao_resize* in,
+                              void* workspace, size_t workspace_bytes, void* stream);
+msao_status msao_cache_resize_workspace(const msao_kv_cache* cache, const msao_resize* in, size_t* bytes);
+
 /* Mean milliseconds per launch of the cache's kernels since the previous query,
  * as msao_kernel_times gives them for the others. */
 #define MSAO_CACHE_KERNEL_APPEND 0

@@ -125,6 +125,15 @@ class MsaoAppend(ctypes.Structure):
                 ("n_axes", ctypes.c_int32), ("sections", ctypes.c_int32 * MAX_AXES), ("flags", ctypes.c_uint32)]
 
 
+class MsaoPagePool(ctypes.Structure):
+    _fields_ = [("free", _P), ("count", _P)]
+
+
+class MsaoResize(ctypes.Structure):
+    _fields_ = [("want", _P), ("held", _P), ("columns", _P), ("start", _P), ("slots", _P), ("positions", _P),
+                ("n_rows", ctypes.c_int32), ("granted", _P)]
+
+
 class MsaoSampling(ctypes.Structure):
     _fields_ = [(n, _P) for n in ("temperature", "top_k", "top_p", "min_p")]
 
@@ -194,6 +203,8 @@ SIGNATURES = [
                                         ctypes.c_size_t, _P]),
     ("msao_cache_evict_workspace", ctypes.c_int, [_P, _P]),
     ("msao_cache_kernel_times", ctypes.c_int, [_P, _P]),
+    ("msao_cache_resize", ctypes.c_int, [_P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
+    ("msao_cache_resize_workspace", ctypes.c_int, [_P, _P, _P]),
     ("msao_sample", ctypes.c_int, [_P, _P, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int, _P, _P, _P, _P,
                                    ctypes.c_size_t, _P]),
     ("msao_sample_workspace", ctypes.c_int, [ctypes.c_int64, ctypes.c_int64, ctypes.c_int, _P]),
@@ -1040,6 +1051,82 @@ def msao_cache_evict(cache: KvCache, budget: torch.Tensor, n_first: int = 0, n_r
                                   _fits("n_first", min(n_first, INT_MAX)), _fits("n_recent", min(n_recent, INT_MAX)), kept_idx.data_ptr(), kept_idx.shape[2],
                                   workspace.data_ptr(), _bytes_of(workspace), _stream_of(cache, stream)), ctx)
     return {"kept_idx": kept_idx, "kept_count": (to or cache).length}
+
+
+class PagePool:
+    """The pages of a cache that no sequence has (msao_page_pool): free int32 [n_pages], of which the
+    first count (int32 [1]) are free, the last of them the next to be taken. Used in place."""
+
+    def __init__(self, free: torch.Tensor, count: torch.Tensor):
+        _int32("free", free, 1)
+        _int32("count", count, 1)
+        if count.shape[0] != 1:
+            raise ValueError("count must have one entry")
+        self.index = free.get_device()
+        _same_device(self.index, "count", count)
+        self.free, self.count, self.n_pages = free, count, int(free.shape[0])
+        self.struct = MsaoPagePool(free.data_ptr() if self.n_pages else None, count.data_ptr())
+        self.addr = _addr(self.struct)
+
+
+def _resize_struct(cache: KvCache, want: torch.Tensor, held, columns, start, slots, positions, granted) -> MsaoResize:
+    n, r = cache.n_seqs, MsaoResize()
+    rows = None
+    for name, t, entries, dtype in (("want", want, n, torch.int32), ("held", held, n, torch.int32), ("columns", columns, n, torch.int32),
+                                    ("start", start, n + 1, torch.int32), ("slots", slots, None, torch.int64),
+                                    ("positions", positions, None, torch.int32), ("granted", granted, n, torch.uint8)):
+        if t is None:
+            continue
+        if t.dtype is not dtype or t.dim() != 1 or (entries is not None and t.shape[0] != entries):
+            raise ValueError(f"{name} must be {str(dtype)[6:]} [{'rows' if entries is None else entries}]")
+        if t.shape[0] > 1 and t.stride(0) != 1:
+            raise ValueError(f"{name} must be contiguous")
+        if entries is None:
+            if rows is not None and t.shape[0] != rows:
+                raise ValueError("slots and positions differ in rows")
+            rows = t.shape[0]
+        setattr(r, name, t.data_ptr())
+    _same_device(cache.index, "every tensor of the call", want, held, columns, start, slots, positions, granted)
+    r.n_rows = _fits("rows", rows or 0)
+    return r
+
+
+def cache_resize_workspace(cache: KvCache, rows: int = 0) -> int:
+    """Bytes of workspace that msao_cache_resize needs for slots or positions of that many rows."""
+    r, n = MsaoResize(), ctypes.c_size_t()
+    r.n_rows = _fits("rows", rows)
+    if rows > 0:
+        r.positions = 4  # (that there are some is all that counts)
+    _check(lib().msao_cache_resize_workspace(cache.addr, ctypes.byref(r), ctypes.byref(n)))
+    return n.value
+
+
+def msao_cache_resize(cache: KvCache, pool: PagePool, want: torch.Tensor, held: Optional[torch.Tensor] = None,
+                      columns: Optional[torch.Tensor] = None, start: Optional[torch.Tensor] = None,
+                      slots: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                      granted: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                      ctx: Optional[Context] = None, stream=None) -> Dict[str, Optional[torch.Tensor]]:
+    """Each sequence's length set to want[s] (int32 [n_seqs]) and its table given the pages that these
+    tokens take, from the pool or back to it; all of it on the device. held int32 [n_seqs]: the first columns
+    of a table that are not the sequence's own. columns int32 [n_seqs], updated: how many columns name pages
+    (None: as many as the lengths take; pass it where msao_cache_evict shortens sequences). Filled:
+    start int32 [n_seqs + 1], the chunk that the growth is, and granted uint8 [n_seqs], 0 where the pool has
+    too few pages (both allocated when None); slots int64 [rows] and positions int32 [rows] where given: place
+    in the pool and in the sequence of each row below start[n_seqs]. Returns them."""
+    ctx = _cache_ctx(cache, ctx, stream)
+    if pool.index != cache.index or pool.n_pages != cache.n_pages:
+        raise ValueError("the pool must be on the cache's device and have an entry for each of its pages")
+    if start is None or granted is None:
+        with _on(stream):
+            start = torch.empty(cache.n_seqs + 1, dtype=torch.int32, device=cache.device) if start is None else start
+            granted = torch.empty(cache.n_seqs, dtype=torch.uint8, device=cache.device) if granted is None else granted
+    r = _resize_struct(cache, want, held, columns, start, slots, positions, granted)
+    need = ctypes.c_size_t()
+    if workspace is None:
+        _check(lib().msao_cache_resize_workspace(cache.addr, ctypes.byref(r), ctypes.byref(need)))
+    ws, given, _keep = _workspace_for(workspace, need.value, cache.device, cache.index, stream)
+    _check(lib().msao_cache_resize(ctx.handle, cache.addr, pool.addr, ctypes.byref(r), ws, given, _stream_of(cache, stream)), ctx)
+    return {"start": start, "slots": slots, "positions": positions, "granted": granted}
 
 
 # ---- Sec. 4.2: drawing tokens, and verifying drafts ------------------------------

@@ -11,7 +11,7 @@ LIB = os.path.join(HERE, "libmsao.so")
 SOURCES = [os.path.join(HERE, "csrc", f) for f in
            ("msao_host.cpp", "msao_sched.cpp", "msao_kernels.hip", "msao_entropy.hip", "msao_simhash.hip",
             "msao_scratch.hip", "msao_calib.hip", "msao_upload.hip", "msao_cache_host.cpp", "msao_cache.hip",
-            "msao_attend.hip", "msao_sample_host.cpp", "msao_sample.hip")]
+            "msao_attend.hip", "msao_pages.hip", "msao_sample_host.cpp", "msao_sample.hip")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

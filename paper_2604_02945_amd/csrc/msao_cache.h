@@ -184,6 +184,66 @@ struct EvictArgs {
     Group units;                   // 16-byte pieces of a row's part
 };
 
+// ---- pages from lengths -----------------------------------------------------------
+struct ResizePlan {                // of one sequence
+    int32_t length, columns;       // before
+    int32_t need;                  // columns after
+    int32_t take, back;            // pages taken and given back by the sequences before it
+    int32_t row;                   // rows before its first
+};
+struct ResizeArgs {
+    int32_t* pages;
+    int64_t table_stride;
+    int32_t* length;
+    int32_t per_seq, page_shift, n_seqs, n_pages;
+    int32_t* free;
+    int32_t* count;
+    const int32_t* want;
+    const int32_t* held;           // NULL: none
+    int32_t* columns;              // NULL: from the length
+    int32_t* start;
+    int64_t* slots;
+    int32_t* positions;
+    uint8_t* granted;
+    int32_t n_rows;
+    // workspace, where the launch is two
+    ResizePlan* plan;              // [n_seqs]
+    int32_t* moved;                // [4]: pages taken, given back, free afterwards below what is given back; rows
+    int32_t* taken;                // [resize_most_taken] the pages taken, in their order
+};
+// Up to so many sequences and rows one workgroup does everything.
+constexpr int32_t kResizeSeqs = 1024, kResizeRows = 8192;
+MSAO_HD bool resize_in_one(const ResizeArgs& a) { return a.n_seqs <= kResizeSeqs && a.n_rows <= kResizeRows; }
+MSAO_HD int64_t resize_most_taken(const ResizeArgs& a)
+{
+    const int64_t all = (int64_t)a.n_seqs * a.per_seq;
+    return all < a.n_pages ? all : a.n_pages;
+}
+
+// Columns that n tokens take; a sequence's own begin behind the held ones.
+MSAO_HD int columns_of(const ResizeArgs& a, int n, int held)
+{
+    const int c = (int)(((int64_t)n + ((int64_t)1 << a.page_shift) - 1) >> a.page_shift);
+    return c > held ? c : held;
+}
+
+// The last of n ascending offsets (each what lies before an item; the first is 0) that is at most i: the item
+// that i falls into, as the ones of no extent have the next one's offset.
+template <typename F>
+MSAO_HD int item_of(int n, int64_t i, F offset)
+{
+    int lo = 0, hi = n;  // offset(lo) <= i < offset(hi)
+    while (hi - lo > 1) {
+        const int mid = (int)(((unsigned)lo + (unsigned)hi) >> 1);
+        if (offset(mid) <= i) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+int launch_resize(const ResizeArgs& a, void* stream, void* ev0, void* ev1);
+int launch_resize_fill(const ResizeArgs& a, void* stream, void* ev0, void* ev1);
+
 int launch_append(const AppendArgs& a, void* stream, void* ev0, void* ev1);
 int launch_attend(const AttendArgs& a, void* stream, void* ev0, void* ev1);
 int launch_combine(const AttendArgs& a, void* stream, void* ev0, void* ev1);

@@ -235,6 +235,51 @@ int run_weight_join(const void* a, void* s, void* e0, void* e1) { return launch_
 int run_select(const void* a, void* s, void* e0, void* e1) { return launch_select(*(const EvictArgs*)a, s, e0, e1); }
 int run_move(const void* a, void* s, void* e0, void* e1) { return launch_move(*(const EvictArgs*)a, s, e0, e1); }
 
+int run_resize(const void* a, void* s, void* e0, void* e1) { return launch_resize(*(const ResizeArgs*)a, s, e0, e1); }
+int run_resize_fill(const void* a, void* s, void* e0, void* e1) { return launch_resize_fill(*(const ResizeArgs*)a, s, e0, e1); }
+
+// The arguments and the workspace of a resize.
+struct ResizeSizes {
+    ResizeArgs a;
+    size_t plan, moved, taken, total;
+};
+msao_status resize_plan(const msao_kv_cache* cache, const msao_resize* in, ResizeSizes& pl, std::string* err)
+{
+    MSAO_TRY(check_cache(cache, err));
+    if (!in) return bad(err, "in is NULL");
+    if (in->n_rows < 0) return bad(err, "n_rows is negative");
+    ResizeArgs& a = pl.a;
+    std::memset(&a, 0, sizeof a);
+    a.pages = const_cast<int32_t*>(cache->pages);
+    a.table_stride = cache->table_stride;
+    a.length = cache->length;
+    a.per_seq = cache->pages_per_seq;
+    a.page_shift = shift_of(cache->page_size);
+    a.n_seqs = cache->n_seqs;
+    a.n_pages = cache->n_pages;
+    a.want = in->want;
+    a.held = in->held;
+    a.columns = in->columns;
+    a.start = in->start;
+    a.slots = in->slots;
+    a.positions = in->positions;
+    a.granted = in->granted;
+    a.n_rows = in->slots || in->positions ? in->n_rows : 0;
+    if ((int64_t)a.n_seqs * a.per_seq > INT32_MAX) return fail(err, MSAO_ERR_UNSUPPORTED, "tables of 2^31 columns or more");
+    pl.plan = pl.moved = pl.taken = pl.total = 0;
+    if (!resize_in_one(a)) {
+        pl.moved = align_up((size_t)a.n_seqs * sizeof(ResizePlan), kWsAlign);
+        pl.taken = pl.moved + kWsAlign;
+        pl.total = pl.taken + align_up((size_t)resize_most_taken(a) * 4, kWsAlign);
+    }
+    return MSAO_OK;
+}
+
+msao_status round_launch(msao_ctx* ctx, int kernel, void* stream, int (*fn)(const void*, void*, void*, void*), const void* a)
+{
+    return launched_in(ctx, ctx->round_rec[kernel], (hipStream_t)stream, fn, a);
+}
+
 msao_status cache_launch(msao_ctx* ctx, int kernel, void* stream, int (*fn)(const void*, void*, void*, void*), const void* a)
 {
     return launched_in(ctx, ctx->cache_rec[kernel], (hipStream_t)stream, fn, a);
@@ -416,6 +461,47 @@ msao_status msao_cache_evict(msao_ctx* ctx, const msao_kv_cache* from, const msa
         DeviceGuard guard(ctx->device);
         MSAO_TRY(cache_launch(ctx, MSAO_CACHE_KERNEL_SELECT, stream, run_select, &a));
         return cache_launch(ctx, MSAO_CACHE_KERNEL_MOVE, stream, run_move, &a);
+    });
+}
+
+msao_status msao_cache_resize_workspace(const msao_kv_cache* cache, const msao_resize* in, size_t* bytes)
+{
+    return guarded([&]() -> msao_status {
+        if (!bytes) return bad(&g_err, "bytes is NULL");
+        ResizeSizes pl;
+        MSAO_TRY(resize_plan(cache, in, pl, &g_err));
+        *bytes = pl.total;
+        return MSAO_OK;
+    });
+}
+
+msao_status msao_cache_resize(msao_ctx* ctx, const msao_kv_cache* cache, const msao_page_pool* pool, const msao_resize* in,
+                              void* workspace, size_t workspace_bytes, void* stream)
+{
+    return guarded([&]() -> msao_status {
+        std::string* err = ctx ? &ctx->err : &g_err;
+        ResizeSizes pl;
+        MSAO_TRY(resize_plan(cache, in, pl, err));
+        ResizeArgs& a = pl.a;
+        if (!pool || !pool->count || (!pool->free && cache->n_pages > 0)) return bad(err, "pool, its pages or its count is NULL");
+        if (cache->n_seqs > 0 && !in->want) return bad(err, "want is NULL");
+        if (!aligned(pool->free, 4) || !aligned(pool->count, 4) || !aligned(in->want, 4) || !aligned(in->held, 4) ||
+            !aligned(in->columns, 4) || !aligned(in->start, 4) || !aligned(in->positions, 4) || !aligned(in->slots, 8))
+            return fail(err, MSAO_ERR_ALIGNMENT, "an array is not naturally aligned");
+        MSAO_TRY(check_workspace(workspace, workspace_bytes, pl.total, err));
+        if (!ctx) return bad(err, "ctx is NULL");
+        if (cache->n_seqs == 0 && !in->start) return MSAO_OK;
+        a.free = pool->free;
+        a.count = pool->count;
+        uint8_t* ws = (uint8_t*)workspace;
+        if (!resize_in_one(a)) {
+            a.plan = (ResizePlan*)(ws + pl.plan);
+            a.moved = (int32_t*)(ws + pl.moved);
+            a.taken = (int32_t*)(ws + pl.taken);
+        }
+        DeviceGuard guard(ctx->device);
+        MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_RESIZE, stream, run_resize, &a));
+        return round_launch(ctx, MSAO_ROUND_KERNEL_RESIZE_FILL, stream, run_resize_fill, &a);
     });
 }
 
