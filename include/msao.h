@@ -605,6 +605,37 @@ msao_status msao_cache_attention(msao_ctx* ctx, const msao_kv_cache* cache, cons
 msao_status msao_cache_attention_workspace(const msao_kv_cache* cache, const msao_chunk* chunk, int heads,
                                            uint32_t flags, size_t* bytes);
 
+/* Which sequences share their first tokens (a system prompt, an image, a document that many requests
+ * ask about). Group g is the sequences group[g] .. group[g+1]-1 (device [n_groups + 1], ascending), whose first
+ * tokens[g] (device [n_groups]) tokens are the same: their tables name pages that hold the same keys and
+ * values for them, as a rule the same pages. The first sequence's are read for all. A sequence may be in no group.
+ * max_seqs, max_tokens: the host's bounds on a group's sequences and tokens; a group of more tokens, and what
+ * is past max_seqs * max_new rows of a group, is computed as if nothing were shared. max_own: about how many tokens a
+ * sequence has beside its group's (0: the capacity less max_tokens); one that has more takes longer. */
+typedef struct {
+    const int32_t* group;
+    const int32_t* tokens;
+    int32_t n_groups;
+    int32_t max_seqs;
+    int32_t max_tokens;
+    int32_t max_own;
+} msao_prefix;
+
+/* msao_cache_attention of sequences of which groups share a prefix: the same results, up to the order
+ * of sums, with a prefix' keys and values read once for the rows of all its sequences together (128 at a time;
+ * float32 64) instead of once for each sequence. Rows have to see the whole prefix, so where tokens[g] is
+ * more than a sequence had before the step (its length, without MSAO_ATTEND_CAUSAL) that
+ * sequence is computed as if nothing were shared. Up to 15 tokens past a multiple of 16 of a prefix are
+ * read by each sequence as its own. Arguments, limits and errors as for msao_cache_attention; a NULL or
+ * misaligned array and a negative count of the prefix are refused. MSAO_ATTEND_WEIGHT reads the
+ * keys once more for each sequence. Workspace from msao_cache_attention_shared_workspace. */
+msao_status msao_cache_attention_shared(msao_ctx* ctx, const msao_kv_cache* cache, const msao_prefix* prefix,
+                                        const msao_chunk* chunk, const void* q, int64_t q_stride, int heads, float scale,
+                                        uint32_t flags, void* out, int64_t out_stride, float* lse, void* workspace,
+                                        size_t workspace_bytes, void* stream);
+msao_status msao_cache_attention_shared_workspace(const msao_kv_cache* cache, const msao_prefix* prefix,
+                                                  const msao_chunk* chunk, int heads, uint32_t flags, size_t* bytes);
+
 /* Eviction by the accumulated weight: of each sequence s the k = min(length[s],
  * max(budget[s], 0), capacity of `to`) tokens that stay are, for each kv head on
  * its own, the first min(n_first, k), the last min(n_recent, the rest of k), and

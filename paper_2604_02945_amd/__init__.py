@@ -18,5 +18,6 @@ from .binding import (  # noqa: F401
     msao_mas_score_learned, msao_temporal_simhash, msao_run_simhash, FLAG_SELECT_PER_FRAME,
     msao_run_noalloc, msao_stream_read, msao_run_learned,
     KvCache, cache_attention_workspace, msao_cache_append, msao_cache_attention, msao_cache_evict,
+    SharedPrefix, cache_attention_shared_workspace, msao_cache_attention_shared,
     PagePool, cache_resize_workspace, msao_cache_resize, msao_sample, msao_verify, sample_workspace, verify_workspace,
 )

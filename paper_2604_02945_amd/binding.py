@@ -125,6 +125,11 @@ class MsaoAppend(ctypes.Structure):
                 ("n_axes", ctypes.c_int32), ("sections", ctypes.c_int32 * MAX_AXES), ("flags", ctypes.c_uint32)]
 
 
+class MsaoPrefix(ctypes.Structure):
+    _fields_ = [("group", _P), ("tokens", _P), ("n_groups", ctypes.c_int32), ("max_seqs", ctypes.c_int32),
+                ("max_tokens", ctypes.c_int32), ("max_own", ctypes.c_int32)]
+
+
 class MsaoPagePool(ctypes.Structure):
     _fields_ = [("free", _P), ("count", _P)]
 
@@ -203,6 +208,9 @@ SIGNATURES = [
                                         ctypes.c_size_t, _P]),
     ("msao_cache_evict_workspace", ctypes.c_int, [_P, _P]),
     ("msao_cache_kernel_times", ctypes.c_int, [_P, _P]),
+    ("msao_cache_attention_shared", ctypes.c_int, [_P, _P, _P, _P, _P, ctypes.c_int64, ctypes.c_int, ctypes.c_float,
+                                                   ctypes.c_uint32, _P, ctypes.c_int64, _P, _P, ctypes.c_size_t, _P]),
+    ("msao_cache_attention_shared_workspace", ctypes.c_int, [_P, _P, _P, ctypes.c_int, ctypes.c_uint32, _P]),
     ("msao_cache_resize", ctypes.c_int, [_P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
     ("msao_cache_resize_workspace", ctypes.c_int, [_P, _P, _P]),
     ("msao_sample", ctypes.c_int, [_P, _P, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int, _P, _P, _P, _P,
@@ -983,19 +991,9 @@ def cache_attention_workspace(cache: KvCache, start: torch.Tensor, n_rows: int, 
     return n.value
 
 
-def msao_cache_attention(cache: KvCache, start: torch.Tensor, max_new: int, q: torch.Tensor,
-                         scale: Optional[float] = None, causal: bool = True, out: Optional[torch.Tensor] = None,
-                         lse: Optional[torch.Tensor] = None, accumulate: bool = False,
-                         workspace: Optional[torch.Tensor] = None, ctx: Optional[Context] = None,
-                         stream=None) -> torch.Tensor:
-    """Attention of q [rows, heads, head_dim] (rows of sequences as for
-    msao_cache_append) over the cache; scale 1/sqrt(head_dim) when None. lse
-    float32 [rows, heads] is filled if given; accumulate adds to cache.weight what
-    each token receives. workspace: uint8, 256-byte aligned, of
-    cache_attention_workspace bytes (allocated when None). Returns out, which must
-    share no memory with q; rows of no sequence, and those from max_new on of a longer
-    one, keep what `out` held (0 in one allocated here)."""
-    ctx = _cache_ctx(cache, ctx, stream)
+def _attention_args(cache: KvCache, start: torch.Tensor, max_new: int, q: torch.Tensor, causal: bool, out, lse, accumulate: bool,
+                    workspace, stream):
+    """Checked: out, the chunk, flags, and the strides of q and out."""
     q_stride = _head_rows("q", q, cache.dtype, None, cache.head_dim)
     rows, heads = q.shape[0], q.shape[1]
     if out is None:
@@ -1009,6 +1007,24 @@ def msao_cache_attention(cache: KvCache, start: torch.Tensor, max_new: int, q: t
     _same_device(cache.index, "q, out, lse and workspace", q, out, lse, workspace)
     ch = _chunk(cache, start, rows, max_new)
     flags = (ATTEND_CAUSAL if causal else 0) | (ATTEND_WEIGHT if accumulate else 0)
+    return out, ch, flags, q_stride, out_stride
+
+
+def msao_cache_attention(cache: KvCache, start: torch.Tensor, max_new: int, q: torch.Tensor,
+                         scale: Optional[float] = None, causal: bool = True, out: Optional[torch.Tensor] = None,
+                         lse: Optional[torch.Tensor] = None, accumulate: bool = False,
+                         workspace: Optional[torch.Tensor] = None, ctx: Optional[Context] = None,
+                         stream=None) -> torch.Tensor:
+    """Attention of q [rows, heads, head_dim] (rows of sequences as for
+    msao_cache_append) over the cache; scale 1/sqrt(head_dim) when None. lse
+    float32 [rows, heads] is filled if given; accumulate adds to cache.weight what
+    each token receives. workspace: uint8, 256-byte aligned, of
+    cache_attention_workspace bytes (allocated when None). Returns out, which must
+    share no memory with q; rows of no sequence, and those from max_new on of a longer
+    one, keep what `out` held (0 in one allocated here)."""
+    ctx = _cache_ctx(cache, ctx, stream)
+    out, ch, flags, q_stride, out_stride = _attention_args(cache, start, max_new, q, causal, out, lse, accumulate, workspace, stream)
+    heads = q.shape[1]
     if workspace is None:
         need = ctypes.c_size_t()
         _check(lib().msao_cache_attention_workspace(cache.addr, ctypes.byref(ch), heads, flags, ctypes.byref(need)))
@@ -1017,6 +1033,61 @@ def msao_cache_attention(cache: KvCache, start: torch.Tensor, max_new: int, q: t
                                       cache.head_dim ** -0.5 if scale is None else scale, flags, out.data_ptr(),
                                       out_stride, None if lse is None else lse.data_ptr(), workspace.data_ptr(),
                                       _bytes_of(workspace), _stream_of(cache, stream)), ctx)
+    return out
+
+
+class SharedPrefix:
+    """Which sequences share their first tokens (msao_prefix): sequences group[g] .. group[g+1]-1 (int32
+    [n_groups + 1], ascending) have the same first tokens[g] (int32 [n_groups]) tokens. max_seqs and
+    max_tokens bound a group's sequences and tokens; max_own is about how many tokens a sequence has beside its
+    group's (None: the capacity less max_tokens). The tensors are read when the kernels run."""
+
+    def __init__(self, group: torch.Tensor, tokens: torch.Tensor, max_seqs: int, max_tokens: int, max_own: Optional[int] = None):
+        _int32("group", group, 1)
+        _int32("tokens", tokens, 1)
+        n = int(tokens.shape[0])
+        if group.shape[0] != n + 1:
+            raise ValueError("group must have an entry more than tokens")
+        self.index = group.get_device()
+        _same_device(self.index, "tokens", tokens)
+        self.group, self.tokens = group, tokens
+        self.struct = MsaoPrefix(group.data_ptr(), tokens.data_ptr() if n else None, n, _fits("max_seqs", max_seqs),
+                                 _fits("max_tokens", max_tokens), _fits("max_own", max_own or 0))
+        self.addr = _addr(self.struct)
+
+
+def cache_attention_shared_workspace(cache: KvCache, prefix: SharedPrefix, start: torch.Tensor, n_rows: int, max_new: int,
+                                     heads: int, causal: bool = True, accumulate: bool = False) -> int:
+    """Bytes of workspace that msao_cache_attention_shared needs for such a call."""
+    ch, n = _chunk(cache, start, n_rows, max_new), ctypes.c_size_t()
+    flags = (ATTEND_CAUSAL if causal else 0) | (ATTEND_WEIGHT if accumulate else 0)
+    _check(lib().msao_cache_attention_shared_workspace(cache.addr, prefix.addr, _addr(ch), _fits("heads", heads), flags,
+                                                       ctypes.byref(n)))
+    return n.value
+
+
+def msao_cache_attention_shared(cache: KvCache, prefix: SharedPrefix, start: torch.Tensor, max_new: int, q: torch.Tensor,
+                                scale: Optional[float] = None, causal: bool = True, out: Optional[torch.Tensor] = None,
+                                lse: Optional[torch.Tensor] = None, accumulate: bool = False,
+                                workspace: Optional[torch.Tensor] = None, ctx: Optional[Context] = None,
+                                stream=None) -> torch.Tensor:
+    """msao_cache_attention of sequences of which groups share a prefix: its keys and values are read once for the
+    rows of all its sequences. Arguments and results as there; workspace of
+    cache_attention_shared_workspace bytes."""
+    ctx = _cache_ctx(cache, ctx, stream)
+    if prefix.index != cache.index:
+        raise ValueError("the prefix must be on the cache's device")
+    out, ch, flags, q_stride, out_stride = _attention_args(cache, start, max_new, q, causal, out, lse, accumulate, workspace, stream)
+    heads = q.shape[1]
+    if workspace is None:
+        need = ctypes.c_size_t()
+        _check(lib().msao_cache_attention_shared_workspace(cache.addr, prefix.addr, ctypes.byref(ch), heads, flags,
+                                                           ctypes.byref(need)))
+        workspace = _scratch(cache, need.value, stream)
+    _check(lib().msao_cache_attention_shared(ctx.handle, cache.addr, prefix.addr, ctypes.byref(ch), q.data_ptr(), q_stride, heads,
+                                             cache.head_dim ** -0.5 if scale is None else scale, flags, out.data_ptr(),
+                                             out_stride, None if lse is None else lse.data_ptr(), workspace.data_ptr(),
+                                             _bytes_of(workspace), _stream_of(cache, stream)), ctx)
     return out
 
 

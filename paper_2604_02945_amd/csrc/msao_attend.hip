@@ -165,6 +165,76 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a, int sh)
     return p;
 }
 
+// What a launch attends to: every token of a sequence; the tokens that a group of sequences shares,
+// for the rows of all of them; a sequence's tokens behind those.
+enum : int { kAll = 0, kShared = 1, kOwn = 2 };
+
+// The group that sequence s would be in: the last one that begins at it or before it.
+__device__ __forceinline__ int group_at(const PrefixDev& pre, int s)
+{
+    const int lane = threadIdx.x & (kWave - 1);
+    int n = 0;
+    for (int g = 0; g < pre.n_groups; g += kWave) n += __popcll(__ballot(g + lane < pre.n_groups && pre.group[min(g + lane, pre.n_groups)] <= s));
+    return uniform(n) - 1;
+}
+
+template <int MODE>
+__device__ __forceinline__ Place place_in(const AttendArgs& a, int sh, int& from)
+{
+    from = 0;
+    if constexpr (MODE == kShared) {
+        const int g = sh / a.c.kv_heads;
+        const GroupRows r = group_rows(a.pre, a.ch, g);
+        Place p;
+        p.seq = r.first;
+        p.head = sh - g * a.c.kv_heads;
+        p.begin = r.begin;
+        p.n_new = r.first < a.pre.n_seqs ? r.n : 0;
+        p.length = group_tokens(a.pre, capacity(a.c), g);
+        return p;
+    } else {
+        const Place p = place_of(a, sh);
+        if constexpr (MODE == kOwn)
+            from = prefix_of(a.pre, a.ch, capacity(a.c), p.seq, group_at(a.pre, p.seq), Rows{p.begin, p.n_new}, p.length, a.causal);
+        return p;
+    }
+}
+
+// Part `split` of the `seen` tokens from `from` on: how many parts there are, whether one is all there is to a
+// row, the part's tokens, its place in the workspace.
+struct Part {
+    bool there, alone;
+    int lo, hi, at;
+};
+template <int MODE>
+__device__ __forceinline__ Part part_of(const AttendArgs& a, int seen, int from, int split)
+{
+    Part t;
+    if constexpr (MODE == kAll) {
+        const int parts = parts_of(seen, a.part_tokens);
+        t.there = split < max(parts, 1);
+        t.alone = parts <= 1;
+        t.lo = split * a.part_tokens;
+        t.hi = min(seen, t.lo + a.part_tokens);
+        t.at = split;
+    } else if constexpr (MODE == kShared) {
+        t.there = split < parts_of(seen, a.part_tokens);
+        t.alone = false;
+        t.lo = split * a.part_tokens;
+        t.hi = min(seen, t.lo + a.part_tokens);
+        t.at = split;
+    } else {
+        // (the last part has what is more than the caller thought)
+        const int parts = min(parts_of(seen - from, a.part_tokens), a.splits);
+        t.there = split < max(parts, 1);
+        t.alone = parts <= 1 && from == 0;
+        t.lo = from + split * a.part_tokens;
+        t.hi = split >= parts - 1 ? seen : t.lo + a.part_tokens;
+        t.at = a.part_base + split;
+    }
+    return t;
+}
+
 // Rows of the sequence that the call computes (max_new bounds the grid).
 __device__ __forceinline__ int call_rows(const AttendArgs& a, const Place& p) { return min(p.n_new, a.ch.max_new) * a.group.n; }
 
@@ -266,7 +336,7 @@ struct KeyOffsets {
     }
 };
 
-template <int DT, int DP, int MT, int RW>
+template <int DT, int DP, int MT, int RW, int MODE>
 __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArgs a)
 {
     constexpr int ES = Type<DT>::kSize;
@@ -294,14 +364,15 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArg
     const int per_pair = a.row_tiles * a.splits, sh = blockIdx.x / per_pair;
     const int j = (blockIdx.x - sh * per_pair + sh) % per_pair;
     const int split = j / a.row_tiles, tile = a.row_tiles - 1 - (j - split * a.row_tiles);
-    const Place p = place_of(a, sh);
+    int from;
+    const Place p = place_in<MODE>(a, sh, from);
     const int n_rows = call_rows(a, p), r0 = tile * RW * MT * 16;
     if (r0 >= n_rows) return;
     const int r_end = min(r0 + RW * MT * 16, n_rows);
     const int seen = group_sees(p.length, p.n_new, a.group, r_end - 1, a.causal);
-    const int parts = parts_of(seen, a.part_tokens);
-    if (split >= max(parts, 1)) return;
-    const int lo = split * a.part_tokens, hi = min(seen, lo + a.part_tokens);
+    const Part part = part_of<MODE>(a, seen, from, split);
+    if (!part.there) return;
+    const int lo = part.lo, hi = part.hi;
 
     const int row_bytes = a.c.dim * ES, mask = (1 << a.c.page_shift) - 1;
     const uint8_t* kb = a.c.k + (int64_t)p.head * a.c.k_head;
@@ -565,7 +636,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArg
             }
             const int tok = a.group.of(row), head = p.head * a.group.n + (row - tok * a.group.n);
             const int64_t at = (int64_t)(p.begin + tok) * a.heads + head;
-            if (parts <= 1) {
+            if (part.alone) {
                 const float inv = 1.0f / l;
                 uint8_t* dst = a.out + (int64_t)(p.begin + tok) * a.out_stride + ((int64_t)head * a.c.dim + od) * ES;
                 // (the head's last channels may be part of what the thread has)
@@ -583,11 +654,11 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArg
                 }
             } else {
                 const int64_t all = (int64_t)a.ch.n_rows * a.heads;
-                float* po = a.part_o + (split * all + at) * a.c.dim + od;
+                float* po = a.part_o + (part.at * all + at) * a.c.dim + od;
 #pragma unroll
                 for (int t = 0; t < E; t += S)
                     if (od + t < a.c.dim) store_values<kF32, S>((uint8_t*)(po + t), &acc[t]);
-                if (od == 0) *(f32x2*)(a.part_ml + 2 * (split * all + at)) = f32x2{mm, l};
+                if (od == 0) *(f32x2*)(a.part_ml + 2 * (part.at * all + at)) = f32x2{mm, l};
             }
         }
     }
@@ -632,7 +703,7 @@ __device__ __forceinline__ void load_to_lds(const u32x4& buffer, uint32_t to, in
 __device__ __forceinline__ void stage_came() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 constexpr int kRowLevel = 32;
-template <int DP, int MT, int NW, int ST, int WPS>
+template <int DP, int MT, int NW, int ST, int WPS, int MODE>
 __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
 {
     constexpr int KS = DP / 32, VT = DP / 16;        // steps of a score; tiles of channels
@@ -654,14 +725,15 @@ __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
     const int width = min(kRowLevel, per_pair - level * kRowLevel), sh = in_level / width;
     const int j = level * kRowLevel + (in_level - sh * width + sh) % width;
     const int split = j / a.row_tiles, tile = a.row_tiles - 1 - (j - split * a.row_tiles);
-    const Place p = place_of(a, sh);
+    int from;
+    const Place p = place_in<MODE>(a, sh, from);
     const int n_rows = call_rows(a, p), r0 = tile * NW * MT * 16;
     if (r0 >= n_rows) return;
     const int r_end = min(r0 + NW * MT * 16, n_rows);
     const int seen = group_sees(p.length, p.n_new, a.group, r_end - 1, a.causal);
-    const int parts = parts_of(seen, a.part_tokens);
-    if (split >= max(parts, 1)) return;
-    const int lo = split * a.part_tokens, hi = min(seen, lo + a.part_tokens);
+    const Part part = part_of<MODE>(a, seen, from, split);
+    if (!part.there) return;
+    const int lo = part.lo, hi = part.hi;
 
     const int row_bytes = a.c.dim * 2, mask = (1 << a.c.page_shift) - 1;
     const uint8_t* kb = a.c.k + (int64_t)p.head * a.c.k_head;
@@ -885,7 +957,7 @@ __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
         if (row >= n_rows) continue;
         const int tok = a.group.of(row), head = p.head * a.group.n + (row - tok * a.group.n);
         const int64_t at = (int64_t)(p.begin + tok) * a.heads + head;
-        if (parts <= 1) {
+        if (part.alone) {
             const float inv = 1.0f / sum[m];
             auto of = [&](int t, int r) { return normed(o[m][t][r], inv, sum[m]); };
             uint8_t* dst = a.out + (int64_t)(p.begin + tok) * a.out_stride + (int64_t)head * row_bytes;
@@ -902,30 +974,36 @@ __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
             }
         } else {
             const int64_t all = (int64_t)a.ch.n_rows * a.heads;
-            float* po = a.part_o + (split * all + at) * a.c.dim;
+            float* po = a.part_o + (part.at * all + at) * a.c.dim;
 #pragma unroll
             for (int t = 0; t < VT; ++t)
                 if (16 * t + 4 * c < a.c.dim) *(f32x4*)(po + 16 * t + 4 * c) = o[m][t];
-            if (c == 0) *(f32x2*)(a.part_ml + 2 * (split * all + at)) = f32x2{ref[m], sum[m]};
+            if (c == 0) *(f32x2*)(a.part_ml + 2 * (part.at * all + at)) = f32x2{ref[m], sum[m]};
         }
     }
 }
 
 // Parts of split rows joined: W wavefronts a row. DP / 4 lanes hold four channels each of a
 // part; the lanes' groups take parts in turn, four in flight, and join at the end.
-template <int DT, int DP, int W>
+template <int DT, int DP, int W, int MODE>
 __global__ __launch_bounds__(kBlock) void k_combine(AttendArgs a, int blocks_per)
 {
     constexpr int ES = Type<DT>::kSize;
     constexpr int LP = DP == 96 ? 32 : DP / 4, kGroups = W * kWave / LP, kFly = 4;
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
     const int sh = blockIdx.x / blocks_per;
-    const Place p = place_of(a, sh);
+    int from;
+    const Place p = place_in<MODE>(a, sh, from);
     const int n_rows = call_rows(a, p), row = (blockIdx.x - sh * blocks_per) * (kWaves / W) + wave / W;
     if (row >= n_rows) return;  // (W = kWaves: the whole block)
     const int r_end = min(row / a.tile_rows * a.tile_rows + a.tile_rows, n_rows);
     const int seen = group_sees(p.length, p.n_new, a.group, r_end - 1, a.causal);
-    const int parts = parts_of(seen, a.part_tokens);
+    int shared = 0, parts = parts_of(seen, a.part_tokens);
+    if constexpr (MODE == kOwn) {  // the prefix' parts, then the own ones, of which there is one at least
+        shared = parts_of(from, a.pre.part_tokens);
+        parts = min(parts_of(seen - from, a.part_tokens), a.splits);
+        if (from > 0) parts = shared + max(parts, 1);
+    }
     if (parts <= 1) return;  // written by k_attend
     const int tok = a.group.of(row), head = p.head * a.group.n + (row - tok * a.group.n);
     const int64_t all = (int64_t)a.ch.n_rows * a.heads, at = (int64_t)(p.begin + tok) * a.heads + head;
@@ -950,8 +1028,9 @@ __global__ __launch_bounds__(kBlock) void k_combine(AttendArgs a, int blocks_per
             ml[f] = f32x2{-INFINITY, 0.0f};
             o[f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             if (i < parts) {
-                ml[f] = *(const f32x2*)(a.part_ml + 2 * (i * all + at));
-                if (has) o[f] = *(const f32x4*)(a.part_o + (i * all + at) * a.c.dim + ch);
+                const int64_t j = MODE == kOwn && i >= shared ? a.part_base + i - shared : i;
+                ml[f] = *(const f32x2*)(a.part_ml + 2 * (j * all + at));
+                if (has) o[f] = *(const f32x4*)(a.part_o + (j * all + at) * a.c.dim + ch);
             }
         }
 #pragma unroll
@@ -1264,7 +1343,7 @@ int padded_dim(int dim) { return dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 
 int64_t pairs(const AttendArgs& a) { return (int64_t)a.c.n_seqs * a.c.kv_heads; }
 
 // Of rows with many parts k_combine has the whole block on one row.
-bool block_a_row(const AttendArgs& a) { return a.splits > 16; }
+bool block_a_row(const AttendArgs& a) { return a.part_base + a.splits > 16; }
 
 // bf16 rows go through k_attend_rows from 17 on: stages of 64 tokens serve all four wavefronts,
 // where k_attend reads a tile once for each 32 rows (64 requests of up to 16,000 tokens: with 21
@@ -1283,35 +1362,35 @@ bool block_a_row(const AttendArgs& a) { return a.splits > 16; }
 constexpr int kFewRows = 16;
 constexpr int stage_of(int dp) { return dp == 256 ? 32 : 64; }
 // Rows of a workgroup: what the registers of its wavefronts hold.
-template <int DT, int DP>
+template <int DT, int DP, int MODE>
 int attend_rows(const AttendArgs& a, void* st, void* e0, void* e1)
 {
     const int64_t blocks = pairs(a) * attend_blocks(a).attend;
     if constexpr (DT == kBF16) {
         constexpr int kPerSimd = DP == 64 ? 3 : 2;
-        if (a.tile_rows == 64) return enqueue(k_attend_rows<DP, 1, kWaves, stage_of(DP), kPerSimd>, blocks, st, e0, e1, a);
+        if (a.tile_rows == 64) return enqueue(k_attend_rows<DP, 1, kWaves, stage_of(DP), kPerSimd, MODE>, blocks, st, e0, e1, a);
         if constexpr (DP != 256) {
-            if (a.tile_rows == 128) return enqueue(k_attend_rows<DP, 2, kWaves, stage_of(DP), kPerSimd>, blocks, st, e0, e1, a);
-            if (a.tile_rows == 16) return enqueue(k_attend<DT, DP, 1, 1>, blocks, st, e0, e1, a);
+            if (a.tile_rows == 128) return enqueue(k_attend_rows<DP, 2, kWaves, stage_of(DP), kPerSimd, MODE>, blocks, st, e0, e1, a);
+            if (a.tile_rows == 16) return enqueue(k_attend<DT, DP, 1, 1, MODE>, blocks, st, e0, e1, a);
         }
     } else {
-        if (a.tile_rows == 16) return enqueue(k_attend<DT, DP, 1, 1>, blocks, st, e0, e1, a);
+        if (a.tile_rows == 16) return enqueue(k_attend<DT, DP, 1, 1, MODE>, blocks, st, e0, e1, a);
         if constexpr (DP == 256) {
-            if (a.tile_rows == 32) return enqueue(k_attend<DT, DP, 1, 2>, blocks, st, e0, e1, a);
+            if (a.tile_rows == 32) return enqueue(k_attend<DT, DP, 1, 2, MODE>, blocks, st, e0, e1, a);
         } else {
-            if (a.tile_rows == 32) return enqueue(k_attend<DT, DP, 2, 1>, blocks, st, e0, e1, a);
-            if (a.tile_rows == 64) return enqueue(k_attend<DT, DP, 2, 2>, blocks, st, e0, e1, a);
+            if (a.tile_rows == 32) return enqueue(k_attend<DT, DP, 2, 1, MODE>, blocks, st, e0, e1, a);
+            if (a.tile_rows == 64) return enqueue(k_attend<DT, DP, 2, 2, MODE>, blocks, st, e0, e1, a);
         }
     }
     return (int)hipErrorInvalidValue;
 }
 
-template <int DT, int DP>
+template <int DT, int DP, int MODE>
 int combine_rows(const AttendArgs& a, void* st, void* e0, void* e1)
 {
     const int per = (int)attend_blocks(a).combine;
-    return block_a_row(a) ? enqueue(k_combine<DT, DP, kWaves>, pairs(a) * per, st, e0, e1, a, per)
-                          : enqueue(k_combine<DT, DP, 1>, pairs(a) * per, st, e0, e1, a, per);
+    return block_a_row(a) ? enqueue(k_combine<DT, DP, kWaves, MODE>, pairs(a) * per, st, e0, e1, a, per)
+                          : enqueue(k_combine<DT, DP, 1, MODE>, pairs(a) * per, st, e0, e1, a, per);
 }
 
 template <int DT, int DP>
@@ -1334,10 +1413,19 @@ int by_type(const AttendArgs& a, void* st, void* e0, void* e1)
          : dp == 128 ? F<kF32, 128>::go(a, st, e0, e1) : F<kF32, 256>::go(a, st, e0, e1);
 }
 template <int DT, int DP> struct Attend {
-    static int go(const AttendArgs& a, void* st, void* e0, void* e1) { return attend_rows<DT, DP>(a, st, e0, e1); }
+    static int go(const AttendArgs& a, void* st, void* e0, void* e1) { return attend_rows<DT, DP, kAll>(a, st, e0, e1); }
+};
+template <int DT, int DP> struct AttendShared {
+    static int go(const AttendArgs& a, void* st, void* e0, void* e1) { return attend_rows<DT, DP, kShared>(a, st, e0, e1); }
+};
+template <int DT, int DP> struct AttendOwn {
+    static int go(const AttendArgs& a, void* st, void* e0, void* e1) { return attend_rows<DT, DP, kOwn>(a, st, e0, e1); }
 };
 template <int DT, int DP> struct Combine {
-    static int go(const AttendArgs& a, void* st, void* e0, void* e1) { return combine_rows<DT, DP>(a, st, e0, e1); }
+    static int go(const AttendArgs& a, void* st, void* e0, void* e1) { return combine_rows<DT, DP, kAll>(a, st, e0, e1); }
+};
+template <int DT, int DP> struct CombineShared {
+    static int go(const AttendArgs& a, void* st, void* e0, void* e1) { return combine_rows<DT, DP, kOwn>(a, st, e0, e1); }
 };
 template <int DT, int DP> struct Weight {
     static int go(const AttendArgs& a, void* st, void* e0, void* e1) { return weight_rows<DT, DP>(a, st, e0, e1); }
@@ -1400,11 +1488,32 @@ void attend_shape(AttendArgs& a)
     }
 }
 
+void shared_shape(AttendArgs& a, AttendArgs& pre, int max_own)
+{
+    const int page = 1 << a.c.page_shift;
+    attend_shape(a);
+    AttendArgs own = a;
+    own.c.per_seq = std::min(a.c.per_seq, (max_own + page - 1) / page);
+    attend_shape(own);
+    a.part_tokens = own.part_tokens;
+    a.splits = own.splits;
+    pre = a;
+    pre.c.n_seqs = a.pre.n_groups;
+    pre.c.per_seq = std::min(a.c.per_seq, (a.pre.max_tokens + page - 1) / page);
+    pre.ch.max_new = a.pre.max_rows;
+    pre.causal = pre.add_weight = 0;
+    attend_shape(pre);
+    a.pre.part_tokens = pre.part_tokens;
+    a.pre.splits = pre.splits;
+    a.part_base = pre.splits;
+    pre.pre = a.pre;
+}
+
 AttendBlocks attend_blocks(const AttendArgs& a)
 {
     const int64_t rows = (int64_t)a.ch.max_new * a.group.n;
     AttendBlocks b{(int64_t)a.row_tiles * a.splits, 0, 0, 0};
-    if (a.splits > 1) b.combine = block_a_row(a) ? rows : (rows + kWaves - 1) / kWaves;
+    if (a.part_base + a.splits > 1) b.combine = block_a_row(a) ? rows : (rows + kWaves - 1) / kWaves;
     if (a.add_weight) b.weight = (int64_t)a.weight_parts * a.row_parts;
     if (a.add_weight && a.row_parts > 1) b.join = ((int64_t)capacity(a.c) + 4 * kBlock - 1) / (4 * kBlock);
     return b;
@@ -1414,9 +1523,10 @@ AttendBytes attend_bytes(const AttendArgs& a)
 {
     const size_t rows = (size_t)a.ch.n_rows * (size_t)a.heads;
     AttendBytes b{0, 0, 0, 0};
-    if (a.splits > 1) {
-        b.part_o = rows * (size_t)a.splits * (size_t)a.c.dim * 4;
-        b.part_ml = rows * (size_t)a.splits * 8;
+    const size_t splits = (size_t)a.part_base + (size_t)a.splits;
+    if (splits > 1) {
+        b.part_o = rows * splits * (size_t)a.c.dim * 4;
+        b.part_ml = rows * splits * 8;
     }
     if (a.add_weight) b.lse2 = rows * 4;
     if (a.add_weight && a.row_parts > 1) b.part_w = (size_t)a.row_parts * (size_t)pairs(a) * (size_t)capacity(a.c) * 4;
@@ -1424,6 +1534,10 @@ AttendBytes attend_bytes(const AttendArgs& a)
 }
 
 int launch_attend(const AttendArgs& a, void* st, void* e0, void* e1) { return by_type<Attend>(a, st, e0, e1); }
+
+int launch_shared(const AttendArgs& a, void* st, void* e0, void* e1) { return by_type<AttendShared>(a, st, e0, e1); }
+int launch_own(const AttendArgs& a, void* st, void* e0, void* e1) { return by_type<AttendOwn>(a, st, e0, e1); }
+int launch_shared_join(const AttendArgs& a, void* st, void* e0, void* e1) { return by_type<CombineShared>(a, st, e0, e1); }
 
 int launch_combine(const AttendArgs& a, void* st, void* e0, void* e1)
 {

@@ -143,6 +143,51 @@ struct AppendArgs {
 };
 
 // ---- attention ------------------------------------------------------------------
+// msao_prefix as the kernels take it: group g's sequences are entries group[g] .. group[g + 1] - 1.
+struct PrefixDev {
+    const int32_t* group;
+    const int32_t* tokens;
+    int32_t n_groups, n_seqs;
+    int32_t max_seqs, max_tokens;
+    int32_t max_rows;              // rows (tokens) of a group that its prefix is computed for
+    int32_t part_tokens, splits;   // parts of a prefix, and most of them
+};
+
+// Rows (tokens) of group g's sequences.
+struct GroupRows {
+    int first, end, begin, n;
+};
+MSAO_HD GroupRows group_rows(const PrefixDev& pre, const ChunkDev& ch, int g)
+{
+    GroupRows r;
+    r.first = clamp_int(entry(pre.group, g), 0, pre.n_seqs);
+    r.end = clamp_int(entry(pre.group, g + 1), r.first, pre.n_seqs);
+    r.begin = clamp_int(entry(ch.start, r.first), 0, ch.n_rows);
+    r.n = clamp_int(entry(ch.start, r.end), r.begin, ch.n_rows) - r.begin;
+    return r;
+}
+
+// Tokens of its prefix that are computed once: whole half tiles, which lie in one page each. What
+// is left of them the sequences read as their own.
+MSAO_HD int group_tokens(const PrefixDev& pre, int cap, int g)
+{
+    const int t = entry(pre.tokens, g);
+    return t <= 0 || t > pre.max_tokens || t > cap ? 0 : t & ~15;
+}
+
+// How many tokens sequence s has from group g: 0 where it is none of the group, or where its rows are not all among
+// the ones that the prefix is computed for, or do not all see the whole prefix.
+MSAO_HD int prefix_of(const PrefixDev& pre, const ChunkDev& ch, int cap, int s, int g, const Rows& rows, int length, bool causal)
+{
+    if (g < 0 || g >= pre.n_groups) return 0;
+    const GroupRows gr = group_rows(pre, ch, g);
+    if (s < gr.first || s >= gr.end) return 0;
+    const int n = rows.n < ch.max_new ? rows.n : ch.max_new, most = gr.n < pre.max_rows ? gr.n : pre.max_rows;
+    if (rows.begin < gr.begin || rows.begin + n - gr.begin > most) return 0;
+    const int t = group_tokens(pre, cap, g);
+    return t <= (causal ? length - rows.n : length) ? t : 0;
+}
+
 struct AttendArgs {
     CacheDev c;
     ChunkDev ch;
@@ -160,6 +205,8 @@ struct AttendArgs {
     int32_t weight_tokens;         // tokens of a part in the weight pass
     int32_t weight_parts;          // most of them for each (sequence, kv head)
     int32_t row_parts;             // and of the rows
+    PrefixDev pre;                 // of a call with shared prefixes
+    int32_t part_base;             // first of the parts that hold a sequence's own tokens
     // workspace
     float* part_o;                 // [splits][n_rows * heads][dim], a part's sum of 2^(x - m) v
     float* part_ml;                // [splits][n_rows * heads][2], its m and sum of 2^(x - m)
@@ -247,6 +294,10 @@ int launch_resize_fill(const ResizeArgs& a, void* stream, void* ev0, void* ev1);
 int launch_append(const AppendArgs& a, void* stream, void* ev0, void* ev1);
 int launch_attend(const AttendArgs& a, void* stream, void* ev0, void* ev1);
 int launch_combine(const AttendArgs& a, void* stream, void* ev0, void* ev1);
+// A call with shared prefixes: `a` over the prefixes (shared_shape makes it), over the rest, joined.
+int launch_shared(const AttendArgs& a, void* stream, void* ev0, void* ev1);
+int launch_own(const AttendArgs& a, void* stream, void* ev0, void* ev1);
+int launch_shared_join(const AttendArgs& a, void* stream, void* ev0, void* ev1);
 int launch_weight(const AttendArgs& a, void* stream, void* ev0, void* ev1);
 int launch_weight_join(const AttendArgs& a, void* stream, void* ev0, void* ev1);
 int launch_select(const EvictArgs& a, void* stream, void* ev0, void* ev1);
@@ -257,6 +308,9 @@ void append_shape(AppendArgs& a);
 void evict_shape(EvictArgs& a);
 // Launch shape of an attention call: fills part_tokens .. row_parts.
 void attend_shape(AttendArgs& a);
+// Of one with shared prefixes: `pre` becomes the call over the prefixes and `a` the one over the rest, of which
+// sequences mostly have max_own tokens.
+void shared_shape(AttendArgs& a, AttendArgs& pre, int max_own);
 // Workgroups that its kernels launch for each (sequence, kv head); 0: no such launch.
 struct AttendBlocks {
     int64_t attend, combine, weight, join;

@@ -179,20 +179,18 @@ CacheDev cache_dev(const msao_kv_cache& c)
 
 ChunkDev chunk_dev(const msao_chunk& ch) { return ChunkDev{ch.start, ch.n_rows, std::min(ch.max_new, ch.n_rows)}; }
 
-// The launch shape and the workspace of an attention call.
+// The launch shape and the workspace of an attention call; `pre` of one with shared prefixes.
 struct AttendPlan {
-    AttendArgs a;
+    AttendArgs a, pre;
     size_t part_o, part_ml, lse2, part_w, total;
 };
-msao_status attend_plan(const msao_kv_cache* cache, const msao_chunk* chunk, int heads, uint32_t flags, AttendPlan& pl,
-                        std::string* err)
+msao_status attend_args(const msao_kv_cache* cache, const msao_chunk* chunk, int heads, uint32_t flags, AttendArgs& a, std::string* err)
 {
     MSAO_TRY(check_cache(cache, err));
     MSAO_TRY(check_chunk(chunk, *cache, err));
     MSAO_TRY(check_heads(heads, *cache, *chunk, err));
     if (flags & ~(MSAO_ATTEND_CAUSAL | MSAO_ATTEND_WEIGHT)) return bad(err, "unknown flag bits");
     if ((flags & MSAO_ATTEND_WEIGHT) && !cache->weight && has_tokens(*cache)) return bad(err, "the cache has no weight to add to");
-    AttendArgs& a = pl.a;
     std::memset(&a, 0, sizeof a);
     a.c = cache_dev(*cache);
     a.ch = chunk_dev(*chunk);
@@ -201,19 +199,62 @@ msao_status attend_plan(const msao_kv_cache* cache, const msao_chunk* chunk, int
     a.dtype = cache->dtype;
     a.causal = flags & MSAO_ATTEND_CAUSAL ? 1 : 0;
     a.add_weight = flags & MSAO_ATTEND_WEIGHT ? 1 : 0;
-    const int64_t groups = (int64_t)a.c.n_seqs * a.c.kv_heads;
     // (before the shape, whose products of counts would pass 63 bits)
-    if (groups > kMaxBlocks) return fail(err, MSAO_ERR_UNSUPPORTED, "more workgroups than one launch takes");
-    attend_shape(a);
-    const AttendBlocks n = attend_blocks(a);
-    const int64_t most = std::max(std::max(n.attend, n.combine), std::max(n.weight, n.join));
+    if ((int64_t)a.c.n_seqs * a.c.kv_heads > kMaxBlocks) return fail(err, MSAO_ERR_UNSUPPORTED, "more workgroups than one launch takes");
+    return MSAO_OK;
+}
+msao_status check_blocks(int64_t groups, int64_t most, std::string* err)
+{
     if (groups > 0 && most > kMaxBlocks / groups) return fail(err, MSAO_ERR_UNSUPPORTED, "more workgroups than one launch takes");
-    const AttendBytes b = attend_bytes(a);
+    return MSAO_OK;
+}
+void attend_workspace(AttendPlan& pl)
+{
+    const AttendBytes b = attend_bytes(pl.a);
     pl.part_o = 0;
     pl.part_ml = align_up(b.part_o, kWsAlign);
     pl.lse2 = pl.part_ml + align_up(b.part_ml, kWsAlign);
     pl.part_w = pl.lse2 + align_up(b.lse2, kWsAlign);
     pl.total = pl.part_w + align_up(b.part_w, kWsAlign);
+}
+msao_status attend_plan(const msao_kv_cache* cache, const msao_chunk* chunk, int heads, uint32_t flags, AttendPlan& pl,
+                        std::string* err)
+{
+    MSAO_TRY(attend_args(cache, chunk, heads, flags, pl.a, err));
+    attend_shape(pl.a);
+    const AttendBlocks n = attend_blocks(pl.a);
+    MSAO_TRY(check_blocks((int64_t)pl.a.c.n_seqs * pl.a.c.kv_heads, std::max(std::max(n.attend, n.combine), std::max(n.weight, n.join)), err));
+    attend_workspace(pl);
+    return MSAO_OK;
+}
+
+// With shared prefixes.
+msao_status shared_plan(const msao_kv_cache* cache, const msao_prefix* prefix, const msao_chunk* chunk, int heads, uint32_t flags,
+                        AttendPlan& pl, std::string* err)
+{
+    AttendArgs& a = pl.a;
+    MSAO_TRY(attend_args(cache, chunk, heads, flags, a, err));
+    if (!prefix) return bad(err, "prefix is NULL");
+    if (prefix->n_groups < 0 || prefix->max_seqs < 0 || prefix->max_tokens < 0 || prefix->max_own < 0)
+        return bad(err, "a count of the prefix is negative");
+    if (prefix->n_groups > 0 && (!prefix->group || !prefix->tokens)) return bad(err, "group or tokens is NULL");
+    if (!aligned(prefix->group, 4) || !aligned(prefix->tokens, 4))
+        return fail(err, MSAO_ERR_ALIGNMENT, "group or tokens is not 4-byte aligned");
+    const int64_t cap = (int64_t)cache->pages_per_seq * cache->page_size, groups = (int64_t)prefix->n_groups * a.c.kv_heads;
+    if (groups > kMaxBlocks) return fail(err, MSAO_ERR_UNSUPPORTED, "more workgroups than one launch takes");
+    a.pre.group = prefix->group;
+    a.pre.tokens = prefix->tokens;
+    a.pre.n_groups = prefix->n_groups;
+    a.pre.n_seqs = a.c.n_seqs;
+    a.pre.max_seqs = prefix->max_seqs;
+    a.pre.max_tokens = (int32_t)std::min<int64_t>(prefix->max_tokens, cap);
+    a.pre.max_rows = (int32_t)std::min<int64_t>(a.ch.n_rows, (int64_t)std::min(prefix->max_seqs, a.c.n_seqs) * a.ch.max_new);
+    const int64_t own = prefix->max_own > 0 ? prefix->max_own : cap - a.pre.max_tokens;
+    shared_shape(a, pl.pre, (int)std::min<int64_t>(std::max<int64_t>(own, 1), std::max<int64_t>(cap, 1)));
+    const AttendBlocks n = attend_blocks(a), m = attend_blocks(pl.pre);
+    MSAO_TRY(check_blocks((int64_t)a.c.n_seqs * a.c.kv_heads, std::max(std::max(n.attend, n.combine), std::max(n.weight, n.join)), err));
+    MSAO_TRY(check_blocks(groups, m.attend, err));
+    attend_workspace(pl);
     return MSAO_OK;
 }
 
@@ -227,8 +268,47 @@ msao_status check_workspace(void* ws, size_t given, size_t needed, std::string* 
     return MSAO_OK;
 }
 
+// The rest of an attention call's checks, and its pointers.
+msao_status attend_call(msao_ctx* ctx, const msao_kv_cache& cache, const msao_chunk& chunk, const void* q, int64_t q_stride, float scale,
+                        void* out, int64_t out_stride, float* lse, void* workspace, size_t workspace_bytes, AttendPlan& pl, std::string* err)
+{
+    AttendArgs& a = pl.a;
+    const int64_t es = elt_size(cache.dtype), values = (int64_t)a.heads * cache.head_dim;
+    // (in base 2, as the kernels take it, too)
+    const float scale2 = (float)((double)scale * 1.44269504088896340736);
+    if (!std::isfinite(scale2)) return bad(err, "scale is not finite");
+    if (chunk.n_rows > 0) {
+        MSAO_TRY(check_rows(q, q_stride, values, es, "q", err));
+        if (q_stride * es >= kMaxRowBytes) return fail(err, MSAO_ERR_UNSUPPORTED, "a stride of q of 32 MiB or more");
+        MSAO_TRY(check_rows(out, out_stride, values, es, "out", err));
+    }
+    if (!aligned(lse, 4)) return fail(err, MSAO_ERR_ALIGNMENT, "lse is not 4-byte aligned");
+    MSAO_TRY(check_workspace(workspace, workspace_bytes, pl.total, err));
+    if (!ctx) return bad(err, "ctx is NULL");
+    if (rows_meet(q, q_stride * es, out, out_stride * es, values * es, chunk.n_rows)) return bad(err, "out overlaps q");
+    a.q = (const uint8_t*)q;
+    a.out = (uint8_t*)out;
+    a.q_stride = q_stride * es;
+    a.out_stride = out_stride * es;
+    a.lse = lse;
+    a.scale = scale2;
+    uint8_t* ws = (uint8_t*)workspace;
+    if (a.part_base + a.splits > 1) {
+        a.part_o = (float*)(ws + pl.part_o);
+        a.part_ml = (float*)(ws + pl.part_ml);
+    }
+    if (a.add_weight) {
+        a.lse2 = (float*)(ws + pl.lse2);
+        a.part_w = (float*)(ws + pl.part_w);
+    }
+    return MSAO_OK;
+}
+
 int run_append(const void* a, void* s, void* e0, void* e1) { return launch_append(*(const AppendArgs*)a, s, e0, e1); }
 int run_attend(const void* a, void* s, void* e0, void* e1) { return launch_attend(*(const AttendArgs*)a, s, e0, e1); }
+int run_shared(const void* a, void* s, void* e0, void* e1) { return launch_shared(*(const AttendArgs*)a, s, e0, e1); }
+int run_own(const void* a, void* s, void* e0, void* e1) { return launch_own(*(const AttendArgs*)a, s, e0, e1); }
+int run_shared_join(const void* a, void* s, void* e0, void* e1) { return launch_shared_join(*(const AttendArgs*)a, s, e0, e1); }
 int run_combine(const void* a, void* s, void* e0, void* e1) { return launch_combine(*(const AttendArgs*)a, s, e0, e1); }
 int run_weight(const void* a, void* s, void* e0, void* e1) { return launch_weight(*(const AttendArgs*)a, s, e0, e1); }
 int run_weight_join(const void* a, void* s, void* e0, void* e1) { return launch_weight_join(*(const AttendArgs*)a, s, e0, e1); }
@@ -362,39 +442,53 @@ msao_status msao_cache_attention(msao_ctx* ctx, const msao_kv_cache* cache, cons
         std::string* err = ctx ? &ctx->err : &g_err;
         AttendPlan pl;
         MSAO_TRY(attend_plan(cache, chunk, heads, flags, pl, err));
-        AttendArgs& a = pl.a;
-        const int64_t es = elt_size(cache->dtype), values = (int64_t)heads * cache->head_dim;
-        // (in base 2, as the kernels take it, too)
-        const float scale2 = (float)((double)scale * 1.44269504088896340736);
-        if (!std::isfinite(scale2)) return bad(err, "scale is not finite");
-        if (chunk->n_rows > 0) {
-            MSAO_TRY(check_rows(q, q_stride, values, es, "q", err));
-            if (q_stride * es >= kMaxRowBytes) return fail(err, MSAO_ERR_UNSUPPORTED, "a stride of q of 32 MiB or more");
-            MSAO_TRY(check_rows(out, out_stride, values, es, "out", err));
-        }
-        if (!aligned(lse, 4)) return fail(err, MSAO_ERR_ALIGNMENT, "lse is not 4-byte aligned");
-        MSAO_TRY(check_workspace(workspace, workspace_bytes, pl.total, err));
-        if (!ctx) return bad(err, "ctx is NULL");
-        if (rows_meet(q, q_stride * es, out, out_stride * es, values * es, chunk->n_rows)) return bad(err, "out overlaps q");
+        MSAO_TRY(attend_call(ctx, *cache, *chunk, q, q_stride, scale, out, out_stride, lse, workspace, workspace_bytes, pl, err));
         if (chunk->max_new == 0 || cache->n_seqs == 0) return MSAO_OK;
-        a.q = (const uint8_t*)q;
-        a.out = (uint8_t*)out;
-        a.q_stride = q_stride * es;
-        a.out_stride = out_stride * es;
-        a.lse = lse;
-        a.scale = scale2;
-        uint8_t* ws = (uint8_t*)workspace;
-        if (a.splits > 1) {
-            a.part_o = (float*)(ws + pl.part_o);
-            a.part_ml = (float*)(ws + pl.part_ml);
-        }
-        if (a.add_weight) {
-            a.lse2 = (float*)(ws + pl.lse2);
-            a.part_w = (float*)(ws + pl.part_w);
-        }
+        const AttendArgs& a = pl.a;
         DeviceGuard guard(ctx->device);
         MSAO_TRY(cache_launch(ctx, MSAO_CACHE_KERNEL_ATTEND, stream, run_attend, &a));
         MSAO_TRY(cache_launch(ctx, MSAO_CACHE_KERNEL_COMBINE, stream, run_combine, &a));
+        MSAO_TRY(cache_launch(ctx, MSAO_CACHE_KERNEL_WEIGHT, stream, run_weight, &a));
+        return cache_launch(ctx, MSAO_CACHE_KERNEL_WEIGHT_JOIN, stream, run_weight_join, &a);
+    });
+}
+
+msao_status msao_cache_attention_shared_workspace(const msao_kv_cache* cache, const msao_prefix* prefix, const msao_chunk* chunk,
+                                                  int heads, uint32_t flags, size_t* bytes)
+{
+    return guarded([&]() -> msao_status {
+        if (!bytes) return bad(&g_err, "bytes is NULL");
+        AttendPlan pl;
+        MSAO_TRY(shared_plan(cache, prefix, chunk, heads, flags, pl, &g_err));
+        *bytes = pl.total;
+        return MSAO_OK;
+    });
+}
+
+msao_status msao_cache_attention_shared(msao_ctx* ctx, const msao_kv_cache* cache, const msao_prefix* prefix,
+                                        const msao_chunk* chunk, const void* q, int64_t q_stride, int heads, float scale,
+                                        uint32_t flags, void* out, int64_t out_stride, float* lse, void* workspace,
+                                        size_t workspace_bytes, void* stream)
+{
+    return guarded([&]() -> msao_status {
+        std::string* err = ctx ? &ctx->err : &g_err;
+        AttendPlan pl;
+        MSAO_TRY(shared_plan(cache, prefix, chunk, heads, flags, pl, err));
+        MSAO_TRY(attend_call(ctx, *cache, *chunk, q, q_stride, scale, out, out_stride, lse, workspace, workspace_bytes, pl, err));
+        if (chunk->max_new == 0 || cache->n_seqs == 0) return MSAO_OK;
+        AttendArgs pre = pl.a;  // (with what the call has filled in)
+        pre.c = pl.pre.c;
+        pre.ch = pl.pre.ch;
+        pre.causal = pre.add_weight = 0;
+        pre.part_tokens = pl.pre.part_tokens;
+        pre.splits = pl.pre.splits;
+        pre.row_tiles = pl.pre.row_tiles;
+        pre.tile_rows = pl.pre.tile_rows;
+        const AttendArgs& a = pl.a;
+        DeviceGuard guard(ctx->device);
+        if (a.pre.max_rows > 0 && a.pre.max_tokens > 0) MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_SHARED, stream, run_shared, &pre));
+        MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_OWN, stream, run_own, &a));
+        MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_SHARED_JOIN, stream, run_shared_join, &a));
         MSAO_TRY(cache_launch(ctx, MSAO_CACHE_KERNEL_WEIGHT, stream, run_weight, &a));
         return cache_launch(ctx, MSAO_CACHE_KERNEL_WEIGHT_JOIN, stream, run_weight_join, &a);
     });
