@@ -32,35 +32,41 @@ constexpr int kFillThreads = 256;
 struct Sums {
     int64_t take, back, rows;
 };
-__device__ __forceinline__ Sums operator+(const Sums& a, const Sums& b) { return Sums{a.take + b.take, a.back + b.back, a.rows + b.rows}; }
 
-// Sums over the threads before this one (and over all): all threads of the workgroup.
-__device__ __forceinline__ int64_t before(int64_t v, int64_t* room, int64_t& total)
+// N values: the sums over the threads before this one in their place, and over all threads.
+template <int N>
+__device__ __forceinline__ void sum_before(int64_t (&v)[N], int64_t (&total)[N], int64_t (*room)[kWaves])
 {
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
-    int64_t upto = v;
+    auto scan = [&](int64_t x, int width) {
 #pragma unroll
-    for (int s = 1; s < kWave; s <<= 1) {
-        const int64_t o = __shfl_up(upto, s);
-        if (lane >= s) upto += o;
-    }
-    if (lane == kWave - 1) room[wave] = upto;
-    __syncthreads();
-    int64_t b = 0;
-    total = 0;
+        for (int s = 1; s < width; s <<= 1) {
+            const int64_t o = __shfl_up(x, s);
+            if (lane >= s) x += o;
+        }
+        return x;
+    };
+    int64_t upto[N];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        b += w < wave ? room[w] : 0;
-        total += room[w];
+    for (int i = 0; i < N; ++i) {
+        upto[i] = scan(v[i], kWave);
+        if (lane == kWave - 1) room[i][wave] = upto[i];
     }
     __syncthreads();
-    return b + upto - v;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int64_t w = scan(lane < kWaves ? room[i][lane] : 0, kWaves);
+        total[i] = __shfl(w, kWaves - 1);
+        const int64_t b = __shfl(w, max(wave - 1, 0));
+        v[i] = (wave > 0 ? b : 0) + upto[i] - v[i];
+    }
+    __syncthreads();
 }
 
 __device__ __forceinline__ int saturated(int64_t v) { return (int)(v < INT32_MAX ? v : INT32_MAX); }
 
 // Plans of all sequences, their new lengths, columns, starts; what is taken and given back.
-__device__ __forceinline__ Sums plan_all(const ResizeArgs& a, ResizePlan* plan, int64_t* room, int count)
+__device__ __forceinline__ Sums plan_all(const ResizeArgs& a, ResizePlan* plan, int64_t (*room)[kWaves], int count)
 {
     Sums at{0, 0, 0};
     if (a.n_seqs == 0 && a.start && threadIdx.x == 0) a.start[0] = 0;
@@ -77,29 +83,34 @@ __device__ __forceinline__ Sums plan_all(const ResizeArgs& a, ResizePlan* plan, 
             old = a.columns ? clamp_int(a.columns[s], 0, a.per_seq) : columns_of(a, length, held);
             need = columns_of(a, want, held);
         }
-        int64_t t_take, t_back, t_rows, t_taken;
-        const int64_t asks = need > old ? need - old : 0, take = at.take + before(asks, room, t_take);
+        const int64_t asks = need > old ? need - old : 0;
+        int64_t take[1] = {asks}, more[3], t_take[1], t_more[3];
+        sum_before(take, t_take, room);
+        take[0] += at.take;
         // (nobody behind one who gets no page takes any: what is left is not enough for its sum)
-        const bool ok = asks == 0 || take + asks <= count;
+        const bool ok = asks == 0 || take[0] + asks <= count;
         if (!ok) {
             want = length;
             need = old;
         }
-        const int64_t back = at.back + before(old > need ? old - need : 0, room, t_back);
-        const int64_t row = at.rows + before(want > length ? want - length : 0, room, t_rows);
-        (void)before(ok ? asks : 0, room, t_taken);
+        const int64_t grows = want > length ? want - length : 0;
+        more[0] = old > need ? old - need : 0;
+        more[1] = grows;
+        more[2] = ok ? asks : 0;
+        sum_before(more, t_more, room);
+        const int64_t row = at.rows + more[1];
         if (there) {
-            plan[s] = ResizePlan{length, old, need, saturated(take), (int)back, saturated(row)};
+            plan[s] = ResizePlan{length, old, need, saturated(take[0]), (int)(at.back + more[0]), saturated(row)};
             a.length[s] = want;
             if (a.columns) a.columns[s] = need;
             if (a.start) {
                 a.start[s] = saturated(row);
-                if (s == a.n_seqs - 1) a.start[a.n_seqs] = saturated(row + (want > length ? want - length : 0));
+                if (s == a.n_seqs - 1) a.start[a.n_seqs] = saturated(row + grows);
             }
             if (a.granted) a.granted[s] = ok ? 1 : 0;
         }
-        at = at + Sums{t_take, t_back, t_rows};
-        taken += t_taken;
+        at = Sums{at.take + t_take[0], at.back + t_more[0], at.rows + t_more[1]};
+        taken += t_more[2];
     }
     at.take = taken;
     return at;
@@ -141,7 +152,7 @@ __device__ __forceinline__ void give_back(const ResizeArgs& a, const ResizePlan*
 __global__ __launch_bounds__(kThreads) void k_resize_one(ResizeArgs a)
 {
     __shared__ ResizePlan plan[kResizeSeqs];
-    __shared__ int64_t room[kWaves];
+    __shared__ int64_t room[3][kWaves];
     const int count = clamp_int(a.count[0], 0, a.n_pages);
     const Sums all = plan_all(a, plan, room, count);
     __syncthreads();
@@ -153,7 +164,7 @@ __global__ __launch_bounds__(kThreads) void k_resize_one(ResizeArgs a)
 
 __global__ __launch_bounds__(kThreads) void k_resize_plan(ResizeArgs a)
 {
-    __shared__ int64_t room[kWaves];
+    __shared__ int64_t room[3][kWaves];
     const int count = clamp_int(a.count[0], 0, a.n_pages);
     const Sums all = plan_all(a, a.plan, room, count);
     for (int64_t i = threadIdx.x; i < all.take; i += kThreads) a.taken[i] = a.free[count - 1 - i];
