@@ -25,6 +25,26 @@ struct SamplingDev {
 
 constexpr int64_t kMaxVocab = (int64_t)1 << 20;
 
+// What the rows' first reading leaves, row by row (a verification's drafts' logits behind the others). A segment
+// is 64 loads of 16 bytes, a share `lanes` of them.
+struct ScanDev {
+    float* most;               // [rows][shares] the largest logit, NaN for what makes a row have no distribution
+    double* sum;               // [rows][segments] the weights' sum relative to the segment's largest logit,
+    float* of;                 // [rows][segments] which this is
+    int32_t lanes, shares, segments;
+    int32_t per, parts;        // segments of a workgroup; workgroups of a row (0: rows are not read first)
+};
+struct RowScan {
+    float* most;
+    double* sum;
+    float* of;
+};
+MSAO_HD RowScan scan_of(const ScanDev& s, int64_t row)
+{
+    return RowScan{s.most + row * s.shares, s.sum + row * s.segments, s.of + row * s.segments};
+}
+void scan_shape(ScanDev& d, int64_t rows, int64_t vocab, int dtype);
+
 struct SampleArgs {
     LogitRows logits;
     SamplingDev set;
@@ -33,6 +53,7 @@ struct SampleArgs {
     int32_t* token;
     float* logprob;
     int32_t* kept;
+    ScanDev scan;              // workspace
 };
 
 struct VerifyArgs {
@@ -52,8 +73,11 @@ struct VerifyArgs {
     int32_t* row_token;        // the token that follows the row
     float* row_logprob;
     int32_t* row_yes;          // whether it is the row's draft
+    ScanDev scan;
 };
 
+int launch_scan(const SampleArgs& a, void* stream, void* ev0, void* ev1);
+int launch_verify_scan(const VerifyArgs& a, void* stream, void* ev0, void* ev1);
 int launch_sample(const SampleArgs& a, void* stream, void* ev0, void* ev1);
 int launch_verify(const VerifyArgs& a, void* stream, void* ev0, void* ev1);
 int launch_verify_join(const VerifyArgs& a, void* stream, void* ev0, void* ev1);

@@ -8,23 +8,26 @@
 // 64-bit weights and sums: in 32 bits sums over 10^5 tokens are off by more than the
 // lightest token's weight, and the answer would be another token now and then.
 //
-// One workgroup of 1,024 threads has a row. What the settings need decides what it does with it:
-//  - one reading for the largest logit of each thread's share, and where every token may
-//    stay also the weights' sums over segments of 64 threads' 16 bytes, in the order of the
-//    indices and relative to the largest logit of the row's first part;
-//  - the head of the order is mostly short. The j-th largest of the 1,024 threads' maxima is a
-//    bound that j tokens at least reach and few more, and only the threads whose maximum
-//    reaches it read their share again. Up to 1,024 such tokens are ranked in LDS, by
-//    comparing each with each, and the row is not read again;
-//  - a longer head ends at the key (its logit's bits in order) that histograms of the keys find:
-//    2,048 bins between bounds that close in on it, counted, or weighed as integers in two
-//    words, so that no order of atomics shows; further readings for what it needs then.
-// A weight is 17 instructions of 64 bits (a polynomial of degree 9), which for a row that is
-// summed takes about as long as reading it from memory does.
+// k_scan reads the rows, many workgroups a row, and leaves for each segment (a wavefront's 64 loads
+// of 16 bytes) the largest logit, the largest of each share of it (1, 4 or 16 loads), and where every
+// token may stay the sum of the weights relative to the segment's largest. Then one workgroup of 1,024
+// threads has a row (k_sample, k_verify):
+//  - without top_k, top_p and min_p the segments' sums say in which one the token lies;
+//  - the head of the order is mostly short. The j-th largest of the shares' maxima is a bound
+//    that j tokens at least reach and few more, and only shares whose maximum reaches it are
+//    read again. Up to 1,024 such tokens are ranked in LDS, by comparing each with each;
+//  - a longer head is found by 2,048 bins that are even in the logit, between the largest one and one
+//    below which too little weight lies: 32-bit sums say which bins the head may end in, then
+//    one reading sums the weights above them in 64 bits and collects the tokens in them, which
+//    are ranked as above. That the head ends there is checked;
+//  - where it does not, or the bins hold too many tokens (equal ones), bins of keys close in on its end.
+// A weight is some 18 instructions of 64 bits (a polynomial of degree 9): a summed row is bound by
+// them, any other one by its reading.
 #include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "msao_device.h"
@@ -42,7 +45,10 @@ constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kBins = 2 * kThreads;
 constexpr int kList = kThreads;            // tokens that are ranked in LDS
-constexpr int kTryHead = 256;              // of the threads' maxima, for a head whose length top_p decides
+constexpr int kTryHead = 256;              // of the shares' maxima, for a head whose length top_p decides
+constexpr int64_t kScanTarget = 2048;      // workgroups of a scan
+constexpr int kScanThreads = 256, kScanWaves = kScanThreads / kWave, kScanAhead = 4;
+constexpr double kMagic = 6755399441055744.0;  // 1.5 2^52: added to a number it leaves its nearest integer in the low word
 constexpr double kLog2e = 1.4426950408889634074;
 constexpr double kLn2 = 0.69314718055994530942;
 constexpr int kMostSegments = 4096;        // of a row of kMaxVocab float32 logits
@@ -59,12 +65,15 @@ __device__ __forceinline__ float value_of(uint32_t key)
     return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
 }
 
-// 2^t for t of at most a few hundred: 2^n times a polynomial in t - n, |t - n| <= 1/2. The
+// 2^(d inv) for d of at most 0: 2^n times a polynomial in d inv - n, which is within 1/2 of 0. The
 // coefficients are those of the interpolation of 2^r at Chebyshev's nodes, with the first one made 1 so that
-// equal logits have the weight 1; off by 3.3e-14 of the value at most.
-__device__ __forceinline__ double exp2_of(double t)
+// equal logits have the weight 1; off by 3.3e-14 of the value at most. `least` is -1100 / inv: below it, and of
+// -inf, the power is 0.
+__device__ __forceinline__ double exp2_of(double d, double inv, double least)
 {
-    const double n = __builtin_rint(t), r = t - n;
+    d = fmax(d, least);
+    const double t = fma(d, inv, kMagic), r = fma(d, inv, kMagic - t);
+    const int n = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
     double p = 1.020869083593037e-07;
     p = fma(p, r, 1.3259646250270451e-06);
     p = fma(p, r, 1.5252657257186041e-05);
@@ -75,29 +84,12 @@ __device__ __forceinline__ double exp2_of(double t)
     p = fma(p, r, 0.240226506956403);
     p = fma(p, r, 0.69314718055995);
     p = fma(p, r, 1.0);
-    return __builtin_ldexp(p, (int)n);
+    if (__builtin_expect(n < -1000, 0)) return __builtin_ldexp(p, n);  // (fewer digits, or none)
+    return __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, p) + ((uint64_t)(uint32_t)n << 52));
 }
 
-// Scratch that the steps of a row share.
-struct Lds {
-    union {
-        uint64_t mass[2][kBins];      // a bin's weight in units of 2^-43 and of 2^-86
-        uint32_t count[kBins];
-        double segment[kMostSegments];
-        struct {
-            uint64_t packed[kList];   // key, and the index' complement: the order of the tokens, upside down
-            double ranked[kList];
-        };
-    };
-    float list_x[kList];              // a head of the order, by index; what does not stay is -inf
-    int list_at[kList];
-    double wave_d[kWaves];
-    int wave_i[kWaves];
-    float wave_f[kWaves];
-    int wave_b[kWaves];
-    double found_d;
-    int found_i[3];
-};
+// log2(e) / T, of an infinite T not quite 0, so that -inf stays without weight.
+__device__ __forceinline__ double inverse_of(float temperature) { return fmax(kLog2e / (double)temperature, 1e-300); }
 
 // 16 bytes of a row, widened; what lies past its end, and -inf, is the value that no token has.
 template <int DT>
@@ -119,20 +111,22 @@ struct Chunk {
     }
 };
 
-// A row of logits as the workgroup walks it: step i has thread t at the 16 bytes i * kThreads + t,
-// so that (step, wavefront, lane) is the order of the indices.
+// A row of logits as a workgroup walks it: step i has thread t at the 16 bytes i * kThreads + t,
+// so that (step, wavefront, lane) is the order of the indices. Segment i * kWaves + w is wavefront w's.
 template <int DT>
 struct Row {
     static constexpr int N = Chunk<DT>::N, kAhead = 4;
     rsrc_t r;
-    int vocab, steps;
+    int vocab, steps, segments;
     __device__ __forceinline__ Row(const LogitRows& rows, int64_t row, int vocab_) : vocab(vocab_)
     {
         constexpr int es = DT == kBF16 ? 2 : 4;
         // (whole words: a row's pitch is a multiple of 16 bytes)
         r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(rows.base) + row * rows.row_bytes, (short)0,
                                               (vocab * es + 3) & ~3, 0x00020000);
-        steps = ((vocab + N - 1) / N + kThreads - 1) / kThreads;
+        const int chunks = (vocab + N - 1) / N;
+        steps = (chunks + kThreads - 1) / kThreads;
+        segments = (chunks + kWave - 1) / kWave;
     }
     __device__ __forceinline__ u32x4 load(int chunk) const { return __builtin_amdgcn_raw_buffer_load_b128(r, chunk * 16, 0, 0); }
     __device__ __forceinline__ Chunk<DT> at(int chunk) const
@@ -141,7 +135,7 @@ struct Row {
         c.end(vocab - chunk * N);
         return c;
     }
-    // f(step, first index, chunk) for every step, by the threads that call it
+    // f(step, first index, chunk) for every step
     template <typename F>
     __device__ __forceinline__ void each(F f) const
     {
@@ -168,27 +162,20 @@ struct Row {
     }
 };
 
-// A row's distribution.
-struct Dist {
-    bool none;        // a NaN, +inf, or no finite logit
-    bool listed;      // the tokens that stay are in lds.list, in the order of their indices
-    bool summed;      // every token stays, and lds.segment has the sums relative to `ref`
-    int best;         // of a row whose largest logit alone stays, its index; else -1
-    int kept;         // how many stay where that is known, else -1
-    int n;            // entries of the list
-    double m, inv;    // largest logit; log2(e) / T
-    double ref;
-    float cut;        // tokens stay with a logit above it, or equal to it and an index up to cut_at,
-    int cut_at;
-    double least;     // and (x - m) inv of at least this
-    double total;     // of the weights, where it is known
-    __device__ __forceinline__ double exponent(float x) const { return ((double)x - m) * inv; }
-    __device__ __forceinline__ bool stays(float x, int v) const
-    {
-        return (x > cut || (x == cut && v <= cut_at)) && exponent(x) >= least;
-    }
-    __device__ __forceinline__ double weight(float x, int v) const { return stays(x, v) ? exp2_of(exponent(x)) : 0.0; }
+// The settings of row r.
+struct Settings {
+    float temperature, top_p, min_p;
+    int top_k;
+    __device__ __forceinline__ bool greedy() const { return !(temperature > 0.0f); }
+    __device__ __forceinline__ bool by_k(int vocab) const { return top_k > 0 && top_k < vocab; }
+    // whether the sum over all tokens is needed
+    __device__ __forceinline__ bool sums(int vocab) const { return !greedy() && !by_k(vocab) && (top_p < 1.0f || !(min_p > 0.0f)); }
 };
+__device__ __forceinline__ Settings settings_of(const SamplingDev& s, int r)
+{
+    return Settings{s.temperature ? s.temperature[r] : 1.0f, s.top_p ? s.top_p[r] : 1.0f, s.min_p ? s.min_p[r] : 0.0f,
+                    s.top_k ? s.top_k[r] : 0};
+}
 
 // The lane's value with DPP control CTRL in the rows of ROWS, 0 where there is none.
 template <int CTRL, int ROWS>
@@ -199,6 +186,11 @@ __device__ __forceinline__ double moved(double v)
     const uint64_t b = __builtin_bit_cast(uint64_t, v);
     const uint32_t lo = (uint32_t)moved<CTRL, ROWS>((int)(uint32_t)b), hi = (uint32_t)moved<CTRL, ROWS>((int)(uint32_t)(b >> 32));
     return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <int CTRL>
+__device__ __forceinline__ float turned(float v)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, false));
 }
 
 // Sums of the lanes up to each: within rows of 16 lanes, then lane 15 of a row to the next row and
@@ -214,6 +206,146 @@ __device__ __forceinline__ T wave_scan(T v)
     v += moved<0x143, 0xC>(v);
     return v;
 }
+
+// ---- the rows' first reading ---------------------------------------------------------
+
+// Segments s, s + step, .. up to `end` of a row, by one wavefront.
+template <int DT, int SHARE>
+__device__ __forceinline__ void scan_segments(const Row<DT>& row, const RowScan& scan, const Settings& set, int first, int step, int end)
+{
+    constexpr int N = Chunk<DT>::N;
+    const int lane = threadIdx.x & (kWave - 1);
+    const bool sums = set.sums(row.vocab);
+    const double inv = inverse_of(set.temperature), least = -1100.0 / inv;
+#pragma unroll 1
+    for (int s0 = first; s0 < end; s0 += step * kScanAhead) {
+        u32x4 w[kScanAhead];
+#pragma unroll
+        for (int a = 0; a < kScanAhead; ++a) w[a] = row.load(min(s0 + a * step, end - 1) * kWave + lane);
+#pragma unroll
+        for (int a = 0; a < kScanAhead; ++a) {
+            const int s = s0 + a * step;
+            if (s >= end) break;
+            Chunk<DT> c(w[a]);
+            if ((s + 1) * kWave * N > row.vocab) c.end(row.vocab - (s * kWave + lane) * N);
+            bool bad = false;
+            float m = c.x[0];
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                bad = bad || !(c.x[e] < INFINITY);
+                m = fmaxf(m, c.x[e]);
+            }
+            if (bad) m = __builtin_nanf("");  // (kept by the comparisons below, so that the row knows)
+            auto join = [](float a, float b) { return a > b || !(a == a) ? a : b; };
+            if (SHARE >= 4) {
+                m = join(m, turned<0xB1>(m));  // lanes of four
+                m = join(m, turned<0x4E>(m));
+            }
+            if (SHARE == 16) {
+                m = join(m, turned<0x124>(m));  // rows of 16 turned by 4 and 8
+                m = join(m, turned<0x128>(m));
+            }
+            if (lane % SHARE == 0) scan.most[s * (kWave / SHARE) + lane / SHARE] = m;
+            if (!sums) continue;
+            if (SHARE == 1) {
+                m = join(m, turned<0xB1>(m));
+                m = join(m, turned<0x4E>(m));
+            }
+            if (SHARE <= 4) {
+                m = join(m, turned<0x124>(m));
+                m = join(m, turned<0x128>(m));
+            }
+            m = join(m, __shfl_xor(m, 16));
+            m = join(m, __shfl_xor(m, 32));
+            double sum = 0.0;
+            if (m > -INFINITY) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) sum += exp2_of((double)c.x[e] - (double)m, inv, least);
+            }
+            sum = wave_scan(sum);
+            if (lane == kWave - 1) {
+                scan.sum[s] = sum;
+                scan.of[s] = m;
+            }
+        }
+    }
+}
+
+template <int DT, int SHARE>
+__device__ __forceinline__ void scan_part(const LogitRows& rows, const ScanDev& scan, const SamplingDev& set, int vocab, int r, int at, int part)
+{
+    const Row<DT> row(rows, r, vocab);
+    const int wave = uniform(threadIdx.x >> 6), first = part * scan.per;
+    scan_segments<DT, SHARE>(row, scan_of(scan, at), settings_of(set, r), first + wave, kScanWaves, min(first + scan.per, row.segments));
+}
+
+template <int DT, int SHARE>
+__global__ __launch_bounds__(kScanThreads) void k_scan(SampleArgs a)
+{
+    const int r = blockIdx.x / a.scan.parts, part = blockIdx.x - r * a.scan.parts;
+    scan_part<DT, SHARE>(a.logits, a.scan, a.set, a.vocab, r, r, part);
+}
+
+// Of a verification: the rows that it looks at, and the ones of the drafts' logits that it needs.
+template <int DT, int SHARE>
+__global__ __launch_bounds__(kScanThreads) void k_verify_scan(VerifyArgs a)
+{
+    const int item = blockIdx.x / a.scan.parts, part = blockIdx.x - item * a.scan.parts;
+    const int pairs = a.n_seqs * a.ch.max_new, which = item >= pairs ? 1 : 0, s = (item - which * pairs) / a.ch.max_new;
+    const int i = item - which * pairs - s * a.ch.max_new;
+    const Rows rows = seq_rows(a.ch, s);
+    if (i >= min(rows.n, a.ch.max_new) - which) return;
+    const int r = rows.begin + i;
+    scan_part<DT, SHARE>(which ? a.draft : a.logits, a.scan, a.set, a.vocab, r, which * a.ch.n_rows + r, part);
+}
+
+// ---- one row ---------------------------------------------------------------------------
+
+// Scratch that the steps of a row share.
+struct Lds {
+    union {
+        uint64_t mass[2][kBins];      // a bin's weight in units of 2^-43 and of 2^-86
+        uint32_t count[kBins];
+        float light[kBins];
+        double segment[kMostSegments];
+    };
+    uint64_t packed[kList];           // key, and the index' complement: the order of the tokens, upside down
+    union {
+        double ranked[kList];
+        int share[kList];
+    };
+    float list_x[kList];              // tokens by index; what does not stay is -inf
+    int list_at[kList];
+    double wave_d[kWaves];
+    int wave_i[kWaves];
+    float wave_f[kWaves];
+    double found_d;
+    int found_i[3];
+    int n;
+};
+
+// A row's distribution.
+struct Dist {
+    bool none;        // a NaN, +inf, or no finite logit
+    bool listed;      // the tokens that stay are in lds.list, in the order of their indices
+    bool summed;      // lds.segment has the sums of the weights
+    int best;         // of a row whose largest logit alone stays, its index; else -1
+    int kept;         // how many stay where that is known, else -1
+    int n;            // entries of the list
+    double m, inv;    // largest logit; log2(e) / T
+    double zero;      // differences of logits below it have no weight
+    float cut;        // tokens stay with a logit above it, or equal to it and an index up to cut_at,
+    int cut_at;
+    double least;     // and (x - m) inv of at least this
+    double total;     // of the weights; known where `kept` is or `summed`
+    __device__ __forceinline__ double exponent(float x) const { return ((double)x - m) * inv; }
+    __device__ __forceinline__ double power(float x) const { return exp2_of((double)x - m, inv, zero); }
+    __device__ __forceinline__ bool stays(float x, int v) const
+    {
+        return (x > cut || (x == cut && v <= cut_at)) && exponent(x) >= least;
+    }
+    __device__ __forceinline__ double weight(float x, int v) const { return stays(x, v) ? power(x) : 0.0; }
+};
 
 __device__ __forceinline__ double* room_of(Lds& lds, double) { return lds.wave_d; }
 __device__ __forceinline__ int* room_of(Lds& lds, int) { return lds.wave_i; }
@@ -256,6 +388,15 @@ __device__ __forceinline__ void sum_segments(const Row<DT>& row, Lds& lds, F f)
         s = wave_scan(s);
         if (lane == kWave - 1) segment[i * kWaves + wave] = s;
     });
+    __syncthreads();
+}
+
+__device__ __forceinline__ double sum_of_segments(Lds& lds, int segments)
+{
+    double part = 0.0, total;
+    for (int s = threadIdx.x; s < segments; s += kThreads) part += lds.segment[s];
+    (void)block_before(part, lds, total);
+    return total;
 }
 
 // With the segments' sums in LDS: the first index whose running sum passes target(total); the last
@@ -276,8 +417,8 @@ __device__ __forceinline__ Found<T> locate(const Row<DT>& row, Lds& lds, F f, G 
         lds.found_i[1] = -1;
     }
     __syncthreads();
-    const int segments = row.steps * kWaves, per = (segments + kThreads - 1) / kThreads;
-    const int s0 = min((int)threadIdx.x * per, segments), s1 = min(s0 + per, segments);
+    const int per = (row.segments + kThreads - 1) / kThreads;
+    const int s0 = min((int)threadIdx.x * per, row.segments), s1 = min(s0 + per, row.segments);
     T mine = 0;
     for (int s = s0; s < s1; ++s) mine += segment[s];
     T total;
@@ -298,7 +439,6 @@ __device__ __forceinline__ Found<T> locate(const Row<DT>& row, Lds& lds, F f, G 
         }
         run += w;
     }
-    // (one atomic a wavefront: most have neither or both)
     const uint64_t hits = __ballot(passed != kNone), any = __ballot(last >= 0);
     if (hits && lane == __builtin_ctzll(hits)) atomicMin(&lds.found_i[0], passed);
     if (any && lane == 63 - __builtin_clzll(any)) atomicMax(&lds.found_i[1], last);
@@ -308,7 +448,7 @@ __device__ __forceinline__ Found<T> locate(const Row<DT>& row, Lds& lds, F f, G 
     __syncthreads();
     base = (T)lds.found_d;
     if (s >= 0 && wave == 0) {
-        const int step = s / kWaves, chunk = step * kThreads + (s - step * kWaves) * kWave + lane;
+        const int chunk = s * kWave + lane;
         const Chunk<DT> c = row.at(chunk);
         T w[N], sum = 0;
         int top = -1;
@@ -339,12 +479,11 @@ template <typename T, int DT, typename F, typename G>
 __device__ __forceinline__ Found<T> find_in_order(const Row<DT>& row, Lds& lds, F f, G target_of)
 {
     sum_segments<T>(row, lds, f);
-    __syncthreads();
     return locate<T>(row, lds, f, target_of);
 }
 
 // Of kBins measures, two a thread from the top down, the first place (from the top) where their running
-// sum from `run` on reaches the target, and what lies above it; `last`: of sums that end below it by a
+// sum from `base` on reaches the target, and what lies above it; `last_too`: of sums that end below it by a
 // rounding, the last one that has anything. -1 where there is none.
 struct Place {
     int at;
@@ -394,18 +533,43 @@ __device__ __forceinline__ void clear_bins(Lds& lds, bool masses)
     __syncthreads();
 }
 
-// A value that at least j of the threads' values reach and, but for its lower bits, no larger one; -inf where
+// The shares of a row and their largest logits; the first ones of each thread in registers.
+struct Shares {
+    static constexpr int kOwn = 4;
+    const float* most;
+    int n;
+    float own[kOwn];
+    __device__ __forceinline__ Shares(const float* most_, int n_) : most(most_), n(n_)
+    {
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            const int s = i * kThreads + (int)threadIdx.x;
+            own[i] = s < n ? most[s] : -INFINITY;
+        }
+    }
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const
+    {
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i)
+            if (i * kThreads + (int)threadIdx.x < n) f(i * kThreads + (int)threadIdx.x, own[i]);
+        for (int s = kOwn * kThreads + (int)threadIdx.x; s < n; s += kThreads) f(s, most[s]);
+    }
+};
+
+// A value that at least j of the shares' reach and, but for its lower bits, no larger one; -inf where
 // there are fewer.
-__device__ __forceinline__ float reached_by(Lds& lds, float mine, int j)
+__device__ __forceinline__ float reached_by(Lds& lds, const Shares& shares, int j)
 {
-    const uint32_t k = key_of(mine);
-    const bool there = mine > -INFINITY;
     uint32_t prefix = 0;
     double above = 0.0;
 #pragma unroll 1
     for (int shift = 21; shift >= 10; shift -= 11) {
         clear_bins(lds, false);
-        if (there && (shift == 21 || k >> 21 == prefix >> 21)) atomicAdd(&lds.count[(k >> shift) & (kBins - 1)], 1u);
+        shares.each([&](int, float x) {
+            const uint32_t k = key_of(x);
+            if (x > -INFINITY && (shift == 21 || k >> 21 == prefix >> 21)) atomicAdd(&lds.count[(k >> shift) & (kBins - 1)], 1u);
+        });
         __syncthreads();
         const int b0 = kBins - 1 - 2 * (int)threadIdx.x;
         const Place p = top_place(lds, (double)lds.count[b0], (double)lds.count[b0 - 1], above, (double)j, false);
@@ -414,6 +578,186 @@ __device__ __forceinline__ float reached_by(Lds& lds, float mine, int j)
         above = p.above;
     }
     return value_of(prefix);
+}
+
+// One token more in lds.packed, in no order: their ranks give them one.
+__device__ __forceinline__ void push(Lds& lds, float x, int v)
+{
+    const int at = atomicAdd(&lds.n, 1);
+    if (at < kList) lds.packed[at] = (uint64_t)key_of(x) << 32 | (uint32_t)~(uint32_t)v;
+}
+
+// The tokens of `bound` and above in LDS: how many, which may be more than there is room for.
+template <int DT>
+__device__ __forceinline__ int collect(const Row<DT>& row, Lds& lds, const Shares& shares, int lanes, float bound)
+{
+    constexpr int N = Row<DT>::N;
+    int some = 0, total;
+    shares.each([&](int, float x) { some += x >= bound && x > -INFINITY ? 1 : 0; });
+    int at = block_before(some, lds, total);
+    if (total > kList) return total;
+    if (threadIdx.x == 0) lds.n = 0;
+    shares.each([&](int s, float x) {
+        if (x >= bound && x > -INFINITY) lds.share[at++] = s;
+    });
+    __syncthreads();
+    for (int j = (int)threadIdx.x / lanes; j < total; j += kThreads / lanes) {
+        const int chunk = lds.share[j] * lanes + (int)threadIdx.x % lanes;
+        const Chunk<DT> c = row.at(chunk);
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (c.x[e] >= bound && c.x[e] > -INFINITY) push(lds, c.x[e], chunk * N + e);
+    }
+    __syncthreads();
+    const int n = lds.n;
+    __syncthreads();
+    return n;
+}
+
+// With n tokens in lds.packed, which are what comes in the order behind `before` tokens of the weight `above`: which of
+// them stay of a head of `most` tokens, or of the weight `target` (0: top_p of the n), with min_p. False, and
+// nothing changed, where the head does not end among them. `light`: the head is `most`
+// tokens, whatever top_p and min_p say.
+template <bool KEEP>
+__device__ __forceinline__ bool rank(Lds& lds, Dist& d, const Settings& set, int n, double most, double target, double above, bool light)
+{
+    const int t = threadIdx.x;
+    const bool there = t < n;
+    const uint64_t mine = there ? lds.packed[t] : 0;
+    int by_key = 0, by_index = 0;
+    if (uniform(t & ~(kWave - 1)) < n) {
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) {
+            const uint64_t a = lds.packed[j];
+            by_key += a > mine ? 1 : 0;
+            by_index += (uint32_t)a > (uint32_t)mine ? 1 : 0;
+        }
+    }
+    const float x = value_of((uint32_t)(mine >> 32));
+    const int at = (int)~(uint32_t)mine;
+    const double w = there ? d.power(x) : 0.0;
+    __syncthreads();  // (lds.share has been read)
+    if (there) lds.ranked[by_key] = w;
+    __syncthreads();
+    // thread r has the token of rank r
+    bool in = t < n && (double)t < most;
+    const double r_w = in ? lds.ranked[t] : 0.0;
+    double sum;
+    const double before = above + block_before(r_w, lds, sum);
+    if (set.top_p < 1.0f && !light) {
+        if (target > 0.0 && (above >= target || above + sum < target)) return false;
+        const double of = target > 0.0 ? target : (double)set.top_p * sum;
+        in = in && ((t == 0 && above == 0.0) || before < of);
+    }
+    // (all of them a head of the order: their number says which)
+    int kept;
+    (void)block_before(in ? 1 : 0, lds, kept);
+    const double least = set.min_p > 0.0f && !light ? fmin(log2((double)set.min_p), 0.0) : -INFINITY;
+    const bool stays = there && by_key < kept && d.exponent(x) >= least;
+    (void)block_before(stays ? 1 : 0, lds, kept);
+    (void)block_before(t < kept ? r_w : 0.0, lds, d.total);
+    if (stays && by_key == kept - 1) {
+        lds.found_d = (double)x;
+        lds.found_i[0] = at;
+    }
+    if (KEEP && there) {
+        lds.list_x[by_index] = stays ? x : -INFINITY;
+        lds.list_at[by_index] = at;
+    }
+    __syncthreads();
+    if (kept > 0) {
+        d.cut = (float)lds.found_d;
+        d.cut_at = lds.found_i[0];
+    }
+    d.kept = kept;
+    d.n = n;
+    __syncthreads();
+    return true;
+}
+
+// A long head, of `k` tokens or of the weight `target` (0: by number), of the tokens that stay in d: with its end in d, the sums of
+// its weights in lds.segment. False, and nothing changed, where the bins do not give its end. `lowest`: a logit that it
+// does not go below.
+template <bool KEEP, int DT>
+__device__ __forceinline__ bool long_head(const Row<DT>& row, Lds& lds, Dist& d, const Settings& set, float lowest, double k, double target)
+{
+    constexpr int N = Row<DT>::N;
+    const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
+    const bool by_number = !(target > 0.0);
+    const float m = (float)d.m, scale = (float)(kBins - 1) / (m - lowest), inv = (float)d.inv;
+    if (!(scale > 0.0f) || !(scale < 3e38f)) return false;
+    // (rounded, but never out of the logits' order)
+    auto bin_of = [&](float x) { return min((int)((x - lowest) * scale), kBins - 1); };
+    clear_bins(lds, false);
+    row.each([&](int, int v, const Chunk<DT>& c) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            if (!(c.x[e] >= lowest) || !d.stays(c.x[e], v + e)) continue;
+            const int b = bin_of(c.x[e]);
+            if (by_number) atomicAdd(&lds.count[b], 1u);
+            else atomicAdd(&lds.light[b], __builtin_amdgcn_exp2f((c.x[e] - m) * inv));
+        }
+    });
+    __syncthreads();
+    const int b0 = kBins - 1 - 2 * (int)threadIdx.x;
+    const double m0 = by_number ? (double)lds.count[b0] : (double)lds.light[b0], m1 = by_number ? (double)lds.count[b0 - 1] : (double)lds.light[b0 - 1];
+    // sums of 32-bit weights are off by less than one in 20,000 as a rule; what they give is checked below
+    const double goal = by_number ? k : target;
+    const Place from = top_place(lds, m0, m1, 0.0, by_number ? goal : goal * (1.0 - 5e-5), false);
+    const Place to = by_number ? from : top_place(lds, m0, m1, 0.0, goal * (1.0 + 5e-5), true);
+    if (from.at < 0 || to.at < 0) return false;
+    const int upper = kBins - 1 - from.at, lower = kBins - 1 - to.at;
+    if (threadIdx.x == 0) lds.n = 0;
+    __syncthreads();
+    int over = 0;
+    row.each([&](int i, int v, const Chunk<DT>& c) {
+        double s = 0.0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            if (!(c.x[e] >= lowest) || !d.stays(c.x[e], v + e)) continue;
+            const int b = bin_of(c.x[e]);
+            if (b > upper) {
+                s += d.power(c.x[e]);
+                ++over;
+            } else if (b >= lower) push(lds, c.x[e], v + e);
+        }
+        s = wave_scan(s);
+        if (lane == kWave - 1) lds.segment[i * kWaves + wave] = s;
+    });
+    __syncthreads();
+    const int n = lds.n;
+    const double above = sum_of_segments(lds, row.segments);
+    int number;
+    (void)block_before(over, lds, number);
+    if (n < 1 || n > kList) return false;
+    Dist next = d;
+    if (by_number) {
+        if ((double)number >= k || (double)(number + n) < k) return false;
+        (void)rank<KEEP>(lds, next, set, n, k - (double)number, 0.0, above, true);
+    } else {
+        Settings p = set;
+        p.min_p = 0.0f;
+        if (!rank<KEEP>(lds, next, p, n, (double)n, target, above, false)) return false;
+    }
+    // the tokens of these bins that stay join their segments, each segment's in the order of their indices
+    if (KEEP && (int)threadIdx.x < n) {
+        const int t = threadIdx.x;
+        auto segment = [&](int i) { return lds.list_at[i] / (kWave * N); };
+        const int mine = segment(t);
+        if (t == 0 || segment(t - 1) != mine) {
+            double s = lds.segment[mine];
+            for (int i = t; i < n && segment(i) == mine; ++i)
+                if (lds.list_x[i] > -INFINITY) s += d.power(lds.list_x[i]);
+            lds.segment[mine] = s;
+        }
+    }
+    __syncthreads();
+    next.kept += number;
+    next.total += above;
+    next.summed = KEEP;
+    next.listed = false;
+    d = next;
+    return true;
 }
 
 // Where the order of the tokens that stay in d reaches the target: the key's value, how many tokens of that
@@ -445,7 +789,7 @@ __device__ __forceinline__ Cut cut_of(const Row<DT>& row, Lds& lds, const Dist& 
                 if (k < lo || k > hi || !d.stays(c.x[e], v + e)) continue;
                 const int bin = (int)((k - lo) >> shift);
                 if (MASS && !exact) {
-                    const double w = exp2_of(d.exponent(c.x[e])) * kHi;
+                    const double w = d.power(c.x[e]) * kHi;
                     const uint64_t up = (uint64_t)w;
                     atomicAdd((unsigned long long*)&lds.mass[0][bin], up);
                     atomicAdd((unsigned long long*)&lds.mass[1][bin], (uint64_t)((w - (double)up) * kHi));
@@ -459,7 +803,7 @@ __device__ __forceinline__ Cut cut_of(const Row<DT>& row, Lds& lds, const Dist& 
             if (!MASS) return (double)lds.count[bin];
             if (!exact) return (double)lds.mass[0][bin] * kInvHi + (double)lds.mass[1][bin] * (kInvHi * kInvHi);
             const uint32_t n = lds.count[bin];
-            return n ? (double)n * exp2_of(d.exponent(value(lo + (uint32_t)bin))) : 0.0;
+            return n ? (double)n * d.power(value(lo + (uint32_t)bin)) : 0.0;
         };
         const int b0 = kBins - 1 - 2 * (int)threadIdx.x;
         const Place p = top_place(lds, measure(b0), measure(b0 - 1), above, target, !first);
@@ -471,7 +815,7 @@ __device__ __forceinline__ Cut cut_of(const Row<DT>& row, Lds& lds, const Dist& 
             Cut cut;
             cut.there = true;
             cut.x = value(lo + bin);
-            const double w = MASS ? exp2_of(d.exponent(cut.x)) : 1.0, count = (double)lds.count[bin];
+            const double w = MASS ? d.power(cut.x) : 1.0, count = (double)lds.count[bin];
             double n = fmax(ceil((target - above) / w), 1.0);
             if (n > 1.0 && above + (n - 1.0) * w >= target) n -= 1.0;
             cut.n = fmin(n, count);
@@ -484,187 +828,81 @@ __device__ __forceinline__ Cut cut_of(const Row<DT>& row, Lds& lds, const Dist& 
     }
 }
 
-// The settings of row r.
-struct Settings {
-    float temperature, top_p, min_p;
-    int top_k;
-};
-__device__ __forceinline__ Settings settings_of(const SamplingDev& s, int r)
-{
-    return Settings{s.temperature ? s.temperature[r] : 1.0f, s.top_p ? s.top_p[r] : 1.0f, s.min_p ? s.min_p[r] : 0.0f,
-                    s.top_k ? s.top_k[r] : 0};
-}
-
-// The tokens of `bound` and above in LDS, packed, in an order that is always the same: how many, or more
-// than kList, of which none is there. `mine`: the largest logit of the thread's share.
-template <int DT>
-__device__ __forceinline__ int collect(const Row<DT>& row, Lds& lds, float mine, float bound)
-{
-    constexpr int N = Row<DT>::N;
-    const bool some = mine >= bound && mine > -INFINITY;
-    int n = 0, total;
-    if (some)
-        row.each([&](int, int, const Chunk<DT>& c) {
-#pragma unroll
-            for (int e = 0; e < N; ++e) n += c.x[e] >= bound && c.x[e] > -INFINITY ? 1 : 0;
-        });
-    int at = block_before(n, lds, total);
-    if (total > kList) return total;
-    if (some)
-        row.each([&](int, int v, const Chunk<DT>& c) {
-#pragma unroll
-            for (int e = 0; e < N; ++e)
-                if (c.x[e] >= bound && c.x[e] > -INFINITY) lds.packed[at++] = (uint64_t)key_of(c.x[e]) << 32 | (uint32_t)~(uint32_t)(v + e);
-        });
-    if (threadIdx.x == 0 && total < kList) lds.packed[total] = 0;  // (they are read in pairs)
-    __syncthreads();
-    return total;
-}
-
-// With n tokens packed in LDS, which are a head of the order: what of them stays. `whole`: the weight that top_p is
-// of, or 0 for that of the first top_k of them. False, and nothing changed, where top_p's head goes on behind them.
-template <bool KEEP>
-__device__ __forceinline__ bool rank(Lds& lds, Dist& d, const Settings& set, int n, int most, double whole)
-{
-    const int t = threadIdx.x;
-    const bool there = t < n;
-    const uint64_t mine = there ? lds.packed[t] : 0;
-    int by_key = 0, by_index = 0;
-    if (uniform(t & ~(kWave - 1)) < n) {
-        for (int j = 0; j < n; j += 2) {
-            const uint64_t a = lds.packed[j], b = lds.packed[j + 1 < kList ? j + 1 : j];
-            by_key += a > mine ? 1 : 0;
-            by_index += (uint32_t)a > (uint32_t)mine ? 1 : 0;
-            if (j + 1 < n) {
-                by_key += b > mine ? 1 : 0;
-                by_index += (uint32_t)b > (uint32_t)mine ? 1 : 0;
-            }
-        }
-    }
-    const float x = value_of((uint32_t)(mine >> 32));
-    const int at = (int)~(uint32_t)mine;
-    const double e = there ? d.exponent(x) : 0.0, w = there ? exp2_of(e) : 0.0;
-    if (there) lds.ranked[by_key] = w;
-    __syncthreads();
-    // thread r has the token of rank r
-    const double r_w = t < n && t < most ? lds.ranked[t] : 0.0;
-    double sum;
-    const double before = block_before(r_w, lds, sum);
-    bool in = t < n && t < most;
-    if (set.top_p < 1.0f) {
-        const double of = whole > 0.0 ? whole : sum, target = (double)set.top_p * of;
-        if (whole > 0.0 && sum < target) return false;
-        in = in && (t == 0 || before < target);
-    }
-    // (all of them a head of the order: their number says which)
-    int kept;
-    (void)block_before(in ? 1 : 0, lds, kept);
-    const double least = set.min_p > 0.0f ? fmin(log2((double)set.min_p), 0.0) : -INFINITY;
-    const bool stays = there && by_key < kept && e >= least;
-    (void)block_before(stays ? 1 : 0, lds, kept);
-    (void)block_before(t < kept ? r_w : 0.0, lds, d.total);
-    if (stays && by_key == kept - 1) {
-        lds.found_d = (double)x;
-        lds.found_i[0] = at;
-    }
-    if (KEEP && there) {
-        lds.list_x[by_index] = stays ? x : -INFINITY;
-        lds.list_at[by_index] = at;
-    }
-    __syncthreads();
-    d.cut = (float)lds.found_d;
-    d.cut_at = lds.found_i[0];
-    d.kept = kept;
-    d.n = n;
-    d.listed = KEEP;
-    __syncthreads();
-    return true;
-}
-
-// KEEP: lds.list may be written.
+// KEEP: what a pick needs is left in LDS.
 template <bool KEEP, int DT>
-__device__ __forceinline__ Dist solve(const Row<DT>& row, Lds& lds, const Settings& set)
+__device__ __forceinline__ Dist solve(const Row<DT>& row, Lds& lds, const Settings& set, const RowScan& scan, int lanes)
 {
     constexpr int N = Row<DT>::N;
+    constexpr float kLowest = -3.402823466e38f;
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
     Dist d;
-    d.inv = kLog2e / (double)set.temperature;
+    d.inv = inverse_of(set.temperature);
+    d.zero = -1100.0 / d.inv;
     d.cut = -INFINITY;
     d.cut_at = -1;
     d.least = -INFINITY;
     d.listed = d.summed = false;
     d.best = d.kept = -1;
     d.n = 0;
-    d.total = d.ref = 0.0;
-    const bool greedy = !(set.temperature > 0.0f), by_k = set.top_k > 0 && set.top_k < row.vocab;
-    const bool small = row.vocab <= kList;  // every token is ranked
-    const bool sums = !greedy && !by_k && !small && (set.top_p < 1.0f || !(set.min_p > 0.0f));
-
-    // the largest logit, of each thread and of all; with the sums relative to the largest of the row's first part
-    auto largest = [&](float mine, bool bad, bool& any_bad) {
-        float m = mine;
-#pragma unroll
-        for (int s = 1; s < kWave; s <<= 1) m = fmaxf(m, __shfl_xor(m, s));
-        const bool b = __ballot(bad) != 0;
-        __syncthreads();
-        if (lane == 0) {
-            lds.wave_f[wave] = m;
-            lds.wave_b[wave] = b;
-        }
-        __syncthreads();
-        any_bad = false;
-        for (int w = 0; w < kWaves; ++w) {
-            m = fmaxf(m, lds.wave_f[w]);
-            any_bad = any_bad || lds.wave_b[w] != 0;
-        }
-        return m;
-    };
+    d.total = 0.0;
+    const bool small = row.vocab <= kList;  // every token is ranked: no scan
+    const int n_shares = small ? 0 : row.segments * (kWave / lanes);
+    const Shares shares(scan.most, n_shares);
     float mine = -INFINITY;
     bool bad = false;
-    auto look = [&](const Chunk<DT>& c) {
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            bad = bad || !(c.x[e] < INFINITY);
-            mine = fmaxf(mine, c.x[e]);
-        }
+    auto look = [&](float x) {
+        bad = bad || !(x < INFINITY);
+        mine = fmaxf(mine, x);
     };
-    if (sums) {
+    if (small) {
         const Chunk<DT> c = row.at(threadIdx.x);
-        float f = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < N; ++e) f = fmaxf(f, c.x[e]);
-        bool ignored;
-        f = largest(f, false, ignored);
-        d.ref = f > -INFINITY && f < INFINITY ? (double)f : 0.0;
-        __syncthreads();
-        row.each([&](int i, int, const Chunk<DT>& c) {
-            look(c);
-            double s = 0.0;
-#pragma unroll
-            for (int e = 0; e < N; ++e) s += c.x[e] > -INFINITY ? exp2_of(((double)c.x[e] - d.ref) * d.inv) : 0.0;
-            s = wave_scan(s);
-            if (lane == kWave - 1) lds.segment[i * kWaves + wave] = s;
-        });
+        for (int e = 0; e < N; ++e) look(c.x[e]);
     } else
-        row.each([&](int, int, const Chunk<DT>& c) { look(c); });
-    bool any_bad;
-    const float m = largest(mine, bad, any_bad);
+        shares.each([&](int, float x) { look(x); });
+#pragma unroll
+    for (int s = 1; s < kWave; s <<= 1) mine = fmaxf(mine, __shfl_xor(mine, s));
+    const bool wave_bad = __ballot(bad) != 0;
+    if (lane == 0) {
+        lds.wave_f[wave] = mine;
+        lds.wave_i[wave] = wave_bad;
+    }
+    if (threadIdx.x == 0) {
+        lds.found_i[0] = kNone;
+        lds.n = 0;
+    }
+    __syncthreads();
+    float m = mine;
+    bool any_bad = false;
+    for (int w = 0; w < kWaves; ++w) {
+        m = fmaxf(m, lds.wave_f[w]);
+        any_bad = any_bad || lds.wave_i[w] != 0;
+    }
+    __syncthreads();
     d.none = any_bad || m == -INFINITY;
     d.m = m;
     if (d.none) return d;
-    if (greedy) {  // the largest alone: the first of equal ones
-        if (threadIdx.x == 0) lds.found_i[0] = kNone;
-        __syncthreads();
+    if (set.greedy()) {  // the largest alone: the first of equal ones
+        int s = kNone;
+        if (small) s = threadIdx.x;
+        else {
+            shares.each([&](int i, float x) { s = x == m ? min(s, i) : s; });
+            if (s != kNone) atomicMin(&lds.found_i[0], s);
+            __syncthreads();
+            s = lds.found_i[0] * lanes + (int)threadIdx.x;
+            __syncthreads();
+            if (threadIdx.x == 0) lds.found_i[0] = kNone;
+            __syncthreads();
+        }
+        const Chunk<DT> c = row.at(s);
         int at = kNone;
-        if (mine == m)
-            row.each([&](int, int v, const Chunk<DT>& c) {
 #pragma unroll
-                for (int e = 0; e < N; ++e) at = c.x[e] == m ? min(at, v + e) : at;
-            });
-        if (at != kNone) atomicMin(&lds.found_i[0], at);
+        for (int e = N - 1; e >= 0; --e) at = c.x[e] == m ? s * N + e : at;
+        if (at != kNone && (small || (int)threadIdx.x < lanes)) atomicMin(&lds.found_i[0], at);
         __syncthreads();
         d.best = d.cut_at = lds.found_i[0];
         d.inv = 0.0;
+        d.zero = -1.0;
         d.cut = m;
         d.kept = 1;
         d.total = 1.0;
@@ -672,78 +910,95 @@ __device__ __forceinline__ Dist solve(const Row<DT>& row, Lds& lds, const Settin
         return d;
     }
 
+    const bool by_k = set.by_k(row.vocab), sums = !small && set.sums(row.vocab);
     const int k = by_k ? set.top_k : row.vocab;
     double whole = 0.0;
     if (sums) {
-        auto weigh = [&](float x, int) { return x > -INFINITY ? exp2_of(((double)x - d.ref) * d.inv) : 0.0; };
-        if ((d.m - d.ref) * d.inv > 900.0) {  // (sums of such weights may not hold)
-            d.ref = d.m;
-            sum_segments<double>(row, lds, weigh);
+        for (int s = threadIdx.x; s < row.segments; s += kThreads) {
+            const float of = scan.of[s];
+            lds.segment[s] = of > -INFINITY ? scan.sum[s] * d.power(of) : 0.0;
         }
+        __syncthreads();
+        whole = sum_of_segments(lds, row.segments);
         if (!(set.top_p < 1.0f)) {
             d.summed = true;
+            d.total = whole;
             return d;
         }
-        __syncthreads();
-        double part = 0.0;
-        for (int s = threadIdx.x; s < row.steps * kWaves; s += kThreads) part += lds.segment[s];
-        (void)block_before(part, lds, whole);
-        whole *= exp2_of((d.ref - d.m) * d.inv);
     }
-    // a short head: its tokens, or more than kList
+    // a short head: its tokens, or more than there is room for
     const double target = (double)set.top_p * whole;
     float bound = -INFINITY;
-    bool attempt = small;
-    if (!small && by_k) {
-        bound = reached_by(lds, mine, min(k, kThreads));
-        attempt = k <= kThreads;
-    } else if (!small && sums) {
-        attempt = target < (double)kList;  // (no weight is above 1)
-        if (attempt) bound = reached_by(lds, mine, kTryHead);
-    } else if (!small) {
-        attempt = true;  // min_p alone: the tokens of that weight, and some below it by the rounding of the bound
-        bound = (float)(d.m + (log2(fmin((double)set.min_p, 1.0)) - 1e-3) / d.inv);
-        bound = bound - fabsf(bound) * 1e-6f;
-    }
-    if (attempt) {
-        const int n = collect(row, lds, mine, bound);
-        if (n > 0 && n <= kList && rank<KEEP>(lds, d, set, n, min(k, n), by_k || small || !sums ? 0.0 : whole)) return d;
+    int n = 0;
+    if (small) {
+        const Chunk<DT> c = row.at(threadIdx.x);
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (c.x[e] > -INFINITY) push(lds, c.x[e], (int)threadIdx.x * N + e);
         __syncthreads();
+        n = lds.n;
+        __syncthreads();
+    } else {
+        bool attempt = true;
+        if (by_k) {
+            attempt = k <= kList;
+            if (attempt) bound = reached_by(lds, shares, k);
+        } else if (sums) {
+            attempt = target < (double)kList;  // (no weight is above 1)
+            if (attempt) bound = reached_by(lds, shares, kTryHead);
+        } else {  // min_p alone: the tokens of that weight, and some below it by the rounding of the bound
+            bound = (float)(d.m + (log2(fmin((double)set.min_p, 1.0)) - 1e-3) / d.inv);
+            bound = bound - fabsf(bound) * 1e-6f;
+        }
+        if (attempt) n = collect(row, lds, shares, lanes, bound);
     }
+    if (n > 0 && n <= kList && rank<KEEP>(lds, d, set, n, (double)min(k, n), sums ? fmax(target, 1e-300) : 0.0, 0.0, false)) {
+        d.listed = KEEP;
+        return d;
+    }
+    __syncthreads();
 
     // a long one
     auto narrow = [&](const Cut& c) {
+        const Dist before = d;
+        d.kept = -1;
+        d.summed = false;
         d.cut_at = kNone;
-        if (!c.all) {  // the first of the tokens of that value
-            const Dist before = d;
+        if (!c.all)  // the first of the tokens of that value
             d.cut_at = find_in_order<int>(row, lds, [&](float x, int v) { return x == c.x && before.stays(x, v) ? 1 : 0; },
                                           [&](int) { return (int)c.n - 1; }).at;
-        }
         d.cut = c.x;
     };
     if (by_k) {
-        const Cut c = cut_of<false>(row, lds, d, bound > -INFINITY && k <= kThreads ? bound : -3.402823466e38f, (double)k);
-        if (c.there) narrow(c);
+        const float lowest = bound > -INFINITY ? bound : kLowest;
+        if (!long_head<KEEP>(row, lds, d, set, lowest, (double)k, 0.0)) {
+            const Cut c = cut_of<false>(row, lds, d, lowest, (double)k);
+            if (c.there) narrow(c);
+        }
     }
     if (set.top_p < 1.0f) {
-        double t = target;
         if (!sums) {
-            sum_segments<double>(row, lds, [&](float x, int v) { return d.weight(x, v); });
-            __syncthreads();
-            double part = 0.0;
-            for (int s = threadIdx.x; s < row.steps * kWaves; s += kThreads) part += lds.segment[s];
-            (void)block_before(part, lds, whole);
-            t = (double)set.top_p * whole;
+            if (d.kept < 0) {
+                sum_segments<double>(row, lds, [&](float x, int v) { return d.weight(x, v); });
+                whole = sum_of_segments(lds, row.segments);
+            } else whole = d.total;
         }
+        const double goal = fmax((double)set.top_p * whole, 1e-300);
         // the tokens below a (1 - top_p) / vocab of the whole are less than (1 - top_p) of it together; at
         // least the first stays
         const double share = fmax((1.0 - (double)set.top_p) * whole / (double)row.vocab, 1e-300);
         const double low = d.m + (log2(fmin(share, 1.0)) - 1e-3) / d.inv;
-        const float lowest = fmaxf((float)(low - fabs(low) * 1e-6), -3.402823466e38f);
-        const Cut c = cut_of<true>(row, lds, d, lowest, fmax(t, 1e-300));
-        if (c.there) narrow(c);
+        const float lowest = fmaxf((float)(low - fabs(low) * 1e-6), kLowest);
+        if (!long_head<KEEP>(row, lds, d, set, lowest, 0.0, goal)) {
+            const Cut c = cut_of<true>(row, lds, d, lowest, goal);
+            if (c.there) narrow(c);
+        }
     }
-    if (set.min_p > 0.0f) d.least = fmin(log2((double)set.min_p), 0.0);
+    if (set.min_p > 0.0f) {
+        d.least = fmin(log2((double)set.min_p), 0.0);
+        d.kept = -1;
+        d.summed = false;
+    }
     return d;
 }
 
@@ -780,27 +1035,18 @@ template <int DT>
 __device__ __forceinline__ Found<double> draw(const Row<DT>& row, Lds& lds, const Dist& d, float u)
 {
     if (d.best >= 0) return Found<double>{d.best, 1.0};
-    if (d.summed) {
-        Found<double> f = locate<double>(row, lds, [&](float x, int) { return x > -INFINITY ? exp2_of(((double)x - d.ref) * d.inv) : 0.0; },
-                                         [&](double total) { return drawn(u, total); });
-        f.total *= exp2_of((d.ref - d.m) * d.inv);
-        // (relative to a smaller logit than the largest a weight may be above 0 that is not)
-        if (f.at >= 0 && exp2_of(d.exponent(row.value(f.at))) > 0.0) return f;
-    }
-    return pick(row, lds, d, u, [&](float x, int v) { return d.weight(x, v); });
+    auto weight = [&](float x, int v) { return d.weight(x, v); };
+    if (d.summed) return locate<double>(row, lds, weight, [&](double total) { return drawn(u, total); });
+    return pick(row, lds, d, u, weight);
 }
 
 // The weights' sum alone.
 template <int DT>
 __device__ __forceinline__ double whole_of(const Row<DT>& row, Lds& lds, const Dist& d)
 {
-    if (d.best >= 0 || d.kept >= 0) return d.total;
-    if (!d.summed) sum_segments<double>(row, lds, [&](float x, int v) { return d.weight(x, v); });
-    __syncthreads();
-    double part = 0.0, total;
-    for (int s = threadIdx.x; s < row.steps * kWaves; s += kThreads) part += lds.segment[s];
-    (void)block_before(part, lds, total);
-    return d.summed ? total * exp2_of((d.ref - d.m) * d.inv) : total;
+    if (d.kept >= 0 || d.summed) return d.total;
+    sum_segments<double>(row, lds, [&](float x, int v) { return d.weight(x, v); });
+    return sum_of_segments(lds, row.segments);
 }
 
 // ln p of token v.
@@ -816,7 +1062,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     __shared__ Lds lds;
     const int r = blockIdx.x;
     const Row<DT> row(a.logits, r, a.vocab);
-    const Dist d = solve<true>(row, lds, settings_of(a.set, r));
+    const Dist d = solve<true>(row, lds, settings_of(a.set, r), scan_of(a.scan, r), a.scan.lanes);
     Found<double> f{-1, 0.0};
     int kept = 0;
     if (!d.none) {
@@ -850,7 +1096,7 @@ __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a)
     const bool last = i == n - 1;
     const Row<DT> row(a.logits, r, a.vocab);
     const Settings set = settings_of(a.set, r);
-    const Dist p = solve<true>(row, lds, set);
+    Dist p = solve<true>(row, lds, set, scan_of(a.scan, r), a.scan.lanes);
     int token = -1;
     bool yes = false;
     double total = 1.0;
@@ -865,8 +1111,9 @@ __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a)
             bool certain = a.draft.base == nullptr;
             if (!certain) {
                 const Row<DT> other(a.draft, r, a.vocab);
-                const Dist q = solve<false>(other, lds, set);
+                const Dist q = solve<false>(other, lds, set, scan_of(a.scan, a.ch.n_rows + r), a.scan.lanes);
                 certain = q.none;
+                p.summed = false;  // (the segments are q's by now)
                 if (!certain) {
                     const double qt = whole_of(other, lds, q), qd = known ? q.weight(other.value(draft), draft) : 0.0;
                     yes = ua * qd * total < wd * qt;
@@ -879,14 +1126,15 @@ __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a)
             }
             if (certain) {
                 yes = ua * total < wd;
-                if (!yes) token = pick(row, lds, p, u, [&](float x, int v) { return v == draft ? 0.0 : p.weight(x, v); }).at;
+                if (!yes) {
+                    token = pick(row, lds, p, u, [&](float x, int v) { return v == draft ? 0.0 : p.weight(x, v); }).at;
+                    p.summed = false;
+                }
             }
             if (yes) token = draft;
         }
         if (token < 0) {
-            Dist again = p;
-            if (!last) again.summed = false;  // (the segments are others' by now)
-            const Found<double> f = draw(row, lds, again, u);
+            const Found<double> f = draw(row, lds, p, u);
             token = f.at;
             total = f.total;
         }
@@ -932,6 +1180,53 @@ int enqueue(K kernel, int64_t blocks, int threads, void* stream, void* ev0, void
 }
 
 }  // namespace
+
+// Shares of a row by the loads of 16 bytes that it has: 1,024 or more of them where there are as many loads, and not
+// many more, so that their maxima take little beside the row.
+void scan_shape(ScanDev& d, int64_t rows, int64_t vocab, int dtype)
+{
+    const int64_t per_load = dtype == kBF16 ? 8 : 4, chunks = (vocab + per_load - 1) / per_load, segments = (chunks + kWave - 1) / kWave;
+    d.lanes = chunks <= 2048 ? 1 : chunks <= 8192 ? 4 : 16;
+    d.segments = (int32_t)segments;
+    d.shares = (int32_t)(segments * (kWave / d.lanes));
+    // workgroups of one segment a wavefront at least, and about kScanTarget of them
+    const int64_t each = (rows * segments + kScanTarget * kScanWaves - 1) / (kScanTarget * kScanWaves);
+    d.per = (int32_t)(std::max<int64_t>(1, std::min(each, (segments + kScanWaves - 1) / kScanWaves)) * kScanWaves);
+    d.parts = (int32_t)((segments + d.per - 1) / d.per);
+    if (vocab <= kList) d.parts = d.segments = d.shares = 0;
+}
+
+namespace {
+
+template <int DT>
+int scan_rows(const SampleArgs& a, void* st, void* e0, void* e1)
+{
+    const int64_t blocks = (int64_t)a.rows * a.scan.parts;
+    return a.scan.lanes == 1   ? enqueue(k_scan<DT, 1>, blocks, kScanThreads, st, e0, e1, a)
+           : a.scan.lanes == 4 ? enqueue(k_scan<DT, 4>, blocks, kScanThreads, st, e0, e1, a)
+                               : enqueue(k_scan<DT, 16>, blocks, kScanThreads, st, e0, e1, a);
+}
+
+template <int DT>
+int verify_scan_rows(const VerifyArgs& a, void* st, void* e0, void* e1)
+{
+    const int64_t blocks = (int64_t)a.n_seqs * a.ch.max_new * (a.draft.base ? 2 : 1) * a.scan.parts;
+    return a.scan.lanes == 1   ? enqueue(k_verify_scan<DT, 1>, blocks, kScanThreads, st, e0, e1, a)
+           : a.scan.lanes == 4 ? enqueue(k_verify_scan<DT, 4>, blocks, kScanThreads, st, e0, e1, a)
+                               : enqueue(k_verify_scan<DT, 16>, blocks, kScanThreads, st, e0, e1, a);
+}
+
+}  // namespace
+
+int launch_scan(const SampleArgs& a, void* st, void* e0, void* e1)
+{
+    return a.dtype == kBF16 ? scan_rows<kBF16>(a, st, e0, e1) : scan_rows<kF32>(a, st, e0, e1);
+}
+
+int launch_verify_scan(const VerifyArgs& a, void* st, void* e0, void* e1)
+{
+    return a.dtype == kBF16 ? verify_scan_rows<kBF16>(a, st, e0, e1) : verify_scan_rows<kF32>(a, st, e0, e1);
+}
 
 int launch_sample(const SampleArgs& a, void* st, void* e0, void* e1)
 {

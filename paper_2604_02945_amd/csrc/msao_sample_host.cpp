@@ -79,8 +79,41 @@ msao_status check_rows_count(int64_t rows, std::string* err)
     return MSAO_OK;
 }
 
+// Offsets of the arrays that the rows' first reading leaves.
+struct ScanPlan {
+    ScanDev scan;
+    size_t most, sum, of, total;
+};
+ScanPlan scan_plan(int64_t work, int64_t rows, int64_t vocab, int dtype)
+{
+    ScanPlan pl;
+    std::memset(&pl, 0, sizeof pl);
+    scan_shape(pl.scan, work, vocab, dtype);
+    pl.sum = 0;
+    pl.most = pl.sum + align_up((size_t)rows * (size_t)pl.scan.segments * 8, kWsAlign);
+    pl.of = pl.most + align_up((size_t)rows * (size_t)pl.scan.shares * 4, kWsAlign);
+    pl.total = pl.of + align_up((size_t)rows * (size_t)pl.scan.segments * 4, kWsAlign);
+    return pl;
+}
+ScanDev scan_at(const ScanPlan& pl, uint8_t* ws)
+{
+    ScanDev d = pl.scan;
+    if (d.parts > 0) {
+        d.sum = (double*)(ws + pl.sum);
+        d.most = (float*)(ws + pl.most);
+        d.of = (float*)(ws + pl.of);
+    }
+    return d;
+}
+msao_status check_scan(const ScanPlan& pl, int64_t rows, std::string* err)
+{
+    if (rows > 0 && pl.scan.parts > kMaxRows / rows) return fail(err, MSAO_ERR_UNSUPPORTED, "more workgroups than one launch takes");
+    return MSAO_OK;
+}
+
 // Offsets of a verification's workspace arrays.
 struct VerifyPlan {
+    ScanPlan scan;
     size_t token, logprob, yes, total;
     int32_t max_new;
 };
@@ -92,13 +125,19 @@ msao_status verify_plan(const msao_chunk* ch, int32_t n_seqs, int64_t vocab, int
     pl.max_new = std::min(ch->max_new, ch->n_rows);
     if ((int64_t)n_seqs * std::max(pl.max_new, 1) > kMaxRows) return fail(err, MSAO_ERR_UNSUPPORTED, "2^24 rows or more");
     const size_t rows = align_up((size_t)ch->n_rows * 4, kWsAlign);
-    pl.token = 0;
-    pl.logprob = rows;
-    pl.yes = 2 * rows;
-    pl.total = 3 * rows;
+    // (of the drafts' logits too, whether there are any or not)
+    const int64_t items = 2 * (int64_t)n_seqs * pl.max_new;
+    pl.scan = scan_plan(std::min<int64_t>(items, 2 * (int64_t)ch->n_rows), 2 * (int64_t)ch->n_rows, vocab, dtype);
+    MSAO_TRY(check_scan(pl.scan, items, err));
+    pl.token = pl.scan.total;
+    pl.logprob = pl.token + rows;
+    pl.yes = pl.logprob + rows;
+    pl.total = pl.yes + rows;
     return MSAO_OK;
 }
 
+int run_scan(const void* a, void* s, void* e0, void* e1) { return launch_scan(*(const SampleArgs*)a, s, e0, e1); }
+int run_verify_scan(const void* a, void* s, void* e0, void* e1) { return launch_verify_scan(*(const VerifyArgs*)a, s, e0, e1); }
 int run_sample(const void* a, void* s, void* e0, void* e1) { return launch_sample(*(const SampleArgs*)a, s, e0, e1); }
 int run_verify(const void* a, void* s, void* e0, void* e1) { return launch_verify(*(const VerifyArgs*)a, s, e0, e1); }
 int run_join(const void* a, void* s, void* e0, void* e1) { return launch_verify_join(*(const VerifyArgs*)a, s, e0, e1); }
@@ -118,7 +157,9 @@ msao_status msao_sample_workspace(int64_t rows, int64_t vocab, int dtype, size_t
         if (!bytes) return bad(&g_err, "bytes is NULL");
         MSAO_TRY(check_rows_count(rows, &g_err));
         MSAO_TRY(check_vocab(vocab, dtype, &g_err));
-        *bytes = 0;
+        const ScanPlan pl = scan_plan(rows, rows, vocab, dtype);
+        MSAO_TRY(check_scan(pl, rows, &g_err));
+        *bytes = pl.total;
         return MSAO_OK;
     });
 }
@@ -138,9 +179,9 @@ msao_status msao_sample(msao_ctx* ctx, const void* logits, int64_t rows, int64_t
         if (!out) return bad(err, "out is NULL");
         if (rows > 0 && !u) return bad(err, "u is NULL");
         MSAO_TRY(check_words({u, out->token, out->logprob, out->kept}, err));
-        size_t need = 0;
-        MSAO_TRY(msao_sample_workspace(rows, vocab, dtype, &need));
-        MSAO_TRY(check_workspace(workspace, workspace_bytes, need, err));
+        const ScanPlan pl = scan_plan(rows, rows, vocab, dtype);
+        MSAO_TRY(check_scan(pl, rows, err));
+        MSAO_TRY(check_workspace(workspace, workspace_bytes, pl.total, err));
         if (!ctx) return bad(err, "ctx is NULL");
         if (rows == 0) return MSAO_OK;
         a.logits = LogitRows{(const uint8_t*)logits, row_stride * elt_size(dtype)};
@@ -151,7 +192,9 @@ msao_status msao_sample(msao_ctx* ctx, const void* logits, int64_t rows, int64_t
         a.token = out->token;
         a.logprob = out->logprob;
         a.kept = out->kept;
+        a.scan = scan_at(pl, (uint8_t*)workspace);
         DeviceGuard guard(ctx->device);
+        MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_SCAN, stream, run_scan, &a));
         return round_launch(ctx, MSAO_ROUND_KERNEL_SAMPLE, stream, run_sample, &a);
     });
 }
@@ -208,7 +251,9 @@ msao_status msao_verify(msao_ctx* ctx, const msao_chunk* chunk, int32_t n_seqs, 
         a.row_token = (int32_t*)(ws + pl.token);
         a.row_logprob = (float*)(ws + pl.logprob);
         a.row_yes = (int32_t*)(ws + pl.yes);
+        a.scan = scan_at(pl.scan, ws);
         DeviceGuard guard(ctx->device);
+        MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_SCAN, stream, run_verify_scan, &a));
         MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_VERIFY, stream, run_verify, &a));
         return round_launch(ctx, MSAO_ROUND_KERNEL_VERIFY_JOIN, stream, run_join, &a);
     });
