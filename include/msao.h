@@ -713,7 +713,7 @@ msao_status msao_cache_kernel_times(msao_ctx* ctx, float* ms);
 
 /* How a row's distribution is made from its logits x_v, each array device [rows] or NULL
  * (the value in brackets for every row). With m the largest logit and z_v = (x_v - m) /
- * temperature, w_v = exp(z_v) is a token's weight. Tokens are in order by logit, the largest
+ * temperature, w_v = exp(z_v) is a token's weight, and below 2^-1000 no weight. Tokens are in order by logit, the largest
  * first, equal ones by index. Of this order stay
  *   the first top_k (<= 0, or vocab and more: all) [all],
  *   of these the fewest whose weight is at least top_p of theirs, one at least (1 or more,

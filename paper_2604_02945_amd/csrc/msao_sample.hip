@@ -65,31 +65,60 @@ __device__ __forceinline__ float value_of(uint32_t key)
     return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
 }
 
-// 2^(d inv) for d of at most 0: 2^n times a polynomial in d inv - n, which is within 1/2 of 0. The
-// coefficients are those of the interpolation of 2^r at Chebyshev's nodes, with the first one made 1 so that
-// equal logits have the weight 1; off by 3.3e-14 of the value at most. `least` is -1100 / inv: below it, and of
-// -inf, the power is 0.
-__device__ __forceinline__ double exp2_of(double d, double inv, double least)
+// a b + c with c in scalar registers: for a polynomial's constants the compiler takes the form that adds to its own
+// operand, and a move of the constant with it (a scan of 256 rows with sums 54 us, 25 with this).
+__device__ __forceinline__ double fma_constant(double a, double b, double c)
 {
-    d = fmax(d, least);
-    const double t = fma(d, inv, kMagic), r = fma(d, inv, kMagic - t);
-    const int n = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
-    double p = 1.020869083593037e-07;
-    p = fma(p, r, 1.3259646250270451e-06);
-    p = fma(p, r, 1.5252657257186041e-05);
-    p = fma(p, r, 0.00015403433746224196);
-    p = fma(p, r, 0.0013333558230170627);
-    p = fma(p, r, 0.009618129193942167);
-    p = fma(p, r, 0.05550410866444768);
-    p = fma(p, r, 0.240226506956403);
-    p = fma(p, r, 0.69314718055995);
-    p = fma(p, r, 1.0);
-    if (__builtin_expect(n < -1000, 0)) return __builtin_ldexp(p, n);  // (fewer digits, or none)
-    return __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, p) + ((uint64_t)(uint32_t)n << 52));
+    double r;
+    asm("v_fma_f64 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "s"(c));
+    return r;
 }
 
-// log2(e) / T, of an infinite T not quite 0, so that -inf stays without weight.
+// 2^(d inv) for d of at most 0: 2^n times a polynomial in d inv - n, which is within 1/2 of 0. The
+// coefficients are those of the interpolation of 2^r at Chebyshev's nodes, with the first one made 1 so that
+// equal logits have the weight 1; off by 3.3e-14 of the value at most. `least` is -1000 / inv: what lies below
+// it, -inf too, gives 2^-1000. M at a time, so that no step waits for the one before it.
+template <int M>
+__device__ __forceinline__ void exp2_of(double (&d)[M], double inv, double least)
+{
+    double r[M];
+    int n[M];
+#pragma unroll
+    for (int e = 0; e < M; ++e) {
+        d[e] = fmax(d[e], least);
+        const double t = fma(d[e], inv, kMagic);
+        r[e] = fma(d[e], inv, kMagic - t);
+        n[e] = __double2loint(t);  // of -1000 at least: added to the exponent
+        d[e] = fma_constant(r[e], 1.020869083593037e-07, 1.3259646250270451e-06);
+    }
+    auto step = [&](double c) {
+#pragma unroll
+        for (int e = 0; e < M; ++e) d[e] = fma_constant(d[e], r[e], c);
+    };
+    step(1.5252657257186041e-05);
+    step(0.00015403433746224196);
+    step(0.0013333558230170627);
+    step(0.009618129193942167);
+    step(0.05550410866444768);
+    step(0.240226506956403);
+    step(0.69314718055995);
+#pragma unroll
+    for (int e = 0; e < M; ++e) {
+        d[e] = fma(d[e], r[e], 1.0);
+        d[e] = __hiloint2double(__double2hiint(d[e]) + (n[e] << 20), __double2loint(d[e]));
+    }
+}
+__device__ __forceinline__ double exp2_of(double d, double inv, double least)
+{
+    double v[1] = {d};
+    exp2_of(v, inv, least);
+    return v[0];
+}
+
+// log2(e) / T, of an infinite T not quite 0, so that the exponent of -inf is
+// no product of 0 and an infinity.
 __device__ __forceinline__ double inverse_of(float temperature) { return fmax(kLog2e / (double)temperature, 1e-300); }
+constexpr double kLeast = -1000.0;  // exponents below it are no weight
 
 // 16 bytes of a row, widened; what lies past its end, and -inf, is the value that no token has.
 template <int DT>
@@ -216,7 +245,7 @@ __device__ __forceinline__ void scan_segments(const Row<DT>& row, const RowScan&
     constexpr int N = Chunk<DT>::N;
     const int lane = threadIdx.x & (kWave - 1);
     const bool sums = set.sums(row.vocab);
-    const double inv = inverse_of(set.temperature), least = -1100.0 / inv;
+    const double inv = inverse_of(set.temperature), least = kLeast / inv;
 #pragma unroll 1
     for (int s0 = first; s0 < end; s0 += step * kScanAhead) {
         u32x4 w[kScanAhead];
@@ -257,10 +286,17 @@ __device__ __forceinline__ void scan_segments(const Row<DT>& row, const RowScan&
             }
             m = join(m, __shfl_xor(m, 16));
             m = join(m, __shfl_xor(m, 32));
+            // (the largest adds 1: what 2^-1000 of the others does not change)
             double sum = 0.0;
             if (m > -INFINITY) {
 #pragma unroll
-                for (int e = 0; e < N; ++e) sum += exp2_of((double)c.x[e] - (double)m, inv, least);
+                for (int h = 0; h < N; h += 4) {
+                    double w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = (double)c.x[h + e] - (double)m;
+                    exp2_of(w, inv, least);
+                    sum += (w[0] + w[1]) + (w[2] + w[3]);
+                }
             }
             sum = wave_scan(sum);
             if (lane == kWave - 1) {
@@ -302,26 +338,54 @@ __global__ __launch_bounds__(kScanThreads) void k_verify_scan(VerifyArgs a)
 // ---- one row ---------------------------------------------------------------------------
 
 // Scratch that the steps of a row share.
-struct Lds {
+struct Scratch {
     union {
         uint64_t mass[2][kBins];      // a bin's weight in units of 2^-43 and of 2^-86
         uint32_t count[kBins];
-        float light[kBins];
         double segment[kMostSegments];
     };
     uint64_t packed[kList];           // key, and the index' complement: the order of the tokens, upside down
     union {
-        double ranked[kList];
+        struct {
+            double ranked[kList];
+            float ranked_x[kList];
+        };
         int share[kList];
     };
     float list_x[kList];              // tokens by index; what does not stay is -inf
     int list_at[kList];
-    double wave_d[kWaves];
-    int wave_i[kWaves];
-    float wave_f[kWaves];
+    double wave_d[2][kWaves];
+    int wave_i[2][kWaves];
+    float wave_f[2][kWaves];
     double found_d;
     int found_i[3];
     int n;
+};
+
+// A thread's view of it. Sums over the workgroup use two rooms in turn, so that one barrier each is enough: who
+// writes a room again has passed the barrier of the sum between, and with it everybody has read.
+struct Lds {
+    Scratch& s;
+    uint64_t (&mass)[2][kBins];
+    uint32_t (&count)[kBins];
+    double (&segment)[kMostSegments];
+    uint64_t (&packed)[kList];
+    double (&ranked)[kList];
+    float (&ranked_x)[kList];
+    int (&share)[kList];
+    float (&list_x)[kList];
+    int (&list_at)[kList];
+    double& found_d;
+    int (&found_i)[3];
+    int& n;
+    int turn = 0;
+    __device__ __forceinline__ explicit Lds(Scratch& r)
+        : s(r), mass(r.mass), count(r.count), segment(r.segment), packed(r.packed), ranked(r.ranked), ranked_x(r.ranked_x), share(r.share),
+          list_x(r.list_x), list_at(r.list_at), found_d(r.found_d), found_i(r.found_i), n(r.n)
+    {
+    }
+    __device__ __forceinline__ double* room(double) { return s.wave_d[turn ^= 1]; }
+    __device__ __forceinline__ int* room(int) { return s.wave_i[turn ^= 1]; }
 };
 
 // A row's distribution.
@@ -339,23 +403,24 @@ struct Dist {
     double least;     // and (x - m) inv of at least this
     double total;     // of the weights; known where `kept` is or `summed`
     __device__ __forceinline__ double exponent(float x) const { return ((double)x - m) * inv; }
-    __device__ __forceinline__ double power(float x) const { return exp2_of((double)x - m, inv, zero); }
+    __device__ __forceinline__ double power(float x) const
+    {
+        const double by = (double)x - m, p = exp2_of(by, inv, zero);
+        return by >= zero ? p : 0.0;
+    }
     __device__ __forceinline__ bool stays(float x, int v) const
     {
-        return (x > cut || (x == cut && v <= cut_at)) && exponent(x) >= least;
+        return (x > cut || (x == cut && v <= cut_at)) && (least == -INFINITY || exponent(x) >= least);
     }
     __device__ __forceinline__ double weight(float x, int v) const { return stays(x, v) ? power(x) : 0.0; }
 };
-
-__device__ __forceinline__ double* room_of(Lds& lds, double) { return lds.wave_d; }
-__device__ __forceinline__ int* room_of(Lds& lds, int) { return lds.wave_i; }
 
 // Sum over the threads before this one, and the whole. All threads.
 template <typename T>
 __device__ __forceinline__ T block_before(T v, Lds& lds, T& total)
 {
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
-    T* room = room_of(lds, T(0));
+    T* room = lds.room(T(0));
     const T upto = wave_scan(v);
     if (lane == kWave - 1) room[wave] = upto;
     __syncthreads();
@@ -367,7 +432,6 @@ __device__ __forceinline__ T block_before(T v, Lds& lds, T& total)
         before += w < wave ? s : T(0);
         total += s;
     }
-    __syncthreads();
     return before + (upto - v);
 }
 
@@ -557,27 +621,23 @@ struct Shares {
     }
 };
 
-// A value that at least j of the shares' reach and, but for its lower bits, no larger one; -inf where
-// there are fewer.
-__device__ __forceinline__ float reached_by(Lds& lds, const Shares& shares, int j)
+// A value that at least j of the shares' maxima reach and few more: the lower edge of a bin of those between `least`
+// and the largest of them, `most`; -inf where there are fewer.
+__device__ __forceinline__ float reached_by(Lds& lds, const Shares& shares, int j, float least, float most)
 {
-    uint32_t prefix = 0;
-    double above = 0.0;
-#pragma unroll 1
-    for (int shift = 21; shift >= 10; shift -= 11) {
-        clear_bins(lds, false);
-        shares.each([&](int, float x) {
-            const uint32_t k = key_of(x);
-            if (x > -INFINITY && (shift == 21 || k >> 21 == prefix >> 21)) atomicAdd(&lds.count[(k >> shift) & (kBins - 1)], 1u);
-        });
-        __syncthreads();
-        const int b0 = kBins - 1 - 2 * (int)threadIdx.x;
-        const Place p = top_place(lds, (double)lds.count[b0], (double)lds.count[b0 - 1], above, (double)j, false);
-        if (p.at < 0) return -INFINITY;
-        prefix |= (uint32_t)(kBins - 1 - p.at) << shift;
-        above = p.above;
-    }
-    return value_of(prefix);
+    const float scale = (float)(kBins - 1) / (most - least);
+    if (!(scale > 0.0f) || !(scale < 3e38f)) return least < most ? -INFINITY : most;
+    clear_bins(lds, false);
+    shares.each([&](int, float x) {
+        if (x >= least) atomicAdd(&lds.count[min((int)((x - least) * scale), kBins - 1)], 1u);
+    });
+    __syncthreads();
+    const int b0 = kBins - 1 - 2 * (int)threadIdx.x;
+    const Place p = top_place(lds, (double)lds.count[b0], (double)lds.count[b0 - 1], 0.0, (double)j, false);
+    if (p.at < 0) return -INFINITY;
+    // (a little below the edge, by what the bins' numbers round)
+    const float edge = least + (float)(kBins - 1 - p.at) / scale;
+    return edge - 4e-7f * (fabsf(edge) + fabsf(least) + fabsf(most));
 }
 
 // One token more in lds.packed, in no order: their ranks give them one.
@@ -585,6 +645,16 @@ __device__ __forceinline__ void push(Lds& lds, float x, int v)
 {
     const int at = atomicAdd(&lds.n, 1);
     if (at < kList) lds.packed[at] = (uint64_t)key_of(x) << 32 | (uint32_t)~(uint32_t)v;
+}
+
+// The ones of `which` from index v on; few as a rule, and so read again.
+template <int DT>
+__device__ __forceinline__ void push_some(const Row<DT>& row, Lds& lds, uint32_t which, int v)
+{
+    for (; which; which &= which - 1) {
+        const int i = v + __builtin_ctz(which);
+        push(lds, row.value(i), i);
+    }
 }
 
 // The tokens of `bound` and above in LDS: how many, which may be more than there is room for.
@@ -604,9 +674,10 @@ __device__ __forceinline__ int collect(const Row<DT>& row, Lds& lds, const Share
     for (int j = (int)threadIdx.x / lanes; j < total; j += kThreads / lanes) {
         const int chunk = lds.share[j] * lanes + (int)threadIdx.x % lanes;
         const Chunk<DT> c = row.at(chunk);
+        uint32_t which = 0;
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-            if (c.x[e] >= bound && c.x[e] > -INFINITY) push(lds, c.x[e], chunk * N + e);
+        for (int e = 0; e < N; ++e) which |= c.x[e] >= bound && c.x[e] > -INFINITY ? 1u << e : 0u;
+        push_some(row, lds, which, chunk * N);
     }
     __syncthreads();
     const int n = lds.n;
@@ -635,9 +706,11 @@ __device__ __forceinline__ bool rank(Lds& lds, Dist& d, const Settings& set, int
     }
     const float x = value_of((uint32_t)(mine >> 32));
     const int at = (int)~(uint32_t)mine;
-    const double w = there ? d.power(x) : 0.0;
     __syncthreads();  // (lds.share has been read)
-    if (there) lds.ranked[by_key] = w;
+    if (there) {
+        lds.ranked[by_key] = d.power(x);
+        lds.ranked_x[by_key] = x;
+    }
     __syncthreads();
     // thread r has the token of rank r
     bool in = t < n && (double)t < most;
@@ -649,20 +722,18 @@ __device__ __forceinline__ bool rank(Lds& lds, Dist& d, const Settings& set, int
         const double of = target > 0.0 ? target : (double)set.top_p * sum;
         in = in && ((t == 0 && above == 0.0) || before < of);
     }
+    if (set.min_p > 0.0f && !light) in = in && d.exponent(lds.ranked_x[t]) >= fmin(log2((double)set.min_p), 0.0);
     // (all of them a head of the order: their number says which)
     int kept;
     (void)block_before(in ? 1 : 0, lds, kept);
-    const double least = set.min_p > 0.0f && !light ? fmin(log2((double)set.min_p), 0.0) : -INFINITY;
-    const bool stays = there && by_key < kept && d.exponent(x) >= least;
-    (void)block_before(stays ? 1 : 0, lds, kept);
-    (void)block_before(t < kept ? r_w : 0.0, lds, d.total);
-    if (stays && by_key == kept - 1) {
+    (void)block_before(in ? r_w : 0.0, lds, d.total);
+    if (KEEP && there) {
+        lds.list_x[by_index] = by_key < kept ? x : -INFINITY;
+        lds.list_at[by_index] = at;
+    }
+    if (there && by_key == kept - 1) {
         lds.found_d = (double)x;
         lds.found_i[0] = at;
-    }
-    if (KEEP && there) {
-        lds.list_x[by_index] = stays ? x : -INFINITY;
-        lds.list_at[by_index] = at;
     }
     __syncthreads();
     if (kept > 0) {
@@ -675,17 +746,21 @@ __device__ __forceinline__ bool rank(Lds& lds, Dist& d, const Settings& set, int
     return true;
 }
 
-// A long head, of `k` tokens or of the weight `target` (0: by number), of the tokens that stay in d: with its end in d, the sums of
+// A long head, of `k` tokens or of the weight `target` (0: by number) of `whole`, of the tokens that stay in d: with its end in d, the sums of
 // its weights in lds.segment. False, and nothing changed, where the bins do not give its end. `lowest`: a logit that it
 // does not go below.
 template <bool KEEP, int DT>
-__device__ __forceinline__ bool long_head(const Row<DT>& row, Lds& lds, Dist& d, const Settings& set, float lowest, double k, double target)
+__device__ __forceinline__ bool long_head(const Row<DT>& row, Lds& lds, Dist& d, const Settings& set, float lowest, double k, double target, double whole)
 {
     constexpr int N = Row<DT>::N;
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
     const bool by_number = !(target > 0.0);
     const float m = (float)d.m, scale = (float)(kBins - 1) / (m - lowest), inv = (float)d.inv;
     if (!(scale > 0.0f) || !(scale < 3e38f)) return false;
+    // weights in units of which the whole has 2^31 (integers: an addition of floats in LDS takes some three clocks a
+    // lane, and a flat row of 151,936 tokens 190 us)
+    const float unit = by_number ? 0.0f : (float)(2147483648.0 / whole);
+    const double each = by_number ? 1.0 : whole / 2147483648.0;
     // (rounded, but never out of the logits' order)
     auto bin_of = [&](float x) { return min((int)((x - lowest) * scale), kBins - 1); };
     clear_bins(lds, false);
@@ -694,13 +769,12 @@ __device__ __forceinline__ bool long_head(const Row<DT>& row, Lds& lds, Dist& d,
         for (int e = 0; e < N; ++e) {
             if (!(c.x[e] >= lowest) || !d.stays(c.x[e], v + e)) continue;
             const int b = bin_of(c.x[e]);
-            if (by_number) atomicAdd(&lds.count[b], 1u);
-            else atomicAdd(&lds.light[b], __builtin_amdgcn_exp2f((c.x[e] - m) * inv));
+            atomicAdd(&lds.count[b], by_number ? 1u : (uint32_t)fmaf(__builtin_amdgcn_exp2f((c.x[e] - m) * inv), unit, 0.5f));
         }
     });
     __syncthreads();
     const int b0 = kBins - 1 - 2 * (int)threadIdx.x;
-    const double m0 = by_number ? (double)lds.count[b0] : (double)lds.light[b0], m1 = by_number ? (double)lds.count[b0 - 1] : (double)lds.light[b0 - 1];
+    const double m0 = (double)lds.count[b0] * each, m1 = (double)lds.count[b0 - 1] * each;
     // sums of 32-bit weights are off by less than one in 20,000 as a rule; what they give is checked below
     const double goal = by_number ? k : target;
     const Place from = top_place(lds, m0, m1, 0.0, by_number ? goal : goal * (1.0 - 5e-5), false);
@@ -712,15 +786,16 @@ __device__ __forceinline__ bool long_head(const Row<DT>& row, Lds& lds, Dist& d,
     int over = 0;
     row.each([&](int i, int v, const Chunk<DT>& c) {
         double s = 0.0;
+        uint32_t which = 0;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            if (!(c.x[e] >= lowest) || !d.stays(c.x[e], v + e)) continue;
-            const int b = bin_of(c.x[e]);
-            if (b > upper) {
-                s += d.power(c.x[e]);
-                ++over;
-            } else if (b >= lower) push(lds, c.x[e], v + e);
+            const bool in = c.x[e] >= lowest && d.stays(c.x[e], v + e);
+            const int b = in ? bin_of(c.x[e]) : -1;
+            if (b > upper) s += d.power(c.x[e]);
+            over += b > upper ? 1 : 0;
+            which |= b <= upper && b >= lower ? 1u << e : 0u;
         }
+        push_some(row, lds, which, v);
         s = wave_scan(s);
         if (lane == kWave - 1) lds.segment[i * kWaves + wave] = s;
     });
@@ -837,7 +912,7 @@ __device__ __forceinline__ Dist solve(const Row<DT>& row, Lds& lds, const Settin
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
     Dist d;
     d.inv = inverse_of(set.temperature);
-    d.zero = -1100.0 / d.inv;
+    d.zero = kLeast / d.inv;
     d.cut = -INFINITY;
     d.cut_at = -1;
     d.least = -INFINITY;
@@ -848,11 +923,12 @@ __device__ __forceinline__ Dist solve(const Row<DT>& row, Lds& lds, const Settin
     const bool small = row.vocab <= kList;  // every token is ranked: no scan
     const int n_shares = small ? 0 : row.segments * (kWave / lanes);
     const Shares shares(scan.most, n_shares);
-    float mine = -INFINITY;
+    float mine = -INFINITY, low = INFINITY;
     bool bad = false;
     auto look = [&](float x) {
         bad = bad || !(x < INFINITY);
         mine = fmaxf(mine, x);
+        low = x > -INFINITY ? fminf(low, x) : low;
     };
     if (small) {
         const Chunk<DT> c = row.at(threadIdx.x);
@@ -861,11 +937,16 @@ __device__ __forceinline__ Dist solve(const Row<DT>& row, Lds& lds, const Settin
     } else
         shares.each([&](int, float x) { look(x); });
 #pragma unroll
-    for (int s = 1; s < kWave; s <<= 1) mine = fmaxf(mine, __shfl_xor(mine, s));
+    for (int s = 1; s < kWave; s <<= 1) {
+        mine = fmaxf(mine, __shfl_xor(mine, s));
+        low = fminf(low, __shfl_xor(low, s));
+    }
     const bool wave_bad = __ballot(bad) != 0;
+    int* room = lds.room(0);
     if (lane == 0) {
-        lds.wave_f[wave] = mine;
-        lds.wave_i[wave] = wave_bad;
+        lds.s.wave_f[0][wave] = mine;
+        lds.s.wave_f[1][wave] = low;
+        room[wave] = wave_bad;
     }
     if (threadIdx.x == 0) {
         lds.found_i[0] = kNone;
@@ -874,9 +955,11 @@ __device__ __forceinline__ Dist solve(const Row<DT>& row, Lds& lds, const Settin
     __syncthreads();
     float m = mine;
     bool any_bad = false;
+#pragma unroll 4
     for (int w = 0; w < kWaves; ++w) {
-        m = fmaxf(m, lds.wave_f[w]);
-        any_bad = any_bad || lds.wave_i[w] != 0;
+        m = fmaxf(m, lds.s.wave_f[0][w]);
+        low = fminf(low, lds.s.wave_f[1][w]);
+        any_bad = any_bad || room[w] != 0;
     }
     __syncthreads();
     d.none = any_bad || m == -INFINITY;
@@ -928,13 +1011,16 @@ __device__ __forceinline__ Dist solve(const Row<DT>& row, Lds& lds, const Settin
     }
     // a short head: its tokens, or more than there is room for
     const double target = (double)set.top_p * whole;
+    // (of the shares' maxima, those that 2^-100 of the largest weight and more belong to)
+    const float floor = fmaxf(low, fmaxf((float)(d.m - 100.0 / d.inv), kLowest));
     float bound = -INFINITY;
     int n = 0;
     if (small) {
         const Chunk<DT> c = row.at(threadIdx.x);
+        uint32_t which = 0;
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-            if (c.x[e] > -INFINITY) push(lds, c.x[e], (int)threadIdx.x * N + e);
+        for (int e = 0; e < N; ++e) which |= c.x[e] > -INFINITY ? 1u << e : 0u;
+        push_some(row, lds, which, (int)threadIdx.x * N);
         __syncthreads();
         n = lds.n;
         __syncthreads();
@@ -942,17 +1028,18 @@ __device__ __forceinline__ Dist solve(const Row<DT>& row, Lds& lds, const Settin
         bool attempt = true;
         if (by_k) {
             attempt = k <= kList;
-            if (attempt) bound = reached_by(lds, shares, k);
+            if (attempt) bound = reached_by(lds, shares, k, floor, m);
         } else if (sums) {
             attempt = target < (double)kList;  // (no weight is above 1)
-            if (attempt) bound = reached_by(lds, shares, kTryHead);
+            if (attempt) bound = reached_by(lds, shares, kTryHead, floor, m);
         } else {  // min_p alone: the tokens of that weight, and some below it by the rounding of the bound
             bound = (float)(d.m + (log2(fmin((double)set.min_p, 1.0)) - 1e-3) / d.inv);
             bound = bound - fabsf(bound) * 1e-6f;
         }
         if (attempt) n = collect(row, lds, shares, lanes, bound);
     }
-    if (n > 0 && n <= kList && rank<KEEP>(lds, d, set, n, (double)min(k, n), sums ? fmax(target, 1e-300) : 0.0, 0.0, false)) {
+    const bool enough = !by_k || n >= k || !(bound > -INFINITY);  // (or all there are)
+    if (enough && n > 0 && n <= kList && rank<KEEP>(lds, d, set, n, (double)min(k, n), sums ? fmax(target, 1e-300) : 0.0, 0.0, false)) {
         d.listed = KEEP;
         return d;
     }
@@ -970,9 +1057,13 @@ __device__ __forceinline__ Dist solve(const Row<DT>& row, Lds& lds, const Settin
         d.cut = c.x;
     };
     if (by_k) {
-        const float lowest = bound > -INFINITY ? bound : kLowest;
-        if (!long_head<KEEP>(row, lds, d, set, lowest, (double)k, 0.0)) {
-            const Cut c = cut_of<false>(row, lds, d, lowest, (double)k);
+        // (a head of more tokens than are ranked: about the logit that it ends above. Most shares of 16 loads have
+        // a few above the least of their maxima; below 2^-60 of the largest weight there is little to end it)
+        float near = bound;
+        if (k > kList && k <= 2 * n_shares) near = floor;
+        if (!(near > -INFINITY)) near = fmaxf((float)(d.m - 60.0 / d.inv), kLowest);
+        if (!long_head<KEEP>(row, lds, d, set, near, (double)k, 0.0, 0.0)) {
+            const Cut c = cut_of<false>(row, lds, d, kLowest, (double)k);
             if (c.there) narrow(c);
         }
     }
@@ -989,7 +1080,7 @@ __device__ __forceinline__ Dist solve(const Row<DT>& row, Lds& lds, const Settin
         const double share = fmax((1.0 - (double)set.top_p) * whole / (double)row.vocab, 1e-300);
         const double low = d.m + (log2(fmin(share, 1.0)) - 1e-3) / d.inv;
         const float lowest = fmaxf((float)(low - fabs(low) * 1e-6), kLowest);
-        if (!long_head<KEEP>(row, lds, d, set, lowest, 0.0, goal)) {
+        if (!long_head<KEEP>(row, lds, d, set, lowest, 0.0, goal, whole)) {
             const Cut c = cut_of<true>(row, lds, d, lowest, goal);
             if (c.there) narrow(c);
         }
@@ -1059,7 +1150,8 @@ __device__ __forceinline__ float logprob_of(const Row<DT>& row, const Dist& d, i
 template <int DT>
 __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
 {
-    __shared__ Lds lds;
+    __shared__ Scratch scratch;
+    Lds lds(scratch);
     const int r = blockIdx.x;
     const Row<DT> row(a.logits, r, a.vocab);
     const Dist d = solve<true>(row, lds, settings_of(a.set, r), scan_of(a.scan, r), a.scan.lanes);
@@ -1087,7 +1179,8 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
 template <int DT>
 __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a)
 {
-    __shared__ Lds lds;
+    __shared__ Scratch scratch;
+    Lds lds(scratch);
     const int s = blockIdx.x / a.ch.max_new, i = blockIdx.x - s * a.ch.max_new;
     const Rows rows = seq_rows(a.ch, s);
     const int n = min(rows.n, a.ch.max_new);

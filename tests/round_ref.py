@@ -21,7 +21,7 @@ def distribution(x, temperature=None, top_k=None, top_p=None, min_p=None):
         order = order[:top_k]
     with np.errstate(over="ignore", under="ignore"):
         z = (x[order] - x.max()) / t
-        w = np.exp(z)
+        w = np.where(z >= -1000 * math.log(2), np.exp(z), 0.0)
     if top_p is not None and float(top_p) < 1:
         n = 1 + int((np.cumsum(w)[:-1] < float(top_p) * math.fsum(w)).sum())
         order, z, w = order[:n], z[:n], w[:n]
