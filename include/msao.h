@@ -872,14 +872,15 @@ double msao_expected_e2e_latency(const msao_latency_model* m);
 /* And of the kernels of a speculative round, for msao_round_kernel_times. */
 #define MSAO_ROUND_KERNEL_SCAN 0          /* the logits' first reading */
 #define MSAO_ROUND_KERNEL_SAMPLE 1
-#define MSAO_ROUND_KERNEL_VERIFY 2        /* each row's draft and token */
-#define MSAO_ROUND_KERNEL_VERIFY_JOIN 3   /* up to the first draft that does not stand */
-#define MSAO_ROUND_KERNEL_RESIZE 4
-#define MSAO_ROUND_KERNEL_RESIZE_FILL 5   /* its tables and slots where they are many */
-#define MSAO_ROUND_KERNEL_SHARED 6        /* attention over the shared prefixes */
-#define MSAO_ROUND_KERNEL_OWN 7           /* and over each sequence's own tokens */
-#define MSAO_ROUND_KERNEL_SHARED_JOIN 8
-#define MSAO_NUM_ROUND_KERNELS 9
+#define MSAO_ROUND_KERNEL_DISTRIBUTE 2    /* the rows' and the drafts' distributions */
+#define MSAO_ROUND_KERNEL_VERIFY 3        /* each row's draft and token */
+#define MSAO_ROUND_KERNEL_VERIFY_JOIN 4   /* up to the first draft that does not stand */
+#define MSAO_ROUND_KERNEL_RESIZE 5
+#define MSAO_ROUND_KERNEL_RESIZE_FILL 6   /* its tables and slots where they are many */
+#define MSAO_ROUND_KERNEL_SHARED 7        /* attention over the shared prefixes */
+#define MSAO_ROUND_KERNEL_OWN 8           /* and over each sequence's own tokens */
+#define MSAO_ROUND_KERNEL_SHARED_JOIN 9
+#define MSAO_NUM_ROUND_KERNELS 10
 msao_status msao_round_kernel_times(msao_ctx* ctx, float* ms);
 
 /* When enabled, every launch is bracketed by a pair of HIP events recorded on

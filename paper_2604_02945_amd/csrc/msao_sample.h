@@ -56,6 +56,13 @@ struct SampleArgs {
     ScanDev scan;              // workspace
 };
 
+// Of a distribution what weighs a token in it.
+struct Known {
+    double m, inv, zero, least, total;
+    float cut;
+    int32_t cut_at, kept, best, none;
+};
+
 struct VerifyArgs {
     LogitRows logits, draft;   // draft.base NULL: drafts are certain
     SamplingDev set;
@@ -73,12 +80,14 @@ struct VerifyArgs {
     int32_t* row_token;        // the token that follows the row
     float* row_logprob;
     int32_t* row_yes;          // whether it is the row's draft
+    Known* known;              // [2 n_rows], the drafts' ones behind the rows'
     ScanDev scan;
 };
 
 int launch_scan(const SampleArgs& a, void* stream, void* ev0, void* ev1);
 int launch_verify_scan(const VerifyArgs& a, void* stream, void* ev0, void* ev1);
 int launch_sample(const SampleArgs& a, void* stream, void* ev0, void* ev1);
+int launch_distribute(const VerifyArgs& a, void* stream, void* ev0, void* ev1);
 int launch_verify(const VerifyArgs& a, void* stream, void* ev0, void* ev1);
 int launch_verify_join(const VerifyArgs& a, void* stream, void* ev0, void* ev1);
 

@@ -48,7 +48,7 @@ constexpr int kList = kThreads;            // tokens that are ranked in LDS
 constexpr int kTryHead = 256;              // of the shares' maxima, for a head whose length top_p decides
 constexpr int64_t kScanTarget = 2048;      // workgroups of a scan
 constexpr int kScanThreads = 256, kScanWaves = kScanThreads / kWave, kScanAhead = 4;
-constexpr double kMagic = 6755399441055744.0;  // 1.5 2^52: added to a number it leaves its nearest integer in the low word
+constexpr double kMagic = 26388279066624.0;  // 1.5 2^44: a number added to it is rounded to 1 / 256, which is its last digit
 constexpr double kLog2e = 1.4426950408889634074;
 constexpr double kLn2 = 0.69314718055994530942;
 constexpr int kMostSegments = 4096;        // of a row of kMaxVocab float32 logits
@@ -66,7 +66,7 @@ __device__ __forceinline__ float value_of(uint32_t key)
 }
 
 // a b + c with c in scalar registers: for a polynomial's constants the compiler takes the form that adds to its own
-// operand, and a move of the constant with it (a scan of 256 rows with sums 54 us, 25 with this).
+// operand, and a move of the constant with it.
 __device__ __forceinline__ double fma_constant(double a, double b, double c)
 {
     double r;
@@ -74,45 +74,61 @@ __device__ __forceinline__ double fma_constant(double a, double b, double c)
     return r;
 }
 
-// 2^(d inv) for d of at most 0: 2^n times a polynomial in d inv - n, which is within 1/2 of 0. The
-// coefficients are those of the interpolation of 2^r at Chebyshev's nodes, with the first one made 1 so that
-// equal logits have the weight 1; off by 3.3e-14 of the value at most. `least` is -1000 / inv: what lies below
-// it, -inf too, gives 2^-1000. M at a time, so that no step waits for the one before it.
+// 2^(d inv) for d of at most 0: 2^n times 2^(k / 256) from a table times a polynomial of degree 3 in the rest, which is
+// within 1/512 of 0: off by (ln 2 / 512)^4 / 24, 1.4e-13 of the value, and by the table's 3.3e-14; equal logits
+// have the weight 1. `least` is -1000 / inv: what lies below it, -inf too, gives 2^-1000. M at a time, so that no
+// step waits for the one before it. An instruction of 64 bits takes eight clocks a wavefront: a polynomial of degree 9
+// without a table takes 1.5 times as long (a scan of 256 rows with sums 40 us).
+constexpr int kTable = 256;
 template <int M>
-__device__ __forceinline__ void exp2_of(double (&d)[M], double inv, double least)
+__device__ __forceinline__ void exp2_of(const double* table, double (&d)[M], double inv, double least)
 {
-    double r[M];
+    double r[M], w[M];
     int n[M];
 #pragma unroll
     for (int e = 0; e < M; ++e) {
         d[e] = fmax(d[e], least);
-        const double t = fma(d[e], inv, kMagic);
+        const double t = fma(d[e], inv, kMagic);  // in its low word 256 d inv, rounded (an ulp is 1 / 256)
         r[e] = fma(d[e], inv, kMagic - t);
-        n[e] = __double2loint(t);  // of -1000 at least: added to the exponent
-        d[e] = fma_constant(r[e], 1.020869083593037e-07, 1.3259646250270451e-06);
+        n[e] = __double2loint(t);
+        w[e] = table[n[e] & (kTable - 1)];
+        d[e] = fma_constant(r[e], 0.05550410866482158, 0.24022650695910072);  // ln 2^3 / 6, ln 2^2 / 2
     }
-    auto step = [&](double c) {
 #pragma unroll
-        for (int e = 0; e < M; ++e) d[e] = fma_constant(d[e], r[e], c);
-    };
-    step(1.5252657257186041e-05);
-    step(0.00015403433746224196);
-    step(0.0013333558230170627);
-    step(0.009618129193942167);
-    step(0.05550410866444768);
-    step(0.240226506956403);
-    step(0.69314718055995);
+    for (int e = 0; e < M; ++e) d[e] = fma_constant(d[e], r[e], 0.6931471805599453);
 #pragma unroll
     for (int e = 0; e < M; ++e) {
-        d[e] = fma(d[e], r[e], 1.0);
-        d[e] = __hiloint2double(__double2hiint(d[e]) + (n[e] << 20), __double2loint(d[e]));
+        d[e] = fma(w[e] * r[e], d[e], w[e]);
+        // (n of -1000 at least: added to the exponent)
+        d[e] = __hiloint2double(__double2hiint(d[e]) + ((n[e] >> 8) << 20), __double2loint(d[e]));
     }
 }
-__device__ __forceinline__ double exp2_of(double d, double inv, double least)
+__device__ __forceinline__ double exp2_of(const double* table, double d, double inv, double least)
 {
     double v[1] = {d};
-    exp2_of(v, inv, least);
+    exp2_of(table, v, inv, least);
     return v[0];
+}
+
+// The table: 2^r by a polynomial, the interpolation of 2^r at Chebyshev's nodes in [-1/2, 1/2] with the first
+// coefficient made 1, off by 3.3e-14.
+__device__ __forceinline__ void fill_table(double* table)
+{
+    for (int k = threadIdx.x; k < kTable; k += blockDim.x) {
+        const double r = (k < kTable / 2 ? k : k - kTable) * (1.0 / kTable);
+        double p = 1.020869083593037e-07;
+        p = fma(p, r, 1.3259646250270451e-06);
+        p = fma(p, r, 1.5252657257186041e-05);
+        p = fma(p, r, 0.00015403433746224196);
+        p = fma(p, r, 0.0013333558230170627);
+        p = fma(p, r, 0.009618129193942167);
+        p = fma(p, r, 0.05550410866444768);
+        p = fma(p, r, 0.240226506956403);
+        p = fma(p, r, 0.69314718055995);
+        p = fma(p, r, 1.0);
+        table[k] = k < kTable / 2 ? p : 2.0 * p;
+    }
+    __syncthreads();
 }
 
 // log2(e) / T, of an infinite T not quite 0, so that the exponent of -inf is
@@ -144,7 +160,7 @@ struct Chunk {
 // so that (step, wavefront, lane) is the order of the indices. Segment i * kWaves + w is wavefront w's.
 template <int DT>
 struct Row {
-    static constexpr int N = Chunk<DT>::N, kAhead = 4;
+    static constexpr int N = Chunk<DT>::N;
     rsrc_t r;
     int vocab, steps, segments;
     __device__ __forceinline__ Row(const LogitRows& rows, int64_t row, int vocab_) : vocab(vocab_)
@@ -164,8 +180,8 @@ struct Row {
         c.end(vocab - chunk * N);
         return c;
     }
-    // f(step, first index, chunk) for every step
-    template <typename F>
+    // f(step, first index, chunk) for every step, kAhead of which are loaded at a time (two where f takes many registers)
+    template <int kAhead = 4, typename F>
     __device__ __forceinline__ void each(F f) const
     {
         const int t = threadIdx.x, wave_end = (uniform(t >> 6) + 1) * kWave;
@@ -240,7 +256,7 @@ __device__ __forceinline__ T wave_scan(T v)
 
 // Segments s, s + step, .. up to `end` of a row, by one wavefront.
 template <int DT, int SHARE>
-__device__ __forceinline__ void scan_segments(const Row<DT>& row, const RowScan& scan, const Settings& set, int first, int step, int end)
+__device__ __forceinline__ void scan_segments(const double* table, const Row<DT>& row, const RowScan& scan, const Settings& set, int first, int step, int end)
 {
     constexpr int N = Chunk<DT>::N;
     const int lane = threadIdx.x & (kWave - 1);
@@ -294,7 +310,7 @@ __device__ __forceinline__ void scan_segments(const Row<DT>& row, const RowScan&
                     double w[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) w[e] = (double)c.x[h + e] - (double)m;
-                    exp2_of(w, inv, least);
+                    exp2_of(table, w, inv, least);
                     sum += (w[0] + w[1]) + (w[2] + w[3]);
                 }
             }
@@ -310,9 +326,12 @@ __device__ __forceinline__ void scan_segments(const Row<DT>& row, const RowScan&
 template <int DT, int SHARE>
 __device__ __forceinline__ void scan_part(const LogitRows& rows, const ScanDev& scan, const SamplingDev& set, int vocab, int r, int at, int part)
 {
+    __shared__ double table[kTable];
     const Row<DT> row(rows, r, vocab);
     const int wave = uniform(threadIdx.x >> 6), first = part * scan.per;
-    scan_segments<DT, SHARE>(row, scan_of(scan, at), settings_of(set, r), first + wave, kScanWaves, min(first + scan.per, row.segments));
+    const Settings mine = settings_of(set, r);
+    if (mine.sums(vocab)) fill_table(table);
+    scan_segments<DT, SHARE>(table, row, scan_of(scan, at), mine, first + wave, kScanWaves, min(first + scan.per, row.segments));
 }
 
 template <int DT, int SHARE>
@@ -351,12 +370,14 @@ struct Scratch {
             float ranked_x[kList];
         };
         int share[kList];
+        int order[kMostSegments];     // counts of segments
     };
     float list_x[kList];              // tokens by index; what does not stay is -inf
     int list_at[kList];
     double wave_d[2][kWaves];
     int wave_i[2][kWaves];
     float wave_f[2][kWaves];
+    double table[kTable];             // 2^(k / 256)
     double found_d;
     int found_i[3];
     int n;
@@ -373,6 +394,7 @@ struct Lds {
     double (&ranked)[kList];
     float (&ranked_x)[kList];
     int (&share)[kList];
+    int (&order)[kMostSegments];
     float (&list_x)[kList];
     int (&list_at)[kList];
     double& found_d;
@@ -381,7 +403,7 @@ struct Lds {
     int turn = 0;
     __device__ __forceinline__ explicit Lds(Scratch& r)
         : s(r), mass(r.mass), count(r.count), segment(r.segment), packed(r.packed), ranked(r.ranked), ranked_x(r.ranked_x), share(r.share),
-          list_x(r.list_x), list_at(r.list_at), found_d(r.found_d), found_i(r.found_i), n(r.n)
+          order(r.order), list_x(r.list_x), list_at(r.list_at), found_d(r.found_d), found_i(r.found_i), n(r.n)
     {
     }
     __device__ __forceinline__ double* room(double) { return s.wave_d[turn ^= 1]; }
@@ -402,10 +424,11 @@ struct Dist {
     int cut_at;
     double least;     // and (x - m) inv of at least this
     double total;     // of the weights; known where `kept` is or `summed`
+    const double* table;
     __device__ __forceinline__ double exponent(float x) const { return ((double)x - m) * inv; }
     __device__ __forceinline__ double power(float x) const
     {
-        const double by = (double)x - m, p = exp2_of(by, inv, zero);
+        const double by = (double)x - m, p = exp2_of(table, by, inv, zero);
         return by >= zero ? p : 0.0;
     }
     __device__ __forceinline__ bool stays(float x, int v) const
@@ -436,7 +459,7 @@ __device__ __forceinline__ T block_before(T v, Lds& lds, T& total)
 }
 
 __device__ __forceinline__ double* segments_of(Lds& lds, double) { return lds.segment; }
-__device__ __forceinline__ int* segments_of(Lds& lds, int) { return (int*)lds.segment; }
+__device__ __forceinline__ int* segments_of(Lds& lds, int) { return lds.order; }
 
 // The sums of f(x, v) >= 0 over the row's segments, in the order of the indices.
 template <typename T, int DT, typename F>
@@ -445,10 +468,28 @@ __device__ __forceinline__ void sum_segments(const Row<DT>& row, Lds& lds, F f)
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
     T* segment = segments_of(lds, T(0));
     __syncthreads();
-    row.each([&](int i, int v, const Chunk<DT>& c) {
+    row.template each<2>([&](int i, int v, const Chunk<DT>& c) {
         T s = 0;
 #pragma unroll
         for (int e = 0; e < Row<DT>::N; ++e) s += f(c.x[e], v + e);
+        s = wave_scan(s);
+        if (lane == kWave - 1) segment[i * kWaves + wave] = s;
+    });
+    __syncthreads();
+}
+
+// Of f(x, y, v) with y the other row's logit.
+template <typename T, int DT, typename F>
+__device__ __forceinline__ void sum_segments(const Row<DT>& row, Lds& lds, const Row<DT>& other, F f)
+{
+    const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
+    T* segment = segments_of(lds, T(0));
+    __syncthreads();
+    row.template each<2>([&](int i, int v, const Chunk<DT>& c) {
+        const Chunk<DT> o = other.at(i * kThreads + (int)threadIdx.x);
+        T s = 0;
+#pragma unroll
+        for (int e = 0; e < Row<DT>::N; ++e) s += f(c.x[e], o.x[e], v + e);
         s = wave_scan(s);
         if (lane == kWave - 1) segment[i * kWaves + wave] = s;
     });
@@ -685,11 +726,28 @@ __device__ __forceinline__ int collect(const Row<DT>& row, Lds& lds, const Share
     return n;
 }
 
+// Every token of a row of at most kList.
+template <int DT>
+__device__ __forceinline__ int collect_all(const Row<DT>& row, Lds& lds)
+{
+    constexpr int N = Row<DT>::N;
+    const Chunk<DT> c = row.at(threadIdx.x);
+    uint32_t which = 0;
+#pragma unroll
+    for (int e = 0; e < N; ++e) which |= c.x[e] > -INFINITY ? 1u << e : 0u;
+    if (threadIdx.x == 0) lds.n = 0;
+    __syncthreads();
+    push_some(row, lds, which, (int)threadIdx.x * N);
+    __syncthreads();
+    const int n = lds.n;
+    __syncthreads();
+    return n;
+}
+
 // With n tokens in lds.packed, which are what comes in the order behind `before` tokens of the weight `above`: which of
 // them stay of a head of `most` tokens, or of the weight `target` (0: top_p of the n), with min_p. False, and
 // nothing changed, where the head does not end among them. `light`: the head is `most`
 // tokens, whatever top_p and min_p say.
-template <bool KEEP>
 __device__ __forceinline__ bool rank(Lds& lds, Dist& d, const Settings& set, int n, double most, double target, double above, bool light)
 {
     const int t = threadIdx.x;
@@ -727,7 +785,7 @@ __device__ __forceinline__ bool rank(Lds& lds, Dist& d, const Settings& set, int
     int kept;
     (void)block_before(in ? 1 : 0, lds, kept);
     (void)block_before(in ? r_w : 0.0, lds, d.total);
-    if (KEEP && there) {
+    if (there) {
         lds.list_x[by_index] = by_key < kept ? x : -INFINITY;
         lds.list_at[by_index] = at;
     }
@@ -746,10 +804,19 @@ __device__ __forceinline__ bool rank(Lds& lds, Dist& d, const Settings& set, int
     return true;
 }
 
+// A value's place among the ones between lo and hi of a type's keys: bf16 values differ in the upper half of theirs.
+template <int DT>
+struct Keys {
+    static constexpr int kUnit = DT == kBF16 ? 16 : 0;
+    __device__ static __forceinline__ uint32_t of(float x) { return key_of(x) >> kUnit; }
+    // (of a bf16 value the lower half is zeros, of a negative one's key ones)
+    __device__ static __forceinline__ float value(uint32_t k) { return value_of(kUnit && !(k & 0x8000u) ? k << kUnit | 0xFFFFu : k << kUnit); }
+};
+
 // A long head, of `k` tokens or of the weight `target` (0: by number) of `whole`, of the tokens that stay in d: with its end in d, the sums of
 // its weights in lds.segment. False, and nothing changed, where the bins do not give its end. `lowest`: a logit that it
 // does not go below.
-template <bool KEEP, int DT>
+template <int DT>
 __device__ __forceinline__ bool long_head(const Row<DT>& row, Lds& lds, Dist& d, const Settings& set, float lowest, double k, double target, double whole)
 {
     constexpr int N = Row<DT>::N;
@@ -757,20 +824,19 @@ __device__ __forceinline__ bool long_head(const Row<DT>& row, Lds& lds, Dist& d,
     const bool by_number = !(target > 0.0);
     const float m = (float)d.m, scale = (float)(kBins - 1) / (m - lowest), inv = (float)d.inv;
     if (!(scale > 0.0f) || !(scale < 3e38f)) return false;
+    const bool all = !(d.cut > -INFINITY);  // every token of `lowest` and above stays in d
+    // (rounded, but never out of the logits' order)
+    auto bin_of = [&](float x) { return min((int)((x - lowest) * scale), kBins - 1); };
     // weights in units of which the whole has 2^31 (integers: an addition of floats in LDS takes some three clocks a
     // lane, and a flat row of 151,936 tokens 190 us)
     const float unit = by_number ? 0.0f : (float)(2147483648.0 / whole);
     const double each = by_number ? 1.0 : whole / 2147483648.0;
-    // (rounded, but never out of the logits' order)
-    auto bin_of = [&](float x) { return min((int)((x - lowest) * scale), kBins - 1); };
     clear_bins(lds, false);
     row.each([&](int, int v, const Chunk<DT>& c) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            if (!(c.x[e] >= lowest) || !d.stays(c.x[e], v + e)) continue;
-            const int b = bin_of(c.x[e]);
-            atomicAdd(&lds.count[b], by_number ? 1u : (uint32_t)fmaf(__builtin_amdgcn_exp2f((c.x[e] - m) * inv), unit, 0.5f));
-        }
+        for (int e = 0; e < N; ++e)
+            if (c.x[e] >= lowest && (all || d.stays(c.x[e], v + e)))
+                atomicAdd(&lds.count[bin_of(c.x[e])], by_number ? 1u : (uint32_t)fmaf(__builtin_amdgcn_exp2f((c.x[e] - m) * inv), unit, 0.5f));
     });
     __syncthreads();
     const int b0 = kBins - 1 - 2 * (int)threadIdx.x;
@@ -781,21 +847,64 @@ __device__ __forceinline__ bool long_head(const Row<DT>& row, Lds& lds, Dist& d,
     const Place to = by_number ? from : top_place(lds, m0, m1, 0.0, goal * (1.0 + 5e-5), true);
     if (from.at < 0 || to.at < 0) return false;
     const int upper = kBins - 1 - from.at, lower = kBins - 1 - to.at;
+    // about how many tokens lie in these bins
+    auto number_in = [&](int b, double mass) {
+        return b > upper || b < lower || !(mass > 0.0) ? 0.0 : by_number ? mass : mass / fmax(d.power(fminf(lowest + ((float)b + 0.5f) / scale, m)), 1e-300);
+    };
+    double expected;
+    (void)block_before(number_in(b0, m0) + number_in(b0 - 1, m1), lds, expected);
+    // the least logits of the bins `lower` and `upper` + 1, by halves between two keys
+    auto least_of = [&](int bin) {
+        uint32_t a = key_of(lowest), z = key_of(m) + 1;  // (m lies in the last bin)
+        while (a < z) {
+            const uint32_t mid = a + (z - a) / 2;
+            if (bin_of(value_of(mid)) >= bin) z = mid;
+            else a = mid + 1;
+        }
+        return value_of(a);
+    };
+    const float x_lo = least_of(lower), x_hi = upper + 1 < kBins ? least_of(upper + 1) : INFINITY;
+    // more of them than can be ranked are equal ones as a rule: counted by value then
+    uint32_t* const values = (uint32_t*)lds.packed;
+    const bool ranked = expected <= 0.95 * kList;
+    uint32_t lo = 0;
+    if (!ranked) {
+        lo = Keys<DT>::of(x_lo);
+        if (Keys<DT>::of(fminf(x_hi, m)) - lo >= (uint32_t)kBins) return false;
+        static_assert(sizeof(uint64_t) * kList >= 4 * kBins, "");
+        for (int b = threadIdx.x; b < kBins; b += kThreads) values[b] = 0;
+    }
     if (threadIdx.x == 0) lds.n = 0;
     __syncthreads();
     int over = 0;
-    row.each([&](int i, int v, const Chunk<DT>& c) {
+    row.template each<2>([&](int i, int v, const Chunk<DT>& c) {
         double s = 0.0;
         uint32_t which = 0;
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const bool in = c.x[e] >= lowest && d.stays(c.x[e], v + e);
-            const int b = in ? bin_of(c.x[e]) : -1;
-            if (b > upper) s += d.power(c.x[e]);
-            over += b > upper ? 1 : 0;
-            which |= b <= upper && b >= lower ? 1u << e : 0u;
+        for (int h = 0; h < N; h += 4) {
+            double w[4];
+            uint32_t in = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float x = c.x[h + e];
+                const bool some = x >= x_lo && (all || d.stays(x, v + h + e));
+                in |= some && x >= x_hi ? 1u << e : 0u;
+                which |= some && x < x_hi ? 1u << (h + e) : 0u;
+                w[e] = (double)x - d.m;
+            }
+            over += __popc(in);
+            if (in) {
+                exp2_of(d.table, w, d.inv, d.zero);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s += in >> e & 1 ? w[e] : 0.0;
+            }
         }
-        push_some(row, lds, which, v);
+        if (ranked) push_some(row, lds, which, v);
+        else
+            for (; which; which &= which - 1) {
+                const uint32_t at = Keys<DT>::of(row.value(v + __builtin_ctz(which))) - lo;
+                if (at < (uint32_t)kBins) atomicAdd(&values[at], 1u);
+            }
         s = wave_scan(s);
         if (lane == kWave - 1) lds.segment[i * kWaves + wave] = s;
     });
@@ -804,18 +913,61 @@ __device__ __forceinline__ bool long_head(const Row<DT>& row, Lds& lds, Dist& d,
     const double above = sum_of_segments(lds, row.segments);
     int number;
     (void)block_before(over, lds, number);
-    if (n < 1 || n > kList) return false;
     Dist next = d;
+    next.summed = true;
+    next.listed = false;
+    if (!ranked) {
+        if (by_number ? (double)number >= k : above >= target) return false;
+        auto measure = [&](int b) { return by_number || values[b] == 0 ? (double)values[b] : (double)values[b] * d.power(Keys<DT>::value(lo + (uint32_t)b)); };
+        const Place p = top_place(lds, measure(b0), measure(b0 - 1), by_number ? (double)number : above, goal, false);
+        if (p.at < 0) return false;
+        const int bin = kBins - 1 - p.at;
+        const double w = by_number ? 1.0 : d.power(Keys<DT>::value(lo + (uint32_t)bin)), there = (double)values[bin];
+        double some = fmax(ceil((goal - p.above) / w), 1.0);
+        if (some > 1.0 && p.above + (some - 1.0) * w >= goal) some -= 1.0;
+        some = fmin(some, there);
+        next.cut = Keys<DT>::value(lo + (uint32_t)bin);
+        next.cut_at = kNone;
+        if (some < there) {
+            const float x0 = next.cut;
+            next.cut_at = find_in_order<int>(row, lds, [&](float x, int v) { return x == x0 && d.stays(x, v) ? 1 : 0; }, [&](int) { return (int)some - 1; }).at;
+        }
+        // the weights of these bins' tokens that stay join their segments
+        int inside = 0;
+        row.template each<2>([&](int i, int v, const Chunk<DT>& c) {
+            double s = 0.0;
+            bool any = false;
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float x = c.x[e];
+                if (x >= x_lo && x < x_hi && next.stays(x, v + e)) {
+                    s += d.power(x);
+                    any = true;
+                    ++inside;
+                }
+            }
+            if (!__ballot(any)) return;
+            s = wave_scan(s);
+            if (lane == kWave - 1) lds.segment[i * kWaves + wave] += s;
+        });
+        __syncthreads();
+        (void)block_before(inside, lds, next.kept);
+        next.kept += number;
+        next.total = sum_of_segments(lds, row.segments);
+        d = next;
+        return true;
+    }
+    if (n < 1 || n > kList) return false;
     if (by_number) {
         if ((double)number >= k || (double)(number + n) < k) return false;
-        (void)rank<KEEP>(lds, next, set, n, k - (double)number, 0.0, above, true);
+        (void)rank(lds, next, set, n, k - (double)number, 0.0, above, true);
     } else {
         Settings p = set;
         p.min_p = 0.0f;
-        if (!rank<KEEP>(lds, next, p, n, (double)n, target, above, false)) return false;
+        if (!rank(lds, next, p, n, (double)n, target, above, false)) return false;
     }
     // the tokens of these bins that stay join their segments, each segment's in the order of their indices
-    if (KEEP && (int)threadIdx.x < n) {
+    if ((int)threadIdx.x < n) {
         const int t = threadIdx.x;
         auto segment = [&](int i) { return lds.list_at[i] / (kWave * N); };
         const int mine = segment(t);
@@ -829,8 +981,6 @@ __device__ __forceinline__ bool long_head(const Row<DT>& row, Lds& lds, Dist& d,
     __syncthreads();
     next.kept += number;
     next.total += above;
-    next.summed = KEEP;
-    next.listed = false;
     d = next;
     return true;
 }
@@ -846,9 +996,9 @@ struct Cut {
 template <bool MASS, int DT>
 __device__ __forceinline__ Cut cut_of(const Row<DT>& row, Lds& lds, const Dist& d, float lowest, double target)
 {
-    constexpr int N = Row<DT>::N, kUnit = DT == kBF16 ? 16 : 0;  // bf16 values differ in the upper half of their keys
+    constexpr int N = Row<DT>::N;
     constexpr double kHi = 8796093022208.0, kInvHi = 1.0 / kHi;  // 2^43
-    uint32_t lo = key_of(lowest) >> kUnit, hi = key_of((float)d.m) >> kUnit;
+    uint32_t lo = Keys<DT>::of(lowest), hi = Keys<DT>::of((float)d.m);
     double above = 0.0;
     bool first = true;
 #pragma unroll 1
@@ -857,10 +1007,10 @@ __device__ __forceinline__ Cut cut_of(const Row<DT>& row, Lds& lds, const Dist& 
         while ((hi - lo) >> shift >= (uint32_t)kBins) ++shift;
         const bool exact = shift == 0;  // a bin is a value: counting weighs it
         clear_bins(lds, MASS && !exact);
-        row.each([&](int, int v, const Chunk<DT>& c) {
+        row.template each<2>([&](int, int v, const Chunk<DT>& c) {
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                const uint32_t k = key_of(c.x[e]) >> kUnit;
+                const uint32_t k = Keys<DT>::of(c.x[e]);
                 if (k < lo || k > hi || !d.stays(c.x[e], v + e)) continue;
                 const int bin = (int)((k - lo) >> shift);
                 if (MASS && !exact) {
@@ -872,8 +1022,7 @@ __device__ __forceinline__ Cut cut_of(const Row<DT>& row, Lds& lds, const Dist& 
             }
         });
         __syncthreads();
-        // (of a bf16 value the lower half is zeros, of a negative one's key ones)
-        auto value = [&](uint32_t k) { return value_of(kUnit && !(k & 0x8000u) ? k << kUnit | 0xFFFFu : k << kUnit); };
+        auto value = [&](uint32_t k) { return Keys<DT>::value(k); };
         auto measure = [&](int bin) {
             if (!MASS) return (double)lds.count[bin];
             if (!exact) return (double)lds.mass[0][bin] * kInvHi + (double)lds.mass[1][bin] * (kInvHi * kInvHi);
@@ -903,14 +1052,59 @@ __device__ __forceinline__ Cut cut_of(const Row<DT>& row, Lds& lds, const Dist& 
     }
 }
 
-// KEEP: what a pick needs is left in LDS.
-template <bool KEEP, int DT>
+// The segments' sums that the scan left, relative to the row's largest logit.
+template <int DT>
+__device__ __forceinline__ void spread_sums(const Row<DT>& row, Lds& lds, const RowScan& scan, const Dist& d)
+{
+    __syncthreads();
+    for (int s = threadIdx.x; s < row.segments; s += kThreads) {
+        const float of = scan.of[s];
+        lds.segment[s] = of > -INFINITY ? scan.sum[s] * d.power(of) : 0.0;
+    }
+    __syncthreads();
+}
+
+// One segment's sum of f(x, v).
+template <int DT, typename F>
+__device__ __forceinline__ void sum_again(const Row<DT>& row, Lds& lds, int segment, F f)
+{
+    constexpr int N = Row<DT>::N;
+    const int lane = threadIdx.x & (kWave - 1);
+    if ((int)threadIdx.x < kWave) {
+        const int chunk = segment * kWave + lane;
+        const Chunk<DT> c = row.at(chunk);
+        double s = 0.0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) s += f(c.x[e], chunk * N + e);
+        s = wave_scan(s);
+        if (lane == kWave - 1) lds.segment[segment] = s;
+    }
+    __syncthreads();
+}
+
+// The segments' sums of the weights, the whole and the number, of a distribution that has none of them.
+template <int DT>
+__device__ __forceinline__ void weigh_again(const Row<DT>& row, Lds& lds, Dist& d)
+{
+    int stay = 0;
+    sum_segments<double>(row, lds, [&](float x, int v) {
+        if (!d.stays(x, v)) return 0.0;
+        ++stay;
+        return d.power(x);
+    });
+    d.total = sum_of_segments(lds, row.segments);
+    (void)block_before(stay, lds, d.kept);
+    d.summed = true;
+}
+
+template <int DT>
 __device__ __forceinline__ Dist solve(const Row<DT>& row, Lds& lds, const Settings& set, const RowScan& scan, int lanes)
 {
     constexpr int N = Row<DT>::N;
     constexpr float kLowest = -3.402823466e38f;
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
     Dist d;
+    d.table = lds.s.table;
     d.inv = inverse_of(set.temperature);
     d.zero = kLeast / d.inv;
     d.cut = -INFINITY;
@@ -997,11 +1191,7 @@ __device__ __forceinline__ Dist solve(const Row<DT>& row, Lds& lds, const Settin
     const int k = by_k ? set.top_k : row.vocab;
     double whole = 0.0;
     if (sums) {
-        for (int s = threadIdx.x; s < row.segments; s += kThreads) {
-            const float of = scan.of[s];
-            lds.segment[s] = of > -INFINITY ? scan.sum[s] * d.power(of) : 0.0;
-        }
-        __syncthreads();
+        spread_sums(row, lds, scan, d);
         whole = sum_of_segments(lds, row.segments);
         if (!(set.top_p < 1.0f)) {
             d.summed = true;
@@ -1016,14 +1206,7 @@ __device__ __forceinline__ Dist solve(const Row<DT>& row, Lds& lds, const Settin
     float bound = -INFINITY;
     int n = 0;
     if (small) {
-        const Chunk<DT> c = row.at(threadIdx.x);
-        uint32_t which = 0;
-#pragma unroll
-        for (int e = 0; e < N; ++e) which |= c.x[e] > -INFINITY ? 1u << e : 0u;
-        push_some(row, lds, which, (int)threadIdx.x * N);
-        __syncthreads();
-        n = lds.n;
-        __syncthreads();
+        n = collect_all(row, lds);
     } else {
         bool attempt = true;
         if (by_k) {
@@ -1039,8 +1222,8 @@ __device__ __forceinline__ Dist solve(const Row<DT>& row, Lds& lds, const Settin
         if (attempt) n = collect(row, lds, shares, lanes, bound);
     }
     const bool enough = !by_k || n >= k || !(bound > -INFINITY);  // (or all there are)
-    if (enough && n > 0 && n <= kList && rank<KEEP>(lds, d, set, n, (double)min(k, n), sums ? fmax(target, 1e-300) : 0.0, 0.0, false)) {
-        d.listed = KEEP;
+    if (enough && n > 0 && n <= kList && rank(lds, d, set, n, (double)min(k, n), sums ? fmax(target, 1e-300) : 0.0, 0.0, false)) {
+        d.listed = true;
         return d;
     }
     __syncthreads();
@@ -1062,33 +1245,33 @@ __device__ __forceinline__ Dist solve(const Row<DT>& row, Lds& lds, const Settin
         float near = bound;
         if (k > kList && k <= 2 * n_shares) near = floor;
         if (!(near > -INFINITY)) near = fmaxf((float)(d.m - 60.0 / d.inv), kLowest);
-        if (!long_head<KEEP>(row, lds, d, set, near, (double)k, 0.0, 0.0)) {
+        if (!long_head(row, lds, d, set, near, (double)k, 0.0, 0.0)) {
             const Cut c = cut_of<false>(row, lds, d, kLowest, (double)k);
             if (c.there) narrow(c);
         }
     }
+    if (set.top_p < 1.0f && !sums) {
+        if (d.kept < 0) weigh_again(row, lds, d);
+        whole = d.total;
+    }
+    const double goal = fmax((double)set.top_p * whole, 1e-300);
+    if (set.min_p > 0.0f) {  // what it leaves is all that stays, if that weighs less than top_p's head: else it leaves that head
+        Dist t = d;
+        t.least = fmin(log2((double)set.min_p), 0.0);
+        weigh_again(row, lds, t);
+        if (!(set.top_p < 1.0f) || t.total < goal) return t;
+        d.summed = false;
+    }
     if (set.top_p < 1.0f) {
-        if (!sums) {
-            if (d.kept < 0) {
-                sum_segments<double>(row, lds, [&](float x, int v) { return d.weight(x, v); });
-                whole = sum_of_segments(lds, row.segments);
-            } else whole = d.total;
-        }
-        const double goal = fmax((double)set.top_p * whole, 1e-300);
         // the tokens below a (1 - top_p) / vocab of the whole are less than (1 - top_p) of it together; at
         // least the first stays
         const double share = fmax((1.0 - (double)set.top_p) * whole / (double)row.vocab, 1e-300);
         const double low = d.m + (log2(fmin(share, 1.0)) - 1e-3) / d.inv;
         const float lowest = fmaxf((float)(low - fabs(low) * 1e-6), kLowest);
-        if (!long_head<KEEP>(row, lds, d, set, lowest, 0.0, goal, whole)) {
+        if (!long_head(row, lds, d, set, lowest, 0.0, goal, whole)) {
             const Cut c = cut_of<true>(row, lds, d, lowest, goal);
             if (c.there) narrow(c);
         }
-    }
-    if (set.min_p > 0.0f) {
-        d.least = fmin(log2((double)set.min_p), 0.0);
-        d.kept = -1;
-        d.summed = false;
     }
     return d;
 }
@@ -1096,12 +1279,10 @@ __device__ __forceinline__ Dist solve(const Row<DT>& row, Lds& lds, const Settin
 // u as the running sum's target: [0, 1), NaN as 0.
 __device__ __forceinline__ double drawn(float u, double total) { return (u > 0.0f ? (double)u : 0.0) * total; }
 
-// The first token whose running sum of f(x, v) >= 0, 0 of a token that does not stay, passes u times the
-// whole; -1 where nothing is.
-template <int DT, typename F>
-__device__ __forceinline__ Found<double> pick(const Row<DT>& row, Lds& lds, const Dist& d, float u, F f)
+// Of the list, the first token whose running sum of f(x, v) >= 0 passes u times the whole; -1 where nothing is.
+template <typename F>
+__device__ __forceinline__ Found<double> pick_listed(Lds& lds, const Dist& d, float u, F f)
 {
-    if (!d.listed) return find_in_order<double>(row, lds, f, [&](double total) { return drawn(u, total); });
     const int t = threadIdx.x, lane = t & (kWave - 1);
     const float x = t < d.n ? lds.list_x[t] : -INFINITY;
     const double w = x > -INFINITY ? f(x, lds.list_at[t]) : 0.0;
@@ -1121,30 +1302,21 @@ __device__ __forceinline__ Found<double> pick(const Row<DT>& row, Lds& lds, cons
     return out;
 }
 
-// A token of the distribution, with the weights' sum.
+// A token of a distribution that is listed, summed or one token.
 template <int DT>
-__device__ __forceinline__ Found<double> draw(const Row<DT>& row, Lds& lds, const Dist& d, float u)
+__device__ __forceinline__ int draw(const Row<DT>& row, Lds& lds, const Dist& d, float u)
 {
-    if (d.best >= 0) return Found<double>{d.best, 1.0};
+    if (d.best >= 0) return d.best;
     auto weight = [&](float x, int v) { return d.weight(x, v); };
-    if (d.summed) return locate<double>(row, lds, weight, [&](double total) { return drawn(u, total); });
-    return pick(row, lds, d, u, weight);
-}
-
-// The weights' sum alone.
-template <int DT>
-__device__ __forceinline__ double whole_of(const Row<DT>& row, Lds& lds, const Dist& d)
-{
-    if (d.kept >= 0 || d.summed) return d.total;
-    sum_segments<double>(row, lds, [&](float x, int v) { return d.weight(x, v); });
-    return sum_of_segments(lds, row.segments);
+    if (d.listed) return pick_listed(lds, d, u, weight).at;
+    return locate<double>(row, lds, weight, [&](double total) { return drawn(u, total); }).at;
 }
 
 // ln p of token v.
 template <int DT>
-__device__ __forceinline__ float logprob_of(const Row<DT>& row, const Dist& d, int v, double total)
+__device__ __forceinline__ float logprob_of(const Row<DT>& row, const Dist& d, int v)
 {
-    return (float)((d.exponent(row.value(v)) - log2(total)) * kLn2);
+    return (float)((d.exponent(row.value(v)) - log2(d.total)) * kLn2);
 }
 
 template <int DT>
@@ -1152,15 +1324,16 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
 {
     __shared__ Scratch scratch;
     Lds lds(scratch);
+    fill_table(scratch.table);
     const int r = blockIdx.x;
     const Row<DT> row(a.logits, r, a.vocab);
-    const Dist d = solve<true>(row, lds, settings_of(a.set, r), scan_of(a.scan, r), a.scan.lanes);
-    Found<double> f{-1, 0.0};
-    int kept = 0;
+    Dist d = solve(row, lds, settings_of(a.set, r), scan_of(a.scan, r), a.scan.lanes);
+    int token = -1, kept = 0;
     if (!d.none) {
-        f = draw(row, lds, d, a.u[r]);
+        if (d.kept < 0 && !d.summed) weigh_again(row, lds, d);
+        token = draw(row, lds, d, a.u[r]);
         kept = d.kept;
-        if (a.kept && kept < 0) {
+        if (a.kept && kept < 0) {  // (every one above -inf)
             int n = 0;
             row.each([&](int, int v, const Chunk<DT>& c) {
 #pragma unroll
@@ -1170,9 +1343,46 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
         }
     }
     if (threadIdx.x != 0) return;
-    if (a.token) a.token[r] = f.at;
+    if (a.token) a.token[r] = token;
     if (a.kept) a.kept[r] = kept;
-    if (a.logprob) a.logprob[r] = f.at < 0 ? __builtin_nanf("") : logprob_of(row, d, f.at, f.total);
+    if (a.logprob) a.logprob[r] = token < 0 ? __builtin_nanf("") : logprob_of(row, d, token);
+}
+
+// The distributions of a verification, the rows' and the drafts' ones side by side: of each what weighs a token.
+template <int DT>
+__global__ __launch_bounds__(kThreads) void k_distribute(VerifyArgs a)
+{
+    __shared__ Scratch scratch;
+    Lds lds(scratch);
+    fill_table(scratch.table);
+    const int pairs = a.n_seqs * a.ch.max_new, which = (int)blockIdx.x >= pairs ? 1 : 0;
+    const int s = ((int)blockIdx.x - which * pairs) / a.ch.max_new, i = (int)blockIdx.x - which * pairs - s * a.ch.max_new;
+    const Rows rows = seq_rows(a.ch, s);
+    if (i >= min(rows.n, a.ch.max_new) - which) return;
+    const int r = rows.begin + i, at = which * a.ch.n_rows + r;
+    const Row<DT> row(which ? a.draft : a.logits, r, a.vocab);
+    Dist d = solve(row, lds, settings_of(a.set, r), scan_of(a.scan, at), a.scan.lanes);
+    if (!d.none && d.kept < 0 && !d.summed) weigh_again(row, lds, d);
+    if (threadIdx.x == 0) a.known[at] = Known{d.m, d.inv, d.zero, d.least, d.total, d.cut, d.cut_at, d.kept, d.best, d.none ? 1 : 0};
+}
+
+__device__ __forceinline__ Dist known_of(const Known& k, const double* table)
+{
+    Dist d;
+    d.none = k.none != 0;
+    d.listed = d.summed = false;
+    d.best = k.best;
+    d.kept = k.kept;
+    d.n = 0;
+    d.m = k.m;
+    d.inv = k.inv;
+    d.zero = k.zero;
+    d.cut = k.cut;
+    d.cut_at = k.cut_at;
+    d.least = k.least;
+    d.total = k.total;
+    d.table = table;
+    return d;
 }
 
 // Row i of sequence s: whether its draft stands, and the token that follows it.
@@ -1181,61 +1391,70 @@ __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a)
 {
     __shared__ Scratch scratch;
     Lds lds(scratch);
+    fill_table(scratch.table);
     const int s = blockIdx.x / a.ch.max_new, i = blockIdx.x - s * a.ch.max_new;
     const Rows rows = seq_rows(a.ch, s);
     const int n = min(rows.n, a.ch.max_new);
     if (i >= n) return;
     const int r = rows.begin + i;
-    const bool last = i == n - 1;
-    const Row<DT> row(a.logits, r, a.vocab);
-    const Settings set = settings_of(a.set, r);
-    Dist p = solve<true>(row, lds, set, scan_of(a.scan, r), a.scan.lanes);
+    const bool last = i == n - 1, has_draft = a.draft.base && !last;
+    const Row<DT> row(a.logits, r, a.vocab), other(has_draft ? a.draft : a.logits, r, a.vocab);
+    Dist p = known_of(a.known[r], scratch.table);
     int token = -1;
     bool yes = false;
-    double total = 1.0;
     if (!p.none) {
-        const float u = a.u[r];
-        if (!last) {
-            const int draft = a.tokens[r + 1];
-            const bool known = draft >= 0 && draft < a.vocab;
-            const double wd = known ? p.weight(row.value(draft), draft) : 0.0;
+        const int draft = last ? -1 : a.tokens[r + 1];
+        const Dist q = known_of(a.known[has_draft ? a.ch.n_rows + r : r], scratch.table);
+        const bool certain = !has_draft || q.none;
+        const double qt = certain ? 1.0 : q.total;
+        if (draft >= 0 && draft < a.vocab) {
             const double ua = a.u_accept[r] > 0.0f ? (double)a.u_accept[r] : 0.0;
-            total = whole_of(row, lds, p);
-            bool certain = a.draft.base == nullptr;
-            if (!certain) {
-                const Row<DT> other(a.draft, r, a.vocab);
-                const Dist q = solve<false>(other, lds, set, scan_of(a.scan, a.ch.n_rows + r), a.scan.lanes);
-                certain = q.none;
-                p.summed = false;  // (the segments are q's by now)
-                if (!certain) {
-                    const double qt = whole_of(other, lds, q), qd = known ? q.weight(other.value(draft), draft) : 0.0;
-                    yes = ua * qd * total < wd * qt;
-                    if (!yes)  // what p has more than q
-                        token = pick(row, lds, p, u, [&](float x, int v) {
-                            const double w = p.weight(x, v);
-                            return w > 0.0 ? fmax(w * qt - q.weight(other.value(v), v) * total, 0.0) : 0.0;
-                        }).at;
-                }
-            }
-            if (certain) {
-                yes = ua * total < wd;
-                if (!yes) {
-                    token = pick(row, lds, p, u, [&](float x, int v) { return v == draft ? 0.0 : p.weight(x, v); }).at;
-                    p.summed = false;
-                }
-            }
-            if (yes) token = draft;
+            const double qd = certain ? 1.0 : q.weight(other.value(draft), draft);
+            yes = ua * qd * p.total < p.weight(row.value(draft), draft) * qt;
         }
-        if (token < 0) {
-            const Found<double> f = draw(row, lds, p, u);
-            token = f.at;
-            total = f.total;
+        if (yes) token = draft;
+        else {
+            const float u = a.u[r];
+            // what p has more than q, of the last row p itself
+            auto more = [&](float x, float y, int v) {
+                const double w = p.weight(x, v);
+                if (last || certain) return v == draft ? 0.0 : w;
+                return w > 0.0 ? fmax(w * qt - q.weight(y, v) * p.total, 0.0) : 0.0;
+            };
+            auto one = [&](float x, int v) { return more(x, last || certain ? 0.0f : other.value(v), v); };
+            auto weight = [&](float x, int v) { return p.weight(x, v); };
+            // few tokens are listed again; of more the row is read
+            bool listed = false;
+            if (p.kept > 0 && p.kept <= kList && p.best < 0) {
+                int m;
+                if (a.vocab <= kList) m = collect_all(row, lds);
+                else {
+                    const RowScan scan = scan_of(a.scan, r);
+                    m = collect(row, lds, Shares(scan.most, a.scan.shares), a.scan.lanes, p.cut);
+                }
+                listed = m > 0 && m <= kList;
+                if (listed) (void)rank(lds, p, Settings{1.0f, 1.0f, 0.0f, 0}, m, (double)p.kept, 0.0, 0.0, true);
+            }
+            if (p.best >= 0) token = p.best == draft ? -1 : p.best;
+            else if (listed) token = pick_listed(lds, p, u, one).at;
+            else {
+                if (p.kept < 0 && (last || certain)) {  // every token stays: the segments' sums are known, but for the draft's
+                    spread_sums(row, lds, scan_of(a.scan, r), p);
+                    if (draft >= 0 && draft < a.vocab) sum_again(row, lds, draft / (kWave * Row<DT>::N), one);
+                } else sum_segments<double>(row, lds, other, more);
+                token = locate<double>(row, lds, one, [&](double t) { return drawn(u, t); }).at;
+            }
+            if (token < 0) {  // (nothing more)
+                if (p.best >= 0) token = p.best;
+                else if (listed) token = pick_listed(lds, p, u, weight).at;
+                else token = find_in_order<double>(row, lds, weight, [&](double t) { return drawn(u, t); }).at;
+            }
         }
     }
     if (threadIdx.x != 0) return;
     a.row_token[r] = token;
     a.row_yes[r] = yes ? 1 : 0;
-    a.row_logprob[r] = token < 0 ? __builtin_nanf("") : logprob_of(row, p, token, total);
+    a.row_logprob[r] = token < 0 ? __builtin_nanf("") : logprob_of(row, p, token);
 }
 
 // A sequence's drafts stand up to the first that does not; a wavefront a sequence.
@@ -1325,6 +1544,13 @@ int launch_sample(const SampleArgs& a, void* st, void* e0, void* e1)
 {
     return a.dtype == kBF16 ? enqueue(k_sample<kBF16>, a.rows, kThreads, st, e0, e1, a)
                             : enqueue(k_sample<kF32>, a.rows, kThreads, st, e0, e1, a);
+}
+
+int launch_distribute(const VerifyArgs& a, void* st, void* e0, void* e1)
+{
+    const int64_t blocks = (int64_t)a.n_seqs * a.ch.max_new * (a.draft.base ? 2 : 1);
+    return a.dtype == kBF16 ? enqueue(k_distribute<kBF16>, blocks, kThreads, st, e0, e1, a)
+                            : enqueue(k_distribute<kF32>, blocks, kThreads, st, e0, e1, a);
 }
 
 int launch_verify(const VerifyArgs& a, void* st, void* e0, void* e1)

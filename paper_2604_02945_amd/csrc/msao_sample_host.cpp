@@ -114,7 +114,7 @@ msao_status check_scan(const ScanPlan& pl, int64_t rows, std::string* err)
 // Offsets of a verification's workspace arrays.
 struct VerifyPlan {
     ScanPlan scan;
-    size_t token, logprob, yes, total;
+    size_t token, logprob, yes, known, total;
     int32_t max_new;
 };
 msao_status verify_plan(const msao_chunk* ch, int32_t n_seqs, int64_t vocab, int dtype, VerifyPlan& pl, std::string* err)
@@ -132,13 +132,15 @@ msao_status verify_plan(const msao_chunk* ch, int32_t n_seqs, int64_t vocab, int
     pl.token = pl.scan.total;
     pl.logprob = pl.token + rows;
     pl.yes = pl.logprob + rows;
-    pl.total = pl.yes + rows;
+    pl.known = pl.yes + rows;
+    pl.total = pl.known + align_up(2 * (size_t)ch->n_rows * sizeof(Known), kWsAlign);
     return MSAO_OK;
 }
 
 int run_scan(const void* a, void* s, void* e0, void* e1) { return launch_scan(*(const SampleArgs*)a, s, e0, e1); }
 int run_verify_scan(const void* a, void* s, void* e0, void* e1) { return launch_verify_scan(*(const VerifyArgs*)a, s, e0, e1); }
 int run_sample(const void* a, void* s, void* e0, void* e1) { return launch_sample(*(const SampleArgs*)a, s, e0, e1); }
+int run_distribute(const void* a, void* s, void* e0, void* e1) { return launch_distribute(*(const VerifyArgs*)a, s, e0, e1); }
 int run_verify(const void* a, void* s, void* e0, void* e1) { return launch_verify(*(const VerifyArgs*)a, s, e0, e1); }
 int run_join(const void* a, void* s, void* e0, void* e1) { return launch_verify_join(*(const VerifyArgs*)a, s, e0, e1); }
 
@@ -251,9 +253,11 @@ msao_status msao_verify(msao_ctx* ctx, const msao_chunk* chunk, int32_t n_seqs, 
         a.row_token = (int32_t*)(ws + pl.token);
         a.row_logprob = (float*)(ws + pl.logprob);
         a.row_yes = (int32_t*)(ws + pl.yes);
+        a.known = (Known*)(ws + pl.known);
         a.scan = scan_at(pl.scan, ws);
         DeviceGuard guard(ctx->device);
         MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_SCAN, stream, run_verify_scan, &a));
+        MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_DISTRIBUTE, stream, run_distribute, &a));
         MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_VERIFY, stream, run_verify, &a));
         return round_launch(ctx, MSAO_ROUND_KERNEL_VERIFY_JOIN, stream, run_join, &a);
     });
