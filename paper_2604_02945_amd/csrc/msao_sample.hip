@@ -15,7 +15,7 @@
 //  - without top_k, top_p and min_p the segments' sums say in which one the token lies;
 //  - the head of the order is mostly short. The j-th largest of the shares' maxima is a bound
 //    that j tokens at least reach and few more, and only shares whose maximum reaches it are
-//    read again. Up to 1,024 such tokens are ranked in LDS, by comparing each with each;
+//    read again. Up to 1,024 such tokens are sorted;
 //  - a longer head is found by 2,048 bins that are even in the logit, between the largest one and one
 //    below which too little weight lies: 32-bit sums say which bins the head may end in, then
 //    one reading sums the weights above them in 64 bits and collects the tokens in them, which
@@ -365,14 +365,10 @@ struct Scratch {
     };
     uint64_t packed[kList];           // key, and the index' complement: the order of the tokens, upside down
     union {
-        struct {
-            double ranked[kList];
-            float ranked_x[kList];
-        };
         int share[kList];
         int order[kMostSegments];     // counts of segments
     };
-    float list_x[kList];              // tokens by index; what does not stay is -inf
+    float list_x[kList];              // tokens that stay, by index
     int list_at[kList];
     double wave_d[2][kWaves];
     int wave_i[2][kWaves];
@@ -391,8 +387,6 @@ struct Lds {
     uint32_t (&count)[kBins];
     double (&segment)[kMostSegments];
     uint64_t (&packed)[kList];
-    double (&ranked)[kList];
-    float (&ranked_x)[kList];
     int (&share)[kList];
     int (&order)[kMostSegments];
     float (&list_x)[kList];
@@ -402,7 +396,7 @@ struct Lds {
     int& n;
     int turn = 0;
     __device__ __forceinline__ explicit Lds(Scratch& r)
-        : s(r), mass(r.mass), count(r.count), segment(r.segment), packed(r.packed), ranked(r.ranked), ranked_x(r.ranked_x), share(r.share),
+        : s(r), mass(r.mass), count(r.count), segment(r.segment), packed(r.packed), share(r.share),
           order(r.order), list_x(r.list_x), list_at(r.list_at), found_d(r.found_d), found_i(r.found_i), n(r.n)
     {
     }
@@ -744,62 +738,91 @@ __device__ __forceinline__ int collect_all(const Row<DT>& row, Lds& lds)
     return n;
 }
 
-// With n tokens in lds.packed, which are what comes in the order behind `before` tokens of the weight `above`: which of
-// them stay of a head of `most` tokens, or of the weight `target` (0: top_p of the n), with min_p. False, and
-// nothing changed, where the head does not end among them. `light`: the head is `most`
+// The values of threads 0 .. n-1 (above 0, all different; the others' count as 0) in descending order, one a thread. Few
+// are compared each with each (50 tokens: a row 14.5 us, 19 by sorting; 430: 36, 34; 1,000: 45 more). More by a bitonic
+// sort of as many as the next power of two: partners in a wavefront exchange by shuffles, others through LDS. All threads.
+constexpr int kCompared = 256;
+__device__ __forceinline__ uint64_t sorted(Lds& lds, uint64_t v, int n)
+{
+    const int t = threadIdx.x;
+    if (n <= kCompared) {
+        __syncthreads();
+        if (t < n) lds.packed[t] = v;
+        __syncthreads();
+        int place = 0;
+        if (uniform(t & ~(kWave - 1)) < n) {
+#pragma unroll 4
+            for (int j = 0; j < n; ++j) place += lds.packed[j] > v ? 1 : 0;
+        }
+        __syncthreads();
+        if (t < n) lds.packed[place] = v;
+        __syncthreads();
+        return t < n ? lds.packed[t] : 0;
+    }
+    int size = 2;
+    while (size < n) size <<= 1;
+    if (t >= n) v = 0;
+#pragma unroll 1
+    for (int k = 2; k <= size; k <<= 1) {
+#pragma unroll 1
+        for (int j = k >> 1; j > 0; j >>= 1) {
+            uint64_t o;
+            if (j < kWave) o = __shfl_xor(v, j);
+            else {
+                __syncthreads();
+                lds.packed[t] = v;
+                __syncthreads();
+                o = lds.packed[t ^ j];
+            }
+            // the upper part of a descending pair, the lower part of an ascending one, keeps the larger
+            const bool larger = ((t & j) == 0) == ((t & k) == 0);
+            v = (o > v) == larger ? o : v;
+        }
+    }
+    return v;
+}
+
+// With n tokens in lds.packed, which are what comes in the order behind others of the weight `above`: which of
+// them stay of a head of `most` tokens, or of the weight `target` (0: top_p of the n), with min_p. They are left in the
+// list. False, and nothing changed, where the head does not end among them. `light`: the head is `most`
 // tokens, whatever top_p and min_p say.
 __device__ __forceinline__ bool rank(Lds& lds, Dist& d, const Settings& set, int n, double most, double target, double above, bool light)
 {
     const int t = threadIdx.x;
-    const bool there = t < n;
-    const uint64_t mine = there ? lds.packed[t] : 0;
-    int by_key = 0, by_index = 0;
-    if (uniform(t & ~(kWave - 1)) < n) {
-#pragma unroll 4
-        for (int j = 0; j < n; ++j) {
-            const uint64_t a = lds.packed[j];
-            by_key += a > mine ? 1 : 0;
-            by_index += (uint32_t)a > (uint32_t)mine ? 1 : 0;
-        }
-    }
-    const float x = value_of((uint32_t)(mine >> 32));
-    const int at = (int)~(uint32_t)mine;
-    __syncthreads();  // (lds.share has been read)
-    if (there) {
-        lds.ranked[by_key] = d.power(x);
-        lds.ranked_x[by_key] = x;
-    }
-    __syncthreads();
+    uint64_t mine = t < n ? lds.packed[t] : 0;
+    mine = sorted(lds, mine, n);
     // thread r has the token of rank r
+    const float x = value_of((uint32_t)(mine >> 32));
     bool in = t < n && (double)t < most;
-    const double r_w = in ? lds.ranked[t] : 0.0;
+    const double w = in ? d.power(x) : 0.0;
     double sum;
-    const double before = above + block_before(r_w, lds, sum);
+    const double before = above + block_before(w, lds, sum);
     if (set.top_p < 1.0f && !light) {
         if (target > 0.0 && (above >= target || above + sum < target)) return false;
         const double of = target > 0.0 ? target : (double)set.top_p * sum;
         in = in && ((t == 0 && above == 0.0) || before < of);
     }
-    if (set.min_p > 0.0f && !light) in = in && d.exponent(lds.ranked_x[t]) >= fmin(log2((double)set.min_p), 0.0);
+    if (set.min_p > 0.0f && !light) in = in && d.exponent(x) >= fmin(log2((double)set.min_p), 0.0);
     // (all of them a head of the order: their number says which)
     int kept;
     (void)block_before(in ? 1 : 0, lds, kept);
-    (void)block_before(in ? r_w : 0.0, lds, d.total);
-    if (there) {
-        lds.list_x[by_index] = by_key < kept ? x : -INFINITY;
-        lds.list_at[by_index] = at;
-    }
-    if (there && by_key == kept - 1) {
+    (void)block_before(in ? w : 0.0, lds, d.total);
+    if (t == kept - 1) {
         lds.found_d = (double)x;
-        lds.found_i[0] = at;
+        lds.found_i[0] = (int)~(uint32_t)mine;
+    }
+    // by index: the complements, which mine has in its lower half
+    mine = sorted(lds, t < kept ? mine << 32 | __float_as_uint(x) : 0, kept);
+    if (t < kept) {
+        lds.list_x[t] = __uint_as_float((uint32_t)mine);
+        lds.list_at[t] = (int)~(uint32_t)(mine >> 32);
     }
     __syncthreads();
     if (kept > 0) {
         d.cut = (float)lds.found_d;
         d.cut_at = lds.found_i[0];
     }
-    d.kept = kept;
-    d.n = n;
+    d.kept = d.n = kept;
     __syncthreads();
     return true;
 }
@@ -967,14 +990,14 @@ __device__ __forceinline__ bool long_head(const Row<DT>& row, Lds& lds, Dist& d,
         if (!rank(lds, next, p, n, (double)n, target, above, false)) return false;
     }
     // the tokens of these bins that stay join their segments, each segment's in the order of their indices
-    if ((int)threadIdx.x < n) {
+    const int stay = next.n;
+    if ((int)threadIdx.x < stay) {
         const int t = threadIdx.x;
         auto segment = [&](int i) { return lds.list_at[i] / (kWave * N); };
         const int mine = segment(t);
         if (t == 0 || segment(t - 1) != mine) {
             double s = lds.segment[mine];
-            for (int i = t; i < n && segment(i) == mine; ++i)
-                if (lds.list_x[i] > -INFINITY) s += d.power(lds.list_x[i]);
+            for (int i = t; i < stay && segment(i) == mine; ++i) s += d.power(lds.list_x[i]);
             lds.segment[mine] = s;
         }
     }
@@ -1284,8 +1307,7 @@ template <typename F>
 __device__ __forceinline__ Found<double> pick_listed(Lds& lds, const Dist& d, float u, F f)
 {
     const int t = threadIdx.x, lane = t & (kWave - 1);
-    const float x = t < d.n ? lds.list_x[t] : -INFINITY;
-    const double w = x > -INFINITY ? f(x, lds.list_at[t]) : 0.0;
+    const double w = t < d.n ? f(lds.list_x[t], lds.list_at[t]) : 0.0;
     if (t == 0) {
         lds.found_i[0] = kNone;
         lds.found_i[1] = -1;
