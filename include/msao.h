@@ -877,10 +877,9 @@ double msao_expected_e2e_latency(const msao_latency_model* m);
 #define MSAO_ROUND_KERNEL_VERIFY_JOIN 4   /* up to the first draft that does not stand */
 #define MSAO_ROUND_KERNEL_RESIZE 5
 #define MSAO_ROUND_KERNEL_RESIZE_FILL 6   /* its tables and slots where they are many */
-#define MSAO_ROUND_KERNEL_SHARED 7        /* attention over the shared prefixes */
-#define MSAO_ROUND_KERNEL_OWN 8           /* and over each sequence's own tokens */
-#define MSAO_ROUND_KERNEL_SHARED_JOIN 9
-#define MSAO_NUM_ROUND_KERNELS 10
+#define MSAO_ROUND_KERNEL_SHARED 7        /* attention over shared prefixes and each sequence's own tokens */
+#define MSAO_ROUND_KERNEL_SHARED_JOIN 8
+#define MSAO_NUM_ROUND_KERNELS 9
 msao_status msao_round_kernel_times(msao_ctx* ctx, float* ms);
 
 /* When enabled, every launch is bracketed by a pair of HIP events recorded on

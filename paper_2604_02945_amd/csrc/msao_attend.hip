@@ -165,9 +165,9 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a, int sh)
     return p;
 }
 
-// What a launch attends to: every token of a sequence; the tokens that a group of sequences shares,
-// for the rows of all of them; a sequence's tokens behind those.
-enum : int { kAll = 0, kShared = 1, kOwn = 2 };
+// What a launch attends to: every token of a sequence (kAll); or in its first workgroups the tokens that a group of
+// sequences shares, for the rows of all of them, and in the others a sequence's tokens behind those (kBoth).
+enum : int { kAll = 0, kBoth = 1 };
 
 // The group that sequence s would be in: the last one that begins at it or before it.
 __device__ __forceinline__ int group_at(const PrefixDev& pre, int s)
@@ -178,26 +178,59 @@ __device__ __forceinline__ int group_at(const PrefixDev& pre, int s)
     return uniform(n) - 1;
 }
 
+// A workgroup's place in its part of the launch.
+struct Grid {
+    bool shared;
+    int block, row_tiles, splits, pairs;
+};
 template <int MODE>
-__device__ __forceinline__ Place place_in(const AttendArgs& a, int sh, int& from)
+__device__ __forceinline__ Grid grid_of(const AttendArgs& a)
 {
-    from = 0;
-    if constexpr (MODE == kShared) {
+    if (MODE == kBoth && (int)blockIdx.x < a.pre.blocks)
+        return Grid{true, (int)blockIdx.x, a.pre.row_tiles, a.pre.splits, a.pre.n_groups * a.c.kv_heads};
+    return Grid{false, (int)blockIdx.x - (MODE == kBoth ? a.pre.blocks : 0), a.row_tiles, a.splits, a.c.n_seqs * a.c.kv_heads};
+}
+
+// The tiles of rows that read a part of a prefix lie on one XCD, whose L2 then has the part for all of them: every
+// eighth workgroup is on the same one.
+__device__ __forceinline__ void shared_place(const Grid& grid, int& sh, int& split, int& tile)
+{
+    const int units = grid.pairs * grid.splits, eight = grid.block / (8 * grid.row_tiles), in = grid.block - eight * 8 * grid.row_tiles;
+    const int width = min(8, units - 8 * eight), unit = 8 * eight + in % width;
+    tile = in / width;
+    sh = unit / grid.splits;
+    split = unit - sh * grid.splits;
+}
+
+// What it computes: whose rows, how many, the first token, whether rows see different ones.
+struct Work {
+    Place p;
+    int n_rows, from;
+    bool causal;
+};
+template <int MODE>
+__device__ __forceinline__ Work work_of(const AttendArgs& a, const Grid& grid, int sh)
+{
+    Work w;
+    w.from = 0;
+    if (MODE == kBoth && grid.shared) {
         const int g = sh / a.c.kv_heads;
         const GroupRows r = group_rows(a.pre, a.ch, g);
-        Place p;
-        p.seq = r.first;
-        p.head = sh - g * a.c.kv_heads;
-        p.begin = r.begin;
-        p.n_new = r.first < a.pre.n_seqs ? r.n : 0;
-        p.length = group_tokens(a.pre, capacity(a.c), g);
-        return p;
-    } else {
-        const Place p = place_of(a, sh);
-        if constexpr (MODE == kOwn)
-            from = prefix_of(a.pre, a.ch, capacity(a.c), p.seq, group_at(a.pre, p.seq), Rows{p.begin, p.n_new}, p.length, a.causal);
-        return p;
+        w.p.seq = r.first;
+        w.p.head = sh - g * a.c.kv_heads;
+        w.p.begin = r.begin;
+        w.p.n_new = r.first < a.pre.n_seqs ? r.n : 0;
+        w.p.length = group_tokens(a.pre, capacity(a.c), g);
+        w.n_rows = w.p.length > 0 ? min(w.p.n_new, a.pre.max_rows) * a.group.n : 0;
+        w.causal = false;
+        return w;
     }
+    w.p = place_of(a, sh);
+    w.n_rows = min(w.p.n_new, a.ch.max_new) * a.group.n;
+    w.causal = a.causal;
+    if (MODE == kBoth)
+        w.from = prefix_of(a.pre, a.ch, capacity(a.c), w.p.seq, group_at(a.pre, w.p.seq), Rows{w.p.begin, w.p.n_new}, w.p.length, a.causal);
+    return w;
 }
 
 // Part `split` of the `seen` tokens from `from` on: how many parts there are, whether one is all there is to a
@@ -207,31 +240,24 @@ struct Part {
     int lo, hi, at;
 };
 template <int MODE>
-__device__ __forceinline__ Part part_of(const AttendArgs& a, int seen, int from, int split)
+__device__ __forceinline__ Part part_of(const AttendArgs& a, const Grid& grid, int seen, int from, int split)
 {
     Part t;
-    if constexpr (MODE == kAll) {
-        const int parts = parts_of(seen, a.part_tokens);
-        t.there = split < max(parts, 1);
-        t.alone = parts <= 1;
-        t.lo = split * a.part_tokens;
-        t.hi = min(seen, t.lo + a.part_tokens);
-        t.at = split;
-    } else if constexpr (MODE == kShared) {
-        t.there = split < parts_of(seen, a.part_tokens);
+    if (MODE == kBoth && grid.shared) {
+        t.there = split < parts_of(seen, a.pre.part_tokens);
         t.alone = false;
-        t.lo = split * a.part_tokens;
-        t.hi = min(seen, t.lo + a.part_tokens);
+        t.lo = split * a.pre.part_tokens;
+        t.hi = min(seen, t.lo + a.pre.part_tokens);
         t.at = split;
-    } else {
-        // (the last part has what is more than the caller thought)
-        const int parts = min(parts_of(seen - from, a.part_tokens), a.splits);
-        t.there = split < max(parts, 1);
-        t.alone = parts <= 1 && from == 0;
-        t.lo = from + split * a.part_tokens;
-        t.hi = split >= parts - 1 ? seen : t.lo + a.part_tokens;
-        t.at = a.part_base + split;
+        return t;
     }
+    const int parts = MODE == kBoth ? min(parts_of(seen - from, a.part_tokens), a.splits) : parts_of(seen, a.part_tokens);
+    t.there = split < max(parts, 1);
+    t.alone = parts <= 1 && from == 0;
+    t.lo = from + split * a.part_tokens;
+    // (of a call with prefixes the last part has what is more than the caller thought)
+    t.hi = MODE == kBoth && split >= parts - 1 ? seen : min(seen, t.lo + a.part_tokens);
+    t.at = (MODE == kBoth ? a.part_base : 0) + split;
     return t;
 }
 
@@ -361,16 +387,24 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArg
     const int i16 = lane & 15, c = lane >> 4, rw = wave % RW, tw = wave / RW;
     // neighbouring blocks lie on different XCDs: the parts of a pair start at a place of its own,
     // so that first parts, which every sequence has, are spread; last tiles, which see most, first
-    const int per_pair = a.row_tiles * a.splits, sh = blockIdx.x / per_pair;
-    const int j = (blockIdx.x - sh * per_pair + sh) % per_pair;
-    const int split = j / a.row_tiles, tile = a.row_tiles - 1 - (j - split * a.row_tiles);
-    int from;
-    const Place p = place_in<MODE>(a, sh, from);
-    const int n_rows = call_rows(a, p), r0 = tile * RW * MT * 16;
+    const Grid grid = grid_of<MODE>(a);
+    int sh, split, tile;
+    if (MODE == kBoth && grid.shared) shared_place(grid, sh, split, tile);
+    else {
+        const int per_pair = grid.row_tiles * grid.splits;
+        sh = grid.block / per_pair;
+        const int j = (grid.block - sh * per_pair + sh) % per_pair;
+        split = j / grid.row_tiles;
+        tile = grid.row_tiles - 1 - (j - split * grid.row_tiles);
+    }
+    const Work work = work_of<MODE>(a, grid, sh);
+    const Place& p = work.p;
+    const bool causal = work.causal;
+    const int n_rows = work.n_rows, r0 = tile * RW * MT * 16;
     if (r0 >= n_rows) return;
     const int r_end = min(r0 + RW * MT * 16, n_rows);
-    const int seen = group_sees(p.length, p.n_new, a.group, r_end - 1, a.causal);
-    const Part part = part_of<MODE>(a, seen, from, split);
+    const int seen = group_sees(p.length, p.n_new, a.group, r_end - 1, causal);
+    const Part part = part_of<MODE>(a, grid, seen, work.from, split);
     if (!part.there) return;
     const int lo = part.lo, hi = part.hi;
 
@@ -389,9 +423,9 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArg
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
         const int row = r0 + line0 + 16 * m + i16;
-        last[m] = a.causal ? p.length - p.n_new + a.group.of(row) : p.length - 1;
+        last[m] = causal ? p.length - p.n_new + a.group.of(row) : p.length - 1;
     }
-    const int least = a.causal ? p.length - p.n_new + a.group.of(r0) : p.length - 1;  // of all rows
+    const int least = causal ? p.length - p.n_new + a.group.of(r0) : p.length - 1;  // of all rows
 
     f32x4 o[MT][E];
     float ref[MT], sum[MT];
@@ -501,7 +535,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArg
                 sum[m] += x[m][e];
             }
         }
-        if (!seen_whole && a.causal) {
+        if (!seen_whole && causal) {
             // a value that some rows must not see is 0 times its weight there, and that is NaN
             // for one that is not finite: such values stay out of the product (see below)
             bool any = false;
@@ -720,18 +754,26 @@ __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
     // and values in the caches. 8 prompts of 1,500 tokens 71 us (83 pair by pair, 65 tile by tile),
     // one of 8,000 574 us (665, 543), chunks of 2,048 over 12,288 717 us (746, 780; the
     // clock takes 30 passes to rise, whose first take up to 1,020)
-    const int per_pair = a.row_tiles * a.splits, pairs = a.c.n_seqs * a.c.kv_heads;
-    const int level = min((int)blockIdx.x / (kRowLevel * pairs), per_pair / kRowLevel), in_level = blockIdx.x - level * kRowLevel * pairs;
-    const int width = min(kRowLevel, per_pair - level * kRowLevel), sh = in_level / width;
-    const int j = level * kRowLevel + (in_level - sh * width + sh) % width;
-    const int split = j / a.row_tiles, tile = a.row_tiles - 1 - (j - split * a.row_tiles);
-    int from;
-    const Place p = place_in<MODE>(a, sh, from);
-    const int n_rows = call_rows(a, p), r0 = tile * NW * MT * 16;
+    const Grid grid = grid_of<MODE>(a);
+    const int per_pair = grid.row_tiles * grid.splits, pairs = grid.pairs;
+    int sh, split, tile;
+    if (MODE == kBoth && grid.shared) shared_place(grid, sh, split, tile);
+    else {
+        const int level = min(grid.block / (kRowLevel * pairs), per_pair / kRowLevel), in_level = grid.block - level * kRowLevel * pairs;
+        const int width = min(kRowLevel, per_pair - level * kRowLevel);
+        sh = in_level / width;
+        const int j = level * kRowLevel + (in_level - sh * width + sh) % width;
+        split = j / grid.row_tiles;
+        tile = grid.row_tiles - 1 - (j - split * grid.row_tiles);
+    }
+    const Work work = work_of<MODE>(a, grid, sh);
+    const Place& p = work.p;
+    const bool causal = work.causal;
+    const int n_rows = work.n_rows, r0 = tile * NW * MT * 16;
     if (r0 >= n_rows) return;
     const int r_end = min(r0 + NW * MT * 16, n_rows);
-    const int seen = group_sees(p.length, p.n_new, a.group, r_end - 1, a.causal);
-    const Part part = part_of<MODE>(a, seen, from, split);
+    const int seen = group_sees(p.length, p.n_new, a.group, r_end - 1, causal);
+    const Part part = part_of<MODE>(a, grid, seen, work.from, split);
     if (!part.there) return;
     const int lo = part.lo, hi = part.hi;
 
@@ -757,13 +799,13 @@ __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
         const int row = w0 + 16 * m + i16;
 #pragma unroll
         for (int s = 0; s < KS; ++s) q[m].v[s] = Queries<kBF16, DP>::fetch(a, p, row, n_rows, 4 * s + c) ^ (a.scale < 0.0f ? 0x80008000u : 0u);
-        last[m] = a.causal ? p.length - p.n_new + a.group.of(row) : p.length - 1;
+        last[m] = causal ? p.length - p.n_new + a.group.of(row) : p.length - 1;
     }
-    const int least = a.causal ? p.length - p.n_new + a.group.of(w0) : p.length - 1;
-    const int least_of_all = a.causal ? p.length - p.n_new + a.group.of(r0) : p.length - 1;
+    const int least = causal ? p.length - p.n_new + a.group.of(w0) : p.length - 1;
+    const int least_of_all = causal ? p.length - p.n_new + a.group.of(r0) : p.length - 1;
     if (threadIdx.x == 0) lds_left_out = 0;
     // tokens that the wavefront's own last row sees
-    const int w_hi = used > 0 ? min(hi, group_sees(p.length, p.n_new, a.group, min(w0 + MT * 16, n_rows) - 1, a.causal)) : lo;
+    const int w_hi = used > 0 ? min(hi, group_sees(p.length, p.n_new, a.group, min(w0 + MT * 16, n_rows) - 1, causal)) : lo;
 
     // the scale's sign is the queries', so that the largest product gives the largest score;
     // above 0, so that what is masked stays at -inf
@@ -817,7 +859,7 @@ __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
         stage_came();
         __syncthreads();
         if (st + 1 < stages) bring(st + 1);
-        if (a.causal && !(lo + ST * st + ST <= hi && lo + ST * st + ST - 1 <= least_of_all)) {
+        if (causal && !(lo + ST * st + ST <= hi && lo + ST * st + ST - 1 <= least_of_all)) {
             // some row does not see all of the stage: what is not finite of its values stays out of
             // the products (see k_attend). Each wavefront looks at the 16 tokens it brought
             if (NW < kTasks || (wave >= ST / 16 && wave < kTasks)) {
@@ -992,14 +1034,14 @@ __global__ __launch_bounds__(kBlock) void k_combine(AttendArgs a, int blocks_per
     constexpr int LP = DP == 96 ? 32 : DP / 4, kGroups = W * kWave / LP, kFly = 4;
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
     const int sh = blockIdx.x / blocks_per;
-    int from;
-    const Place p = place_in<MODE>(a, sh, from);
-    const int n_rows = call_rows(a, p), row = (blockIdx.x - sh * blocks_per) * (kWaves / W) + wave / W;
+    const Work work = work_of<MODE>(a, Grid{}, sh);
+    const Place& p = work.p;
+    const int from = work.from, n_rows = work.n_rows, row = (blockIdx.x - sh * blocks_per) * (kWaves / W) + wave / W;
     if (row >= n_rows) return;  // (W = kWaves: the whole block)
     const int r_end = min(row / a.tile_rows * a.tile_rows + a.tile_rows, n_rows);
     const int seen = group_sees(p.length, p.n_new, a.group, r_end - 1, a.causal);
     int shared = 0, parts = parts_of(seen, a.part_tokens);
-    if constexpr (MODE == kOwn) {  // the prefix' parts, then the own ones, of which there is one at least
+    if constexpr (MODE == kBoth) {  // the prefix' parts, then the own ones, of which there is one at least
         shared = parts_of(from, a.pre.part_tokens);
         parts = min(parts_of(seen - from, a.part_tokens), a.splits);
         if (from > 0) parts = shared + max(parts, 1);
@@ -1028,7 +1070,7 @@ __global__ __launch_bounds__(kBlock) void k_combine(AttendArgs a, int blocks_per
             ml[f] = f32x2{-INFINITY, 0.0f};
             o[f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             if (i < parts) {
-                const int64_t j = MODE == kOwn && i >= shared ? a.part_base + i - shared : i;
+                const int64_t j = MODE == kBoth && i >= shared ? a.part_base + i - shared : i;
                 ml[f] = *(const f32x2*)(a.part_ml + 2 * (j * all + at));
                 if (has) o[f] = *(const f32x4*)(a.part_o + (j * all + at) * a.c.dim + ch);
             }
@@ -1365,13 +1407,14 @@ constexpr int stage_of(int dp) { return dp == 256 ? 32 : 64; }
 template <int DT, int DP, int MODE>
 int attend_rows(const AttendArgs& a, void* st, void* e0, void* e1)
 {
-    const int64_t blocks = pairs(a) * attend_blocks(a).attend;
+    const int64_t blocks = pairs(a) * attend_blocks(a).attend + (MODE == kBoth ? a.pre.blocks : 0);
     if constexpr (DT == kBF16) {
         constexpr int kPerSimd = DP == 64 ? 3 : 2;
         if (a.tile_rows == 64) return enqueue(k_attend_rows<DP, 1, kWaves, stage_of(DP), kPerSimd, MODE>, blocks, st, e0, e1, a);
         if constexpr (DP != 256) {
             if (a.tile_rows == 128) return enqueue(k_attend_rows<DP, 2, kWaves, stage_of(DP), kPerSimd, MODE>, blocks, st, e0, e1, a);
-            if (a.tile_rows == 16) return enqueue(k_attend<DT, DP, 1, 1, MODE>, blocks, st, e0, e1, a);
+            if constexpr (MODE == kAll)
+                if (a.tile_rows == 16) return enqueue(k_attend<DT, DP, 1, 1, MODE>, blocks, st, e0, e1, a);
         }
     } else {
         if (a.tile_rows == 16) return enqueue(k_attend<DT, DP, 1, 1, MODE>, blocks, st, e0, e1, a);
@@ -1416,16 +1459,13 @@ template <int DT, int DP> struct Attend {
     static int go(const AttendArgs& a, void* st, void* e0, void* e1) { return attend_rows<DT, DP, kAll>(a, st, e0, e1); }
 };
 template <int DT, int DP> struct AttendShared {
-    static int go(const AttendArgs& a, void* st, void* e0, void* e1) { return attend_rows<DT, DP, kShared>(a, st, e0, e1); }
-};
-template <int DT, int DP> struct AttendOwn {
-    static int go(const AttendArgs& a, void* st, void* e0, void* e1) { return attend_rows<DT, DP, kOwn>(a, st, e0, e1); }
+    static int go(const AttendArgs& a, void* st, void* e0, void* e1) { return attend_rows<DT, DP, kBoth>(a, st, e0, e1); }
 };
 template <int DT, int DP> struct Combine {
     static int go(const AttendArgs& a, void* st, void* e0, void* e1) { return combine_rows<DT, DP, kAll>(a, st, e0, e1); }
 };
 template <int DT, int DP> struct CombineShared {
-    static int go(const AttendArgs& a, void* st, void* e0, void* e1) { return combine_rows<DT, DP, kOwn>(a, st, e0, e1); }
+    static int go(const AttendArgs& a, void* st, void* e0, void* e1) { return combine_rows<DT, DP, kBoth>(a, st, e0, e1); }
 };
 template <int DT, int DP> struct Weight {
     static int go(const AttendArgs& a, void* st, void* e0, void* e1) { return weight_rows<DT, DP>(a, st, e0, e1); }
@@ -1488,25 +1528,38 @@ void attend_shape(AttendArgs& a)
     }
 }
 
-void shared_shape(AttendArgs& a, AttendArgs& pre, int max_own)
+// Of a call with shared prefixes. The prefixes' workgroups and the others are one launch, so that loads of the
+// ones pass beside products of the others, and their tiles have the same rows, those of the prefixes (128 requests behind
+// four documents of up to 16,384 tokens 142 us, in two launches 221; 32 behind 6,016 tokens 28, 32). Parts for
+// kSharedTarget workgroups if every group had the rows and tokens it can have (the 128 requests 142 us with 1,024, 153
+// with 2,048, 173 with 4,096), of kSharedLeast tokens or more, as each writes and reads 512 bytes a row (the 32 requests
+// with the join 33 us for 256, 38 for 128; small batches 9-10 for 256, 12-14 for 512), float32 of half as many (24 requests of
+// float32 21 us, 25). The other parts as for few rows, by what sequences mostly have.
+constexpr int64_t kSharedTarget = 1024, kSharedLeast = 256, kOwnTarget = 2048;
+void shared_shape(AttendArgs& a, int max_own)
 {
     const int page = 1 << a.c.page_shift;
+    auto up = [](int64_t v, int64_t to) { return (v + to - 1) / to * to; };
     attend_shape(a);
-    AttendArgs own = a;
-    own.c.per_seq = std::min(a.c.per_seq, (max_own + page - 1) / page);
-    attend_shape(own);
-    a.part_tokens = own.part_tokens;
-    a.splits = own.splits;
-    pre = a;
-    pre.c.n_seqs = a.pre.n_groups;
-    pre.c.per_seq = std::min(a.c.per_seq, (a.pre.max_tokens + page - 1) / page);
-    pre.ch.max_new = a.pre.max_rows;
-    pre.causal = pre.add_weight = 0;
-    attend_shape(pre);
-    a.pre.part_tokens = pre.part_tokens;
-    a.pre.splits = pre.splits;
+    PrefixDev& pre = a.pre;
+    const int64_t mine = (int64_t)a.ch.max_new * a.group.n, rows = std::max((int64_t)pre.max_rows * a.group.n, mine);
+    const bool wide = padded_dim(a.c.dim) == 256;
+    if (a.dtype == kBF16) a.tile_rows = rows <= 64 || wide ? 64 : 128;
+    else a.tile_rows = rows <= 16 ? 16 : rows <= 32 || wide ? 32 : 64;
+    a.row_tiles = (int)((mine + a.tile_rows - 1) / a.tile_rows);
+    pre.row_tiles = (int)(((int64_t)pre.max_rows * a.group.n + a.tile_rows - 1) / a.tile_rows);
+    const int64_t tiles = std::min<int64_t>((int64_t)pre.n_groups * a.c.kv_heads * pre.row_tiles, (int64_t)1 << 30);
+    // (and of either no more than kMostParts tiles have: the workspace holds each part of every row)
+    const int64_t all_tiles = ((int64_t)a.ch.n_rows * a.group.n + a.tile_rows - 1) / a.tile_rows * a.c.kv_heads;
+    const int64_t least = a.dtype == kBF16 ? kSharedLeast : kSharedLeast / 2, most = pre.max_tokens;
+    const int64_t per = std::max({least, (tiles * most + kSharedTarget - 1) / kSharedTarget, (all_tiles * most + kMostParts - 1) / kMostParts});
+    pre.part_tokens = (int)std::min<int64_t>(up(per, kPartLeast), std::max<int64_t>(up(most, kPartLeast), kPartLeast));
+    pre.splits = std::max(1, parts_of(pre.max_tokens, pre.part_tokens));
     a.part_base = pre.splits;
-    pre.pre = a.pre;
+    const int64_t others = std::min<int64_t>(pairs(a) * a.row_tiles, (int64_t)1 << 30), cap = std::min<int64_t>(capacity(a.c), up(max_own, page));
+    const int64_t mine_per = std::max(std::min<int64_t>((others * cap + kOwnTarget - 1) / kOwnTarget, kPartMost), (others * cap + kMostParts - 1) / kMostParts);
+    a.part_tokens = (int)std::min<int64_t>(std::max<int64_t>(up(mine_per, kPartLeast), kPartLeast), std::max<int64_t>(up(cap, kTile), kTile));
+    a.splits = std::max(1, parts_of((int)cap, a.part_tokens));
 }
 
 AttendBlocks attend_blocks(const AttendArgs& a)
@@ -1536,7 +1589,6 @@ AttendBytes attend_bytes(const AttendArgs& a)
 int launch_attend(const AttendArgs& a, void* st, void* e0, void* e1) { return by_type<Attend>(a, st, e0, e1); }
 
 int launch_shared(const AttendArgs& a, void* st, void* e0, void* e1) { return by_type<AttendShared>(a, st, e0, e1); }
-int launch_own(const AttendArgs& a, void* st, void* e0, void* e1) { return by_type<AttendOwn>(a, st, e0, e1); }
 int launch_shared_join(const AttendArgs& a, void* st, void* e0, void* e1) { return by_type<CombineShared>(a, st, e0, e1); }
 
 int launch_combine(const AttendArgs& a, void* st, void* e0, void* e1)

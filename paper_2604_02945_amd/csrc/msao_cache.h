@@ -151,6 +151,8 @@ struct PrefixDev {
     int32_t max_seqs, max_tokens;
     int32_t max_rows;              // rows (tokens) of a group that its prefix is computed for
     int32_t part_tokens, splits;   // parts of a prefix, and most of them
+    int32_t row_tiles;             // groups of a (group, kv head)'s rows
+    int32_t blocks;                // workgroups over the prefixes, which come before the others
 };
 
 // Rows (tokens) of group g's sequences.
@@ -294,9 +296,8 @@ int launch_resize_fill(const ResizeArgs& a, void* stream, void* ev0, void* ev1);
 int launch_append(const AppendArgs& a, void* stream, void* ev0, void* ev1);
 int launch_attend(const AttendArgs& a, void* stream, void* ev0, void* ev1);
 int launch_combine(const AttendArgs& a, void* stream, void* ev0, void* ev1);
-// A call with shared prefixes: `a` over the prefixes (shared_shape makes it), over the rest, joined.
+// A call with shared prefixes: over the prefixes and the rest, and joined.
 int launch_shared(const AttendArgs& a, void* stream, void* ev0, void* ev1);
-int launch_own(const AttendArgs& a, void* stream, void* ev0, void* ev1);
 int launch_shared_join(const AttendArgs& a, void* stream, void* ev0, void* ev1);
 int launch_weight(const AttendArgs& a, void* stream, void* ev0, void* ev1);
 int launch_weight_join(const AttendArgs& a, void* stream, void* ev0, void* ev1);
@@ -308,9 +309,8 @@ void append_shape(AppendArgs& a);
 void evict_shape(EvictArgs& a);
 // Launch shape of an attention call: fills part_tokens .. row_parts.
 void attend_shape(AttendArgs& a);
-// Of one with shared prefixes: `pre` becomes the call over the prefixes and `a` the one over the rest, of which
-// sequences mostly have max_own tokens.
-void shared_shape(AttendArgs& a, AttendArgs& pre, int max_own);
+// Of one with shared prefixes, beside which sequences mostly have max_own tokens.
+void shared_shape(AttendArgs& a, int max_own);
 // Workgroups that its kernels launch for each (sequence, kv head); 0: no such launch.
 struct AttendBlocks {
     int64_t attend, combine, weight, join;

@@ -179,9 +179,9 @@ CacheDev cache_dev(const msao_kv_cache& c)
 
 ChunkDev chunk_dev(const msao_chunk& ch) { return ChunkDev{ch.start, ch.n_rows, std::min(ch.max_new, ch.n_rows)}; }
 
-// The launch shape and the workspace of an attention call; `pre` of one with shared prefixes.
+// The launch shape and the workspace of an attention call.
 struct AttendPlan {
-    AttendArgs a, pre;
+    AttendArgs a;
     size_t part_o, part_ml, lse2, part_w, total;
 };
 msao_status attend_args(const msao_kv_cache* cache, const msao_chunk* chunk, int heads, uint32_t flags, AttendArgs& a, std::string* err)
@@ -250,10 +250,14 @@ msao_status shared_plan(const msao_kv_cache* cache, const msao_prefix* prefix, c
     a.pre.max_tokens = (int32_t)std::min<int64_t>(prefix->max_tokens, cap);
     a.pre.max_rows = (int32_t)std::min<int64_t>(a.ch.n_rows, (int64_t)std::min(prefix->max_seqs, a.c.n_seqs) * a.ch.max_new);
     const int64_t own = prefix->max_own > 0 ? prefix->max_own : cap - a.pre.max_tokens;
-    shared_shape(a, pl.pre, (int)std::min<int64_t>(std::max<int64_t>(own, 1), std::max<int64_t>(cap, 1)));
-    const AttendBlocks n = attend_blocks(a), m = attend_blocks(pl.pre);
-    MSAO_TRY(check_blocks((int64_t)a.c.n_seqs * a.c.kv_heads, std::max(std::max(n.attend, n.combine), std::max(n.weight, n.join)), err));
-    MSAO_TRY(check_blocks(groups, m.attend, err));
+    shared_shape(a, (int)std::min<int64_t>(std::max<int64_t>(own, 1), std::max<int64_t>(cap, 1)));
+    const AttendBlocks n = attend_blocks(a);
+    const int64_t pairs = (int64_t)a.c.n_seqs * a.c.kv_heads;
+    MSAO_TRY(check_blocks(pairs, std::max(std::max(n.attend, n.combine), std::max(n.weight, n.join)), err));
+    const int64_t each = (int64_t)a.pre.row_tiles * a.pre.splits;
+    MSAO_TRY(check_blocks(groups, each, err));
+    if (a.pre.max_tokens > 0) a.pre.blocks = (int32_t)(groups * each);
+    if (a.pre.blocks + pairs * n.attend > kMaxBlocks) return fail(err, MSAO_ERR_UNSUPPORTED, "more workgroups than one launch takes");
     attend_workspace(pl);
     return MSAO_OK;
 }
@@ -307,7 +311,6 @@ msao_status attend_call(msao_ctx* ctx, const msao_kv_cache& cache, const msao_ch
 int run_append(const void* a, void* s, void* e0, void* e1) { return launch_append(*(const AppendArgs*)a, s, e0, e1); }
 int run_attend(const void* a, void* s, void* e0, void* e1) { return launch_attend(*(const AttendArgs*)a, s, e0, e1); }
 int run_shared(const void* a, void* s, void* e0, void* e1) { return launch_shared(*(const AttendArgs*)a, s, e0, e1); }
-int run_own(const void* a, void* s, void* e0, void* e1) { return launch_own(*(const AttendArgs*)a, s, e0, e1); }
 int run_shared_join(const void* a, void* s, void* e0, void* e1) { return launch_shared_join(*(const AttendArgs*)a, s, e0, e1); }
 int run_combine(const void* a, void* s, void* e0, void* e1) { return launch_combine(*(const AttendArgs*)a, s, e0, e1); }
 int run_weight(const void* a, void* s, void* e0, void* e1) { return launch_weight(*(const AttendArgs*)a, s, e0, e1); }
@@ -476,18 +479,9 @@ msao_status msao_cache_attention_shared(msao_ctx* ctx, const msao_kv_cache* cach
         MSAO_TRY(shared_plan(cache, prefix, chunk, heads, flags, pl, err));
         MSAO_TRY(attend_call(ctx, *cache, *chunk, q, q_stride, scale, out, out_stride, lse, workspace, workspace_bytes, pl, err));
         if (chunk->max_new == 0 || cache->n_seqs == 0) return MSAO_OK;
-        AttendArgs pre = pl.a;  // (with what the call has filled in)
-        pre.c = pl.pre.c;
-        pre.ch = pl.pre.ch;
-        pre.causal = pre.add_weight = 0;
-        pre.part_tokens = pl.pre.part_tokens;
-        pre.splits = pl.pre.splits;
-        pre.row_tiles = pl.pre.row_tiles;
-        pre.tile_rows = pl.pre.tile_rows;
         const AttendArgs& a = pl.a;
         DeviceGuard guard(ctx->device);
-        if (a.pre.max_rows > 0 && a.pre.max_tokens > 0) MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_SHARED, stream, run_shared, &pre));
-        MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_OWN, stream, run_own, &a));
+        MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_SHARED, stream, run_shared, &a));
         MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_SHARED_JOIN, stream, run_shared_join, &a));
         MSAO_TRY(cache_launch(ctx, MSAO_CACHE_KERNEL_WEIGHT, stream, run_weight, &a));
         return cache_launch(ctx, MSAO_CACHE_KERNEL_WEIGHT_JOIN, stream, run_weight_join, &a);

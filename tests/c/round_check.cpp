@@ -53,7 +53,13 @@ int main()
         for (int i = 0, at = 0; i <= groups; ++i) group[i] = wild ? rnd(20) - 5 : (at += rnd(4));
         for (int& t : tokens) t = rnd(300) - 20;
         const ChunkDev ch{start.data(), rows, rnd(6)};
-        PrefixDev pre{group.data(), tokens.data(), groups, seqs, 0, rnd(300), rnd(40), 128, 1};
+        PrefixDev pre{};
+        pre.group = group.data();
+        pre.tokens = tokens.data();
+        pre.n_groups = groups;
+        pre.n_seqs = seqs;
+        pre.max_tokens = rnd(300);
+        pre.max_rows = rnd(40);
         const int cap = 16 * rnd(30);
         for (int g = 0; g < groups; ++g) {
             const GroupRows gr = group_rows(pre, ch, g);

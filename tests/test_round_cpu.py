@@ -146,6 +146,20 @@ def test_workspaces():
         assert f() == INVALID
 
 
+@pytest.mark.parametrize("seqs,rows,new,tokens,max_seqs,own", [(256, 1536, 6, 1 << 19, 256, 0), (256, 1536, 6, 1 << 19, 2, 0), (256, 1536, 6, 0, 256, 0),
+                                                               (64, 4096, 64, 1 << 20, 1, 4096), (2, 8192, 4096, 1 << 20, 2, 64)])
+def test_workspaces_of_wide_tables_are_bounded(seqs, rows, new, tokens, max_seqs, own):
+    """The parts of every row, whatever the table's width: at most 2^14 tiles of prefixes and as many of the rest, of 128 rows
+    of 516 bytes, and as many tiles as there are more than that."""
+    n, L = ctypes.c_size_t(), B.lib()
+    c = cache(n_seqs=seqs, pages_per_seq=1 << 14, table_stride=1 << 14, weight_stride=1 << 20)
+    p = B.MsaoPrefix(FAKE, FAKE, 4, max_seqs, tokens, own)
+    ch = chunk(n_rows=rows, max_new=new)
+    assert L.msao_cache_attention_shared_workspace(B._addr(c), B._addr(p), B._addr(ch), 32, 1, ctypes.byref(n)) == OK, message()
+    tiles = 8 * -(-rows * 4 // 64)
+    assert n.value <= 2 * (2 ** 14 + tiles + seqs * 8) * 128 * 520
+
+
 def test_the_bindings_checks():
     k = torch.zeros(6, 2, 16, 64)
     pages, length = torch.zeros(3, 2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
