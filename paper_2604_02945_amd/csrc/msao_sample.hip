@@ -21,8 +21,8 @@
 //    one reading sums the weights above them in 64 bits and collects the tokens in them, which
 //    are ranked as above. That the head ends there is checked;
 //  - where it does not, or the bins hold too many tokens (equal ones), bins of keys close in on its end.
-// A weight is some 18 instructions of 64 bits (a polynomial of degree 9): a summed row is bound by
-// them, any other one by its reading.
+// A weight is some ten instructions of 64 bits (a table of 256 and a polynomial of degree 3): a summed row is
+// bound by them, any other one by its reading.
 #include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -77,8 +77,8 @@ __device__ __forceinline__ double fma_constant(double a, double b, double c)
 // 2^(d inv) for d of at most 0: 2^n times 2^(k / 256) from a table times a polynomial of degree 3 in the rest, which is
 // within 1/512 of 0: off by (ln 2 / 512)^4 / 24, 1.4e-13 of the value, and by the table's 3.3e-14; equal logits
 // have the weight 1. `least` is -1000 / inv: what lies below it, -inf too, gives 2^-1000. M at a time, so that no
-// step waits for the one before it. An instruction of 64 bits takes eight clocks a wavefront: a polynomial of degree 9
-// without a table takes 1.5 times as long (a scan of 256 rows with sums 40 us).
+// step waits for the one before it. An instruction of 64 bits takes some eight clocks a wavefront: a scan of 256 bf16 rows of
+// 151,936 with sums 38 us, 16 without them (by a polynomial of degree 9 and no table 40).
 constexpr int kTable = 256;
 template <int M>
 __device__ __forceinline__ void exp2_of(const double* table, double (&d)[M], double inv, double least)
@@ -949,10 +949,10 @@ __device__ __forceinline__ bool long_head(const Row<DT>& row, Lds& lds, Dist& d,
         double some = fmax(ceil((goal - p.above) / w), 1.0);
         if (some > 1.0 && p.above + (some - 1.0) * w >= goal) some -= 1.0;
         some = fmin(some, there);
-        next.cut = Keys<DT>::value(lo + (uint32_t)bin);
-        next.cut_at = kNone;
+        const float x0 = Keys<DT>::value(lo + (uint32_t)bin);
+        next.cut_at = x0 == d.cut ? d.cut_at : kNone;  // (all that stay: of the value that d ends in, those that d has)
+        next.cut = x0;
         if (some < there) {
-            const float x0 = next.cut;
             next.cut_at = find_in_order<int>(row, lds, [&](float x, int v) { return x == x0 && d.stays(x, v) ? 1 : 0; }, [&](int) { return (int)some - 1; }).at;
         }
         // the weights of these bins' tokens that stay join their segments
@@ -1256,8 +1256,8 @@ __device__ __forceinline__ Dist solve(const Row<DT>& row, Lds& lds, const Settin
         const Dist before = d;
         d.kept = -1;
         d.summed = false;
-        d.cut_at = kNone;
-        if (!c.all)  // the first of the tokens of that value
+        d.cut_at = c.x == before.cut ? before.cut_at : kNone;  // (all that stay of that value)
+        if (!c.all)  // the first of them
             d.cut_at = find_in_order<int>(row, lds, [&](float x, int v) { return x == c.x && before.stays(x, v) ? 1 : 0; },
                                           [&](int) { return (int)c.n - 1; }).at;
         d.cut = c.x;

@@ -161,6 +161,50 @@ def test_a_draw_reaches_every_token_by_its_weight():
     assert got["token"].tolist() == list(range(8))
 
 
+def families(seed, rows, vocab, dtype):
+    """Rows of every kind of spread: even, two clusters, few values, values far apart and nearly equal, steps of the type,
+    many masked, a heavy token in a flat row."""
+    g = torch.Generator().manual_seed(seed)
+    n = lambda *s: torch.randn(*s, generator=g)  # noqa: E731
+    x = n(rows, vocab)
+    low = torch.finfo(dtype).min
+    for r in range(rows):
+        k = r % 10
+        if k == 1:
+            x[r] = torch.where(torch.rand(vocab, generator=g) < 0.3, x[r] * 0.1, x[r] - 9)
+        elif k == 2:
+            x[r] = torch.randint(0, 5, (vocab,), generator=g) * 0.5
+        elif k == 3:
+            x[r] = x[r] * 10.0 ** torch.randint(-6, 30, (vocab,), generator=g)
+        elif k == 4:
+            x[r] = 1.0 + x[r] * 1e-6
+        elif k == 5:
+            x[r] = torch.rand(vocab, generator=g) * 0.01 - 0.005
+        elif k == 6:
+            x[r, torch.rand(vocab, generator=g) < 0.9] = low
+        elif k == 7:
+            x[r, torch.rand(vocab, generator=g) < 0.9] = -INF
+        elif k == 8:
+            x[r, int(torch.randint(vocab, (1,), generator=g))] = 11.0
+        elif k == 9:
+            x[r] *= 0.3
+    return x.to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [1025, 2049, 6000, 17000, 70001])
+def test_every_spread_with_every_setting(dtype, vocab):
+    rows = 40
+    x = families(vocab, rows, vocab, dtype)
+    g = np.random.default_rng(vocab)
+    f = lambda v: torch.tensor(g.choice(v, rows), dtype=F32)  # noqa: E731
+    k = torch.tensor(g.choice([3, 300, 1000, 1024, 1025, 1500, vocab // 2, vocab - 1], rows), dtype=torch.int32)
+    p, m, t = f([0.05, 0.5, 0.9, 0.99, 0.9999, 1 - 2.0 ** -20]), f([1e-9, 1e-4, 0.01, 0.3]), f([0.1, 0.7, 1.0, 3.0, 100.0])
+    for i, s in enumerate(({"top_k": k}, {"top_p": p}, {"min_p": m}, {"top_k": k, "top_p": p}, {"top_p": p, "min_p": m},
+                           {"top_k": k, "top_p": p, "min_p": m, "temperature": t}, {"top_p": p, "temperature": t}, {"temperature": t})):
+        check(x, uniform(vocab + i, rows), {**none(), **s})
+
+
 def test_outputs_one_by_one_streams_and_repeats():
     import paper_2604_02945_amd as msao
     x, u = device_rows(rows_of(50, 9, 40000, BF16)), uniform(51, 9).to(DEV)
