@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import round_ref as ref
-from test_gpu_sample import device_rows, none, rows_of, settings_of, uniform
+from test_gpu_sample import device_rows, families, none, rows_of, settings_of, uniform
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -77,6 +77,28 @@ def test_confident_rows(dtype, drawn):
     some = check(*args, none(), 6)
     assert max(some) > 1 and min(some) == 0
     check(*args, settings_of(13, 41), 6)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("drawn", [False, True], ids=["greedy", "drawn"])
+@pytest.mark.parametrize("vocab", [1025, 5000, 40001])
+def test_every_spread_with_every_setting(dtype, drawn, vocab):
+    """Drafts of the likeliest, of light and of removed tokens; the rows they were drawn from of the same spread or another."""
+    counts = [6, 4, 6, 1, 5, 6, 6, 6]
+    rows = sum(counts)
+    x = families(vocab, rows, vocab, dtype)
+    y = (x.float() * 0.9).to(dtype) if vocab == 5000 else families(vocab + 1, rows, vocab, dtype)
+    g = np.random.default_rng(vocab)
+    order = torch.argsort(x.double(), dim=1, descending=True, stable=True)
+    tokens = order[torch.arange(rows), torch.from_numpy(g.choice([0, 0, 0, 1, 7, vocab // 2], rows))].roll(1).to(torch.int32)
+    start = torch.tensor(np.concatenate([[0], np.cumsum(counts)]), dtype=torch.int32)
+    length = torch.full((len(counts),), 100, dtype=torch.int32)
+    f = lambda v: torch.tensor(g.choice(v, rows), dtype=F32)  # noqa: E731
+    k = torch.tensor(g.choice([1, 3, 300, 1024, 1025, 1500, vocab // 2, vocab - 1], rows), dtype=torch.int32)
+    p, m, t = f([0.05, 0.5, 0.9, 0.99, 0.9999]), f([1e-9, 1e-4, 0.01, 0.3]), f([0.1, 0.7, 1.0, 3.0, 100.0])
+    for i, s in enumerate(({}, {"top_k": k}, {"top_p": p}, {"min_p": m, "temperature": t}, {"top_k": k, "top_p": p},
+                           {"top_k": k, "top_p": p, "min_p": m, "temperature": t})):
+        check(x, y if drawn else None, tokens, start, length, uniform(vocab + i, rows) ** 2, uniform(vocab + i + 10, rows), {**none(), **s}, 6)
 
 
 @pytest.mark.parametrize("drawn", [False, True], ids=["greedy", "drawn"])
