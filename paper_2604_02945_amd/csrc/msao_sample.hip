@@ -51,6 +51,8 @@ constexpr int kScanThreads = 256, kScanWaves = kScanThreads / kWave, kScanAhead 
 constexpr double kMagic = 26388279066624.0;  // 1.5 2^44: a number added to it is rounded to 1 / 256, which is its last digit
 constexpr double kLog2e = 1.4426950408889634074;
 constexpr double kLn2 = 0.69314718055994530942;
+constexpr double kSame = 0x1p-42;          // of a weight: no more than this is none (the weights' error; their sums' is less), so that
+                                           // equal distributions have nothing between them, whichever way each was summed
 constexpr int kMostSegments = 4096;        // of a row of kMaxVocab float32 logits
 constexpr int kNone = 0x7FFFFFFF;
 
@@ -1441,7 +1443,9 @@ __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a)
             auto more = [&](float x, float y, int v) {
                 const double w = p.weight(x, v);
                 if (last || certain) return v == draft ? 0.0 : w;
-                return w > 0.0 ? fmax(w * qt - q.weight(y, v) * p.total, 0.0) : 0.0;
+                if (!(w > 0.0)) return 0.0;
+                const double has = w * qt, over = has - q.weight(y, v) * p.total;
+                return over > has * kSame ? over : 0.0;
             };
             auto one = [&](float x, int v) { return more(x, last || certain ? 0.0f : other.value(v), v); };
             auto weight = [&](float x, int v) { return p.weight(x, v); };

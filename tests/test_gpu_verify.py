@@ -117,6 +117,28 @@ def test_drafts_that_equal_the_models_own_all_stand():
     assert check(x, x.clone(), tokens, start, length, ua, u, none(), 8) == [7] * 6
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [40, 1024, 5000, 40000])
+def test_equal_distributions_leave_nothing_between_them(dtype, vocab):
+    """A draft that is no token never stands; where the draft's logits are the row's and a number more, whose steps every one of
+    them keeps, nothing of p is above q, and the token is one of p."""
+    g = torch.Generator().manual_seed(vocab)
+    rows, many = 36, torch.tensor([1, 1.5, 40, 0.25, 3, 0.7]).repeat(6)
+    x = (torch.randint(0, 64, (rows, vocab), generator=g) / 64 + 1.0).to(dtype)
+    x[::2, :5] += 1.0
+    x[::2] = (x[::2].float() * 32).round().div(32).clamp(max=1.96875).to(dtype)
+    y = (x.float() - 0.5).to(dtype)
+    assert torch.equal(y.double() + 0.5, x.double())
+    tokens = torch.full((rows,), -1, dtype=torch.int32)
+    start = torch.arange(0, rows + 1, 6, dtype=torch.int32)
+    length = torch.full((6,), 9, dtype=torch.int32)
+    k = torch.tensor([2, 3, 30, 1024, 1300, vocab - 1], dtype=torch.int32).repeat(6)
+    for i, s in enumerate(({}, {"temperature": many}, {"top_k": k}, {"top_k": k, "temperature": many}, {"top_p": torch.full((rows,), 0.7)})):
+        for first in range(6):  # (each row of a sequence of six is once its first)
+            one = torch.cat([torch.zeros(1), start[1:] - (6 - first)]).clamp(min=0).to(torch.int32)
+            check(x, y, tokens, one, length, uniform(i, rows), uniform(i + 50, rows), {**none(), **s}, 6)
+
+
 @pytest.mark.parametrize("drawn", [False, True], ids=["greedy", "drawn"])
 def test_rows_that_have_no_distribution_and_tokens_that_are_none(drawn):
     x, y, tokens, start, length, ua, u = make(8, [6, 6, 6, 6, 6, 3], 900, BF16, drawn)
