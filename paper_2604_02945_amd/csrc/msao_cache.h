@@ -147,6 +147,7 @@ struct AppendArgs {
 struct PrefixDev {
     const int32_t* group;
     const int32_t* tokens;
+    const int32_t* length;         // the sequences'
     int32_t n_groups, n_seqs;
     int32_t max_seqs, max_tokens;
     int32_t max_rows;              // rows (tokens) of a group that its prefix is computed for
@@ -170,11 +171,14 @@ MSAO_HD GroupRows group_rows(const PrefixDev& pre, const ChunkDev& ch, int g)
 }
 
 // Tokens of its prefix that are computed once: whole half tiles, which lie in one page each. What
-// is left of them the sequences read as their own.
+// is left of them the sequences read as their own. None where the first sequence, whose pages are
+// read, holds fewer.
 MSAO_HD int group_tokens(const PrefixDev& pre, int cap, int g)
 {
-    const int t = entry(pre.tokens, g);
-    return t <= 0 || t > pre.max_tokens || t > cap ? 0 : t & ~15;
+    const int t = entry(pre.tokens, g), lead = clamp_int(entry(pre.group, g), 0, pre.n_seqs);
+    if (t <= 0 || t > pre.max_tokens || t > cap || lead >= pre.n_seqs) return 0;
+    const int whole = t & ~15;
+    return whole <= entry(pre.length, lead) ? whole : 0;
 }
 
 // How many tokens sequence s has from group g: 0 where it is none of the group, or where its rows are not all among

@@ -245,6 +245,7 @@ msao_status shared_plan(const msao_kv_cache* cache, const msao_prefix* prefix, c
     a.pre.group = prefix->group;
     a.pre.tokens = prefix->tokens;
     a.pre.n_groups = prefix->n_groups;
+    a.pre.length = a.c.length;
     a.pre.n_seqs = a.c.n_seqs;
     a.pre.max_seqs = prefix->max_seqs;
     a.pre.max_tokens = (int32_t)std::min<int64_t>(prefix->max_tokens, cap);

@@ -48,14 +48,16 @@ int main()
             }
     for (int trial = 0; trial < 20000; ++trial) {
         const int seqs = 1 + rnd(9), groups = 1 + rnd(4), rows = rnd(30), wild = rnd(3) == 0;
-        std::vector<int> start(seqs + 1), group(groups + 1), tokens(groups);
+        std::vector<int> start(seqs + 1), group(groups + 1), tokens(groups), lengths(seqs);
         for (int i = 0, at = 0; i <= seqs; ++i) start[i] = wild ? rnd(60) - 15 : (at += i ? rnd(4) : 0);
         for (int i = 0, at = 0; i <= groups; ++i) group[i] = wild ? rnd(20) - 5 : (at += rnd(4));
         for (int& t : tokens) t = rnd(300) - 20;
+        for (int& n : lengths) n = rnd(500) - 20;
         const ChunkDev ch{start.data(), rows, rnd(6)};
         PrefixDev pre{};
         pre.group = group.data();
         pre.tokens = tokens.data();
+        pre.length = lengths.data();
         pre.n_groups = groups;
         pre.n_seqs = seqs;
         pre.max_tokens = rnd(300);
@@ -66,6 +68,7 @@ int main()
             CHECK(0 <= gr.first && gr.first <= gr.end && gr.end <= seqs && 0 <= gr.begin && gr.n >= 0 && gr.begin + gr.n <= rows);
             const int t = group_tokens(pre, cap, g);
             CHECK(t >= 0 && t % 16 == 0 && t <= cap && t <= pre.max_tokens && (t == 0 || (t <= tokens[g] && tokens[g] < t + 16)));
+            CHECK(t == 0 || (gr.first < seqs && t <= lengths[gr.first]));
         }
         for (int s = 0; s < seqs; ++s)
             for (int g = -1; g <= groups; ++g) {

@@ -97,6 +97,15 @@ def test_sequences_that_cannot_share(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("lead", [0, 1, 95, 96, 97])
+def test_a_first_sequence_that_holds_less_than_the_prefix(dtype, lead):
+    """Nothing is read from it then: a server's first request ended, the others go on."""
+    lengths, new = [lead, 200, 150, 99, 0, 120, 130], [min(lead, 1), 4, 1, 2, 0, 1, 3]
+    for causal in (True, False):
+        check(share(Case(6, lengths, new, 6, 2, 64, 32, dtype), [0, 5, 7], [96, 96]), [0, 5, 7], [96, 96], causal)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
 def test_bounds_that_are_too_small(dtype):
     """More sequences, tokens, own tokens than the host said: the same results."""
     lengths, new = [400, 390, 500, 333, 700, 340], [2, 1, 6, 3, 5, 1]
