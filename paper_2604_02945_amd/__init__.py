@@ -2,8 +2,9 @@
 (Sec. 4.1, with the MAS-guided selection and compaction it drives) and of the
 decoding-side pieces of its speculative offloading (Sec. 4.2): the draft
 model's confidence on the GPU, Algorithm 1's threshold logic on the host, and
-for the model that verifies the drafts its paged key-value cache: append,
-attention, eviction (`KvCache`, `msao_cache_*`).
+for the model that verifies the drafts its paged key-value cache: pages, append,
+attention, eviction (`KvCache`, `PagePool`, `SharedPrefix`, `msao_cache_*`), and the draw of
+tokens and verification of drafts on its logits (`msao_sample`, `msao_verify`).
 
 The HIP kernels and the C ABI live in libmsao.so (sources in csrc/, ABI in
 include/msao.h at the repository root); `binding` is a thin ctypes layer over
