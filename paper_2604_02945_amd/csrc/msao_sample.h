@@ -30,7 +30,8 @@ constexpr int64_t kMaxVocab = (int64_t)1 << 20;
 struct ScanDev {
     float* most;               // [rows][shares] the largest logit, NaN for what makes a row have no distribution
     double* sum;               // [rows][segments] the weights' sum relative to the segment's largest logit,
-    float* of;                 // [rows][segments] which this is
+    float* of;                 // [rows][segments] which this is,
+    int32_t* number;           // [rows][segments] and how many of them are above -inf
     int32_t lanes, shares, segments;
     int32_t per, parts;        // segments of a workgroup; workgroups of a row (0: rows are not read first)
 };
@@ -38,10 +39,11 @@ struct RowScan {
     float* most;
     double* sum;
     float* of;
+    int32_t* number;
 };
 MSAO_HD RowScan scan_of(const ScanDev& s, int64_t row)
 {
-    return RowScan{s.most + row * s.shares, s.sum + row * s.segments, s.of + row * s.segments};
+    return RowScan{s.most + row * s.shares, s.sum + row * s.segments, s.of + row * s.segments, s.number + row * s.segments};
 }
 void scan_shape(ScanDev& d, int64_t rows, int64_t vocab, int dtype);
 

@@ -10,7 +10,7 @@
 //
 // k_scan reads the rows, many workgroups a row, and leaves for each segment (a wavefront's 64 loads
 // of 16 bytes) the largest logit, the largest of each share of it (1, 4 or 16 loads), and where every
-// token may stay the sum of the weights relative to the segment's largest. Then one workgroup of 1,024
+// token may stay the sum of the weights relative to the segment's largest and their number. Then one workgroup of 1,024
 // threads has a row (k_sample, k_verify):
 //  - without top_k, top_p and min_p the segments' sums say in which one the token lies;
 //  - the head of the order is mostly short. The j-th largest of the shares' maxima is a bound
@@ -306,6 +306,9 @@ __device__ __forceinline__ void scan_segments(const double* table, const Row<DT>
             m = join(m, __shfl_xor(m, 32));
             // (the largest adds 1: what 2^-1000 of the others does not change)
             double sum = 0.0;
+            int number = 0;
+#pragma unroll
+            for (int e = 0; e < N; ++e) number += __popcll(__ballot(c.x[e] > -INFINITY));
             if (m > -INFINITY) {
 #pragma unroll
                 for (int h = 0; h < N; h += 4) {
@@ -320,6 +323,7 @@ __device__ __forceinline__ void scan_segments(const double* table, const Row<DT>
             if (lane == kWave - 1) {
                 scan.sum[s] = sum;
                 scan.of[s] = m;
+                scan.number[s] = number;
             }
         }
     }
@@ -1358,11 +1362,9 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
         token = draw(row, lds, d, a.u[r]);
         kept = d.kept;
         if (a.kept && kept < 0) {  // (every one above -inf)
+            const RowScan scan = scan_of(a.scan, r);
             int n = 0;
-            row.each([&](int, int v, const Chunk<DT>& c) {
-#pragma unroll
-                for (int e = 0; e < Row<DT>::N; ++e) n += d.stays(c.x[e], v + e) ? 1 : 0;
-            });
+            for (int s = threadIdx.x; s < row.segments; s += kThreads) n += scan.number[s];
             (void)block_before(n, lds, kept);
         }
     }

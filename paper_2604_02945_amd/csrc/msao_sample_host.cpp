@@ -82,7 +82,7 @@ msao_status check_rows_count(int64_t rows, std::string* err)
 // Offsets of the arrays that the rows' first reading leaves.
 struct ScanPlan {
     ScanDev scan;
-    size_t most, sum, of, total;
+    size_t most, sum, of, number, total;
 };
 ScanPlan scan_plan(int64_t work, int64_t rows, int64_t vocab, int dtype)
 {
@@ -92,7 +92,8 @@ ScanPlan scan_plan(int64_t work, int64_t rows, int64_t vocab, int dtype)
     pl.sum = 0;
     pl.most = pl.sum + align_up((size_t)rows * (size_t)pl.scan.segments * 8, kWsAlign);
     pl.of = pl.most + align_up((size_t)rows * (size_t)pl.scan.shares * 4, kWsAlign);
-    pl.total = pl.of + align_up((size_t)rows * (size_t)pl.scan.segments * 4, kWsAlign);
+    pl.number = pl.of + align_up((size_t)rows * (size_t)pl.scan.segments * 4, kWsAlign);
+    pl.total = pl.number + align_up((size_t)rows * (size_t)pl.scan.segments * 4, kWsAlign);
     return pl;
 }
 ScanDev scan_at(const ScanPlan& pl, uint8_t* ws)
@@ -102,6 +103,7 @@ ScanDev scan_at(const ScanPlan& pl, uint8_t* ws)
         d.sum = (double*)(ws + pl.sum);
         d.most = (float*)(ws + pl.most);
         d.of = (float*)(ws + pl.of);
+        d.number = (int32_t*)(ws + pl.number);
     }
     return d;
 }
