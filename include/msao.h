@@ -7,8 +7,9 @@
  * side of its speculative offloading (Sec. 4.2): the draft model's
  * confidence per generation step on the GPU (Eq. 9-10), on the host the
  * latency model (Eq. 8, 12-14) and Algorithm 1's threshold logic, and for the
- * model that verifies the drafts its paged key-value cache: append, attention,
- * eviction.
+ * model that verifies the drafts its paged key-value cache: pages, append,
+ * attention, eviction, and on its logits the draw of tokens and the
+ * verification of drafts.
  *
  * Paper: "MSAO" (arXiv 2604.02945). Sec. 4.1 defines the probing module:
  * spatial sparsity (Sec. 4.1.1, Eq. 3-4), temporal sparsity (Sec. 4.1.2,
@@ -880,7 +881,8 @@ double msao_expected_e2e_latency(const msao_latency_model* m);
 #define MSAO_ROUND_KERNEL_RESIZE_FILL 6   /* its tables and slots where they are many */
 #define MSAO_ROUND_KERNEL_SHARED 7        /* attention over shared prefixes and each sequence's own tokens */
 #define MSAO_ROUND_KERNEL_SHARED_JOIN 8
-#define MSAO_NUM_ROUND_KERNELS 9
+#define MSAO_ROUND_KERNEL_VERIFY_SUMS 9   /* sums of rows of which many tokens may be drawn */
+#define MSAO_NUM_ROUND_KERNELS 10
 msao_status msao_round_kernel_times(msao_ctx* ctx, float* ms);
 
 /* When enabled, every launch is bracketed by a pair of HIP events recorded on

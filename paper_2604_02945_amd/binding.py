@@ -33,7 +33,8 @@ ATTEND_CAUSAL, ATTEND_WEIGHT = 1, 2
 (CACHE_KERNEL_APPEND, CACHE_KERNEL_ATTEND, CACHE_KERNEL_COMBINE, CACHE_KERNEL_WEIGHT,
  CACHE_KERNEL_WEIGHT_JOIN, CACHE_KERNEL_SELECT, CACHE_KERNEL_MOVE, NUM_CACHE_KERNELS) = 0, 1, 2, 3, 4, 5, 6, 7
 (ROUND_KERNEL_SCAN, ROUND_KERNEL_SAMPLE, ROUND_KERNEL_DISTRIBUTE, ROUND_KERNEL_VERIFY, ROUND_KERNEL_VERIFY_JOIN,
- ROUND_KERNEL_RESIZE, ROUND_KERNEL_RESIZE_FILL, ROUND_KERNEL_SHARED, ROUND_KERNEL_SHARED_JOIN, NUM_ROUND_KERNELS) = range(10)
+ ROUND_KERNEL_RESIZE, ROUND_KERNEL_RESIZE_FILL, ROUND_KERNEL_SHARED, ROUND_KERNEL_SHARED_JOIN, ROUND_KERNEL_VERIFY_SUMS,
+ NUM_ROUND_KERNELS) = range(11)
 
 STATUS = {0: "MSAO_OK", 1: "MSAO_ERR_INVALID_ARG", 2: "MSAO_ERR_ALIGNMENT", 3: "MSAO_ERR_WORKSPACE",
           4: "MSAO_ERR_UNSUPPORTED", 5: "MSAO_ERR_HIP"}

@@ -90,6 +90,7 @@ int launch_scan(const SampleArgs& a, void* stream, void* ev0, void* ev1);
 int launch_verify_scan(const VerifyArgs& a, void* stream, void* ev0, void* ev1);
 int launch_sample(const SampleArgs& a, void* stream, void* ev0, void* ev1);
 int launch_distribute(const VerifyArgs& a, void* stream, void* ev0, void* ev1);
+int launch_verify_sums(const VerifyArgs& a, void* stream, void* ev0, void* ev1);
 int launch_verify(const VerifyArgs& a, void* stream, void* ev0, void* ev1);
 int launch_verify_join(const VerifyArgs& a, void* stream, void* ev0, void* ev1);
 

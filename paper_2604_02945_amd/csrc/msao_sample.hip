@@ -833,6 +833,24 @@ __device__ __forceinline__ bool rank(Lds& lds, Dist& d, const Settings& set, int
     return true;
 }
 
+// With n tokens in lds.packed, among them all that stay in d: these into the list.
+__device__ __forceinline__ void relist(Lds& lds, Dist& d, int n)
+{
+    const int t = threadIdx.x;
+    uint64_t mine = t < n ? lds.packed[t] : 0;
+    const float x = value_of((uint32_t)(mine >> 32));
+    const bool in = t < n && d.stays(x, (int)~(uint32_t)mine);
+    int kept;
+    (void)block_before(in ? 1 : 0, lds, kept);
+    mine = sorted(lds, in ? mine << 32 | __float_as_uint(x) : 0, n);  // (of what is 0 nothing is used)
+    if (t < kept) {
+        lds.list_x[t] = __uint_as_float((uint32_t)mine);
+        lds.list_at[t] = (int)~(uint32_t)(mine >> 32);
+    }
+    d.n = kept;
+    __syncthreads();
+}
+
 // A value's place among the ones between lo and hi of a type's keys: bf16 values differ in the upper half of theirs.
 template <int DT>
 struct Keys {
@@ -1411,6 +1429,118 @@ __device__ __forceinline__ Dist known_of(const Known& k, const double* table)
     return d;
 }
 
+// What is asked of row r of a sequence: whether the draft behind it stands, and of what its token is drawn where it does not.
+struct Answer {
+    Dist p, q;
+    double qt;          // q's whole
+    int draft;          // -1 behind the last row
+    bool last, certain; // the draft was drawn from no distribution
+    bool yes;
+    // what p has more than q, of the last row p itself
+    __device__ __forceinline__ double more(double w, double z, int v) const
+    {
+        if (last || certain) return v == draft ? 0.0 : w;
+        const double has = w * qt, over = has - z * p.total;
+        return over > has * kSame ? over : 0.0;
+    }
+    __device__ __forceinline__ bool alone() const { return last || certain; }
+    // whether so many tokens may be drawn that the row's segments are summed by k_verify_sums
+    __device__ __forceinline__ bool many() const
+    {
+        return !p.none && !yes && p.best < 0 && (p.kept < 0 ? !alone() : p.kept > kList);
+    }
+};
+template <int DT>
+__device__ __forceinline__ Answer answer_of(const VerifyArgs& a, const double* table, const Row<DT>& row, const Row<DT>& other, int r, bool last, bool has_draft)
+{
+    Answer w;
+    w.p = known_of(a.known[r], table);
+    w.q = known_of(a.known[has_draft ? a.ch.n_rows + r : r], table);
+    w.last = last;
+    w.certain = !has_draft || w.q.none;
+    w.qt = w.certain ? 1.0 : w.q.total;
+    w.draft = last ? -1 : a.tokens[r + 1];
+    w.yes = false;
+    if (!w.p.none && w.draft >= 0 && w.draft < a.vocab) {
+        const double ua = a.u_accept[r] > 0.0f ? (double)a.u_accept[r] : 0.0;
+        const double qd = w.certain ? 1.0 : w.q.weight(other.value(w.draft), w.draft);
+        w.yes = ua * qd * w.p.total < w.p.weight(row.value(w.draft), w.draft) * w.qt;
+    }
+    return w;
+}
+// (a row of which more than kList tokens stay, or of which all do and the draft was drawn)
+__device__ __forceinline__ bool may_be_many(const VerifyArgs& a)
+{
+    return a.scan.parts > 0 && (a.draft.base || a.set.top_k || a.set.top_p || a.set.min_p);
+}
+
+// The segments' sums of what the token of a row is drawn from, where many may be: by as many workgroups as read the row first (by the
+// row's own one, 150 of 256 rows of 151,936 bf16 logits with their drafts' 72-100 us).
+template <int DT>
+__global__ __launch_bounds__(kScanThreads) void k_verify_sums(VerifyArgs a)
+{
+    constexpr int N = Chunk<DT>::N, kAhead = 2;
+    __shared__ double table[kTable];
+    fill_table(table);
+    const int item = blockIdx.x / a.scan.parts, part = blockIdx.x - item * a.scan.parts;
+    const int s = item / a.ch.max_new, i = item - s * a.ch.max_new;
+    const Rows rows = seq_rows(a.ch, s);
+    const int n = min(rows.n, a.ch.max_new);
+    if (i >= n) return;
+    const int r = rows.begin + i, lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x >> 6);
+    const bool last = i == n - 1, has_draft = a.draft.base && !last;
+    const Row<DT> row(a.logits, r, a.vocab), other(has_draft ? a.draft : a.logits, r, a.vocab);
+    const Answer w = answer_of(a, table, row, other, r, last, has_draft);
+    if (!w.many()) return;
+    const RowScan scan = scan_of(a.scan, r);
+    const int first = part * a.scan.per, end = min(first + a.scan.per, row.segments);
+#pragma unroll 1
+    for (int s0 = first + wave; s0 < end; s0 += kScanWaves * kAhead) {
+        u32x4 mine[kAhead], its[kAhead];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+            const int chunk = min(s0 + e * kScanWaves, end - 1) * kWave + lane;
+            mine[e] = row.load(chunk);
+            its[e] = w.alone() ? mine[e] : other.load(chunk);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int at = s0 + k * kScanWaves, v = (at * kWave + lane) * N;
+            if (at >= end) break;
+            Chunk<DT> x(mine[k]), y(its[k]);
+            x.end(a.vocab - v);
+            y.end(a.vocab - v);
+            double sum = 0.0;
+#pragma unroll
+            for (int h = 0; h < N; h += 4) {
+                double by[4], to[4], z[4];
+                uint32_t in = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    by[e] = (double)x.x[h + e] - w.p.m;
+                    to[e] = (double)y.x[h + e] - w.q.m;
+                    in |= w.p.stays(x.x[h + e], v + h + e) && by[e] >= w.p.zero ? 1u << e : 0u;
+                    z[e] = 0.0;
+                }
+                if (!in) continue;
+                exp2_of(table, by, w.p.inv, w.p.zero);
+                if (!w.alone()) {
+                    uint32_t q = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) q |= w.q.stays(y.x[h + e], v + h + e) && to[e] >= w.q.zero ? 1u << e : 0u;
+                    exp2_of(table, to, w.q.inv, w.q.zero);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) z[e] = q >> e & 1 ? to[e] : 0.0;
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum += in >> e & 1 ? w.more(by[e], z[e], v + h + e) : 0.0;
+            }
+            sum = wave_scan(sum);
+            if (lane == kWave - 1) scan.sum[at] = sum;
+        }
+    }
+}
+
 // Row i of sequence s: whether its draft stands, and the token that follows it.
 template <int DT>
 __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a)
@@ -1425,33 +1555,20 @@ __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a)
     const int r = rows.begin + i;
     const bool last = i == n - 1, has_draft = a.draft.base && !last;
     const Row<DT> row(a.logits, r, a.vocab), other(has_draft ? a.draft : a.logits, r, a.vocab);
-    Dist p = known_of(a.known[r], scratch.table);
+    Answer w = answer_of(a, scratch.table, row, other, r, last, has_draft);
+    Dist& p = w.p;
     int token = -1;
-    bool yes = false;
     if (!p.none) {
-        const int draft = last ? -1 : a.tokens[r + 1];
-        const Dist q = known_of(a.known[has_draft ? a.ch.n_rows + r : r], scratch.table);
-        const bool certain = !has_draft || q.none;
-        const double qt = certain ? 1.0 : q.total;
-        if (draft >= 0 && draft < a.vocab) {
-            const double ua = a.u_accept[r] > 0.0f ? (double)a.u_accept[r] : 0.0;
-            const double qd = certain ? 1.0 : q.weight(other.value(draft), draft);
-            yes = ua * qd * p.total < p.weight(row.value(draft), draft) * qt;
-        }
-        if (yes) token = draft;
+        if (w.yes) token = w.draft;
         else {
             const float u = a.u[r];
-            // what p has more than q, of the last row p itself
             auto more = [&](float x, float y, int v) {
-                const double w = p.weight(x, v);
-                if (last || certain) return v == draft ? 0.0 : w;
-                if (!(w > 0.0)) return 0.0;
-                const double has = w * qt, over = has - q.weight(y, v) * p.total;
-                return over > has * kSame ? over : 0.0;
+                const double mine = p.weight(x, v);
+                return w.alone() || mine > 0.0 ? w.more(mine, w.alone() ? 0.0 : w.q.weight(y, v), v) : 0.0;
             };
-            auto one = [&](float x, int v) { return more(x, last || certain ? 0.0f : other.value(v), v); };
+            auto one = [&](float x, int v) { return more(x, w.alone() ? 0.0f : other.value(v), v); };
             auto weight = [&](float x, int v) { return p.weight(x, v); };
-            // few tokens are listed again; of more the row is read
+            // few tokens are listed again; of more the row's sums are there, or it is read
             bool listed = false;
             if (p.kept > 0 && p.kept <= kList && p.best < 0) {
                 int m;
@@ -1461,14 +1578,18 @@ __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a)
                     m = collect(row, lds, Shares(scan.most, a.scan.shares), a.scan.lanes, p.cut);
                 }
                 listed = m > 0 && m <= kList;
-                if (listed) (void)rank(lds, p, Settings{1.0f, 1.0f, 0.0f, 0}, m, (double)p.kept, 0.0, 0.0, true);
+                if (listed) relist(lds, p, m);
             }
-            if (p.best >= 0) token = p.best == draft ? -1 : p.best;
+            if (p.best >= 0) token = p.best == w.draft ? -1 : p.best;
             else if (listed) token = pick_listed(lds, p, u, one).at;
             else {
-                if (p.kept < 0 && (last || certain)) {  // every token stays: the segments' sums are known, but for the draft's
+                if (w.many() && may_be_many(a)) {
+                    const RowScan scan = scan_of(a.scan, r);
+                    for (int at = threadIdx.x; at < row.segments; at += kThreads) lds.segment[at] = scan.sum[at];
+                    __syncthreads();
+                } else if (p.kept < 0 && w.alone()) {  // every token stays: the segments' sums are known, but for the draft's
                     spread_sums(row, lds, scan_of(a.scan, r), p);
-                    if (draft >= 0 && draft < a.vocab) sum_again(row, lds, draft / (kWave * Row<DT>::N), one);
+                    if (w.draft >= 0 && w.draft < a.vocab) sum_again(row, lds, w.draft / (kWave * Row<DT>::N), one);
                 } else sum_segments<double>(row, lds, other, more);
                 token = locate<double>(row, lds, one, [&](double t) { return drawn(u, t); }).at;
             }
@@ -1481,7 +1602,7 @@ __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a)
     }
     if (threadIdx.x != 0) return;
     a.row_token[r] = token;
-    a.row_yes[r] = yes ? 1 : 0;
+    a.row_yes[r] = w.yes ? 1 : 0;
     a.row_logprob[r] = token < 0 ? __builtin_nanf("") : logprob_of(row, p, token);
 }
 
@@ -1579,6 +1700,14 @@ int launch_distribute(const VerifyArgs& a, void* st, void* e0, void* e1)
     const int64_t blocks = (int64_t)a.n_seqs * a.ch.max_new * (a.draft.base ? 2 : 1);
     return a.dtype == kBF16 ? enqueue(k_distribute<kBF16>, blocks, kThreads, st, e0, e1, a)
                             : enqueue(k_distribute<kF32>, blocks, kThreads, st, e0, e1, a);
+}
+
+int launch_verify_sums(const VerifyArgs& a, void* st, void* e0, void* e1)
+{
+    if (!a.draft.base && !a.set.top_k && !a.set.top_p && !a.set.min_p) return kNoLaunch;  // (see may_be_many)
+    const int64_t blocks = (int64_t)a.n_seqs * a.ch.max_new * a.scan.parts;
+    return a.dtype == kBF16 ? enqueue(k_verify_sums<kBF16>, blocks, kScanThreads, st, e0, e1, a)
+                            : enqueue(k_verify_sums<kF32>, blocks, kScanThreads, st, e0, e1, a);
 }
 
 int launch_verify(const VerifyArgs& a, void* st, void* e0, void* e1)

@@ -143,6 +143,7 @@ int run_scan(const void* a, void* s, void* e0, void* e1) { return launch_scan(*(
 int run_verify_scan(const void* a, void* s, void* e0, void* e1) { return launch_verify_scan(*(const VerifyArgs*)a, s, e0, e1); }
 int run_sample(const void* a, void* s, void* e0, void* e1) { return launch_sample(*(const SampleArgs*)a, s, e0, e1); }
 int run_distribute(const void* a, void* s, void* e0, void* e1) { return launch_distribute(*(const VerifyArgs*)a, s, e0, e1); }
+int run_verify_sums(const void* a, void* s, void* e0, void* e1) { return launch_verify_sums(*(const VerifyArgs*)a, s, e0, e1); }
 int run_verify(const void* a, void* s, void* e0, void* e1) { return launch_verify(*(const VerifyArgs*)a, s, e0, e1); }
 int run_join(const void* a, void* s, void* e0, void* e1) { return launch_verify_join(*(const VerifyArgs*)a, s, e0, e1); }
 
@@ -260,6 +261,7 @@ msao_status msao_verify(msao_ctx* ctx, const msao_chunk* chunk, int32_t n_seqs, 
         DeviceGuard guard(ctx->device);
         MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_SCAN, stream, run_verify_scan, &a));
         MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_DISTRIBUTE, stream, run_distribute, &a));
+        MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_VERIFY_SUMS, stream, run_verify_sums, &a));
         MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_VERIFY, stream, run_verify, &a));
         return round_launch(ctx, MSAO_ROUND_KERNEL_VERIFY_JOIN, stream, run_join, &a);
     });

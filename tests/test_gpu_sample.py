@@ -205,6 +205,27 @@ def test_every_spread_with_every_setting(dtype, vocab):
         check(x, uniform(vocab + i, rows), {**none(), **s})
 
 
+def test_logits_past_four_gigabytes():
+    """Rows by offsets of 64 bits: the last rows of many are those of a call of their own."""
+    import paper_2604_02945_amd as msao
+    rows, vocab = 15000, 151936
+    x = torch.zeros(rows, vocab, dtype=BF16, device=DEV)
+    x[-6:] = rows_of(80, 6, vocab, BF16).to(DEV)
+    x[:-6, 7::1000] = 20.0
+    u = uniform(81, rows).to(DEV)
+    s = {k: None if v is None else v.repeat(rows // 6).to(DEV) for k, v in settings_of(82, 6).items()}
+    got = msao.msao_sample(x, u, **s)
+    last = {k: None if v is None else v[-6:].clone() for k, v in s.items()}
+    want = msao.msao_sample(x[-6:].clone(), u[-6:].clone(), **last)
+    for k in want:
+        assert torch.equal(got[k][-6:], want[k]), k
+    start = torch.arange(0, rows + 1, 6, dtype=torch.int32, device=DEV)
+    tokens = torch.full((rows,), 7, dtype=torch.int32, device=DEV)
+    got = msao.msao_verify(start, 6, tokens, x, u, u, **s)
+    want = msao.msao_verify(start[:2].clone(), 6, tokens[-6:].clone(), x[-6:].clone(), u[-6:].clone(), u[-6:].clone(), **last)
+    assert torch.equal(got["next"][-6:], want["next"]) and torch.equal(got["accepted"][-1:], want["accepted"])
+
+
 def test_outputs_one_by_one_streams_and_repeats():
     import paper_2604_02945_amd as msao
     x, u = device_rows(rows_of(50, 9, 40000, BF16)), uniform(51, 9).to(DEV)
