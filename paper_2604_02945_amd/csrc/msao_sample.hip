@@ -790,7 +790,7 @@ __device__ __forceinline__ uint64_t sorted(Lds& lds, uint64_t v, int n)
 
 // With n tokens in lds.packed, which are what comes in the order behind others of the weight `above`: which of
 // them stay of a head of `most` tokens, or of the weight `target` (0: top_p of the n), with min_p. They are left in the
-// list. False, and nothing changed, where the head does not end among them. `light`: the head is `most`
+// list. False, and nothing changed but the order of lds.packed, where the head does not end among them. `light`: the head is `most`
 // tokens, whatever top_p and min_p say.
 __device__ __forceinline__ bool rank(Lds& lds, Dist& d, const Settings& set, int n, double most, double target, double above, bool light)
 {
@@ -804,7 +804,12 @@ __device__ __forceinline__ bool rank(Lds& lds, Dist& d, const Settings& set, int
     double sum;
     const double before = above + block_before(w, lds, sum);
     if (set.top_p < 1.0f && !light) {
-        if (target > 0.0 && (above >= target || above + sum < target)) return false;
+        if (target > 0.0 && (above >= target || above + sum < target)) {
+            __syncthreads();
+            lds.packed[t] = mine;
+            __syncthreads();
+            return false;
+        }
         const double of = target > 0.0 ? target : (double)set.top_p * sum;
         in = in && ((t == 0 && above == 0.0) || before < of);
     }
@@ -1250,8 +1255,14 @@ __device__ __forceinline__ Dist solve(const Row<DT>& row, Lds& lds, const Settin
     const double target = (double)set.top_p * whole;
     // (of the shares' maxima, those that 2^-100 of the largest weight and more belong to)
     const float floor = fmaxf(low, fmaxf((float)(d.m - 100.0 / d.inv), kLowest));
+    // below it min_p leaves nothing (and, by the rounding of the bound, above it some)
+    auto lightest = [&] {
+        const float b = (float)(d.m + (log2(fmin((double)set.min_p, 1.0)) - 1e-3) / d.inv);
+        return b - fabsf(b) * 1e-6f;
+    };
     float bound = -INFINITY;
     int n = 0;
+    bool all_of_min_p = false;  // the tokens listed are all that min_p leaves
     if (small) {
         n = collect_all(row, lds);
     } else {
@@ -1262,10 +1273,11 @@ __device__ __forceinline__ Dist solve(const Row<DT>& row, Lds& lds, const Settin
         } else if (sums) {
             attempt = target < (double)kList;  // (no weight is above 1)
             if (attempt) bound = reached_by(lds, shares, kTryHead, floor, m);
-        } else {  // min_p alone: the tokens of that weight, and some below it by the rounding of the bound
-            bound = (float)(d.m + (log2(fmin((double)set.min_p, 1.0)) - 1e-3) / d.inv);
-            bound = bound - fabsf(bound) * 1e-6f;
-        }
+            if (set.min_p > 0.0f && (!attempt || lightest() >= bound)) {
+                bound = lightest();
+                attempt = all_of_min_p = true;
+            }
+        } else bound = lightest();  // min_p alone
         if (attempt) n = collect(row, lds, shares, lanes, bound);
     }
     const bool enough = !by_k || n >= k || !(bound > -INFINITY);  // (or all there are)
@@ -1274,6 +1286,17 @@ __device__ __forceinline__ Dist solve(const Row<DT>& row, Lds& lds, const Settin
         return d;
     }
     __syncthreads();
+    if (!small && sums && set.min_p > 0.0f) {  // what min_p leaves: top_p's head ends in it, or it is all that stays
+        if (!all_of_min_p) n = collect(row, lds, shares, lanes, lightest());
+        if (n > 0 && n <= kList) {
+            Settings alone = set;
+            alone.top_p = 1.0f;
+            if (all_of_min_p || !rank(lds, d, set, n, (double)n, fmax(target, 1e-300), 0.0, false)) (void)rank(lds, d, alone, n, (double)n, 0.0, 0.0, false);
+            d.listed = true;
+            return d;
+        }
+        __syncthreads();
+    }
 
     // a long one
     auto narrow = [&](const Cut& c) {
@@ -1305,6 +1328,10 @@ __device__ __forceinline__ Dist solve(const Row<DT>& row, Lds& lds, const Settin
     if (set.min_p > 0.0f) {  // what it leaves is all that stays, if that weighs less than top_p's head: else it leaves that head
         Dist t = d;
         t.least = fmin(log2((double)set.min_p), 0.0);
+        if (lightest() > t.cut) {  // (so that these can be listed without reading the row)
+            t.cut = lightest();
+            t.cut_at = kNone;
+        }
         weigh_again(row, lds, t);
         if (!(set.top_p < 1.0f) || t.total < goal) return t;
         d.summed = false;
