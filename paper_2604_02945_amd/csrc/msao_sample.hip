@@ -1501,15 +1501,17 @@ __device__ __forceinline__ bool may_be_many(const VerifyArgs& a)
     return a.scan.parts > 0 && (a.draft.base || a.set.top_k || a.set.top_p || a.set.min_p);
 }
 
-// The segments' sums of what the token of a row is drawn from, where many may be: by as many workgroups as read the row first (by the
-// row's own one, 150 of 256 rows of 151,936 bf16 logits with their drafts' 72-100 us).
+// The segments' sums of what the token of a row is drawn from, where many may be: by many workgroups a row, as few rows
+// have them: 256 rows of 151,936 bf16 logits and their drafts' 20 us (by each row's own one 72-100 with k_verify's 16; by as many
+// workgroups as read the rows first 44). Bound by the 64-bit weights of both rows.
+constexpr int64_t kSumsTarget = 8192;
 template <int DT>
-__global__ __launch_bounds__(kScanThreads) void k_verify_sums(VerifyArgs a)
+__global__ __launch_bounds__(kScanThreads) void k_verify_sums(VerifyArgs a, int parts, int per)
 {
     constexpr int N = Chunk<DT>::N, kAhead = 2;
     __shared__ double table[kTable];
     fill_table(table);
-    const int item = blockIdx.x / a.scan.parts, part = blockIdx.x - item * a.scan.parts;
+    const int item = blockIdx.x / parts, part = blockIdx.x - item * parts;
     const int s = item / a.ch.max_new, i = item - s * a.ch.max_new;
     const Rows rows = seq_rows(a.ch, s);
     const int n = min(rows.n, a.ch.max_new);
@@ -1520,7 +1522,7 @@ __global__ __launch_bounds__(kScanThreads) void k_verify_sums(VerifyArgs a)
     const Answer w = answer_of(a, table, row, other, r, last, has_draft);
     if (!w.many()) return;
     const RowScan scan = scan_of(a.scan, r);
-    const int first = part * a.scan.per, end = min(first + a.scan.per, row.segments);
+    const int first = part * per, end = min(first + per, row.segments);
 #pragma unroll 1
     for (int s0 = first + wave; s0 < end; s0 += kScanWaves * kAhead) {
         u32x4 mine[kAhead], its[kAhead];
@@ -1656,14 +1658,14 @@ __global__ __launch_bounds__(256) void k_verify_join(VerifyArgs a)
     if (a.length_out) a.length_out[s] = a.length[s] - (n > 0 ? rows.n - 1 - accepted : 0);
 }
 
-template <typename K, typename A>
-int enqueue(K kernel, int64_t blocks, int threads, void* stream, void* ev0, void* ev1, const A& a)
+template <typename K, typename... A>
+int enqueue(K kernel, int64_t blocks, int threads, void* stream, void* ev0, void* ev1, const A&... a)
 {
     if (blocks <= 0) return kNoLaunch;
     if (ev0 && ev1)
-        hipExtLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), 0, (hipStream_t)stream, (hipEvent_t)ev0, (hipEvent_t)ev1, 0, a);
+        hipExtLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), 0, (hipStream_t)stream, (hipEvent_t)ev0, (hipEvent_t)ev1, 0, a...);
     else
-        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), 0, (hipStream_t)stream, a);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), 0, (hipStream_t)stream, a...);
     return (int)hipGetLastError();
 }
 
@@ -1732,9 +1734,13 @@ int launch_distribute(const VerifyArgs& a, void* st, void* e0, void* e1)
 int launch_verify_sums(const VerifyArgs& a, void* st, void* e0, void* e1)
 {
     if (!a.draft.base && !a.set.top_k && !a.set.top_p && !a.set.min_p) return kNoLaunch;  // (see may_be_many)
-    const int64_t blocks = (int64_t)a.n_seqs * a.ch.max_new * a.scan.parts;
-    return a.dtype == kBF16 ? enqueue(k_verify_sums<kBF16>, blocks, kScanThreads, st, e0, e1, a)
-                            : enqueue(k_verify_sums<kF32>, blocks, kScanThreads, st, e0, e1, a);
+    if (a.scan.parts == 0) return kNoLaunch;
+    const int64_t items = (int64_t)a.n_seqs * a.ch.max_new;
+    const int most = (a.scan.segments + 2 * kScanWaves - 1) / (2 * kScanWaves);
+    const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(most, kSumsTarget / std::max<int64_t>(items, 1)));
+    const int per = (a.scan.segments + parts - 1) / parts;
+    return a.dtype == kBF16 ? enqueue(k_verify_sums<kBF16>, items * parts, kScanThreads, st, e0, e1, a, parts, per)
+                            : enqueue(k_verify_sums<kF32>, items * parts, kScanThreads, st, e0, e1, a, parts, per);
 }
 
 int launch_verify(const VerifyArgs& a, void* st, void* e0, void* e1)
