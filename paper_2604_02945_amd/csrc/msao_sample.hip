@@ -11,7 +11,8 @@
 // k_scan reads the rows, many workgroups a row, and leaves for each segment (a wavefront's 64 loads
 // of 16 bytes) the largest logit, the largest of each share of it (1, 4 or 16 loads), and where every
 // token may stay the sum of the weights relative to the segment's largest and their number. Then one workgroup of 1,024
-// threads has a row (k_sample, k_verify):
+// threads has a row (k_sample; of a verification k_distribute finds the distributions, k_verify_sums the sums of
+// rows of which many tokens may be drawn, k_verify the tokens):
 //  - without top_k, top_p and min_p the segments' sums say in which one the token lies;
 //  - the head of the order is mostly short. The j-th largest of the shares' maxima is a bound
 //    that j tokens at least reach and few more, and only shares whose maximum reaches it are
