@@ -610,7 +610,8 @@ msao_status msao_cache_attention_workspace(const msao_kv_cache* cache, const msa
  * ask about). Group g is the sequences group[g] .. group[g+1]-1 (device [n_groups + 1], ascending), whose first
  * tokens[g] (device [n_groups]) tokens are the same: their tables name pages that hold the same keys and
  * values for them, as a rule the same pages. The first sequence's are read for all (where it holds fewer than
- * tokens[g], nothing is shared). A sequence may be in no group.
+ * tokens[g], nothing is shared). A sequence may be in no group. Of an array that descends anywhere no group shares
+ * anything.
  * max_seqs, max_tokens: the host's bounds on a group's sequences and tokens; a group of more tokens, and what
  * is past max_seqs * max_new rows of a group, is computed as if nothing were shared. max_own: about how many tokens a
  * sequence has beside its group's (0: the capacity less max_tokens); one that has more takes longer. */

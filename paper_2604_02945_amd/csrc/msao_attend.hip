@@ -169,13 +169,25 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a, int sh)
 // sequences shares, for the rows of all of them, and in the others a sequence's tokens behind those (kBoth).
 enum : int { kAll = 0, kBoth = 1 };
 
-// The group that sequence s would be in: the last one that begins at it or before it.
+// Whether the prefixes' groups are a list that ascends.
+__device__ __forceinline__ bool ascending(const PrefixDev& pre)
+{
+    return __ballot(!groups_ascend(pre, threadIdx.x & (kWave - 1), kWave)) == 0;
+}
+
+// The group that sequence s would be in: the last one that begins at it or before it; none of a list that does not ascend.
 __device__ __forceinline__ int group_at(const PrefixDev& pre, int s)
 {
-    const int lane = threadIdx.x & (kWave - 1);
     int n = 0;
-    for (int g = 0; g < pre.n_groups; g += kWave) n += __popcll(__ballot(g + lane < pre.n_groups && pre.group[min(g + lane, pre.n_groups)] <= s));
-    return uniform(n) - 1;
+    bool ascend = true;
+    const int lane = threadIdx.x & (kWave - 1);
+    for (int g = 0; g < pre.n_groups; g += kWave) {
+        const bool in = g + lane < pre.n_groups;
+        const int at = pre.group[min(g + lane, pre.n_groups)], end = pre.group[min(g + lane + 1, pre.n_groups)];
+        n += __popcll(__ballot(in && at <= s));
+        ascend = ascend && __ballot(in && at > end) == 0;
+    }
+    return ascend ? uniform(n) - 1 : -1;
 }
 
 // A workgroup's place in its part of the launch.
@@ -221,7 +233,7 @@ __device__ __forceinline__ Work work_of(const AttendArgs& a, const Grid& grid, i
         w.p.begin = r.begin;
         w.p.n_new = r.first < a.pre.n_seqs ? r.n : 0;
         w.p.length = group_tokens(a.pre, capacity(a.c), g);
-        w.n_rows = w.p.length > 0 ? min(w.p.n_new, a.pre.max_rows) * a.group.n : 0;
+        w.n_rows = ascending(a.pre) && w.p.length > 0 ? min(w.p.n_new, a.pre.max_rows) * a.group.n : 0;
         w.causal = false;
         return w;
     }

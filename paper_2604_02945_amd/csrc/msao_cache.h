@@ -156,6 +156,15 @@ struct PrefixDev {
     int32_t blocks;                // workgroups over the prefixes, which come before the others
 };
 
+// Whether the list ascends, as far as entries lane, lane + lanes, .. say. Of one that descends anywhere nothing is
+// shared: its groups may have sequences in common, and two would write the same rows' parts.
+MSAO_HD bool groups_ascend(const PrefixDev& pre, int lane, int lanes)
+{
+    bool up = true;
+    for (int64_t g = lane; g < pre.n_groups; g += lanes) up = up && entry(pre.group, g) <= entry(pre.group, g + 1);
+    return up;
+}
+
 // Rows (tokens) of group g's sequences.
 struct GroupRows {
     int first, end, begin, n;
