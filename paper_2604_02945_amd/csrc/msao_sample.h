@@ -24,6 +24,19 @@ struct SamplingDev {
 };
 
 constexpr int64_t kMaxVocab = (int64_t)1 << 20;
+constexpr int kRowThreads = 1024;   // of the kernels that have a workgroup a row,
+constexpr int kScanThreads = 256;   // and of those with many workgroups a row
+
+// Workgroups of `threads` threads in launches of fewer than 2^32 threads each, which is what one takes: f(first, how many) for
+// each launch until one does not give 0.
+template <typename F>
+int in_launches(int64_t workgroups, int threads, F f)
+{
+    const int64_t most = (((int64_t)1 << 32) - 1) / threads;
+    int rc = 0;
+    for (int64_t at = 0; at < workgroups && rc == 0; at += most) rc = f(at, workgroups - at < most ? workgroups - at : most);
+    return rc;
+}
 
 // What the rows' first reading leaves, row by row (a verification's drafts' logits behind the others). A segment
 // is 64 loads of 16 bytes, a share `lanes` of them.
@@ -52,6 +65,7 @@ struct SampleArgs {
     SamplingDev set;
     const float* u;
     int32_t rows, vocab, dtype;
+    int32_t first, blocks;     // workgroups of this launch
     int32_t* token;
     float* logprob;
     int32_t* kept;
@@ -70,6 +84,7 @@ struct VerifyArgs {
     SamplingDev set;
     ChunkDev ch;
     int32_t n_seqs, vocab, dtype;
+    int32_t first, blocks;     // workgroups of this launch
     const int32_t* tokens;
     const float* u_accept;
     const float* u;

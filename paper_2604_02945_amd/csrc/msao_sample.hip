@@ -42,13 +42,13 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef __amdgpu_buffer_rsrc_t rsrc_t;
 
 constexpr int kWave = 64;
-constexpr int kThreads = 1024;
+constexpr int kThreads = kRowThreads;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kBins = 2 * kThreads;
 constexpr int kList = kThreads;            // tokens that are ranked in LDS
 constexpr int kTryHead = 256;              // of the shares' maxima, for a head whose length top_p decides
 constexpr int64_t kScanTarget = 2048;      // workgroups of a scan
-constexpr int kScanThreads = 256, kScanWaves = kScanThreads / kWave, kScanAhead = 4;
+constexpr int kScanWaves = kScanThreads / kWave, kScanAhead = 4;
 constexpr double kMagic = 26388279066624.0;  // 1.5 2^44: a number added to it is rounded to 1 / 256, which is its last digit
 constexpr double kLog2e = 1.4426950408889634074;
 constexpr double kLn2 = 0.69314718055994530942;
@@ -352,7 +352,7 @@ __global__ __launch_bounds__(kScanThreads) void k_scan(SampleArgs a)
 template <int DT, int SHARE>
 __global__ __launch_bounds__(kScanThreads) void k_verify_scan(VerifyArgs a)
 {
-    const int item = blockIdx.x / a.scan.parts, part = blockIdx.x - item * a.scan.parts;
+    const int block = a.first + (int)blockIdx.x, item = block / a.scan.parts, part = block - item * a.scan.parts;
     const int pairs = a.n_seqs * a.ch.max_new, which = item >= pairs ? 1 : 0, s = (item - which * pairs) / a.ch.max_new;
     const int i = item - which * pairs - s * a.ch.max_new;
     const Rows rows = seq_rows(a.ch, s);
@@ -1399,7 +1399,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     __shared__ Scratch scratch;
     Lds lds(scratch);
     fill_table(scratch.table);
-    const int r = blockIdx.x;
+    const int r = a.first + (int)blockIdx.x;
     const Row<DT> row(a.logits, r, a.vocab);
     Dist d = solve(row, lds, settings_of(a.set, r), scan_of(a.scan, r), a.scan.lanes);
     int token = -1, kept = 0;
@@ -1427,8 +1427,8 @@ __global__ __launch_bounds__(kThreads) void k_distribute(VerifyArgs a)
     __shared__ Scratch scratch;
     Lds lds(scratch);
     fill_table(scratch.table);
-    const int pairs = a.n_seqs * a.ch.max_new, which = (int)blockIdx.x >= pairs ? 1 : 0;
-    const int s = ((int)blockIdx.x - which * pairs) / a.ch.max_new, i = (int)blockIdx.x - which * pairs - s * a.ch.max_new;
+    const int block = a.first + (int)blockIdx.x, pairs = a.n_seqs * a.ch.max_new, which = block >= pairs ? 1 : 0;
+    const int s = (block - which * pairs) / a.ch.max_new, i = block - which * pairs - s * a.ch.max_new;
     const Rows rows = seq_rows(a.ch, s);
     if (i >= min(rows.n, a.ch.max_new) - which) return;
     const int r = rows.begin + i, at = which * a.ch.n_rows + r;
@@ -1578,7 +1578,7 @@ __global__ __launch_bounds__(kThreads) void k_verify(VerifyArgs a)
     __shared__ Scratch scratch;
     Lds lds(scratch);
     fill_table(scratch.table);
-    const int s = blockIdx.x / a.ch.max_new, i = blockIdx.x - s * a.ch.max_new;
+    const int block = a.first + (int)blockIdx.x, s = block / a.ch.max_new, i = block - s * a.ch.max_new;
     const Rows rows = seq_rows(a.ch, s);
     const int n = min(rows.n, a.ch.max_new);
     if (i >= n) return;
@@ -1701,10 +1701,9 @@ int scan_rows(const SampleArgs& a, void* st, void* e0, void* e1)
 template <int DT>
 int verify_scan_rows(const VerifyArgs& a, void* st, void* e0, void* e1)
 {
-    const int64_t blocks = (int64_t)a.n_seqs * a.ch.max_new * (a.draft.base ? 2 : 1) * a.scan.parts;
-    return a.scan.lanes == 1   ? enqueue(k_verify_scan<DT, 1>, blocks, kScanThreads, st, e0, e1, a)
-           : a.scan.lanes == 4 ? enqueue(k_verify_scan<DT, 4>, blocks, kScanThreads, st, e0, e1, a)
-                               : enqueue(k_verify_scan<DT, 16>, blocks, kScanThreads, st, e0, e1, a);
+    return a.scan.lanes == 1   ? enqueue(k_verify_scan<DT, 1>, a.blocks, kScanThreads, st, e0, e1, a)
+           : a.scan.lanes == 4 ? enqueue(k_verify_scan<DT, 4>, a.blocks, kScanThreads, st, e0, e1, a)
+                               : enqueue(k_verify_scan<DT, 16>, a.blocks, kScanThreads, st, e0, e1, a);
 }
 
 }  // namespace
@@ -1721,15 +1720,14 @@ int launch_verify_scan(const VerifyArgs& a, void* st, void* e0, void* e1)
 
 int launch_sample(const SampleArgs& a, void* st, void* e0, void* e1)
 {
-    return a.dtype == kBF16 ? enqueue(k_sample<kBF16>, a.rows, kThreads, st, e0, e1, a)
-                            : enqueue(k_sample<kF32>, a.rows, kThreads, st, e0, e1, a);
+    return a.dtype == kBF16 ? enqueue(k_sample<kBF16>, a.blocks, kThreads, st, e0, e1, a)
+                            : enqueue(k_sample<kF32>, a.blocks, kThreads, st, e0, e1, a);
 }
 
 int launch_distribute(const VerifyArgs& a, void* st, void* e0, void* e1)
 {
-    const int64_t blocks = (int64_t)a.n_seqs * a.ch.max_new * (a.draft.base ? 2 : 1);
-    return a.dtype == kBF16 ? enqueue(k_distribute<kBF16>, blocks, kThreads, st, e0, e1, a)
-                            : enqueue(k_distribute<kF32>, blocks, kThreads, st, e0, e1, a);
+    return a.dtype == kBF16 ? enqueue(k_distribute<kBF16>, a.blocks, kThreads, st, e0, e1, a)
+                            : enqueue(k_distribute<kF32>, a.blocks, kThreads, st, e0, e1, a);
 }
 
 int launch_verify_sums(const VerifyArgs& a, void* st, void* e0, void* e1)
@@ -1746,9 +1744,8 @@ int launch_verify_sums(const VerifyArgs& a, void* st, void* e0, void* e1)
 
 int launch_verify(const VerifyArgs& a, void* st, void* e0, void* e1)
 {
-    const int64_t blocks = (int64_t)a.n_seqs * a.ch.max_new;
-    return a.dtype == kBF16 ? enqueue(k_verify<kBF16>, blocks, kThreads, st, e0, e1, a)
-                            : enqueue(k_verify<kF32>, blocks, kThreads, st, e0, e1, a);
+    return a.dtype == kBF16 ? enqueue(k_verify<kBF16>, a.blocks, kThreads, st, e0, e1, a)
+                            : enqueue(k_verify<kF32>, a.blocks, kThreads, st, e0, e1, a);
 }
 
 int launch_verify_join(const VerifyArgs& a, void* st, void* e0, void* e1)

@@ -15,7 +15,7 @@ using namespace msao;
 
 namespace {
 
-constexpr int64_t kMaxRows = (1 << 24) - 1;       // workgroups of a launch
+constexpr int64_t kMaxRows = (1 << 24) - 1;
 constexpr int64_t kMaxRowStride = (int64_t)1 << 31;
 
 // A call that the C ABI must not leave by an exception.
@@ -107,11 +107,6 @@ ScanDev scan_at(const ScanPlan& pl, uint8_t* ws)
     }
     return d;
 }
-msao_status check_scan(const ScanPlan& pl, int64_t rows, std::string* err)
-{
-    if (rows > 0 && pl.scan.parts > kMaxRows / rows) return fail(err, MSAO_ERR_UNSUPPORTED, "more workgroups than one launch takes");
-    return MSAO_OK;
-}
 
 // Offsets of a verification's workspace arrays.
 struct VerifyPlan {
@@ -127,10 +122,10 @@ msao_status verify_plan(const msao_chunk* ch, int32_t n_seqs, int64_t vocab, int
     pl.max_new = std::min(ch->max_new, ch->n_rows);
     if ((int64_t)n_seqs * std::max(pl.max_new, 1) > kMaxRows) return fail(err, MSAO_ERR_UNSUPPORTED, "2^24 rows or more");
     const size_t rows = align_up((size_t)ch->n_rows * 4, kWsAlign);
-    // (of the drafts' logits too, whether there are any or not)
+    // (of the drafts' logits too, whether there are any or not; and shaped for more rows than there are where most of the
+    // sequences have none: each adds its workgroups to the launches)
     const int64_t items = 2 * (int64_t)n_seqs * pl.max_new;
-    pl.scan = scan_plan(std::min<int64_t>(items, 2 * (int64_t)ch->n_rows), 2 * (int64_t)ch->n_rows, vocab, dtype);
-    MSAO_TRY(check_scan(pl.scan, items, err));
+    pl.scan = scan_plan(std::max(std::min<int64_t>(items, 2 * (int64_t)ch->n_rows), items >> 13), 2 * (int64_t)ch->n_rows, vocab, dtype);
     pl.token = pl.scan.total;
     pl.logprob = pl.token + rows;
     pl.yes = pl.logprob + rows;
@@ -152,6 +147,17 @@ msao_status round_launch(msao_ctx* ctx, int kernel, void* stream, int (*fn)(cons
     return launched_in(ctx, ctx->round_rec[kernel], (hipStream_t)stream, fn, a);
 }
 
+// A kernel of `workgroups` workgroups of `threads` threads, in as many launches as that takes.
+template <typename A>
+msao_status row_launches(msao_ctx* ctx, int kernel, void* stream, int (*fn)(const void*, void*, void*, void*), A& a, int64_t workgroups, int threads)
+{
+    return (msao_status)in_launches(workgroups, threads, [&](int64_t first, int64_t n) -> int {
+        a.first = (int32_t)first;
+        a.blocks = (int32_t)n;
+        return round_launch(ctx, kernel, stream, fn, &a);
+    });
+}
+
 }  // namespace
 
 extern "C" {
@@ -163,7 +169,6 @@ msao_status msao_sample_workspace(int64_t rows, int64_t vocab, int dtype, size_t
         MSAO_TRY(check_rows_count(rows, &g_err));
         MSAO_TRY(check_vocab(vocab, dtype, &g_err));
         const ScanPlan pl = scan_plan(rows, rows, vocab, dtype);
-        MSAO_TRY(check_scan(pl, rows, &g_err));
         *bytes = pl.total;
         return MSAO_OK;
     });
@@ -185,7 +190,6 @@ msao_status msao_sample(msao_ctx* ctx, const void* logits, int64_t rows, int64_t
         if (rows > 0 && !u) return bad(err, "u is NULL");
         MSAO_TRY(check_words({u, out->token, out->logprob, out->kept}, err));
         const ScanPlan pl = scan_plan(rows, rows, vocab, dtype);
-        MSAO_TRY(check_scan(pl, rows, err));
         MSAO_TRY(check_workspace(workspace, workspace_bytes, pl.total, err));
         if (!ctx) return bad(err, "ctx is NULL");
         if (rows == 0) return MSAO_OK;
@@ -200,7 +204,7 @@ msao_status msao_sample(msao_ctx* ctx, const void* logits, int64_t rows, int64_t
         a.scan = scan_at(pl, (uint8_t*)workspace);
         DeviceGuard guard(ctx->device);
         MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_SCAN, stream, run_scan, &a));
-        return round_launch(ctx, MSAO_ROUND_KERNEL_SAMPLE, stream, run_sample, &a);
+        return row_launches(ctx, MSAO_ROUND_KERNEL_SAMPLE, stream, run_sample, a, rows, kRowThreads);
     });
 }
 
@@ -259,10 +263,11 @@ msao_status msao_verify(msao_ctx* ctx, const msao_chunk* chunk, int32_t n_seqs, 
         a.known = (Known*)(ws + pl.known);
         a.scan = scan_at(pl.scan, ws);
         DeviceGuard guard(ctx->device);
-        MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_SCAN, stream, run_verify_scan, &a));
-        MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_DISTRIBUTE, stream, run_distribute, &a));
+        const int64_t pairs = (int64_t)n_seqs * pl.max_new, both = draft_logits ? 2 * pairs : pairs;
+        MSAO_TRY(row_launches(ctx, MSAO_ROUND_KERNEL_SCAN, stream, run_verify_scan, a, both * a.scan.parts, kScanThreads));
+        MSAO_TRY(row_launches(ctx, MSAO_ROUND_KERNEL_DISTRIBUTE, stream, run_distribute, a, both, kRowThreads));
         MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_VERIFY_SUMS, stream, run_verify_sums, &a));
-        MSAO_TRY(round_launch(ctx, MSAO_ROUND_KERNEL_VERIFY, stream, run_verify, &a));
+        MSAO_TRY(row_launches(ctx, MSAO_ROUND_KERNEL_VERIFY, stream, run_verify, a, pairs, kRowThreads));
         return round_launch(ctx, MSAO_ROUND_KERNEL_VERIFY_JOIN, stream, run_join, &a);
     });
 }
