@@ -255,7 +255,10 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _addr(struct) -> ctypes.c_void_p:
-    return ctypes.cast(ctypes.byref(struct), ctypes.c_void_p)
+    """The struct's address, which keeps it."""
+    p = ctypes.c_void_p(ctypes.addressof(struct))
+    p.struct = struct
+    return p
 
 
 def default_params() -> dict:

@@ -1,8 +1,10 @@
 """How many rows a draw or a verification may have, on the CPU: the launches that they take
 (tests/c/round_launch_check.cpp), and calls up to the stated limits."""
 import ctypes
+import gc
 import os
 import subprocess
+import weakref
 
 import pytest
 
@@ -37,3 +39,12 @@ def test_rows_of_a_verification(seqs, new, rows, draft, vocab):
     n, ch, want = ctypes.c_size_t(), chunk(n_rows=rows, max_new=new), OK if seqs * new < 1 << 24 else UNSUP
     assert B.lib().msao_verify_workspace(B._addr(ch), seqs, vocab, B.BF16, ctypes.byref(n)) == want
     refused(verify(ch=ch, seqs=seqs, draft=draft, vocab=vocab, stride=vocab, dstride=vocab, ws_bytes=1 << 62), want)
+
+
+def test_an_address_keeps_its_struct():
+    """A call's temporary struct is there until the call has ended."""
+    s = chunk()
+    alive, a = weakref.ref(s), B._addr(s)
+    del s
+    gc.collect()
+    assert alive() is not None and a.value == ctypes.addressof(alive())
