@@ -79,6 +79,10 @@ struct Known {
     int32_t cut_at, kept, best, none;
 };
 
+// Place of row r's distribution, or (`which` 1) of the draft's behind it, which lie behind all rows' ones: past 31 bits of
+// more than 2^30 rows.
+MSAO_HD int64_t dist_at(const ChunkDev& ch, int which, int r) { return (int64_t)which * ch.n_rows + r; }
+
 struct VerifyArgs {
     LogitRows logits, draft;   // draft.base NULL: drafts are certain
     SamplingDev set;

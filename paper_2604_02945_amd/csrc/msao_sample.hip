@@ -331,7 +331,7 @@ __device__ __forceinline__ void scan_segments(const double* table, const Row<DT>
 }
 
 template <int DT, int SHARE>
-__device__ __forceinline__ void scan_part(const LogitRows& rows, const ScanDev& scan, const SamplingDev& set, int vocab, int r, int at, int part)
+__device__ __forceinline__ void scan_part(const LogitRows& rows, const ScanDev& scan, const SamplingDev& set, int vocab, int r, int64_t at, int part)
 {
     __shared__ double table[kTable];
     const Row<DT> row(rows, r, vocab);
@@ -358,7 +358,7 @@ __global__ __launch_bounds__(kScanThreads) void k_verify_scan(VerifyArgs a)
     const Rows rows = seq_rows(a.ch, s);
     if (i >= min(rows.n, a.ch.max_new) - which) return;
     const int r = rows.begin + i;
-    scan_part<DT, SHARE>(which ? a.draft : a.logits, a.scan, a.set, a.vocab, r, which * a.ch.n_rows + r, part);
+    scan_part<DT, SHARE>(which ? a.draft : a.logits, a.scan, a.set, a.vocab, r, dist_at(a.ch, which, r), part);
 }
 
 // ---- one row ---------------------------------------------------------------------------
@@ -1431,7 +1431,8 @@ __global__ __launch_bounds__(kThreads) void k_distribute(VerifyArgs a)
     const int s = (block - which * pairs) / a.ch.max_new, i = block - which * pairs - s * a.ch.max_new;
     const Rows rows = seq_rows(a.ch, s);
     if (i >= min(rows.n, a.ch.max_new) - which) return;
-    const int r = rows.begin + i, at = which * a.ch.n_rows + r;
+    const int r = rows.begin + i;
+    const int64_t at = dist_at(a.ch, which, r);
     const Row<DT> row(which ? a.draft : a.logits, r, a.vocab);
     Dist d = solve(row, lds, settings_of(a.set, r), scan_of(a.scan, at), a.scan.lanes);
     if (!d.none && d.kept < 0 && !d.summed) weigh_again(row, lds, d);
@@ -1483,7 +1484,7 @@ __device__ __forceinline__ Answer answer_of(const VerifyArgs& a, const double* t
 {
     Answer w;
     w.p = known_of(a.known[r], table);
-    w.q = known_of(a.known[has_draft ? a.ch.n_rows + r : r], table);
+    w.q = known_of(a.known[dist_at(a.ch, has_draft ? 1 : 0, r)], table);
     w.last = last;
     w.certain = !has_draft || w.q.none;
     w.qt = w.certain ? 1.0 : w.q.total;

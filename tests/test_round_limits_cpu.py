@@ -1,5 +1,5 @@
-"""How many rows a draw or a verification may have, on the CPU: the launches that they take
-(tests/c/round_launch_check.cpp), and calls up to the stated limits."""
+"""How many rows a draw or a verification may have, on the CPU: the launches that they take and the places of their
+distributions (tests/c/round_launch_check.cpp, tests/c/round_places_check.cpp), and calls up to the stated limits."""
 import ctypes
 import gc
 import os
@@ -13,11 +13,12 @@ from test_cache_cpu import FAKE, OK, ROOT, UNSUP, chunk
 from test_round_cpu import refused, sample, verify
 
 
-def test_launches_take_every_workgroup(tmp_path):
-    exe = str(tmp_path / "round_launch_check")
+@pytest.mark.parametrize("name", ["round_launch_check", "round_places_check"])
+def test_launches_and_places(tmp_path, name):
+    exe = str(tmp_path / name)
     subprocess.check_call(["g++", "-std=c++17", "-O2", "-Wall", "-Wextra", "-Werror", "-fsanitize=address,undefined",
                            "-fno-sanitize-recover=all", "-I", os.path.join(ROOT, "paper_2604_02945_amd", "csrc"),
-                           os.path.join(ROOT, "tests", "c", "round_launch_check.cpp"), "-o", exe])
+                           os.path.join(ROOT, "tests", "c", name + ".cpp"), "-o", exe])
     r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0, r.stdout + r.stderr
 
