@@ -667,8 +667,8 @@ typedef struct {
  *   want [n_seqs]: tokens that each sequence is to have, taken into [0, capacity].
  *   held [n_seqs], taken into [0, pages_per_seq]: the first columns of a sequence's table that are
  *     not its own (a shared prefix's): never given back, and none are taken for them.
- *   columns [n_seqs]: how many columns of its table name pages, the held ones among them; read and
- *     updated. NULL: as many as length and held take.
+ *   columns [n_seqs]: how many columns of its table name pages, the held ones among them (fewer
+ *     than held count as held); read and updated. NULL: as many as length and held take.
  *   start [n_seqs + 1]: the chunk that the growth is: sequence s grows by rows start[s] ..
  *     start[s+1] - 1 (one that does not grow has none).
  *   slots, positions [n_rows]: of each such row below n_rows its place in the pool, page *

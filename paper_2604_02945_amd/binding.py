@@ -1183,8 +1183,8 @@ def msao_cache_resize(cache: KvCache, pool: PagePool, want: torch.Tensor, held: 
                       ctx: Optional[Context] = None, stream=None) -> Dict[str, Optional[torch.Tensor]]:
     """Each sequence's length set to want[s] (int32 [n_seqs]) and its table given the pages that these
     tokens take, from the pool or back to it; all of it on the device. held int32 [n_seqs]: the first columns
-    of a table that are not the sequence's own. columns int32 [n_seqs], updated: how many columns name pages
-    (None: as many as the lengths take; pass it where msao_cache_evict shortens sequences). Filled:
+    of a table that are not the sequence's own. columns int32 [n_seqs], updated: how many columns name pages, the held
+    ones at least (None: as many as the lengths take; pass it where msao_cache_evict shortens sequences). Filled:
     start int32 [n_seqs + 1], the chunk that the growth is, and granted uint8 [n_seqs], 0 where the pool has
     too few pages (both allocated when None); slots int64 [rows] and positions int32 [rows] where given: place
     in the pool and in the sequence of each row below start[n_seqs]. Returns them."""

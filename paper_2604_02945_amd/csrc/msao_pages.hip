@@ -81,7 +81,8 @@ __device__ __forceinline__ Sums plan_all(const ResizeArgs& a, ResizePlan* plan, 
             length = clamp_int(a.length[s], 0, cap);
             want = clamp_int(a.want[s], 0, cap);
             const int held = a.held ? clamp_int(a.held[s], 0, a.per_seq) : 0;
-            old = a.columns ? clamp_int(a.columns[s], 0, a.per_seq) : columns_of(a, length, held);
+            // (the held ones are named, whatever `columns` says: no page is taken in the place of one)
+            old = a.columns ? max(clamp_int(a.columns[s], 0, a.per_seq), held) : columns_of(a, length, held);
             need = columns_of(a, want, held);
         }
         const int64_t asks = need > old ? need - old : 0;
