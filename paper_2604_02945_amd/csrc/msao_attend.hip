@@ -543,6 +543,8 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_attend(AttendArg
             const float base = ref[m] == -INFINITY ? 0.0f : ref[m];
 #pragma unroll
             for (int e = 0; e < 4 * NH; ++e) {
+#pragma clang fp contract(off)
+                // (of a rounded score: 0 where that is the reference, however far it is)
                 x[m][e] = __builtin_amdgcn_exp2f(x[m][e] - base);
                 sum[m] += x[m][e];
             }
@@ -748,6 +750,13 @@ __device__ __forceinline__ void load_to_lds(const u32x4& buffer, uint32_t to, in
 }
 __device__ __forceinline__ void stage_came() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
+// A score s scale enters the exponent by one fused s scale - ref, which keeps what ref has lost of it by its rounding, up
+// to 2^-24 of it: past 2^31 the power of that is infinite or 0 for the largest score itself. From kFarScore on a row's scale
+// is the power of 2 below it, whose products are exact: its scores differ by 128 and more where they differ at all, and
+// by half of that they have no weight as well. (A rounded product less ref would be an instruction more for each score.)
+constexpr float kFarScore = 0x1p30f;
+__device__ __forceinline__ bool is_far(float x) { return fabsf(x) >= kFarScore && fabsf(x) < INFINITY; }
+
 constexpr int kRowLevel = 32;
 template <int DP, int MT, int NW, int ST, int WPS, int MODE>
 __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
@@ -823,9 +832,10 @@ __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
     // above 0, so that what is masked stays at -inf
     const float scale = fmaxf(fabsf(a.scale), 1.17549435e-38f);
     f32x4 o[MT][VT];
-    float ref[MT], sum[MT];
+    float ref[MT], sum[MT], by[MT];  // by: the row's scale
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
+        by[m] = scale;
         ref[m] = -INFINITY;
         sum[m] = 0.0f;
 #pragma unroll
@@ -933,12 +943,18 @@ __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
                 float most = x[m][0];
 #pragma unroll
                 for (int e = 1; e < 8; ++e) most = fmaxf(most, x[m][e]);
-                most *= scale;
-                if (__ballot(most > ref[m] + kSlack) != 0) {
+                if (__ballot(most * by[m] > ref[m] + kSlack) != 0) {
                     most = fmaxf(most, __shfl_xor(most, 16));
                     most = fmaxf(most, __shfl_xor(most, 32));
-                    const float up = most > ref[m] + kSlack ? most : ref[m];
-                    const float sc = ref[m] == up ? 1.0f : ref[m] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref[m] - up);
+                    const bool moves = most * by[m] > ref[m] + kSlack;
+                    float up = moves ? most * by[m] : ref[m];
+                    float sc = ref[m] == up ? 1.0f : ref[m] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref[m] - up);
+                    if (__builtin_expect(__ballot(is_far(up) || by[m] != scale) != 0, 0) && moves) {
+                        // (the old reference and the new one in the scale's own units, whichever they are in)
+                        sc = __builtin_amdgcn_exp2f(fminf(ref[m] * (scale / by[m]) - most * scale, 0.0f));
+                        by[m] = is_far(most * scale) ? __uint_as_float(__float_as_uint(scale) & 0x7F800000u) : scale;
+                        up = most * by[m];
+                    }
                     ref[m] = up;
                     sum[m] *= sc;
 #pragma unroll
@@ -949,7 +965,7 @@ __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
                 const float base = ref[m] == -INFINITY ? 0.0f : ref[m];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    x[m][e] = __builtin_amdgcn_exp2f(fmaf(x[m][e], scale, -base));
+                    x[m][e] = __builtin_amdgcn_exp2f(fmaf(x[m][e], by[m], -base));
                     sum[m] += x[m][e];
                 }
 #pragma unroll
@@ -1007,6 +1023,7 @@ __global__ __launch_bounds__(NW * kWave, WPS) void k_attend_rows(AttendArgs a)
     for (int m = 0; m < MT; ++m) {
         sum[m] += __shfl_xor(sum[m], 16);
         sum[m] += __shfl_xor(sum[m], 32);
+        if (by[m] != scale) ref[m] *= scale / by[m];  // (the quotient is exact)
         const int row = w0 + 16 * m + i16;
         if (row >= n_rows) continue;
         const int tok = a.group.of(row), head = p.head * a.group.n + (row - tok * a.group.n);
