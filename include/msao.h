@@ -593,7 +593,8 @@ msao_status msao_cache_append(msao_ctx* ctx, const msao_kv_cache* cache, const m
  * whatever it holds, and a value that is not finite makes its channel infinite or NaN
  * in the other rows that see it, whatever their p. With MSAO_ATTEND_WEIGHT, weight of
  * (s, kv head, j) grows by the sum of p_ij over the chunk's rows and the query heads
- * of the kv head; the order of every sum is fixed: the same call gives the same bits.
+ * of the kv head; a row whose lse is 2^24 ln 2 (1.16e7) or more in size adds none, as in 32 bits
+ * it does not say what p_ij are. The order of every sum is fixed: the same call gives the same bits.
  * For bf16, the p_ij that multiply v are rounded to bf16; sums, lse and weight are
  * not. Workspace from msao_cache_attention_workspace, used only while the call runs on
  * the GPU. A call of 2^24 workgroups or more gives MSAO_ERR_UNSUPPORTED: one takes 16

@@ -1146,10 +1146,15 @@ __global__ __launch_bounds__(kBlock) void k_combine(AttendArgs a, int blocks_per
     }
 }
 
+constexpr float kMostSum = 0x1p24f;  // of a row that gives weight
+__device__ __forceinline__ float weighing(float z) { return fabsf(z) >= kMostSum ? INFINITY : z; }
+
 // The weight that each token receives, once the rows' sums (lse2) are known:
 //   weight_j += sum_i 2^(x_ij - lse2_i).
 // Lane (c, q) sums tokens 4c + r over its rows, and 16 lanes are added at the end. Every
 // token has one wavefront, so no atomics, and the order of the sum is fixed.
+// A row's sum is off by its rounding, 2^-24 of it, and so is the exponent: from 2^24 on nothing is known of x_ij - lse2_i,
+// whose power is anything up to infinite past 2^31. Such rows add nothing, as ones that see nothing.
 //
 // Few rows (k_weight): K streams by, 16 tokens a wavefront, past the queries in LDS. HBM
 // bound; 60 registers leave eight wavefronts on a SIMD, which is what hides the loads (32
@@ -1184,7 +1189,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight(AttendArg
     for (int m = 0; m < MT; ++m) {
         const int row = min(16 * m + i16, n_rows - 1), tok = a.group.of(row), head = p.head * a.group.n + (row - tok * a.group.n);
         z[m] = 16 * m + i16 < n_rows ? a.lse2[(int64_t)(p.begin + tok) * a.heads + head] : INFINITY;
-        if (z[m] == -INFINITY) z[m] = INFINITY;
+        z[m] = weighing(z[m]);
         last[m] = a.causal ? p.length - p.n_new + tok : p.length - 1;
     }
     const int least = a.causal ? p.length - p.n_new : p.length - 1;
@@ -1311,7 +1316,7 @@ __global__ __launch_bounds__(kBlock, waves_per_simd(DP)) void k_weight_rows(Atte
         if (threadIdx.x < kStep) {
             const int row = r0 + threadIdx.x, t = a.group.of(row), head = p.head * a.group.n + (row - t * a.group.n);
             next_z = row < n_rows ? a.lse2[(int64_t)(p.begin + t) * a.heads + head] : INFINITY;
-            if (next_z == -INFINITY) next_z = INFINITY;
+            next_z = weighing(next_z);
             next_last = row >= n_rows ? -1 : a.causal ? p.length - p.n_new + t : p.length - 1;
         }
     };

@@ -86,3 +86,32 @@ def test_the_largest_of_far_scores_has_all_weight(dtype, heads, kv_heads, dim, s
             assert (np.abs(out[i, h].double().cpu().numpy() - want) <= tol * np.abs(want)).all()
         s = value[at[best]] * scale
         assert (np.abs(lse[i].double().cpu().numpy() - s) <= 2.0 ** -21 * abs(s)).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("shared", [False, True], ids=["alone", "shared"])
+@pytest.mark.parametrize("value", [-1e30, 1e30, 1e10, -3e9, 5e8, -1e6, 100.0])
+@pytest.mark.parametrize("heads,kv_heads,dim,new", [(14, 2, 128, NEW), (4, 2, 64, NEW), (4, 2, 64, [60, 20, 1, 70]), (34, 2, 96, [40, 3, 1, 2]), (4, 2, 256, NEW)])
+def test_weights_of_far_scores(dtype, shared, value, heads, kv_heads, dim, new):
+    """A row past 2^24 in base 2 adds nothing; of another the tokens' weights are the 1 / n that they are, times 2 to the
+    power of what lse has lost, 2^-24 of it at most, and of the other roundings of exponents of that size."""
+    case = far_case(dtype, heads, kv_heads, dim, value, new)
+    cache, _, _ = run(case, GROUP, TOKENS, accumulate=True) if shared else alone(case, True)
+    got = cache.weight.double().cpu().numpy() - case.weight.double().numpy()
+    z = case.q[..., 0].double().numpy() * float(torch.tensor(value).to(dtype)) * dim ** -0.5 / np.log(2)
+    far = np.abs(z) >= 2.0 ** 24 * 1.001
+    assert (far | (np.abs(z) < 2.0 ** 24 * 0.999)).all()
+    G = heads // kv_heads
+    for b in range(case.B):
+        for g in range(kv_heads):
+            least, most = np.zeros(case.cap), np.zeros(case.cap)
+            for i in range(case.new[b]):
+                row, n = case.start[b] + i, case.lengths[b] - case.new[b] + i + 1
+                for h in range(g * G, (g + 1) * G):
+                    if far[row, h]:
+                        continue
+                    off = 2.0 ** (4 * 2.0 ** -24 * abs(z[row, h]) + 2.0 ** -10)
+                    least[:n] += 1 / n / off
+                    most[:n] += 1 / n * off
+            # (added in 32 bits to a weight of up to 1)
+            assert (got[b, g] >= least - 2.0 ** -22).all() and (got[b, g] <= most + 2.0 ** -22 * (1 + most)).all()
