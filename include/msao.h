@@ -725,7 +725,8 @@ msao_status msao_cache_kernel_times(msao_ctx* ctx, float* ms);
  *   of these the ones with w_v >= min_p (0 or less, or NaN: all; more than 1 counts as 1) [all].
  * A temperature of 0 or less, or NaN, leaves the first alone [1]. p_v = w_v / W, W the sum of
  * those that stay. A token of logit -inf never stays. A row with a NaN or +inf logit, or with
- * no finite one, has no distribution. Weights and their sums are 64-bit, whatever the logits. */
+ * no finite one, has no distribution. Weights and their sums are 64-bit, whatever the logits; a weight
+ * is within 2^-42 of itself. */
 typedef struct {
     const float* temperature;
     const int32_t* top_k;
@@ -774,7 +775,8 @@ typedef struct {
  * (row i's for the draft in row i + 1), by the same settings; without draft_logits (NULL), or where
  * their row has no distribution, q(d) is 1. In the first row whose draft does not stand a token is
  * drawn from what p has more than q, max(p - q, 0), in the last row of a sequence one from p: as
- * msao_sample draws it, by u. (Where p has nothing more than q, from p.) So the tokens are
+ * msao_sample draws it, by u. (Where p has nothing more than q, from p. 2^-42 of p and less is no
+ * more: of equal distributions nothing is left, whichever way each was summed.) So the tokens are
  * distributed as if each had been drawn from p. A draft outside [0, vocab) does not stand. A row
  * without a distribution ends its sequence with the token -1. u_accept, u: device [n_rows],
  * given random numbers as in msao_sample. Of a sequence with more than max_new rows the first max_new are

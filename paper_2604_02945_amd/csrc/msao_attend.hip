@@ -1564,11 +1564,12 @@ void attend_shape(AttendArgs& a)
 
 // Of a call with shared prefixes. The prefixes' workgroups and the others are one launch, so that loads of the
 // ones pass beside products of the others, and their tiles have the same rows, those of the prefixes (128 requests behind
-// four documents of up to 16,384 tokens 142 us, in two launches 221; 32 behind 6,016 tokens 28, 32). Parts for
-// kSharedTarget workgroups if every group had the rows and tokens it can have (the 128 requests 142 us with 1,024, 153
-// with 2,048, 173 with 4,096), of kSharedLeast tokens or more, as each writes and reads 512 bytes a row (the 32 requests
-// with the join 33 us for 256, 38 for 128; small batches 9-10 for 256, 12-14 for 512), float32 of half as many (24 requests of
-// float32 21 us, 25). The other parts as for few rows, by what sequences mostly have.
+// four documents of up to 16,384 tokens 142 us, in two launches 221, when that was chosen; 32 behind 6,016 tokens 28, 32). Parts
+// for kSharedTarget workgroups if every group had the rows and tokens it can have (the 128 requests with the join 151 us
+// for 1,024, 164 for 2,048, 190 for 4,096), of kSharedLeast tokens or more, as each writes and reads 512 bytes a row (the 32
+// requests with the join 35 us for 256, 40 for 128, 32 for 512; small batches 9-10 for 256, 12-14 for 512), float32 of half as
+// many (24 requests of float32 27 us with the join, 30). The other parts for kOwnTarget workgroups, by what sequences mostly
+// have (the 128 requests 151 us, 142 for 1,024 and 137 for 4,096; the 32 requests 35, 39 and 35).
 constexpr int64_t kSharedTarget = 1024, kSharedLeast = 256, kOwnTarget = 2048;
 void shared_shape(AttendArgs& a, int max_own)
 {

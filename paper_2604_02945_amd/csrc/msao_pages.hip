@@ -9,7 +9,7 @@
 // given back is found again by the next round, and its stack is the one before it.
 //
 // Bound by latency: a few dependent loads. Up to 1,024 sequences and 8,192 rows one workgroup
-// does everything in one launch, with its sums in LDS; beyond that it leaves them in the
+// does everything in one launch, with its plans in LDS; beyond that it leaves them in the
 // workspace, with a copy of the pages taken (the places they leave are given away meanwhile),
 // and a second launch fills tables and slots from many workgroups.
 #include <hip/hip_ext.h>
@@ -151,8 +151,8 @@ __device__ __forceinline__ void give_back(const ResizeArgs& a, const ResizePlan*
         *entry = -1;
         return;
     }
-    // many: a wavefront has a sequence's, kAhead loads on their way (34,000 of 96 sequences by one workgroup 19 us, each found
-    // by itself 33)
+    // many: a wavefront has a sequence's, kAhead loads on their way (34,000 of 96 sequences by one workgroup 12 us, each found
+    // by itself 31; of 4 sequences 21, 19; of one alone 61, 14, as the other wavefronts have none)
     const int lane = from & (kWave - 1);
     for (int s = from / kWave; s < a.n_seqs; s += step / kWave) {
         const ResizePlan p = plan[s];

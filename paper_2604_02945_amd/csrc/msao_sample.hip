@@ -22,8 +22,8 @@
 //    one reading sums the weights above them in 64 bits and collects the tokens in them, which
 //    are ranked as above. That the head ends there is checked;
 //  - where it does not, or the bins hold too many tokens (equal ones), bins of keys close in on its end.
-// A weight is some ten instructions of 64 bits (a table of 256 and a polynomial of degree 3): a summed row is
-// bound by them, any other one by its reading.
+// A weight is some ten instructions of 64 bits (a table of 256 and a polynomial of degree 3), which take two thirds of
+// a summed row's time; any other row is bound by its reading.
 #include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -46,8 +46,11 @@ constexpr int kThreads = kRowThreads;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kBins = 2 * kThreads;
 constexpr int kList = kThreads;            // tokens that are ranked in LDS
-constexpr int kTryHead = 256;              // of the shares' maxima, for a head whose length top_p decides
-constexpr int64_t kScanTarget = 2048;      // workgroups of a scan
+// Of the shares' maxima, for a head whose length top_p decides: 256 rows with mixed settings 112 us in the row kernel, 106
+// with 128 and 117 with 512 (more to rank, for few heads that are longer).
+constexpr int kTryHead = 256;
+// Workgroups of a scan: 64 requests' drafts 37 us, 47 with 1,024, 29 with 4,096; 256 rows 27, 31, 23.
+constexpr int64_t kScanTarget = 2048;
 constexpr int kScanWaves = kScanThreads / kWave, kScanAhead = 4;
 constexpr double kMagic = 26388279066624.0;  // 1.5 2^44: a number added to it is rounded to 1 / 256, which is its last digit
 constexpr double kLog2e = 1.4426950408889634074;
@@ -80,8 +83,9 @@ __device__ __forceinline__ double fma_constant(double a, double b, double c)
 // 2^(d inv) for d of at most 0: 2^n times 2^(k / 256) from a table times a polynomial of degree 3 in the rest, which is
 // within 1/512 of 0: off by (ln 2 / 512)^4 / 24, 1.4e-13 of the value, and by the table's 3.3e-14; equal logits
 // have the weight 1. `least` is -1000 / inv: what lies below it, -inf too, gives 2^-1000. M at a time, so that no
-// step waits for the one before it. An instruction of 64 bits takes some eight clocks a wavefront: a scan of 256 bf16 rows of
-// 151,936 with sums 38 us, 16 without them (by a polynomial of degree 9 and no table 40).
+// step waits for the one before it. A scan of 256 bf16 rows of 151,936 with sums takes 38 us, 16 without them (by a polynomial
+// of degree 9 and no table 40): of 160 float32 rows' 35 us vector instructions are issued for 24, at four clocks a wavefront
+// each, and the table's reads have bank conflicts for 3.
 constexpr int kTable = 256;
 template <int M>
 __device__ __forceinline__ void exp2_of(const double* table, double (&d)[M], double inv, double least)
