@@ -726,7 +726,7 @@ msao_status msao_cache_kernel_times(msao_ctx* ctx, float* ms);
  * A temperature of 0 or less, or NaN, leaves the first alone [1]. p_v = w_v / W, W the sum of
  * those that stay. A token of logit -inf never stays. A row with a NaN or +inf logit, or with
  * no finite one, has no distribution. Weights and their sums are 64-bit, whatever the logits; a weight
- * is within 2^-42 of itself. */
+ * is off by less than 2^-41 of itself. */
 typedef struct {
     const float* temperature;
     const int32_t* top_k;

@@ -275,7 +275,7 @@ struct ResizeArgs {
 };
 // Up to so many sequences and rows one workgroup does everything. Growth and return in one graph, by one workgroup and by two
 // launches each: 64 sequences of 1 row 13.5 us, 16.6; 256 of 32 rows 21.3, 22.9; 1,024 of 1 row 14.9, 20.0; 1,024 of 8
-// rows 22.7, 20.2; past the border 1,024 of 32 rows 70, 47.7, and 2,000 of 4 rows 33.3, 31.1 (1,500 of 1 row 25.1, 30.0).
+// rows 22.7, 20.2; past the border 1,024 of 32 rows 70, 26, and 2,000 of 4 rows 33.3, 31.1 (1,500 of 1 row 25.1, 30.0).
 constexpr int32_t kResizeSeqs = 1024, kResizeRows = 8192;
 MSAO_HD bool resize_in_one(const ResizeArgs& a) { return a.n_seqs <= kResizeSeqs && a.n_rows <= kResizeRows; }
 MSAO_HD int64_t resize_most_taken(const ResizeArgs& a)
